@@ -355,6 +355,183 @@ flock_status mask_components_frames(const float *prob, int32_t n_frames, int32_t
  * bit per pixel. */
 size_t mask_components_frames_workspace(int32_t n_frames, int32_t width, int32_t height, int32_t connectivity);
 
+/*
+ * Per-bird encoder
+ * ----------------
+ * Learned functions of ragged sets of birds (activity classes or weights per
+ * bird, Section 2.3, from models that a user trains) run on the same CSR
+ * batches: the birds of a frame, or the detections of one bird's track, attend
+ * to each other.  The entries below are its operators and their gradients.
+ *
+ * Features are matrices of `dtype` in device memory.  Rows may lie apart: a
+ * stride is the distance between the starts of two rows in elements, so that
+ * queries, keys and values can be slices of one projection.  The heads of a
+ * row are contiguous, head h at h * head_dim.  No output may overlap an input,
+ * except as stated at rotary_frames.
+ */
+#define FLOCK_F32 0
+#define FLOCK_F16 1
+#define FLOCK_BF16 2
+
+/*
+ * layer_norm_rows - layer norm of every row, with an optional residual.
+ *
+ *   h = x, or x + residual rounded to dtype, which is written to sum;
+ *   y = (h - mean) * rstd * weight + bias,
+ *   mean = sum h / width,  rstd = 1 / sqrt(sum (h - mean)^2 / width + eps)
+ * Statistics are taken in 32 bits, the variance from the centred values.
+ *
+ * Arguments:
+ *   dtype          FLOCK_F32, FLOCK_F16 or FLOCK_BF16: x, residual, y, sum.
+ *   x, residual    device in, [rows][width]; residual may be NULL.
+ *   rows, width    rows >= 0, width 1 .. 2^20.
+ *   *_stride       >= 0 for inputs, >= width for outputs.
+ *   weight, bias   device in, float[width], or NULL (1 and 0).
+ *   eps            finite, >= 0.
+ *   y, sum         device out, [rows][width]; sum must be given with residual,
+ *                  and is not used without.  y may be x, and sum residual.
+ *   mean, rstd     device out, float[rows], or NULL: what the backward pass takes.
+ */
+flock_status layer_norm_rows(int32_t dtype, const void *x, int64_t x_stride, const void *residual,
+                             int64_t residual_stride, int32_t rows, int32_t width, const float *weight,
+                             const float *bias, float eps, void *y, int64_t y_stride, void *sum,
+                             int64_t sum_stride, float *mean, float *rstd, void *stream);
+
+/*
+ * layer_norm_rows_backward - gradients of layer_norm_rows.
+ *
+ * With xh = (x - mean) * rstd and g = grad_y * weight, per row
+ *   grad_x = rstd * (g - mean(g) - xh * mean(g * xh)) (+ grad_sum)
+ * and over the rows, in a fixed order,
+ *   grad_weight = sum grad_y * xh,  grad_bias = sum grad_y.
+ *
+ * Arguments:
+ *   grad_y         device in, [rows][width].
+ *   grad_sum       device in, [rows][width], or NULL: the gradient that the
+ *                  kept sum got elsewhere.  grad_x is the gradient of x and of
+ *                  the residual alike.
+ *   x              device in: what was normalised (x, or the kept sum).
+ *   mean, rstd     device in, float[rows], from layer_norm_rows.
+ *   grad_x         device out, [rows][width].
+ *   grad_weight, grad_bias   device out, float[width], or NULL.
+ *   workspace      as for cluster_frames, sized by
+ *                  layer_norm_rows_backward_workspace(...).
+ */
+flock_status layer_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t grad_y_stride,
+                                      const void *grad_sum, int64_t grad_sum_stride, const void *x,
+                                      int64_t x_stride, int32_t rows, int32_t width, const float *weight,
+                                      const float *mean, const float *rstd, void *grad_x,
+                                      int64_t grad_x_stride, float *grad_weight, float *grad_bias,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace layer_norm_rows_backward needs for its column sums. */
+size_t layer_norm_rows_backward_workspace(int32_t rows, int32_t width);
+
+/*
+ * rotary_frames - rotary positions of queries and keys from time, y and x.
+ *
+ * Pair p of a head's dimensions is turned by angle_p = position * freq[p]:
+ * the bird's time for the first n_time pairs, its y in px for the next n_y,
+ * its x in px for the next n_x:
+ *   (a, b) -> (a cos - b sin, a sin + b cos).
+ * With P pairs in all, pair p is dimensions (p, p + P), or (2 p, 2 p + 1) where
+ * interleaved; dimensions from 2 P on are copied.  inverse turns back, which is
+ * the gradient of the turn.  Phases are integer products of position and
+ * frequency (64-bit fractions of a turn), so far birds lose no digits.
+ *
+ * Arguments:
+ *   dtype          FLOCK_F32, FLOCK_F16 or FLOCK_BF16.
+ *   q, k           device in, [total][q_heads][head_dim], [total][k_heads][head_dim].
+ *   q_heads, k_heads   0 .. 256 each (0: that tensor is not used), one at least.
+ *   head_dim       1 .. 256.
+ *   xy             device in, as for cluster_frames; NULL if n_y = n_x = 0.
+ *   time           device in, int32[total]; NULL if n_time = 0.
+ *   freq           host in, double[n_time + n_y + n_x], finite: radians per
+ *                  unit of time, then per px.  Copied during the call.
+ *   n_time, n_y, n_x   >= 0, 1 <= sum, 2 * sum <= head_dim.
+ *   q_out, k_out   device out; may be q and k with the same strides (in place).
+ */
+flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           int32_t total, int32_t q_heads, int32_t k_heads, int32_t head_dim,
+                           const int32_t *xy, const int32_t *time, const double *freq, int32_t n_time,
+                           int32_t n_y, int32_t n_x, int32_t interleaved, int32_t inverse, void *q_out,
+                           int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream);
+
+/*
+ * attention_frames - attention of queries over the keys of their frame.
+ *
+ * For query i and key j of frame f (indices within the frame, n_q queries and
+ * n_k keys), query head h and its kv head h / (q_heads / kv_heads):
+ *   t = scale * q_i . k_j;  with cap > 0: t = cap * tanh(t / cap)
+ *   s = t - slopes[h] * |place_i - place_j|^2          (px^2, with slopes)
+ *   seen: keep[j] != 0, and in causal frames j < prefix[f] or j <= i + n_k - n_q
+ *   out_i = sum over the keys seen of softmax_j(s) v_j;  lse_i = log sum exp(s)
+ * A query that sees no key gets zeros and lse -infinity.  Hidden keys' (keep =
+ * 0) features are not read.  What order alone hides must be finite.
+ * slopes = 1 / (2 sigma^2) weighs keys by the Gaussian that density_frames
+ * adds per bird.  Products take 16-bit factors with 32-bit sums; the softmax
+ * is in 32 bits, its weights rounded to dtype for the product with v.
+ *
+ * Arguments:
+ *   dtype          FLOCK_F16 or FLOCK_BF16.
+ *   q, k, v        device in, [total_q][q_heads][head_dim] and
+ *                  [total_k][kv_heads][head_dim], 16-byte aligned, strides
+ *                  multiples of 8.
+ *   n_frames       frames of both batches.
+ *   q_offsets, k_offsets   device in, int32[n_frames + 1] each; the same array
+ *                  where the birds of a frame attend to each other.
+ *   q_heads, kv_heads      1 .. 256, q_heads a multiple of kv_heads.
+ *   head_dim       8 .. 128, a multiple of 8.
+ *   q_xy, k_xy     device in, int32[total][2], 1/16 px, with slopes.
+ *   slopes         device in, float[q_heads], finite, or NULL.
+ *   keep           device in, uint8[total_k], or NULL (all kept).
+ *   causal         0 or 1.
+ *   prefix         device in, int32[n_frames], or NULL (0); used when causal.
+ *   scale, cap     finite; scale > 0, cap >= 0 (0: none).
+ *   out            device out, [total_q][q_heads][head_dim].
+ *   lse            device out, double[total_q][q_heads], or NULL: what the
+ *                  backward pass takes.
+ *   workspace      as for cluster_frames, sized by
+ *                  attention_frames_workspace(...).
+ */
+flock_status attention_frames(int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, const int32_t *q_offsets,
+                              const int32_t *k_offsets, int32_t n_frames, int32_t total_q, int32_t total_k,
+                              int32_t q_heads, int32_t kv_heads, int32_t head_dim, const int32_t *q_xy,
+                              const int32_t *k_xy, const float *slopes, const uint8_t *keep, int32_t causal,
+                              const int32_t *prefix, float scale, float cap, void *out, int64_t out_stride,
+                              double *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace attention_frames needs for this batch shape (may be 0):
+ * partial results where several workgroups share a query's keys. */
+size_t attention_frames_workspace(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads,
+                                  int32_t kv_heads, int32_t head_dim);
+
+/*
+ * attention_frames_backward - gradients of attention_frames.
+ *
+ * Takes the forward call's arguments with its out and lse, and grad_out
+ * [total_q][q_heads][head_dim]; writes grad_q, grad_k and grad_v (shaped as q,
+ * k and v; the query heads of a kv head are summed), and with slopes
+ * grad_slopes, float[q_heads] or NULL.  Hidden keys and queries without keys
+ * get zeros.  Every sum has a fixed order: no atomics.
+ * workspace: as for cluster_frames, sized by
+ * attention_frames_backward_workspace(...).
+ */
+flock_status attention_frames_backward(
+    int32_t dtype, const void *grad_out, int64_t grad_out_stride, const void *q, int64_t q_stride,
+    const void *k, int64_t k_stride, const void *v, int64_t v_stride, const void *out, int64_t out_stride,
+    const double *lse, const int32_t *q_offsets, const int32_t *k_offsets, int32_t n_frames, int32_t total_q,
+    int32_t total_k, int32_t q_heads, int32_t kv_heads, int32_t head_dim, const int32_t *q_xy,
+    const int32_t *k_xy, const float *slopes, const uint8_t *keep, int32_t causal, const int32_t *prefix,
+    float scale, float cap, void *grad_q, int64_t grad_q_stride, void *grad_k, int64_t grad_k_stride,
+    void *grad_v, int64_t grad_v_stride, float *grad_slopes, void *workspace, size_t workspace_bytes,
+    void *stream);
+
+/* Bytes of workspace attention_frames_backward needs for this batch shape. */
+size_t attention_frames_backward_workspace(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads,
+                                           int32_t kv_heads, int32_t head_dim);
+
 /* Text of the last error on this thread ("" if none); valid until the next
  * library call on this thread. */
 const char *flock_last_error(void);

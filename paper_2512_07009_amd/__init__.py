@@ -15,12 +15,21 @@ kernels behind a C ABI (include/flock.h, libflock.so).  This package is the thin
     near = drinker_proximity_frames(xy, offsets, drinker_segments_quanta, threshold_quanta)
     det = mask_components_frames(prob, threshold, connectivity)
 
+and the operators of per-bird encoders, learned functions of the birds of a
+frame or of a track, with their gradients:
+
+    y, h, mean, rstd = layer_norm_rows(x, weight, bias, eps, residual)
+    q, k = rotary_frames(q, k, xy, RotaryAxes(time=..., y=..., x=...), time)
+    out = attention_frames(q, k, v, offsets, q_xy=xy, slopes=slopes)
+
 ``workloads`` holds the seeded synthetic input generators.
 """
 
-from .binding import (FlockError, cluster_frames, density_frames, drinker_proximity_frames,  # noqa: F401
-                      eps_to_quanta, heatmap_frames, lib, mask_capacity, mask_components_frames,
-                      roi_filter_frames, version)
+from .binding import (FlockError, RotaryAxes, attention_frames, attention_frames_backward,  # noqa: F401
+                      cluster_frames, density_frames, drinker_proximity_frames, eps_to_quanta, heatmap_frames,
+                      layer_norm_rows, layer_norm_rows_backward, lib, mask_capacity, mask_components_frames,
+                      roi_filter_frames, rotary_frames, version)
 
 __all__ = ["cluster_frames", "density_frames", "heatmap_frames", "roi_filter_frames", "drinker_proximity_frames",
-           "mask_components_frames", "mask_capacity", "eps_to_quanta", "lib", "version", "FlockError"]
+           "mask_components_frames", "mask_capacity", "layer_norm_rows", "layer_norm_rows_backward", "RotaryAxes",
+           "rotary_frames", "attention_frames", "attention_frames_backward", "eps_to_quanta", "lib", "version", "FlockError"]

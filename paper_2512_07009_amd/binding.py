@@ -70,6 +70,27 @@ def lib() -> ctypes.CDLL:
         L.mask_components_frames.restype = i32
         L.mask_components_frames_workspace.argtypes = [i32, i32, i32, i32]
         L.mask_components_frames_workspace.restype = sz
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        L.layer_norm_rows.argtypes = [i32, p, i64, p, i64, i32, i32, p, p, f32, p, i64, p, i64, p, p, p]
+        L.layer_norm_rows.restype = i32
+        L.layer_norm_rows_backward.argtypes = [i32, p, i64, p, i64, p, i64, i32, i32, p, p, p, p, i64, p, p, p, sz, p]
+        L.layer_norm_rows_backward.restype = i32
+        L.layer_norm_rows_backward_workspace.argtypes = [i32, i32]
+        L.layer_norm_rows_backward_workspace.restype = sz
+        L.rotary_frames.argtypes = [i32, p, i64, p, i64, i32, i32, i32, i32, p, p, p, i32, i32, i32, i32, i32,
+                                    p, i64, p, i64, p]
+        L.rotary_frames.restype = i32
+        L.attention_frames.argtypes = [i32, p, i64, p, i64, p, i64, p, p, i32, i32, i32, i32, i32, i32, p, p, p, p, i32,
+                                       p, f32, f32, p, i64, p, p, sz, p]
+        L.attention_frames.restype = i32
+        L.attention_frames_workspace.argtypes = [i32, i32, i32, i32, i32, i32]
+        L.attention_frames_workspace.restype = sz
+        L.attention_frames_backward.argtypes = [i32, p, i64, p, i64, p, i64, p, i64, p, i64, p, p, p, i32, i32, i32, i32,
+                                                i32, i32, p, p, p, p, i32, p, f32, f32, p, i64, p, i64, p, i64, p, p,
+                                                sz, p]
+        L.attention_frames_backward.restype = i32
+        L.attention_frames_backward_workspace.argtypes = [i32, i32, i32, i32, i32, i32]
+        L.attention_frames_backward_workspace.restype = sz
         L.flock_last_error.argtypes = []
         L.flock_last_error.restype = ctypes.c_char_p
         L.flock_version.argtypes = []
@@ -313,6 +334,268 @@ def mask_components_frames(prob: torch.Tensor, threshold: float, connectivity: i
           _ptr(out.get("area")), _ptr(out.get("box")), _ptr(out.get("centroid")), _ptr(out.get("xy")),
           _ptr(out.get("score")), _ptr(ws), ws_bytes)
     return out
+
+
+# ---------------------------------------------------------------------------
+# Per-bird encoder
+# ---------------------------------------------------------------------------
+
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _dtype(t):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"features of {t.dtype}: expected float32, float16 or bfloat16")
+    return code
+
+
+def _rows(t, name, like=None):
+    """Stride of a device matrix [rows, width] whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a device matrix with contiguous rows")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name} must have the shape, type and device of its counterpart")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _heads(t, name, rows=None, dtype=None, dev=None):
+    """Stride of a device tensor [birds, heads, head_dim] whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1) or \
+            (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+        raise ValueError(f"{name} must be a device tensor [birds, heads, head_dim] with contiguous rows")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name} holds {t.shape[0]} birds, expected {rows}")
+    if dtype is not None and (t.dtype != dtype or t.device != dev):
+        raise ValueError(f"{name} must have the type and device of the queries")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _vector(t, name, dtype, numel, dev):
+    if t.dtype != dtype or t.device != dev or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name} must be {numel} contiguous {dtype} values on the features' device")
+
+
+def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                    eps: float = 1e-5, residual: torch.Tensor | None = None, out=None, stream=None):
+    """Layer norm of every row of x [N, width] (float32, float16 or bfloat16),
+    or of x + residual, with float32 weight and bias.
+
+    Returns (y, h, mean, rstd): h is what was normalised (x itself, or the sum
+    in x's type), and h, mean and rstd (float32 [N]) are what
+    layer_norm_rows_backward takes.
+    out: optional (y, h, mean, rstd) tensors to write into (h only with residual).
+    """
+    code, xs = _dtype(x), _rows(x, "x")
+    n, width = x.shape
+    dev = x.device
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            _vector(t, name, torch.float32, width, dev)
+    rs = _rows(residual, "residual", x) if residual is not None else 0
+    if out is None:
+        y = torch.empty((n, width), dtype=x.dtype, device=dev)
+        h = torch.empty((n, width), dtype=x.dtype, device=dev) if residual is not None else x
+        stats = torch.empty((2, n), dtype=torch.float32, device=dev)
+        mean, rstd = stats[0], stats[1]
+        ys = hs = width
+    else:
+        y, h, mean, rstd = out
+        ys = _rows(y, "y", x)
+        hs = _rows(h, "h", x) if residual is not None else 0
+        _vector(mean, "mean", torch.float32, n, dev)
+        _vector(rstd, "rstd", torch.float32, n, dev)
+        if residual is None:
+            h = x
+    _call(lib().layer_norm_rows, dev, stream, code, x.data_ptr(), xs, _ptr(residual), rs, n, width, _ptr(weight),
+          _ptr(bias), eps, y.data_ptr(), ys, h.data_ptr() if residual is not None else None, hs, mean.data_ptr(),
+          rstd.data_ptr())
+    return y, h, mean, rstd
+
+
+def layer_norm_rows_backward(grad_y: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor,
+                             rstd: torch.Tensor, grad_sum: torch.Tensor | None = None, stream=None):
+    """Gradients of layer_norm_rows from its h, mean and rstd; grad_sum is the
+    gradient that h got elsewhere.
+
+    Returns (grad_x in h's type, also the residual's gradient; grad_weight and
+    grad_bias float32 [width]).
+    """
+    code, xs = _dtype(h), _rows(h, "h")
+    n, width = h.shape
+    dev = h.device
+    gs = _rows(grad_y, "grad_y", h)
+    ss = _rows(grad_sum, "grad_sum", h) if grad_sum is not None else 0
+    if weight is not None:
+        _vector(weight, "weight", torch.float32, width, dev)
+    _vector(mean, "mean", torch.float32, n, dev)
+    _vector(rstd, "rstd", torch.float32, n, dev)
+    dx = torch.empty((n, width), dtype=h.dtype, device=dev)
+    dw = torch.empty(width, dtype=torch.float32, device=dev)
+    db = torch.empty(width, dtype=torch.float32, device=dev)
+    L = lib()
+    ws_bytes = L.layer_norm_rows_backward_workspace(n, width)
+    ws = _workspace(ws_bytes, dev, stream)
+    _call(L.layer_norm_rows_backward, dev, stream, code, grad_y.data_ptr(), gs, _ptr(grad_sum), ss, h.data_ptr(), xs, n,
+          width, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), width, dw.data_ptr(), db.data_ptr(),
+          _ptr(ws), ws_bytes)
+    return dx, dw, db
+
+
+class RotaryAxes:
+    """The frequencies of rotary_frames: radians per unit of time for the first
+    pairs of dimensions, per px of y for the next, per px of x for the last."""
+
+    def __init__(self, time=(), y=(), x=()):
+        freq = [float(f) for f in (*time, *y, *x)]
+        self.counts = (len(time), len(y), len(x))
+        self.pairs = len(freq)
+        self.freq = (ctypes.c_double * max(len(freq), 1))(*freq)
+
+
+def rotary_frames(q: torch.Tensor | None, k: torch.Tensor | None, xy: torch.Tensor | None, axes: RotaryAxes,
+                  time: torch.Tensor | None = None, interleaved: bool = False, inverse: bool = False, out=None,
+                  stream=None):
+    """Rotary positions from time (int32 [T]), y and x (xy, 1/16 px) of queries
+    [T, Hq, D] and keys [T, Hk, D] (either may be None); returns (q, k) turned.
+
+    Pair p of the axes' pairs is dimensions (p, p + pairs), or (2p, 2p + 1)
+    where interleaved; the rest is copied.  inverse turns back: with the
+    gradients of the turned tensors it gives the gradients of q and k.
+    out: optional (q, k) to write into, which may be q and k themselves.
+    """
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q or k must be given")
+    code, dev, n = _dtype(first), first.device, first.shape[0]
+    dim = first.shape[-1]
+    qs = _heads(q, "q") if q is not None else 0
+    ks = _heads(k, "k", n, first.dtype, dev) if k is not None else 0
+    if k is not None and k.shape[2] != dim:
+        raise ValueError("q and k must have the same head_dim")
+    nt, ny, nx = axes.counts
+    if ny or nx:
+        if xy is None or xy.dtype != torch.int32 or xy.device != dev or tuple(xy.shape) != (n, 2) \
+                or not xy.is_contiguous():
+            raise ValueError("xy must be a contiguous int32 [T, 2] tensor on the features' device")
+    if nt:
+        if time is None:
+            raise ValueError("time is needed by the axes' time pairs")
+        _vector(time, "time", torch.int32, n, dev)
+    qo, ko = out if out is not None else (None, None)
+    if qo is None and q is not None:
+        qo = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if ko is None and k is not None:
+        ko = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    for got, want, name in ((qo, q, "q"), (ko, k, "k")):
+        if got is not None and want is not None and got.shape != want.shape:
+            raise ValueError(f"out's {name} must have the shape of {name}")
+    qos = _heads(qo, "out's q", n, first.dtype, dev) if q is not None else 0
+    kos = _heads(ko, "out's k", n, first.dtype, dev) if k is not None else 0
+    _call(lib().rotary_frames, dev, stream, code, _ptr(q), qs, _ptr(k), ks, n, q.shape[1] if q is not None else 0,
+          k.shape[1] if k is not None else 0, dim, _ptr(xy) if ny or nx else None, _ptr(time) if nt else None,
+          axes.freq, nt, ny, nx, int(interleaved), int(inverse), _ptr(qo), qos, _ptr(ko), kos)
+    return qo, ko
+
+
+def _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal):
+    """The checked arguments that the forward and the backward call share."""
+    code, dev = _dtype(q), q.device
+    tq = q.shape[0]
+    tk = k.shape[0]
+    qs = _heads(q, "q")
+    ks = _heads(k, "k", tk, q.dtype, dev)
+    vs = _heads(v, "v", tk, q.dtype, dev)
+    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("k and v must have one shape, with the head_dim of q")
+    if k_offsets is None:
+        k_offsets = q_offsets
+    F = q_offsets.numel() - 1
+    if F < 0 or q_offsets.dim() != 1:
+        raise ValueError("q_offsets must be a contiguous [F + 1] tensor")
+    _vector(q_offsets, "q_offsets", torch.int32, F + 1, dev)
+    if k_offsets is not q_offsets:
+        _vector(k_offsets, "k_offsets", torch.int32, F + 1, dev)
+    if slopes is not None:
+        _vector(slopes, "slopes", torch.float32, q.shape[1], dev)
+        if k_xy is None:
+            k_xy = q_xy
+        if q_xy is None:
+            raise ValueError("q_xy is needed with slopes")
+        _vector(q_xy, "q_xy", torch.int32, 2 * tq, dev)
+        _vector(k_xy, "k_xy", torch.int32, 2 * tk, dev)
+    else:
+        q_xy = k_xy = None
+    if keep is not None:
+        _vector(keep, "keep", torch.uint8, tk, dev)
+    if prefix is not None:
+        _vector(prefix, "prefix", torch.int32, F, dev)
+    head = (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs)
+    tail = (q_offsets.data_ptr(), k_offsets.data_ptr(), F, tq, tk, q.shape[1], k.shape[1], q.shape[2], _ptr(q_xy),
+            _ptr(k_xy), _ptr(slopes), _ptr(keep), int(causal), _ptr(prefix) if causal else None)
+    return code, dev, (F, tq, tk, q.shape[1], k.shape[1], q.shape[2]), head, tail
+
+
+def attention_frames(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
+                     k_offsets: torch.Tensor | None = None, q_xy: torch.Tensor | None = None,
+                     k_xy: torch.Tensor | None = None, slopes: torch.Tensor | None = None,
+                     scale: float | None = None, cap: float = 0.0, keep: torch.Tensor | None = None,
+                     causal: bool = False, prefix: torch.Tensor | None = None, return_lse: bool = False, out=None,
+                     stream=None):
+    """Attention of queries [Tq, Hq, D] over the keys and values [Tk, Hkv, D] of
+    their frame (float16 or bfloat16), frames given by CSR offsets.
+
+    k_offsets: the keys' offsets (None: the queries').  slopes: float32 [Hq],
+    with places q_xy and k_xy (None: q_xy) in 1/16 px: slopes[h] times the
+    squared distance in px is taken off the scores.  scale: 1 / sqrt(D) if None.
+    cap: scores become cap * tanh(score / cap).  keep: uint8 [Tk], 0 hides a
+    key.  causal: key j of a frame is seen by query i if j < prefix[frame]
+    (int32 [F], None: 0) or j <= i + keys - queries.
+    Returns out [Tq, Hq, D], or (out, lse float64 [Tq, Hq]) with return_lse.
+    out: optional tensor to write into.
+    """
+    code, dev, shape, head, tail = _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    elif out.shape != q.shape:
+        raise ValueError("out must have the shape of q")
+    os_ = _heads(out, "out", q.shape[0], q.dtype, dev)
+    lse = torch.empty((shape[1], shape[3]), dtype=torch.float64, device=dev) if return_lse else None
+    L = lib()
+    ws_bytes = L.attention_frames_workspace(*shape)
+    ws = _workspace(ws_bytes, dev, stream)
+    _call(L.attention_frames, dev, stream, code, *head, *tail, q.shape[2] ** -0.5 if scale is None else scale, cap,
+          out.data_ptr(), os_, _ptr(lse), _ptr(ws), ws_bytes)
+    return (out, lse) if return_lse else out
+
+
+def attention_frames_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                              out: torch.Tensor, lse: torch.Tensor, q_offsets: torch.Tensor,
+                              k_offsets: torch.Tensor | None = None, q_xy: torch.Tensor | None = None,
+                              k_xy: torch.Tensor | None = None, slopes: torch.Tensor | None = None,
+                              scale: float | None = None, cap: float = 0.0, keep: torch.Tensor | None = None,
+                              causal: bool = False, prefix: torch.Tensor | None = None, stream=None):
+    """Gradients of attention_frames: its arguments with its out and lse, and
+    grad_out.  Returns (grad_q, grad_k, grad_v, grad_slopes float32 [Hq], or
+    None without slopes)."""
+    code, dev, shape, head, tail = _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal)
+    gs = _heads(grad_out, "grad_out", q.shape[0], q.dtype, dev)
+    os_ = _heads(out, "out", q.shape[0], q.dtype, dev)
+    if grad_out.shape != q.shape or out.shape != q.shape:
+        raise ValueError("grad_out and out must have the shape of q")
+    _vector(lse, "lse", torch.float64, shape[1] * shape[3], dev)
+    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    dk = torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dv = torch.empty(k.shape, dtype=q.dtype, device=dev)
+    ds = torch.empty(shape[3], dtype=torch.float32, device=dev) if slopes is not None else None
+    q_row, k_row = shape[3] * shape[5], shape[4] * shape[5]
+    L = lib()
+    ws_bytes = L.attention_frames_backward_workspace(*shape)
+    ws = _workspace(ws_bytes, dev, stream)
+    _call(L.attention_frames_backward, dev, stream, code, grad_out.data_ptr(), gs, *head, out.data_ptr(), os_,
+          lse.data_ptr(), *tail, q.shape[2] ** -0.5 if scale is None else scale, cap, dq.data_ptr(), q_row,
+          dk.data_ptr(), k_row, dv.data_ptr(), k_row, _ptr(ds), _ptr(ws), ws_bytes)
+    return dq, dk, dv, ds
 
 
 def version() -> str:

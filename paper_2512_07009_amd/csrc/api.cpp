@@ -726,3 +726,431 @@ flock_status mask_components_frames(const float *prob, int32_t n_frames, int32_t
 }
 
 }  // extern "C"
+
+// ----------------------------------------------------------------------------
+// Per-bird encoder
+// ----------------------------------------------------------------------------
+namespace {
+
+bool is_dtype(int32_t dtype) { return dtype == FLOCK_F32 || dtype == FLOCK_F16 || dtype == FLOCK_BF16; }
+
+size_t dtype_size(int32_t dtype) { return dtype == FLOCK_F32 ? 4 : 2; }
+
+// The caller's workspace, or a stream-ordered allocation that release() frees.
+struct Workspace {
+    void *ptr = nullptr;
+    bool owned = false;
+
+    flock_status take(void *workspace, size_t bytes, size_t need, hipStream_t s) {
+        if (workspace && bytes < need) return fail(FLOCK_ENOMEM, "workspace of %zu bytes, %zu needed", bytes, need);
+        if (workspace && !aligned(workspace, 256)) return fail(FLOCK_EINVAL, "workspace must be 256-byte aligned");
+        ptr = workspace;
+        if (!ptr && need > 0) {
+            const hipError_t err = hipMallocAsync(&ptr, need, s);
+            if (err != hipSuccess) return fail(FLOCK_ENOMEM, "hipMallocAsync(%zu): %s", need, hipGetErrorString(err));
+            owned = true;
+        }
+        return FLOCK_OK;
+    }
+    hipError_t release(hipStream_t s) { return owned ? hipFreeAsync(ptr, s) : hipSuccess; }
+};
+
+int device_cus() {
+    const DeviceInfo *dev = nullptr;
+    const int n = device_info(&dev) == FLOCK_OK ? dev->n_cus : 256;
+    g_error[0] = '\0';
+    return n;
+}
+
+flock_status check_norm(int32_t dtype, int32_t rows, int32_t width) {
+    if (!is_dtype(dtype)) return fail(FLOCK_EINVAL, "dtype = %d, expected FLOCK_F32, FLOCK_F16 or FLOCK_BF16", dtype);
+    if (rows < 0) return fail(FLOCK_EINVAL, "rows = %d < 0", rows);
+    if (width < 1 || width > (1 << 20)) return fail(FLOCK_EINVAL, "width = %d outside 1..2^20", width);
+    return FLOCK_OK;
+}
+
+// The arguments that attention_frames and its backward pass share.
+flock_status check_attention(int32_t dtype, const flock::AttentionArgs &a) {
+    if (dtype != FLOCK_F16 && dtype != FLOCK_BF16)
+        return fail(FLOCK_EINVAL, "dtype = %d, expected FLOCK_F16 or FLOCK_BF16", dtype);
+    if (a.n_frames < 0) return fail(FLOCK_EINVAL, "n_frames = %d < 0", a.n_frames);
+    if (a.total_q < 0 || a.total_k < 0)
+        return fail(FLOCK_EINVAL, "total_q = %d, total_k = %d must be >= 0", a.total_q, a.total_k);
+    if (a.kv_heads < 1 || a.kv_heads > 256 || a.q_heads < 1 || a.q_heads > 256)
+        return fail(FLOCK_EINVAL, "q_heads = %d, kv_heads = %d outside 1..256", a.q_heads, a.kv_heads);
+    if (a.q_heads % a.kv_heads)
+        return fail(FLOCK_EINVAL, "q_heads = %d is not a multiple of kv_heads = %d", a.q_heads, a.kv_heads);
+    if (a.dim < 8 || a.dim > flock::kAttentionMaxDim || a.dim % 8)
+        return fail(FLOCK_EINVAL, "head_dim = %d is not a multiple of 8 in 8..%d", a.dim, flock::kAttentionMaxDim);
+    if (a.causal != 0 && a.causal != 1) return fail(FLOCK_EINVAL, "causal = %d, expected 0 or 1", a.causal);
+    if (!std::isfinite(a.scale) || !(a.scale > 0.0f)) return fail(FLOCK_EINVAL, "scale must be finite and > 0");
+    if (!std::isfinite(a.cap) || !(a.cap >= 0.0f)) return fail(FLOCK_EINVAL, "cap must be finite and >= 0");
+    if (a.q_stride < 0 || a.k_stride < 0 || a.v_stride < 0 || a.q_stride % 8 || a.k_stride % 8 || a.v_stride % 8)
+        return fail(FLOCK_EINVAL, "strides of q, k and v must be multiples of 8, >= 0");
+    if (a.out_stride < (int64_t)a.q_heads * a.dim || a.out_stride % 8)
+        return fail(FLOCK_EINVAL, "out's stride must be a multiple of 8 that holds a row");
+    return FLOCK_OK;
+}
+
+flock_status check_attention_pointers(const flock::AttentionArgs &a) {
+    if (!a.q_offsets || !a.k_offsets) return fail(FLOCK_EINVAL, "q_offsets and k_offsets must be non-NULL");
+    if (a.total_q > 0 && (!a.q || !a.out)) return fail(FLOCK_EINVAL, "q and out must be non-NULL when total_q > 0");
+    if (a.total_k > 0 && (!a.k || !a.v)) return fail(FLOCK_EINVAL, "k and v must be non-NULL when total_k > 0");
+    if (a.slopes && ((a.total_q > 0 && !a.q_xy) || (a.total_k > 0 && !a.k_xy)))
+        return fail(FLOCK_EINVAL, "q_xy and k_xy must be non-NULL with slopes");
+    if (!aligned(a.q, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.out, 16))
+        return fail(FLOCK_EINVAL, "q, k, v and out must be 16-byte aligned");
+    if (!aligned(a.q_xy, 8) || !aligned(a.k_xy, 8)) return fail(FLOCK_EINVAL, "q_xy and k_xy must be 8-byte aligned");
+    if (!aligned(a.q_offsets, 4) || !aligned(a.k_offsets, 4) || !aligned(a.slopes, 4) || !aligned(a.prefix, 4))
+        return fail(FLOCK_EINVAL, "q_offsets, k_offsets, slopes and prefix must be 4-byte aligned");
+    if (!aligned(a.lse, 8)) return fail(FLOCK_EINVAL, "lse must be 8-byte aligned");
+    // rows are numbered in 32 bits in a frame's tile, tiles in a launch's grid
+    if (((int64_t)a.total_q * a.group / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL ||
+        ((int64_t)a.total_k / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL)
+        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 - 1 tiles");
+    return FLOCK_OK;
+}
+
+flock_status validate_offsets(const char *name, const int32_t *offsets, int32_t n_frames, int32_t total,
+                              hipStream_t stream) {
+    std::vector<int32_t> off((size_t)n_frames + 1);
+    hipError_t err = hipMemcpyAsync(off.data(), offsets, off.size() * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
+    if (err == hipSuccess) err = hipStreamSynchronize(stream);
+    if (err != hipSuccess) return hip_fail(err, "FLOCK_VALIDATE offsets copy");
+    if (off[0] != 0) return fail(FLOCK_EINVAL, "%s[0] = %d, expected 0", name, off[0]);
+    for (int32_t f = 0; f < n_frames; ++f)
+        if (off[f + 1] < off[f]) return fail(FLOCK_EINVAL, "%s decrease at frame %d", name, f);
+    if (off[n_frames] != total) return fail(FLOCK_EINVAL, "%s[n_frames] = %d but its total is %d", name, off[n_frames], total);
+    return FLOCK_OK;
+}
+
+flock_status validate_attention(const flock::AttentionArgs &a, hipStream_t s) {
+    flock_status st = validate_offsets("q_offsets", a.q_offsets, a.n_frames, a.total_q, s);
+    if (st == FLOCK_OK && a.k_offsets != a.q_offsets)
+        st = validate_offsets("k_offsets", a.k_offsets, a.n_frames, a.total_k, s);
+    else if (st == FLOCK_OK && a.total_k != a.total_q)
+        st = fail(FLOCK_EINVAL, "k_offsets[n_frames] = %d but its total is %d", a.total_q, a.total_k);
+    return st;
+}
+
+}  // namespace
+
+extern "C" {
+
+flock_status layer_norm_rows(int32_t dtype, const void *x, int64_t x_stride, const void *residual,
+                             int64_t residual_stride, int32_t rows, int32_t width, const float *weight,
+                             const float *bias, float eps, void *y, int64_t y_stride, void *sum, int64_t sum_stride,
+                             float *mean, float *rstd, void *stream) {
+    g_error[0] = '\0';
+    flock_status st = check_norm(dtype, rows, width);
+    if (st != FLOCK_OK) return st;
+    if (!std::isfinite(eps) || !(eps >= 0.0f)) return fail(FLOCK_EINVAL, "eps must be finite and >= 0");
+    if (x_stride < 0 || (residual && residual_stride < 0)) return fail(FLOCK_EINVAL, "input strides must be >= 0");
+    if (y_stride < width || (residual && sum_stride < width))
+        return fail(FLOCK_EINVAL, "output strides must hold a row");
+    if (rows == 0) return FLOCK_OK;
+    if (!x || !y) return fail(FLOCK_EINVAL, "x and y must be non-NULL");
+    if (residual && !sum) return fail(FLOCK_EINVAL, "sum must be non-NULL with residual");
+    const size_t size = dtype_size(dtype);
+    if (!aligned(x, size) || !aligned(y, size) || !aligned(residual, size) || !aligned(sum, size))
+        return fail(FLOCK_EINVAL, "x, residual, y and sum must be aligned to their elements");
+    if (!aligned(weight, 4) || !aligned(bias, 4) || !aligned(mean, 4) || !aligned(rstd, 4))
+        return fail(FLOCK_EINVAL, "weight, bias, mean and rstd must be 4-byte aligned");
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    flock::NormArgs a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.residual = residual;
+    a.residual_stride = residual ? residual_stride : 0;
+    a.rows = rows;
+    a.width = width;
+    a.weight = weight;
+    a.bias = bias;
+    a.eps = eps;
+    a.y = y;
+    a.y_stride = y_stride;
+    a.sum = residual ? sum : nullptr;
+    a.sum_stride = residual ? sum_stride : 0;
+    a.mean = mean;
+    a.rstd = rstd;
+    const hipError_t err = flock::launch_norm(a, dtype, reinterpret_cast<hipStream_t>(stream));
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "layer norm kernel launch");
+}
+
+size_t layer_norm_rows_backward_workspace(int32_t rows, int32_t width) {
+    return flock::norm_backward_workspace_bytes(rows, width, device_cus());
+}
+
+flock_status layer_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t grad_y_stride, const void *grad_sum,
+                                      int64_t grad_sum_stride, const void *x, int64_t x_stride, int32_t rows,
+                                      int32_t width, const float *weight, const float *mean, const float *rstd,
+                                      void *grad_x, int64_t grad_x_stride, float *grad_weight, float *grad_bias,
+                                      void *workspace, size_t workspace_bytes, void *stream) {
+    g_error[0] = '\0';
+    flock_status st = check_norm(dtype, rows, width);
+    if (st != FLOCK_OK) return st;
+    if (grad_y_stride < 0 || x_stride < 0 || (grad_sum && grad_sum_stride < 0))
+        return fail(FLOCK_EINVAL, "input strides must be >= 0");
+    if (grad_x_stride < width) return fail(FLOCK_EINVAL, "output strides must hold a row");
+    if (rows > 0 && (!grad_y || !x || !mean || !rstd || !grad_x))
+        return fail(FLOCK_EINVAL, "grad_y, x, mean, rstd and grad_x must be non-NULL");
+    const size_t size = dtype_size(dtype);
+    if (!aligned(grad_y, size) || !aligned(x, size) || !aligned(grad_sum, size) || !aligned(grad_x, size))
+        return fail(FLOCK_EINVAL, "grad_y, grad_sum, x and grad_x must be aligned to their elements");
+    if (!aligned(weight, 4) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(grad_weight, 4) || !aligned(grad_bias, 4))
+        return fail(FLOCK_EINVAL, "weight, mean, rstd, grad_weight and grad_bias must be 4-byte aligned");
+    if (rows == 0 && !grad_weight && !grad_bias) return FLOCK_OK;
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    const bool columns = grad_weight || grad_bias;
+    Workspace ws;
+    st = ws.take(workspace, workspace_bytes,
+                 columns ? flock::norm_backward_workspace_bytes(rows, width, dev->n_cus) : 0, s);
+    if (st != FLOCK_OK) return st;
+    flock::NormBackwardArgs a{};
+    a.grad_y = grad_y;
+    a.grad_y_stride = grad_y_stride;
+    a.grad_sum = grad_sum;
+    a.grad_sum_stride = grad_sum ? grad_sum_stride : 0;
+    a.x = x;
+    a.x_stride = x_stride;
+    a.rows = rows;
+    a.width = width;
+    a.weight = weight;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.grad_x = grad_x;
+    a.grad_x_stride = grad_x_stride;
+    hipError_t err = flock::launch_norm_backward(a, dtype, ws.ptr, dev->n_cus, grad_weight, grad_bias, s);
+    const hipError_t ferr = ws.release(s);
+    if (err == hipSuccess) err = ferr;
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "layer norm backward kernels");
+}
+
+flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                           int32_t total, int32_t q_heads, int32_t k_heads, int32_t head_dim, const int32_t *xy,
+                           const int32_t *time, const double *freq, int32_t n_time, int32_t n_y, int32_t n_x,
+                           int32_t interleaved, int32_t inverse, void *q_out, int64_t q_out_stride, void *k_out,
+                           int64_t k_out_stride, void *stream) {
+    g_error[0] = '\0';
+    if (!is_dtype(dtype)) return fail(FLOCK_EINVAL, "dtype = %d, expected FLOCK_F32, FLOCK_F16 or FLOCK_BF16", dtype);
+    if (total < 0) return fail(FLOCK_EINVAL, "total = %d < 0", total);
+    if (q_heads < 0 || q_heads > 256 || k_heads < 0 || k_heads > 256 || q_heads + k_heads < 1)
+        return fail(FLOCK_EINVAL, "q_heads = %d, k_heads = %d outside 0..256, or none", q_heads, k_heads);
+    if (head_dim < 1 || head_dim > 2 * flock::kRotaryMaxPairs)
+        return fail(FLOCK_EINVAL, "head_dim = %d outside 1..%d", head_dim, 2 * flock::kRotaryMaxPairs);
+    if (n_time < 0 || n_y < 0 || n_x < 0 || (int64_t)n_time + n_y + n_x < 1 ||
+        2 * ((int64_t)n_time + n_y + n_x) > head_dim)
+        return fail(FLOCK_EINVAL, "n_time = %d, n_y = %d, n_x = %d pairs do not fit head_dim = %d", n_time, n_y, n_x,
+                    head_dim);
+    if (!freq) return fail(FLOCK_EINVAL, "freq is NULL");
+    const int32_t pairs = n_time + n_y + n_x;
+    for (int32_t p = 0; p < pairs; ++p)
+        if (!std::isfinite(freq[p])) return fail(FLOCK_EINVAL, "freq[%d] is not finite", p);
+    if ((q_heads && (q_stride < 0 || q_out_stride < (int64_t)q_heads * head_dim)) ||
+        (k_heads && (k_stride < 0 || k_out_stride < (int64_t)k_heads * head_dim)))
+        return fail(FLOCK_EINVAL, "strides must be >= 0, and hold a row for outputs");
+    if ((q_heads && q == q_out && q_stride != q_out_stride) || (k_heads && k == k_out && k_stride != k_out_stride))
+        if (total > 0 && (q || k)) return fail(FLOCK_EINVAL, "an output in place has its input's stride");
+    if (total == 0) return FLOCK_OK;
+    if ((q_heads && (!q || !q_out)) || (k_heads && (!k || !k_out)))
+        return fail(FLOCK_EINVAL, "q, k, q_out and k_out must be non-NULL where they have heads");
+    if ((n_y || n_x) && !xy) return fail(FLOCK_EINVAL, "xy is NULL with y or x pairs");
+    if (n_time && !time) return fail(FLOCK_EINVAL, "time is NULL with time pairs");
+    const size_t size = dtype_size(dtype);
+    if (!aligned(q, size) || !aligned(k, size) || !aligned(q_out, size) || !aligned(k_out, size))
+        return fail(FLOCK_EINVAL, "q, k, q_out and k_out must be aligned to their elements");
+    if (!aligned(xy, 8) || !aligned(time, 4))
+        return fail(FLOCK_EINVAL, "xy must be 8-byte aligned, time 4-byte aligned");
+    const DeviceInfo *dev = nullptr;
+    const flock_status st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    flock::RotaryArgs a{};
+    a.q = q_heads ? q : nullptr;
+    a.k = k_heads ? k : nullptr;
+    a.q_out = q_heads ? q_out : nullptr;
+    a.k_out = k_heads ? k_out : nullptr;
+    a.q_stride = q_heads ? q_stride : 0;
+    a.k_stride = k_heads ? k_stride : 0;
+    a.q_out_stride = q_heads ? q_out_stride : 0;
+    a.k_out_stride = k_heads ? k_out_stride : 0;
+    a.xy = xy;
+    a.time = time;
+    a.total = total;
+    a.q_heads = q_heads;
+    a.k_heads = k_heads;
+    a.head_dim = head_dim;
+    a.n_time = n_time;
+    a.n_y = n_y;
+    a.pairs = pairs;
+    a.interleaved = interleaved != 0;
+    a.inverse = inverse != 0;
+    for (int32_t p = 0; p < pairs; ++p) {
+        // turns per unit, whole turns dropped, in 2^-64 turns (rounded down to the double's last digit)
+        double turns = freq[p] / (2.0 * 3.14159265358979323846) / (p < n_time ? 1.0 : 16.0);
+        const bool back = turns < 0.0;
+        turns = std::fmod(std::fabs(turns), 1.0);
+        const uint64_t step = (uint64_t)std::ldexp(turns, 64);
+        a.step[p] = back ? 0 - step : step;
+    }
+    const hipError_t err = flock::launch_rotary(a, dtype, reinterpret_cast<hipStream_t>(stream));
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "rotary kernel launch");
+}
+
+size_t attention_frames_workspace(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads,
+                                  int32_t kv_heads, int32_t head_dim) {
+    if (n_frames <= 0 || total_q <= 0 || total_k <= 0 || q_heads < 1 || kv_heads < 1 || head_dim < 1) return 0;
+    const flock::AttentionPlan plan = flock::plan_attention(n_frames, total_q, total_k, q_heads, kv_heads, device_cus());
+    return flock::attention_workspace_bytes(plan, total_q, q_heads, head_dim);
+}
+
+flock_status attention_frames(int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, const int32_t *q_offsets, const int32_t *k_offsets,
+                              int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads, int32_t kv_heads,
+                              int32_t head_dim, const int32_t *q_xy, const int32_t *k_xy, const float *slopes,
+                              const uint8_t *keep, int32_t causal, const int32_t *prefix, float scale, float cap,
+                              void *out, int64_t out_stride, double *lse, void *workspace, size_t workspace_bytes,
+                              void *stream) {
+    g_error[0] = '\0';
+    flock::AttentionArgs a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.out_stride = out_stride;
+    a.q_offsets = q_offsets;
+    a.k_offsets = k_offsets;
+    a.n_frames = n_frames;
+    a.total_q = total_q;
+    a.total_k = total_k;
+    a.q_heads = q_heads;
+    a.kv_heads = kv_heads;
+    a.dim = head_dim;
+    a.q_xy = q_xy;
+    a.k_xy = k_xy;
+    a.slopes = slopes;
+    a.keep = keep;
+    a.prefix = prefix;
+    a.causal = causal;
+    a.scale = scale;
+    a.cap = cap;
+    a.lse = lse;
+    flock_status st = check_attention(dtype, a);
+    if (st != FLOCK_OK) return st;
+    a.group = q_heads / kv_heads;
+    if (n_frames == 0 || total_q == 0) return FLOCK_OK;
+    st = check_attention_pointers(a);
+    if (st != FLOCK_OK) return st;
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (validate_requested()) {
+        st = validate_attention(a, s);
+        if (st != FLOCK_OK) return st;
+    }
+    const flock::AttentionPlan plan = flock::plan_attention(n_frames, total_q, total_k, q_heads, kv_heads, dev->n_cus);
+    Workspace ws;
+    st = ws.take(workspace, workspace_bytes, flock::attention_workspace_bytes(plan, total_q, q_heads, head_dim), s);
+    if (st != FLOCK_OK) return st;
+    hipError_t err = flock::launch_attention(a, dtype, plan, ws.ptr, s);
+    const hipError_t ferr = ws.release(s);
+    if (err == hipSuccess) err = ferr;
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "attention kernels");
+}
+
+size_t attention_frames_backward_workspace(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads,
+                                           int32_t kv_heads, int32_t head_dim) {
+    if (n_frames <= 0 || total_q < 0 || total_k < 0 || q_heads < 1 || kv_heads < 1 || head_dim < 1) return 0;
+    return flock::attention_backward_workspace_bytes(total_q, q_heads);
+}
+
+flock_status attention_frames_backward(
+    int32_t dtype, const void *grad_out, int64_t grad_out_stride, const void *q, int64_t q_stride, const void *k,
+    int64_t k_stride, const void *v, int64_t v_stride, const void *out, int64_t out_stride, const double *lse,
+    const int32_t *q_offsets, const int32_t *k_offsets, int32_t n_frames, int32_t total_q, int32_t total_k,
+    int32_t q_heads, int32_t kv_heads, int32_t head_dim, const int32_t *q_xy, const int32_t *k_xy,
+    const float *slopes, const uint8_t *keep, int32_t causal, const int32_t *prefix, float scale, float cap,
+    void *grad_q, int64_t grad_q_stride, void *grad_k, int64_t grad_k_stride, void *grad_v, int64_t grad_v_stride,
+    float *grad_slopes, void *workspace, size_t workspace_bytes, void *stream) {
+    g_error[0] = '\0';
+    flock::AttentionBackwardArgs b{};
+    flock::AttentionArgs &a = b.fwd;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = const_cast<void *>(out);  // read only
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.out_stride = out_stride;
+    a.q_offsets = q_offsets;
+    a.k_offsets = k_offsets;
+    a.n_frames = n_frames;
+    a.total_q = total_q;
+    a.total_k = total_k;
+    a.q_heads = q_heads;
+    a.kv_heads = kv_heads;
+    a.dim = head_dim;
+    a.q_xy = q_xy;
+    a.k_xy = k_xy;
+    a.slopes = slopes;
+    a.keep = keep;
+    a.prefix = prefix;
+    a.causal = causal;
+    a.scale = scale;
+    a.cap = cap;
+    a.lse = const_cast<double *>(lse);  // read only
+    b.grad_out = grad_out;
+    b.grad_out_stride = grad_out_stride;
+    b.grad_q = grad_q;
+    b.grad_q_stride = grad_q_stride;
+    b.grad_k = grad_k;
+    b.grad_k_stride = grad_k_stride;
+    b.grad_v = grad_v;
+    b.grad_v_stride = grad_v_stride;
+    flock_status st = check_attention(dtype, a);
+    if (st != FLOCK_OK) return st;
+    a.group = q_heads / kv_heads;
+    const int64_t q_row = (int64_t)q_heads * head_dim, kv_row = (int64_t)kv_heads * head_dim;
+    if (grad_out_stride < 0 || grad_out_stride % 8)
+        return fail(FLOCK_EINVAL, "grad_out's stride must be a multiple of 8, >= 0");
+    if (grad_q_stride < q_row || grad_k_stride < kv_row || grad_v_stride < kv_row || grad_q_stride % 8 ||
+        grad_k_stride % 8 || grad_v_stride % 8)
+        return fail(FLOCK_EINVAL, "strides of grad_q, grad_k and grad_v must be multiples of 8 that hold a row");
+    if (grad_slopes && !slopes) return fail(FLOCK_EINVAL, "grad_slopes without slopes");
+    if (n_frames == 0) return FLOCK_OK;
+    st = check_attention_pointers(a);
+    if (st != FLOCK_OK) return st;
+    if (total_q > 0 && (!grad_out || !lse || !grad_q))
+        return fail(FLOCK_EINVAL, "grad_out, lse and grad_q must be non-NULL when total_q > 0");
+    if (total_k > 0 && (!grad_k || !grad_v))
+        return fail(FLOCK_EINVAL, "grad_k and grad_v must be non-NULL when total_k > 0");
+    if (!aligned(grad_out, 16) || !aligned(grad_q, 16) || !aligned(grad_k, 16) || !aligned(grad_v, 16))
+        return fail(FLOCK_EINVAL, "grad_out, grad_q, grad_k and grad_v must be 16-byte aligned");
+    if (!aligned(grad_slopes, 4)) return fail(FLOCK_EINVAL, "grad_slopes must be 4-byte aligned");
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (validate_requested()) {
+        st = validate_attention(a, s);
+        if (st != FLOCK_OK) return st;
+    }
+    Workspace ws;
+    st = ws.take(workspace, workspace_bytes, flock::attention_backward_workspace_bytes(total_q, q_heads), s);
+    if (st != FLOCK_OK) return st;
+    hipError_t err = flock::launch_attention_backward(b, dtype, ws.ptr, grad_slopes, s);
+    const hipError_t ferr = ws.release(s);
+    if (err == hipSuccess) err = ferr;
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "attention backward kernels");
+}
+
+}  // extern "C"

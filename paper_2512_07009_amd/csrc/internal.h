@@ -192,4 +192,98 @@ struct MaskArgs {
 size_t mask_workspace_bytes(int32_t n_frames, int32_t width, int32_t height, int32_t connectivity);
 hipError_t launch_mask(MaskArgs a, void *workspace, hipStream_t stream);
 
+// ----------------------------------------------------------------------------
+// Per-bird encoder: layer norm, rotary positions, attention
+// ----------------------------------------------------------------------------
+struct NormArgs {
+    const void *x, *residual;          // [rows][width], strides in elements; residual may be nullptr
+    int64_t x_stride, residual_stride;
+    int64_t rows;
+    int32_t width;
+    const float *weight, *bias;        // [width] or nullptr
+    float eps;
+    void *y, *sum;                     // sum only with residual
+    int64_t y_stride, sum_stride;
+    float *mean, *rstd;                // [rows] or nullptr
+};
+hipError_t launch_norm(const NormArgs &a, int32_t dtype, hipStream_t stream);
+
+struct NormBackwardArgs {
+    const void *grad_y, *grad_sum, *x;  // grad_sum may be nullptr
+    int64_t grad_y_stride, grad_sum_stride, x_stride;
+    int64_t rows;
+    int32_t width;
+    const float *weight;                // [width] or nullptr
+    const float *mean, *rstd;           // [rows]
+    void *grad_x;
+    int64_t grad_x_stride;
+    float *partial;                     // set by launch_norm_backward
+};
+size_t norm_backward_workspace_bytes(int64_t rows, int32_t width, int n_cus);
+hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspace, int n_cus, float *grad_weight,
+                                float *grad_bias, hipStream_t stream);
+
+constexpr int kRotaryMaxPairs = 128;
+
+struct RotaryArgs {
+    const void *q, *k;                 // [total][heads][head_dim], strides of birds in elements
+    void *q_out, *k_out;
+    int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+    const int32_t *xy;                 // [total][2], or nullptr without y and x pairs
+    const int32_t *time;               // [total], or nullptr without time pairs
+    int64_t total;
+    int32_t q_heads, k_heads, head_dim;
+    int32_t n_time, n_y, pairs;        // pairs = n_time + n_y + n_x
+    int32_t interleaved, inverse;
+    int32_t tail, birds_per_block;     // set by launch_rotary
+    uint32_t chunk_reciprocal, head_reciprocal;
+    uint64_t step[kRotaryMaxPairs];    // 2^-64 turns per unit
+};
+hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);
+
+constexpr int kAttentionMaxDim = 128;
+
+struct AttentionArgs {
+    const void *q, *k, *v;             // [total][heads][dim], strides of birds in elements
+    void *out;
+    int64_t q_stride, k_stride, v_stride, out_stride;
+    const int32_t *q_offsets, *k_offsets;  // [n_frames + 1]
+    int32_t n_frames, total_q, total_k;
+    int32_t q_heads, kv_heads, group, dim;  // group = q_heads / kv_heads
+    const int32_t *q_xy, *k_xy;        // 1/16 px, with slopes
+    const float *slopes;               // [q_heads] or nullptr
+    const uint8_t *keep;               // [total_k] or nullptr
+    const int32_t *prefix;             // [n_frames] or nullptr
+    int32_t causal;
+    float scale, cap;                  // cap = 0: none
+    double *lse;                       // [total_q][q_heads] or nullptr
+    int64_t slots;                     // set by the launches: numbers of row tiles
+    int32_t splits;
+    float *part_out, *part_stat;
+};
+
+// How the rows of a forward launch are dealt out.
+struct AttentionPlan {
+    bool split;      // 32 rows a workgroup and a quarter of the keys a wave
+    int32_t splits;  // workgroups that share a row's keys
+    int64_t slots;
+};
+AttentionPlan plan_attention(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads, int32_t kv_heads,
+                             int n_cus);
+size_t attention_workspace_bytes(const AttentionPlan &p, int32_t total_q, int32_t q_heads, int32_t dim);
+hipError_t launch_attention(AttentionArgs a, int32_t dtype, const AttentionPlan &p, void *workspace,
+                            hipStream_t stream);
+
+struct AttentionBackwardArgs {
+    AttentionArgs fwd;
+    const void *grad_out;
+    void *grad_q, *grad_k, *grad_v;
+    int64_t grad_out_stride, grad_q_stride, grad_k_stride, grad_v_stride;
+    float *delta, *row_slopes;         // set by launch_attention_backward: [total_q][q_heads]
+    int64_t key_slots;
+};
+size_t attention_backward_workspace_bytes(int32_t total_q, int32_t q_heads);
+hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, void *workspace, float *grad_slopes,
+                                     hipStream_t stream);
+
 }  // namespace flock

@@ -1,0 +1,328 @@
+"""attention_frames and its backward pass against the 64-bit reference: sizes
+around the tiles, ragged and empty frames, shared heads, all head widths,
+distances, caps, hidden keys, order with prefixes, single queries, strides,
+far offsets, streams and graphs; gradients also against differences."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2512_07009_amd as flock
+from tests import encoder_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def offsets(counts):
+    off = [0]
+    for c in counts:
+        off.append(off[-1] + c)
+    return off
+
+
+def make(seed, q_counts, k_counts, Hq, Hk, D, dtype, distance=False, hidden=0.0, causal=False, prefix=None, cap=0.0,
+         far=0, sigma=(20.0, 300.0), spread=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    tq, tk = sum(q_counts), sum(k_counts)
+    own = q_counts is k_counts
+    rnd = lambda *s: (spread * torch.randn(*s, generator=gen)).to(dtype)  # noqa: E731
+    c = dict(q=rnd(tq, Hq, D), k=rnd(tk, Hk, D), v=rnd(tk, Hk, D), q_off=offsets(q_counts), k_off=offsets(k_counts),
+             scale=D ** -0.5, cap=cap, causal=causal)
+    c["grad"] = rnd(tq, Hq, D)
+    if distance:
+        c["k_xy"] = (torch.rand(tk, 2, generator=gen) * 16 * 400).int() + far
+        c["q_xy"] = c["k_xy"] if own else (torch.rand(tq, 2, generator=gen) * 16 * 400).int() + far
+        sig = sigma[0] * (sigma[1] / sigma[0]) ** (torch.arange(Hq) / max(Hq - 1, 1))
+        c["slopes"] = (0.5 / sig ** 2).float()
+    if hidden:
+        c["keep"] = (torch.rand(tk, generator=gen) >= hidden).to(torch.uint8)
+    if prefix is not None:
+        c["prefix"] = torch.tensor(prefix, dtype=torch.int32)
+    return c
+
+
+def call(c, train=True, stream=None):
+    d = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in c.items()}
+    qo = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    ko = torch.tensor(c["k_off"], dtype=torch.int32).cuda()
+    more = dict(k_offsets=ko, q_xy=d.get("q_xy"), k_xy=d.get("k_xy"), slopes=d.get("slopes"), scale=c["scale"],
+                cap=c["cap"], keep=d.get("keep"), causal=c["causal"], prefix=d.get("prefix"))
+    out, lse = flock.attention_frames(d["q"], d["k"], d["v"], qo, return_lse=True, **more)
+    r = {"out": out, "lse": lse}
+    if train:
+        r["dq"], r["dk"], r["dv"], r["ds"] = flock.attention_frames_backward(d["grad"], d["q"], d["k"], d["v"], out,
+                                                                            lse, qo, **more)
+    torch.cuda.synchronize()
+    return r
+
+
+def reference(c, train=True):
+    return ref.attention(c["q"], c["k"], c["v"], c["q_off"], c["k_off"], c["scale"], c["cap"], c.get("q_xy"),
+                         c.get("k_xy"), c.get("slopes"), c.get("keep"), c["causal"], c.get("prefix"),
+                         c["grad"] if train else None)
+
+
+def compare(c, train=True):
+    got = call(c, train)
+    want, bound = reference(c, train)
+    for n in want:
+        if n == "ds" and got[n] is None:
+            continue
+        ref.check(got[n], want[n], bound[n], n)
+    return got
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 200, 300])
+def test_one_frame(n, dtype):
+    compare(make(n, [n], [n], 2, 2, 64, dtype, distance=True))
+
+
+@pytest.mark.parametrize("dim", [8, 16, 24, 32, 40, 64, 80, 96, 104, 128])
+@pytest.mark.parametrize("heads", [(1, 1), (3, 3), (4, 2), (6, 1), (8, 8)])
+def test_widths_and_heads(dim, heads):
+    counts = [70, 0, 5, 131]
+    compare(make(dim, counts, counts, *heads, dim, torch.bfloat16, distance=dim % 16 == 0, cap=5.0 if dim > 64 else 0.0))
+
+
+@pytest.mark.parametrize("flags", [dict(), dict(distance=True), dict(cap=2.0), dict(distance=True, cap=2.0),
+                                   dict(hidden=0.3), dict(hidden=0.9, distance=True), dict(causal=True),
+                                   dict(causal=True, hidden=0.5, cap=3.0), dict(causal=True, distance=True),
+                                   dict(causal=True, prefix=[0, 40, 3, 1000, 1])])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_masks_and_scores(flags, dtype):
+    counts = [100, 77, 0, 258, 1]
+    compare(make(7, counts, counts, 4, 2, 64, dtype, **flags))
+
+
+# enough rows for 128-row tiles (more tiles than twice the card's compute units)
+@pytest.mark.parametrize("flags", [dict(distance=True), dict(causal=True, prefix=[5] * 90), dict(hidden=0.4, cap=4.0),
+                                   dict(causal=True, hidden=0.2, distance=True)])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_many_frames(flags, dim):
+    counts = [(37 * f) % 190 for f in range(90)]
+    compare(make(dim, counts, counts, 8, 8, dim, torch.bfloat16, **flags))
+
+
+@pytest.mark.parametrize("queries", [1, 2, 5, 17])
+@pytest.mark.parametrize("heads", [(1, 1), (8, 2), (6, 6)])
+@pytest.mark.parametrize("flags", [dict(), dict(distance=True, hidden=0.2), dict(causal=True), dict(cap=10.0)])
+def test_few_queries_over_long_histories(queries, heads, flags):
+    k_counts = [1500, 0, 3, 1, 700, 129]
+    c = make(queries, [queries] * 6, k_counts, *heads, 64 if heads[0] != 6 else 128, torch.bfloat16, **flags)
+    compare(c)
+
+
+@pytest.mark.parametrize("n", [4097, 9000])
+def test_long_history(n):
+    compare(make(n, [1], [n], 8, 1, 64, torch.float16, distance=True))
+    compare(make(n, [3], [n], 2, 2, 40, torch.bfloat16, causal=True))
+
+
+def test_queries_beyond_the_keys_of_an_ordered_frame():
+    """More queries than keys: the first ones see nothing."""
+    c = make(3, [9, 70], [4, 30], 2, 1, 64, torch.bfloat16, causal=True)
+    got = compare(c)
+    assert (got["out"][:5] == 0).all() and (got["lse"][:5] == -math.inf).all() and (got["dq"][:5] == 0).all()
+
+
+def test_frames_whose_keys_are_all_hidden():
+    c = make(4, [40, 200, 33], [40, 200, 33], 4, 4, 64, torch.bfloat16, distance=True, hidden=0.1)
+    c["keep"][40:240] = 0
+    got = compare(c)
+    assert (got["out"][40:240] == 0).all() and (got["lse"][40:240] == -math.inf).all()
+    assert (got["dk"][40:240] == 0).all() and (got["dv"][40:240] == 0).all() and (got["dq"][40:240] == 0).all()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("causal", [False, True])
+def test_hidden_keys_are_not_read(bad, causal):
+    c = make(5, [150], [150], 2, 2, 64, torch.bfloat16, distance=True, hidden=0.3, causal=causal)
+    gone = c["keep"] == 0
+    c["k"][gone] = bad
+    c["v"][gone] = bad
+    compare(c)
+
+
+def test_lowest_and_largest_scores():
+    """Scores far beyond exp's range, and many that underflow."""
+    c = make(6, [130], [130], 2, 2, 64, torch.bfloat16, distance=True, sigma=(0.05, 2.0))
+    compare(c)
+    c = make(8, [64], [64], 2, 2, 64, torch.bfloat16)
+    c["q"] = c["q"] * 32
+    # scores of some thousand: their 32-bit rounding alone moves the weights, so only the winner is checked
+    got = call(c, train=False)
+    want, _ = reference(c, train=False)
+    assert torch.isfinite(got["out"].float()).all()
+    assert (got["lse"].cpu().double() - want["lse"]).abs().max() <= 1e-5 * want["lse"].abs().max()
+
+
+def test_birds_far_from_the_origin():
+    """Distances come from exact differences, wherever the birds are."""
+    compare(make(9, [200], [200], 4, 4, 64, torch.bfloat16, distance=True, far=(1 << 24) - 16 * 400 - 1))
+
+
+def test_slices_of_one_projection():
+    c = make(10, [90, 45], [90, 45], 4, 2, 64, torch.bfloat16, distance=True)
+    n = 135
+    qkv = torch.zeros(n, 8, 64, dtype=torch.bfloat16, device="cuda")
+    qkv[:, :4], qkv[:, 4:6], qkv[:, 6:] = c["q"].cuda(), c["k"].cuda(), c["v"].cuda()
+    off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    xy, sl = c["q_xy"].cuda(), c["slopes"].cuda()
+    a = flock.attention_frames(qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], off, q_xy=xy, slopes=sl, return_lse=True)
+    b = flock.attention_frames(c["q"].cuda(), c["k"].cuda(), c["v"].cuda(), off, q_xy=xy, slopes=sl, return_lse=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    # every frame attends to the same row of keys (stride 0)
+    one_k, one_v = c["k"][:1].cuda().expand(n, 2, 64), c["v"][:1].cuda().expand(n, 2, 64)
+    got = flock.attention_frames(qkv[:, :4], one_k, one_v, off)
+    assert torch.allclose(got.float(), c["v"][0].cuda().repeat_interleave(2, 0).float().expand(n, 4, 64), rtol=2 ** -7)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows that begin more than 2^32 elements into their tensor."""
+    n, stride = 600, 1 << 23
+    big = torch.empty(n * stride, dtype=torch.bfloat16, device="cuda")
+    c = make(11, [1, 40], [n - 60, 60], 2, 1, 64, torch.bfloat16)
+    k, v = big.as_strided((n, 1, 64), (stride, 64, 1)), big.as_strided((n, 1, 64), (stride, 64, 1), 128)
+    k.copy_(c["k"].cuda())
+    v.copy_(c["v"].cuda())
+    q, go = c["q"].cuda(), c["grad"].cuda()
+    qo, ko = (torch.tensor(c[x], dtype=torch.int32).cuda() for x in ("q_off", "k_off"))
+    out, lse = flock.attention_frames(q, k, v, qo, k_offsets=ko, return_lse=True)
+    dq, dk, dv, _ = flock.attention_frames_backward(go, q, k, v, out, lse, qo, k_offsets=ko)
+    want, bound = reference(c)
+    for name, got in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        ref.check(got, want[name], bound[name], name)
+
+
+def test_same_bits_again_and_in_any_batch():
+    c = make(12, [260, 129, 64], [260, 129, 64], 4, 2, 64, torch.bfloat16, distance=True)
+    a, b = call(c), call(c)
+    for n in a:
+        assert torch.equal(a[n], b[n]), n
+
+
+def test_gradients_against_differences():
+    """Directional derivatives of the 64-bit forward pass."""
+    c = make(13, [20, 13], [20, 13], 2, 1, 16, torch.bfloat16, distance=True, cap=4.0, causal=True, prefix=[3, 0])
+    got = call(c)
+    _, bound = reference(c)
+    gen = torch.Generator().manual_seed(99)
+    eps = 1e-4
+
+    def loss(moved):
+        class Wide(torch.Tensor):
+            pass
+        d = {n: (c[n].double() if n in ("q", "k", "v") else c[n]) for n in c}
+        for n, t in moved.items():
+            d[n] = (d[n].double() if n != "slopes" else d[n].double()) + t
+        ref.UNIT[torch.float64] = 0.0
+        ref.TINY[torch.float64] = 0.0
+        r, _ = ref.attention(d["q"], d["k"], d["v"], d["q_off"], d["k_off"], d["scale"], d["cap"], d["q_xy"], d["k_xy"],
+                             d["slopes"], None, True, d["prefix"])
+        return (r["out"] * c["grad"].double()).sum()
+
+    for name, g in (("q", "dq"), ("k", "dk"), ("v", "dv"), ("slopes", "ds")):
+        step = torch.randn(c[name].shape, generator=gen, dtype=torch.float64)
+        if name == "slopes":
+            step = step * c["slopes"].double()
+        diff = (loss({name: eps * step}) - loss({name: -eps * step})) / (2 * eps)
+        mine = (got[g].cpu().double() * step).sum()
+        room = (bound[g] * step.abs()).sum() + 1e-5 * (1 + diff.abs())
+        assert (mine - diff).abs() <= room, (name, float(mine), float(diff), float(room))
+
+
+def test_on_another_stream():
+    c = make(14, [300], [300], 2, 2, 64, torch.bfloat16)
+    want = call(c, train=False)["out"]
+    d = {n: c[n].cuda() for n in ("q", "k", "v")}
+    off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = flock.attention_frames(d["q"], d["k"], d["v"], off, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_in_a_graph():
+    """Replays equal the eager call, with other work between them."""
+    c = make(15, [1], [5000], 8, 2, 64, torch.bfloat16, distance=True)
+    d = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in c.items()}
+    qo, ko = (torch.tensor(c[x], dtype=torch.int32).cuda() for x in ("q_off", "k_off"))
+
+    def step():
+        o, l = flock.attention_frames(d["q"], d["k"], d["v"], qo, k_offsets=ko, q_xy=d["q_xy"], k_xy=d["k_xy"],
+                                      slopes=d["slopes"], return_lse=True)
+        return (o, l) + flock.attention_frames_backward(d["grad"], d["q"], d["k"], d["v"], o, l, qo, k_offsets=ko,
+                                                        q_xy=d["q_xy"], k_xy=d["k_xy"], slopes=d["slopes"])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for turn in range(3):
+        d["q"].mul_(-1 if turn else 1)
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b)
+
+
+def test_inconsistent_offsets_leave_their_outputs():
+    """A frame whose offsets run backwards or past the end is not read."""
+    c = make(16, [50, 50, 50], [50, 50, 50], 2, 2, 64, torch.bfloat16)
+    q, k, v = (c[n].cuda() for n in "qkv")
+    for off in ([0, 50, 400, 150], [0, 90, 50, 150], [-5, 50, 100, 150]):
+        o = torch.tensor(off, dtype=torch.int32).cuda()
+        out = torch.full_like(q, 7.0)
+        flock.attention_frames(q, k, v, o, out=out)
+        torch.cuda.synchronize()
+        bad = [not (0 <= off[f] <= off[f + 1] <= 150) for f in range(3)]
+        if off[0] == -5:
+            assert (out[:50] == 7).all()
+            assert (out[50:] != 7).any()
+        assert any(bad)
+
+
+def test_empty_calls():
+    z = torch.empty(0, 2, 64, dtype=torch.bfloat16, device="cuda")
+    off0 = torch.zeros(1, dtype=torch.int32, device="cuda")
+    off2 = torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert flock.attention_frames(z, z, z, off0).shape == (0, 2, 64)
+    assert flock.attention_frames(z, z, z, off2).shape == (0, 2, 64)
+    q = torch.ones(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    qo = torch.tensor([0, 1, 3], dtype=torch.int32, device="cuda")
+    out, lse = flock.attention_frames(q, z, z, qo, k_offsets=off2, return_lse=True)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    dq, dk, dv, _ = flock.attention_frames_backward(q, q, z, z, out, lse, qo, k_offsets=off2)
+    assert (dq == 0).all() and dk.shape == (0, 2, 64)
+    dq, dk, dv, _ = flock.attention_frames_backward(z, z, q, q, z, lse[:0], off2, k_offsets=qo)
+    assert (dk == 0).all() and (dv == 0).all()
+
+
+def test_python_refusals():
+    q = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda")
+    off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="dtype"):
+        flock.attention_frames(q.float(), q.float(), q.float(), off)
+    with pytest.raises(ValueError, match="multiple of 8"):
+        flock.attention_frames(q[..., :60].contiguous(), q[..., :60].contiguous(), q[..., :60].contiguous(), off)
+    with pytest.raises(ValueError, match="type and device"):
+        flock.attention_frames(q, q.half(), q.half(), off)
+    with pytest.raises(ValueError, match="contiguous rows"):
+        flock.attention_frames(q[..., ::2], q[..., ::2], q[..., ::2], off)
+    with pytest.raises(ValueError, match="q_offsets"):
+        flock.attention_frames(q, q, q, off.long())
+    with pytest.raises(ValueError, match="q_xy"):
+        flock.attention_frames(q, q, q, off, slopes=torch.ones(2, device="cuda"))
+    with pytest.raises(ValueError, match="keep"):
+        flock.attention_frames(q, q, q, off, keep=torch.ones(4, dtype=torch.bool, device="cuda"))
+    with pytest.raises(ValueError, match="16-byte"):
+        z = torch.zeros(4 * 2 * 64 + 1, dtype=torch.bfloat16, device="cuda")[1:].view(4, 2, 64)
+        flock.attention_frames(z, q, q, off)
+    with pytest.raises(ValueError, match="cap"):
+        flock.attention_frames(q, q, q, off, cap=-1.0)
