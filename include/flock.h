@@ -476,7 +476,7 @@ flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const
  *   dtype          FLOCK_F16 or FLOCK_BF16.
  *   q, k, v        device in, [total_q][q_heads][head_dim] and
  *                  [total_k][kv_heads][head_dim], 16-byte aligned, strides
- *                  multiples of 8.
+ *                  multiples of 8 below 2^24.
  *   n_frames       frames of both batches.
  *   q_offsets, k_offsets   device in, int32[n_frames + 1] each; the same array
  *                  where the birds of a frame attend to each other.

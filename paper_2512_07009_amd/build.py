@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libflock.so")
 SOURCES = ["api.cpp", "cluster.hip", "cluster_big.hip", "density.hip", "heatmap.hip", "roi.hip", "mask.hip",
-           "norm.hip", "rotary.hip", "attention.hip"]
+           "norm.hip", "rotary.hip", "attention.hip", "attention_backward.hip"]
 ARCH = "gfx950"
 
 

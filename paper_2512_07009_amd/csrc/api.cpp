@@ -787,6 +787,9 @@ flock_status check_attention(int32_t dtype, const flock::AttentionArgs &a) {
     if (!std::isfinite(a.cap) || !(a.cap >= 0.0f)) return fail(FLOCK_EINVAL, "cap must be finite and >= 0");
     if (a.q_stride < 0 || a.k_stride < 0 || a.v_stride < 0 || a.q_stride % 8 || a.k_stride % 8 || a.v_stride % 8)
         return fail(FLOCK_EINVAL, "strides of q, k and v must be multiples of 8, >= 0");
+    if (a.q_stride > flock::kAttentionMaxStride || a.k_stride > flock::kAttentionMaxStride ||
+        a.v_stride > flock::kAttentionMaxStride)
+        return fail(FLOCK_EINVAL, "strides of q, k and v above %lld", (long long)flock::kAttentionMaxStride);
     if (a.out_stride < (int64_t)a.q_heads * a.dim || a.out_stride % 8)
         return fail(FLOCK_EINVAL, "out's stride must be a multiple of 8 that holds a row");
     return FLOCK_OK;
@@ -1120,8 +1123,9 @@ flock_status attention_frames_backward(
     if (st != FLOCK_OK) return st;
     a.group = q_heads / kv_heads;
     const int64_t q_row = (int64_t)q_heads * head_dim, kv_row = (int64_t)kv_heads * head_dim;
-    if (grad_out_stride < 0 || grad_out_stride % 8)
-        return fail(FLOCK_EINVAL, "grad_out's stride must be a multiple of 8, >= 0");
+    if (grad_out_stride < 0 || grad_out_stride % 8 || grad_out_stride > flock::kAttentionMaxStride)
+        return fail(FLOCK_EINVAL, "grad_out's stride must be a multiple of 8 in 0..%lld",
+                    (long long)flock::kAttentionMaxStride);
     if (grad_q_stride < q_row || grad_k_stride < kv_row || grad_v_stride < kv_row || grad_q_stride % 8 ||
         grad_k_stride % 8 || grad_v_stride % 8)
         return fail(FLOCK_EINVAL, "strides of grad_q, grad_k and grad_v must be multiples of 8 that hold a row");

@@ -242,6 +242,8 @@ struct RotaryArgs {
 hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);
 
 constexpr int kAttentionMaxDim = 128;
+// 64 rows of a tile lie within 2^31 bytes
+constexpr int64_t kAttentionMaxStride = (1 << 24) - 8;
 
 struct AttentionArgs {
     const void *q, *k, *v;             // [total][heads][dim], strides of birds in elements
