@@ -84,13 +84,8 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
     // any of the workgroup's sees
     int wave_end = sp.nk, wave_all = sp.nk, end = sp.nk;
     if (a.causal) {
-        wave_end = wave_all = limit;
-        for (int d = 16; d > 0; d >>= 1) {
-            wave_end = max(wave_end, __shfl_xor(wave_end, d));
-            wave_all = min(wave_all, __shfl_xor(wave_all, d));
-        }
-        wave_end = __builtin_amdgcn_readfirstlane(wave_end);
-        wave_all = __builtin_amdgcn_readfirstlane(wave_all);
+        wave_end = wave_max(limit);
+        wave_all = -wave_max(-limit);
         const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
         end = (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk);
     }
@@ -101,30 +96,42 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
     // scores stay products of queries and keys until the exponential
     constexpr bool PLAIN = !DIST && !CAP;
     f32x16 s[2];
-    // the scores of a tile; PENALTY: some of its keys are hidden, LIMIT: or not seen by some of the rows
-    auto finish_scores = [&](const typename Tile::Lds &t, int kt, auto penalty, auto limited) {
-        constexpr bool PENALTY = decltype(penalty)::value, LIMIT = decltype(limited)::value;
+    auto finish_scores = [&](const typename Tile::Lds &t) {
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            const uint32_t seen = LIMIT ? seen_bits(0xffffffffu, limit, kt + 32 * sub, h) : 0;
+        for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                float kx[4], ky[4], pen[4] = {};
+                float kx[4], ky[4];
                 if (DIST) {
                     *reinterpret_cast<float4 *>(kx) = read4(t.x, 32 * sub, r, h);
                     *reinterpret_cast<float4 *>(ky) = read4(t.y, 32 * sub, r, h);
                 }
-                if (PENALTY) *reinterpret_cast<float4 *>(pen) = read4(t.penalty, 32 * sub, r, h);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
                     float th;
-                    float v = PLAIN ? s[sub][r + e] + pen[e]
-                                    : score<DIST, CAP>(s[sub][r + e], scale, cap2, d2, slope2, th, pen[e]);
-                    if (LIMIT) v = (seen >> out_row(r + e, 0)) & 1 ? v : -INFINITY;
-                    s[sub][r + e] = v;
+                    s[sub][r + e] = score<DIST, CAP>(s[sub][r + e], scale, cap2, d2, slope2, th);
                 }
             }
+    };
+    auto hide = [&](const typename Tile::Lds &t) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float4 pen = read4(t.penalty, 32 * sub, r, h);
+                s[sub][r] += pen.x;
+                s[sub][r + 1] += pen.y;
+                s[sub][r + 2] += pen.z;
+                s[sub][r + 3] += pen.w;
+            }
+    };
+    auto cut = [&](int kt) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+            const uint32_t seen = seen_bits(0xffffffffu, limit, kt + 32 * sub, h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[sub][r] = (seen >> out_row(r, 0)) & 1 ? s[sub][r] : -INFINITY;
         }
     };
 
@@ -148,9 +155,9 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
 #pragma unroll
                 for (int st = 0; st < DP / 16; ++st)
                     s[sub] = mfma(read_rows<T, DP>(t.k, 32 * sub + col, st, h), q[st], s[sub]);
-            if (kt + kTileKeys > wave_all) finish_scores(t, kt, std::true_type{}, std::true_type{});
-            else if (!all) finish_scores(t, kt, std::true_type{}, std::false_type{});
-            else if (!PLAIN) finish_scores(t, kt, std::false_type{}, std::false_type{});
+            if (!PLAIN) finish_scores(t);
+            if (!all) hide(t);
+            if (kt + kTileKeys > wave_all) cut(kt);
             float top = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);

@@ -40,17 +40,15 @@ __global__ void __launch_bounds__(kThreads) attention_delta_kernel(AttentionBack
     }
 }
 
-// Gradients of the queries: 128 rows a workgroup, over the keys they see.
+// Gradients of the queries: 128 rows a workgroup, 32 a wave, over the tiles of
+// keys that they see.
 template <typename T, int DP, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
-    constexpr int kRows = 128, kKeys = 64;
+    using Tile = KeyTile<DP>;
+    constexpr int kRows = 128;
     const AttentionArgs &a = b.fwd;
-    extern __shared__ i16x8 lds[];
-    i16x8 *const k_lds = lds;
-    i16x8 *const v_lds = lds + kKeys * (DP / 8 + 1);
-    float *const kx = reinterpret_cast<float *>(v_lds + kKeys * (DP / 8 + 1));
-    float *const ky = kx + kKeys;
+    extern __shared__ char shared[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
     const int64_t id = xcd_order(blockIdx.x, gridDim.x);
     const int head = (int)(id / a.slots);
@@ -75,79 +73,110 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         go[s] = load_frag<T>(g_row, s, h, a.dim);
     }
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
-    const int limit = !valid ? 0 : a.causal ? min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    const int limit = valid && a.causal ? (int)min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
     float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
     if (DIST && valid) {
-        qx = (float)a.q_xy[2 * qrow] * kPxPerQuantum;
-        qy = (float)a.q_xy[2 * qrow + 1] * kPxPerQuantum;
+        const int2 place = reinterpret_cast<const int2 *>(a.q_xy)[qrow];
+        qx = (float)place.x * kPxPerQuantum;
+        qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
     const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
     float shift, rest;
     split_lse(valid ? a.lse[qrow * a.q_heads + qh] : -INFINITY, shift, rest);
     const float delta = valid ? b.delta[qrow * a.q_heads + qh] * rest : 0.0f;
-    const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
-    const int end = a.causal ? (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    int wave_end = sp.nk, wave_all = sp.nk, end = sp.nk;
+    if (a.causal) {
+        wave_end = wave_max(limit);
+        wave_all = -wave_max(-limit);
+        const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
+        end = (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk);
+    }
 
     f32x16 dq[DP / 32] = {};
     // sums of P dP, P d2 and P dP d2: the slope's gradient takes delta from the
     // same P, since dS = P (dP - delta) sums to zero only then to 32 bits
     float pdp = 0.0f, pd2 = 0.0f, pdpd2 = 0.0f;
-    for (int kt = 0; kt < end; kt += kKeys) {
-        __syncthreads();
-        auto key_row = [&](const void *base, int64_t stride, int r) -> const short * {
-            const int j = kt + r;
-            if (j >= end || (a.keep && !a.keep[sp.k0 + j])) return nullptr;
-            return static_cast<const short *>(base) + (int64_t)(sp.k0 + j) * stride + head * a.dim;
-        };
-        stage_rows<DP, kKeys>(k_lds, a.dim, [&](int r) { return key_row(a.k, a.k_stride, r); });
-        stage_rows<DP, kKeys>(v_lds, a.dim, [&](int r) { return key_row(a.v, a.v_stride, r); });
-        if (DIST && threadIdx.x < kKeys) {
-            const int j = kt + (int)threadIdx.x;
-            kx[threadIdx.x] = j < end ? (float)a.k_xy[2 * (int64_t)(sp.k0 + j)] * kPxPerQuantum : 0.0f;
-            ky[threadIdx.x] = j < end ? (float)a.k_xy[2 * (int64_t)(sp.k0 + j) + 1] * kPxPerQuantum : 0.0f;
+    auto sub_tile = [&](const typename Tile::Lds &t, int kt, int first, bool hidden, bool limited) {
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int st = 0; st < DP / 16; ++st) {
+            s = mfma(read_rows<T, DP>(t.k, first + col, st, h), q[st], s);
+            dp = mfma(read_rows<T, DP>(t.v, first + col, st, h), go[st], dp);
         }
-        __syncthreads();
+        float d2[DIST ? 16 : 1], th[CAP ? 16 : 1];
 #pragma unroll
-        for (int sub = 0; sub < kKeys / 32; ++sub) {
-            const int k0 = 32 * sub;
-            const int j = kt + k0 + col;
-            const uint32_t bits = (uint32_t)__ballot(h == 0 && j < end && (!a.keep || a.keep[sp.k0 + j]));
-            if (bits == 0) continue;
-            f32x16 s = {}, dp = {};
-#pragma unroll
-            for (int st = 0; st < DP / 16; ++st) {
-                s = mfma(read_rows<T, DP>(k_lds, k0 + col, st, h), q[st], s);
-                dp = mfma(read_rows<T, DP>(v_lds, k0 + col, st, h), go[st], dp);
+        for (int r = 0; r < 16; r += 4) {
+            float kx[4], ky[4];
+            if (DIST) {
+                *reinterpret_cast<float4 *>(kx) = read4(t.x, first, r, h);
+                *reinterpret_cast<float4 *>(ky) = read4(t.y, first, r, h);
             }
-            const uint32_t seen = seen_bits(bits, limit, kt + k0, h);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int kr = k0 + out_row(r, h);
-                float d2 = 0.0f;
-                if (DIST) {
-                    d2 = distance2(qx - kx[kr], qy - ky[kr]);
-                }
-                float th;
-                const float v = score<DIST, CAP>(s[r], scale, cap2, d2, slope2, th);
-                // P / rest; rest is in the other factors
-                const float p = (seen >> out_row(r, 0)) & 1 ? exp2_fast(v - shift) : 0.0f;
-                if (DIST) {
-                    const float pd = p * dp[r];
-                    pdp += pd;
-                    pd2 += p * d2;
-                    pdpd2 += pd * d2;
-                }
-                float ds = p * __builtin_fmaf(dp[r], rest, -delta);
-                if (CAP) ds *= 1.0f - th * th;
-                s[r] = ds;
+            for (int e = 0; e < 4; ++e) {
+                if (DIST) d2[r + e] = distance2(qx - kx[e], qy - ky[e]);
+                s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, DIST ? d2[r + e] : 0.0f, slope2, th[CAP ? r + e : 0]);
             }
+        }
+        if (hidden) {
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const float4 pen = read4(t.penalty, first, r, h);
+                s[r] += pen.x;
+                s[r + 1] += pen.y;
+                s[r + 2] += pen.z;
+                s[r + 3] += pen.w;
+            }
+        }
+        if (limited) {
+            const uint32_t seen = seen_bits(0xffffffffu, limit, kt + first, h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = (seen >> out_row(r, 0)) & 1 ? s[r] : -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float p = exp2_fast(s[r] - shift);  // P / rest; rest is in the other factors
+            if (DIST) {
+                const float pd = p * dp[r];
+                pdp += pd;
+                pd2 = __builtin_fmaf(p, d2[r], pd2);
+                pdpd2 = __builtin_fmaf(pd, d2[r], pdpd2);
+            }
+            float ds = p * __builtin_fmaf(dp[r], rest, -delta);
+            if (CAP) ds *= __builtin_fmaf(-th[r], th[r], 1.0f);
+            s[r] = ds;
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const F d = round_frag<T>(s, part);
 #pragma unroll
             for (int blk = 0; blk < DP / 32; ++blk)
-#pragma unroll
-                for (int part = 0; part < 2; ++part)
-                    dq[blk] = mfma(read_columns<T, DP>(k_lds, k0 + 16 * part, blk, lane), round_frag<T>(s, part), dq[blk]);
+                dq[blk] = mfma(read_columns<T, DP>(t.k, first + 16 * part, blk, lane), d, dq[blk]);
         }
+    };
+
+    Tile next;
+    if (end > 0) {
+        next.template load<DIST>(a, sp, head, 0, end);
+        next.template store<DIST>(a, typename Tile::Lds(shared));
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int kt = 0; kt < end; kt += kTileKeys) {
+        const bool more = kt + kTileKeys < end;
+        if (more) next.template load<DIST>(a, sp, head, kt + kTileKeys, end);
+        const typename Tile::Lds t(shared + buffer * Tile::kBytes);
+        const uint64_t seen = *t.seen;
+        if (kt < wave_end) {
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+                const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
+                if (bits != 0) sub_tile(t, kt, 32 * sub, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
+            }
+        }
+        buffer ^= 1;
+        if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes));
+        __syncthreads();
     }
     if (DIST && b.row_slopes) {
         auto add = [](float x, float y) { return x + y; };
@@ -171,24 +200,120 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         }
 }
 
-// Gradients of keys and values: 128 keys a workgroup, 32 a wave, over the rows
-// that see them.  The products are S = Q K^T and dP = dO V^T here, so that a lane
-// holds one key.
-template <typename T, int DP, bool DIST, bool CAP>
+// A tile of 64 rows (queries of the heads that share a kv head), their output
+// gradients and what their scores need, on its way to LDS as KeyTile is.
+constexpr int kTileRows = 64;
+
+template <int DP>
+struct RowTile {
+    static constexpr int kChunks = DP / 8;
+    static constexpr int kPitch = DP / 8 + 1;
+    static constexpr int kLoads = kTileRows * kChunks / kThreads;
+    static constexpr int kRowChunks = kTileRows * kPitch;
+    static constexpr int kBytes = 2 * kRowChunks * 16 + 7 * kTileRows * 4 + 16;
+
+    struct Lds {
+        i16x8 *q, *g;
+        float *x, *y, *slope, *shift, *delta, *rest;
+        int *limit, *exact;
+        __device__ __forceinline__ explicit Lds(char *base) {
+            q = reinterpret_cast<i16x8 *>(base);
+            g = q + kRowChunks;
+            x = reinterpret_cast<float *>(g + kRowChunks);
+            y = x + kTileRows;
+            slope = y + kTileRows;
+            shift = slope + kTileRows;
+            delta = shift + kTileRows;
+            rest = delta + kTileRows;
+            limit = reinterpret_cast<int *>(rest + kTileRows);
+            exact = limit + kTileRows;
+        }
+    };
+
+    i32x4 q[kLoads], g[kLoads];
+    float x, y, slope, shift, delta, rest;
+    int limit;
+
+    template <bool DIST>
+    __device__ __forceinline__ void load(const AttentionBackwardArgs &b, const Span &sp, int head, int prefix,
+                                         int64_t first, int64_t n_rows) {
+        const AttentionArgs &a = b.fwd;
+        const int64_t i0 = first / a.group;
+        const int g0 = (int)(first - i0 * a.group);
+        const int rows = (int)min(n_rows - first, (int64_t)kTileRows);
+        const int queries = (g0 + rows - 1) / a.group;  // beyond the first
+        const int q_step = (int)a.q_stride * 2, g_step = (int)b.grad_out_stride * 2;
+        const int bytes = a.group * a.dim * 2;
+        const auto qr = tile_resource(a.q, (sp.q0 + i0) * a.q_stride + head * a.group * a.dim, queries * q_step + bytes);
+        const auto gr = tile_resource(b.grad_out, (sp.q0 + i0) * b.grad_out_stride + head * a.group * a.dim,
+                                      queries * g_step + bytes);
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+            const int e = threadIdx.x + n * kThreads;
+            const int r = e / kChunks, c = e % kChunks;
+            const uint32_t i = group_quotient(g0 + r, b.group_reciprocal), gg = g0 + r - i * a.group;
+            const bool in = c * 8 < a.dim && r < rows;
+            q[n] = __builtin_amdgcn_raw_buffer_load_b128(qr, in ? (int)i * q_step + (int)gg * a.dim * 2 + c * 16 : kBeyond, 0, 0);
+            g[n] = __builtin_amdgcn_raw_buffer_load_b128(gr, in ? (int)i * g_step + (int)gg * a.dim * 2 + c * 16 : kBeyond, 0, 0);
+        }
+        if (threadIdx.x < kTileRows) {
+            x = y = slope = delta = rest = 0.0f;
+            shift = INFINITY;
+            limit = 0;
+            if ((int)threadIdx.x < rows) {
+                const uint32_t i = group_quotient(g0 + threadIdx.x, b.group_reciprocal);
+                const int qh = head * a.group + (int)(g0 + threadIdx.x - i * a.group);
+                const int64_t row = sp.q0 + i0 + i;
+                split_lse(a.lse[row * a.q_heads + qh], shift, rest);
+                delta = b.delta[row * a.q_heads + qh];
+                if (DIST) {
+                    const int2 place = reinterpret_cast<const int2 *>(a.q_xy)[row];
+                    x = (float)place.x * kPxPerQuantum;
+                    y = (float)place.y * kPxPerQuantum;
+                    slope = a.slopes[qh] * kLog2e;
+                }
+                limit = a.causal ? (int)min(max((int64_t)prefix, i0 + i + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+            }
+        }
+    }
+
+    template <bool DIST>
+    __device__ __forceinline__ void store(const Lds &lds) const {
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) {
+            const int e = threadIdx.x + n * kThreads;
+            const int at = e / kChunks * kPitch + e % kChunks;
+            lds.q[at] = __builtin_bit_cast(i16x8, q[n]);
+            lds.g[at] = __builtin_bit_cast(i16x8, g[n]);
+        }
+        if (threadIdx.x < kTileRows) {  // the first wave
+            if (DIST) {
+                lds.x[threadIdx.x] = x;
+                lds.y[threadIdx.x] = y;
+                lds.slope[threadIdx.x] = slope;
+            }
+            lds.shift[threadIdx.x] = shift;
+            lds.delta[threadIdx.x] = delta;
+            lds.rest[threadIdx.x] = rest;
+            lds.limit[threadIdx.x] = limit;
+            // rest is 1 to a rounding of the weights, but for large scores (absent rows have P = 0)
+            const bool one = __all(fabsf(rest - 1.0f) < 0x1p-16f || shift == INFINITY);
+            if (threadIdx.x == 0) *lds.exact = one ? 1 : 0;
+        }
+    }
+};
+
+// Gradients of keys and values: 32 BLOCKS keys a wave, over the rows that see
+// them.  The products are S = Q K^T and dP = dO V^T here, so that a lane holds one
+// key (of each block); what is read of a row from LDS serves all blocks, which
+// is what LDS bandwidth asks for where registers allow it.
+template <typename T, int DP, int BLOCKS, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
-    constexpr int kKeys = 128, kRows = 64;
+    using Tile = RowTile<DP>;
+    constexpr int kKeys = 128 * BLOCKS;
     const AttentionArgs &a = b.fwd;
-    extern __shared__ i16x8 lds[];
-    i16x8 *const q_lds = lds;
-    i16x8 *const g_lds = lds + kRows * (DP / 8 + 1);
-    float *const r_shift = reinterpret_cast<float *>(g_lds + kRows * (DP / 8 + 1));
-    float *const r_rest = r_shift + kRows;
-    float *const r_delta = r_rest + kRows;
-    float *const r_x = r_delta + kRows;
-    float *const r_y = r_x + kRows;
-    float *const r_slope = r_y + kRows;
-    int *const r_limit = reinterpret_cast<int *>(r_slope + kRows);
+    extern __shared__ char shared[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
     const int64_t id = xcd_order(blockIdx.x, gridDim.x);
     const int head = (int)(id / b.key_slots);
@@ -199,116 +324,159 @@ __global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) attention_dkv_kern
     const int64_t key0 = tile * kKeys;
     if (key0 >= sp.nk) return;
     const int64_t n_rows = (int64_t)sp.nq * a.group;
-    const int64_t key = key0 + 32 * wave + col;
-    const bool valid = key < sp.nk;
-    const int64_t krow = sp.k0 + (valid ? key : 0);
-    const bool kept = valid && (!a.keep || a.keep[krow]);
-    const short *k_row = kept ? static_cast<const short *>(a.k) + krow * a.k_stride + head * a.dim : nullptr;
-    const short *v_row = kept ? static_cast<const short *>(a.v) + krow * a.v_stride + head * a.dim : nullptr;
-    F k[DP / 16], v[DP / 16];
+    F k[BLOCKS][DP / 16], v[BLOCKS][DP / 16];
+    float kx[BLOCKS], ky[BLOCKS];
+    bool kept[BLOCKS];
+    const int wave_key = (int)key0 + 32 * BLOCKS * wave;  // the wave's first key
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s) {
-        k[s] = load_frag<T>(k_row, s, h, a.dim);
-        v[s] = load_frag<T>(v_row, s, h, a.dim);
-    }
-    float kx = 0.0f, ky = 0.0f;
-    if (DIST && valid) {
-        kx = (float)a.k_xy[2 * krow] * kPxPerQuantum;
-        ky = (float)a.k_xy[2 * krow + 1] * kPxPerQuantum;
+    for (int n = 0; n < BLOCKS; ++n) {
+        const int key = wave_key + 32 * n + col;
+        const bool valid = key < sp.nk;
+        const int64_t krow = sp.k0 + (valid ? key : 0);
+        kept[n] = valid && (!a.keep || a.keep[krow]);
+        const short *k_row = kept[n] ? static_cast<const short *>(a.k) + krow * a.k_stride + head * a.dim : nullptr;
+        const short *v_row = kept[n] ? static_cast<const short *>(a.v) + krow * a.v_stride + head * a.dim : nullptr;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            k[n][s] = load_frag<T>(k_row, s, h, a.dim);
+            v[n][s] = load_frag<T>(v_row, s, h, a.dim);
+        }
+        kx[n] = ky[n] = 0.0f;
+        if (DIST && valid) {
+            const int2 place = reinterpret_cast<const int2 *>(a.k_xy)[krow];
+            kx[n] = (float)place.x * kPxPerQuantum;
+            ky[n] = (float)place.y * kPxPerQuantum;
+        }
     }
     const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     // the first query that sees the workgroup's first key
     int64_t begin = 0;
-    if (a.causal && key0 >= prefix) begin = max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kRows * kRows;
+    if (a.causal && key0 >= prefix)
+        begin = max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows;
 
-    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
-    for (int64_t rt = begin; rt < n_rows; rt += kRows) {
-        __syncthreads();
-        auto row_of = [&](const void *base, int64_t stride, int r) -> const short * {
-            const int64_t row = rt + r;
-            if (row >= n_rows) return nullptr;
-            return static_cast<const short *>(base) + (sp.q0 + row / a.group) * stride +
-                   (head * a.group + (int)(row % a.group)) * a.dim;
-        };
-        stage_rows<DP, kRows>(q_lds, a.dim, [&](int r) { return row_of(a.q, a.q_stride, r); });
-        stage_rows<DP, kRows>(g_lds, a.dim, [&](int r) { return row_of(b.grad_out, b.grad_out_stride, r); });
-        if (threadIdx.x < kRows) {
-            const int64_t row = rt + threadIdx.x;
-            float shift = INFINITY, rest = 0.0f, delta = 0.0f, x = 0.0f, y = 0.0f, slope2 = 0.0f;
-            int limit = 0;
-            if (row < n_rows) {
-                const int64_t i = row / a.group;
-                const int qh = head * a.group + (int)(row % a.group);
-                split_lse(a.lse[(sp.q0 + i) * a.q_heads + qh], shift, rest);
-                delta = b.delta[(sp.q0 + i) * a.q_heads + qh];
-                if (DIST) {
-                    x = (float)a.q_xy[2 * (sp.q0 + i)] * kPxPerQuantum;
-                    y = (float)a.q_xy[2 * (sp.q0 + i) + 1] * kPxPerQuantum;
-                    slope2 = a.slopes[qh] * kLog2e;
-                }
-                limit = a.causal ? (int)min(max((int64_t)prefix, i + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
-            }
-            r_shift[threadIdx.x] = shift;
-            r_rest[threadIdx.x] = rest;
-            r_delta[threadIdx.x] = delta;
-            r_x[threadIdx.x] = x;
-            r_y[threadIdx.x] = y;
-            r_slope[threadIdx.x] = slope2;
-            r_limit[threadIdx.x] = limit;
-        }
-        __syncthreads();
+    f32x16 dk[BLOCKS][DP / 32] = {}, dv[BLOCKS][DP / 32] = {};
+    auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact) {
+        F qf[DP / 16], gf[DP / 16];
 #pragma unroll
-        for (int sub = 0; sub < kRows / 32; ++sub) {
-            const int r0 = 32 * sub;
+        for (int st = 0; st < DP / 16; ++st) {
+            qf[st] = read_rows<T, DP>(t.q, first + col, st, h);
+            gf[st] = read_rows<T, DP>(t.g, first + col, st, h);
+        }
+        F p[BLOCKS][2], ds[BLOCKS][2];
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int st = 0; st < DP / 16; ++st) {
-                s = mfma(read_rows<T, DP>(q_lds, r0 + col, st, h), k[st], s);
-                dp = mfma(read_rows<T, DP>(g_lds, r0 + col, st, h), v[st], dp);
+                s = mfma(qf[st], k[n][st], s);
+                dp = mfma(gf[st], v[n][st], dp);
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int rr = r0 + out_row(r, h);
-                float th, d2 = 0.0f;
-                if (DIST) d2 = distance2(r_x[rr] - kx, r_y[rr] - ky);
-                const float z = score<DIST, CAP>(s[r], scale, cap2, d2, DIST ? r_slope[rr] : 0.0f, th);
-                float p = exp2_fast(z - r_shift[rr]) * r_rest[rr];
-                if (a.causal && key >= r_limit[rr]) p = 0.0f;
-                float ds = p * (dp[r] - r_delta[rr]);
-                if (CAP) ds *= 1.0f - th * th;
-                s[r] = p;
-                dp[r] = ds;
-            }
-#pragma unroll
-            for (int blk = 0; blk < DP / 32; ++blk)
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    dv[blk] = mfma(read_columns<T, DP>(g_lds, r0 + 16 * part, blk, lane), round_frag<T>(s, part), dv[blk]);
-                    dk[blk] = mfma(read_columns<T, DP>(q_lds, r0 + 16 * part, blk, lane), round_frag<T>(dp, part), dk[blk]);
+            for (int r = 0; r < 16; r += 4) {
+                float x[4], y[4], slope[4] = {}, shift[4], delta[4];
+                if (DIST) {
+                    *reinterpret_cast<float4 *>(x) = read4(t.x, first, r, h);
+                    *reinterpret_cast<float4 *>(y) = read4(t.y, first, r, h);
+                    *reinterpret_cast<float4 *>(slope) = read4(t.slope, first, r, h);
                 }
-        }
-    }
-    if (!valid) return;
-    // a hidden key's scores are not masked above: its gradients are zero
-    T *dk_out = static_cast<T *>(b.grad_k) + krow * b.grad_k_stride + head * a.dim;
-    T *dv_out = static_cast<T *>(b.grad_v) + krow * b.grad_v_stride + head * a.dim;
-#pragma unroll
-    for (int blk = 0; blk < DP / 32; ++blk)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int d = 32 * blk + out_row(r, h);
-            if (d < a.dim) {
-                float x[4], y[4];
+                *reinterpret_cast<float4 *>(shift) = read4(t.shift, first, r, h);
+                *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    x[e] = kept ? dk[blk][r + e] * a.scale : 0.0f;
-                    y[e] = kept ? dv[blk][r + e] : 0.0f;
+                    const float d2 = DIST ? distance2(x[e] - kx[n], y[e] - ky[n]) : 0.0f;
+                    float th;
+                    const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e], th);
+                    s[r + e] = exp2_fast(z - shift[e]);
+                    float d = s[r + e] * (dp[r + e] - delta[e]);
+                    if (CAP) d *= __builtin_fmaf(-th, th, 1.0f);
+                    dp[r + e] = d;
                 }
-                store_pack<T, 4>(dk_out + d, x);
-                store_pack<T, 4>(dv_out + d, y);
+            }
+            if (limited) {
+                const int key = wave_key + 32 * n + col;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (key >= t.limit[first + out_row(r, h)]) s[r] = dp[r] = 0.0f;
+            }
+            if (!exact) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float rest = t.rest[first + out_row(r, h)];
+                    s[r] *= rest;
+                    dp[r] *= rest;
+                }
+            }
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                p[n][part] = round_frag<T>(s, part);
+                ds[n][part] = round_frag<T>(dp, part);
             }
         }
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+            for (int blk = 0; blk < DP / 32; ++blk) {
+                const F gc = read_columns<T, DP>(t.g, first + 16 * part, blk, lane);
+                const F qc = read_columns<T, DP>(t.q, first + 16 * part, blk, lane);
+#pragma unroll
+                for (int n = 0; n < BLOCKS; ++n) {
+                    dv[n][blk] = mfma(gc, p[n][part], dv[n][blk]);
+                    dk[n][blk] = mfma(qc, ds[n][part], dk[n][blk]);
+                }
+            }
+    };
+
+    Tile next;
+    if (begin < n_rows) {
+        next.template load<DIST>(b, sp, head, prefix, begin, n_rows);
+        next.template store<DIST>(typename Tile::Lds(shared));
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int64_t rt = begin; rt < n_rows; rt += kTileRows) {
+        const bool more = rt + kTileRows < n_rows;
+        if (more) next.template load<DIST>(b, sp, head, prefix, rt + kTileRows, n_rows);
+        const typename Tile::Lds t(shared + buffer * Tile::kBytes);
+        const bool exact = __builtin_amdgcn_readfirstlane(*t.exact) != 0;
+        // limits grow with the rows: those of the first and of the last row say which keys all and some rows see
+        const int64_t last = min(rt + kTileRows, n_rows) - 1;
+        const int some = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[(int)(last - rt)]) : sp.nk;
+        const int all = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[0]) : sp.nk;
+        if (wave_key < some) {
+#pragma unroll 1
+            for (int sub = 0; sub < kTileRows / 32; ++sub)
+                sub_tile(t, 32 * sub, min(wave_key + 32 * BLOCKS, sp.nk) > all, exact);
+        }
+        buffer ^= 1;
+        if (more) next.template store<DIST>(typename Tile::Lds(shared + buffer * Tile::kBytes));
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < BLOCKS; ++n) {
+        const int key = wave_key + 32 * n + col;
+        if (key >= sp.nk) continue;
+        const int64_t krow = sp.k0 + key;
+        T *dk_out = static_cast<T *>(b.grad_k) + krow * b.grad_k_stride + head * a.dim;
+        T *dv_out = static_cast<T *>(b.grad_v) + krow * b.grad_v_stride + head * a.dim;
+#pragma unroll
+        for (int blk = 0; blk < DP / 32; ++blk)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int d = 32 * blk + out_row(r, h);
+                if (d < a.dim) {
+                    // a hidden key's scores are not masked above: its gradients are zero
+                    float x[4], y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = kept[n] ? dk[n][blk][r + e] * a.scale : 0.0f;
+                        y[e] = kept[n] ? dv[n][blk][r + e] : 0.0f;
+                    }
+                    store_pack<T, 4>(dk_out + d, x);
+                    store_pack<T, 4>(dv_out + d, y);
+                }
+            }
+    }
 }
 
 // Gradient of a head's slope: the queries' shares, a block per head and part
@@ -353,7 +521,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
     b.row_slopes = grad_slopes ? reinterpret_cast<float *>(ws + align256(all * sizeof(float))) : nullptr;
     double *parts = reinterpret_cast<double *>(ws + 2 * align256(all * sizeof(float)));
     a.slots = (int64_t)a.total_q * a.group / 128 + a.n_frames;
-    b.key_slots = (int64_t)a.total_k / 128 + a.n_frames;
+    b.group_reciprocal = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0;
     hipError_t err = hipSuccess;
     if (a.total_q > 0) {
         const dim3 grid((uint32_t)((all + 15) / 16));
@@ -368,15 +536,17 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
         constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
         hipError_t e = hipSuccess;
         if (a.total_q > 0) {
-            constexpr size_t bytes = 2 * 64 * (DP + 8) * 2 + 2 * 64 * 4;
+            constexpr size_t bytes = 2 * KeyTile<DP>::kBytes;
             auto kernel = attention_dq_kernel<T, DP, DIST, CAP>;
             hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.slots * a.kv_heads)), dim3(kThreads), bytes, stream, b);
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
         if (a.total_k > 0) {
-            constexpr size_t bytes = 2 * 64 * (DP + 8) * 2 + 7 * 64 * 4;
-            auto kernel = attention_dkv_kernel<T, DP, DIST, CAP>;
+            constexpr size_t bytes = 2 * RowTile<DP>::kBytes;
+            constexpr int kBlocks = 1;
+            b.key_slots = (int64_t)a.total_k / (128 * kBlocks) + a.n_frames;
+            auto kernel = attention_dkv_kernel<T, DP, kBlocks, DIST, CAP>;
             hipLaunchKernelGGL(kernel, dim3((uint32_t)(b.key_slots * a.kv_heads)), dim3(kThreads), bytes, stream, b);
             e = hipGetLastError();
         }

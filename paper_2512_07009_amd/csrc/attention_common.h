@@ -43,6 +43,16 @@ __device__ __forceinline__ float tanh_fast(float x) {
     return 1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_fast(2.0f * kLog2e * x) + 1.0f);
 }
 
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) x = max(x, __shfl_xor(x, d));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// n / group for m = ceil(2^32 / group), 0 for a group of one: exact for
+// n < 2^16, group <= 256.
+__device__ __forceinline__ uint32_t group_quotient(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
+
 // Row (of 32) that register r of a lane in half h holds of a product.
 __device__ __forceinline__ constexpr int out_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
@@ -265,14 +275,13 @@ __device__ __forceinline__ float4 read4(const float *p, int first, int r, int h)
 __device__ __forceinline__ float distance2(float dx, float dy) { return __builtin_fmaf(dx, dx, dy * dy); }
 
 template <bool DIST, bool CAP>
-__device__ __forceinline__ float score(float qk, float scale, float cap2, float d2, float slope2, float &th,
-                                       float penalty = 0.0f) {
+__device__ __forceinline__ float score(float qk, float scale, float cap2, float d2, float slope2, float &th) {
     float s;
     if (CAP) {
         th = tanh_fast(qk * scale);  // scale holds scale / cap
-        s = __builtin_fmaf(cap2, th, penalty);
+        s = cap2 * th;
     } else {
-        s = __builtin_fmaf(qk, scale, penalty);  // scale holds scale * log2 e
+        s = qk * scale;              // scale holds scale * log2 e
     }
     if (DIST) s = __builtin_fmaf(-slope2, d2, s);
     return s;

@@ -283,6 +283,7 @@ struct AttentionBackwardArgs {
     int64_t grad_out_stride, grad_q_stride, grad_k_stride, grad_v_stride;
     float *delta, *row_slopes;         // set by launch_attention_backward: [total_q][q_heads]
     int64_t key_slots;
+    uint32_t group_reciprocal;
 };
 size_t attention_backward_workspace_bytes(int32_t total_q, int32_t q_heads);
 hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, void *workspace, float *grad_slopes,
