@@ -223,21 +223,17 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
 
 template <int DP>
 constexpr int split_lds_bytes() {
-    const int bytes = 2 * 128 * (DP + 8) * 2 + 2 * 128 * 4;
     const int join = 4 * 32 * (DP + 2) * 4;
-    return join > bytes ? join : bytes;
+    const int tiles = KeyTile<DP, 128>::kBytes + 32 * KeyTile<DP>::kPitch * 16;
+    return join > tiles ? join : tiles;
 }
 
 template <typename T, int DP, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionArgs a) {
     using F = typename Frag<T>::type;
-    constexpr int kRows = 32;
-    constexpr int kKeys = 128;
-    extern __shared__ i16x8 lds[];
-    i16x8 *const k_lds = lds;
-    i16x8 *const v_lds = lds + kKeys * (DP / 8 + 1);
-    float *const kx = reinterpret_cast<float *>(v_lds + kKeys * (DP / 8 + 1));
-    float *const ky = kx + kKeys;
+    constexpr int kRows = 32, kKeys = 128;
+    using Tile = KeyTile<DP, kKeys>;
+    extern __shared__ char shared[];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
     const int64_t id = xcd_order(blockIdx.x, gridDim.x);
@@ -251,98 +247,113 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
     const int64_t row0 = tile * kRows;
     if (row0 >= n_rows) return;
 
-    // this lane's query
-    const int64_t row = row0 + col;
-    const bool valid = row < n_rows;
-    const int qi = valid ? (int)(row / a.group) : 0, g = valid ? (int)(row % a.group) : 0;
-    const int qh = head * a.group + g;
-    const short *q_row = valid ? static_cast<const short *>(a.q) + (int64_t)(sp.q0 + qi) * a.q_stride + qh * a.dim
-                               : nullptr;
-    F q[DP / 16];
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) q[s] = load_frag<T>(q_row, s, h, a.dim);
-    const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
-    const int limit = !valid ? 0 : a.causal ? min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
-    float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
-    if (DIST && valid) {
-        qx = (float)a.q_xy[2 * (int64_t)(sp.q0 + qi)] * kPxPerQuantum;
-        qy = (float)a.q_xy[2 * (int64_t)(sp.q0 + qi) + 1] * kPxPerQuantum;
-        slope2 = a.slopes[qh] * kLog2e;
-    }
-    const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
-
     // keys that any of the workgroup's rows sees
+    const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
     int end = a.causal ? (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
     int begin = 0;
     if (a.splits > 1) {
         const int per = ((sp.nk + a.splits - 1) / a.splits + kKeys - 1) / kKeys * kKeys;
-        begin = min((int64_t)split * per, (int64_t)end);
-        end = min(begin + (int64_t)per, (int64_t)end);
+        begin = (int)min((int64_t)split * per, (int64_t)end);
+        end = (int)min(begin + (int64_t)per, (int64_t)end);
     }
+    Tile next;
+    if (begin < end) next.template load<DIST>(a, sp, head, begin, end);
+
+    // this lane's query
+    const int64_t row = row0 + col;
+    const bool valid = row < n_rows;
+    const int qi = valid ? (int)(row / a.group) : 0, g = valid ? (int)(row % a.group) : 0;
+    const int qh = head * a.group + g;
+    // the rows stay in LDS: the loads in flight take the registers
+    i16x8 *const q_lds = reinterpret_cast<i16x8 *>(shared + Tile::kBytes);
+    for (int e = threadIdx.x; e < kRows * Tile::kChunks; e += kThreads) {
+        const int r = e / Tile::kChunks, c = e % Tile::kChunks;
+        i16x8 z = {};
+        if (row0 + r < n_rows && c * 8 < a.dim) {
+            const int64_t i = sp.q0 + (row0 + r) / a.group;
+            const int hh = head * a.group + (int)((row0 + r) % a.group);
+            z = *reinterpret_cast<const i16x8 *>(static_cast<const short *>(a.q) + i * a.q_stride + hh * a.dim + c * 8);
+        }
+        q_lds[r * Tile::kPitch + c] = z;
+    }
+    const int limit = valid && a.causal ? (int)min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    const int all_end = a.causal ? -wave_max(-limit) : sp.nk;
+    float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
+    if (DIST && valid) {
+        const int2 place = reinterpret_cast<const int2 *>(a.q_xy)[sp.q0 + qi];
+        qx = (float)place.x * kPxPerQuantum;
+        qy = (float)place.y * kPxPerQuantum;
+        slope2 = a.slopes[qh] * kLog2e;
+    }
+    const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
 
     f32x16 o[DP / 32] = {};
-    float m = -INFINITY, l = 0.0f;
+    float m = -INFINITY, shift = 0.0f, l = 0.0f;
+    const typename Tile::Lds t(shared);
+    const int k0 = 32 * wave;
     for (int kt = begin; kt < end; kt += kKeys) {
+        if (kt > begin) __syncthreads();
+        next.template store<DIST>(a, t);
         __syncthreads();
-        auto key_row = [&](const void *base, int64_t stride, int r) -> const short * {
-            const int j = kt + r;
-            if (j >= end || (a.keep && !a.keep[sp.k0 + j])) return nullptr;
-            return static_cast<const short *>(base) + (int64_t)(sp.k0 + j) * stride + head * a.dim;
-        };
-        stage_rows<DP, kKeys>(k_lds, a.dim, [&](int r) { return key_row(a.k, a.k_stride, r); });
-        stage_rows<DP, kKeys>(v_lds, a.dim, [&](int r) { return key_row(a.v, a.v_stride, r); });
-        if (DIST && threadIdx.x < kKeys) {
-            const int j = kt + (int)threadIdx.x;
-            kx[threadIdx.x] = j < end ? (float)a.k_xy[2 * (int64_t)(sp.k0 + j)] * kPxPerQuantum : 0.0f;
-            ky[threadIdx.x] = j < end ? (float)a.k_xy[2 * (int64_t)(sp.k0 + j) + 1] * kPxPerQuantum : 0.0f;
-        }
-        __syncthreads();
-            const int k0 = 32 * wave;
-            const int j = kt + k0 + col;
-            const uint32_t bits = (uint32_t)__ballot(h == 0 && j < end && (!a.keep || a.keep[sp.k0 + j]));
-            if (bits == 0) continue;
-            f32x16 s = {};
+        if (kt + kKeys < end) next.template load<DIST>(a, sp, head, kt + kKeys, end);
+        const uint32_t bits = __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t *>(t.seen)[wave]);
+        if (bits == 0) continue;
+        f32x16 s = {};
 #pragma unroll
-            for (int st = 0; st < DP / 16; ++st) s = mfma(read_rows<T, DP>(k_lds, k0 + col, st, h), q[st], s);
-            const uint32_t seen = seen_bits(bits, limit, kt + k0, h);
-            float top = -INFINITY;
+        for (int st = 0; st < DP / 16; ++st) 
+            s = mfma(read_rows<T, DP>(t.k, k0 + col, st, h), read_rows<T, DP>(q_lds, col, st, h), s);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int kr = k0 + out_row(r, h);
-                float d2 = 0.0f;
-                if (DIST) {
-                    d2 = distance2(qx - kx[kr], qy - ky[kr]);
-                }
-                float th;
-                const float v = score<DIST, CAP>(s[r], scale, cap2, d2, slope2, th);
-                s[r] = (seen >> out_row(r, 0)) & 1 ? v : -INFINITY;
-                top = fmaxf(top, s[r]);
+        for (int r = 0; r < 16; r += 4) {
+            float kx[4], ky[4], pen[4] = {};
+            if (DIST) {
+                *reinterpret_cast<float4 *>(kx) = read4(t.x, k0, r, h);
+                *reinterpret_cast<float4 *>(ky) = read4(t.y, k0, r, h);
             }
-            top = across(top, [](float x, float y) { return fmaxf(x, y); });
-            const float m_new = fmaxf(m, top);
-            const float shift = m_new == -INFINITY ? 0.0f : m_new;
-            const float fade = exp2_fast(m - shift);
-            m = m_new;
+            if (bits != 0xffffffffu) *reinterpret_cast<float4 *>(pen) = read4(t.penalty, k0, r, h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
+                float th;
+                s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope2, th) + pen[e];
+            }
+        }
+        if (kt + k0 + 32 > all_end) {
+            const uint32_t seen = seen_bits(0xffffffffu, limit, kt + k0, h);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = (seen >> out_row(r, 0)) & 1 ? s[r] : -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+        top = across(top, [](float x, float y) { return fmaxf(x, y); });
+        if (__any(top > m + kSlack)) {
+            m = fmaxf(m, top);
+            const float to = m == -INFINITY ? 0.0f : m;
+            const float fade = exp2_fast(fminf(shift - to, 0.0f));
+            shift = to;
             l *= fade;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = exp2_fast(s[r] - shift);
-                l += s[r];
-            }
-#pragma unroll
-            for (int b = 0; b < DP / 32; ++b) {
+            for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[b][r] *= fade;
+        }
 #pragma unroll
-                for (int part = 0; part < 2; ++part)
-                    o[b] = mfma(read_columns<T, DP>(v_lds, k0 + 16 * part, b, lane), round_frag<T>(s, part), o[b]);
-            }
+        for (int r = 0; r < 16; ++r) {
+            s[r] = exp2_fast(s[r] - shift);
+            l += s[r];
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const F p = round_frag<T>(s, part);
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b) o[b] = mfma(read_columns<T, DP>(t.v, k0 + 16 * part, b, lane), p, o[b]);
+        }
     }
     l = across(l, [](float x, float y) { return x + y; });
 
     // join the waves' shares of the keys
-    float *const join = reinterpret_cast<float *>(lds);
+    float *const join = reinterpret_cast<float *>(shared);
     constexpr int kPitch = DP + 2;
     __syncthreads();
     {
@@ -352,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
 #pragma unroll
             for (int r = 0; r < 16; ++r) mine[32 * b + out_row(r, h)] = o[b][r];
         if (h == 0) {
-            mine[DP] = m;
+            mine[DP] = m == -INFINITY ? m : shift;
             mine[DP + 1] = l;
         }
     }

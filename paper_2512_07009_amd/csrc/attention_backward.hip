@@ -308,7 +308,7 @@ struct RowTile {
 // key (of each block); what is read of a row from LDS serves all blocks, which
 // is what LDS bandwidth asks for where registers allow it.
 template <typename T, int DP, int BLOCKS, bool DIST, bool CAP>
-__global__ void __launch_bounds__(kThreads, DP <= 96 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
+__global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = RowTile<DP>;
     constexpr int kKeys = 128 * BLOCKS;

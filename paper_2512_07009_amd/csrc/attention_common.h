@@ -160,16 +160,16 @@ __device__ __forceinline__ uint32_t seen_bits(uint32_t bits, int limit, int firs
     return bits >> (4 * h);
 }
 
-// A tile of 64 keys and its values on its way from memory to LDS: load() starts
+// A tile of 64 keys (or KEYS) and its values on its way from memory to LDS: load() starts
 // the loads into registers, so that they run under the products of the tile
 // before, store() puts them into an LDS buffer.  Hidden and absent keys become
 // zeros there and get a penalty of -infinity on their scores, so that nothing
-// else need tell them apart; `seen` has a bit for each key that takes part.
+// else need tell them apart; `seen` has a bit for each key that takes part, 64 a word.
 //
 // A tile is one buffer resource whose end is the end of its last key, so that
 // loads beyond it (absent keys, dimensions beyond the head's, which are sent
 // there) return zeros without a test; offsets within it stay below 2^31
-// (kMaxStride), tiles begin at 64-bit addresses.
+// (kAttentionMaxStride), tiles begin at 64-bit addresses.
 constexpr int kTileKeys = 64;
 constexpr int kBeyond = 0x7ffffff0;
 
@@ -180,13 +180,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_resource(const void *base
         const_cast<short *>(static_cast<const short *>(base) + first_element), 0, bytes, 0x00027000);
 }
 
-template <int DP>
+template <int DP, int KEYS = kTileKeys>
 struct KeyTile {
     static constexpr int kChunks = DP / 8;                       // of 16 bytes in a row
     static constexpr int kPitch = DP / 8 + 1;                    // LDS row, one chunk of padding
-    static constexpr int kLoads = kTileKeys * kChunks / kThreads;
-    static constexpr int kRowChunks = kTileKeys * kPitch;
-    static constexpr int kBytes = 2 * kRowChunks * 16 + 3 * kTileKeys * 4 + 16;
+    static constexpr int kLoads = KEYS * kChunks / kThreads;
+    static constexpr int kRowChunks = KEYS * kPitch;
+    static constexpr int kBytes = 2 * kRowChunks * 16 + 3 * KEYS * 4 + 16;
 
     struct Lds {
         i16x8 *k, *v;
@@ -196,24 +196,25 @@ struct KeyTile {
             k = reinterpret_cast<i16x8 *>(base);
             v = k + kRowChunks;
             x = reinterpret_cast<float *>(v + kRowChunks);
-            y = x + kTileKeys;
-            penalty = y + kTileKeys;
-            seen = reinterpret_cast<uint64_t *>(penalty + kTileKeys);
+            y = x + KEYS;
+            penalty = y + KEYS;
+            seen = reinterpret_cast<uint64_t *>(penalty + KEYS);
         }
     };
 
     i32x4 k[kLoads], v[kLoads];
-    uint8_t kept[kLoads];
+    uint32_t kept;  // a bit per load
     int2 place;
     bool key_kept;
 
     template <bool DIST>
     __device__ __forceinline__ void load(const AttentionArgs &a, const Span &sp, int head, int first, int end) {
-        const int rows = min(end - first, kTileKeys);
+        const int rows = min(end - first, KEYS);
         const int64_t row0 = sp.k0 + first;
         const int k_step = (int)a.k_stride * 2, v_step = (int)a.v_stride * 2;
         const auto kr = tile_resource(a.k, row0 * a.k_stride + head * a.dim, (rows - 1) * k_step + a.dim * 2);
         const auto vr = tile_resource(a.v, row0 * a.v_stride + head * a.dim, (rows - 1) * v_step + a.dim * 2);
+        kept = 0;
         constexpr bool kEven = kThreads % kChunks == 0;  // a thread's loads are of one column
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
@@ -223,9 +224,9 @@ struct KeyTile {
             const int more = kEven ? n * (kThreads / kChunks) : 0;
             k[n] = __builtin_amdgcn_raw_buffer_load_b128(kr, in ? r * k_step + c * 16 : kBeyond, more * k_step, 0);
             v[n] = __builtin_amdgcn_raw_buffer_load_b128(vr, in ? r * v_step + c * 16 : kBeyond, more * v_step, 0);
-            if (a.keep) kept[n] = r + more < rows ? a.keep[row0 + r + more] : 0;
+            if (a.keep && r + more < rows && a.keep[row0 + r + more]) kept |= 1u << n;
         }
-        if (threadIdx.x < kTileKeys) {
+        if (threadIdx.x < KEYS) {
             key_kept = false;
             place = make_int2(0, 0);
             if ((int)threadIdx.x < rows) {
@@ -240,7 +241,7 @@ struct KeyTile {
         if (a.keep) {
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
-                if (!kept[n]) k[n] = v[n] = i32x4{0, 0, 0, 0};
+                if (!(kept >> n & 1)) k[n] = v[n] = i32x4{0, 0, 0, 0};
             }
         }
 #pragma unroll
@@ -250,14 +251,14 @@ struct KeyTile {
             lds.k[at] = __builtin_bit_cast(i16x8, k[n]);
             lds.v[at] = __builtin_bit_cast(i16x8, v[n]);
         }
-        if (threadIdx.x < kTileKeys) {  // the first wave
+        if (threadIdx.x < KEYS) {  // whole waves
             if (DIST) {
                 lds.x[threadIdx.x] = (float)place.x * kPxPerQuantum;
                 lds.y[threadIdx.x] = (float)place.y * kPxPerQuantum;
             }
             lds.penalty[threadIdx.x] = key_kept ? 0.0f : -INFINITY;
             const uint64_t seen = __ballot(key_kept);
-            if (threadIdx.x == 0) *lds.seen = seen;
+            if ((threadIdx.x & 63) == 0) lds.seen[threadIdx.x >> 6] = seen;
         }
     }
 };
