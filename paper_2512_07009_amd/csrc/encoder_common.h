@@ -14,9 +14,10 @@ namespace flock {
 using half_t = _Float16;
 using bf16_t = __bf16;
 
-// N elements moved by loads or stores of 16 bytes at most.
+// N elements moved by loads or stores of 16 bytes at most.  Memory may hold a
+// pack at any element: the hardware's wide accesses need no more.
 template <typename T, int N>
-struct alignas(sizeof(T) * N < 16 ? sizeof(T) * N : 16) Pack {
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
     T v[N];
 };
 
@@ -33,6 +34,28 @@ __device__ __forceinline__ void store_pack(T *p, const float (&in)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) a.v[i] = static_cast<T>(in[i]);
     *reinterpret_cast<Pack<T, N> *>(p) = a;
+}
+
+// The first n (of N) elements of a pack, zeros after them.
+template <typename T, int N>
+__device__ __forceinline__ void load_some(const T *p, int n, float (&out)[N]) {
+    if (n >= N) {
+        load_pack<T, N>(p, out);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = i < n ? static_cast<float>(p[i]) : 0.0f;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_some(T *p, int n, const float (&in)[N]) {
+    if (n >= N) {
+        store_pack<T, N>(p, in);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < n) p[i] = static_cast<T>(in[i]);
 }
 
 // fn(T{}) with the element type of `dtype`.

@@ -236,7 +236,7 @@ struct RotaryArgs {
     int32_t n_time, n_y, pairs;        // pairs = n_time + n_y + n_x
     int32_t interleaved, inverse;
     int32_t tail, birds_per_block;     // set by launch_rotary
-    uint32_t chunk_reciprocal, head_reciprocal;
+    uint32_t chunk_reciprocal, head_reciprocal, pair_reciprocal;
     uint64_t step[kRotaryMaxPairs];    // 2^-64 turns per unit
 };
 hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);

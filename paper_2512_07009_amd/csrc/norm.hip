@@ -49,12 +49,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
         const int c = (i * TPR + lane) * VEC;
-        if (c < width) {
-            load_pack<T, VEC>(x + c, h[i]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) h[i][e] = 0.0f;
-        }
+        load_some<T, VEC>(x + c, width - c, h[i]);
     }
     if (a.residual) {
         const T *r = static_cast<const T *>(a.residual) + row * a.residual_stride;
@@ -62,14 +57,12 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
             const int c = (i * TPR + lane) * VEC;
-            if (c < width) {
-                float t[VEC];
-                load_pack<T, VEC>(r + c, t);
-                // what is normalised is the sum as it is kept
+            float t[VEC];
+            load_some<T, VEC>(r + c, width - c, t);
+            // what is normalised is the sum as it is kept
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) h[i][e] = static_cast<float>(static_cast<T>(h[i][e] + t[e]));
-                store_pack<T, VEC>(s + c, h[i]);
-            }
+            for (int e = 0; e < VEC; ++e) h[i][e] = static_cast<float>(static_cast<T>(h[i][e] + t[e]));
+            store_some<T, VEC>(s + c, width - c, h[i]);
         }
     }
 #pragma unroll
@@ -80,12 +73,11 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
     float sq = 0.0f;
 #pragma unroll
     for (int i = 0; i < ITER; ++i) {
-        if ((i * TPR + lane) * VEC < width) {
+        const int c = (i * TPR + lane) * VEC;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                h[i][e] -= mean;
-                sq += h[i][e] * h[i][e];
-            }
+        for (int e = 0; e < VEC; ++e) {
+            h[i][e] -= mean;
+            if (c + e < width) sq += h[i][e] * h[i][e];
         }
     }
     const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, sums[1]) / (float)width + a.eps);
@@ -102,16 +94,16 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) o[e] = h[i][e] * rstd;
             if (a.weight) {
-                load_pack<float, VEC>(a.weight + c, w);
+                load_some<float, VEC>(a.weight + c, width - c, w);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) o[e] *= w[e];
             }
             if (a.bias) {
-                load_pack<float, VEC>(a.bias + c, w);
+                load_some<float, VEC>(a.bias + c, width - c, w);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) o[e] += w[e];
             }
-            store_pack<T, VEC>(y + c, o);
+            store_some<T, VEC>(y + c, width - c, o);
         }
     }
 }
@@ -172,7 +164,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormBackwardArg
             dw[i][e] = db[i][e] = 0.0f;
             w[i][e] = 1.0f;
         }
-        if (a.weight && c < width) load_pack<float, VEC>(a.weight + c, w[i]);
+        if (a.weight) load_some<float, VEC>(a.weight + c, width - c, w[i]);
     }
     int turn = 0;
     for (int64_t row = (int64_t)blockIdx.x * kGroups + group; row < a.rows; row += (int64_t)gridDim.x * kGroups) {
@@ -184,16 +176,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormBackwardArg
 #pragma unroll
         for (int i = 0; i < ITER; ++i) {
             const int c = (i * TPR + lane) * VEC;
-            if (c < width) {
-                load_pack<T, VEC>(x + c, xh[i]);
-                load_pack<T, VEC>(gy + c, g[i]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    xh[i][e] = mean;
-                    g[i][e] = 0.0f;
-                }
-            }
+            load_some<T, VEC>(x + c, width - c, xh[i]);
+            load_some<T, VEC>(gy + c, width - c, g[i]);  // zeros beyond the row: nothing there counts
         }
 #pragma unroll
         for (int i = 0; i < ITER; ++i)
@@ -221,11 +205,11 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormBackwardArg
                 for (int e = 0; e < VEC; ++e) o[e] = rstd * (g[i][e] - s1 - xh[i][e] * s2);
                 if (gs) {
                     float t[VEC];
-                    load_pack<T, VEC>(gs + c, t);
+                    load_some<T, VEC>(gs + c, width - c, t);
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) o[e] += t[e];
                 }
-                store_pack<T, VEC>(dx + c, o);
+                store_some<T, VEC>(dx + c, width - c, o);
             }
         }
     }
@@ -249,8 +233,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_kernel(NormBackwardArg
             }
             const int c = (i * TPR + lane) * VEC;
             if (group == 0 && c < width) {
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) part[(int64_t)which * width + c + e] = d[e];
+                store_some<float, VEC>(part + (int64_t)which * width + c, width - c, d);
             }
         }
     }
@@ -299,44 +282,35 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormBackwardArgs
     a.partial[(int64_t)blockIdx.y * 2 * a.width + a.width + c] = db;
 }
 
-// Sum of the blocks' shares, in a fixed order: 64 columns a block, 16 lanes
-// of shares each.
+// Sum of the blocks' shares, in a fixed order: 16 columns a block, 64 lanes of
+// shares each (64 columns and 16 lanes: 16 workgroups for 512 columns, 20 us for
+// 1024 shares).
 __global__ void __launch_bounds__(1024) norm_reduce_kernel(const float *partial, int n, int width, float *dw,
                                                            float *db) {
-    __shared__ float part[16][64];
-    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6;
-    const int c = blockIdx.x * 64 + lane;
+    __shared__ float part[64][16];
+    const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int c = blockIdx.x * 16 + lane;
     float s = 0.0f;
-    if (c < 2 * width)
-        for (int i = share; i < n; i += 16) s += partial[(int64_t)i * 2 * width + c];
+    if (c < 2 * width) {
+#pragma unroll 4
+        for (int i = share; i < n; i += 64) s += partial[(int64_t)i * 2 * width + c];
+    }
     part[share][lane] = s;
-    __syncthreads();
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        __syncthreads();
+        if (share < d) part[share][lane] += part[share + d][lane];
+    }
     if (share != 0 || c >= 2 * width) return;
-    for (int i = 1; i < 16; ++i) s += part[i][lane];
     if (c < width) {
-        if (dw) dw[c] = s;
+        if (dw) dw[c] = part[0][lane];
     } else if (db) {
-        db[c - width] = s;
+        db[c - width] = part[0][lane];
     }
 }
 
-bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-// Packs of 16 bytes where every row starts on one and holds whole ones.
-template <typename T>
-bool packed(int32_t width, std::initializer_list<const void *> ptrs, std::initializer_list<int64_t> strides) {
-    constexpr int kVec = 16 / (int)sizeof(T);
-    if (width % kVec) return false;
-    for (const void *p : ptrs)
-        if (!aligned16(p)) return false;
-    for (int64_t s : strides)
-        if (s % kVec) return false;
-    return true;
-}
-
-// fn<VEC, ITER, TPR>() for a row of `width`: TPR lanes a row, ITER packs a
-// lane, the fewest lanes that keep a row's packs at 32 elements a lane;
-// wide() above 32 elements x 256 lanes (16 x 256 for single elements).
+// fn(ITER, TPR) for a row of `width`: TPR lanes a row, ITER packs a lane, the
+// fewest lanes that keep a lane at 4 packs; wide() above 4 packs x 256 lanes.
 template <int VEC, typename F, typename W>
 hipError_t with_shape(int32_t width, F &&fn, W &&wide) {
     const int packs = (width + VEC - 1) / VEC;
@@ -348,8 +322,6 @@ hipError_t with_shape(int32_t width, F &&fn, W &&wide) {
     if (packs <= 256) return fn(std::integral_constant<int, 4>{}, std::integral_constant<int, 64>{});
     if (packs <= 512) return fn(std::integral_constant<int, 2>{}, std::integral_constant<int, 256>{});
     if (packs <= 1024) return fn(std::integral_constant<int, 4>{}, std::integral_constant<int, 256>{});
-    if (VEC == 1 && packs <= 2048) return fn(std::integral_constant<int, VEC == 1 ? 8 : 4>{}, std::integral_constant<int, 256>{});
-    if (VEC == 1 && packs <= 4096) return fn(std::integral_constant<int, VEC == 1 ? 16 : 4>{}, std::integral_constant<int, 256>{});
     return wide();
 }
 
@@ -374,14 +346,12 @@ hipError_t launch_norm(const NormArgs &a, int32_t dtype, hipStream_t stream) {
     return with_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
         constexpr int kVec = 16 / (int)sizeof(T);
-        auto go = [&](auto vec) {
-            constexpr int VEC = decltype(vec)::value;
-            return with_shape<VEC>(
+        return with_shape<kVec>(
                 a.width,
                 [&](auto iter, auto tpr) {
                     constexpr int ITER = decltype(iter)::value, TPR = decltype(tpr)::value;
                     constexpr int kRows = kThreads / TPR;
-                    hipLaunchKernelGGL((norm_kernel<T, VEC, ITER, TPR>), dim3((uint32_t)((a.rows + kRows - 1) / kRows)),
+                    hipLaunchKernelGGL((norm_kernel<T, kVec, ITER, TPR>), dim3((uint32_t)((a.rows + kRows - 1) / kRows)),
                                        dim3(kThreads), 0, stream, a);
                     return hipGetLastError();
                 },
@@ -389,11 +359,6 @@ hipError_t launch_norm(const NormArgs &a, int32_t dtype, hipStream_t stream) {
                     hipLaunchKernelGGL((norm_wide_kernel<T>), dim3((uint32_t)a.rows), dim3(kThreads), 0, stream, a);
                     return hipGetLastError();
                 });
-        };
-        if (packed<T>(a.width, {a.x, a.residual, a.sum, a.y, a.weight, a.bias},
-                      {a.x_stride, a.residual_stride, a.sum_stride, a.y_stride}))
-            return go(std::integral_constant<int, kVec>{});
-        return go(std::integral_constant<int, 1>{});
     });
 }
 
@@ -404,15 +369,13 @@ hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspa
     hipError_t err = a.rows == 0 ? hipSuccess : with_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
         constexpr int kVec = 16 / (int)sizeof(T);
-        auto go = [&](auto vec) {
-            constexpr int VEC = decltype(vec)::value;
-            return with_shape<VEC>(
+        return with_shape<kVec>(
                 a.width,
                 [&](auto iter, auto tpr) {
                     constexpr int ITER = decltype(iter)::value, TPR = decltype(tpr)::value;
                     constexpr int kRows = kThreads / TPR;
                     shares = (int)std::min<int64_t>(shares, (a.rows + kRows - 1) / kRows);
-                    hipLaunchKernelGGL((norm_backward_kernel<T, VEC, ITER, TPR>), dim3(shares), dim3(kThreads), 0,
+                    hipLaunchKernelGGL((norm_backward_kernel<T, kVec, ITER, TPR>), dim3(shares), dim3(kThreads), 0,
                                        stream, a);
                     return hipGetLastError();
                 },
@@ -426,14 +389,9 @@ hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspa
                                        dim3(kThreads), 0, stream, a);
                     return hipGetLastError();
                 });
-        };
-        if (packed<T>(a.width, {a.x, a.grad_y, a.grad_sum, a.grad_x, a.weight},
-                      {a.x_stride, a.grad_y_stride, a.grad_sum_stride, a.grad_x_stride}))
-            return go(std::integral_constant<int, kVec>{});
-        return go(std::integral_constant<int, 1>{});
     });
     if (err != hipSuccess || !(grad_weight || grad_bias)) return err;
-    hipLaunchKernelGGL(norm_reduce_kernel, dim3((2 * a.width + 63) / 64), dim3(1024), 0, stream, a.partial, shares,
+    hipLaunchKernelGGL(norm_reduce_kernel, dim3((2 * a.width + 15) / 16), dim3(1024), 0, stream, a.partial, shares,
                        a.width, grad_weight, grad_bias);
     return hipGetLastError();
 }

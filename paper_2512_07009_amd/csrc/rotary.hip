@@ -23,9 +23,14 @@ constexpr int kThreads = 256;
 constexpr int kTable = 1024;  // (cos, sin) pairs in LDS
 
 // n / d for m = ceil(2^32 / d), 0 for d = 1: exact while n d < 2^32 (here at
-// most 2^25: the items of a block are at most 4 x 256, or one bird's 512 heads
-// of 256 dimensions).
+// most 2^23: the items of a block are at most 4 x 256, or one bird's 512 heads
+// of 64 chunks).
 __device__ __forceinline__ uint32_t quotient(uint32_t n, uint32_t m) { return m ? __umulhi(n, m) : n; }
+
+// A block's work items are (bird, head, chunk of VEC pairs, then of VEC
+// dimensions that are only passed on), at most kItems a thread.  Their loads
+// are started first, the table is made while they run.
+constexpr int kItems = 4;
 
 template <typename T, int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
@@ -33,86 +38,95 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(RotaryArgs a) {
     const int pairs = a.pairs;
     const int64_t first = (int64_t)blockIdx.x * a.birds_per_block;
     const int birds = (int)min((int64_t)a.birds_per_block, a.total - first);
-    for (int e = threadIdx.x; e < birds * pairs; e += kThreads) {
-        const int b = e / pairs, p = e - b * pairs;
-        const int64_t bird = first + b;
-        int64_t pos;
-        if (p < a.n_time) pos = a.time[bird];
-        else pos = a.xy[2 * bird + (p < a.n_time + a.n_y ? 1 : 0)];
-        const uint64_t phase = (uint64_t)pos * a.step[p];
-        const float turns = (float)(int32_t)(phase >> 32) * 0x1p-32f;
-        const float sn = __builtin_amdgcn_sinf(turns);
-        table[e] = make_float2(__builtin_amdgcn_cosf(turns), a.inverse ? -sn : sn);
-    }
-    __syncthreads();
-    // work items: bird, head, chunk of VEC pairs (then of VEC dimensions that are only passed on)
     const int heads = a.q_heads + a.k_heads;
-    const int turned = pairs / VEC;
-    const int chunks = turned + a.tail / VEC;
+    const int turned = (pairs + VEC - 1) / VEC;
+    const int chunks = turned + (a.tail + VEC - 1) / VEC;
     const int items = birds * heads * chunks;
-    for (int e = threadIdx.x; e < items; e += kThreads) {
-        const int bh = quotient(e, a.chunk_reciprocal), c = e - bh * chunks;
-        const int b = quotient(bh, a.head_reciprocal), hd = bh - b * heads;
-        const int64_t bird = first + b;
-        const T *in;
-        T *out;
-        if (hd < a.q_heads) {
-            in = static_cast<const T *>(a.q) + bird * a.q_stride + hd * a.head_dim;
-            out = static_cast<T *>(a.q_out) + bird * a.q_out_stride + hd * a.head_dim;
-        } else {
-            in = static_cast<const T *>(a.k) + bird * a.k_stride + (hd - a.q_heads) * a.head_dim;
-            out = static_cast<T *>(a.k_out) + bird * a.k_out_stride + (hd - a.q_heads) * a.head_dim;
+    float u[kItems][VEC], v[kItems][VEC];
+    T *out[kItems];
+    int bird_of[kItems], chunk[kItems];
+    for (int base = 0; base < items; base += kItems * kThreads) {
+#pragma unroll
+        for (int n = 0; n < kItems; ++n) {
+            const int e = base + n * kThreads + threadIdx.x;
+            if (e >= items) continue;
+            const int bh = quotient(e, a.chunk_reciprocal), c = e - bh * chunks;
+            const int b = quotient(bh, a.head_reciprocal), hd = bh - b * heads;
+            const int64_t bird = first + b;
+            const T *in;
+            if (hd < a.q_heads) {
+                in = static_cast<const T *>(a.q) + bird * a.q_stride + hd * a.head_dim;
+                out[n] = static_cast<T *>(a.q_out) + bird * a.q_out_stride + hd * a.head_dim;
+            } else {
+                in = static_cast<const T *>(a.k) + bird * a.k_stride + (hd - a.q_heads) * a.head_dim;
+                out[n] = static_cast<T *>(a.k_out) + bird * a.k_out_stride + (hd - a.q_heads) * a.head_dim;
+            }
+            bird_of[n] = b;
+            chunk[n] = c;
+            if (c >= turned) {
+                const int d = (c - turned) * VEC;
+                load_some<T, VEC>(in + 2 * pairs + d, a.tail - d, u[n]);
+            } else if (INTERLEAVED) {
+                load_some<T, VEC>(in + 2 * c * VEC, 2 * (pairs - c * VEC), u[n]);
+                load_some<T, VEC>(in + 2 * c * VEC + VEC, 2 * (pairs - c * VEC) - VEC, v[n]);
+            } else {
+                load_some<T, VEC>(in + c * VEC, pairs - c * VEC, u[n]);
+                load_some<T, VEC>(in + pairs + c * VEC, pairs - c * VEC, v[n]);
+            }
         }
-        if (c >= turned) {
-            const int d = 2 * pairs + (c - turned) * VEC;
-            float z[VEC];
-            load_pack<T, VEC>(in + d, z);
-            store_pack<T, VEC>(out + d, z);
-            continue;
+        if (base == 0) {
+            for (int e = threadIdx.x; e < birds * pairs; e += kThreads) {
+                const int b = quotient(e, a.pair_reciprocal), p = e - b * pairs;
+                const int64_t bird = first + b;
+                int64_t pos;
+                if (p < a.n_time) pos = a.time[bird];
+                else pos = a.xy[2 * bird + (p < a.n_time + a.n_y ? 1 : 0)];
+                const uint64_t phase = (uint64_t)pos * a.step[p];
+                const float turns = (float)(int32_t)(phase >> 32) * 0x1p-32f;
+                const float sn = __builtin_amdgcn_sinf(turns);
+                table[e] = make_float2(__builtin_amdgcn_cosf(turns), a.inverse ? -sn : sn);
+            }
+            __syncthreads();
         }
-        const float2 *t = table + b * pairs + c * VEC;
-        float u[VEC], v[VEC];
-        if (INTERLEAVED) {
-            load_pack<T, VEC>(in + 2 * c * VEC, u);
-            load_pack<T, VEC>(in + 2 * c * VEC + VEC, v);
-            if (VEC == 1) {
-                const float2 w = t[0];
-                const float x = u[0] * w.x - v[0] * w.y;
-                v[0] = u[0] * w.y + v[0] * w.x;
-                u[0] = x;
+#pragma unroll
+        for (int n = 0; n < kItems; ++n) {
+            if (base + n * kThreads + (int)threadIdx.x >= items) continue;
+            const int c = chunk[n];
+            if (c >= turned) {
+                const int d = (c - turned) * VEC;
+                store_some<T, VEC>(out[n] + 2 * pairs + d, a.tail - d, u[n]);
+                continue;
+            }
+            const float2 *t = table + bird_of[n] * pairs + c * VEC;
+            const int left = pairs - c * VEC;
+            if (INTERLEAVED) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float2 w = t[min(i, left - 1)];
+                    float &x = i < VEC / 2 ? u[n][2 * i] : v[n][2 * i - VEC];
+                    float &y = i < VEC / 2 ? u[n][2 * i + 1] : v[n][2 * i + 1 - VEC];
+                    const float z = x * w.x - y * w.y;
+                    y = x * w.y + y * w.x;
+                    x = z;
+                }
+                store_some<T, VEC>(out[n] + 2 * c * VEC, 2 * left, u[n]);
+                store_some<T, VEC>(out[n] + 2 * c * VEC + VEC, 2 * left - VEC, v[n]);
             } else {
 #pragma unroll
-                for (int i = 0; i < VEC / 2; ++i) {
-                    const float2 w0 = t[i], w1 = t[VEC / 2 + i];
-                    const float x0 = u[2 * i] * w0.x - u[2 * i + 1] * w0.y;
-                    u[2 * i + 1] = u[2 * i] * w0.y + u[2 * i + 1] * w0.x;
-                    u[2 * i] = x0;
-                    const float x1 = v[2 * i] * w1.x - v[2 * i + 1] * w1.y;
-                    v[2 * i + 1] = v[2 * i] * w1.y + v[2 * i + 1] * w1.x;
-                    v[2 * i] = x1;
+                for (int i = 0; i < VEC; ++i) {
+                    const float2 w = t[min(i, left - 1)];
+                    const float z = u[n][i] * w.x - v[n][i] * w.y;
+                    v[n][i] = u[n][i] * w.y + v[n][i] * w.x;
+                    u[n][i] = z;
                 }
+                store_some<T, VEC>(out[n] + c * VEC, left, u[n]);
+                store_some<T, VEC>(out[n] + pairs + c * VEC, left, v[n]);
             }
-            store_pack<T, VEC>(out + 2 * c * VEC, u);
-            store_pack<T, VEC>(out + 2 * c * VEC + VEC, v);
-        } else {
-            load_pack<T, VEC>(in + c * VEC, u);
-            load_pack<T, VEC>(in + pairs + c * VEC, v);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float2 w = t[i];
-                const float x = u[i] * w.x - v[i] * w.y;
-                v[i] = u[i] * w.y + v[i] * w.x;
-                u[i] = x;
-            }
-            store_pack<T, VEC>(out + c * VEC, u);
-            store_pack<T, VEC>(out + pairs + c * VEC, v);
         }
     }
 }
 
 uint32_t reciprocal(uint32_t d) { return d > 1 ? (uint32_t)(((1ull << 32) + d - 1) / d) : 0; }
-
-bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace
 
@@ -122,27 +136,19 @@ hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream) {
     return with_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
         constexpr int kVec = 16 / (int)sizeof(T);
-        const bool packs = a.pairs % kVec == 0 && a.head_dim % kVec == 0 && on16(a.q) && on16(a.k) && on16(a.q_out) &&
-                           on16(a.k_out) && a.q_stride % kVec == 0 && a.k_stride % kVec == 0 &&
-                           a.q_out_stride % kVec == 0 && a.k_out_stride % kVec == 0;
-        const int vec = packs ? kVec : 1;
         const int heads = a.q_heads + a.k_heads;
-        const int chunks = a.pairs / vec + a.tail / vec;
+        const int chunks = (a.pairs + kVec - 1) / kVec + (a.tail + kVec - 1) / kVec;
         a.birds_per_block = 1;
-        // a few items a thread, and the table within LDS
+        // as many birds as keep a thread at kItems items, the table within LDS
         while (a.birds_per_block < 64 && 2 * a.birds_per_block * a.pairs <= kTable &&
-               2 * a.birds_per_block * heads * chunks <= 4 * kThreads)
+               2 * a.birds_per_block * heads * chunks <= kItems * kThreads)
             a.birds_per_block *= 2;
         a.chunk_reciprocal = reciprocal(chunks);
         a.head_reciprocal = reciprocal(heads);
+        a.pair_reciprocal = reciprocal(a.pairs);
         const dim3 grid((uint32_t)((a.total + a.birds_per_block - 1) / a.birds_per_block));
-        if (packs) {
-            if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, kVec, true>), grid, dim3(kThreads), 0, stream, a);
-            else hipLaunchKernelGGL((rotary_kernel<T, kVec, false>), grid, dim3(kThreads), 0, stream, a);
-        } else {
-            if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, 1, true>), grid, dim3(kThreads), 0, stream, a);
-            else hipLaunchKernelGGL((rotary_kernel<T, 1, false>), grid, dim3(kThreads), 0, stream, a);
-        }
+        if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, kVec, true>), grid, dim3(kThreads), 0, stream, a);
+        else hipLaunchKernelGGL((rotary_kernel<T, kVec, false>), grid, dim3(kThreads), 0, stream, a);
         return hipGetLastError();
     });
 }
