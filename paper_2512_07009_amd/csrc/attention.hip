@@ -140,6 +140,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
         next.template load<DIST>(a, sp, head, 0, end);
         next.template store<DIST>(a, typename Tile::Lds(shared));
     }
+    wait_for_loads();
     __syncthreads();
     int buffer = 0;
     for (int kt = 0; kt < end; kt += kTileKeys) {

@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         next.template load<DIST>(a, sp, head, 0, end);
         next.template store<DIST>(a, typename Tile::Lds(shared));
     }
+    wait_for_loads();
     __syncthreads();
     int buffer = 0;
     for (int kt = 0; kt < end; kt += kTileKeys) {
@@ -231,7 +232,10 @@ struct RowTile {
     };
 
     i32x4 q[kLoads], g[kLoads];
-    float x, y, slope, shift, delta, rest;
+    // as loaded: what is made of them waits for the loads, so it is made in store()
+    double lse;
+    int2 place;
+    float slope, delta;
     int limit;
 
     template <bool DIST>
@@ -257,23 +261,19 @@ struct RowTile {
             g[n] = __builtin_amdgcn_raw_buffer_load_b128(gr, in ? (int)i * g_step + (int)gg * a.dim * 2 + c * 16 : kBeyond, 0, 0);
         }
         if (threadIdx.x < kTileRows) {
-            x = y = slope = delta = rest = 0.0f;
-            shift = INFINITY;
-            limit = 0;
-            if ((int)threadIdx.x < rows) {
-                const uint32_t i = group_quotient(g0 + threadIdx.x, b.group_reciprocal);
-                const int qh = head * a.group + (int)(g0 + threadIdx.x - i * a.group);
-                const int64_t row = sp.q0 + i0 + i;
-                split_lse(a.lse[row * a.q_heads + qh], shift, rest);
-                delta = b.delta[row * a.q_heads + qh];
-                if (DIST) {
-                    const int2 place = reinterpret_cast<const int2 *>(a.q_xy)[row];
-                    x = (float)place.x * kPxPerQuantum;
-                    y = (float)place.y * kPxPerQuantum;
-                    slope = a.slopes[qh] * kLog2e;
-                }
-                limit = a.causal ? (int)min(max((int64_t)prefix, i0 + i + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+            // absent rows read the last one's values and have no weights
+            const uint32_t r = g0 + min((int)threadIdx.x, rows - 1);
+            const uint32_t i = group_quotient(r, b.group_reciprocal);
+            const int qh = head * a.group + (int)(r - i * a.group);
+            const int64_t row = sp.q0 + i0 + i;
+            lse = a.lse[row * a.q_heads + qh];
+            delta = b.delta[row * a.q_heads + qh];
+            if (DIST) {
+                place = reinterpret_cast<const int2 *>(a.q_xy)[row];
+                slope = a.slopes[qh];
             }
+            limit = a.causal ? (int)min(max((int64_t)prefix, i0 + i + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+            if ((int)threadIdx.x >= rows) limit = -1;
         }
     }
 
@@ -287,16 +287,19 @@ struct RowTile {
             lds.g[at] = __builtin_bit_cast(i16x8, g[n]);
         }
         if (threadIdx.x < kTileRows) {  // the first wave
+            const bool absent = limit < 0;
             if (DIST) {
-                lds.x[threadIdx.x] = x;
-                lds.y[threadIdx.x] = y;
-                lds.slope[threadIdx.x] = slope;
+                lds.x[threadIdx.x] = (float)place.x * kPxPerQuantum;
+                lds.y[threadIdx.x] = (float)place.y * kPxPerQuantum;
+                lds.slope[threadIdx.x] = slope * kLog2e;
             }
+            float shift, rest;
+            split_lse(absent ? -INFINITY : lse, shift, rest);
             lds.shift[threadIdx.x] = shift;
             lds.delta[threadIdx.x] = delta;
             lds.rest[threadIdx.x] = rest;
             lds.limit[threadIdx.x] = limit;
-            // rest is 1 to a rounding of the weights, but for large scores (absent rows have P = 0)
+            // rest is 1 to a rounding of the weights, but for large scores (rows without keys have P = 0)
             const bool one = __all(fabsf(rest - 1.0f) < 0x1p-16f || shift == INFINITY);
             if (threadIdx.x == 0) *lds.exact = one ? 1 : 0;
         }
@@ -432,6 +435,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         next.template load<DIST>(b, sp, head, prefix, begin, n_rows);
         next.template store<DIST>(typename Tile::Lds(shared));
     }
+    wait_for_loads();
     __syncthreads();
     int buffer = 0;
     for (int64_t rt = begin; rt < n_rows; rt += kTileRows) {

@@ -142,6 +142,10 @@ __device__ __forceinline__ typename Frag<T>::type load_frag(const short *row, in
     return __builtin_bit_cast(typename Frag<T>::type, z);
 }
 
+// Waits for the loads so far.  Before a loop that keeps loads in flight: else the
+// first use of what was loaded before it waits, in every turn, for those too.
+__device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 // Half of a product's registers as the right factor of the next one.
 template <typename T>
 __device__ __forceinline__ typename Frag<T>::type round_frag(const f32x16 &s, int part) {
@@ -203,9 +207,9 @@ struct KeyTile {
     };
 
     i32x4 k[kLoads], v[kLoads];
-    uint32_t kept;  // a bit per load
+    // as loaded: what is made of them waits for the loads, so it is made in store()
+    uint8_t kept[kLoads], key_kept;
     int2 place;
-    bool key_kept;
 
     template <bool DIST>
     __device__ __forceinline__ void load(const AttentionArgs &a, const Span &sp, int head, int first, int end) {
@@ -214,7 +218,6 @@ struct KeyTile {
         const int k_step = (int)a.k_stride * 2, v_step = (int)a.v_stride * 2;
         const auto kr = tile_resource(a.k, row0 * a.k_stride + head * a.dim, (rows - 1) * k_step + a.dim * 2);
         const auto vr = tile_resource(a.v, row0 * a.v_stride + head * a.dim, (rows - 1) * v_step + a.dim * 2);
-        kept = 0;
         constexpr bool kEven = kThreads % kChunks == 0;  // a thread's loads are of one column
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
@@ -224,15 +227,13 @@ struct KeyTile {
             const int more = kEven ? n * (kThreads / kChunks) : 0;
             k[n] = __builtin_amdgcn_raw_buffer_load_b128(kr, in ? r * k_step + c * 16 : kBeyond, more * k_step, 0);
             v[n] = __builtin_amdgcn_raw_buffer_load_b128(vr, in ? r * v_step + c * 16 : kBeyond, more * v_step, 0);
-            if (a.keep && r + more < rows && a.keep[row0 + r + more]) kept |= 1u << n;
+            if (a.keep) kept[n] = a.keep[row0 + min(r + more, rows - 1)];
         }
         if (threadIdx.x < KEYS) {
-            key_kept = false;
-            place = make_int2(0, 0);
-            if ((int)threadIdx.x < rows) {
-                key_kept = !a.keep || a.keep[row0 + threadIdx.x];
-                if (DIST) place = reinterpret_cast<const int2 *>(a.k_xy)[row0 + threadIdx.x];
-            }
+            key_kept = (int)threadIdx.x < rows;
+            const int64_t row = row0 + min((int)threadIdx.x, rows - 1);
+            if (a.keep && key_kept) key_kept = a.keep[row];
+            if (DIST) place = reinterpret_cast<const int2 *>(a.k_xy)[row];
         }
     }
 
@@ -241,7 +242,7 @@ struct KeyTile {
         if (a.keep) {
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
-                if (!(kept >> n & 1)) k[n] = v[n] = i32x4{0, 0, 0, 0};
+                if (kept[n] == 0) k[n] = v[n] = i32x4{0, 0, 0, 0};
             }
         }
 #pragma unroll
@@ -256,8 +257,8 @@ struct KeyTile {
                 lds.x[threadIdx.x] = (float)place.x * kPxPerQuantum;
                 lds.y[threadIdx.x] = (float)place.y * kPxPerQuantum;
             }
-            lds.penalty[threadIdx.x] = key_kept ? 0.0f : -INFINITY;
-            const uint64_t seen = __ballot(key_kept);
+            lds.penalty[threadIdx.x] = key_kept != 0 ? 0.0f : -INFINITY;
+            const uint64_t seen = __ballot(key_kept != 0);
             if ((threadIdx.x & 63) == 0) lds.seen[threadIdx.x >> 6] = seen;
         }
     }
