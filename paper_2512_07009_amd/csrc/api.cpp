@@ -807,10 +807,11 @@ flock_status check_attention_pointers(const flock::AttentionArgs &a) {
     if (!aligned(a.q_offsets, 4) || !aligned(a.k_offsets, 4) || !aligned(a.slopes, 4) || !aligned(a.prefix, 4))
         return fail(FLOCK_EINVAL, "q_offsets, k_offsets, slopes and prefix must be 4-byte aligned");
     if (!aligned(a.lse, 8)) return fail(FLOCK_EINVAL, "lse must be 8-byte aligned");
-    // rows are numbered in 32 bits in a frame's tile, tiles in a launch's grid
-    if (((int64_t)a.total_q * a.group / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL ||
+    // rows are numbered in 31 bits, tiles in a launch's grid
+    if ((int64_t)a.total_q * a.group > 0x7fffff00LL ||
+        ((int64_t)a.total_q * a.group / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL ||
         ((int64_t)a.total_k / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL)
-        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 - 1 tiles");
+        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 rows or tiles");
     return FLOCK_OK;
 }
 

@@ -56,14 +56,15 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
     const int f = find_frame(a.q_offsets, a.n_frames, a.group, kRows, id % a.slots, &tile);
     const Span sp = frame_span(a, f);
     if (!sp.ok || tile < 0) return;
-    const int64_t n_rows = (int64_t)sp.nq * a.group;
-    const int64_t row0 = tile * kRows;
-    if (row0 >= n_rows) return;
+    const int n_rows = sp.nq * a.group;
+    if (tile * kRows >= n_rows) return;
+    const int row0 = (int)tile * kRows;
+    const RowRun run(a, row0);
 
     // this lane's query
-    const int64_t row = row0 + 32 * wave + col;
-    const bool valid = row < n_rows;
-    const int qi = valid ? (int)(row / a.group) : 0, g = valid ? (int)(row % a.group) : 0;
+    const bool valid = row0 + 32 * wave + col < n_rows;
+    int qi = 0, g = 0;
+    if (valid) run.find(a, 32 * wave + col, qi, g);
     const int qh = head * a.group + g;
     const short *q_row = valid ? static_cast<const short *>(a.q) + (int64_t)(sp.q0 + qi) * a.q_stride + qh * a.dim
                                : nullptr;
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) q[s] = load_frag<T>(q_row, s, h, a.dim);
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
-    const int limit = valid && a.causal ? (int)min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    const int limit = valid ? seen_limit(a, sp, prefix, qi) : sp.nk;
     float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
     if (DIST && valid) {
         const int2 place = reinterpret_cast<const int2 *>(a.q_xy)[sp.q0 + qi];
@@ -86,8 +87,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
     if (a.causal) {
         wave_end = wave_max(limit);
         wave_all = -wave_max(-limit);
-        const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
-        end = (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk);
+        end = seen_limit(a, sp, prefix, run.query(a, min(kRows, n_rows - row0) - 1));
     }
 
     f32x16 o[DP / 32] = {};
@@ -244,14 +244,14 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
     const int f = find_frame(a.q_offsets, a.n_frames, a.group, kRows, id % a.slots, &tile);
     const Span sp = frame_span(a, f);
     if (!sp.ok || tile < 0) return;
-    const int64_t n_rows = (int64_t)sp.nq * a.group;
-    const int64_t row0 = tile * kRows;
-    if (row0 >= n_rows) return;
+    const int n_rows = sp.nq * a.group;
+    if (tile * kRows >= n_rows) return;
+    const int row0 = (int)tile * kRows;
+    const RowRun run(a, row0);
 
     // keys that any of the workgroup's rows sees
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
-    const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
-    int end = a.causal ? (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    int end = seen_limit(a, sp, prefix, run.query(a, min(kRows, n_rows - row0) - 1));
     int begin = 0;
     if (a.splits > 1) {
         const int per = ((sp.nk + a.splits - 1) / a.splits + kKeys - 1) / kKeys * kKeys;
@@ -262,9 +262,9 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
     if (begin < end) next.template load<DIST>(a, sp, head, begin, end);
 
     // this lane's query
-    const int64_t row = row0 + col;
-    const bool valid = row < n_rows;
-    const int qi = valid ? (int)(row / a.group) : 0, g = valid ? (int)(row % a.group) : 0;
+    const bool valid = row0 + col < n_rows;
+    int qi = 0, g = 0;
+    if (valid) run.find(a, col, qi, g);
     const int qh = head * a.group + g;
     // the rows stay in LDS: the loads in flight take the registers
     i16x8 *const q_lds = reinterpret_cast<i16x8 *>(shared + Tile::kBytes);
@@ -272,13 +272,14 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         const int r = e / Tile::kChunks, c = e % Tile::kChunks;
         i16x8 z = {};
         if (row0 + r < n_rows && c * 8 < a.dim) {
-            const int64_t i = sp.q0 + (row0 + r) / a.group;
-            const int hh = head * a.group + (int)((row0 + r) % a.group);
-            z = *reinterpret_cast<const i16x8 *>(static_cast<const short *>(a.q) + i * a.q_stride + hh * a.dim + c * 8);
+            int i, gg;
+            run.find(a, r, i, gg);
+            z = *reinterpret_cast<const i16x8 *>(static_cast<const short *>(a.q) + (int64_t)(sp.q0 + i) * a.q_stride +
+                                                 (head * a.group + gg) * a.dim + c * 8);
         }
         q_lds[r * Tile::kPitch + c] = z;
     }
-    const int limit = valid && a.causal ? (int)min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    const int limit = valid ? seen_limit(a, sp, prefix, qi) : sp.nk;
     const int all_end = a.causal ? -wave_max(-limit) : sp.nk;
     float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
     if (DIST && valid) {
@@ -371,8 +372,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
     __syncthreads();
     for (int e = threadIdx.x; e < 32 * DP; e += kThreads) {
         const int c = e / DP, d = e % DP;
-        const int64_t r = row0 + c;
-        if (r >= n_rows || d >= a.dim) continue;
+        if (row0 + c >= n_rows || d >= a.dim) continue;
         float top = -INFINITY;
         for (int w = 0; w < 4; ++w) top = fmaxf(top, join[(w * 32 + c) * kPitch + DP]);
         const float shift = top == -INFINITY ? 0.0f : top;
@@ -383,8 +383,10 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
             sum += p[DP + 1] * fade;
             z += p[d] * fade;
         }
-        const int64_t i = sp.q0 + r / a.group;
-        const int hh = head * a.group + (int)(r % a.group);
+        int iq, gg;
+        run.find(a, c, iq, gg);
+        const int64_t i = sp.q0 + iq;
+        const int hh = head * a.group + gg;
         const int64_t at = i * a.q_heads + hh;
         if (a.splits > 1) {
             const int64_t all = (int64_t)a.total_q * a.q_heads;
@@ -467,6 +469,7 @@ hipError_t launch_attention(AttentionArgs a, int32_t dtype, const AttentionPlan 
                             hipStream_t stream) {
     a.slots = p.slots;
     a.splits = p.splits;
+    a.group_reciprocal = group_reciprocal(a.group);
     if (p.splits > 1) {
         const size_t all = (size_t)a.total_q * (size_t)a.q_heads * (size_t)p.splits;
         a.part_out = static_cast<float *>(workspace);

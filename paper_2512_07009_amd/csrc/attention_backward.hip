@@ -56,12 +56,13 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
     const int f = find_frame(a.q_offsets, a.n_frames, a.group, kRows, id % a.slots, &tile);
     const Span sp = frame_span(a, f);
     if (!sp.ok || tile < 0) return;
-    const int64_t n_rows = (int64_t)sp.nq * a.group;
-    const int64_t row0 = tile * kRows;
-    if (row0 >= n_rows) return;
-    const int64_t row = row0 + 32 * wave + col;
-    const bool valid = row < n_rows;
-    const int qi = valid ? (int)(row / a.group) : 0, g = valid ? (int)(row % a.group) : 0;
+    const int n_rows = sp.nq * a.group;
+    if (tile * kRows >= n_rows) return;
+    const int row0 = (int)tile * kRows;
+    const RowRun run(a, row0);
+    const bool valid = row0 + 32 * wave + col < n_rows;
+    int qi = 0, g = 0;
+    if (valid) run.find(a, 32 * wave + col, qi, g);
     const int qh = head * a.group + g;
     const int64_t qrow = sp.q0 + qi;
     const short *q_row = valid ? static_cast<const short *>(a.q) + qrow * a.q_stride + qh * a.dim : nullptr;
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         go[s] = load_frag<T>(g_row, s, h, a.dim);
     }
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
-    const int limit = valid && a.causal ? (int)min(max((int64_t)prefix, (int64_t)qi + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+    const int limit = valid ? seen_limit(a, sp, prefix, qi) : sp.nk;
     float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
     if (DIST && valid) {
         const int2 place = reinterpret_cast<const int2 *>(a.q_xy)[qrow];
@@ -89,8 +90,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
     if (a.causal) {
         wave_end = wave_max(limit);
         wave_all = -wave_max(-limit);
-        const int last = (int)((min(row0 + kRows, n_rows) - 1) / a.group);
-        end = (int)min(max((int64_t)prefix, (int64_t)last + sp.nk - sp.nq + 1), (int64_t)sp.nk);
+        end = seen_limit(a, sp, prefix, run.query(a, min(kRows, n_rows - row0) - 1));
     }
 
     f32x16 dq[DP / 32] = {};
@@ -240,39 +240,37 @@ struct RowTile {
 
     template <bool DIST>
     __device__ __forceinline__ void load(const AttentionBackwardArgs &b, const Span &sp, int head, int prefix,
-                                         int64_t first, int64_t n_rows) {
+                                         const RowRun &run, int rows) {
         const AttentionArgs &a = b.fwd;
-        const int64_t i0 = first / a.group;
-        const int g0 = (int)(first - i0 * a.group);
-        const int rows = (int)min(n_rows - first, (int64_t)kTileRows);
-        const int queries = (g0 + rows - 1) / a.group;  // beyond the first
+        const int64_t first = sp.q0 + run.first_query;
         const int q_step = (int)a.q_stride * 2, g_step = (int)b.grad_out_stride * 2;
-        const int bytes = a.group * a.dim * 2;
-        const auto qr = tile_resource(a.q, (sp.q0 + i0) * a.q_stride + head * a.group * a.dim, queries * q_step + bytes);
-        const auto gr = tile_resource(b.grad_out, (sp.q0 + i0) * b.grad_out_stride + head * a.group * a.dim,
-                                      queries * g_step + bytes);
+        // absent rows and dimensions go beyond the resource, everything else is within the tile
+        const auto qr = tile_resource(a.q, first * a.q_stride + head * a.group * a.dim, kBeyond);
+        const auto gr = tile_resource(b.grad_out, first * b.grad_out_stride + head * a.group * a.dim, kBeyond);
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
             const int e = threadIdx.x + n * kThreads;
             const int r = e / kChunks, c = e % kChunks;
-            const uint32_t i = group_quotient(g0 + r, b.group_reciprocal), gg = g0 + r - i * a.group;
+            const uint32_t u = run.first_g + r, i = group_quotient(u, a.group_reciprocal);
+            const int at = (int)__umul24(u - __umul24(i, a.group), a.dim * 2) + c * 16;
             const bool in = c * 8 < a.dim && r < rows;
-            q[n] = __builtin_amdgcn_raw_buffer_load_b128(qr, in ? (int)i * q_step + (int)gg * a.dim * 2 + c * 16 : kBeyond, 0, 0);
-            g[n] = __builtin_amdgcn_raw_buffer_load_b128(gr, in ? (int)i * g_step + (int)gg * a.dim * 2 + c * 16 : kBeyond, 0, 0);
+            const int q_at = (int)i * q_step + at, g_at = (int)i * g_step + at;
+            q[n] = __builtin_amdgcn_raw_buffer_load_b128(qr, in ? q_at : kBeyond, 0, 0);
+            g[n] = __builtin_amdgcn_raw_buffer_load_b128(gr, in ? g_at : kBeyond, 0, 0);
         }
         if (threadIdx.x < kTileRows) {
             // absent rows read the last one's values and have no weights
-            const uint32_t r = g0 + min((int)threadIdx.x, rows - 1);
-            const uint32_t i = group_quotient(r, b.group_reciprocal);
-            const int qh = head * a.group + (int)(r - i * a.group);
-            const int64_t row = sp.q0 + i0 + i;
+            int i, gg;
+            run.find(a, min((int)threadIdx.x, rows - 1), i, gg);
+            const int qh = head * a.group + gg;
+            const int64_t row = sp.q0 + i;
             lse = a.lse[row * a.q_heads + qh];
             delta = b.delta[row * a.q_heads + qh];
             if (DIST) {
                 place = reinterpret_cast<const int2 *>(a.q_xy)[row];
                 slope = a.slopes[qh];
             }
-            limit = a.causal ? (int)min(max((int64_t)prefix, i0 + i + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+            limit = seen_limit(a, sp, prefix, i);
             if ((int)threadIdx.x >= rows) limit = -1;
         }
     }
@@ -326,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
     if (!sp.ok || tile < 0) return;
     const int64_t key0 = tile * kKeys;
     if (key0 >= sp.nk) return;
-    const int64_t n_rows = (int64_t)sp.nq * a.group;
+    const int n_rows = sp.nq * a.group;
     F k[BLOCKS][DP / 16], v[BLOCKS][DP / 16];
     float kx[BLOCKS], ky[BLOCKS];
     bool kept[BLOCKS];
@@ -354,9 +352,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
     const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     // the first query that sees the workgroup's first key
-    int64_t begin = 0;
+    int begin = 0;
     if (a.causal && key0 >= prefix)
-        begin = max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows;
+        begin = (int)(max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows);
 
     f32x16 dk[BLOCKS][DP / 32] = {}, dv[BLOCKS][DP / 32] = {};
     auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact) {
@@ -431,21 +429,22 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
     };
 
     Tile next;
+    RowRun run(a, begin);
     if (begin < n_rows) {
-        next.template load<DIST>(b, sp, head, prefix, begin, n_rows);
+        next.template load<DIST>(b, sp, head, prefix, run, min(kTileRows, n_rows - begin));
         next.template store<DIST>(typename Tile::Lds(shared));
     }
     wait_for_loads();
     __syncthreads();
     int buffer = 0;
-    for (int64_t rt = begin; rt < n_rows; rt += kTileRows) {
+    for (int rt = begin; rt < n_rows; rt += kTileRows) {
         const bool more = rt + kTileRows < n_rows;
-        if (more) next.template load<DIST>(b, sp, head, prefix, rt + kTileRows, n_rows);
+        run.advance(a, kTileRows);
+        if (more) next.template load<DIST>(b, sp, head, prefix, run, min(kTileRows, n_rows - rt - kTileRows));
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const bool exact = __builtin_amdgcn_readfirstlane(*t.exact) != 0;
         // limits grow with the rows: those of the first and of the last row say which keys all and some rows see
-        const int64_t last = min(rt + kTileRows, n_rows) - 1;
-        const int some = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[(int)(last - rt)]) : sp.nk;
+        const int some = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[min(kTileRows, n_rows - rt) - 1]) : sp.nk;
         const int all = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[0]) : sp.nk;
         if (wave_key < some) {
 #pragma unroll 1
@@ -525,7 +524,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
     b.row_slopes = grad_slopes ? reinterpret_cast<float *>(ws + align256(all * sizeof(float))) : nullptr;
     double *parts = reinterpret_cast<double *>(ws + 2 * align256(all * sizeof(float)));
     a.slots = (int64_t)a.total_q * a.group / 128 + a.n_frames;
-    b.group_reciprocal = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0;
+    a.group_reciprocal = group_reciprocal(a.group);
     hipError_t err = hipSuccess;
     if (a.total_q > 0) {
         const dim3 grid((uint32_t)((all + 15) / 16));

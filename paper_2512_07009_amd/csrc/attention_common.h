@@ -73,6 +73,38 @@ __device__ __forceinline__ Span frame_span(const AttentionArgs &a, int f) {
     return s;
 }
 
+// A run of rows of a frame and kv head, row r of it being head g of query i:
+// only the run's beginning is divided by the heads in full.
+struct RowRun {
+    int first_query, first_g;
+    __device__ __forceinline__ RowRun(const AttentionArgs &a, int row0) {
+        first_query = (int)((uint32_t)row0 / (uint32_t)a.group);
+        first_g = row0 - first_query * a.group;
+    }
+    __device__ __forceinline__ void find(const AttentionArgs &a, int r, int &query, int &g) const {
+        const uint32_t u = first_g + r, n = group_quotient(u, a.group_reciprocal);
+        query = first_query + (int)n;
+        g = (int)(u - __umul24(n, a.group));
+    }
+    __device__ __forceinline__ int query(const AttentionArgs &a, int r) const {
+        return first_query + (int)group_quotient(first_g + r, a.group_reciprocal);
+    }
+    __device__ __forceinline__ void advance(const AttentionArgs &a, int rows) {
+        const int whole = (int)group_quotient(first_g + rows, a.group_reciprocal);
+        first_query += whole;
+        first_g += rows - whole * a.group;
+    }
+};
+
+// The first key that query i of a frame does not see (without hidden keys).
+__device__ __forceinline__ int seen_limit(const AttentionArgs &a, const Span &sp, int prefix, int i) {
+    return a.causal ? (int)min(max((int64_t)prefix, (int64_t)i + sp.nk - sp.nq + 1), (int64_t)sp.nk) : sp.nk;
+}
+
+inline uint32_t group_reciprocal(int group) {
+    return group > 1 ? (uint32_t)(((1ull << 32) + group - 1) / group) : 0;
+}
+
 // Tiles of `tile` rows are numbered without knowing the frames on the host:
 // frame f's begin at offsets[f] * group / tile + f, which leaves it at least as
 // many numbers as it has tiles.  Returns the frame of tile number `slot`, and

@@ -252,6 +252,7 @@ struct AttentionArgs {
     const int32_t *q_offsets, *k_offsets;  // [n_frames + 1]
     int32_t n_frames, total_q, total_k;
     int32_t q_heads, kv_heads, group, dim;  // group = q_heads / kv_heads
+    uint32_t group_reciprocal;         // set by the launches
     const int32_t *q_xy, *k_xy;        // 1/16 px, with slopes
     const float *slopes;               // [q_heads] or nullptr
     const uint8_t *keep;               // [total_k] or nullptr
@@ -283,7 +284,6 @@ struct AttentionBackwardArgs {
     int64_t grad_out_stride, grad_q_stride, grad_k_stride, grad_v_stride;
     float *delta, *row_slopes;         // set by launch_attention_backward: [total_q][q_heads]
     int64_t key_slots;
-    uint32_t group_reciprocal;
 };
 size_t attention_backward_workspace_bytes(int32_t total_q, int32_t q_heads);
 hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, void *workspace, float *grad_slopes,
