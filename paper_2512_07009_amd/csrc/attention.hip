@@ -42,10 +42,13 @@ using namespace attention;
 // only now and then.
 constexpr float kSlack = 8.0f;
 
+template <int DP, bool DIST>
+using RowsTile = KeyTile<DP, kTileKeys, Pitch<DP>::kRows, Pitch<DP>::kColumns, DIST>;
+
 template <typename T, int DP, bool DIST, bool CAP>
-__global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_kernel(AttentionArgs a) {
     using F = typename Frag<T>::type;
-    using Tile = KeyTile<DP>;
+    using Tile = RowsTile<DP, DIST>;
     constexpr int kRows = 128;
     extern __shared__ char shared[];
 
@@ -81,6 +84,27 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
         slope2 = a.slopes[qh] * kLog2e;
     }
     const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    // distances on the matrix cores: the row's factors, what they leave for the
+    // row, and the largest |b|^2 that any slope of the rows' heads allows
+    int2 origin = make_int2(0, 0);
+    float largest = 0.0f, row_term = 0.0f;
+    bool row_near = false;
+    bf16x8 row_slots = {};
+    if (DIST) {
+        int i, gg;
+        run.find(a, min(col, n_rows - 1 - row0), i, gg);
+        origin = near_origin(reinterpret_cast<const int2 *>(a.q_xy)[sp.q0 + i]);
+        float steepest = 0.0f;
+        for (int e = 0; e < a.group; ++e) steepest = fmaxf(steepest, fabsf(a.slopes[head * a.group + e]) * kLog2e);
+        largest = kNearLimit * 256.0f / steepest;
+        const int ax = (int)(qx * 16.0f) - origin.x, ay = (int)(qy * 16.0f) - origin.y;
+        const float n = square_quanta(ax, ay), weight = slope2 / 256.0f;
+        row_near = __all(!valid || near_enough(ax, ay, n, largest));
+        const float units = CAP ? weight : weight / scale;
+        row_term = -units * n;
+        const NearSlots s = near_row(ax, ay, units);
+        row_slots = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
+    }
     // the keys that any of the wave's rows sees, that all of them see, and that
     // any of the workgroup's sees
     int wave_end = sp.nk, wave_all = sp.nk, end = sp.nk;
@@ -93,52 +117,95 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
     f32x16 o[DP / 32] = {};
     float m = -INFINITY, shift = 0.0f, l = 0.0f;
 
-    // scores stay products of queries and keys until the exponential
+    // Half a tile.  A weight is 2^(s * unit - shift): scores without caps (and with
+    // distances on the matrix cores) stay products until then.
     constexpr bool PLAIN = !DIST && !CAP;
-    f32x16 s[2];
-    auto finish_scores = [&](const typename Tile::Lds &t) {
+    auto half_tile = [&](const typename Tile::Lds &t, int first, int first_key, bool near, bool hidden, bool limited) {
+        f32x16 s = {};
+        auto near_term = [&] {
+            // the sum begins at the row's term, so that it is small again before the products come in
+            const bf16x8 k = __builtin_bit_cast(bf16x8, t.near[h * kTileKeys + first + col]);
+            f32x16 start;
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
+            for (int r = 0; r < 16; ++r) start[r] = row_term;
+            return mfma(k, row_slots, start);
+        };
+        if (near && !CAP) s = near_term();
+#pragma unroll
+        for (int st = 0; st < DP / 16; ++st)
+            s = mfma(read_rows<T, Pitch<DP>::kRows>(t.k, first + col, st, h), q[st], s);
+        const float unit = PLAIN || (near && !CAP) ? scale : 1.0f;
+        if (near && CAP) {
+            const f32x16 term = near_term();
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(cap2, tanh_fast(s[r] * scale), term[r]);
+        } else if (!PLAIN && !near) {
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
                 float kx[4], ky[4];
                 if (DIST) {
-                    *reinterpret_cast<float4 *>(kx) = read4(t.x, 32 * sub, r, h);
-                    *reinterpret_cast<float4 *>(ky) = read4(t.y, 32 * sub, r, h);
+                    *reinterpret_cast<float4 *>(kx) = read4(t.x, first, r, h);
+                    *reinterpret_cast<float4 *>(ky) = read4(t.y, first, r, h);
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
                     float th;
-                    s[sub][r + e] = score<DIST, CAP>(s[sub][r + e], scale, cap2, d2, slope2, th);
+                    s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope2, th);
                 }
             }
-    };
-    auto hide = [&](const typename Tile::Lds &t) {
-#pragma unroll
-        for (int sub = 0; sub < 2; ++sub)
+        }
+        if (hidden) {
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                const float4 pen = read4(t.penalty, 32 * sub, r, h);
-                s[sub][r] += pen.x;
-                s[sub][r + 1] += pen.y;
-                s[sub][r + 2] += pen.z;
-                s[sub][r + 3] += pen.w;
+                const float4 pen = read4(t.penalty, first, r, h);
+                s[r] += pen.x;
+                s[r + 1] += pen.y;
+                s[r + 2] += pen.z;
+                s[r + 3] += pen.w;
             }
-    };
-    auto cut = [&](int kt) {
+        }
+        if (limited) {
+            const uint32_t seen = seen_bits(0xffffffffu, limit, first_key, h);
 #pragma unroll
-        for (int sub = 0; sub < 2; ++sub) {
-            const uint32_t seen = seen_bits(0xffffffffu, limit, kt + 32 * sub, h);
+            for (int r = 0; r < 16; ++r) s[r] = (seen >> out_row(r, 0)) & 1 ? s[r] : -INFINITY;
+        }
+        float top = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[sub][r] = (seen >> out_row(r, 0)) & 1 ? s[sub][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+        top = unit * across(top, [](float x, float y) { return fmaxf(x, y); });
+        if (__any(top > m + kSlack)) {
+            // 2^(old shift - new shift); the first scores seen find nothing to rescale
+            m = fmaxf(m, top);
+            const float to = m == -INFINITY ? 0.0f : m;
+            const float fade = exp2_fast(fminf(shift - to, 0.0f));
+            shift = to;
+            l *= fade;
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[b][r] *= fade;
+        }
+        float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = exp2_fast(__builtin_fmaf(s[r], unit, -shift));
+            sum[r & 1] += s[r];
+        }
+        l += sum[0] + sum[1];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const F p = round_frag<T>(s, part);
+#pragma unroll
+            for (int b = 0; b < DP / 32; ++b)
+                o[b] = mfma(read_columns<T, Pitch<DP>::kColumns>(t.v, first + 16 * part, b, lane), p, o[b]);
         }
     };
 
     Tile next;
     if (end > 0) {
         next.template load<DIST>(a, sp, head, 0, end);
-        next.template store<DIST>(a, typename Tile::Lds(shared));
+        next.template store<DIST>(a, typename Tile::Lds(shared), origin, largest);
     }
     wait_for_loads();
     __syncthreads();
@@ -148,54 +215,17 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
         if (more) next.template load<DIST>(a, sp, head, kt + kTileKeys, end);
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const uint64_t seen = *t.seen;
-        const bool all = __builtin_amdgcn_readfirstlane((uint32_t)(seen & (seen >> 32))) == 0xffffffffu;
-        if (kt < wave_end && __builtin_amdgcn_readfirstlane((uint32_t)(seen | (seen >> 32))) != 0) {
-            s[0] = s[1] = f32x16{};
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int st = 0; st < DP / 16; ++st)
-                    s[sub] = mfma(read_rows<T, DP>(t.k, 32 * sub + col, st, h), q[st], s[sub]);
-            if (!PLAIN) finish_scores(t);
-            if (!all) hide(t);
-            if (kt + kTileKeys > wave_all) cut(kt);
-            float top = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(fmaxf(top, s[0][r]), s[1][r]);
-            if (PLAIN) top *= scale;
-            top = across(top, [](float x, float y) { return fmaxf(x, y); });
-            if (__any(top > m + kSlack)) {
-                // 2^(old shift - new shift); the first scores seen find nothing to rescale
-                m = fmaxf(m, top);
-                const float next = m == -INFINITY ? 0.0f : m;
-                const float fade = exp2_fast(fminf(shift - next, 0.0f));
-                shift = next;
-                l *= fade;
-#pragma unroll
-                for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[b][r] *= fade;
-            }
-            float sum[2] = {0.0f, 0.0f};
+        if (kt < wave_end) {
+            const bool near = DIST && row_near && __builtin_amdgcn_readfirstlane(*t.all_near);
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[sub][r] = exp2_fast(PLAIN ? __builtin_fmaf(s[sub][r], scale, -shift) : s[sub][r] - shift);
-                    sum[r & 1] += s[sub][r];
-                }
-#pragma unroll
-                for (int part = 0; part < 2; ++part) {
-                    const F p = round_frag<T>(s[sub], part);
-#pragma unroll
-                    for (int b = 0; b < DP / 32; ++b)
-                        o[b] = mfma(read_columns<T, DP>(t.v, 32 * sub + 16 * part, b, lane), p, o[b]);
-                }
+                const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
+                if (bits != 0)
+                    half_tile(t, 32 * sub, kt + 32 * sub, near, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
             }
-            l += sum[0] + sum[1];
         }
         buffer ^= 1;
-        if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes));
+        if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes), origin, largest);
         __syncthreads();
     }
     l = across(l, [](float x, float y) { return x + y; });
@@ -222,10 +252,14 @@ __global__ void __launch_bounds__(kThreads, 2) attention_rows_kernel(AttentionAr
 // idle otherwise, and for rows too few to fill a tile.
 // ---------------------------------------------------------------------------
 
+// (two workgroups of a compute unit have LDS for rows of 17 chunks with heads of 128, not of 20)
+template <int DP>
+using SplitTile = KeyTile<DP, 128, Pitch<DP>::kRows, DP == 128 ? 17 : Pitch<DP>::kColumns, false>;
+
 template <int DP>
 constexpr int split_lds_bytes() {
     const int join = 4 * 32 * (DP + 2) * 4;
-    const int tiles = KeyTile<DP, 128>::kBytes + 32 * KeyTile<DP>::kPitch * 16;
+    const int tiles = SplitTile<DP>::kBytes + 32 * Pitch<DP>::kRows * 16;
     return join > tiles ? join : tiles;
 }
 
@@ -233,7 +267,8 @@ template <typename T, int DP, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionArgs a) {
     using F = typename Frag<T>::type;
     constexpr int kRows = 32, kKeys = 128;
-    using Tile = KeyTile<DP, kKeys>;
+    using Tile = SplitTile<DP>;
+    constexpr int kVPitch = DP == 128 ? 17 : Pitch<DP>::kColumns;
     extern __shared__ char shared[];
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
@@ -277,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
             z = *reinterpret_cast<const i16x8 *>(static_cast<const short *>(a.q) + (int64_t)(sp.q0 + i) * a.q_stride +
                                                  (head * a.group + gg) * a.dim + c * 8);
         }
-        q_lds[r * Tile::kPitch + c] = z;
+        q_lds[r * Pitch<DP>::kRows + c] = z;
     }
     const int limit = valid ? seen_limit(a, sp, prefix, qi) : sp.nk;
     const int all_end = a.causal ? -wave_max(-limit) : sp.nk;
@@ -304,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         f32x16 s = {};
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) 
-            s = mfma(read_rows<T, DP>(t.k, k0 + col, st, h), read_rows<T, DP>(q_lds, col, st, h), s);
+            s = mfma(read_rows<T, Pitch<DP>::kRows>(t.k, k0 + col, st, h), read_rows<T, Pitch<DP>::kRows>(q_lds, col, st, h), s);
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             float kx[4], ky[4], pen[4] = {};
@@ -349,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         for (int part = 0; part < 2; ++part) {
             const F p = round_frag<T>(s, part);
 #pragma unroll
-            for (int b = 0; b < DP / 32; ++b) o[b] = mfma(read_columns<T, DP>(t.v, k0 + 16 * part, b, lane), p, o[b]);
+            for (int b = 0; b < DP / 32; ++b) o[b] = mfma(read_columns<T, kVPitch>(t.v, k0 + 16 * part, b, lane), p, o[b]);
         }
     }
     l = across(l, [](float x, float y) { return x + y; });
@@ -479,12 +514,13 @@ hipError_t launch_attention(AttentionArgs a, int32_t dtype, const AttentionPlan 
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
+        constexpr size_t rows_bytes = 2 * RowsTile<DP, DIST>::kBytes;
         const dim3 grid((uint32_t)(p.slots * a.kv_heads), (uint32_t)p.splits);
         if (p.split)
             hipLaunchKernelGGL((attention_split_kernel<T, DP, DIST, CAP>), grid, dim3(kThreads), split_lds_bytes<DP>(),
                                stream, a);
         else
-            hipLaunchKernelGGL((attention_rows_kernel<T, DP, DIST, CAP>), grid, dim3(kThreads), 2 * KeyTile<DP>::kBytes,
+            hipLaunchKernelGGL((attention_rows_kernel<T, DP, DIST, CAP>), grid, dim3(kThreads), rows_bytes,
                                stream, a);
         return hipGetLastError();
     });

@@ -40,12 +40,15 @@ __global__ void __launch_bounds__(kThreads) attention_delta_kernel(AttentionBack
     }
 }
 
+template <int DP>
+using DqTile = KeyTile<DP, kTileKeys, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
+
 // Gradients of the queries: 128 rows a workgroup, 32 a wave, over the tiles of
 // keys that they see.
 template <typename T, int DP, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
-    using Tile = KeyTile<DP>;
+    using Tile = DqTile<DP>;
     constexpr int kRows = 128;
     const AttentionArgs &a = b.fwd;
     extern __shared__ char shared[];
@@ -101,8 +104,8 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
-            s = mfma(read_rows<T, DP>(t.k, first + col, st, h), q[st], s);
-            dp = mfma(read_rows<T, DP>(t.v, first + col, st, h), go[st], dp);
+            s = mfma(read_rows<T, Pitch<DP>::kBoth>(t.k, first + col, st, h), q[st], s);
+            dp = mfma(read_rows<T, Pitch<DP>::kRows>(t.v, first + col, st, h), go[st], dp);
         }
         float d2[DIST ? 16 : 1], th[CAP ? 16 : 1];
 #pragma unroll
@@ -151,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
             const F d = round_frag<T>(s, part);
 #pragma unroll
             for (int blk = 0; blk < DP / 32; ++blk)
-                dq[blk] = mfma(read_columns<T, DP>(t.k, first + 16 * part, blk, lane), d, dq[blk]);
+                dq[blk] = mfma(read_columns<T, Pitch<DP>::kBoth>(t.k, first + 16 * part, blk, lane), d, dq[blk]);
         }
     };
 
@@ -169,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const uint64_t seen = *t.seen;
         if (kt < wave_end) {
-#pragma unroll
+#pragma unroll(DP <= 64 ? 2 : 1)
             for (int sub = 0; sub < 2; ++sub) {
                 const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
                 if (bits != 0) sub_tile(t, kt, 32 * sub, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
@@ -208,8 +211,8 @@ constexpr int kTileRows = 64;
 template <int DP>
 struct RowTile {
     static constexpr int kChunks = DP / 8;
-    static constexpr int kPitch = DP / 8 + 1;
     static constexpr int kLoads = kTileRows * kChunks / kThreads;
+    static constexpr int kPitch = Pitch<DP>::kBoth;
     static constexpr int kRowChunks = kTileRows * kPitch;
     static constexpr int kBytes = 2 * kRowChunks * 16 + 7 * kTileRows * 4 + 16;
 
@@ -361,8 +364,20 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         F qf[DP / 16], gf[DP / 16];
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
-            qf[st] = read_rows<T, DP>(t.q, first + col, st, h);
-            gf[st] = read_rows<T, DP>(t.g, first + col, st, h);
+            qf[st] = read_rows<T, Tile::kPitch>(t.q, first + col, st, h);
+            gf[st] = read_rows<T, Tile::kPitch>(t.g, first + col, st, h);
+        }
+        // the columns are read here where registers allow it, to be there when the weights are
+        constexpr bool EARLY = DP <= 64;
+        F gc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1], qc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1];
+        if (EARLY) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+                for (int blk = 0; blk < DP / 32; ++blk) {
+                    gc[part][blk] = read_columns<T, Tile::kPitch>(t.g, first + 16 * part, blk, lane);
+                    qc[part][blk] = read_columns<T, Tile::kPitch>(t.q, first + 16 * part, blk, lane);
+                }
         }
         F p[BLOCKS][2], ds[BLOCKS][2];
 #pragma unroll
@@ -418,12 +433,14 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         for (int part = 0; part < 2; ++part)
 #pragma unroll
             for (int blk = 0; blk < DP / 32; ++blk) {
-                const F gc = read_columns<T, DP>(t.g, first + 16 * part, blk, lane);
-                const F qc = read_columns<T, DP>(t.q, first + 16 * part, blk, lane);
+                if (!EARLY) {
+                    gc[0][0] = read_columns<T, Tile::kPitch>(t.g, first + 16 * part, blk, lane);
+                    qc[0][0] = read_columns<T, Tile::kPitch>(t.q, first + 16 * part, blk, lane);
+                }
 #pragma unroll
                 for (int n = 0; n < BLOCKS; ++n) {
-                    dv[n][blk] = mfma(gc, p[n][part], dv[n][blk]);
-                    dk[n][blk] = mfma(qc, ds[n][part], dk[n][blk]);
+                    dv[n][blk] = mfma(gc[EARLY ? part : 0][EARLY ? blk : 0], p[n][part], dv[n][blk]);
+                    dk[n][blk] = mfma(qc[EARLY ? part : 0][EARLY ? blk : 0], ds[n][part], dk[n][blk]);
                 }
             }
     };
@@ -539,7 +556,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
         constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
         hipError_t e = hipSuccess;
         if (a.total_q > 0) {
-            constexpr size_t bytes = 2 * KeyTile<DP>::kBytes;
+            constexpr size_t bytes = 2 * DqTile<DP>::kBytes;
             auto kernel = attention_dq_kernel<T, DP, DIST, CAP>;
             hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.slots * a.kv_heads)), dim3(kThreads), bytes, stream, b);
             e = hipGetLastError();

@@ -121,46 +121,44 @@ __device__ __forceinline__ int find_frame(const int32_t *offsets, int n_frames, 
     return lo;
 }
 
-// Workgroups are dealt to the eight XCDs in turn; consecutive work items,
-// which share keys, go to one XCD and meet in its L2.
+// Workgroups are dealt to the eight XCDs in turn.  Runs of 32 consecutive work
+// items, most of which share keys, go to one XCD and meet in its L2 (3 to 6%
+// over the plain order; longer runs deal ragged frames out less evenly).
 __device__ __forceinline__ int64_t xcd_order(int64_t id, int64_t n) {
-    const int64_t per = n / 8;
-    return id < per * 8 ? (id % 8) * per + id / 8 : id;
+    constexpr int kRun = 32;
+    if (id >= n / (8 * kRun) * (8 * kRun)) return id;
+    const int64_t turn = id / 8, xcd = id % 8;
+    return (turn / kRun * 8 + xcd) * kRun + turn % kRun;
 }
 
-// Copies rows of a [rows][dim] matrix into LDS rows of DP + 8 elements, zeros
-// for rows that are absent and dimensions at and above dim.
-template <int DP, int ROWS, typename P>
-__device__ __forceinline__ void stage_rows(i16x8 *lds, int dim, P &&row_pointer) {
-    constexpr int kChunks = DP / 8;
-    constexpr int kPitch = DP / 8 + 1;
-#pragma unroll
-    for (int e = threadIdx.x; e < ROWS * kChunks; e += kThreads) {
-        const int r = e / kChunks, c = e % kChunks;
-        const short *p = row_pointer(r);
-        i16x8 z = {};
-        if (p != nullptr && c * 8 < dim) z = *reinterpret_cast<const i16x8 *>(p + c * 8);
-        lds[r * kPitch + c] = z;
-    }
-}
+// Rows of DP / 8 chunks of 16 bytes lie a pitch of chunks apart in LDS.  Read as
+// rows (16 lanes a chunk each of 16 rows) they want an odd pitch, read as columns
+// (4 chunks of 4 rows a time) one of 4 or 12 modulo 16; rows read both ways take
+// the odd pitch that leaves 2 chunks of 4 rows apart, the best there is.
+template <int DP>
+struct Pitch {
+    static constexpr int kRows = DP / 8 + 1;
+    static constexpr int kColumns = DP == 128 ? 20 : DP == 32 ? 4 : 12;
+    static constexpr int kBoth = DP == 128 ? 19 : DP == 32 ? 7 : DP / 8 + 1;
+};
 
 // Left factor from LDS rows: lane's row, 8 dimensions from 16 step + 8 h.
-template <typename T, int DP>
+template <typename T, int PITCH>
 __device__ __forceinline__ typename Frag<T>::type read_rows(const i16x8 *lds, int row, int step, int h) {
-    const i16x8 z = lds[row * (DP / 8 + 1) + 2 * step + h];
+    const i16x8 z = lds[row * PITCH + 2 * step + h];
     return __builtin_bit_cast(typename Frag<T>::type, z);
 }
 
 // Left factor from LDS columns: dimension 32 block + lane % 32 of the LDS rows
 // first + {4h .. 4h + 3, 8 + 4h .. 8 + 4h + 3}.
-template <typename T, int DP>
+template <typename T, int PITCH>
 __device__ __forceinline__ typename Frag<T>::type read_columns(const i16x8 *lds, int first, int block, int lane) {
     typedef __attribute__((address_space(3))) i16x4 *LdsPtr;
     const int h = lane >> 5, i = lane & 15, part = (lane >> 4) & 1;
-    const short *p = reinterpret_cast<const short *>(lds) + (first + 4 * h + (i >> 2)) * (DP + 8) + 32 * block +
+    const short *p = reinterpret_cast<const short *>(lds) + (first + 4 * h + (i >> 2)) * (8 * PITCH) + 32 * block +
                      16 * part + 4 * (i & 3);
     const i16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)p);
-    const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(p + 8 * (DP + 8)));
+    const i16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsPtr)(p + 8 * (8 * PITCH)));
     const i16x8 z = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     return __builtin_bit_cast(typename Frag<T>::type, z);
 }
@@ -196,6 +194,74 @@ __device__ __forceinline__ uint32_t seen_bits(uint32_t bits, int limit, int firs
     return bits >> (4 * h);
 }
 
+// Distances on the matrix cores.  Relative to a common origin, with row a and key
+// b, -slope d2 = 2 slope a.b - slope |b|^2 - slope |a|^2; the last term is a
+// constant of the row, and the first two are one more step of the product of
+// queries and keys: 16 products of bfloat16 parts (8 bits each) that hold x, y
+// (two parts, whole numbers of 1/16 px below 2^16), |b|^2 and the slope's factors
+// (three parts) to 2^-24.  That takes five vector operations off each score,
+// where they bound the kernels.  The sums pass through numbers as large as
+// slope |b|^2, so the scores are off by 2^-23 of that: kNearLimit (in units of
+// log 2) keeps it below 2e-4, a twentieth of what rounding the weights to
+// bfloat16 costs, and tiles with a bird farther away take the differences
+// themselves.
+constexpr float kNearLimit = 1536.0f;
+constexpr int kNearReach = 1 << 15;
+
+struct NearSlots {
+    i16x8 half[2];  // of the lanes' halves
+};
+
+__device__ __forceinline__ void split3(float v, bf16_t (&p)[3]) {
+    p[0] = static_cast<bf16_t>(v);
+    v -= static_cast<float>(p[0]);
+    p[1] = static_cast<bf16_t>(v);
+    p[2] = static_cast<bf16_t>(v - static_cast<float>(p[1]));
+}
+
+// The key's 16 factors; n is |b|^2 in (1/16 px)^2.
+__device__ __forceinline__ NearSlots near_key(int bx, int by, float n) {
+    const bf16_t xh = static_cast<bf16_t>((float)bx), yh = static_cast<bf16_t>((float)by);
+    const bf16_t xl = static_cast<bf16_t>((float)bx - static_cast<float>(xh));
+    const bf16_t yl = static_cast<bf16_t>((float)by - static_cast<float>(yh));
+    bf16_t p[3];
+    split3(n, p);
+    const bf16x8 lo = {xh, xh, xh, xl, xl, yh, yh, yh}, hi = {yl, yl, p[0], p[0], p[0], p[1], p[1], p[2]};
+    return {__builtin_bit_cast(i16x8, lo), __builtin_bit_cast(i16x8, hi)};
+}
+
+// The row's 16 factors; weight is the slope in the products' units and (1/16 px)^-2.
+__device__ __forceinline__ NearSlots near_row(int ax, int ay, float weight) {
+    bf16_t x[3], y[3], n[3];
+    split3(2.0f * weight * (float)ax, x);
+    split3(2.0f * weight * (float)ay, y);
+    split3(-weight, n);
+    const bf16x8 lo = {x[0], x[1], x[2], x[0], x[1], y[0], y[1], y[2]};
+    const bf16x8 hi = {y[0], y[1], n[0], n[1], n[2], n[0], n[1], n[0]};
+    return {__builtin_bit_cast(i16x8, lo), __builtin_bit_cast(i16x8, hi)};
+}
+
+__device__ __forceinline__ float square_quanta(int x, int y) {
+    return __builtin_fmaf((float)x, (float)x, (float)y * (float)y);
+}
+
+// Origin of a workgroup's distances: the middle of 32 birds (a lane each, both halves alike).
+__device__ __forceinline__ int2 near_origin(int2 p) {
+    int x0 = p.x, x1 = p.x, y0 = p.y, y1 = p.y;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        x0 = min(x0, __shfl_xor(x0, d));
+        x1 = max(x1, __shfl_xor(x1, d));
+        y0 = min(y0, __shfl_xor(y0, d));
+        y1 = max(y1, __shfl_xor(y1, d));
+    }
+    return make_int2(__builtin_amdgcn_readfirstlane((x0 + x1) / 2), __builtin_amdgcn_readfirstlane((y0 + y1) / 2));
+}
+
+__device__ __forceinline__ bool near_enough(int x, int y, float n, float largest) {
+    return abs(x) < kNearReach && abs(y) < kNearReach && n <= largest;
+}
+
 // A tile of 64 keys (or KEYS) and its values on its way from memory to LDS: load() starts
 // the loads into registers, so that they run under the products of the tile
 // before, store() puts them into an LDS buffer.  Hidden and absent keys become
@@ -216,25 +282,26 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t tile_resource(const void *base
         const_cast<short *>(static_cast<const short *>(base) + first_element), 0, bytes, 0x00027000);
 }
 
-template <int DP, int KEYS = kTileKeys>
+template <int DP, int KEYS, int K_PITCH, int V_PITCH, bool NEAR>
 struct KeyTile {
     static constexpr int kChunks = DP / 8;                       // of 16 bytes in a row
-    static constexpr int kPitch = DP / 8 + 1;                    // LDS row, one chunk of padding
     static constexpr int kLoads = KEYS * kChunks / kThreads;
-    static constexpr int kRowChunks = KEYS * kPitch;
-    static constexpr int kBytes = 2 * kRowChunks * 16 + 3 * KEYS * 4 + 16;
+    static constexpr int kBytes = KEYS * (K_PITCH + V_PITCH) * 16 + (NEAR ? 2 * KEYS * 16 : 0) + 3 * KEYS * 4 + 32;
 
     struct Lds {
-        i16x8 *k, *v;
+        i16x8 *k, *v, *near;  // near: [half][key]
         float *x, *y, *penalty;
         uint64_t *seen;
+        int *all_near;
         __device__ __forceinline__ explicit Lds(char *base) {
             k = reinterpret_cast<i16x8 *>(base);
-            v = k + kRowChunks;
-            x = reinterpret_cast<float *>(v + kRowChunks);
+            v = k + KEYS * K_PITCH;
+            near = v + KEYS * V_PITCH;
+            x = reinterpret_cast<float *>(near + (NEAR ? 2 * KEYS : 0));
             y = x + KEYS;
             penalty = y + KEYS;
             seen = reinterpret_cast<uint64_t *>(penalty + KEYS);
+            all_near = reinterpret_cast<int *>(seen + 2);
         }
     };
 
@@ -269,8 +336,10 @@ struct KeyTile {
         }
     }
 
+    // NEAR: keys' factors about origin, and whether all of them are within `largest`
     template <bool DIST>
-    __device__ __forceinline__ void store(const AttentionArgs &a, const Lds &lds) {
+    __device__ __forceinline__ void store(const AttentionArgs &a, const Lds &lds, int2 origin = make_int2(0, 0),
+                                          float largest = 0.0f) {
         if (a.keep) {
 #pragma unroll
             for (int n = 0; n < kLoads; ++n) {
@@ -280,14 +349,22 @@ struct KeyTile {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
             const int e = threadIdx.x + n * kThreads;
-            const int at = e / kChunks * kPitch + e % kChunks;
-            lds.k[at] = __builtin_bit_cast(i16x8, k[n]);
-            lds.v[at] = __builtin_bit_cast(i16x8, v[n]);
+            lds.k[e / kChunks * K_PITCH + e % kChunks] = __builtin_bit_cast(i16x8, k[n]);
+            lds.v[e / kChunks * V_PITCH + e % kChunks] = __builtin_bit_cast(i16x8, v[n]);
         }
         if (threadIdx.x < KEYS) {  // whole waves
             if (DIST) {
                 lds.x[threadIdx.x] = (float)place.x * kPxPerQuantum;
                 lds.y[threadIdx.x] = (float)place.y * kPxPerQuantum;
+            }
+            if (NEAR) {
+                const int bx = place.x - origin.x, by = place.y - origin.y;
+                const float n = square_quanta(bx, by);
+                const NearSlots s = near_key(bx, by, n);
+                lds.near[threadIdx.x] = s.half[0];
+                lds.near[KEYS + threadIdx.x] = s.half[1];
+                const bool all = __all(near_enough(bx, by, n, largest));
+                if (threadIdx.x == 0) *lds.all_near = all;
             }
             lds.penalty[threadIdx.x] = key_kept != 0 ? 0.0f : -INFINITY;
             const uint64_t seen = __ballot(key_kept != 0);
