@@ -201,11 +201,12 @@ __device__ __forceinline__ uint32_t seen_bits(uint32_t bits, int limit, int firs
 // (two parts, whole numbers of 1/16 px below 2^16), |b|^2 and the slope's factors
 // (three parts) to 2^-24.  That takes five vector operations off each score,
 // where they bound the kernels.  The sums pass through numbers as large as
-// slope |b|^2, so the scores are off by 2^-23 of that: kNearLimit (in units of
-// log 2) keeps it below 2e-4, a twentieth of what rounding the weights to
-// bfloat16 costs, and tiles with a bird farther away take the differences
-// themselves.
-constexpr float kNearLimit = 1536.0f;
+// slope |b|^2, so the scores are off by 2^-23 of that.  near_limit (in units of log
+// 2) keeps the weights' relative error a tenth of what rounding them to the
+// operands' type costs in bfloat16, a quarter in float16, and tiles with a bird
+// farther away take the differences themselves.
+template <typename T> constexpr float near_limit() { return 4096.0f; }
+template <> constexpr float near_limit<half_t>() { return 1536.0f; }
 constexpr int kNearReach = 1 << 15;
 
 struct NearSlots {
