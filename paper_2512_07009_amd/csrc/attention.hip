@@ -117,62 +117,81 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
     f32x16 o[DP / 32] = {};
     float m = -INFINITY, shift = 0.0f, l = 0.0f;
 
-    // Half a tile.  A weight is 2^(s * unit - shift): scores without caps (and with
-    // distances on the matrix cores) stay products until then.
+    // A tile is worked on at once where registers allow it for the waves there are
+    // (no distances; a third faster for it), else by halves.  A weight is
+    // 2^(s * unit - shift): scores without caps (and with distances on the matrix
+    // cores) stay products until then.
     constexpr bool PLAIN = !DIST && !CAP;
-    auto half_tile = [&](const typename Tile::Lds &t, int first, int first_key, bool near, bool hidden, bool limited) {
-        f32x16 s = {};
-        auto near_term = [&] {
-            // the sum begins at the row's term, so that it is small again before the products come in
-            const bf16x8 k = __builtin_bit_cast(bf16x8, t.near[h * kTileKeys + first + col]);
-            f32x16 start;
+    constexpr int SUBS = DIST ? 1 : 2;
+    auto near_term = [&](const typename Tile::Lds &t, int first) {
+        // the sum begins at the row's term, so that it is small again before the products come in
+        const bf16x8 k = __builtin_bit_cast(bf16x8, t.near[h * kTileKeys + first + col]);
+        f32x16 start;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) start[r] = row_term;
-            return mfma(k, row_slots, start);
-        };
-        if (near && !CAP) s = near_term();
+        for (int r = 0; r < 16; ++r) start[r] = row_term;
+        return mfma(k, row_slots, start);
+    };
+    auto work = [&](const typename Tile::Lds &t, int first, int first_key, bool near, bool hidden, bool limited) {
+        f32x16 s[SUBS];
 #pragma unroll
-        for (int st = 0; st < DP / 16; ++st)
-            s = mfma(read_rows<T, Pitch<DP>::kRows>(t.k, first + col, st, h), q[st], s);
+        for (int u = 0; u < SUBS; ++u) {
+            s[u] = f32x16{};
+            if (near && !CAP) s[u] = near_term(t, first + 32 * u);
+#pragma unroll
+            for (int st = 0; st < DP / 16; ++st)
+                s[u] = mfma(read_rows<T, Pitch<DP>::kRows>(t.k, first + 32 * u + col, st, h), q[st], s[u]);
+        }
         const float unit = PLAIN || (near && !CAP) ? scale : 1.0f;
         if (near && CAP) {
-            const f32x16 term = near_term();
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(cap2, tanh_fast(s[r] * scale), term[r]);
+            for (int u = 0; u < SUBS; ++u) {
+                const f32x16 term = near_term(t, first + 32 * u);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(cap2, tanh_fast(s[u][r] * scale), term[r]);
+            }
         } else if (!PLAIN && !near) {
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                float kx[4], ky[4];
-                if (DIST) {
-                    *reinterpret_cast<float4 *>(kx) = read4(t.x, first, r, h);
-                    *reinterpret_cast<float4 *>(ky) = read4(t.y, first, r, h);
-                }
+            for (int u = 0; u < SUBS; ++u)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
-                    float th;
-                    s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope2, th);
+                for (int r = 0; r < 16; r += 4) {
+                    float kx[4], ky[4];
+                    if (DIST) {
+                        *reinterpret_cast<float4 *>(kx) = read4(t.x, first + 32 * u, r, h);
+                        *reinterpret_cast<float4 *>(ky) = read4(t.y, first + 32 * u, r, h);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
+                        float th;
+                        s[u][r + e] = score<DIST, CAP>(s[u][r + e], scale, cap2, d2, slope2, th);
+                    }
                 }
-            }
         }
         if (hidden) {
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const float4 pen = read4(t.penalty, first, r, h);
-                s[r] += pen.x;
-                s[r + 1] += pen.y;
-                s[r + 2] += pen.z;
-                s[r + 3] += pen.w;
-            }
+            for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const float4 pen = read4(t.penalty, first + 32 * u, r, h);
+                    s[u][r] += pen.x;
+                    s[u][r + 1] += pen.y;
+                    s[u][r + 2] += pen.z;
+                    s[u][r + 3] += pen.w;
+                }
         }
         if (limited) {
-            const uint32_t seen = seen_bits(0xffffffffu, limit, first_key, h);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = (seen >> out_row(r, 0)) & 1 ? s[r] : -INFINITY;
+            for (int u = 0; u < SUBS; ++u) {
+                const uint32_t seen = seen_bits(0xffffffffu, limit, first_key + 32 * u, h);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = (seen >> out_row(r, 0)) & 1 ? s[u][r] : -INFINITY;
+            }
         }
         float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) top = fmaxf(top, s[u][r]);
         top = unit * across(top, [](float x, float y) { return fmaxf(x, y); });
         if (__any(top > m + kSlack)) {
             // 2^(old shift - new shift); the first scores seen find nothing to rescale
@@ -188,23 +207,28 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         }
         float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = exp2_fast(__builtin_fmaf(s[r], unit, -shift));
-            sum[r & 1] += s[r];
+        for (int u = 0; u < SUBS; ++u) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[u][r] = exp2_fast(__builtin_fmaf(s[u][r], unit, -shift));
+                sum[r & 1] += s[u][r];
+            }
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const F p = round_frag<T>(s[u], part);
+#pragma unroll
+                for (int b = 0; b < DP / 32; ++b)
+                    o[b] = mfma(read_columns<T, Pitch<DP>::kColumns>(t.v, first + 32 * u + 16 * part, b, lane), p, o[b]);
+            }
         }
         l += sum[0] + sum[1];
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const F p = round_frag<T>(s, part);
-#pragma unroll
-            for (int b = 0; b < DP / 32; ++b)
-                o[b] = mfma(read_columns<T, Pitch<DP>::kColumns>(t.v, first + 16 * part, b, lane), p, o[b]);
-        }
     };
 
     Tile next;
     if (end > 0) {
+        next.look_up(a, sp, 0, end);
         next.template load<DIST>(a, sp, head, 0, end);
+        next.look_up(a, sp, kTileKeys, end);
         next.template store<DIST>(a, typename Tile::Lds(shared), origin, largest);
     }
     wait_for_loads();
@@ -212,16 +236,21 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
     int buffer = 0;
     for (int kt = 0; kt < end; kt += kTileKeys) {
         const bool more = kt + kTileKeys < end;
-        if (more) next.template load<DIST>(a, sp, head, kt + kTileKeys, end);
+        if (more) {
+            next.template load<DIST>(a, sp, head, kt + kTileKeys, end);
+            next.look_up(a, sp, kt + 2 * kTileKeys, end);
+        }
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const uint64_t seen = *t.seen;
         if (kt < wave_end) {
             const bool near = DIST && row_near && __builtin_amdgcn_readfirstlane(*t.all_near);
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
-                if (bits != 0)
-                    half_tile(t, 32 * sub, kt + 32 * sub, near, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
+            for (int sub = 0; sub < 2; sub += SUBS) {
+                constexpr uint64_t kAll = SUBS == 2 ? ~0ull : 0xffffffffull;
+                const uint64_t bits = (seen >> (32 * sub)) & kAll;
+                const uint32_t some = __builtin_amdgcn_readfirstlane((uint32_t)(bits | (bits >> 32)));
+                const bool hidden = __builtin_amdgcn_readfirstlane(bits == kAll) == 0;
+                if (some != 0) work(t, 32 * sub, kt + 32 * sub, near, hidden, kt + 32 * (sub + SUBS) > wave_all);
             }
         }
         buffer ^= 1;
@@ -294,7 +323,11 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         end = (int)min(begin + (int64_t)per, (int64_t)end);
     }
     Tile next;
-    if (begin < end) next.template load<DIST>(a, sp, head, begin, end);
+    if (begin < end) {
+        next.look_up(a, sp, begin, end);
+        next.template load<DIST>(a, sp, head, begin, end);
+        next.look_up(a, sp, begin + kKeys, end);
+    }
 
     // this lane's query
     const bool valid = row0 + col < n_rows;
@@ -333,7 +366,10 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         if (kt > begin) __syncthreads();
         next.template store<DIST>(a, t);
         __syncthreads();
-        if (kt + kKeys < end) next.template load<DIST>(a, sp, head, kt + kKeys, end);
+        if (kt + kKeys < end) {
+            next.template load<DIST>(a, sp, head, kt + kKeys, end);
+            next.look_up(a, sp, kt + 2 * kKeys, end);
+        }
         const uint32_t bits = __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t *>(t.seen)[wave]);
         if (bits == 0) continue;
         f32x16 s = {};

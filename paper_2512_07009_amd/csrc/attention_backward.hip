@@ -40,8 +40,9 @@ __global__ void __launch_bounds__(kThreads) attention_delta_kernel(AttentionBack
     }
 }
 
+// Wide heads leave registers for half as many keys in flight.
 template <int DP>
-using DqTile = KeyTile<DP, kTileKeys, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
+using DqTile = KeyTile<DP, DP <= 64 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
 
 // Gradients of the queries: 128 rows a workgroup, 32 a wave, over the tiles of
 // keys that they see.
@@ -49,7 +50,7 @@ template <typename T, int DP, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = DqTile<DP>;
-    constexpr int kRows = 128;
+    constexpr int kRows = 128, kKeys = DP <= 64 ? 64 : 32;
     const AttentionArgs &a = b.fwd;
     extern __shared__ char shared[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
@@ -160,20 +161,25 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
 
     Tile next;
     if (end > 0) {
+        next.look_up(a, sp, 0, end);
         next.template load<DIST>(a, sp, head, 0, end);
+        next.look_up(a, sp, kKeys, end);
         next.template store<DIST>(a, typename Tile::Lds(shared));
     }
     wait_for_loads();
     __syncthreads();
     int buffer = 0;
-    for (int kt = 0; kt < end; kt += kTileKeys) {
-        const bool more = kt + kTileKeys < end;
-        if (more) next.template load<DIST>(a, sp, head, kt + kTileKeys, end);
+    for (int kt = 0; kt < end; kt += kKeys) {
+        const bool more = kt + kKeys < end;
+        if (more) {
+            next.template load<DIST>(a, sp, head, kt + kKeys, end);
+            next.look_up(a, sp, kt + 2 * kKeys, end);
+        }
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const uint64_t seen = *t.seen;
         if (kt < wave_end) {
-#pragma unroll(DP <= 64 ? 2 : 1)
-            for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+            for (int sub = 0; sub < kKeys / 32; ++sub) {
                 const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
                 if (bits != 0) sub_tile(t, kt, 32 * sub, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
             }

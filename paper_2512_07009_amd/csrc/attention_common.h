@@ -307,9 +307,18 @@ struct KeyTile {
     };
 
     i32x4 k[kLoads], v[kLoads];
-    // as loaded: what is made of them waits for the loads, so it is made in store()
+    // as loaded: what is made of them waits for the loads, so it is made in store(),
+    // and a tile's hidden keys are looked up a tile ahead, so that load() can send
+    // them beyond the resource
     uint8_t kept[kLoads], key_kept;
     int2 place;
+
+    __device__ __forceinline__ void look_up(const AttentionArgs &a, const Span &sp, int first, int end) {
+        if (!a.keep || first >= end) return;
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n)
+            kept[n] = a.keep[sp.k0 + min(first + (int)(threadIdx.x + n * kThreads) / kChunks, end - 1)];
+    }
 
     template <bool DIST>
     __device__ __forceinline__ void load(const AttentionArgs &a, const Span &sp, int head, int first, int end) {
@@ -323,11 +332,11 @@ struct KeyTile {
         for (int n = 0; n < kLoads; ++n) {
             const int e = threadIdx.x + (kEven ? 0 : n * kThreads);
             const int r = e / kChunks, c = e % kChunks;
-            const bool in = c * 8 < a.dim;
+            bool in = c * 8 < a.dim;
             const int more = kEven ? n * (kThreads / kChunks) : 0;
+            if (a.keep) in = in && kept[n] != 0;
             k[n] = __builtin_amdgcn_raw_buffer_load_b128(kr, in ? r * k_step + c * 16 : kBeyond, more * k_step, 0);
             v[n] = __builtin_amdgcn_raw_buffer_load_b128(vr, in ? r * v_step + c * 16 : kBeyond, more * v_step, 0);
-            if (a.keep) kept[n] = a.keep[row0 + min(r + more, rows - 1)];
         }
         if (threadIdx.x < KEYS) {
             key_kept = (int)threadIdx.x < rows;
@@ -341,12 +350,6 @@ struct KeyTile {
     template <bool DIST>
     __device__ __forceinline__ void store(const AttentionArgs &a, const Lds &lds, int2 origin = make_int2(0, 0),
                                           float largest = 0.0f) {
-        if (a.keep) {
-#pragma unroll
-            for (int n = 0; n < kLoads; ++n) {
-                if (kept[n] == 0) k[n] = v[n] = i32x4{0, 0, 0, 0};
-            }
-        }
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
             const int e = threadIdx.x + n * kThreads;
