@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
-    const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
     // distances on the matrix cores: the row's factors, what they leave for the
     // row, and the largest |b|^2 that any slope of the rows' heads allows
     int2 origin = make_int2(0, 0);
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         const float n = square_quanta(ax, ay), weight = slope2 / 256.0f;
         row_near = __all(!valid || near_enough(ax, ay, n, largest));
         const float units = CAP ? weight : weight / scale;
-        row_term = -units * n;
+        row_term = -units * n + (CAP ? cap2 : 0.0f);  // with the constant of tanh = 1 - 2 r
         const NearSlots s = near_row(ax, ay, units);
         row_slots = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
     }
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
             for (int u = 0; u < SUBS; ++u) {
                 const f32x16 term = near_term(t, first + 32 * u);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(cap2, tanh_fast(s[u][r] * scale), term[r]);
+                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(-2.0f * cap2, tanh_part(s[u][r] * scale), term[r]);
             }
         } else if (!PLAIN && !near) {
 #pragma unroll
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
-    const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
 
     f32x16 o[DP / 32] = {};
     float m = -INFINITY, shift = 0.0f, l = 0.0f;

@@ -40,17 +40,17 @@ __global__ void __launch_bounds__(kThreads) attention_delta_kernel(AttentionBack
     }
 }
 
-// Wide heads leave registers for half as many keys in flight.
+// Heads of 128 leave registers for half as many keys in flight.
 template <int DP>
-using DqTile = KeyTile<DP, DP <= 64 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
+using DqTile = KeyTile<DP, DP <= 96 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
 
 // Gradients of the queries: 128 rows a workgroup, 32 a wave, over the tiles of
 // keys that they see.
 template <typename T, int DP, bool DIST, bool CAP>
-__global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBackwardArgs b) {
+__global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_dq_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = DqTile<DP>;
-    constexpr int kRows = 128, kKeys = DP <= 64 ? 64 : 32;
+    constexpr int kRows = 128, kKeys = DP <= 96 ? 64 : 32;
     const AttentionArgs &a = b.fwd;
     extern __shared__ char shared[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
-    const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
     float shift, rest;
     split_lse(valid ? a.lse[qrow * a.q_heads + qh] : -INFINITY, shift, rest);
     const float delta = valid ? b.delta[qrow * a.q_heads + qh] * rest : 0.0f;
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
                 pdpd2 = __builtin_fmaf(pd, d2[r], pdpd2);
             }
             float ds = p * __builtin_fmaf(dp[r], rest, -delta);
-            if (CAP) ds *= __builtin_fmaf(-th[r], th[r], 1.0f);
+            if (CAP) ds *= tanh_slope(th[r]);
             s[r] = ds;
         }
 #pragma unroll
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const uint64_t seen = *t.seen;
         if (kt < wave_end) {
-#pragma unroll
+#pragma unroll(DP <= 64 ? 2 : 1)
             for (int sub = 0; sub < kKeys / 32; ++sub) {
                 const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
                 if (bits != 0) sub_tile(t, kt, 32 * sub, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
@@ -214,29 +214,32 @@ __global__ void __launch_bounds__(kThreads, 2) attention_dq_kernel(AttentionBack
 // gradients and what their scores need, on its way to LDS as KeyTile is.
 constexpr int kTileRows = 64;
 
-template <int DP>
+template <int DP, bool NEAR>
 struct RowTile {
     static constexpr int kChunks = DP / 8;
     static constexpr int kLoads = kTileRows * kChunks / kThreads;
     static constexpr int kPitch = Pitch<DP>::kBoth;
     static constexpr int kRowChunks = kTileRows * kPitch;
-    static constexpr int kBytes = 2 * kRowChunks * 16 + 7 * kTileRows * 4 + 16;
+    static constexpr int kBytes = 2 * kRowChunks * 16 + (NEAR ? 2 * kTileRows * 16 : 0) + 8 * kTileRows * 4 + 16;
 
     struct Lds {
-        i16x8 *q, *g;
-        float *x, *y, *slope, *shift, *delta, *rest;
-        int *limit, *exact;
+        i16x8 *q, *g, *near;  // near: [half][row]
+        float *x, *y, *slope, *shift, *near_shift, *delta, *rest;
+        int *limit, *exact, *all_near;
         __device__ __forceinline__ explicit Lds(char *base) {
             q = reinterpret_cast<i16x8 *>(base);
             g = q + kRowChunks;
-            x = reinterpret_cast<float *>(g + kRowChunks);
+            near = g + kRowChunks;
+            x = reinterpret_cast<float *>(near + (NEAR ? 2 * kTileRows : 0));
             y = x + kTileRows;
             slope = y + kTileRows;
             shift = slope + kTileRows;
-            delta = shift + kTileRows;
+            near_shift = shift + kTileRows;
+            delta = near_shift + kTileRows;
             rest = delta + kTileRows;
             limit = reinterpret_cast<int *>(rest + kTileRows);
             exact = limit + kTileRows;
+            all_near = exact + 1;
         }
     };
 
@@ -284,8 +287,9 @@ struct RowTile {
         }
     }
 
+    // units: of the products, to which the distances are added
     template <bool DIST>
-    __device__ __forceinline__ void store(const Lds &lds) const {
+    __device__ __forceinline__ void store(const Lds &lds, int2 origin, float largest, float units, float constant) const {
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
             const int e = threadIdx.x + n * kThreads;
@@ -303,6 +307,17 @@ struct RowTile {
             float shift, rest;
             split_lse(absent ? -INFINITY : lse, shift, rest);
             lds.shift[threadIdx.x] = shift;
+            if (NEAR) {
+                // the row's term of the distances goes with the shift
+                const int ax = place.x - origin.x, ay = place.y - origin.y;
+                const float n = square_quanta(ax, ay), weight = slope * kLog2e / 256.0f;
+                const NearSlots s = near_row(ax, ay, weight * units);
+                lds.near[threadIdx.x] = s.half[0];
+                lds.near[kTileRows + threadIdx.x] = s.half[1];
+                lds.near_shift[threadIdx.x] = __builtin_fmaf(weight, n, shift - constant);
+                const bool all = __all(near_enough(ax, ay, n, largest));
+                if (threadIdx.x == 0) *lds.all_near = all;
+            }
             lds.delta[threadIdx.x] = delta;
             lds.rest[threadIdx.x] = rest;
             lds.limit[threadIdx.x] = limit;
@@ -320,7 +335,7 @@ struct RowTile {
 template <typename T, int DP, int BLOCKS, bool DIST, bool CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
-    using Tile = RowTile<DP>;
+    using Tile = RowTile<DP, DIST>;
     constexpr int kKeys = 128 * BLOCKS;
     const AttentionArgs &a = b.fwd;
     extern __shared__ char shared[];
@@ -358,7 +373,25 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             ky[n] = (float)place.y * kPxPerQuantum;
         }
     }
-    const float scale = CAP ? a.scale / a.cap : a.scale * kLog2e, cap2 = a.cap * kLog2e;
+    float largest = 0.0f;
+    int2 origin = make_int2(0, 0);
+    bool keys_near = DIST;
+    bf16x8 key_slots[BLOCKS] = {};
+    if (DIST) {
+        origin = near_origin(reinterpret_cast<const int2 *>(a.k_xy)[sp.k0 + min((int)key0 + col, sp.nk - 1)]);
+        float steepest = 0.0f;
+        for (int e = 0; e < a.group; ++e) steepest = fmaxf(steepest, fabsf(a.slopes[head * a.group + e]) * kLog2e);
+        largest = near_limit<T>() * 256.0f / steepest;
+#pragma unroll
+        for (int n = 0; n < BLOCKS; ++n) {
+            const int bx = (int)(kx[n] * 16.0f) - origin.x, by = (int)(ky[n] * 16.0f) - origin.y;
+            const float n2 = square_quanta(bx, by);
+            const NearSlots s = near_key(bx, by, n2);
+            key_slots[n] = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
+            keys_near = keys_near && __all(wave_key + 32 * n + col >= sp.nk || near_enough(bx, by, n2, largest));
+        }
+    }
+    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     // the first query that sees the workgroup's first key
     int begin = 0;
@@ -366,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         begin = (int)(max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows);
 
     f32x16 dk[BLOCKS][DP / 32] = {}, dv[BLOCKS][DP / 32] = {};
-    auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact) {
+    auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact, bool near) {
         F qf[DP / 16], gf[DP / 16];
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
@@ -374,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             gf[st] = read_rows<T, Tile::kPitch>(t.g, first + col, st, h);
         }
         // the columns are read here where registers allow it, to be there when the weights are
-        constexpr bool EARLY = DP <= 64;
+        constexpr bool EARLY = DP <= 64 && !(DIST && CAP);
         F gc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1], qc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1];
         if (EARLY) {
 #pragma unroll
@@ -394,25 +427,50 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
                 s = mfma(qf[st], k[n][st], s);
                 dp = mfma(gf[st], v[n][st], dp);
             }
+            if (near) {
+                const bf16x8 row = __builtin_bit_cast(bf16x8, t.near[h * kTileRows + first + col]);
+                f32x16 bias;
+                if (CAP) bias = mfma(row, key_slots[n], f32x16{});
+                else s = mfma(row, key_slots[n], s);
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                float x[4], y[4], slope[4] = {}, shift[4], delta[4];
-                if (DIST) {
-                    *reinterpret_cast<float4 *>(x) = read4(t.x, first, r, h);
-                    *reinterpret_cast<float4 *>(y) = read4(t.y, first, r, h);
-                    *reinterpret_cast<float4 *>(slope) = read4(t.slope, first, r, h);
+                for (int r = 0; r < 16; r += 4) {
+                    float shift[4], delta[4];
+                    *reinterpret_cast<float4 *>(shift) = read4(t.near_shift, first, r, h);
+                    *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float d = dp[r + e] - delta[e];
+                        if (CAP) {
+                            const float c = tanh_part(s[r + e] * scale);
+                            s[r + e] = exp2_fast(__builtin_fmaf(-2.0f * cap2, c, bias[r + e]) - shift[e]);
+                            d *= tanh_slope(c);
+                        } else {
+                            s[r + e] = exp2_fast(__builtin_fmaf(s[r + e], scale, -shift[e]));
+                        }
+                        dp[r + e] = s[r + e] * d;
+                    }
                 }
-                *reinterpret_cast<float4 *>(shift) = read4(t.shift, first, r, h);
-                *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
+            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float d2 = DIST ? distance2(x[e] - kx[n], y[e] - ky[n]) : 0.0f;
-                    float th;
-                    const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e], th);
-                    s[r + e] = exp2_fast(z - shift[e]);
-                    float d = s[r + e] * (dp[r + e] - delta[e]);
-                    if (CAP) d *= __builtin_fmaf(-th, th, 1.0f);
-                    dp[r + e] = d;
+                for (int r = 0; r < 16; r += 4) {
+                    float x[4], y[4], slope[4] = {}, shift[4], delta[4];
+                    if (DIST) {
+                        *reinterpret_cast<float4 *>(x) = read4(t.x, first, r, h);
+                        *reinterpret_cast<float4 *>(y) = read4(t.y, first, r, h);
+                        *reinterpret_cast<float4 *>(slope) = read4(t.slope, first, r, h);
+                    }
+                    *reinterpret_cast<float4 *>(shift) = read4(t.shift, first, r, h);
+                    *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float d2 = DIST ? distance2(x[e] - kx[n], y[e] - ky[n]) : 0.0f;
+                        float th;
+                        const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e], th);
+                        s[r + e] = exp2_fast(z - shift[e]);
+                        float d = s[r + e] * (dp[r + e] - delta[e]);
+                        if (CAP) d *= tanh_slope(th);
+                        dp[r + e] = d;
+                    }
                 }
             }
             if (limited) {
@@ -451,11 +509,12 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             }
     };
 
+    const float units = CAP ? 1.0f : 1.0f / scale, constant = CAP ? cap2 : 0.0f;
     Tile next;
     RowRun run(a, begin);
     if (begin < n_rows) {
         next.template load<DIST>(b, sp, head, prefix, run, min(kTileRows, n_rows - begin));
-        next.template store<DIST>(typename Tile::Lds(shared));
+        next.template store<DIST>(typename Tile::Lds(shared), origin, largest, units, constant);
     }
     wait_for_loads();
     __syncthreads();
@@ -466,16 +525,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         if (more) next.template load<DIST>(b, sp, head, prefix, run, min(kTileRows, n_rows - rt - kTileRows));
         const typename Tile::Lds t(shared + buffer * Tile::kBytes);
         const bool exact = __builtin_amdgcn_readfirstlane(*t.exact) != 0;
+        const bool near = DIST && keys_near && __builtin_amdgcn_readfirstlane(*t.all_near) != 0;
         // limits grow with the rows: those of the first and of the last row say which keys all and some rows see
         const int some = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[min(kTileRows, n_rows - rt) - 1]) : sp.nk;
         const int all = a.causal ? __builtin_amdgcn_readfirstlane(t.limit[0]) : sp.nk;
         if (wave_key < some) {
 #pragma unroll 1
             for (int sub = 0; sub < kTileRows / 32; ++sub)
-                sub_tile(t, 32 * sub, min(wave_key + 32 * BLOCKS, sp.nk) > all, exact);
+                sub_tile(t, 32 * sub, min(wave_key + 32 * BLOCKS, sp.nk) > all, exact, near);
         }
         buffer ^= 1;
-        if (more) next.template store<DIST>(typename Tile::Lds(shared + buffer * Tile::kBytes));
+        if (more) next.template store<DIST>(typename Tile::Lds(shared + buffer * Tile::kBytes), origin, largest, units, constant);
         __syncthreads();
     }
 #pragma unroll
@@ -569,7 +629,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
             if (e != hipSuccess) return e;
         }
         if (a.total_k > 0) {
-            constexpr size_t bytes = 2 * RowTile<DP>::kBytes;
+            constexpr size_t bytes = 2 * RowTile<DP, DIST>::kBytes;
             constexpr int kBlocks = 1;
             b.key_slots = (int64_t)a.total_k / (128 * kBlocks) + a.n_frames;
             auto kernel = attention_dkv_kernel<T, DP, kBlocks, DIST, CAP>;

@@ -38,10 +38,10 @@ __device__ __forceinline__ float across(float x, F &&f) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh from one exponential: 1 - 2 / (e^2x + 1), exact at both ends.
-__device__ __forceinline__ float tanh_fast(float x) {
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_fast(2.0f * kLog2e * x) + 1.0f);
-}
+// r = 1 / (e^2x + 1) from 2 x log2 e: tanh x = 1 - 2 r, exact at both ends, and its
+// derivative 1 - tanh^2 x = 4 r (1 - r).
+__device__ __forceinline__ float tanh_part(float x2) { return __builtin_amdgcn_rcpf(exp2_fast(x2) + 1.0f); }
+__device__ __forceinline__ float tanh_slope(float r) { return 4.0f * __builtin_fmaf(-r, r, r); }
 
 __device__ __forceinline__ int wave_max(int x) {
 #pragma unroll
@@ -287,6 +287,7 @@ template <int DP, int KEYS, int K_PITCH, int V_PITCH, bool NEAR>
 struct KeyTile {
     static constexpr int kChunks = DP / 8;                       // of 16 bytes in a row
     static constexpr int kLoads = KEYS * kChunks / kThreads;
+    static_assert(kLoads * kThreads == KEYS * kChunks, "every thread loads whole chunks");
     static constexpr int kBytes = KEYS * (K_PITCH + V_PITCH) * 16 + (NEAR ? 2 * KEYS * 16 : 0) + 3 * KEYS * 4 + 32;
 
     struct Lds {
@@ -385,16 +386,16 @@ __device__ __forceinline__ float4 read4(const float *p, int first, int r, int h)
 // Squared distance in px^2, and the scores in units of log 2 from a product of
 // queries and keys.  The products' order is written out, so that every kernel
 // gets the same bits: P = exp(s - lse) of the backward pass is then right even
-// where all of a query's keys are far and its scores are large (th: tanh(t / cap),
-// kept for the gradient).
+// where all of a query's keys are far and its scores are large (r: tanh_part of
+// t / cap, kept for the gradient).
 __device__ __forceinline__ float distance2(float dx, float dy) { return __builtin_fmaf(dx, dx, dy * dy); }
 
 template <bool DIST, bool CAP>
-__device__ __forceinline__ float score(float qk, float scale, float cap2, float d2, float slope2, float &th) {
+__device__ __forceinline__ float score(float qk, float scale, float cap2, float d2, float slope2, float &r) {
     float s;
     if (CAP) {
-        th = tanh_fast(qk * scale);  // scale holds scale / cap
-        s = cap2 * th;
+        r = tanh_part(qk * scale);   // scale holds 2 log2 e scale / cap
+        s = __builtin_fmaf(-2.0f * cap2, r, cap2);
     } else {
         s = qk * scale;              // scale holds scale * log2 e
     }
