@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         l += sum[0] + sum[1];
     };
 
-    Tile next;
+    Tile next(a);
     if (end > 0) {
         next.look_up(a, sp, 0, end);
         next.template load<DIST>(a, sp, head, 0, end);
@@ -293,7 +293,7 @@ constexpr int split_lds_bytes() {
 }
 
 template <typename T, int DP, bool DIST, bool CAP>
-__global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionArgs a) {
+__global__ void __launch_bounds__(kThreads, DP == 128 && DIST && CAP ? 1 : 2) attention_split_kernel(AttentionArgs a) {
     using F = typename Frag<T>::type;
     constexpr int kRows = 32, kKeys = 128;
     using Tile = SplitTile<DP>;
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 2) attention_split_kernel(AttentionA
         begin = (int)min((int64_t)split * per, (int64_t)end);
         end = (int)min(begin + (int64_t)per, (int64_t)end);
     }
-    Tile next;
+    Tile next(a);
     if (begin < end) {
         next.look_up(a, sp, begin, end);
         next.template load<DIST>(a, sp, head, begin, end);

@@ -98,9 +98,9 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
     }
 
     f32x16 dq[DP / 32] = {};
-    // sums of P dP, P d2 and P dP d2: the slope's gradient takes delta from the
-    // same P, since dS = P (dP - delta) sums to zero only then to 32 bits
-    float pdp = 0.0f, pd2 = 0.0f, pdpd2 = 0.0f;
+    // sums of dS, P d2 and dS d2: dS sums to zero but for delta's rounding (it comes
+    // from the rounded output), which the slope's gradient has to be rid of
+    float sum_ds = 0.0f, sum_p_d2 = 0.0f, sum_ds_d2 = 0.0f;
     auto sub_tile = [&](const typename Tile::Lds &t, int kt, int first, bool hidden, bool limited) {
         f32x16 s = {}, dp = {};
 #pragma unroll
@@ -140,13 +140,12 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float p = exp2_fast(s[r] - shift);  // P / rest; rest is in the other factors
-            if (DIST) {
-                const float pd = p * dp[r];
-                pdp += pd;
-                pd2 = __builtin_fmaf(p, d2[r], pd2);
-                pdpd2 = __builtin_fmaf(pd, d2[r], pdpd2);
-            }
             float ds = p * __builtin_fmaf(dp[r], rest, -delta);
+            if (DIST) {
+                sum_ds += ds;
+                sum_p_d2 = __builtin_fmaf(p, d2[r], sum_p_d2);
+                sum_ds_d2 = __builtin_fmaf(ds, d2[r], sum_ds_d2);
+            }
             if (CAP) ds *= tanh_slope(th[r]);
             s[r] = ds;
         }
@@ -159,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
         }
     };
 
-    Tile next;
+    Tile next(a);
     if (end > 0) {
         next.look_up(a, sp, 0, end);
         next.template load<DIST>(a, sp, head, 0, end);
@@ -190,10 +189,10 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
     }
     if (DIST && b.row_slopes) {
         auto add = [](float x, float y) { return x + y; };
-        pdp = across(pdp, add);
-        pd2 = across(pd2, add);
-        pdpd2 = across(pdpd2, add);
-        if (valid && h == 0) b.row_slopes[qrow * a.q_heads + qh] = rest * (rest * pdp * pd2 - pdpd2);
+        sum_ds = across(sum_ds, add);
+        sum_p_d2 = across(sum_p_d2, add);
+        sum_ds_d2 = across(sum_ds_d2, add);
+        if (valid && h == 0) b.row_slopes[qrow * a.q_heads + qh] = rest * sum_p_d2 * sum_ds - sum_ds_d2;
     }
     if (!valid) return;
     T *out = static_cast<T *>(b.grad_q) + qrow * b.grad_q_stride + qh * a.dim;
