@@ -98,9 +98,10 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
     }
 
     f32x16 dq[DP / 32] = {};
-    // sums of dS, P d2 and dS d2: dS sums to zero but for delta's rounding (it comes
-    // from the rounded output), which the slope's gradient has to be rid of
-    float sum_ds = 0.0f, sum_p_d2 = 0.0f, sum_ds_d2 = 0.0f;
+    // sums of P, dS, P d2 and dS d2.  P sums to one but for the rounding of lse, and
+    // dS to zero but for that of delta (it comes from the rounded output); the
+    // slope's gradient is rid of both, and the keys' gradients get the better delta.
+    float sum_p = 0.0f, sum_ds = 0.0f, sum_p_d2 = 0.0f, sum_ds_d2 = 0.0f;
     auto sub_tile = [&](const typename Tile::Lds &t, int kt, int first, bool hidden, bool limited) {
         f32x16 s = {}, dp = {};
 #pragma unroll
@@ -142,6 +143,7 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
             const float p = exp2_fast(s[r] - shift);  // P / rest; rest is in the other factors
             float ds = p * __builtin_fmaf(dp[r], rest, -delta);
             if (DIST) {
+                sum_p += p;
                 sum_ds += ds;
                 sum_p_d2 = __builtin_fmaf(p, d2[r], sum_p_d2);
                 sum_ds_d2 = __builtin_fmaf(ds, d2[r], sum_ds_d2);
@@ -187,12 +189,18 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
         if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes));
         __syncthreads();
     }
-    if (DIST && b.row_slopes) {
+    if (DIST) {
         auto add = [](float x, float y) { return x + y; };
+        sum_p = across(sum_p, add);
         sum_ds = across(sum_ds, add);
         sum_p_d2 = across(sum_p_d2, add);
         sum_ds_d2 = across(sum_ds_d2, add);
-        if (valid && h == 0) b.row_slopes[qrow * a.q_heads + qh] = rest * sum_p_d2 * sum_ds - sum_ds_d2;
+        if (valid && h == 0 && sum_p > 0.0f) {
+            const int64_t at = qrow * a.q_heads + qh;
+            const float one = sum_p * rest, off = sum_ds / sum_p;
+            if (b.row_slopes) b.row_slopes[at] = (off * sum_p_d2 - sum_ds_d2) / one;
+            b.delta[at] = (delta + off) / rest;
+        }
     }
     if (!valid) return;
     T *out = static_cast<T *>(b.grad_q) + qrow * b.grad_q_stride + qh * a.dim;
