@@ -1073,7 +1073,7 @@ flock_status attention_frames(int32_t dtype, const void *q, int64_t q_stride, co
 size_t attention_frames_backward_workspace(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads,
                                            int32_t kv_heads, int32_t head_dim) {
     if (n_frames <= 0 || total_q < 0 || total_k < 0 || q_heads < 1 || kv_heads < 1 || head_dim < 1) return 0;
-    return flock::attention_backward_workspace_bytes(total_q, q_heads);
+    return flock::attention_backward_workspace_bytes(n_frames, total_q, q_heads, kv_heads);
 }
 
 flock_status attention_frames_backward(
@@ -1150,7 +1150,7 @@ flock_status attention_frames_backward(
         if (st != FLOCK_OK) return st;
     }
     Workspace ws;
-    st = ws.take(workspace, workspace_bytes, flock::attention_backward_workspace_bytes(total_q, q_heads), s);
+    st = ws.take(workspace, workspace_bytes, flock::attention_backward_workspace_bytes(n_frames, total_q, q_heads, kv_heads), s);
     if (st != FLOCK_OK) return st;
     hipError_t err = flock::launch_attention_backward(b, dtype, ws.ptr, grad_slopes, s);
     const hipError_t ferr = ws.release(s);

@@ -13,41 +13,16 @@ using namespace attention;
 // Backward
 // ---------------------------------------------------------------------------
 
-// delta = dout.out of every query and head: 16 lanes each.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) attention_delta_kernel(AttentionBackwardArgs b) {
-    const AttentionArgs &a = b.fwd;
-    const int64_t all = (int64_t)a.total_q * a.q_heads;
-    const int64_t at = (int64_t)blockIdx.x * (kThreads / 16) + (threadIdx.x >> 4);
-    if (at >= all) return;
-    const int64_t i = at / a.q_heads;
-    const int hd = (int)(at % a.q_heads);
-    const T *o = static_cast<const T *>(a.out) + i * a.out_stride + hd * a.dim;
-    const T *g = static_cast<const T *>(b.grad_out) + i * b.grad_out_stride + hd * a.dim;
-    float s = 0.0f;
-    for (int d = (threadIdx.x & 15) * 8; d < a.dim; d += 128) {
-        float x[8], y[8];
-        load_pack<T, 8>(o + d, x);
-        load_pack<T, 8>(g + d, y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += x[e] * y[e];
-    }
-#pragma unroll
-    for (int d = 8; d > 0; d >>= 1) s += __shfl_xor(s, d);
-    if ((threadIdx.x & 15) == 0) {
-        b.delta[at] = s;
-        if (b.row_slopes) b.row_slopes[at] = 0.0f;  // queries of inconsistent frames add nothing
-    }
-}
-
 // Heads of 128 leave registers for half as many keys in flight.
 template <int DP>
 using DqTile = KeyTile<DP, DP <= 96 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
 
 // Gradients of the queries: 128 rows a workgroup, 32 a wave, over the tiles of
-// keys that they see.
+// keys that they see.  Also delta = dout.out of every row, which the keys'
+// gradients take from here, and each workgroup's share of its heads' slope
+// gradients (zeros from one without rows, so that every share is written).
 template <typename T, int DP, bool DIST, bool CAP>
-__global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_dq_kernel(AttentionBackwardArgs b) {
+__global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && CAP) ? 1 : 2) attention_dq_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = DqTile<DP>;
     constexpr int kRows = 128, kKeys = DP <= 96 ? 64 : 32;
@@ -59,9 +34,13 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
     int64_t tile;
     const int f = find_frame(a.q_offsets, a.n_frames, a.group, kRows, id % a.slots, &tile);
     const Span sp = frame_span(a, f);
-    if (!sp.ok || tile < 0) return;
-    const int n_rows = sp.nq * a.group;
-    if (tile * kRows >= n_rows) return;
+    const int n_rows = sp.ok ? sp.nq * a.group : 0;
+    float *const shares = DIST && b.slope_shares ? b.slope_shares + id % a.slots * a.q_heads + head * a.group : nullptr;
+    if (tile < 0 || tile * kRows >= n_rows) {
+        if (shares)
+            for (int g = threadIdx.x; g < a.group; g += kThreads) shares[g] = 0.0f;
+        return;
+    }
     const int row0 = (int)tile * kRows;
     const RowRun run(a, row0);
     const bool valid = row0 + 32 * wave + col < n_rows;
@@ -71,12 +50,18 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
     const int64_t qrow = sp.q0 + qi;
     const short *q_row = valid ? static_cast<const short *>(a.q) + qrow * a.q_stride + qh * a.dim : nullptr;
     const short *g_row = valid ? static_cast<const short *>(b.grad_out) + qrow * b.grad_out_stride + qh * a.dim : nullptr;
+    const short *o_row = valid ? static_cast<const short *>(a.out) + qrow * a.out_stride + qh * a.dim : nullptr;
     F q[DP / 16], go[DP / 16];
+    float delta = 0.0f;
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) {
         q[s] = load_frag<T>(q_row, s, h, a.dim);
         go[s] = load_frag<T>(g_row, s, h, a.dim);
+        const F o = load_frag<T>(o_row, s, h, a.dim);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = __builtin_fmaf(static_cast<float>(go[s][e]), static_cast<float>(o[e]), delta);
     }
+    delta = across(delta, [](float x, float y) { return x + y; });
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     const int limit = valid ? seen_limit(a, sp, prefix, qi) : sp.nk;
     float qx = 0.0f, qy = 0.0f, slope2 = 0.0f;
@@ -89,7 +74,7 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
     const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
     float shift, rest;
     split_lse(valid ? a.lse[qrow * a.q_heads + qh] : -INFINITY, shift, rest);
-    const float delta = valid ? b.delta[qrow * a.q_heads + qh] * rest : 0.0f;
+    const float rest_delta = delta * rest;
     int wave_end = sp.nk, wave_all = sp.nk, end = sp.nk;
     if (a.causal) {
         wave_end = wave_max(limit);
@@ -141,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float p = exp2_fast(s[r] - shift);  // P / rest; rest is in the other factors
-            float ds = p * __builtin_fmaf(dp[r], rest, -delta);
+            float ds = p * __builtin_fmaf(dp[r], rest, -rest_delta);
             if (DIST) {
                 sum_p += p;
                 sum_ds += ds;
@@ -195,13 +180,26 @@ __global__ void __launch_bounds__(kThreads, DP >= 96 && DIST ? 1 : 2) attention_
         sum_ds = across(sum_ds, add);
         sum_p_d2 = across(sum_p_d2, add);
         sum_ds_d2 = across(sum_ds_d2, add);
-        if (valid && h == 0 && sum_p > 0.0f) {
-            const int64_t at = qrow * a.q_heads + qh;
+        float share = 0.0f;
+        if (sum_p > 0.0f) {
             const float one = sum_p * rest, off = sum_ds / sum_p;
-            if (b.row_slopes) b.row_slopes[at] = (off * sum_p_d2 - sum_ds_d2) / one;
-            b.delta[at] = (delta + off) / rest;
+            share = (off * sum_p_d2 - sum_ds_d2) / one;
+            delta += off / rest;
+        }
+        if (shares) {
+            // the tiles in LDS are done with; rows of a head are added in their order
+            float *const rows = reinterpret_cast<float *>(shared);
+            if (h == 0) rows[32 * wave + col] = valid ? share : 0.0f;
+            __syncthreads();
+            for (int g = threadIdx.x; g < a.group; g += kThreads) {
+                float sum = 0.0f;
+                for (int r = g >= run.first_g ? g - run.first_g : g - run.first_g + a.group; r < kRows; r += a.group)
+                    sum += rows[r];
+                shares[g] = sum;
+            }
         }
     }
+    if (valid && h == 0) b.delta[qrow * a.q_heads + qh] = delta;
     if (!valid) return;
     T *out = static_cast<T *>(b.grad_q) + qrow * b.grad_q_stride + qh * a.dim;
 #pragma unroll
@@ -572,58 +570,43 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
     }
 }
 
-// Gradient of a head's slope: the queries' shares, a block per head and part
-// of the queries, then the parts, in 64 bits and a fixed order.
-constexpr int kSlopeParts = 64;
-
-__global__ void __launch_bounds__(kThreads) slope_parts_kernel(const float *rows, int64_t total_q, int q_heads,
-                                                               double *parts) {
-    __shared__ double sums[kThreads];
-    const int head = blockIdx.x, part = blockIdx.y;
+// Gradient of a head's slope: the workgroups' shares, in 64 bits and a fixed
+// order, a block a head.
+__global__ void __launch_bounds__(1024) slope_total_kernel(const float *shares, int64_t n, int q_heads,
+                                                           float *grad_slopes) {
+    __shared__ double sums[1024];
     double s = 0.0;
-    for (int64_t i = (int64_t)part * kThreads + threadIdx.x; i < total_q; i += (int64_t)kSlopeParts * kThreads)
-        s += rows[i * q_heads + head];
+    for (int64_t i = threadIdx.x; i < n; i += 1024) s += shares[i * q_heads + blockIdx.x];
     sums[threadIdx.x] = s;
-    for (int d = kThreads / 2; d > 0; d >>= 1) {
+    for (int d = 512; d > 0; d >>= 1) {
         __syncthreads();
         if (threadIdx.x < d) sums[threadIdx.x] += sums[threadIdx.x + d];
     }
-    if (threadIdx.x == 0) parts[head * kSlopeParts + part] = sums[0];
+    if (threadIdx.x == 0) grad_slopes[blockIdx.x] = (float)sums[0];
 }
 
-__global__ void __launch_bounds__(64) slope_total_kernel(const double *parts, float *grad_slopes) {
-    double s = parts[blockIdx.x * kSlopeParts + threadIdx.x];
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-    if (threadIdx.x == 0) grad_slopes[blockIdx.x] = (float)s;
-}
+// Numbers of row tiles of the queries' gradients.
+int64_t backward_slots(int32_t n_frames, int32_t total_q, int group) { return (int64_t)total_q * group / 128 + n_frames; }
 
 }  // namespace
 
-size_t attention_backward_workspace_bytes(int32_t total_q, int32_t q_heads) {
-    const size_t all = (size_t)std::max(total_q, 0) * (size_t)std::max(q_heads, 0);
-    return 2 * align256(all * sizeof(float)) + align256((size_t)std::max(q_heads, 0) * kSlopeParts * sizeof(double));
+size_t attention_backward_workspace_bytes(int32_t n_frames, int32_t total_q, int32_t q_heads, int32_t kv_heads) {
+    if (n_frames <= 0 || total_q < 0 || q_heads <= 0 || kv_heads <= 0) return 0;
+    const size_t slots = (size_t)backward_slots(n_frames, total_q, q_heads / kv_heads);
+    return align256((size_t)total_q * (size_t)q_heads * sizeof(float)) + align256(slots * (size_t)q_heads * sizeof(float));
 }
 
 hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, void *workspace, float *grad_slopes,
                                      hipStream_t stream) {
     AttentionArgs &a = b.fwd;
-    const size_t all = (size_t)a.total_q * (size_t)a.q_heads;
-    char *ws = static_cast<char *>(workspace);
-    b.delta = reinterpret_cast<float *>(ws);
-    b.row_slopes = grad_slopes ? reinterpret_cast<float *>(ws + align256(all * sizeof(float))) : nullptr;
-    double *parts = reinterpret_cast<double *>(ws + 2 * align256(all * sizeof(float)));
-    a.slots = (int64_t)a.total_q * a.group / 128 + a.n_frames;
+    b.delta = static_cast<float *>(workspace);
+    b.slope_shares = nullptr;
+    if (grad_slopes)
+        b.slope_shares = reinterpret_cast<float *>(static_cast<char *>(workspace) +
+                                                   align256((size_t)a.total_q * (size_t)a.q_heads * sizeof(float)));
+    a.slots = backward_slots(a.n_frames, a.total_q, a.group);
     a.group_reciprocal = group_reciprocal(a.group);
-    hipError_t err = hipSuccess;
-    if (a.total_q > 0) {
-        const dim3 grid((uint32_t)((all + 15) / 16));
-        if (dtype == FLOCK_F16) hipLaunchKernelGGL(attention_delta_kernel<half_t>, grid, dim3(kThreads), 0, stream, b);
-        else hipLaunchKernelGGL(attention_delta_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, b);
-        err = hipGetLastError();
-        if (err != hipSuccess) return err;
-    }
-    err = with_kernel(a, dtype, [&](auto t, auto dp, auto dist, auto cap) {
+    hipError_t err = with_kernel(a, dtype, [&](auto t, auto dp, auto dist, auto cap) {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
@@ -646,11 +629,9 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
         return e;
     });
     if (err != hipSuccess || !grad_slopes) return err;
-    hipLaunchKernelGGL(slope_parts_kernel, dim3(a.q_heads, kSlopeParts), dim3(kThreads), 0, stream, b.row_slopes,
-                       (int64_t)a.total_q, a.q_heads, parts);
-    err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    hipLaunchKernelGGL(slope_total_kernel, dim3(a.q_heads), dim3(64), 0, stream, parts, grad_slopes);
+    // without queries there are no shares, and the gradients are zeros
+    hipLaunchKernelGGL(slope_total_kernel, dim3(a.q_heads), dim3(1024), 0, stream, b.slope_shares,
+                       a.total_q > 0 ? a.slots : 0, a.q_heads, grad_slopes);
     return hipGetLastError();
 }
 

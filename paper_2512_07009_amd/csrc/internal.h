@@ -282,10 +282,10 @@ struct AttentionBackwardArgs {
     const void *grad_out;
     void *grad_q, *grad_k, *grad_v;
     int64_t grad_out_stride, grad_q_stride, grad_k_stride, grad_v_stride;
-    float *delta, *row_slopes;         // set by launch_attention_backward: [total_q][q_heads]
+    float *delta, *slope_shares;       // set by launch_attention_backward: [total_q][q_heads], [slots][q_heads]
     int64_t key_slots;
 };
-size_t attention_backward_workspace_bytes(int32_t total_q, int32_t q_heads);
+size_t attention_backward_workspace_bytes(int32_t n_frames, int32_t total_q, int32_t q_heads, int32_t kv_heads);
 hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, void *workspace, float *grad_slopes,
                                      hipStream_t stream);
 
