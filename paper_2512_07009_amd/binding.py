@@ -350,30 +350,42 @@ def _dtype(t):
     return code
 
 
+# The checks below read each attribute once and compare device numbers: a call
+# on few birds is bound by the host.
+
 def _rows(t, name, like=None):
     """Stride of a device matrix [rows, width] whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a device matrix with contiguous rows")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+    stride = t.stride()
+    if stride[1] != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must be a device matrix with contiguous rows")
+    if like is not None and (shape != like.shape or t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the shape, type and device of its counterpart")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return stride[0] if shape[0] > 1 else shape[1]
 
 
-def _heads(t, name, rows=None, dtype=None, dev=None):
-    """Stride of a device tensor [birds, heads, head_dim] whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1) or \
-            (t.shape[1] > 1 and t.stride(1) != t.shape[2]):
+def _heads(t, name, like=None):
+    """Stride of a device tensor [birds, heads, head_dim] whose rows are
+    contiguous, of the type and on the device of `like`."""
+    shape = t.shape
+    if len(shape) != 3 or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor [birds, heads, head_dim] with contiguous rows")
-    if rows is not None and t.shape[0] != rows:
-        raise ValueError(f"{name} holds {t.shape[0]} birds, expected {rows}")
-    if dtype is not None and (t.dtype != dtype or t.device != dev):
+    n, heads, dim = shape
+    stride = t.stride()
+    if (stride[2] != 1 and dim > 1) or (stride[1] != dim and heads > 1):
+        raise ValueError(f"{name} must be a device tensor [birds, heads, head_dim] with contiguous rows")
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the type and device of the queries")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return stride[0] if n > 1 else heads * dim
 
 
-def _vector(t, name, dtype, numel, dev):
-    if t.dtype != dtype or t.device != dev or t.numel() != numel or not t.is_contiguous():
+def _vector(t, name, dtype, numel, index):
+    """Pointer of `numel` contiguous values on device number `index`."""
+    if t.dtype != dtype or t.numel() != numel or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name} must be {numel} contiguous {dtype} values on the features' device")
+    return t.data_ptr()
 
 
 def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
@@ -389,9 +401,9 @@ def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: t
     code, xs = _dtype(x), _rows(x, "x")
     n, width = x.shape
     dev = x.device
-    for t, name in ((weight, "weight"), (bias, "bias")):
-        if t is not None:
-            _vector(t, name, torch.float32, width, dev)
+    index = dev.index
+    wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
+    bp = _vector(bias, "bias", torch.float32, width, index) if bias is not None else None
     rs = _rows(residual, "residual", x) if residual is not None else 0
     if out is None:
         y = torch.empty((n, width), dtype=x.dtype, device=dev)
@@ -403,12 +415,12 @@ def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: t
         y, h, mean, rstd = out
         ys = _rows(y, "y", x)
         hs = _rows(h, "h", x) if residual is not None else 0
-        _vector(mean, "mean", torch.float32, n, dev)
-        _vector(rstd, "rstd", torch.float32, n, dev)
+        _vector(mean, "mean", torch.float32, n, index)
+        _vector(rstd, "rstd", torch.float32, n, index)
         if residual is None:
             h = x
-    _call(lib().layer_norm_rows, dev, stream, code, x.data_ptr(), xs, _ptr(residual), rs, n, width, _ptr(weight),
-          _ptr(bias), eps, y.data_ptr(), ys, h.data_ptr() if residual is not None else None, hs, mean.data_ptr(),
+    _call(lib().layer_norm_rows, dev, stream, code, x.data_ptr(), xs, _ptr(residual), rs, n, width, wp,
+          bp, eps, y.data_ptr(), ys, h.data_ptr() if residual is not None else None, hs, mean.data_ptr(),
           rstd.data_ptr())
     return y, h, mean, rstd
 
@@ -426,18 +438,17 @@ def layer_norm_rows_backward(grad_y: torch.Tensor, h: torch.Tensor, weight: torc
     dev = h.device
     gs = _rows(grad_y, "grad_y", h)
     ss = _rows(grad_sum, "grad_sum", h) if grad_sum is not None else 0
-    if weight is not None:
-        _vector(weight, "weight", torch.float32, width, dev)
-    _vector(mean, "mean", torch.float32, n, dev)
-    _vector(rstd, "rstd", torch.float32, n, dev)
+    index = dev.index
+    wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
+    mp = _vector(mean, "mean", torch.float32, n, index)
+    rp = _vector(rstd, "rstd", torch.float32, n, index)
     dx = torch.empty((n, width), dtype=h.dtype, device=dev)
-    dw = torch.empty(width, dtype=torch.float32, device=dev)
-    db = torch.empty(width, dtype=torch.float32, device=dev)
+    dw, db = torch.empty((2, width), dtype=torch.float32, device=dev)
     L = lib()
     ws_bytes = L.layer_norm_rows_backward_workspace(n, width)
     ws = _workspace(ws_bytes, dev, stream)
     _call(L.layer_norm_rows_backward, dev, stream, code, grad_y.data_ptr(), gs, _ptr(grad_sum), ss, h.data_ptr(), xs, n,
-          width, _ptr(weight), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), width, dw.data_ptr(), db.data_ptr(),
+          width, wp, mp, rp, dx.data_ptr(), width, dw.data_ptr(), db.data_ptr(),
           _ptr(ws), ws_bytes)
     return dx, dw, db
 
@@ -470,28 +481,34 @@ def rotary_frames(q: torch.Tensor | None, k: torch.Tensor | None, xy: torch.Tens
     code, dev, n = _dtype(first), first.device, first.shape[0]
     dim = first.shape[-1]
     qs = _heads(q, "q") if q is not None else 0
-    ks = _heads(k, "k", n, first.dtype, dev) if k is not None else 0
-    if k is not None and k.shape[2] != dim:
-        raise ValueError("q and k must have the same head_dim")
+    ks = _heads(k, "k", first) if k is not None else 0
+    if k is not None and (k.shape[0] != n or k.shape[2] != dim):
+        raise ValueError("q and k must have the same birds and head_dim")
     nt, ny, nx = axes.counts
     if ny or nx:
-        if xy is None or xy.dtype != torch.int32 or xy.device != dev or tuple(xy.shape) != (n, 2) \
+        if xy is None or xy.dtype != torch.int32 or xy.get_device() != dev.index or xy.shape != (n, 2) \
                 or not xy.is_contiguous():
             raise ValueError("xy must be a contiguous int32 [T, 2] tensor on the features' device")
     if nt:
         if time is None:
             raise ValueError("time is needed by the axes' time pairs")
-        _vector(time, "time", torch.int32, n, dev)
+        _vector(time, "time", torch.int32, n, dev.index)
     qo, ko = out if out is not None else (None, None)
-    if qo is None and q is not None:
-        qo = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    if ko is None and k is not None:
-        ko = torch.empty(k.shape, dtype=k.dtype, device=dev)
-    for got, want, name in ((qo, q, "q"), (ko, k, "k")):
-        if got is not None and want is not None and got.shape != want.shape:
-            raise ValueError(f"out's {name} must have the shape of {name}")
-    qos = _heads(qo, "out's q", n, first.dtype, dev) if q is not None else 0
-    kos = _heads(ko, "out's k", n, first.dtype, dev) if k is not None else 0
+    qos = kos = 0
+    if q is not None:
+        if qo is None:
+            qo, qos = torch.empty(q.shape, dtype=q.dtype, device=dev), q.shape[1] * dim
+        else:
+            qos = _heads(qo, "out's q", first)
+            if qo.shape != q.shape:
+                raise ValueError("out's q must have the shape of q")
+    if k is not None:
+        if ko is None:
+            ko, kos = torch.empty(k.shape, dtype=k.dtype, device=dev), k.shape[1] * dim
+        else:
+            kos = _heads(ko, "out's k", first)
+            if ko.shape != k.shape:
+                raise ValueError("out's k must have the shape of k")
     _call(lib().rotary_frames, dev, stream, code, _ptr(q), qs, _ptr(k), ks, n, q.shape[1] if q is not None else 0,
           k.shape[1] if k is not None else 0, dim, _ptr(xy) if ny or nx else None, _ptr(time) if nt else None,
           axes.freq, nt, ny, nx, int(interleaved), int(inverse), _ptr(qo), qos, _ptr(ko), kos)
@@ -500,40 +517,31 @@ def rotary_frames(q: torch.Tensor | None, k: torch.Tensor | None, xy: torch.Tens
 
 def _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal):
     """The checked arguments that the forward and the backward call share."""
-    code, dev = _dtype(q), q.device
-    tq = q.shape[0]
-    tk = k.shape[0]
-    qs = _heads(q, "q")
-    ks = _heads(k, "k", tk, q.dtype, dev)
-    vs = _heads(v, "v", tk, q.dtype, dev)
-    if k.shape != v.shape or k.shape[2] != q.shape[2]:
+    code = _dtype(q)
+    qs, ks, vs = _heads(q, "q"), _heads(k, "k", q), _heads(v, "v", q)
+    tq, hq, dim = q.shape
+    tk, hk, k_dim = k.shape
+    if v.shape != k.shape or k_dim != dim:
         raise ValueError("k and v must have one shape, with the head_dim of q")
-    if k_offsets is None:
-        k_offsets = q_offsets
-    F = q_offsets.numel() - 1
-    if F < 0 or q_offsets.dim() != 1:
+    index = q.get_device()
+    frames = q_offsets.numel() - 1
+    if frames < 0 or q_offsets.dim() != 1:
         raise ValueError("q_offsets must be a contiguous [F + 1] tensor")
-    _vector(q_offsets, "q_offsets", torch.int32, F + 1, dev)
-    if k_offsets is not q_offsets:
-        _vector(k_offsets, "k_offsets", torch.int32, F + 1, dev)
+    qo = _vector(q_offsets, "q_offsets", torch.int32, frames + 1, index)
+    ko = qo
+    if k_offsets is not None and k_offsets is not q_offsets:
+        ko = _vector(k_offsets, "k_offsets", torch.int32, frames + 1, index)
+    sp = qp = kp = None
     if slopes is not None:
-        _vector(slopes, "slopes", torch.float32, q.shape[1], dev)
-        if k_xy is None:
-            k_xy = q_xy
+        sp = _vector(slopes, "slopes", torch.float32, hq, index)
         if q_xy is None:
             raise ValueError("q_xy is needed with slopes")
-        _vector(q_xy, "q_xy", torch.int32, 2 * tq, dev)
-        _vector(k_xy, "k_xy", torch.int32, 2 * tk, dev)
-    else:
-        q_xy = k_xy = None
-    if keep is not None:
-        _vector(keep, "keep", torch.uint8, tk, dev)
-    if prefix is not None:
-        _vector(prefix, "prefix", torch.int32, F, dev)
-    head = (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs)
-    tail = (q_offsets.data_ptr(), k_offsets.data_ptr(), F, tq, tk, q.shape[1], k.shape[1], q.shape[2], _ptr(q_xy),
-            _ptr(k_xy), _ptr(slopes), _ptr(keep), int(causal), _ptr(prefix) if causal else None)
-    return code, dev, (F, tq, tk, q.shape[1], k.shape[1], q.shape[2]), head, tail
+        qp = _vector(q_xy, "q_xy", torch.int32, 2 * tq, index)
+        kp = _vector(q_xy if k_xy is None else k_xy, "k_xy", torch.int32, 2 * tk, index)
+    keep_p = _vector(keep, "keep", torch.uint8, tk, index) if keep is not None else None
+    prefix_p = _vector(prefix, "prefix", torch.int32, frames, index) if prefix is not None else None
+    return (code, q.device, (frames, tq, tk, hq, hk, dim), (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs),
+            (qo, ko, frames, tq, tk, hq, hk, dim, qp, kp, sp, keep_p, int(causal), prefix_p if causal else None))
 
 
 def attention_frames(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
@@ -557,15 +565,17 @@ def attention_frames(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offset
     code, dev, shape, head, tail = _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    elif out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    os_ = _heads(out, "out", q.shape[0], q.dtype, dev)
+        out_stride = shape[3] * shape[5]
+    else:
+        out_stride = _heads(out, "out", q)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
     lse = torch.empty((shape[1], shape[3]), dtype=torch.float64, device=dev) if return_lse else None
     L = lib()
     ws_bytes = L.attention_frames_workspace(*shape)
     ws = _workspace(ws_bytes, dev, stream)
-    _call(L.attention_frames, dev, stream, code, *head, *tail, q.shape[2] ** -0.5 if scale is None else scale, cap,
-          out.data_ptr(), os_, _ptr(lse), _ptr(ws), ws_bytes)
+    _call(L.attention_frames, dev, stream, code, *head, *tail, shape[5] ** -0.5 if scale is None else scale, cap,
+          out.data_ptr(), out_stride, _ptr(lse), _ptr(ws), ws_bytes)
     return (out, lse) if return_lse else out
 
 
@@ -579,21 +589,20 @@ def attention_frames_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     grad_out.  Returns (grad_q, grad_k, grad_v, grad_slopes float32 [Hq], or
     None without slopes)."""
     code, dev, shape, head, tail = _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal)
-    gs = _heads(grad_out, "grad_out", q.shape[0], q.dtype, dev)
-    os_ = _heads(out, "out", q.shape[0], q.dtype, dev)
+    gs = _heads(grad_out, "grad_out", q)
+    out_stride = _heads(out, "out", q)
     if grad_out.shape != q.shape or out.shape != q.shape:
         raise ValueError("grad_out and out must have the shape of q")
-    _vector(lse, "lse", torch.float64, shape[1] * shape[3], dev)
+    lp = _vector(lse, "lse", torch.float64, shape[1] * shape[3], dev.index)
     dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    dk = torch.empty(k.shape, dtype=q.dtype, device=dev)
-    dv = torch.empty(k.shape, dtype=q.dtype, device=dev)
+    dk, dv = torch.empty((2,) + k.shape, dtype=q.dtype, device=dev)
     ds = torch.empty(shape[3], dtype=torch.float32, device=dev) if slopes is not None else None
     q_row, k_row = shape[3] * shape[5], shape[4] * shape[5]
     L = lib()
     ws_bytes = L.attention_frames_backward_workspace(*shape)
     ws = _workspace(ws_bytes, dev, stream)
-    _call(L.attention_frames_backward, dev, stream, code, grad_out.data_ptr(), gs, *head, out.data_ptr(), os_,
-          lse.data_ptr(), *tail, q.shape[2] ** -0.5 if scale is None else scale, cap, dq.data_ptr(), q_row,
+    _call(L.attention_frames_backward, dev, stream, code, grad_out.data_ptr(), gs, *head, out.data_ptr(), out_stride,
+          lp, *tail, shape[5] ** -0.5 if scale is None else scale, cap, dq.data_ptr(), q_row,
           dk.data_ptr(), k_row, dv.data_ptr(), k_row, _ptr(ds), _ptr(ws), ws_bytes)
     return dq, dk, dv, ds
 

@@ -489,21 +489,35 @@ __global__ void __launch_bounds__(kThreads) attention_join_kernel(AttentionArgs 
     }
     const Span sp = frame_span(a, lo);
     if (!sp.ok || i < sp.q0 || i >= sp.q0 + sp.nq) return;
-    float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_stat[2 * (s * all + at)]);
-    const float shift = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    for (int s = 0; s < a.splits; ++s)
-        sum += a.part_stat[2 * (s * all + at) + 1] * exp2_fast(a.part_stat[2 * (s * all + at)] - shift);
-    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    T *out = static_cast<T *>(a.out) + i * a.out_stride + (at % a.q_heads) * a.dim;
-    for (int d = threadIdx.x & 63; d < a.dim; d += 64) {
-        float z = 0.0f;
-        for (int s = 0; s < a.splits; ++s)
-            z += a.part_out[(s * all + at) * a.dim + d] * exp2_fast(a.part_stat[2 * (s * all + at)] - shift);
-        out[d] = static_cast<T>(z * inv);
+    // a lane per share (at most 64) for the weights, a lane per dimension for the sums
+    const int lane = threadIdx.x & 63;
+    float m = -INFINITY, l = 0.0f;
+    if (lane < a.splits) {
+        const float2 stat = *reinterpret_cast<const float2 *>(a.part_stat + 2 * (lane * all + at));
+        m = stat.x;
+        l = stat.y;
     }
-    if (a.lse && (threadIdx.x & 63) == 0) a.lse[at] = row_lse(top, sum);
+    float top = m;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float shift = top == -INFINITY ? 0.0f : top;
+    const float weight = exp2_fast(m - shift);
+    float sum = l * weight;
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+    const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+    float z[2] = {0.0f, 0.0f};  // dimensions lane and lane + 64
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = __shfl(weight, s);
+        const float *part = a.part_out + (s * all + at) * a.dim;
+        if (lane < a.dim) z[0] += part[lane] * w;
+        if (lane + 64 < a.dim) z[1] += part[lane + 64] * w;
+    }
+    T *out = static_cast<T *>(a.out) + i * a.out_stride + (at % a.q_heads) * a.dim;
+    if (lane < a.dim) out[lane] = static_cast<T>(z[0] * inv);
+    if (lane + 64 < a.dim) out[lane + 64] = static_cast<T>(z[1] * inv);
+    if (a.lse && lane == 0) a.lse[at] = row_lse(top, sum);
 }
 
 constexpr int kMaxSplits = 64;
