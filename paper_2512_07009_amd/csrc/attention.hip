@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         largest = near_limit<T>() * 256.0f / steepest;
         const int ax = (int)(qx * 16.0f) - origin.x, ay = (int)(qy * 16.0f) - origin.y;
         const float n = square_quanta(ax, ay), weight = slope2 / 256.0f;
-        row_near = __all(!valid || near_enough(ax, ay, n, largest));
+        row_near = !a.lse && __all(!valid || near_enough(ax, ay, n, largest));
         const float units = CAP ? weight : weight / scale;
         row_term = -units * n + (CAP ? cap2 : 0.0f);  // with the constant of tanh = 1 - 2 r
         const NearSlots s = near_row(ax, ay, units);

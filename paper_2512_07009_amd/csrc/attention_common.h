@@ -199,11 +199,13 @@ __device__ __forceinline__ uint32_t seen_bits(uint32_t bits, int limit, int firs
 // queries and keys: 16 products of bfloat16 parts (8 bits each) that hold x, y
 // (two parts, whole numbers of 1/16 px below 2^16), |b|^2 and the slope's factors
 // (three parts) to 2^-24.  That takes five vector operations off each score,
-// where they bound the kernels.  The sums pass through numbers as large as
-// slope |b|^2, so the scores are off by 2^-23 of that.  near_limit (in units of log
-// 2) keeps the weights' relative error a tenth of what rounding them to the
-// operands' type costs in bfloat16, a quarter in float16, and tiles with a bird
-// farther away take the differences themselves.
+// where they bound the kernels (training step 64 x 2000: 4.18 -> 3.70 ms, 24 x 8000:
+// 9.4 -> 8.7 ms).  The sums pass through numbers as large as slope |b|^2, so scores
+// are off by 2^-22 of that.  near_limit (in units of log 2) keeps the weights'
+// relative error below a fifth of what rounding them to the operands' type costs
+// (7e-4 of 4e-3 in bfloat16, 2.5e-4 of 5e-4 at worst in float16), and tiles with a
+// bird farther away take the differences themselves; so does a forward pass that
+// writes lse, which is exact to 32 bits.
 template <typename T> constexpr float near_limit() { return 4096.0f; }
 template <> constexpr float near_limit<half_t>() { return 1536.0f; }
 constexpr int kNearReach = 1 << 15;
@@ -226,7 +228,7 @@ __device__ __forceinline__ NearSlots near_key(int bx, int by, float n) {
     const bf16_t yl = static_cast<bf16_t>((float)by - static_cast<float>(yh));
     bf16_t p[3];
     split3(n, p);
-    const bf16x8 lo = {xh, xh, xh, xl, xl, yh, yh, yh}, hi = {yl, yl, p[0], p[0], p[0], p[1], p[1], p[2]};
+    const bf16x8 lo = {xh, yh, p[0], xl, xh, yl, yh, p[1]}, hi = {p[0], xh, yh, xl, yl, p[0], p[1], p[2]};
     return {__builtin_bit_cast(i16x8, lo), __builtin_bit_cast(i16x8, hi)};
 }
 
@@ -236,8 +238,8 @@ __device__ __forceinline__ NearSlots near_row(int ax, int ay, float weight) {
     split3(2.0f * weight * (float)ax, x);
     split3(2.0f * weight * (float)ay, y);
     split3(-weight, n);
-    const bf16x8 lo = {x[0], x[1], x[2], x[0], x[1], y[0], y[1], y[2]};
-    const bf16x8 hi = {y[0], y[1], n[0], n[1], n[2], n[0], n[1], n[0]};
+    const bf16x8 lo = {x[0], y[0], n[0], x[0], x[1], y[0], y[1], n[0]};
+    const bf16x8 hi = {n[1], x[2], y[2], x[1], y[1], n[2], n[1], n[0]};
     return {__builtin_bit_cast(i16x8, lo), __builtin_bit_cast(i16x8, hi)};
 }
 
@@ -314,6 +316,7 @@ struct KeyTile {
     // them beyond the resource
     uint8_t kept[kLoads], key_kept;
     i32x2 place;
+    int present;  // keys of the tile
 
     // A thread's loads are of one column, rows kStep apart, unless rows have 12 chunks.
     static constexpr bool kEven = kThreads % kChunks == 0;
@@ -337,7 +340,7 @@ struct KeyTile {
 
     template <bool DIST>
     __device__ __forceinline__ void load(const AttentionArgs &a, const Span &sp, int head, int first, int end) {
-        const int rows = min(end - first, KEYS);
+        const int rows = present = min(end - first, KEYS);
         const int64_t row0 = sp.k0 + first;
         const int k_step = (int)a.k_stride * 2, v_step = (int)a.v_stride * 2;
         constexpr int kParts = KEYS / 64 > 1 && kEven ? KEYS / 64 : 1;  // of 64 rows: fewer offsets to keep
@@ -396,7 +399,9 @@ struct KeyTile {
                 lds.y[threadIdx.x] = (float)place.y * kPxPerQuantum;
             }
             if (NEAR) {
-                const int bx = place.x - origin.x, by = place.y - origin.y;
+                // absent keys are as near as can be
+                const bool here = (int)threadIdx.x < present;
+                const int bx = here ? place.x - origin.x : 0, by = here ? place.y - origin.y : 0;
                 const float n = square_quanta(bx, by);
                 const NearSlots s = near_key(bx, by, n);
                 lds.near[threadIdx.x] = s.half[0];

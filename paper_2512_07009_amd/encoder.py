@@ -1,0 +1,113 @@
+"""A per-bird encoder on ragged frames, trained with torch's autograd.
+
+The library's layer norm, rotary positions and attention as differentiable
+functions, and a block that puts them together:
+
+    block = EncoderBlock(width=256, q_heads=4, axes=RotaryAxes(y=..., x=...)).to("cuda")
+    h = block(features, offsets, xy)         # [T, width] bfloat16, a row per bird
+
+Linear layers are plain matrix products of torch.
+"""
+
+from __future__ import annotations
+
+import torch
+
+from .binding import (RotaryAxes, attention_frames, attention_frames_backward, layer_norm_rows,
+                      layer_norm_rows_backward, rotary_frames)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, bias, eps):
+        y, h, mean, rstd = layer_norm_rows(x, weight, bias, eps, residual=residual)
+        ctx.save_for_backward(h, weight, mean, rstd)
+        ctx.summed = residual is not None
+        return (y, h) if ctx.summed else y
+
+    @staticmethod
+    def backward(ctx, grad_y, grad_h=None):
+        h, weight, mean, rstd = ctx.saved_tensors
+        dx, dw, db = layer_norm_rows_backward(grad_y.contiguous(), h, weight, mean, rstd,
+                                              grad_sum=grad_h.contiguous() if grad_h is not None else None)
+        return dx, dx if ctx.summed else None, dw, db, None
+
+
+def layer_norm(x, weight, bias, eps=1e-5, residual=None):
+    """Layer norm of the rows of x, or of x + residual: y, or (y, the sum)."""
+    return _LayerNorm.apply(x, residual, weight, bias, eps)
+
+
+class _Rotary(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, xy, time, axes):
+        ctx.xy, ctx.time, ctx.axes = xy, time, axes
+        return rotary_frames(q, k, xy, axes, time=time)
+
+    @staticmethod
+    def backward(ctx, grad_q, grad_k):
+        dq, dk = rotary_frames(grad_q.contiguous(), grad_k.contiguous(), ctx.xy, ctx.axes, time=ctx.time, inverse=True)
+        return dq, dk, None, None, None
+
+
+def rotary(q, k, xy, axes: RotaryAxes, time=None):
+    """Queries and keys turned by their birds' time, y and x."""
+    return _Rotary.apply(q, k, xy, time, axes)
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, slopes, offsets, more):
+        out, lse = attention_frames(q, k, v, offsets, slopes=slopes, return_lse=True, **more)
+        ctx.save_for_backward(q, k, v, slopes, offsets, out, lse)
+        ctx.more = more
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        q, k, v, slopes, offsets, out, lse = ctx.saved_tensors
+        dq, dk, dv, ds = attention_frames_backward(grad_out.contiguous(), q, k, v, out, lse, offsets, slopes=slopes,
+                                                   **ctx.more)
+        return dq, dk, dv, ds, None, None
+
+
+def attention(q, k, v, offsets, slopes=None, **more):
+    """attention_frames with gradients of q, k, v and slopes; `more` holds its
+    other arguments (k_offsets, q_xy, k_xy, scale, cap, keep, causal, prefix)."""
+    return _Attention.apply(q, k, v, slopes, offsets, more)
+
+
+class EncoderBlock(torch.nn.Module):
+    """Attention among the birds of a frame, then a layer per bird, each on the
+    layer norm of what came before and added to it."""
+
+    def __init__(self, width: int, q_heads: int, axes: RotaryAxes, kv_heads: int | None = None,
+                 head_dim: int = 64, sigma_px=(30.0, 960.0), cap: float = 0.0, hidden: int | None = None,
+                 dtype=torch.bfloat16):
+        super().__init__()
+        kv_heads = q_heads if kv_heads is None else kv_heads
+        hidden = 4 * width if hidden is None else hidden
+        self.heads = (q_heads, kv_heads, head_dim)
+        self.axes, self.cap = axes, cap
+
+        def linear(rows, columns):
+            return torch.nn.Parameter((torch.randn(rows, columns) * columns ** -0.5).to(dtype))
+
+        self.qkv = linear((q_heads + 2 * kv_heads) * head_dim, width)
+        self.out = linear(width, q_heads * head_dim)
+        self.up, self.down = linear(hidden, width), linear(width, hidden)
+        self.norm_weight = torch.nn.Parameter(torch.ones(2, width))
+        self.norm_bias = torch.nn.Parameter(torch.zeros(2, width))
+        # heads that look from sigma_px[0] to sigma_px[1] around a bird, learned from there
+        low, high = sigma_px
+        sigma = low * (high / low) ** (torch.arange(q_heads) / max(q_heads - 1, 1))
+        self.log_slopes = torch.nn.Parameter(torch.log(0.5 / sigma ** 2))
+
+    def forward(self, x, offsets, xy, time=None, keep=None):
+        hq, hk, dim = self.heads
+        y = layer_norm(x, self.norm_weight[0], self.norm_bias[0])
+        qkv = (y @ self.qkv.t()).view(-1, hq + 2 * hk, dim)
+        q, k = rotary(qkv[:, :hq], qkv[:, hq:hq + hk], xy, self.axes, time)
+        a = attention(q, k, qkv[:, hq + hk:], offsets, self.log_slopes.exp(), q_xy=xy, cap=self.cap, keep=keep)
+        y, x = layer_norm(a.flatten(1) @ self.out.t(), self.norm_weight[1], self.norm_bias[1], residual=x)
+        return x + torch.nn.functional.gelu(y @ self.up.t()) @ self.down.t()

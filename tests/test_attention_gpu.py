@@ -163,6 +163,44 @@ def test_birds_far_from_the_origin():
     compare(make(9, [200], [200], 4, 4, 64, torch.bfloat16, distance=True, far=(1 << 24) - 16 * 400 - 1))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("cap", [0.0, 6.0])
+@pytest.mark.parametrize("heads", [(2, 2), (4, 1)])
+def test_groups_of_birds_far_apart(heads, cap, dtype):
+    """Tiles whose birds are near each other and tiles that are not: distances
+    by matrix products and by differences in one frame (enough rows for tiles
+    of 128)."""
+    counts = [190] * 100
+    c = make(17, counts, counts, *heads, 32, dtype, distance=True, cap=cap, hidden=0.1, sigma=(15.0, 60.0))
+    place = torch.arange(sum(counts))
+    # a third of the birds 20000 px away, in runs of two tiles of keys and mixed with the others
+    far = ((place // 128) % 3 == 1) | (place % 7 == 0)
+    c["k_xy"][:, 0] += far.int() * 16 * 20000
+    compare(c)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("flags", [dict(), dict(cap=5.0), dict(hidden=0.3), dict(causal=True)])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_outputs_without_lse(dim, flags, dtype):
+    """Inference, with sharp and wide heads, two query heads a key head."""
+    counts = [(53 * f) % 260 for f in range(80)]
+    c = make(19 + dim, counts, counts, 8, 4, dim, dtype, distance=True, sigma=(10.0, 300.0), **flags)
+    d = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in c.items()}
+    off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    got = flock.attention_frames(d["q"], d["k"], d["v"], off, q_xy=d["q_xy"], slopes=d["slopes"], scale=c["scale"],
+                                 cap=c["cap"], keep=d.get("keep"), causal=c["causal"])
+    want, bound = reference(c, train=False)
+    ref.check(got, want["out"], bound["out"], "out")
+
+
+def test_steep_flat_and_rising_slopes():
+    """Slopes of zero, below zero and many times a frame's size."""
+    c = make(18, [150, 90], [150, 90], 4, 4, 64, torch.bfloat16, distance=True)
+    c["slopes"] = torch.tensor([0.0, -1e-5, 1e-3, 0.5])
+    compare(c)
+
+
 def test_slices_of_one_projection():
     c = make(10, [90, 45], [90, 45], 4, 2, 64, torch.bfloat16, distance=True)
     n = 135
