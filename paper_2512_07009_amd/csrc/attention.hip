@@ -1,5 +1,5 @@
 // attention.hip - attention of the birds of a frame (or of a track) among
-// themselves, or of a few queries over them, and its backward pass.
+// themselves, or of a few queries over them.
 //
 // For query i and key j of a frame, head h, d2 their squared distance in px^2:
 //   t = scale q_i.k_j, capped: t = cap tanh(t / cap);   s = t - slope_h d2
@@ -35,6 +35,16 @@ using namespace attention;
 // Forward, many rows: 128 rows a workgroup, 32 a wave, all waves over the same
 // tiles of keys.  A tile's loads are in flight while the tile before is worked
 // on, between two LDS buffers with one barrier a tile.
+//
+// Bound by vector instructions, not by the matrix cores: of 32 x 32 scores with
+// heads of 64 the products take 8 x 32 cycles, the softmax at least 480 (a multiply
+// and add, half a maximum, an exponential at a quarter of the rate, a sum and half a
+// rounding to 16 bits each), and distances or caps add to that.  8 heads of 64: 96
+// tracks in order 885 us, 0.63 PFLOP/s (VALU 69% of the time, matrix cores 38%); 64
+// frames of 2000 with distances and lse 1037 us, 0.46 (91%, 23%), with distances and
+// cap 1075 us, 0.44 (86%, 25%).  24 frames of 8000, 8 heads of 128 over 2: 8.9 ms, 0.64
+// PFLOP/s (51%, 33%); registers leave two waves a SIMD there, which do not cover
+// each other's waits, and a third would spill.
 // ---------------------------------------------------------------------------
 
 // Scores above the shift by less than this are left there (their weights reach
@@ -118,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
     float m = -INFINITY, shift = 0.0f, l = 0.0f;
 
     // A tile is worked on at once where registers allow it for the waves there are
-    // (no distances; a third faster for it), else by halves.  A weight is
+    // (no distances), else by halves.  A weight is
     // 2^(s * unit - shift): scores without caps (and with distances on the matrix
     // cores) stay products until then.
     constexpr bool PLAIN = !DIST && !CAP;
@@ -278,7 +288,11 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
 // Forward, few rows: 32 rows a workgroup, its waves over a quarter of the keys
 // each, joined in LDS, and where a.splits > 1 each workgroup over a share of the
 // keys, joined by attention_join_kernel: for launches that would leave the card
-// idle otherwise, and for rows too few to fill a tile.
+// idle otherwise, and for rows too few to fill a tile.  Bound by memory over a
+// long history: 256 frames of one query and 8000 keys, 8 heads over 2 of 128,
+// 352 us, 6.0 TB/s of keys and values (the first form, a tile at a time without
+// loads ahead, took 724); one frame of 500 birds 11.3 us, the chain of loads,
+// four tiles and the joint.
 // ---------------------------------------------------------------------------
 
 // (two workgroups of a compute unit have LDS for rows of 17 chunks with heads of 128, not of 20)
@@ -530,6 +544,7 @@ AttentionPlan plan_attention(int32_t n_frames, int32_t total_q, int32_t total_k,
     if (n_frames <= 0 || total_q <= 0 || q_heads <= 0 || kv_heads <= 0) return p;
     const int64_t rows = (int64_t)total_q * (q_heads / kv_heads);
     const int64_t tiles = rows / 128 + n_frames;
+    // few rows a frame would fill half a 128-row tile at most; few tiles leave compute units idle
     p.split = tiles * kv_heads < 2 * (int64_t)n_cus || rows / n_frames <= 64;
     p.slots = rows / (p.split ? 32 : 128) + n_frames;
     p.splits = 1;
