@@ -353,6 +353,11 @@ def _dtype(t):
 # The checks below read each attribute once and compare device numbers: a call
 # on few birds is bound by the host.
 
+def _like(t):
+    """A contiguous tensor of t's shape, type and device (0.9 us; torch.empty of them takes 1.4)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _rows(t, name, like=None):
     """Stride of a device matrix [rows, width] whose rows are contiguous."""
     shape = t.shape
@@ -406,10 +411,9 @@ def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: t
     bp = _vector(bias, "bias", torch.float32, width, index) if bias is not None else None
     rs = _rows(residual, "residual", x) if residual is not None else 0
     if out is None:
-        y = torch.empty((n, width), dtype=x.dtype, device=dev)
-        h = torch.empty((n, width), dtype=x.dtype, device=dev) if residual is not None else x
-        stats = torch.empty((2, n), dtype=torch.float32, device=dev)
-        mean, rstd = stats[0], stats[1]
+        y = _like(x)
+        h = _like(x) if residual is not None else x
+        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=dev).unbind()
         ys = hs = width
     else:
         y, h, mean, rstd = out
@@ -442,8 +446,8 @@ def layer_norm_rows_backward(grad_y: torch.Tensor, h: torch.Tensor, weight: torc
     wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
     mp = _vector(mean, "mean", torch.float32, n, index)
     rp = _vector(rstd, "rstd", torch.float32, n, index)
-    dx = torch.empty((n, width), dtype=h.dtype, device=dev)
-    dw, db = torch.empty((2, width), dtype=torch.float32, device=dev)
+    dx = _like(h)
+    dw, db = torch.empty((2, width), dtype=torch.float32, device=dev).unbind()
     L = lib()
     ws_bytes = L.layer_norm_rows_backward_workspace(n, width)
     ws = _workspace(ws_bytes, dev, stream)
@@ -497,14 +501,14 @@ def rotary_frames(q: torch.Tensor | None, k: torch.Tensor | None, xy: torch.Tens
     qos = kos = 0
     if q is not None:
         if qo is None:
-            qo, qos = torch.empty(q.shape, dtype=q.dtype, device=dev), q.shape[1] * dim
+            qo, qos = _like(q), q.shape[1] * dim
         else:
             qos = _heads(qo, "out's q", first)
             if qo.shape != q.shape:
                 raise ValueError("out's q must have the shape of q")
     if k is not None:
         if ko is None:
-            ko, kos = torch.empty(k.shape, dtype=k.dtype, device=dev), k.shape[1] * dim
+            ko, kos = _like(k), k.shape[1] * dim
         else:
             kos = _heads(ko, "out's k", first)
             if ko.shape != k.shape:
@@ -564,7 +568,7 @@ def attention_frames(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offset
     """
     code, dev, shape, head, tail = _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = _like(q)
         out_stride = shape[3] * shape[5]
     else:
         out_stride = _heads(out, "out", q)
@@ -594,8 +598,7 @@ def attention_frames_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     if grad_out.shape != q.shape or out.shape != q.shape:
         raise ValueError("grad_out and out must have the shape of q")
     lp = _vector(lse, "lse", torch.float64, shape[1] * shape[3], dev.index)
-    dq = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    dk, dv = torch.empty((2,) + k.shape, dtype=q.dtype, device=dev)
+    dq, dk, dv = _like(q), _like(k), _like(k)
     ds = torch.empty(shape[3], dtype=torch.float32, device=dev) if slopes is not None else None
     q_row, k_row = shape[3] * shape[5], shape[4] * shape[5]
     L = lib()
