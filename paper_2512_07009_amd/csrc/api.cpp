@@ -1131,7 +1131,7 @@ flock_status attention_frames_backward(
         grad_k_stride % 8 || grad_v_stride % 8)
         return fail(FLOCK_EINVAL, "strides of grad_q, grad_k and grad_v must be multiples of 8 that hold a row");
     if (grad_slopes && !slopes) return fail(FLOCK_EINVAL, "grad_slopes without slopes");
-    if (n_frames == 0) return FLOCK_OK;
+    if (n_frames == 0 && !grad_slopes) return FLOCK_OK;  // (else they are zeros)
     st = check_attention_pointers(a);
     if (st != FLOCK_OK) return st;
     if (total_q > 0 && (!grad_out || !lse || !grad_q))

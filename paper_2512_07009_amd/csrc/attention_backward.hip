@@ -617,7 +617,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
                                                    align256((size_t)a.total_q * (size_t)a.q_heads * sizeof(float)));
     a.slots = backward_slots(a.n_frames, a.total_q, a.group);
     a.group_reciprocal = group_reciprocal(a.group);
-    hipError_t err = with_kernel(a, dtype, [&](auto t, auto dp, auto dist, auto cap) {
+    hipError_t err = a.n_frames == 0 ? hipSuccess : with_kernel(a, dtype, [&](auto t, auto dp, auto dist, auto cap) {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
         constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
@@ -640,9 +640,9 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
         return e;
     });
     if (err != hipSuccess || !grad_slopes) return err;
-    // without queries there are no shares, and the gradients are zeros
+    // without frames or queries there are no shares, and the gradients are zeros
     hipLaunchKernelGGL(slope_total_kernel, dim3(a.q_heads), dim3(1024), 0, stream, b.slope_shares,
-                       a.total_q > 0 ? a.slots : 0, a.q_heads, grad_slopes);
+                       a.n_frames > 0 && a.total_q > 0 ? a.slots : 0, a.q_heads, grad_slopes);
     return hipGetLastError();
 }
 

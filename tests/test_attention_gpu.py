@@ -342,6 +342,21 @@ def test_empty_calls():
     assert (dk == 0).all() and (dv == 0).all()
 
 
+@pytest.mark.parametrize("frames,n_q,n_k", [(0, 0, 0), (2, 0, 0), (2, 0, 3), (2, 3, 0)])
+def test_slopes_without_pairs(frames, n_q, n_k):
+    q, k = (torch.ones(n, 2, 64, dtype=torch.bfloat16, device="cuda") for n in (n_q, n_k))
+    qo, ko = (torch.tensor([0, 1, n][:frames + 1] if n else [0] * (frames + 1), dtype=torch.int32, device="cuda")
+              for n in (n_q, n_k))
+    more = dict(k_offsets=ko, slopes=torch.ones(2, device="cuda"), q_xy=torch.ones(n_q, 2, dtype=torch.int32, device="cuda"),
+                k_xy=torch.ones(n_k, 2, dtype=torch.int32, device="cuda"))
+    out, lse = flock.attention_frames(q, k, k, qo, return_lse=True, **more)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    dirty = torch.full((1 << 16,), math.nan, device="cuda")  # what the gradients' memory may hold
+    del dirty
+    dq, dk, dv, ds = flock.attention_frames_backward(q, q, k, k, out, lse, qo, **more)
+    assert (ds == 0).all() and (dq == 0).all() and (dk == 0).all() and (dv == 0).all()
+
+
 def test_python_refusals():
     q = torch.zeros(4, 2, 64, dtype=torch.bfloat16, device="cuda")
     off = torch.tensor([0, 4], dtype=torch.int32, device="cuda")
