@@ -364,7 +364,7 @@ def _rows(t, name, like=None):
     if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a device matrix with contiguous rows")
     stride = t.stride()
-    if stride[1] != 1 and shape[1] > 1:
+    if stride[1] != 1 and shape[1] > 1 and shape[0] > 0:  # (an empty matrix may have any strides)
         raise ValueError(f"{name} must be a device matrix with contiguous rows")
     if like is not None and (shape != like.shape or t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the shape, type and device of its counterpart")
@@ -379,7 +379,7 @@ def _heads(t, name, like=None):
         raise ValueError(f"{name} must be a device tensor [birds, heads, head_dim] with contiguous rows")
     n, heads, dim = shape
     stride = t.stride()
-    if (stride[2] != 1 and dim > 1) or (stride[1] != dim and heads > 1):
+    if n > 0 and ((stride[2] != 1 and dim > 1) or (stride[1] != dim and heads > 1)):
         raise ValueError(f"{name} must be a device tensor [birds, heads, head_dim] with contiguous rows")
     if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} must have the type and device of the queries")

@@ -30,11 +30,13 @@ class _LayerNorm(torch.autograd.Function):
         h, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = layer_norm_rows_backward(grad_y.contiguous(), h, weight, mean, rstd,
                                               grad_sum=grad_h.contiguous() if grad_h is not None else None)
-        return dx, dx if ctx.summed else None, dw, db, None
+        needs = ctx.needs_input_grad
+        return dx, dx if ctx.summed else None, dw if needs[2] else None, db if needs[3] else None, None
 
 
 def layer_norm(x, weight, bias, eps=1e-5, residual=None):
-    """Layer norm of the rows of x, or of x + residual: y, or (y, the sum)."""
+    """Layer norm of the rows of x, or of x + residual: y, or (y, the sum).
+    weight and bias may be None (1 and 0)."""
     return _LayerNorm.apply(x, residual, weight, bias, eps)
 
 
@@ -46,12 +48,12 @@ class _Rotary(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_q, grad_k):
-        dq, dk = rotary_frames(grad_q.contiguous(), grad_k.contiguous(), ctx.xy, ctx.axes, time=ctx.time, inverse=True)
-        return dq, dk, None, None, None
+        grads = (g.contiguous() if g is not None else None for g in (grad_q, grad_k))
+        return *rotary_frames(*grads, ctx.xy, ctx.axes, time=ctx.time, inverse=True), None, None, None
 
 
 def rotary(q, k, xy, axes: RotaryAxes, time=None):
-    """Queries and keys turned by their birds' time, y and x."""
+    """Queries and keys (either may be None) turned by their birds' time, y and x."""
     return _Rotary.apply(q, k, xy, time, axes)
 
 

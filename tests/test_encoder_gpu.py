@@ -55,6 +55,50 @@ def test_frames_do_not_see_each_other():
     assert torch.equal(a[:70], b[:70])
 
 
+@pytest.mark.parametrize("weight,bias", [(False, False), (True, False), (False, True)])
+def test_layer_norm_without_weight_or_bias(weight, bias):
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(20, 48, generator=gen).cuda().requires_grad_()
+    w = torch.rand(48, generator=gen).cuda().requires_grad_() if weight else None
+    b = torch.rand(48, generator=gen).cuda().requires_grad_() if bias else None
+    g = torch.randn(20, 48, generator=gen).cuda()
+    encoder.layer_norm(x, w, b).backward(g)
+    leaves = [t for t in (x, w, b) if t is not None]
+    same = [t.detach().cpu().double().requires_grad_() for t in leaves]
+    rest = same[1:]
+    x64, w64, b64 = same[0], rest.pop(0) if weight else torch.ones(48).double(), rest.pop(0) if bias else 0.0
+    centred = x64 - x64.mean(1, keepdim=True)
+    y = centred / (centred.pow(2).mean(1, keepdim=True) + 1e-5).sqrt() * w64 + b64
+    y.backward(g.cpu().double())
+    for got, want in zip(leaves, same):
+        # 32-bit arithmetic over sums of 48 and 20: well below 2^-17 of the norm
+        assert (got.grad.cpu().double() - want.grad).norm() <= 2 ** -17 * want.grad.norm()
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_rotary_of_queries_or_keys_alone(which):
+    x = torch.randn(9, 2, 8, device="cuda", requires_grad=True)
+    xy = torch.randint(0, 4000, (9, 2), dtype=torch.int32, device="cuda")
+    pair = [None, None]
+    pair[which] = x
+    turned = encoder.rotary(*pair, xy, RotaryAxes(y=[0.1, 0.2], x=[0.3, 0.4]))
+    assert turned[1 - which] is None
+    g = torch.randn(9, 2, 8, device="cuda")
+    turned[which].backward(g)
+    # a turn keeps products (32 bits): <turn x, g> = <x, turned back g>
+    assert torch.allclose((turned[which].double() * g).sum((1, 2)), (x.double() * x.grad).sum((1, 2)), rtol=0, atol=1e-4)
+
+
+@pytest.mark.parametrize("off", [[0], [0, 0, 0]])
+def test_block_without_birds(off):
+    block = encoder.EncoderBlock(64, q_heads=2, head_dim=32, axes=RotaryAxes(y=[0.1] * 8, x=[0.05] * 8)).cuda()
+    x = torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+    y = block(x, torch.tensor(off, dtype=torch.int32, device="cuda"), torch.zeros(0, 2, dtype=torch.int32, device="cuda"))
+    y.sum().backward()
+    assert y.shape == (0, 64)
+    assert all((p.grad == 0).all() for p in block.parameters())
+
+
 def test_example_learns():
     sys.path.insert(0, os.path.join(ROOT, "examples"))
     import bird_encoder
