@@ -37,9 +37,9 @@ using namespace attention;
 // on, between two LDS buffers with one barrier a tile.
 //
 // Bound by vector instructions, not by the matrix cores: of 32 x 32 scores with
-// heads of 64 the products take 8 x 32 cycles, the softmax at least 480 (a multiply
-// and add, half a maximum, an exponential at a quarter of the rate, a sum and half a
-// rounding to 16 bits each), and distances or caps add to that.  8 heads of 64: 96
+// heads of 64 the products take 8 x 32 cycles, the softmax at least 320 (a multiply
+// and add, half a maximum, an exponential at half the rate, a sum and half a rounding
+// to 16 bits each), and distances, caps and masks add to that.  8 heads of 64: 96
 // tracks in order 885 us, 0.63 PFLOP/s (VALU 69% of the time, matrix cores 38%); 64
 // frames of 2000 with distances and lse 1037 us, 0.46 (91%, 23%), with distances and
 // cap 1075 us, 0.44 (86%, 25%).  24 frames of 8000, 8 heads of 128 over 2: 8.9 ms, 0.64
