@@ -270,12 +270,16 @@ __device__ __forceinline__ bool near_enough(int x, int y, float n, float largest
 // zeros there and get a penalty of -infinity on their scores, so that nothing
 // else need tell them apart; `seen` has a bit for each key that takes part, 64 a word.
 //
-// A tile is one buffer resource whose end is the end of its last key, so that
-// loads beyond it (absent keys, dimensions beyond the head's, which are sent
-// there) return zeros without a test; offsets within it stay below 2^31
-// (kAttentionMaxStride), tiles begin at 64-bit addresses.
-constexpr int kTileKeys = 64;
+// Each part of a tile (kPartKeys keys, or all of them) is one buffer resource
+// whose end is the end of its last key, so that loads beyond it (absent keys,
+// dimensions beyond the head's and hidden keys, which are sent there) return zeros
+// without a test; parts begin at 64-bit addresses.  However far rows lie apart, a
+// part ends before kBeyond, and kBeyond with a thread's later rows is below 2^32.
+constexpr int kTileKeys = 64, kPartKeys = 64;
 constexpr int kBeyond = 0x7ffffff0;
+static_assert((kPartKeys - 1) * 2 * kAttentionMaxStride + 2 * kAttentionMaxDim <= kBeyond &&
+                  kBeyond + (kPartKeys - 1) * 2 * kAttentionMaxStride + 2 * kAttentionMaxDim < 1ll << 32,
+              "offsets within a part of a tile fit the resource's 32 bits");
 
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -343,12 +347,15 @@ struct KeyTile {
         const int rows = present = min(end - first, KEYS);
         const int64_t row0 = sp.k0 + first;
         const int k_step = (int)a.k_stride * 2, v_step = (int)a.v_stride * 2;
-        constexpr int kParts = KEYS / 64 > 1 && kEven ? KEYS / 64 : 1;  // of 64 rows: fewer offsets to keep
-        constexpr int kEach = kLoads / kParts;
+        // (wide heads in large tiles: half parts leave a thread fewer offsets to keep)
+        constexpr int kPart = KEYS > kPartKeys && DP == 128 ? kPartKeys / 2 : KEYS < kPartKeys ? KEYS : kPartKeys;
+        constexpr int kParts = KEYS / kPart, kEach = kLoads / kParts;
+        static_assert(kEach * kThreads == kPart * kChunks, "a load of a thread is of one part");
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
-            const int64_t from = row0 + 64 * part;
-            const int left = rows - 64 * part;  // without rows: a resource of no bytes, never looked at beyond its base
+            const int64_t from = row0 + kPart * part;
+            // without rows: a resource of no bytes, never looked at beyond its base
+            const int left = min(rows - kPart * part, kPart);
             const auto kr = tile_resource(a.k, left > 0 ? from * a.k_stride + head * a.dim : 0,
                                           left > 0 ? (left - 1) * k_step + a.dim * 2 : 0);
             const auto vr = tile_resource(a.v, left > 0 ? from * a.v_stride + head * a.dim : 0,
@@ -361,7 +368,7 @@ struct KeyTile {
                 uint32_t k_from = (uint32_t)k_at + (uint32_t)(m * kStep * k_step);
                 uint32_t v_from = (uint32_t)v_at + (uint32_t)(m * kStep * v_step);
                 if (!kEven) {
-                    const int e = threadIdx.x + n * kThreads, r = e / kChunks, c = e % kChunks;
+                    const int e = threadIdx.x + m * kThreads, r = e / kChunks, c = e % kChunks;  // within the part
                     k_from = c * 8 < a.dim ? r * k_step + c * 16 : kBeyond;
                     v_from = c * 8 < a.dim ? r * v_step + c * 16 : kBeyond;
                 }

@@ -242,7 +242,7 @@ struct RotaryArgs {
 hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);
 
 constexpr int kAttentionMaxDim = 128;
-// 64 rows of a tile lie within 2^31 bytes
+// 64 rows lie within 2^31 bytes: a tile's loads go through resources of 64 rows at most
 constexpr int64_t kAttentionMaxStride = (1 << 24) - 8;
 
 struct AttentionArgs {

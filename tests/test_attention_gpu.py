@@ -379,3 +379,22 @@ def test_python_refusals():
         flock.attention_frames(z, q, q, off)
     with pytest.raises(ValueError, match="cap"):
         flock.attention_frames(q, q, q, off, cap=-1.0)
+
+
+@pytest.mark.parametrize("dim", [32, 64, 72, 80, 96, 128])
+def test_rows_as_far_apart_as_they_may_be(dim):
+    """Strides up to the largest, in a tensor of NaN: hidden keys and what lies
+    beyond a head's dimensions are not read, wherever the tile's rows are."""
+    n, stride = 150, (1 << 24) - 8
+    big = torch.full((n * stride,), math.nan, dtype=torch.bfloat16, device="cuda")
+    c = make(20 + dim, [2], [n], 2, 1, dim, torch.bfloat16, hidden=0.2)
+    k, v = big.as_strided((n, 1, dim), (stride, dim, 1)), big.as_strided((n, 1, dim), (stride, dim, 1), 1024)
+    kept = c["keep"].bool().cuda()
+    k[kept], v[kept] = c["k"].cuda()[kept], c["v"].cuda()[kept]
+    q, go, keep = c["q"].cuda(), c["grad"].cuda(), c["keep"].cuda()
+    qo, ko = (torch.tensor(c[x], dtype=torch.int32).cuda() for x in ("q_off", "k_off"))
+    out, lse = flock.attention_frames(q, k, v, qo, k_offsets=ko, keep=keep, return_lse=True)
+    dq, dk, dv, _ = flock.attention_frames_backward(go, q, k, v, out, lse, qo, k_offsets=ko, keep=keep)
+    want, bound = reference(c)
+    for name, got in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        ref.check(got, want[name], bound[name], name)
