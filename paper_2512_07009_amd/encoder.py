@@ -43,13 +43,16 @@ def layer_norm(x, weight, bias, eps=1e-5, residual=None):
 class _Rotary(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, xy, time, axes):
-        ctx.xy, ctx.time, ctx.axes = xy, time, axes
+        # (saved as tensors: autograd then refuses a backward pass on places that were overwritten)
+        ctx.save_for_backward(xy, time)
+        ctx.axes = axes
         return rotary_frames(q, k, xy, axes, time=time)
 
     @staticmethod
     def backward(ctx, grad_q, grad_k):
+        xy, time = ctx.saved_tensors
         grads = (g.contiguous() if g is not None else None for g in (grad_q, grad_k))
-        return *rotary_frames(*grads, ctx.xy, ctx.axes, time=ctx.time, inverse=True), None, None, None
+        return *rotary_frames(*grads, xy, ctx.axes, time=time, inverse=True), None, None, None
 
 
 def rotary(q, k, xy, axes: RotaryAxes, time=None):
@@ -61,15 +64,17 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, slopes, offsets, more):
         out, lse = attention_frames(q, k, v, offsets, slopes=slopes, return_lse=True, **more)
-        ctx.save_for_backward(q, k, v, slopes, offsets, out, lse)
-        ctx.more = more
+        # places and masks too are saved as tensors, so that one that was overwritten is refused
+        ctx.names = [name for name, value in more.items() if torch.is_tensor(value)]
+        ctx.more = {name: value for name, value in more.items() if name not in ctx.names}
+        ctx.save_for_backward(q, k, v, slopes, offsets, out, lse, *(more[name] for name in ctx.names))
         return out
 
     @staticmethod
     def backward(ctx, grad_out):
-        q, k, v, slopes, offsets, out, lse = ctx.saved_tensors
+        q, k, v, slopes, offsets, out, lse, *saved = ctx.saved_tensors
         dq, dk, dv, ds = attention_frames_backward(grad_out.contiguous(), q, k, v, out, lse, offsets, slopes=slopes,
-                                                   **ctx.more)
+                                                   **ctx.more, **dict(zip(ctx.names, saved)))
         return dq, dk, dv, ds, None, None
 
 

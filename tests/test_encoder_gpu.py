@@ -105,3 +105,32 @@ def test_example_learns():
     losses, right = bird_encoder.main(steps=40, frames=4, height=240, width=320, n_birds=150, quiet=True)
     assert torch.isfinite(losses).all()
     assert losses[-5:].mean() < 0.7 * losses[:5].mean()
+
+
+@pytest.mark.parametrize("name", ["q_xy", "k_xy", "k_offsets", "keep", "prefix", "offsets", "slopes", "v"])
+def test_overwritten_inputs_of_attention_are_refused(name):
+    """Gradients of other places or masks than the forward pass had are wrong."""
+    n = 40
+    q = torch.randn(n, 2, 32, device="cuda").to(torch.bfloat16).requires_grad_()
+    v = torch.randn(n, 2, 32, device="cuda").to(torch.bfloat16)
+    offsets = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    slopes = torch.ones(2, device="cuda")
+    more = dict(q_xy=torch.zeros(n, 2, dtype=torch.int32, device="cuda"),
+                k_xy=torch.zeros(n, 2, dtype=torch.int32, device="cuda"), k_offsets=offsets.clone(),
+                keep=torch.ones(n, dtype=torch.uint8, device="cuda"),
+                prefix=torch.zeros(1, dtype=torch.int32, device="cuda"), causal=True)
+    out = encoder.attention(q, q, v, offsets, slopes, **more)
+    dict(more, offsets=offsets, slopes=slopes, v=v)[name].add_(0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+@pytest.mark.parametrize("name", ["xy", "time"])
+def test_overwritten_places_of_rotary_are_refused(name):
+    q = torch.randn(9, 2, 8, device="cuda", requires_grad=True)
+    places = dict(xy=torch.zeros(9, 2, dtype=torch.int32, device="cuda"),
+                  time=torch.zeros(9, dtype=torch.int32, device="cuda"))
+    turned, _ = encoder.rotary(q, None, places["xy"], RotaryAxes(time=[0.1], y=[0.1]), time=places["time"])
+    places[name].add_(0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        turned.sum().backward()
