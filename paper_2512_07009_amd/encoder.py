@@ -6,15 +6,43 @@ functions, and a block that puts them together:
     block = EncoderBlock(width=256, q_heads=4, axes=RotaryAxes(y=..., x=...)).to("cuda")
     h = block(features, offsets, xy)         # [T, width] bfloat16, a row per bird
 
-Linear layers are plain matrix products of torch.
+Linear layers are plain matrix products of torch.  The functions have first
+derivatives only: differentiating their gradients raises.
 """
 
 from __future__ import annotations
+
+import functools
 
 import torch
 
 from .binding import (RotaryAxes, attention_frames, attention_frames_backward, layer_norm_rows,
                       layer_norm_rows_backward, rotary_frames)
+
+
+class _Final(torch.autograd.Function):
+    """Gradients as they are, whose own gradients raise."""
+
+    @staticmethod
+    def forward(ctx, *values):
+        return values
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the encoder's operators have no second derivatives")
+
+
+def _once(backward):
+    """A backward pass by kernels that autograd does not see: under create_graph
+    its results must not pass for constants."""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        with torch.no_grad():
+            result = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return result
+        return _Final.apply(*(r.detach().requires_grad_() if torch.is_tensor(r) else r for r in result))
+    return run
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -26,6 +54,7 @@ class _LayerNorm(torch.autograd.Function):
         return (y, h) if ctx.summed else y
 
     @staticmethod
+    @_once
     def backward(ctx, grad_y, grad_h=None):
         h, weight, mean, rstd = ctx.saved_tensors
         dx, dw, db = layer_norm_rows_backward(grad_y.contiguous(), h, weight, mean, rstd,
@@ -49,6 +78,7 @@ class _Rotary(torch.autograd.Function):
         return rotary_frames(q, k, xy, axes, time=time)
 
     @staticmethod
+    @_once
     def backward(ctx, grad_q, grad_k):
         xy, time = ctx.saved_tensors
         grads = (g.contiguous() if g is not None else None for g in (grad_q, grad_k))
@@ -71,6 +101,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @_once
     def backward(ctx, grad_out):
         q, k, v, slopes, offsets, out, lse, *saved = ctx.saved_tensors
         dq, dk, dv, ds = attention_frames_backward(grad_out.contiguous(), q, k, v, out, lse, offsets, slopes=slopes,

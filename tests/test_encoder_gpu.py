@@ -134,3 +134,31 @@ def test_overwritten_places_of_rotary_are_refused(name):
     places[name].add_(0)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         turned.sum().backward()
+
+
+@pytest.mark.parametrize("steady", [False, True])
+@pytest.mark.parametrize("name", ["norm", "norm of a sum", "rotary", "attention"])
+def test_second_derivatives_are_refused(name, steady):
+    """Also where the first derivative's own input (steady) needs no gradient,
+    and where another path leads to the loss."""
+    x = torch.randn(24, 2, 32, device="cuda").to(torch.bfloat16).requires_grad_()
+    xy = torch.randint(0, 4000, (24, 2), dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 24], dtype=torch.int32, device="cuda")
+
+    def apply():
+        if name == "norm":
+            return encoder.layer_norm(x.flatten(1), None, None)
+        if name == "norm of a sum":
+            return encoder.layer_norm(x.flatten(1), None, None, residual=x.flatten(1))[0]
+        if name == "rotary":
+            return encoder.rotary(x, x, xy, RotaryAxes(x=[0.1]))[1]
+        return encoder.attention(x, x, x, off)
+
+    y = apply().float()
+    first, = torch.autograd.grad((y if steady else y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="no second derivatives"):
+        (first.float().pow(2).sum() + x.float().pow(2).sum()).backward()
+    # create_graph alone changes no first derivative
+    y = apply().float()
+    plain, = torch.autograd.grad((y if steady else y * y).sum(), x)
+    assert torch.equal(plain, first)
