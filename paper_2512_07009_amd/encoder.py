@@ -104,7 +104,10 @@ class _Attention(torch.autograd.Function):
     @_once
     def backward(ctx, grad_out):
         q, k, v, slopes, offsets, out, lse, *saved = ctx.saved_tensors
-        dq, dk, dv, ds = attention_frames_backward(grad_out.contiguous(), q, k, v, out, lse, offsets, slopes=slopes,
+        grad_out = grad_out.contiguous()
+        if grad_out.data_ptr() % 16:  # a part of another gradient
+            grad_out = grad_out.clone()
+        dq, dk, dv, ds = attention_frames_backward(grad_out, q, k, v, out, lse, offsets, slopes=slopes,
                                                    **ctx.more, **dict(zip(ctx.names, saved)))
         return dq, dk, dv, ds, None, None
 

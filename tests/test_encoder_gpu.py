@@ -162,3 +162,17 @@ def test_second_derivatives_are_refused(name, steady):
     y = apply().float()
     plain, = torch.autograd.grad((y if steady else y * y).sum(), x)
     assert torch.equal(plain, first)
+
+
+def test_gradient_that_is_a_part_of_another():
+    """The output's gradient may begin at any element of a larger one."""
+    x = torch.randn(10, 2, 32, device="cuda").to(torch.bfloat16)
+    off = torch.tensor([0, 10], dtype=torch.int32, device="cuda")
+    weights = torch.randn(641, device="cuda").to(torch.bfloat16)
+    grads = []
+    for first in (torch.zeros(1, device="cuda").to(torch.bfloat16), None):
+        q = x.clone().requires_grad_()
+        out = encoder.attention(q, q, q, off).flatten()
+        (torch.cat([first, out]) @ weights if first is not None else out @ weights[1:]).backward()
+        grads.append(q.grad)
+    assert torch.equal(*grads)
