@@ -393,6 +393,13 @@ def _vector(t, name, dtype, numel, index):
     return t.data_ptr()
 
 
+def _matrix(t, name, dtype, rows, columns, index):
+    """Pointer of [rows, columns] contiguous values on device number `index`."""
+    if t.dtype != dtype or t.shape != (rows, columns) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} [{rows}, {columns}] tensor on the features' device")
+    return t.data_ptr()
+
+
 def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
                     eps: float = 1e-5, residual: torch.Tensor | None = None, out=None, stream=None):
     """Layer norm of every row of x [N, width] (float32, float16 or bfloat16),
@@ -540,8 +547,8 @@ def _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, 
         sp = _vector(slopes, "slopes", torch.float32, hq, index)
         if q_xy is None:
             raise ValueError("q_xy is needed with slopes")
-        qp = _vector(q_xy, "q_xy", torch.int32, 2 * tq, index)
-        kp = _vector(q_xy if k_xy is None else k_xy, "k_xy", torch.int32, 2 * tk, index)
+        qp = _matrix(q_xy, "q_xy", torch.int32, tq, 2, index)
+        kp = _matrix(q_xy if k_xy is None else k_xy, "k_xy", torch.int32, tk, 2, index)
     keep_p = _vector(keep, "keep", torch.uint8, tk, index) if keep is not None else None
     prefix_p = _vector(prefix, "prefix", torch.int32, frames, index) if prefix is not None else None
     return (code, q.device, (frames, tq, tk, hq, hk, dim), (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs),
@@ -597,7 +604,7 @@ def attention_frames_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     out_stride = _heads(out, "out", q)
     if grad_out.shape != q.shape or out.shape != q.shape:
         raise ValueError("grad_out and out must have the shape of q")
-    lp = _vector(lse, "lse", torch.float64, shape[1] * shape[3], dev.index)
+    lp = _matrix(lse, "lse", torch.float64, shape[1], shape[3], dev.index)
     dq, dk, dv = _like(q), _like(k), _like(k)
     ds = torch.empty(shape[3], dtype=torch.float32, device=dev) if slopes is not None else None
     q_row, k_row = shape[3] * shape[5], shape[4] * shape[5]

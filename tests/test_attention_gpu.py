@@ -398,3 +398,20 @@ def test_rows_as_far_apart_as_they_may_be(dim):
     want, bound = reference(c)
     for name, got in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
         ref.check(got, want[name], bound[name], name)
+
+
+def test_places_and_lse_of_another_shape_are_refused():
+    """As many values in another order would be read as other places."""
+    q = torch.zeros(6, 2, 64, dtype=torch.bfloat16, device="cuda")
+    off = torch.tensor([0, 6], dtype=torch.int32, device="cuda")
+    xy = torch.zeros(6, 2, dtype=torch.int32, device="cuda")
+    slopes = torch.ones(2, device="cuda")
+    for wrong in (xy.t().contiguous(), xy.flatten(), xy[:, None].contiguous()):
+        with pytest.raises(ValueError, match="q_xy"):
+            flock.attention_frames(q, q, q, off, slopes=slopes, q_xy=wrong)
+        with pytest.raises(ValueError, match="k_xy"):
+            flock.attention_frames(q, q, q, off, slopes=slopes, q_xy=xy, k_xy=wrong)
+    out, lse = flock.attention_frames(q, q, q, off, return_lse=True)
+    for wrong in (lse.t().contiguous(), lse.flatten()):
+        with pytest.raises(ValueError, match="lse"):
+            flock.attention_frames_backward(q, q, q, q, out, wrong, off)
