@@ -126,6 +126,8 @@ class EncoderBlock(torch.nn.Module):
                  head_dim: int = 64, sigma_px=(30.0, 960.0), cap: float = 0.0, hidden: int | None = None,
                  dtype=torch.bfloat16):
         super().__init__()
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError(f"features of {dtype}: attention takes float16 or bfloat16")
         kv_heads = q_heads if kv_heads is None else kv_heads
         hidden = 4 * width if hidden is None else hidden
         self.heads = (q_heads, kv_heads, head_dim)
@@ -146,9 +148,11 @@ class EncoderBlock(torch.nn.Module):
 
     def forward(self, x, offsets, xy, time=None, keep=None):
         hq, hk, dim = self.heads
-        y = layer_norm(x, self.norm_weight[0], self.norm_bias[0])
+        # the norms and the slopes are in 32 bits, whatever type the block was moved to
+        weight, bias, slopes = self.norm_weight.float(), self.norm_bias.float(), self.log_slopes.float().exp()
+        y = layer_norm(x, weight[0], bias[0])
         qkv = (y @ self.qkv.t()).view(-1, hq + 2 * hk, dim)
         q, k = rotary(qkv[:, :hq], qkv[:, hq:hq + hk], xy, self.axes, time)
-        a = attention(q, k, qkv[:, hq + hk:], offsets, self.log_slopes.exp(), q_xy=xy, cap=self.cap, keep=keep)
-        y, x = layer_norm(a.flatten(1) @ self.out.t(), self.norm_weight[1], self.norm_bias[1], residual=x)
+        a = attention(q, k, qkv[:, hq + hk:], offsets, slopes, q_xy=xy, cap=self.cap, keep=keep)
+        y, x = layer_norm(a.flatten(1) @ self.out.t(), weight[1], bias[1], residual=x)
         return x + torch.nn.functional.gelu(y @ self.up.t()) @ self.down.t()

@@ -176,3 +176,27 @@ def test_gradient_that_is_a_part_of_another():
         (torch.cat([first, out]) @ weights if first is not None else out @ weights[1:]).backward()
         grads.append(q.grad)
     assert torch.equal(*grads)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_block_moved_to_a_16_bit_type(dtype):
+    """Its norms and slopes are used in 32 bits, and are trained as they are held."""
+    torch.manual_seed(4)
+    block = encoder.EncoderBlock(64, q_heads=2, head_dim=32, axes=RotaryAxes(y=[0.1] * 8, x=[0.05] * 8)).cuda().to(dtype)
+    x = torch.randn(50, 64, device="cuda").to(dtype)
+    xy = torch.randint(0, 16 * 300, (50, 2), dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 50], dtype=torch.int32, device="cuda")
+    y = block(x, off, xy)
+    y.float().pow(2).sum().backward()
+    assert y.dtype == dtype and torch.isfinite(y).all()
+    assert all(p.grad.dtype == dtype and torch.isfinite(p.grad).all() for p in block.parameters())
+    # the same values held in 32 bits give the same block
+    for p in (block.norm_weight, block.norm_bias, block.log_slopes):
+        p.data = p.data.float()
+    assert torch.equal(block(x, off, xy), y)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float64])
+def test_block_refuses_types_that_attention_does_not_take(dtype):
+    with pytest.raises(ValueError, match="float16 or bfloat16"):
+        encoder.EncoderBlock(64, q_heads=2, axes=RotaryAxes(x=[0.1]), dtype=dtype)
