@@ -133,6 +133,20 @@ def _workspace(nbytes: int, dev, stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=dev)
 
 
+def _new(shape, dtype, dev, stream):
+    """An output of a call, in memory of the stream the kernels run on: a block
+    that the current stream freed may still be in use there.  The current stream
+    is recorded in turn, since the caller goes on with the output there."""
+    if stream is None or stream.cuda_stream == _raw_stream(dev.index):
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.device(dev):
+        here = torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device=dev)
+        t.record_stream(here)
+    return t
+
+
 def _call(fn, dev, stream, *args):
     """fn(*args, stream) with dev as the current device."""
     if _current_device() == dev.index:
@@ -173,9 +187,9 @@ def cluster_frames(xy: torch.Tensor, offsets: torch.Tensor, eps_px: float, min_p
     F, T = _batch(xy, offsets)
     dev = xy.device
     if out is None:
-        labels = torch.empty(T, dtype=torch.int32, device=dev)
-        kind = torch.empty(T, dtype=torch.uint8, device=dev)
-        ncl = torch.empty(max(F, 0), dtype=torch.int32, device=dev)
+        labels = _new(T, torch.int32, dev, stream)
+        kind = _new(T, torch.uint8, dev, stream)
+        ncl = _new(max(F, 0), torch.int32, dev, stream)
     else:
         labels, kind, ncl = out
     L = lib()
@@ -195,8 +209,7 @@ def density_frames(xy: torch.Tensor, offsets: torch.Tensor, width_px: int, heigh
     """
     F, T = _batch(xy, offsets)
     dev = xy.device
-    dens = out if out is not None else torch.empty((max(F, 0), grid_h, grid_w), dtype=torch.float32,
-                                                  device=dev)
+    dens = out if out is not None else _new((max(F, 0), grid_h, grid_w), torch.float32, dev, stream)
     L = lib()
     ws_bytes = L.density_frames_workspace(F, T, int(grid_w), int(grid_h))
     ws = _workspace(ws_bytes, dev, stream)
@@ -221,12 +234,12 @@ def heatmap_frames(density: torch.Tensor, cell_area_px2: float, threshold: float
     F, gh, gw = density.shape
     dev = density.device
     if out is None:
-        out = {"labels": torch.empty((F, gh, gw), dtype=torch.int32, device=dev),
-               "n_components": torch.empty(F, dtype=torch.int32, device=dev),
-               "entropy": torch.empty(F, dtype=torch.float64, device=dev),
-               "degree": torch.empty(F, dtype=torch.float64, device=dev),
-               "comp_cells": torch.empty((F, gh, gw), dtype=torch.int32, device=dev),
-               "comp_mass": torch.empty((F, gh, gw), dtype=torch.float64, device=dev)}
+        out = {"labels": _new((F, gh, gw), torch.int32, dev, stream),
+               "n_components": _new(F, torch.int32, dev, stream),
+               "entropy": _new(F, torch.float64, dev, stream),
+               "degree": _new(F, torch.float64, dev, stream),
+               "comp_cells": _new((F, gh, gw), torch.int32, dev, stream),
+               "comp_mass": _new((F, gh, gw), torch.float64, dev, stream)}
     L = lib()
     ws_bytes = L.heatmap_frames_workspace(F, gw, gh)
     ws = _workspace(ws_bytes, dev, stream)
@@ -250,10 +263,10 @@ def roi_filter_frames(xy: torch.Tensor, offsets: torch.Tensor, roi_xy, with_inde
     poly = np.ascontiguousarray(np.asarray(roi_xy, dtype=np.int32).reshape(-1, 2))
     dev = xy.device
     if out is None:
-        out = {"counts": torch.empty(max(F, 0), dtype=torch.int32, device=dev),
-               "xy": torch.empty((T, 2), dtype=torch.int32, device=dev),
-               "offsets": torch.empty(F + 1, dtype=torch.int32, device=dev),
-               "index": torch.empty(T, dtype=torch.int32, device=dev) if with_index else None}
+        out = {"counts": _new(max(F, 0), torch.int32, dev, stream),
+               "xy": _new((T, 2), torch.int32, dev, stream),
+               "offsets": _new(F + 1, torch.int32, dev, stream),
+               "index": _new(T, torch.int32, dev, stream) if with_index else None}
     L = lib()
     ws_bytes = L.roi_filter_frames_workspace(F, T)
     ws = _workspace(ws_bytes, dev, stream)
@@ -276,9 +289,9 @@ def drinker_proximity_frames(xy: torch.Tensor, offsets: torch.Tensor, lines, thr
     ln = np.ascontiguousarray(np.asarray(lines, dtype=np.int32).reshape(-1, 4))
     dev = xy.device
     if out is None:
-        out = {"drinking": torch.empty(T, dtype=torch.uint8, device=dev),
-               "line": torch.empty(T, dtype=torch.int32, device=dev) if with_line else None,
-               "counts": torch.empty(max(F, 0), dtype=torch.int32, device=dev)}
+        out = {"drinking": _new(T, torch.uint8, dev, stream),
+               "line": _new(T, torch.int32, dev, stream) if with_line else None,
+               "counts": _new(max(F, 0), torch.int32, dev, stream)}
     L = lib()
     ws_bytes = L.drinker_proximity_frames_workspace(F, T)
     ws = _workspace(ws_bytes, dev, stream)
@@ -317,15 +330,15 @@ def mask_components_frames(prob: torch.Tensor, threshold: float, connectivity: i
         capacity = mask_capacity(F, H, W, connectivity)
     C = int(capacity)
     if out is None:
-        out = {"labels": torch.empty((F, H, W), dtype=torch.int32, device=dev) if with_labels else None,
-               "n_components": torch.empty(F, dtype=torch.int32, device=dev),
-               "offsets": torch.empty(F + 1, dtype=torch.int32, device=dev),
-               "label": torch.empty(C, dtype=torch.int32, device=dev),
-               "area": torch.empty(C, dtype=torch.int32, device=dev),
-               "box": torch.empty((C, 4), dtype=torch.int32, device=dev),
-               "centroid": torch.empty((C, 2), dtype=torch.float64, device=dev),
-               "xy": torch.empty((C, 2), dtype=torch.int32, device=dev),
-               "score": torch.empty(C, dtype=torch.float32, device=dev)}
+        out = {"labels": _new((F, H, W), torch.int32, dev, stream) if with_labels else None,
+               "n_components": _new(F, torch.int32, dev, stream),
+               "offsets": _new(F + 1, torch.int32, dev, stream),
+               "label": _new(C, torch.int32, dev, stream),
+               "area": _new(C, torch.int32, dev, stream),
+               "box": _new((C, 4), torch.int32, dev, stream),
+               "centroid": _new((C, 2), torch.float64, dev, stream),
+               "xy": _new((C, 2), torch.int32, dev, stream),
+               "score": _new(C, torch.float32, dev, stream)}
     L = lib()
     ws_bytes = L.mask_components_frames_workspace(F, W, H, int(connectivity))
     ws = _workspace(ws_bytes, dev, stream)
@@ -353,9 +366,12 @@ def _dtype(t):
 # The checks below read each attribute once and compare device numbers: a call
 # on few birds is bound by the host.
 
-def _like(t):
-    """A contiguous tensor of t's shape, type and device (0.9 us; torch.empty of them takes 1.4)."""
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+def _like(t, stream):
+    """A contiguous output of t's shape, type and device (0.9 us on the current
+    stream; torch.empty of them takes 1.4)."""
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    return _new(t.shape, t.dtype, t.device, stream)
 
 
 def _rows(t, name, like=None):
@@ -418,9 +434,9 @@ def layer_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, bias: t
     bp = _vector(bias, "bias", torch.float32, width, index) if bias is not None else None
     rs = _rows(residual, "residual", x) if residual is not None else 0
     if out is None:
-        y = _like(x)
-        h = _like(x) if residual is not None else x
-        mean, rstd = torch.empty((2, n), dtype=torch.float32, device=dev).unbind()
+        y = _like(x, stream)
+        h = _like(x, stream) if residual is not None else x
+        mean, rstd = _new((2, n), torch.float32, dev, stream).unbind()
         ys = hs = width
     else:
         y, h, mean, rstd = out
@@ -453,8 +469,8 @@ def layer_norm_rows_backward(grad_y: torch.Tensor, h: torch.Tensor, weight: torc
     wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
     mp = _vector(mean, "mean", torch.float32, n, index)
     rp = _vector(rstd, "rstd", torch.float32, n, index)
-    dx = _like(h)
-    dw, db = torch.empty((2, width), dtype=torch.float32, device=dev).unbind()
+    dx = _like(h, stream)
+    dw, db = _new((2, width), torch.float32, dev, stream).unbind()
     L = lib()
     ws_bytes = L.layer_norm_rows_backward_workspace(n, width)
     ws = _workspace(ws_bytes, dev, stream)
@@ -508,14 +524,14 @@ def rotary_frames(q: torch.Tensor | None, k: torch.Tensor | None, xy: torch.Tens
     qos = kos = 0
     if q is not None:
         if qo is None:
-            qo, qos = _like(q), q.shape[1] * dim
+            qo, qos = _like(q, stream), q.shape[1] * dim
         else:
             qos = _heads(qo, "out's q", first)
             if qo.shape != q.shape:
                 raise ValueError("out's q must have the shape of q")
     if k is not None:
         if ko is None:
-            ko, kos = _like(k), k.shape[1] * dim
+            ko, kos = _like(k, stream), k.shape[1] * dim
         else:
             kos = _heads(ko, "out's k", first)
             if ko.shape != k.shape:
@@ -575,13 +591,13 @@ def attention_frames(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offset
     """
     code, dev, shape, head, tail = _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, causal)
     if out is None:
-        out = _like(q)
+        out = _like(q, stream)
         out_stride = shape[3] * shape[5]
     else:
         out_stride = _heads(out, "out", q)
         if out.shape != q.shape:
             raise ValueError("out must have the shape of q")
-    lse = torch.empty((shape[1], shape[3]), dtype=torch.float64, device=dev) if return_lse else None
+    lse = _new((shape[1], shape[3]), torch.float64, dev, stream) if return_lse else None
     L = lib()
     ws_bytes = L.attention_frames_workspace(*shape)
     ws = _workspace(ws_bytes, dev, stream)
@@ -605,8 +621,8 @@ def attention_frames_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
     if grad_out.shape != q.shape or out.shape != q.shape:
         raise ValueError("grad_out and out must have the shape of q")
     lp = _matrix(lse, "lse", torch.float64, shape[1], shape[3], dev.index)
-    dq, dk, dv = _like(q), _like(k), _like(k)
-    ds = torch.empty(shape[3], dtype=torch.float32, device=dev) if slopes is not None else None
+    dq, dk, dv = _like(q, stream), _like(k, stream), _like(k, stream)
+    ds = _new(shape[3], torch.float32, dev, stream) if slopes is not None else None
     q_row, k_row = shape[3] * shape[5], shape[4] * shape[5]
     L = lib()
     ws_bytes = L.attention_frames_backward_workspace(*shape)

@@ -6,6 +6,7 @@ import sys
 import pytest
 import torch
 
+import paper_2512_07009_amd as flock
 from paper_2512_07009_amd import RotaryAxes, encoder
 
 pytestmark = pytest.mark.gpu
@@ -200,3 +201,33 @@ def test_block_moved_to_a_16_bit_type(dtype):
 def test_block_refuses_types_that_attention_does_not_take(dtype):
     with pytest.raises(ValueError, match="float16 or bfloat16"):
         encoder.EncoderBlock(64, q_heads=2, axes=RotaryAxes(x=[0.1]), dtype=dtype)
+
+
+@pytest.mark.parametrize("name", ["norm", "norm backward", "rotary", "attention", "attention backward", "density"])
+def test_outputs_on_another_stream_are_not_memory_in_use(name):
+    """A call on a stream of its own must not write into what the current stream
+    freed and is still working on."""
+    n = 300
+    off = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    xy = torch.randint(0, 16 * 1000, (n, 2), dtype=torch.int32, device="cuda")
+    x = torch.randn(n, 8, 64, device="cuda").to(torch.bfloat16)
+    _, h, mean, rstd = flock.layer_norm_rows(x.flatten(1))
+    out, lse = flock.attention_frames(x, x, x, off, return_lse=True)
+    call = {"norm": lambda s: flock.layer_norm_rows(x.flatten(1), stream=s)[0],
+            "norm backward": lambda s: flock.layer_norm_rows_backward(x.flatten(1), h, None, mean, rstd, stream=s)[0],
+            "rotary": lambda s: flock.rotary_frames(x, None, xy, RotaryAxes(x=[0.1]), stream=s)[0],
+            "attention": lambda s: flock.attention_frames(x, x, x, off, stream=s),
+            "attention backward": lambda s: flock.attention_frames_backward(x, x, x, x, out, lse, off, stream=s)[0],
+            "density": lambda s: flock.density_frames(xy, off, 1920, 1080, 128, 72, 40.0, stream=s)}[name]
+    want = call(None)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    freed = [torch.empty_like(want) for _ in range(4)]
+    torch.cuda._sleep(100_000_000)  # some 50 ms
+    for t in freed:
+        t.fill_(7)
+    del freed, t
+    got = call(stream)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
