@@ -487,7 +487,7 @@ flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const
  *   keep           device in, uint8[total_k], or NULL (all kept).
  *   causal         0 or 1.
  *   prefix         device in, int32[n_frames], or NULL (0); used when causal.
- *   scale, cap     finite; scale > 0, cap >= 0 (0: none).
+ *   scale, cap     finite; scale > 0, cap >= 0 (none: 0, or 2^96 and more).
  *   out            device out, [total_q][q_heads][head_dim].
  *   lse            device out, double[total_q][q_heads], or NULL: what the
  *                  backward pass takes.

@@ -55,7 +55,7 @@ constexpr float kSlack = 8.0f;
 template <int DP, bool DIST>
 using RowsTile = KeyTile<DP, kTileKeys, Pitch<DP>::kRows, Pitch<DP>::kColumns, DIST>;
 
-template <typename T, int DP, bool DIST, bool CAP>
+template <typename T, int DP, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_kernel(AttentionArgs a) {
     using F = typename Frag<T>::type;
     using Tile = RowsTile<DP, DIST>;
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
-    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     // distances on the matrix cores: the row's factors, what they leave for the
     // row, and the largest |b|^2 that any slope of the rows' heads allows
     int2 origin = make_int2(0, 0);
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         const float n = square_quanta(ax, ay), weight = slope2 / 256.0f;
         row_near = !a.lse && __all(!valid || near_enough(ax, ay, n, largest));
         const float units = CAP ? weight : weight / scale;
-        row_term = -units * n + (CAP ? cap2 : 0.0f);  // with the constant of tanh = 1 - 2 r
+        row_term = -units * n + (CAP ? cap_constant<CAP>(cap2) : 0.0f);  // with the constant of tanh = 1 - 2 r
         const NearSlots s = near_row(ax, ay, units);
         row_slots = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
     }
@@ -151,13 +151,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
             for (int st = 0; st < DP / 16; ++st)
                 s[u] = mfma(read_rows<T, Pitch<DP>::kRows>(t.k, first + 32 * u + col, st, h), q[st], s[u]);
         }
+        if (CAP) {
+#pragma unroll
+            for (int u = 0; u < SUBS; ++u) cap_parts<CAP>(s[u], scale);
+        }
         const float unit = PLAIN || (near && !CAP) ? scale : 1.0f;
         if (near && CAP) {
 #pragma unroll
             for (int u = 0; u < SUBS; ++u) {
                 const f32x16 term = near_term(t, first + 32 * u);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = __builtin_fmaf(-2.0f * cap2, tanh_part(s[u][r] * scale), term[r]);
+                for (int r = 0; r < 16; ++r) s[u][r] = capped<CAP>(s[u][r], cap2, term[r]);
             }
         } else if (!PLAIN && !near) {
 #pragma unroll
@@ -172,8 +176,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
-                        float th;
-                        s[u][r + e] = score<DIST, CAP>(s[u][r + e], scale, cap2, d2, slope2, th);
+                        s[u][r + e] = score<DIST, CAP>(s[u][r + e], scale, cap2, d2, slope2);
                     }
                 }
         }
@@ -306,7 +309,7 @@ constexpr int split_lds_bytes() {
     return join > tiles ? join : tiles;
 }
 
-template <typename T, int DP, bool DIST, bool CAP>
+template <typename T, int DP, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, DP == 128 && DIST && CAP ? 1 : 2) attention_split_kernel(AttentionArgs a) {
     using F = typename Frag<T>::type;
     constexpr int kRows = 32, kKeys = 128;
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && DIST && CAP ? 1 : 2) at
         qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
-    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
 
     f32x16 o[DP / 32] = {};
     float m = -INFINITY, shift = 0.0f, l = 0.0f;
@@ -390,6 +393,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && DIST && CAP ? 1 : 2) at
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) 
             s = mfma(read_rows<T, Pitch<DP>::kRows>(t.k, k0 + col, st, h), read_rows<T, Pitch<DP>::kRows>(q_lds, col, st, h), s);
+        if (CAP) cap_parts<CAP>(s, scale);
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             float kx[4], ky[4], pen[4] = {};
@@ -401,8 +405,7 @@ __global__ void __launch_bounds__(kThreads, DP == 128 && DIST && CAP ? 1 : 2) at
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float d2 = DIST ? distance2(qx - kx[e], qy - ky[e]) : 0.0f;
-                float th;
-                s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope2, th) + pen[e];
+                s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope2) + pen[e];
             }
         }
         if (kt + k0 + 32 > all_end) {
@@ -578,7 +581,8 @@ hipError_t launch_attention(AttentionArgs a, int32_t dtype, const AttentionPlan 
     hipError_t err = with_kernel(a, dtype, [&](auto t, auto dp, auto dist, auto cap) {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
-        constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
+        constexpr bool DIST = decltype(dist)::value;
+        constexpr int CAP = decltype(cap)::value;
         constexpr size_t rows_bytes = 2 * RowsTile<DP, DIST>::kBytes;
         const dim3 grid((uint32_t)(p.slots * a.kv_heads), (uint32_t)p.splits);
         if (p.split)

@@ -27,7 +27,7 @@ using DqTile = KeyTile<DP, DP <= 96 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRow
 // dS is rounded to the operands' type as a factor of the product with K: that
 // makes dq's error 2.7e-3 of its norm in bfloat16 where rounding dq alone costs
 // 1.7e-3.
-template <typename T, int DP, bool DIST, bool CAP>
+template <typename T, int DP, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && CAP) ? 1 : 2) attention_dq_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = DqTile<DP>;
@@ -77,7 +77,7 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
         qy = (float)place.y * kPxPerQuantum;
         slope2 = a.slopes[qh] * kLog2e;
     }
-    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     float shift, rest;
     split_lse(valid ? a.lse[qrow * a.q_heads + qh] : -INFINITY, shift, rest);
     const float rest_delta = delta * rest;
@@ -100,7 +100,8 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
             s = mfma(read_rows<T, Pitch<DP>::kBoth>(t.k, first + col, st, h), q[st], s);
             dp = mfma(read_rows<T, Pitch<DP>::kRows>(t.v, first + col, st, h), go[st], dp);
         }
-        float d2[DIST ? 16 : 1], th[CAP ? 16 : 1];
+        if (CAP) cap_parts<CAP>(s, scale);
+        float d2[DIST ? 16 : 1], of_cap[CAP ? 16 : 1];
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             float kx[4], ky[4];
@@ -111,7 +112,8 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 if (DIST) d2[r + e] = distance2(qx - kx[e], qy - ky[e]);
-                s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, DIST ? d2[r + e] : 0.0f, slope2, th[CAP ? r + e : 0]);
+                if (CAP) of_cap[r + e] = s[r + e];
+                s[r + e] = score<DIST, CAP>(s[r + e], scale, cap2, DIST ? d2[r + e] : 0.0f, slope2);
             }
         }
         if (hidden) {
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
                 sum_p_d2 = __builtin_fmaf(p, d2[r], sum_p_d2);
                 sum_ds_d2 = __builtin_fmaf(ds, d2[r], sum_ds_d2);
             }
-            if (CAP) ds *= tanh_slope(th[r]);
+            if (CAP) ds *= cap_slope<CAP>(of_cap[r]);
             s[r] = ds;
         }
 #pragma unroll
@@ -348,7 +350,7 @@ struct RowTile {
 // PFLOP/s of four products (VALU 43%, matrix cores 36%, LDS 41% of the time, a fifth
 // of that bank conflicts of rows that are read both ways); the phases of the two
 // waves a SIMD overlap only in part.
-template <typename T, int DP, int BLOCKS, bool DIST, bool CAP>
+template <typename T, int DP, int BLOCKS, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = RowTile<DP, DIST>;
@@ -407,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             keys_near = keys_near && __all(wave_key + 32 * n + col >= sp.nk || near_enough(bx, by, n2, largest));
         }
     }
-    const float scale = (CAP ? 2.0f * a.scale / a.cap : a.scale) * kLog2e, cap2 = a.cap * kLog2e;
+    const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     // the first query that sees the workgroup's first key
     int begin = 0;
@@ -443,6 +445,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
                 s = mfma(qf[st], k[n][st], s);
                 dp = mfma(gf[st], v[n][st], dp);
             }
+            if (CAP) cap_parts<CAP>(s, scale);
             if (near) {
                 const bf16x8 row = __builtin_bit_cast(bf16x8, t.near[h * kTileRows + first + col]);
                 f32x16 bias;
@@ -457,9 +460,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
                     for (int e = 0; e < 4; ++e) {
                         float d = dp[r + e] - delta[e];
                         if (CAP) {
-                            const float c = tanh_part(s[r + e] * scale);
-                            s[r + e] = exp2_fast(__builtin_fmaf(-2.0f * cap2, c, bias[r + e]) - shift[e]);
-                            d *= tanh_slope(c);
+                            d *= cap_slope<CAP>(s[r + e]);
+                            s[r + e] = exp2_fast(capped<CAP>(s[r + e], cap2, bias[r + e]) - shift[e]);
                         } else {
                             s[r + e] = exp2_fast(__builtin_fmaf(s[r + e], scale, -shift[e]));
                         }
@@ -480,11 +482,11 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float d2 = DIST ? distance2(x[e] - kx[n], y[e] - ky[n]) : 0.0f;
-                        float th;
-                        const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e], th);
-                        s[r + e] = exp2_fast(z - shift[e]);
-                        float d = s[r + e] * (dp[r + e] - delta[e]);
-                        if (CAP) d *= tanh_slope(th);
+                        const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e]);
+                        const float p = exp2_fast(z - shift[e]);
+                        float d = p * (dp[r + e] - delta[e]);
+                        if (CAP) d *= cap_slope<CAP>(s[r + e]);
+                        s[r + e] = p;
                         dp[r + e] = d;
                     }
                 }
@@ -525,7 +527,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             }
     };
 
-    const float units = CAP ? 1.0f : 1.0f / scale, constant = CAP ? cap2 : 0.0f;
+    const float units = CAP ? 1.0f : 1.0f / scale, constant = CAP ? cap_constant<CAP>(cap2) : 0.0f;
     Tile next;
     RowRun run(a, begin);
     if (begin < n_rows) {
@@ -620,7 +622,8 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
     hipError_t err = a.n_frames == 0 ? hipSuccess : with_kernel(a, dtype, [&](auto t, auto dp, auto dist, auto cap) {
         using T = decltype(t);
         constexpr int DP = decltype(dp)::value;
-        constexpr bool DIST = decltype(dist)::value, CAP = decltype(cap)::value;
+        constexpr bool DIST = decltype(dist)::value;
+        constexpr int CAP = decltype(cap)::value;
         hipError_t e = hipSuccess;
         if (a.total_q > 0) {
             constexpr size_t bytes = 2 * DqTile<DP>::kBytes;

@@ -38,10 +38,66 @@ __device__ __forceinline__ float across(float x, F &&f) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// r = 1 / (e^2x + 1) from 2 x log2 e: tanh x = 1 - 2 r, exact at both ends, and its
-// derivative 1 - tanh^2 x = 4 r (1 - r).
+// Caps, cap tanh(t / cap), in two forms.  Low ones: r = 1 / (e^2x + 1) from
+// 2 x log2 e, tanh x = 1 - 2 r, and its derivative 1 - tanh^2 x = 4 r (1 - r).  Small
+// scores are then differences of numbers as large as the cap, off by 1.5e-7 of it:
+// up to kLowCap that is 1e-5, what 32-bit sums of products leave them as well.
+// Higher caps take tanh itself, to 2.5e-7 of its size: below 1/2 the continued
+// fraction x / (1 + x^2 / (3 + x^2 / (5 + x^2 / 7))) (its next part is x^2 / 9: off by
+// 4e-8), 1 - 2 r above.  That costs a cap of 100 14% of a forward pass (64 x 2000: 1.10
+// -> 1.25 ms) and 8% of a training step (4.74 -> 5.13 ms).
+constexpr int kNoCap = 0, kLow = 1, kHigh = 2;
+constexpr float kLowCap = 64.0f;
+// A cap from here on changes no score by a rounding of it below 2^83.
+constexpr float kLargestCap = 0x1p96f;
 __device__ __forceinline__ float tanh_part(float x2) { return __builtin_amdgcn_rcpf(exp2_fast(x2) + 1.0f); }
-__device__ __forceinline__ float tanh_slope(float r) { return 4.0f * __builtin_fmaf(-r, r, r); }
+__device__ __forceinline__ float tanh_low(float x) {
+    const float n = x * x;
+    return x * __builtin_fmaf(10.0f, n, 105.0f) * __builtin_amdgcn_rcpf(__builtin_fmaf(n, n + 45.0f, 105.0f));
+}
+// What a score's gradient is multiplied by, from cap_parts below.
+template <int CAP>
+__device__ __forceinline__ float cap_slope(float r) {
+    return CAP == kLow ? 4.0f * __builtin_fmaf(-r, r, r) : __builtin_fmaf(-r, r, 1.0f);
+}
+// The parts of capped scores that their gradients take, from products and
+// score_scale(), and the score in units of log 2 from one; other may be added.
+template <int CAP>
+__device__ __forceinline__ void cap_parts(f32x16 &s, float scale) {
+    if (CAP == kLow) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = tanh_part(s[r] * scale);
+    } else if (CAP == kHigh) {
+        float most = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] *= scale;
+            most = fmaxf(most, fabsf(s[r]));
+        }
+        // where a high cap does its work no score comes near it
+        if (__all(most < 0.5f)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = tanh_low(s[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float high = __builtin_fmaf(-2.0f, tanh_part(s[r] * (2.0f * kLog2e)), 1.0f);
+                s[r] = fabsf(s[r]) < 0.5f ? tanh_low(s[r]) : high;
+            }
+        }
+    }
+}
+template <int CAP>
+__device__ __forceinline__ float capped(float r, float cap2, float other) {
+    return __builtin_fmaf(CAP == kLow ? -2.0f * cap2 : cap2, r, other);
+}
+template <int CAP>
+__device__ __forceinline__ float cap_constant(float cap2) { return CAP == kLow ? cap2 : 0.0f; }
+// What products are multiplied by first.
+template <int CAP>
+__device__ __forceinline__ float score_scale(const AttentionArgs &a) {
+    return CAP == kHigh ? a.scale / a.cap : (CAP == kLow ? 2.0f * a.scale / a.cap : a.scale) * kLog2e;
+}
 
 __device__ __forceinline__ int wave_max(int x) {
 #pragma unroll
@@ -431,19 +487,13 @@ __device__ __forceinline__ float4 read4(const float *p, int first, int r, int h)
 // Squared distance in px^2, and the scores in units of log 2 from a product of
 // queries and keys.  The products' order is written out, so that every kernel
 // gets the same bits: P = exp(s - lse) of the backward pass is then right even
-// where all of a query's keys are far and its scores are large (r: tanh_part of
-// t / cap, kept for the gradient).
+// where all of a query's keys are far and its scores are large.  With a cap, qk is
+// the product's cap_parts().
 __device__ __forceinline__ float distance2(float dx, float dy) { return __builtin_fmaf(dx, dx, dy * dy); }
 
-template <bool DIST, bool CAP>
-__device__ __forceinline__ float score(float qk, float scale, float cap2, float d2, float slope2, float &r) {
-    float s;
-    if (CAP) {
-        r = tanh_part(qk * scale);   // scale holds 2 log2 e scale / cap
-        s = __builtin_fmaf(-2.0f * cap2, r, cap2);
-    } else {
-        s = qk * scale;              // scale holds scale * log2 e
-    }
+template <bool DIST, int CAP>
+__device__ __forceinline__ float score(float qk, float scale, float cap2, float d2, float slope2) {
+    float s = CAP ? capped<CAP>(qk, cap2, cap_constant<CAP>(cap2)) : qk * scale;
     if (DIST) s = __builtin_fmaf(-slope2, d2, s);
     return s;
 }
@@ -471,11 +521,12 @@ __device__ __forceinline__ void split_lse(double lse, float &shift, float &rest)
 template <typename F>
 inline hipError_t with_kernel(const AttentionArgs &a, int32_t dtype, F &&fn) {
     auto flags = [&](auto t, auto dp) {
-        auto yes = std::true_type{};
-        auto no = std::false_type{};
-        const bool dist = a.slopes != nullptr, cap = a.cap > 0.0f;
-        if (dist) return cap ? fn(t, dp, yes, yes) : fn(t, dp, yes, no);
-        return cap ? fn(t, dp, no, yes) : fn(t, dp, no, no);
+        auto caps = [&](auto dist) {
+            if (a.cap == 0.0f || a.cap >= kLargestCap) return fn(t, dp, dist, std::integral_constant<int, kNoCap>{});
+            if (a.cap <= kLowCap) return fn(t, dp, dist, std::integral_constant<int, kLow>{});
+            return fn(t, dp, dist, std::integral_constant<int, kHigh>{});
+        };
+        return a.slopes != nullptr ? caps(std::true_type{}) : caps(std::false_type{});
     };
     auto dims = [&](auto t) {
         if (a.dim <= 32) return flags(t, std::integral_constant<int, 32>{});

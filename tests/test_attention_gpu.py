@@ -415,3 +415,42 @@ def test_places_and_lse_of_another_shape_are_refused():
     for wrong in (lse.t().contiguous(), lse.flatten()):
         with pytest.raises(ValueError, match="lse"):
             flock.attention_frames_backward(q, q, q, q, out, wrong, off)
+
+
+CAPS = [30.0, 64.0, 65.0, 1e3, 1e4, 1e5, 1e6, 1e9, 1e28, 3e38]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("distance", [False, True])
+@pytest.mark.parametrize("cap", CAPS)
+def test_caps_of_any_size(cap, distance, dtype):
+    """Scores far below their cap keep their digits (lse shows them)."""
+    counts = [300, 5]
+    compare(make(31, counts, counts, 2, 2, 64, dtype, distance=distance, cap=cap))
+
+
+@pytest.mark.parametrize("dim", [32, 96, 128])
+@pytest.mark.parametrize("cap", [100.0, 1e5])
+def test_high_caps_that_bite(cap, dim):
+    """Scores on both sides of half their cap, in every width."""
+    c = make(32 + dim, [150, 40], [150, 40], 4, 2, dim, torch.bfloat16, distance=dim != 96, cap=cap)
+    c["q"] = c["q"] / 8
+    c["scale"] = c["scale"] * cap  # scores around cap / 8, a few above half of it: the winner takes all
+    got = call(c)
+    want, bound = reference(c)
+    for n in ("out", "dq", "dk", "dv"):
+        assert torch.isfinite(got[n].float()).all(), n
+    # 32-bit scores: products off by 64 roundings of 2^-24 at most, tanh by 5
+    assert (got["lse"].cpu().double() - want["lse"]).abs().max() <= 2.0 ** -18 * cap
+
+
+@pytest.mark.parametrize("cap", CAPS)
+def test_caps_of_any_size_without_lse(cap):
+    """Inference on rows enough for tiles of 128, with distances."""
+    counts = [(53 * f) % 260 for f in range(80)]
+    c = make(34, counts, counts, 8, 4, 64, torch.float16, distance=True, sigma=(10.0, 300.0), cap=cap)
+    d = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in c.items()}
+    off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    got = flock.attention_frames(d["q"], d["k"], d["v"], off, q_xy=d["q_xy"], slopes=d["slopes"], cap=cap)
+    want, bound = reference(c, train=False)
+    ref.check(got, want["out"], bound["out"], "out")
