@@ -13,6 +13,28 @@ using namespace attention;
 // Backward
 // ---------------------------------------------------------------------------
 
+// dS as a factor of float16 needs a scale: it is about |grad_out| / keys, below the
+// type's normal numbers for ordinary gradients, and may pass its largest.  Each
+// output's sum has its own power of two, which starts at the largest and is lowered
+// to bring what passes 2^15 to 2^8, as a running maximum (gradients of 1e-4 over 2000
+// keys: error of dq 2.6e-2 -> 4.6e-3 of its norm, what rounding dq alone costs; a
+// training step on tracks takes 5% longer for it).
+constexpr float kFirstScale = 0x1p30f, kLargestFactor = 0x1p15f;
+constexpr int kScaleTo = 8;
+
+// The most of 16 factors, of both halves' lanes.
+__device__ __forceinline__ float most_of(const f32x16 &s) {
+    float most = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
+    return across(most, [](float x, float y) { return fmaxf(x, y); });
+}
+
+// What brings `most` to 2^kScaleTo if it is too large, or 1.
+__device__ __forceinline__ float scale_step(float most) {
+    return most > kLargestFactor ? __builtin_ldexpf(1.0f, kScaleTo - __builtin_amdgcn_frexp_expf(most)) : 1.0f;
+}
+
 // Heads of 128 leave registers for half as many keys in flight.
 template <int DP>
 using DqTile = KeyTile<DP, DP <= 96 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRows, false>;
@@ -80,7 +102,9 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
     const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     float shift, rest;
     split_lse(valid ? a.lse[qrow * a.q_heads + qh] : -INFINITY, shift, rest);
-    const float rest_delta = delta * rest;
+    // (dS carries its scale from here, and so do its sums)
+    constexpr bool SCALED = std::is_same_v<T, half_t>;
+    float ds_scale = SCALED ? kFirstScale : 1.0f;
     int wave_end = sp.nk, wave_all = sp.nk, end = sp.nk;
     if (a.causal) {
         wave_end = wave_max(limit);
@@ -94,6 +118,7 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
     // slope's gradient is rid of both, and the keys' gradients get the better delta.
     float sum_p = 0.0f, sum_ds = 0.0f, sum_p_d2 = 0.0f, sum_ds_d2 = 0.0f;
     auto sub_tile = [&](const typename Tile::Lds &t, int kt, int first, bool hidden, bool limited) {
+        const float rest_scale = rest * ds_scale, rest_delta = delta * rest_scale;
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
@@ -134,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float p = exp2_fast(s[r] - shift);  // P / rest; rest is in the other factors
-            float ds = p * __builtin_fmaf(dp[r], rest, -rest_delta);
+            float ds = p * __builtin_fmaf(dp[r], rest_scale, -rest_delta);
             if (DIST) {
                 sum_p += p;
                 sum_ds += ds;
@@ -143,6 +168,21 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
             }
             if (CAP) ds *= cap_slope<CAP>(of_cap[r]);
             s[r] = ds;
+        }
+        if (SCALED) {
+            const float most = most_of(s);
+            if (__any(most > kLargestFactor)) {
+                const float step = scale_step(most);
+                ds_scale *= step;
+                sum_ds *= step;
+                sum_ds_d2 *= step;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= step;
+#pragma unroll
+                for (int blk = 0; blk < DP / 32; ++blk)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dq[blk][r] *= step;
+            }
         }
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
@@ -182,12 +222,13 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
         if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes));
         __syncthreads();
     }
+    const float unscale = 1.0f / ds_scale;  // (a power of two)
     if (DIST) {
         auto add = [](float x, float y) { return x + y; };
         sum_p = across(sum_p, add);
-        sum_ds = across(sum_ds, add);
+        sum_ds = across(sum_ds, add) * unscale;
         sum_p_d2 = across(sum_p_d2, add);
-        sum_ds_d2 = across(sum_ds_d2, add);
+        sum_ds_d2 = across(sum_ds_d2, add) * unscale;
         float share = 0.0f;
         if (sum_p > 0.0f) {
             const float one = sum_p * rest, off = sum_ds / sum_p;
@@ -210,14 +251,15 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
     if (valid && h == 0) b.delta[qrow * a.q_heads + qh] = delta;
     if (!valid) return;
     T *out = static_cast<T *>(b.grad_q) + qrow * b.grad_q_stride + qh * a.dim;
+    const float out_scale = a.scale * unscale;
 #pragma unroll
     for (int blk = 0; blk < DP / 32; ++blk)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * blk + out_row(r, h);
             if (d < a.dim) {
-                const float z[4] = {dq[blk][r] * a.scale, dq[blk][r + 1] * a.scale, dq[blk][r + 2] * a.scale,
-                                    dq[blk][r + 3] * a.scale};
+                const float z[4] = {dq[blk][r] * out_scale, dq[blk][r + 1] * out_scale, dq[blk][r + 2] * out_scale,
+                                    dq[blk][r + 3] * out_scale};
                 store_pack<T, 4>(out + d, z);
             }
         }
@@ -227,7 +269,11 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
 // gradients and what their scores need, on its way to LDS as KeyTile is.
 constexpr int kTileRows = 64;
 
-template <int DP, bool NEAR>
+// Weights are carried as 2^kWeightBits P, which float16 holds to its last digit
+// down to P = 2^-28.
+template <typename T> constexpr float kWeightBits = std::is_same_v<T, half_t> ? 14.0f : 0.0f;
+
+template <typename T, int DP, bool NEAR>
 struct RowTile {
     static constexpr int kChunks = DP / 8;
     static constexpr int kLoads = kTileRows * kChunks / kThreads;
@@ -319,6 +365,7 @@ struct RowTile {
             }
             float shift, rest;
             split_lse(absent ? -INFINITY : lse, shift, rest);
+            shift -= kWeightBits<T>;
             lds.shift[threadIdx.x] = shift;
             if (NEAR) {
                 // the row's term of the distances goes with the shift
@@ -353,7 +400,7 @@ struct RowTile {
 template <typename T, int DP, int BLOCKS, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
-    using Tile = RowTile<DP, DIST>;
+    using Tile = RowTile<T, DP, DIST>;
     constexpr int kKeys = 128 * BLOCKS;
     const AttentionArgs &a = b.fwd;
     extern __shared__ char shared[];
@@ -417,6 +464,10 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         begin = (int)(max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows);
 
     f32x16 dk[BLOCKS][DP / 32] = {}, dv[BLOCKS][DP / 32] = {};
+    constexpr bool SCALED = std::is_same_v<T, half_t>;
+    float ds_scale[BLOCKS];  // beside that of the weights
+#pragma unroll
+    for (int n = 0; n < BLOCKS; ++n) ds_scale[n] = SCALED ? kFirstScale / 0x1p14f : 1.0f;
     auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact, bool near) {
         F qf[DP / 16], gf[DP / 16];
 #pragma unroll
@@ -425,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             gf[st] = read_rows<T, Tile::kPitch>(t.g, first + col, st, h);
         }
         // the columns are read here where registers allow it, to be there when the weights are
-        constexpr bool EARLY = DP <= 64 && !(DIST && CAP);
+        constexpr bool EARLY = DP <= 64 && !(DIST && (CAP || SCALED));
         F gc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1], qc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1];
         if (EARLY) {
 #pragma unroll
@@ -505,6 +556,21 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
                     dp[r] *= rest;
                 }
             }
+            if (SCALED) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] *= ds_scale[n];
+                const float most = most_of(dp);
+                if (__any(most > kLargestFactor)) {
+                    const float step = scale_step(most);
+                    ds_scale[n] *= step;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dp[r] *= step;
+#pragma unroll
+                    for (int blk = 0; blk < DP / 32; ++blk)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) dk[n][blk][r] *= step;
+                }
+            }
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 p[n][part] = round_frag<T>(s, part);
@@ -563,6 +629,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         const int64_t krow = sp.k0 + key;
         T *dk_out = static_cast<T *>(b.grad_k) + krow * b.grad_k_stride + head * a.dim;
         T *dv_out = static_cast<T *>(b.grad_v) + krow * b.grad_v_stride + head * a.dim;
+        constexpr float kUnweight = SCALED ? 0x1p-14f : 1.0f;
+        const float dk_scale = a.scale * kUnweight / ds_scale[n];
 #pragma unroll
         for (int blk = 0; blk < DP / 32; ++blk)
 #pragma unroll
@@ -573,8 +641,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
                     float x[4], y[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        x[e] = kept[n] ? dk[n][blk][r + e] * a.scale : 0.0f;
-                        y[e] = kept[n] ? dv[n][blk][r + e] : 0.0f;
+                        x[e] = kept[n] ? dk[n][blk][r + e] * dk_scale : 0.0f;
+                        y[e] = kept[n] ? dv[n][blk][r + e] * kUnweight : 0.0f;
                     }
                     store_pack<T, 4>(dk_out + d, x);
                     store_pack<T, 4>(dv_out + d, y);
@@ -633,7 +701,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
             if (e != hipSuccess) return e;
         }
         if (a.total_k > 0) {
-            constexpr size_t bytes = 2 * RowTile<DP, DIST>::kBytes;
+            constexpr size_t bytes = 2 * RowTile<T, DP, DIST>::kBytes;
             constexpr int kBlocks = 1;
             b.key_slots = (int64_t)a.total_k / (128 * kBlocks) + a.n_frames;
             auto kernel = attention_dkv_kernel<T, DP, kBlocks, DIST, CAP>;

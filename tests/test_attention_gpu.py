@@ -454,3 +454,52 @@ def test_caps_of_any_size_without_lse(cap):
     got = flock.attention_frames(d["q"], d["k"], d["v"], off, q_xy=d["q_xy"], slopes=d["slopes"], cap=cap)
     want, bound = reference(c, train=False)
     ref.check(got, want["out"], bound["out"], "out")
+
+
+def check_norms(got, want, dtype, names=("out", "dq", "dk", "dv")):
+    """Errors as norms: an output's own rounding, its factor's of 16 bits and its
+    other factors' (delta, weights) are three of one size at most, each on its
+    own: sqrt(3) of one, below 2."""
+    for n in names:
+        x = got[n].cpu().double()
+        assert torch.isfinite(x).all(), n
+        own = (want[n].to(dtype).double() - want[n]).norm()
+        error = (x - want[n]).norm()
+        assert error <= 2 * own, f"{n}: error {error / want[n].norm():.2e} of its norm, its rounding {own / want[n].norm():.2e}"
+
+
+@pytest.mark.parametrize("size", [1e3, 1.0, 1e-1, 1e-2, 1e-3, 1e-4])
+@pytest.mark.parametrize("flags", [dict(), dict(distance=True), dict(causal=True, prefix=[4]), dict(cap=5.0, hidden=0.2)])
+def test_float16_gradients_of_any_size(size, flags):
+    """dS over 2000 keys is far below the type's normal numbers."""
+    c = make(33, [2000], [2000], 2, 1, 64, torch.float16, **flags)
+    c["grad"] = (c["grad"].double() * size).half()
+    got = call(c)
+    want, _ = reference(c)
+    check_norms(got, want, torch.float16)
+
+
+def float16_factors_beyond_the_type(dim, distance):
+    """dS above 65504 in gradients that are not, and values that grow by 2^20
+    along the keys: each sum's scale comes down on its way."""
+    c = make(35, [3, 5], [3, 5], 2, 2, dim, torch.float16, distance=distance)
+    c["grad"] = (c["grad"].float() * 8000).half()
+    c["q"], c["k"] = c["q"] / 64, c["k"] / 64
+    got = call(c)
+    want, _ = reference(c)
+    check_norms(got, want, torch.float16)
+    c = make(36, [500], [500], 1, 1, dim, torch.float16, distance=distance)
+    c["v"] = (c["v"].double() * 2.0 ** (20.0 * torch.arange(500)[:, None, None] / 500 - 12)).half()
+    got = call(c)
+    want, _ = reference(c)
+    check_norms(got, want, torch.float16, ("out", "dq", "dv"))
+    c = make(37, [500], [500], 1, 1, dim, torch.float16, distance=distance)
+    c["grad"] = (c["grad"].double() * 2.0 ** (20.0 * torch.arange(500)[:, None, None] / 500 - 12)).half()
+    got = call(c)
+    want, _ = reference(c)
+    check_norms(got, want, torch.float16, ("out", "dk", "dv"))
+
+
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_float16_factors_beyond_the_type(dim):
+    float16_factors_beyond_the_type(dim, distance=False)
