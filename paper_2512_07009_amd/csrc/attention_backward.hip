@@ -13,13 +13,17 @@ using namespace attention;
 // Backward
 // ---------------------------------------------------------------------------
 
-// dS as a factor of float16 needs a scale: it is about |grad_out| / keys, below the
-// type's normal numbers for ordinary gradients, and may pass its largest.  Each
-// output's sum has its own power of two, which starts at the largest and is lowered
-// to bring what passes 2^15 to 2^8, as a running maximum (gradients of 1e-4 over 2000
-// keys: error of dq 2.6e-2 -> 4.6e-3 of its norm, what rounding dq alone costs; a
-// training step on tracks takes 5% longer for it).
-constexpr float kFirstScale = 0x1p30f, kLargestFactor = 0x1p15f;
+// dS and P as factors of float16 need a scale: dS is about |grad_out| / keys, below
+// the type's normal numbers for ordinary gradients, and may pass its largest.  They
+// are carried times 2^14, which holds P and dS to their last digit down to 2^-28, and
+// each output's sum of dS has a power of two of its own, lowered as for a running
+// maximum: what passes 2^15 is brought to 2^8 (gradients of 1e-4 over 2000 keys: error of
+// dq 2.6e-2 -> 4.6e-3 of its norm, what rounding dq alone costs; a training step on
+// tracks takes 4% longer for it).
+template <typename T> constexpr bool kScaled = std::is_same_v<T, half_t>;
+template <typename T> constexpr float kFactorBits = kScaled<T> ? 14.0f : 0.0f;
+template <typename T> constexpr float kFactorScale = kScaled<T> ? 0x1p14f : 1.0f;
+constexpr float kLargestFactor = 0x1p15f;
 constexpr int kScaleTo = 8;
 
 // The most of 16 factors, of both halves' lanes.
@@ -103,8 +107,7 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
     float shift, rest;
     split_lse(valid ? a.lse[qrow * a.q_heads + qh] : -INFINITY, shift, rest);
     // (dS carries its scale from here, and so do its sums)
-    constexpr bool SCALED = std::is_same_v<T, half_t>;
-    float ds_scale = SCALED ? kFirstScale : 1.0f;
+    float ds_scale = kFactorScale<T>;
     int wave_end = sp.nk, wave_all = sp.nk, end = sp.nk;
     if (a.causal) {
         wave_end = wave_max(limit);
@@ -112,18 +115,31 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
         end = seen_limit(a, sp, prefix, run.query(a, min(kRows, n_rows - row0) - 1));
     }
 
-    f32x16 dq[DP / 32] = {};
-    // sums of P, dS, P d2 and dS d2.  P sums to one but for the rounding of lse, and
-    // dS to zero but for that of delta (it comes from the rounded output); the
-    // slope's gradient is rid of both, and the keys' gradients get the better delta.
-    float sum_p = 0.0f, sum_ds = 0.0f, sum_p_d2 = 0.0f, sum_ds_d2 = 0.0f;
-    auto sub_tile = [&](const typename Tile::Lds &t, int kt, int first, bool hidden, bool limited) {
+    // delta comes from the rounded output, and where the weights are sharp, dP - delta
+    // is small for the keys that have them: with scores eight times normal ones dq's
+    // error is 5.0e-3 of its norm in bfloat16, and 2.4e-3 with the right delta.  The sum
+    // of dS, which should be zero, is what delta is off by: the keys' gradients take
+    // the right one, and dq gets that much of P K taken off.  P K is summed on the way,
+    // beside dq (training steps 2 to 8%), but for wide heads that it would leave one wave
+    // a SIMD (without distances or caps; heads of 128: 1.47 -> 2.03 ms).  Their keys are
+    // gone over again, in workgroups that have a row where it matters: delta's error
+    // above a quarter of a factor's rounding (1.49 ms where none has).
+    constexpr bool SUMMED = DP <= 64 || DIST || (DP == 128 && CAP);
+    constexpr float kTolerated = kScaled<T> ? 0x1p-13f : 0x1p-10f;
+    f32x16 dq[DP / 32] = {}, pk[SUMMED ? DP / 32 : 1] = {};
+    float off = 0.0f;  // what delta is off by, times rest
+    // sums of P, dS, its size, P d2 and dS d2.  P sums to one but for the rounding of
+    // lse; the slope's gradient is rid of that and of delta's error.
+    float sum_p = 0.0f, sum_ds = 0.0f, size_ds = 0.0f, sum_p_d2 = 0.0f, sum_ds_d2 = 0.0f;
+    // (AGAIN: the keys once more, for P K alone)
+    auto sub_tile = [&](auto again, const typename Tile::Lds &t, int kt, int first, bool hidden, bool limited) {
+        constexpr bool AGAIN = decltype(again)::value;
         const float rest_scale = rest * ds_scale, rest_delta = delta * rest_scale;
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int st = 0; st < DP / 16; ++st) {
             s = mfma(read_rows<T, Pitch<DP>::kBoth>(t.k, first + col, st, h), q[st], s);
-            dp = mfma(read_rows<T, Pitch<DP>::kRows>(t.v, first + col, st, h), go[st], dp);
+            if (!AGAIN) dp = mfma(read_rows<T, Pitch<DP>::kRows>(t.v, first + col, st, h), go[st], dp);
         }
         if (CAP) cap_parts<CAP>(s, scale);
         float d2[DIST ? 16 : 1], of_cap[CAP ? 16 : 1];
@@ -159,22 +175,29 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const float p = exp2_fast(s[r] - shift);  // P / rest; rest is in the other factors
-            float ds = p * __builtin_fmaf(dp[r], rest_scale, -rest_delta);
+            const float slope = CAP ? cap_slope<CAP>(of_cap[r]) : 1.0f;
+            if (AGAIN) {
+                s[r] = -off * (CAP ? p * slope : p);
+                continue;
+            }
+            const float ds = p * __builtin_fmaf(dp[r], rest_scale, -rest_delta);
+            sum_ds += ds;
+            if (!SUMMED) size_ds += fabsf(ds);
             if (DIST) {
                 sum_p += p;
-                sum_ds += ds;
                 sum_p_d2 = __builtin_fmaf(p, d2[r], sum_p_d2);
                 sum_ds_d2 = __builtin_fmaf(ds, d2[r], sum_ds_d2);
             }
-            if (CAP) ds *= cap_slope<CAP>(of_cap[r]);
-            s[r] = ds;
+            s[r] = CAP ? ds * slope : ds;
+            if (SUMMED) dp[r] = CAP ? p * slope : p;
         }
-        if (SCALED) {
+        if (kScaled<T> && !AGAIN) {
             const float most = most_of(s);
             if (__any(most > kLargestFactor)) {
                 const float step = scale_step(most);
                 ds_scale *= step;
                 sum_ds *= step;
+                size_ds *= step;
                 sum_ds_d2 *= step;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] *= step;
@@ -187,53 +210,61 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             const F d = round_frag<T>(s, part);
+            F p;
+            if (SUMMED) p = round_frag<T>(dp, part);
 #pragma unroll
-            for (int blk = 0; blk < DP / 32; ++blk)
-                dq[blk] = mfma(read_columns<T, Pitch<DP>::kBoth>(t.k, first + 16 * part, blk, lane), d, dq[blk]);
+            for (int blk = 0; blk < DP / 32; ++blk) {
+                const F k = read_columns<T, Pitch<DP>::kBoth>(t.k, first + 16 * part, blk, lane);
+                dq[blk] = mfma(k, d, dq[blk]);
+                if (SUMMED) pk[blk] = mfma(k, p, pk[blk]);
+            }
         }
     };
 
-    Tile next(a);
-    if (end > 0) {
-        next.look_up(a, sp, 0, end);
-        next.template load<DIST>(a, sp, head, 0, end);
-        next.look_up(a, sp, kKeys, end);
-        next.template store<DIST>(a, typename Tile::Lds(shared));
-    }
-    wait_for_loads();
-    __syncthreads();
-    int buffer = 0;
-    for (int kt = 0; kt < end; kt += kKeys) {
-        const bool more = kt + kKeys < end;
-        if (more) {
-            next.template load<DIST>(a, sp, head, kt + kKeys, end);
-            next.look_up(a, sp, kt + 2 * kKeys, end);
+    auto over_keys = [&](auto again) {
+        Tile next(a);
+        if (end > 0) {
+            next.look_up(a, sp, 0, end);
+            next.template load<DIST>(a, sp, head, 0, end);
+            next.look_up(a, sp, kKeys, end);
+            next.template store<DIST>(a, typename Tile::Lds(shared));
         }
-        const typename Tile::Lds t(shared + buffer * Tile::kBytes);
-        const uint64_t seen = *t.seen;
-        if (kt < wave_end) {
-#pragma unroll(DP <= 64 ? 2 : 1)
-            for (int sub = 0; sub < kKeys / 32; ++sub) {
-                const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
-                if (bits != 0) sub_tile(t, kt, 32 * sub, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
-            }
-        }
-        buffer ^= 1;
-        if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes));
+        wait_for_loads();
         __syncthreads();
-    }
+        int buffer = 0;
+        for (int kt = 0; kt < end; kt += kKeys) {
+            const bool more = kt + kKeys < end;
+            if (more) {
+                next.template load<DIST>(a, sp, head, kt + kKeys, end);
+                next.look_up(a, sp, kt + 2 * kKeys, end);
+            }
+            const typename Tile::Lds t(shared + buffer * Tile::kBytes);
+            const uint64_t seen = *t.seen;
+            if (kt < wave_end) {
+#pragma unroll(DP <= 64 ? 2 : 1)
+                for (int sub = 0; sub < kKeys / 32; ++sub) {
+                    const uint32_t bits = __builtin_amdgcn_readfirstlane((uint32_t)(seen >> (32 * sub)));
+                    if (bits != 0) sub_tile(again, t, kt, 32 * sub, bits != 0xffffffffu, kt + 32 * sub + 32 > wave_all);
+                }
+            }
+            buffer ^= 1;
+            if (more) next.template store<DIST>(a, typename Tile::Lds(shared + buffer * Tile::kBytes));
+            __syncthreads();
+        }
+    };
+    over_keys(std::false_type{});
     const float unscale = 1.0f / ds_scale;  // (a power of two)
+    auto add = [](float x, float y) { return x + y; };
+    sum_ds = across(sum_ds, add) * unscale;
+    off = sum_ds * rest;
     if (DIST) {
-        auto add = [](float x, float y) { return x + y; };
         sum_p = across(sum_p, add);
-        sum_ds = across(sum_ds, add) * unscale;
         sum_p_d2 = across(sum_p_d2, add);
         sum_ds_d2 = across(sum_ds_d2, add) * unscale;
         float share = 0.0f;
         if (sum_p > 0.0f) {
-            const float one = sum_p * rest, off = sum_ds / sum_p;
-            share = (off * sum_p_d2 - sum_ds_d2) / one;
-            delta += off / rest;
+            off = sum_ds / sum_p;
+            share = (off * sum_p_d2 - sum_ds_d2) / (sum_p * rest);
         }
         if (shares) {
             // the tiles in LDS are done with; rows of a head are added in their order
@@ -246,20 +277,41 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
                     sum += rows[r];
                 shares[g] = sum;
             }
+            __syncthreads();
         }
     }
-    if (valid && h == 0) b.delta[qrow * a.q_heads + qh] = delta;
+    if (valid && h == 0) b.delta[qrow * a.q_heads + qh] = rest > 0.0f ? delta + off / rest : delta;
+    if (!SUMMED) {
+        size_ds = across(size_ds, add) * unscale;
+        if (__syncthreads_or(fabsf(sum_ds) > kTolerated * size_ds)) {
+            off *= ds_scale;
+            if (kScaled<T>) {
+                const float step = scale_step(fabsf(off));
+                off *= step;
+                ds_scale *= step;
+#pragma unroll
+                for (int blk = 0; blk < DP / 32; ++blk)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dq[blk][r] *= step;
+            }
+            over_keys(std::true_type{});
+        }
+    }
     if (!valid) return;
     T *out = static_cast<T *>(b.grad_q) + qrow * b.grad_q_stride + qh * a.dim;
-    const float out_scale = a.scale * unscale;
+    const float out_scale = a.scale / ds_scale, off_scale = a.scale * off;
 #pragma unroll
     for (int blk = 0; blk < DP / 32; ++blk)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
             const int d = 32 * blk + out_row(r, h);
             if (d < a.dim) {
-                const float z[4] = {dq[blk][r] * out_scale, dq[blk][r + 1] * out_scale, dq[blk][r + 2] * out_scale,
-                                    dq[blk][r + 3] * out_scale};
+                float z[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    z[e] = dq[blk][r + e] * out_scale;
+                    if (SUMMED) z[e] -= pk[blk][r + e] * off_scale;
+                }
                 store_pack<T, 4>(out + d, z);
             }
         }
@@ -268,10 +320,6 @@ __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && 
 // A tile of 64 rows (queries of the heads that share a kv head), their output
 // gradients and what their scores need, on its way to LDS as KeyTile is.
 constexpr int kTileRows = 64;
-
-// Weights are carried as 2^kWeightBits P, which float16 holds to its last digit
-// down to P = 2^-28.
-template <typename T> constexpr float kWeightBits = std::is_same_v<T, half_t> ? 14.0f : 0.0f;
 
 template <typename T, int DP, bool NEAR>
 struct RowTile {
@@ -365,7 +413,7 @@ struct RowTile {
             }
             float shift, rest;
             split_lse(absent ? -INFINITY : lse, shift, rest);
-            shift -= kWeightBits<T>;
+            shift -= kFactorBits<T>;  // the weights' scale
             lds.shift[threadIdx.x] = shift;
             if (NEAR) {
                 // the row's term of the distances goes with the shift
@@ -464,10 +512,10 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         begin = (int)(max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows);
 
     f32x16 dk[BLOCKS][DP / 32] = {}, dv[BLOCKS][DP / 32] = {};
-    constexpr bool SCALED = std::is_same_v<T, half_t>;
     float ds_scale[BLOCKS];  // beside that of the weights
+    bool lowered = false;    // any lane's
 #pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) ds_scale[n] = SCALED ? kFirstScale / 0x1p14f : 1.0f;
+    for (int n = 0; n < BLOCKS; ++n) ds_scale[n] = 1.0f;
     auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact, bool near) {
         F qf[DP / 16], gf[DP / 16];
 #pragma unroll
@@ -476,7 +524,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             gf[st] = read_rows<T, Tile::kPitch>(t.g, first + col, st, h);
         }
         // the columns are read here where registers allow it, to be there when the weights are
-        constexpr bool EARLY = DP <= 64 && !(DIST && (CAP || SCALED));
+        constexpr bool EARLY = DP <= 64 && !(DIST && (CAP || kScaled<T>));
         F gc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1], qc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1];
         if (EARLY) {
 #pragma unroll
@@ -556,11 +604,14 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
                     dp[r] *= rest;
                 }
             }
-            if (SCALED) {
+            if (kScaled<T>) {
+                if (lowered) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) dp[r] *= ds_scale[n];
+                    for (int r = 0; r < 16; ++r) dp[r] *= ds_scale[n];
+                }
                 const float most = most_of(dp);
                 if (__any(most > kLargestFactor)) {
+                    lowered = true;
                     const float step = scale_step(most);
                     ds_scale[n] *= step;
 #pragma unroll
@@ -629,8 +680,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         const int64_t krow = sp.k0 + key;
         T *dk_out = static_cast<T *>(b.grad_k) + krow * b.grad_k_stride + head * a.dim;
         T *dv_out = static_cast<T *>(b.grad_v) + krow * b.grad_v_stride + head * a.dim;
-        constexpr float kUnweight = SCALED ? 0x1p-14f : 1.0f;
-        const float dk_scale = a.scale * kUnweight / ds_scale[n];
+        constexpr float kUnscale = 1.0f / kFactorScale<T>;
+        const float dk_scale = a.scale * kUnscale / ds_scale[n];
 #pragma unroll
         for (int blk = 0; blk < DP / 32; ++blk)
 #pragma unroll
@@ -642,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         x[e] = kept[n] ? dk[n][blk][r + e] * dk_scale : 0.0f;
-                        y[e] = kept[n] ? dv[n][blk][r + e] * kUnweight : 0.0f;
+                        y[e] = kept[n] ? dv[n][blk][r + e] * kUnscale : 0.0f;
                     }
                     store_pack<T, 4>(dk_out + d, x);
                     store_pack<T, 4>(dv_out + d, y);

@@ -503,3 +503,38 @@ def float16_factors_beyond_the_type(dim, distance):
 @pytest.mark.parametrize("dim", [32, 64, 96, 128])
 def test_float16_factors_beyond_the_type(dim):
     float16_factors_beyond_the_type(dim, distance=False)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("flags", [dict(), dict(distance=True), dict(cap=20.0, causal=True), dict(hidden=0.3)])
+@pytest.mark.parametrize("sharp", [1, 2, 4, 8])
+def test_errors_of_flat_and_sharp_weights(dtype, dim, flags, sharp):
+    """Gradients keep their digits however sharp the weights are, with and
+    without distances (delta as the rounded output gives it is not enough)."""
+    counts = [300, 3, 40]
+    c = make(32, counts, counts, 4, 2, dim, dtype, **flags)
+    c["q"] = c["q"] * sharp
+    got = call(c)
+    want, _ = reference(c)
+    check_norms(got, want, dtype)
+
+
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_float16_factors_beyond_the_type_with_distances(dim):
+    """(So few birds that the weights are sharp.)"""
+    float16_factors_beyond_the_type(dim, distance=True)
+
+
+@pytest.mark.parametrize("dim", [96, 128])
+def test_workgroups_with_and_without_sharp_rows(dim):
+    """One sharp row sends a workgroup of wide heads over its keys again, the
+    others of its rows and other workgroups being flat."""
+    c = make(38, [700], [700], 2, 2, dim, torch.float16)
+    c["q"][200] = c["q"][200] * 30
+    got = call(c)
+    want, _ = reference(c)
+    check_norms(got, want, torch.float16)
+    row = (got["dq"][200].cpu().double() - want["dq"][200]).norm()
+    # three errors of at most 2^-11 of the row's size (its own, its factor's, its weights')
+    assert row <= 3 * 2.0 ** -11 * want["dq"][200].norm()
