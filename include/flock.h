@@ -470,7 +470,11 @@ flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const
  * 0) features are not read.  What order alone hides must be finite.
  * slopes = 1 / (2 sigma^2) weighs keys by the Gaussian that density_frames
  * adds per bird.  Products take 16-bit factors with 32-bit sums; the softmax
- * is in 32 bits, its weights rounded to dtype for the product with v.
+ * is in 32 bits, its weights rounded to dtype for the product with v.  A score's
+ * distance may be a product of bfloat16 parts (without lse, and for the
+ * gradients of k and v): that leaves a weight off by at most 7e-4 of itself in
+ * bfloat16 and 2.5e-4 in float16, below its rounding.  With lse, and for the
+ * gradient of q, distances are differences in 32 bits.
  *
  * Arguments:
  *   dtype          FLOCK_F16 or FLOCK_BF16.

@@ -255,13 +255,15 @@ __device__ __forceinline__ uint32_t seen_bits(uint32_t bits, int limit, int firs
 // queries and keys: 16 products of bfloat16 parts (8 bits each) that hold x, y
 // (two parts, whole numbers of 1/16 px below 2^16), |b|^2 and the slope's factors
 // (three parts) to 2^-24.  That takes five vector operations off each score,
-// where they bound the kernels (training step 64 x 2000: 4.18 -> 3.70 ms, 24 x 8000:
-// 9.4 -> 8.7 ms).  The sums pass through numbers as large as slope |b|^2, so scores
-// are off by 2^-22 of that.  near_limit (in units of log 2) keeps the weights'
-// relative error below a fifth of what rounding them to the operands' type costs
-// (7e-4 of 4e-3 in bfloat16, 2.5e-4 of 5e-4 at worst in float16), and tiles with a
-// bird farther away take the differences themselves; so does a forward pass that
-// writes lse, which is exact to 32 bits.
+// where they bound the kernels (64 x 2000 without lse 1.07 -> 0.87 ms, 24 x 8000 9.6 ->
+// 8.9 ms, a training step, in the keys' gradients, 4.08 -> 3.90).  The sums pass
+// through numbers as large as slope |b|^2, so scores are off by 2^-22 of that.
+// near_limit (in units of log 2) keeps the weights' relative error below what
+// rounding them to the operands' type costs (at worst 7e-4 of 4e-3 in bfloat16,
+// 2.5e-4 of 5e-4 in float16; the outputs' errors are the same to three digits with it
+// and without), and tiles with a bird farther away take the differences themselves.
+// So do a forward pass that writes lse, which is exact to 32 bits, and the queries'
+// gradients, whose sums of dS show what delta is off by.
 template <typename T> constexpr float near_limit() { return 4096.0f; }
 template <> constexpr float near_limit<half_t>() { return 1536.0f; }
 constexpr int kNearReach = 1 << 15;

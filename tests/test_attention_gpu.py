@@ -538,3 +538,27 @@ def test_workgroups_with_and_without_sharp_rows(dim):
     row = (got["dq"][200].cpu().double() - want["dq"][200]).norm()
     # three errors of at most 2^-11 of the row's size (its own, its factor's, its weights')
     assert row <= 3 * 2.0 ** -11 * want["dq"][200].norm()
+
+
+@pytest.mark.parametrize("dtype,limit", [(torch.bfloat16, 4096), (torch.float16, 1536)])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("share", [0.5, 0.95, 1.05])
+def test_distances_at_the_limit_of_products(dtype, limit, cap, share):
+    """Birds of two far spots, with slopes that make the products of the distances
+    as large as they may be (and just larger, where differences are taken): what
+    they leave a weight off by stays below what rounding costs."""
+    counts = [200 - f % 7 for f in range(80)]
+    c = make(39, counts, counts, 8, 4, 64, dtype, distance=True, cap=cap)
+    gen = torch.Generator().manual_seed(40)
+    n = sum(counts)
+    sigma = 8.0
+    c["slopes"] = torch.full((8,), 0.5 / sigma ** 2)
+    reach = math.sqrt(share * limit / (float(c["slopes"][0]) * math.log2(math.e)))  # px
+    spot = (torch.arange(n) % 2)[:, None] * torch.tensor([2 * reach, 0.0])
+    c["q_xy"] = c["k_xy"] = ((spot + 40 + sigma * torch.randn(n, 2, generator=gen)) * 16).int()
+    want, _ = reference(c)
+    check_norms(call(c), want, dtype, ("out", "dq", "dk", "dv"))
+    d = {k: (t.cuda() if torch.is_tensor(t) else t) for k, t in c.items()}
+    off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    out = flock.attention_frames(d["q"], d["k"], d["v"], off, q_xy=d["q_xy"], slopes=d["slopes"], cap=cap)
+    check_norms({"out": out}, want, dtype, ("out",))
