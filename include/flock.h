@@ -481,7 +481,9 @@ flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const
  *   q, k, v        device in, [total_q][q_heads][head_dim] and
  *                  [total_k][kv_heads][head_dim], 16-byte aligned, strides
  *                  multiples of 8 below 2^24.
- *   n_frames       frames of both batches.
+ *   n_frames       frames of both batches.  A batch whose tiles (of 32 or 128 rows
+ *                  or keys of a frame and kv head) are 2^24 or more may be refused
+ *                  (FLOCK_EUNSUPPORTED).
  *   q_offsets, k_offsets   device in, int32[n_frames + 1] each; the same array
  *                  where the birds of a frame attend to each other.
  *   q_heads, kv_heads      1 .. 256, q_heads a multiple of kv_heads.

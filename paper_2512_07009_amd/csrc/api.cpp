@@ -807,11 +807,16 @@ flock_status check_attention_pointers(const flock::AttentionArgs &a) {
     if (!aligned(a.q_offsets, 4) || !aligned(a.k_offsets, 4) || !aligned(a.slopes, 4) || !aligned(a.prefix, 4))
         return fail(FLOCK_EINVAL, "q_offsets, k_offsets, slopes and prefix must be 4-byte aligned");
     if (!aligned(a.lse, 8)) return fail(FLOCK_EINVAL, "lse must be 8-byte aligned");
-    // rows are numbered in 31 bits, tiles in a launch's grid
-    if ((int64_t)a.total_q * a.group > 0x7fffff00LL ||
-        ((int64_t)a.total_q * a.group / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL ||
-        ((int64_t)a.total_k / 32 + a.n_frames) * a.kv_heads > 0x7fffffffLL)
-        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 rows or tiles");
+    // rows are numbered in 31 bits
+    if ((int64_t)a.total_q * a.group > 0x7fffff00LL)
+        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 rows of queries and shared heads");
+    return FLOCK_OK;
+}
+
+flock_status check_workgroups(int64_t n) {
+    if (n > flock::kMaxWorkgroups)
+        return fail(FLOCK_EUNSUPPORTED, "batch of %lld workgroups, more than a launch's %lld: split its frames", (long long)n,
+                    (long long)flock::kMaxWorkgroups);
     return FLOCK_OK;
 }
 
@@ -1052,6 +1057,9 @@ flock_status attention_frames(int32_t dtype, const void *q, int64_t q_stride, co
     if (n_frames == 0 || total_q == 0) return FLOCK_OK;
     st = check_attention_pointers(a);
     if (st != FLOCK_OK) return st;
+    const flock::AttentionPlan plan = flock::plan_attention(n_frames, total_q, total_k, q_heads, kv_heads, device_cus());
+    st = check_workgroups(flock::attention_workgroups(plan, total_q, q_heads, kv_heads));
+    if (st != FLOCK_OK) return st;
     const DeviceInfo *dev = nullptr;
     st = device_info(&dev);
     if (st != FLOCK_OK) return st;
@@ -1060,7 +1068,6 @@ flock_status attention_frames(int32_t dtype, const void *q, int64_t q_stride, co
         st = validate_attention(a, s);
         if (st != FLOCK_OK) return st;
     }
-    const flock::AttentionPlan plan = flock::plan_attention(n_frames, total_q, total_k, q_heads, kv_heads, dev->n_cus);
     Workspace ws;
     st = ws.take(workspace, workspace_bytes, flock::attention_workspace_bytes(plan, total_q, q_heads, head_dim), s);
     if (st != FLOCK_OK) return st;
@@ -1141,6 +1148,8 @@ flock_status attention_frames_backward(
     if (!aligned(grad_out, 16) || !aligned(grad_q, 16) || !aligned(grad_k, 16) || !aligned(grad_v, 16))
         return fail(FLOCK_EINVAL, "grad_out, grad_q, grad_k and grad_v must be 16-byte aligned");
     if (!aligned(grad_slopes, 4)) return fail(FLOCK_EINVAL, "grad_slopes must be 4-byte aligned");
+    st = check_workgroups(flock::attention_backward_workgroups(n_frames, total_q, total_k, q_heads, kv_heads));
+    if (st != FLOCK_OK) return st;
     const DeviceInfo *dev = nullptr;
     st = device_info(&dev);
     if (st != FLOCK_OK) return st;

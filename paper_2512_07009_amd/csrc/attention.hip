@@ -562,6 +562,11 @@ AttentionPlan plan_attention(int32_t n_frames, int32_t total_q, int32_t total_k,
     return p;
 }
 
+int64_t attention_workgroups(const AttentionPlan &p, int32_t total_q, int32_t q_heads, int32_t kv_heads) {
+    const int64_t joins = p.splits > 1 ? ((int64_t)total_q * q_heads + 3) / 4 : 0;
+    return std::max(p.slots * kv_heads, joins);
+}
+
 size_t attention_workspace_bytes(const AttentionPlan &p, int32_t total_q, int32_t q_heads, int32_t dim) {
     if (p.splits <= 1) return 0;
     const size_t all = (size_t)total_q * (size_t)q_heads * (size_t)p.splits;

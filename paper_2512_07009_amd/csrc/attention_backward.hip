@@ -717,10 +717,15 @@ __global__ void __launch_bounds__(1024) slope_total_kernel(const float *shares, 
     if (threadIdx.x == 0) grad_slopes[blockIdx.x] = (float)sums[0];
 }
 
-// Numbers of row tiles of the queries' gradients.
+// Numbers of row tiles of the queries' gradients, of key tiles of the keys'.
 int64_t backward_slots(int32_t n_frames, int32_t total_q, int group) { return (int64_t)total_q * group / 128 + n_frames; }
+int64_t backward_key_slots(int32_t n_frames, int32_t total_k) { return (int64_t)total_k / 128 + n_frames; }
 
 }  // namespace
+
+int64_t attention_backward_workgroups(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads, int32_t kv_heads) {
+    return std::max(backward_slots(n_frames, total_q, q_heads / kv_heads), backward_key_slots(n_frames, total_k)) * kv_heads;
+}
 
 size_t attention_backward_workspace_bytes(int32_t n_frames, int32_t total_q, int32_t q_heads, int32_t kv_heads) {
     if (n_frames <= 0 || total_q < 0 || q_heads <= 0 || kv_heads <= 0) return 0;
@@ -754,7 +759,7 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
         if (a.total_k > 0) {
             constexpr size_t bytes = 2 * RowTile<T, DP, DIST>::kBytes;
             constexpr int kBlocks = 1;
-            b.key_slots = (int64_t)a.total_k / (128 * kBlocks) + a.n_frames;
+            b.key_slots = backward_key_slots(a.n_frames, a.total_k);
             auto kernel = attention_dkv_kernel<T, DP, kBlocks, DIST, CAP>;
             hipLaunchKernelGGL(kernel, dim3((uint32_t)(b.key_slots * a.kv_heads)), dim3(kThreads), bytes, stream, b);
             e = hipGetLastError();

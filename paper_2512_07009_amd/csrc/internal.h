@@ -241,6 +241,9 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);
 
+// Threads of a launch are numbered in 32 bits: workgroups of 256 that one holds.
+constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;
+
 constexpr int kAttentionMaxDim = 128;
 // 64 rows lie within 2^31 bytes: a tile's loads go through resources of 64 rows at most
 constexpr int64_t kAttentionMaxStride = (1 << 24) - 8;
@@ -285,6 +288,9 @@ struct AttentionBackwardArgs {
     float *delta, *slope_shares;       // set by launch_attention_backward: [total_q][q_heads], [slots][q_heads]
     int64_t key_slots;
 };
+// Workgroups of the largest launch, for kMaxWorkgroups.
+int64_t attention_workgroups(const AttentionPlan &p, int32_t total_q, int32_t q_heads, int32_t kv_heads);
+int64_t attention_backward_workgroups(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads, int32_t kv_heads);
 size_t attention_backward_workspace_bytes(int32_t n_frames, int32_t total_q, int32_t q_heads, int32_t kv_heads);
 hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, void *workspace, float *grad_slopes,
                                      hipStream_t stream);

@@ -5,6 +5,7 @@ import ctypes
 import math
 
 import pytest
+import torch
 
 from paper_2512_07009_amd import binding
 
@@ -143,3 +144,33 @@ def test_workspace_queries():
     assert lib.attention_frames_workspace(1, 1, 9000, 8, 2, 64) > 0
     assert lib.attention_frames_backward_workspace(64, 128000, 128000, 8, 8, 64) >= 128000 * 8 * 4
     assert lib.attention_frames_backward_workspace(0, 0, 0, 8, 8, 64) == 0
+
+
+# Threads of a launch are numbered in 32 bits: 2^24 - 1 workgroups of 256.
+@pytest.mark.parametrize("kwargs", [
+    dict(frames=2 ** 21, tq=2 ** 21, tk=2 ** 21, hq=8, hk=8, qs=512, ks=512, vs=512, os=512),    # a tile a track
+    dict(frames=2 ** 21 - 1, tq=2 ** 27, tk=8, hq=8, hk=8, qs=512, ks=512, vs=512, os=512),
+    dict(frames=1, tq=2 ** 31 - 300, tk=8, hq=2, hk=2),
+])
+def test_attention_rejects_more_workgroups_than_a_launch_holds(kwargs):
+    assert attention(**kwargs) == binding.FLOCK_EUNSUPPORTED
+    assert "workgroups" in binding.lib().flock_last_error().decode()
+    assert attention_back(**dict(kwargs, dqs=512, dks=512, dvs=512)) == binding.FLOCK_EUNSUPPORTED
+    assert "workgroups" in binding.lib().flock_last_error().decode()
+
+
+@pytest.mark.parametrize("kwargs", [
+    dict(frames=2 ** 19, tq=2 ** 19, tk=2 ** 19, hq=8, hk=8, qs=512, ks=512, vs=512, os=512),
+    dict(frames=1, tq=2 ** 28, tk=8, hq=2, hk=2),
+])
+def test_attention_takes_batches_within_a_launch(kwargs):
+    """What ends such a call here is the missing device, or its other error, not its size."""
+    assert attention(**kwargs, lse=FAKE4) == binding.FLOCK_EINVAL
+    if not torch.cuda.is_available():
+        assert attention(**kwargs) == binding.FLOCK_EDEVICE
+        assert attention_back(**dict(kwargs, dqs=512, dks=512, dvs=512)) == binding.FLOCK_EDEVICE
+
+
+def test_attention_backward_rejects_too_many_keys():
+    assert attention_back(tk=2 ** 31 - 1, tq=8, frames=1, hq=2, hk=2, ks=128, vs=128, dks=128, dvs=128) == \
+        binding.FLOCK_EUNSUPPORTED
