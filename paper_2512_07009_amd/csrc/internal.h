@@ -195,6 +195,15 @@ hipError_t launch_mask(MaskArgs a, void *workspace, hipStream_t stream);
 // ----------------------------------------------------------------------------
 // Per-bird encoder: layer norm, rotary positions, attention
 // ----------------------------------------------------------------------------
+// Threads of a launch are numbered in 32 bits: workgroups of 256 that one holds.
+constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;
+
+// p, n elements of `size` bytes on; nullptr stays.
+template <typename P>
+inline void move_on(P *&p, int64_t n, size_t size) {
+    if (p) p = reinterpret_cast<P *>(reinterpret_cast<uintptr_t>(p) + n * size);
+}
+
 struct NormArgs {
     const void *x, *residual;          // [rows][width], strides in elements; residual may be nullptr
     int64_t x_stride, residual_stride;
@@ -205,6 +214,15 @@ struct NormArgs {
     void *y, *sum;                     // sum only with residual
     int64_t y_stride, sum_stride;
     float *mean, *rstd;                // [rows] or nullptr
+
+    void advance(int64_t first, size_t size) {
+        move_on(x, first * x_stride, size);
+        move_on(residual, first * residual_stride, size);
+        move_on(y, first * y_stride, size);
+        move_on(sum, first * sum_stride, size);
+        move_on(mean, first, sizeof(float));
+        move_on(rstd, first, sizeof(float));
+    }
 };
 hipError_t launch_norm(const NormArgs &a, int32_t dtype, hipStream_t stream);
 
@@ -218,6 +236,15 @@ struct NormBackwardArgs {
     void *grad_x;
     int64_t grad_x_stride;
     float *partial;                     // set by launch_norm_backward
+
+    void advance(int64_t first, size_t size) {
+        move_on(grad_y, first * grad_y_stride, size);
+        move_on(grad_sum, first * grad_sum_stride, size);
+        move_on(x, first * x_stride, size);
+        move_on(grad_x, first * grad_x_stride, size);
+        move_on(mean, first, sizeof(float));
+        move_on(rstd, first, sizeof(float));
+    }
 };
 size_t norm_backward_workspace_bytes(int64_t rows, int32_t width, int n_cus);
 hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspace, int n_cus, float *grad_weight,
@@ -238,11 +265,17 @@ struct RotaryArgs {
     int32_t tail, birds_per_block;     // set by launch_rotary
     uint32_t chunk_reciprocal, head_reciprocal, pair_reciprocal;
     uint64_t step[kRotaryMaxPairs];    // 2^-64 turns per unit
+
+    void advance(int64_t first, size_t size) {
+        move_on(q, first * q_stride, size);
+        move_on(k, first * k_stride, size);
+        move_on(q_out, first * q_out_stride, size);
+        move_on(k_out, first * k_out_stride, size);
+        move_on(xy, 2 * first, sizeof(int32_t));
+        move_on(time, first, sizeof(int32_t));
+    }
 };
 hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);
-
-// Threads of a launch are numbered in 32 bits: workgroups of 256 that one holds.
-constexpr int64_t kMaxWorkgroups = (1 << 24) - 1;
 
 constexpr int kAttentionMaxDim = 128;
 // 64 rows lie within 2^31 bytes: a tile's loads go through resources of 64 rows at most

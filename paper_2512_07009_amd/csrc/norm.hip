@@ -328,6 +328,22 @@ hipError_t with_shape(int32_t width, F &&fn, W &&wide) {
     return wide();
 }
 
+// launch(part, blocks) over the rows of a, by as many as a launch holds.  Parts
+// begin at a group of rows, so that a row gets the same lanes in any of them.
+template <typename T, typename A, typename F>
+hipError_t by_parts(A a, int rows_per_block, F &&launch) {
+    const int64_t rows = a.rows, most = kMaxWorkgroups * rows_per_block;
+    hipError_t err = hipSuccess;
+    for (int64_t first = 0; first < rows && err == hipSuccess; first += most) {
+        A part = a;
+        part.rows = std::min(rows - first, most);
+        part.advance(first, sizeof(T));
+        launch(part, dim3((uint32_t)((part.rows + rows_per_block - 1) / rows_per_block)));
+        err = hipGetLastError();
+    }
+    return err;
+}
+
 constexpr int kWideShares = 64;
 
 // Blocks of the backward pass: enough to fill the card (four of 256 threads a
@@ -354,14 +370,14 @@ hipError_t launch_norm(const NormArgs &a, int32_t dtype, hipStream_t stream) {
                 a.width,
                 [&](auto iter, auto tpr) {
                     constexpr int ITER = decltype(iter)::value, TPR = decltype(tpr)::value;
-                    constexpr int kRows = kThreads / TPR;
-                    hipLaunchKernelGGL((norm_kernel<T, kVec, ITER, TPR>), dim3((uint32_t)((a.rows + kRows - 1) / kRows)),
-                                       dim3(kThreads), 0, stream, a);
-                    return hipGetLastError();
+                    return by_parts<T>(a, kThreads / TPR, [&](const NormArgs &part, dim3 grid) {
+                        hipLaunchKernelGGL((norm_kernel<T, kVec, ITER, TPR>), grid, dim3(kThreads), 0, stream, part);
+                    });
                 },
                 [&] {
-                    hipLaunchKernelGGL((norm_wide_kernel<T>), dim3((uint32_t)a.rows), dim3(kThreads), 0, stream, a);
-                    return hipGetLastError();
+                    return by_parts<T>(a, 1, [&](const NormArgs &part, dim3 grid) {
+                        hipLaunchKernelGGL((norm_wide_kernel<T>), grid, dim3(kThreads), 0, stream, part);
+                    });
                 });
     });
 }
@@ -384,9 +400,9 @@ hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspa
                     return hipGetLastError();
                 },
                 [&] {
-                    hipLaunchKernelGGL((norm_backward_wide_kernel<T>), dim3((uint32_t)a.rows), dim3(kThreads), 0, stream,
-                                       a);
-                    hipError_t e = hipGetLastError();
+                    hipError_t e = by_parts<T>(a, 1, [&](const NormBackwardArgs &part, dim3 grid) {
+                        hipLaunchKernelGGL((norm_backward_wide_kernel<T>), grid, dim3(kThreads), 0, stream, part);
+                    });
                     if (e != hipSuccess || !a.partial) return e;
                     shares = (int)std::min<int64_t>(kWideShares, a.rows);
                     hipLaunchKernelGGL((norm_columns_kernel<T>), dim3((a.width + kThreads - 1) / kThreads, shares),

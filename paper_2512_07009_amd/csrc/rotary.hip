@@ -148,10 +148,19 @@ hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream) {
         a.chunk_reciprocal = reciprocal(chunks);
         a.head_reciprocal = reciprocal(heads);
         a.pair_reciprocal = reciprocal(a.pairs);
-        const dim3 grid((uint32_t)((a.total + a.birds_per_block - 1) / a.birds_per_block));
-        if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, kVec, true>), grid, dim3(kThreads), 0, stream, a);
-        else hipLaunchKernelGGL((rotary_kernel<T, kVec, false>), grid, dim3(kThreads), 0, stream, a);
-        return hipGetLastError();
+        // by as many birds as a launch holds
+        const int64_t total = a.total, most = kMaxWorkgroups * a.birds_per_block;
+        hipError_t err = hipSuccess;
+        for (int64_t first = 0; first < total && err == hipSuccess; first += most) {
+            RotaryArgs part = a;
+            part.total = std::min(total - first, most);
+            part.advance(first, sizeof(T));
+            const dim3 grid((uint32_t)((part.total + a.birds_per_block - 1) / a.birds_per_block));
+            if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, kVec, true>), grid, dim3(kThreads), 0, stream, part);
+            else hipLaunchKernelGGL((rotary_kernel<T, kVec, false>), grid, dim3(kThreads), 0, stream, part);
+            err = hipGetLastError();
+        }
+        return err;
     });
 }
 

@@ -243,3 +243,38 @@ def test_rotary_refusals():
     with pytest.raises(ValueError, match="q or k"):
         flock.rotary_frames(None, None, xy, flock.RotaryAxes(x=[1.0]))
     assert flock.rotary_frames(q[:0], None, xy[:0], flock.RotaryAxes(x=[1.0]))[0].shape == (0, 2, 8)
+
+
+def ends(n, at):
+    """Rows at the beginning, the end, and round a place between."""
+    return [slice(0, 100), slice(at - 100, at + 100), slice(n - 100, n)]
+
+
+def test_norm_of_more_rows_than_a_launch_holds():
+    """2^24 - 1 workgroups, of 32 narrow rows each."""
+    most = ((1 << 24) - 1) * 32
+    n = most + 1000
+    x = torch.empty(n, 4, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, n, 1 << 26):
+        x[i:i + (1 << 26)].normal_()
+    w = torch.rand(4, device="cuda")
+    y, _, mean, rstd = flock.layer_norm_rows(x, w)
+    for rows in ends(n, most):
+        want = flock.layer_norm_rows(x[rows], w)
+        assert torch.equal(y[rows], want[0]) and torch.equal(mean[rows], want[2]) and torch.equal(rstd[rows], want[3])
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rotary_of_more_birds_than_a_launch_holds(interleaved):
+    """2^24 - 1 workgroups, of 64 birds each."""
+    most = ((1 << 24) - 1) * 64
+    n = most + 1000
+    q = torch.empty(n, 1, 2, dtype=torch.bfloat16, device="cuda")
+    for i in range(0, n, 1 << 26):
+        q[i:i + (1 << 26)].normal_()
+    time = torch.arange(n, dtype=torch.int32, device="cuda")
+    axes = flock.RotaryAxes(time=[0.1])
+    want = [flock.rotary_frames(q[r], None, None, axes, time=time[r], interleaved=interleaved)[0] for r in ends(n, most)]
+    flock.rotary_frames(q, None, None, axes, time=time, interleaved=interleaved, out=(q, None))
+    for r, w in zip(ends(n, most), want):
+        assert torch.equal(q[r], w)
