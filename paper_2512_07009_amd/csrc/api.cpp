@@ -10,7 +10,9 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <memory>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -822,8 +824,10 @@ flock_status check_workgroups(int64_t n) {
 
 flock_status validate_offsets(const char *name, const int32_t *offsets, int32_t n_frames, int32_t total,
                               hipStream_t stream) {
-    std::vector<int32_t> off((size_t)n_frames + 1);
-    hipError_t err = hipMemcpyAsync(off.data(), offsets, off.size() * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
+    const size_t n = (size_t)n_frames + 1;
+    const std::unique_ptr<int32_t[]> off(new (std::nothrow) int32_t[n]);
+    if (!off) return fail(FLOCK_ENOMEM, "no host memory for FLOCK_VALIDATE's copy of %s", name);
+    hipError_t err = hipMemcpyAsync(off.get(), offsets, n * sizeof(int32_t), hipMemcpyDeviceToHost, stream);
     if (err == hipSuccess) err = hipStreamSynchronize(stream);
     if (err != hipSuccess) return hip_fail(err, "FLOCK_VALIDATE offsets copy");
     if (off[0] != 0) return fail(FLOCK_EINVAL, "%s[0] = %d, expected 0", name, off[0]);

@@ -562,3 +562,22 @@ def test_distances_at_the_limit_of_products(dtype, limit, cap, share):
     off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
     out = flock.attention_frames(d["q"], d["k"], d["v"], off, q_xy=d["q_xy"], slopes=d["slopes"], cap=cap)
     check_norms({"out": out}, want, dtype, ("out",))
+
+
+def test_offsets_are_checked_on_request(monkeypatch):
+    monkeypatch.setenv("FLOCK_VALIDATE", "1")
+    q = torch.randn(20, 2, 64, device="cuda").to(torch.bfloat16)
+    good = torch.tensor([0, 7, 20], dtype=torch.int32, device="cuda")
+    out, lse = flock.attention_frames(q, q, q, good, return_lse=True)
+    flock.attention_frames_backward(q, q, q, q, out, lse, good)
+    for bad, text in (([1, 7, 20], r"q_offsets\[0\]"), ([0, 9, 7, 20], "decrease at frame 1"), ([0, 7, 19], "its total is 20")):
+        off = torch.tensor(bad, dtype=torch.int32, device="cuda")
+        held = torch.full_like(q, 7.0)
+        with pytest.raises(ValueError, match=text):
+            flock.attention_frames(q, q, q, off, out=held)
+        assert (held == 7).all()
+        with pytest.raises(ValueError, match=text):
+            flock.attention_frames_backward(q, q, q, q, out, lse, off)
+        if len(bad) == 3:
+            with pytest.raises(ValueError, match=text.replace("q_", "k_")):
+                flock.attention_frames(q, q, q, good, k_offsets=off)
