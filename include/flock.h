@@ -367,7 +367,10 @@ size_t mask_components_frames_workspace(int32_t n_frames, int32_t width, int32_t
  * stride is the distance between the starts of two rows in elements, so that
  * queries, keys and values can be slices of one projection.  The heads of a
  * row are contiguous, head h at h * head_dim.  No output may overlap an input,
- * except as stated at rotary_frames.
+ * except as stated at layer_norm_rows and rotary_frames.
+ * Attention numbers its work by the offsets: in a batch with an inconsistent
+ * frame, what the other frames get is not defined.  Nothing is read or written
+ * out of range, and rows that no consistent frame holds are left untouched.
  */
 #define FLOCK_F32 0
 #define FLOCK_F16 1

@@ -581,3 +581,80 @@ def test_offsets_are_checked_on_request(monkeypatch):
         if len(bad) == 3:
             with pytest.raises(ValueError, match=text.replace("q_", "k_")):
                 flock.attention_frames(q, q, q, good, k_offsets=off)
+
+
+def test_frame_alone_and_in_a_batch():
+    """A frame's results do not depend on the others where the batch takes the
+    same kernel and shares of the keys: few rows a frame, histories below two
+    shares."""
+    counts = [[1, 60, 33], [200, 250, 129]]
+    c = make(41, counts[0], counts[1], 4, 2, 64, torch.bfloat16, distance=True, hidden=0.1)
+    all_of = call(c)
+    for f in range(3):
+        qs, ks = slice(c["q_off"][f], c["q_off"][f + 1]), slice(c["k_off"][f], c["k_off"][f + 1])
+        one = dict(c, q=c["q"][qs], grad=c["grad"][qs], q_xy=c["q_xy"][qs], k=c["k"][ks], v=c["v"][ks], k_xy=c["k_xy"][ks],
+                   keep=c["keep"][ks], q_off=[0, counts[0][f]], k_off=[0, counts[1][f]])
+        got = call(one)
+        for n, rows in (("out", qs), ("lse", qs), ("dq", qs), ("dk", ks), ("dv", ks)):
+            assert torch.equal(got[n], all_of[n][rows]), (f, n)
+
+
+def bad_frames(off, total):
+    return [not (0 <= off[f] <= off[f + 1] <= total) for f in range(len(off) - 1)]
+
+
+@pytest.mark.parametrize("form", ["few rows", "shares of the keys", "many rows"])
+@pytest.mark.parametrize("bad", ["past the end", "backwards", "negative"])
+def test_inconsistent_frames(form, bad):
+    """A frame whose offsets run backwards or past the end is not read, and rows
+    that no consistent frame holds are left alone in every output.  What a
+    consistent frame gets is not defined (tiles are numbered by the offsets), but
+    where one launch makes it, it is right or left alone."""
+    frames, n = (200, 60) if form == "many rows" else (4, 60)
+    heads = (8, 8) if form == "many rows" else (2, 1)
+    total, n_k = frames * n, 3000 if form == "shares of the keys" else n
+    c = make(42, [n] * frames, [n_k] * frames, *heads, 64, torch.bfloat16)
+    want, bound = reference(c)
+    q_off = list(c["q_off"])
+    if bad == "past the end":       # frames 1 and 2 are bad
+        q_off[2] = total + 100
+    elif bad == "backwards":        # frame 1 is bad, frame 2 begins where frame 1 did
+        q_off[2] = q_off[1] - 1 if form == "few rows" else q_off[1] - 7
+    else:                           # frame 0 is bad
+        q_off[0] = -5
+    ok = [not x for x in bad_frames(q_off, total)]
+    d = {k: (t.cuda() if torch.is_tensor(t) else t) for k, t in c.items()}
+    qo = torch.tensor(q_off, dtype=torch.int32).cuda()
+    ko = torch.tensor(c["k_off"], dtype=torch.int32).cuda()
+    out = torch.full_like(d["q"], 7.0)
+    _, lse = flock.attention_frames(d["q"], d["k"], d["v"], qo, k_offsets=ko, out=out, return_lse=True)
+    # rows that only their own, consistent frame holds, and rows of none
+    holders = [[f for f in range(frames) if ok[f] and q_off[f] <= i < q_off[f + 1]] for i in range(total)]
+    right = torch.tensor([h == [i // n] and q_off[h[0]] == c["q_off"][h[0]] and q_off[h[0] + 1] == c["q_off"][h[0] + 1]
+                          for i, h in enumerate(holders)])
+    free = torch.tensor([not h for h in holders])
+    assert right.any() and (free.any() or bad == "backwards")
+    written = right & (out.cpu() != 7).flatten(1).any(1)
+    if form != "shares of the keys":
+        ref.check(out.cpu()[written], want["out"][written], bound["out"][written], "out")
+    assert (out.cpu()[free] == 7).all()
+    # the backward pass by the C ABI, into gradients that hold something
+    dq, dk, dv = (torch.full_like(d[x], 7.0) for x in "qkv")
+    full, full_lse = flock.attention_frames(d["q"], d["k"], d["v"], torch.tensor(c["q_off"], dtype=torch.int32).cuda(),
+                                            k_offsets=ko, return_lse=True)
+    lib = flock.lib()
+    tq, tk, hq, hk, dim = total, frames * n_k, *heads, 64
+    st = lib.attention_frames_backward(2, d["grad"].data_ptr(), hq * dim, d["q"].data_ptr(), hq * dim, d["k"].data_ptr(),
+                                       hk * dim, d["v"].data_ptr(), hk * dim, full.data_ptr(), hq * dim, full_lse.data_ptr(),
+                                       qo.data_ptr(), ko.data_ptr(), frames, tq, tk, hq, hk, dim, None, None, None, None, 0,
+                                       None, c["scale"], 0.0, dq.data_ptr(), hq * dim, dk.data_ptr(), hk * dim, dv.data_ptr(),
+                                       hk * dim, None, None, 0, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert st == 0
+    written = right & (dq.cpu() != 7).flatten(1).any(1)
+    ref.check(dq.cpu()[written], want["dq"][written], bound["dq"][written], "dq")
+    assert (dq.cpu()[free] == 7).all()
+    for f in range(frames):
+        if not ok[f]:
+            keys = slice(f * n_k, (f + 1) * n_k)
+            assert (dk[keys] == 7).all() and (dv[keys] == 7).all(), f
