@@ -436,20 +436,18 @@ struct RowTile {
     }
 };
 
-// Gradients of keys and values: 32 BLOCKS keys a wave, over the rows that see
-// them.  The products are S = Q K^T and dP = dO V^T here, so that a lane holds one
-// key (of each block); what is read of a row from LDS serves all blocks, which
-// is what LDS bandwidth asks for where registers allow it.  They do not yet: two
-// blocks leave one wave a SIMD, 4.37 ms against 3.67 for a training step on 64 frames
-// of 2000, 8 heads of 64 with distances.  One block, same frames: 1454 us, 0.65
-// PFLOP/s of four products (VALU 43%, matrix cores 36%, LDS 41% of the time, a fifth
+// Gradients of keys and values: 32 keys a wave, over the rows that see them.  The
+// products are S = Q K^T and dP = dO V^T here, so that a lane holds one key.  64 keys
+// a wave would halve what is read of LDS for each, but leave one wave a SIMD (4.37 ms
+// against 3.67 for a training step on 64 frames of 2000, 8 heads of 64 with
+// distances).  Same frames, 1454 us, 0.65 PFLOP/s of four products (VALU 43%, matrix cores 36%, LDS 41% of the time, a fifth
 // of that bank conflicts of rows that are read both ways); the phases of the two
 // waves a SIMD overlap only in part.
-template <typename T, int DP, int BLOCKS, bool DIST, int CAP>
+template <typename T, int DP, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
     using Tile = RowTile<T, DP, DIST>;
-    constexpr int kKeys = 128 * BLOCKS;
+    constexpr int kKeys = 128;
     const AttentionArgs &a = b.fwd;
     extern __shared__ char shared[];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
@@ -462,47 +460,39 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
     const int64_t key0 = tile * kKeys;
     if (key0 >= sp.nk) return;
     const int n_rows = sp.nq * a.group;
-    F k[BLOCKS][DP / 16], v[BLOCKS][DP / 16];
-    float kx[BLOCKS], ky[BLOCKS];
-    bool kept[BLOCKS];
-    const int wave_key = (int)key0 + 32 * BLOCKS * wave;  // the wave's first key
+    F k[DP / 16], v[DP / 16];
+    const int wave_key = (int)key0 + 32 * wave;  // the wave's first key
+    const int key = wave_key + col;
+    const bool valid = key < sp.nk;
+    const int64_t krow = sp.k0 + (valid ? key : 0);
+    const bool kept = valid && (!a.keep || a.keep[krow]);
+    const short *k_row = kept ? static_cast<const short *>(a.k) + krow * a.k_stride + head * a.dim : nullptr;
+    const short *v_row = kept ? static_cast<const short *>(a.v) + krow * a.v_stride + head * a.dim : nullptr;
 #pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) {
-        const int key = wave_key + 32 * n + col;
-        const bool valid = key < sp.nk;
-        const int64_t krow = sp.k0 + (valid ? key : 0);
-        kept[n] = valid && (!a.keep || a.keep[krow]);
-        const short *k_row = kept[n] ? static_cast<const short *>(a.k) + krow * a.k_stride + head * a.dim : nullptr;
-        const short *v_row = kept[n] ? static_cast<const short *>(a.v) + krow * a.v_stride + head * a.dim : nullptr;
-#pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
-            k[n][s] = load_frag<T>(k_row, s, h, a.dim);
-            v[n][s] = load_frag<T>(v_row, s, h, a.dim);
-        }
-        kx[n] = ky[n] = 0.0f;
-        if (DIST && valid) {
-            const int2 place = reinterpret_cast<const int2 *>(a.k_xy)[krow];
-            kx[n] = (float)place.x * kPxPerQuantum;
-            ky[n] = (float)place.y * kPxPerQuantum;
-        }
+    for (int s = 0; s < DP / 16; ++s) {
+        k[s] = load_frag<T>(k_row, s, h, a.dim);
+        v[s] = load_frag<T>(v_row, s, h, a.dim);
+    }
+    float kx = 0.0f, ky = 0.0f;
+    if (DIST && valid) {
+        const int2 place = reinterpret_cast<const int2 *>(a.k_xy)[krow];
+        kx = (float)place.x * kPxPerQuantum;
+        ky = (float)place.y * kPxPerQuantum;
     }
     float largest = 0.0f;
     int2 origin = make_int2(0, 0);
-    bool keys_near = DIST;
-    bf16x8 key_slots[BLOCKS] = {};
+    bool keys_near = false;
+    bf16x8 key_slots = {};
     if (DIST) {
         origin = near_origin(reinterpret_cast<const int2 *>(a.k_xy)[sp.k0 + min((int)key0 + col, sp.nk - 1)]);
         float steepest = 0.0f;
         for (int e = 0; e < a.group; ++e) steepest = fmaxf(steepest, fabsf(a.slopes[head * a.group + e]) * kLog2e);
         largest = near_limit<T>() * 256.0f / steepest;
-#pragma unroll
-        for (int n = 0; n < BLOCKS; ++n) {
-            const int bx = (int)(kx[n] * 16.0f) - origin.x, by = (int)(ky[n] * 16.0f) - origin.y;
-            const float n2 = square_quanta(bx, by);
-            const NearSlots s = near_key(bx, by, n2);
-            key_slots[n] = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
-            keys_near = keys_near && __all(wave_key + 32 * n + col >= sp.nk || near_enough(bx, by, n2, largest));
-        }
+        const int bx = (int)(kx * 16.0f) - origin.x, by = (int)(ky * 16.0f) - origin.y;
+        const float n2 = square_quanta(bx, by);
+        const NearSlots s = near_key(bx, by, n2);
+        key_slots = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
+        keys_near = __all(!valid || near_enough(bx, by, n2, largest));
     }
     const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
@@ -511,11 +501,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
     if (a.causal && key0 >= prefix)
         begin = (int)(max((int64_t)0, key0 - sp.nk + sp.nq) * a.group / kTileRows * kTileRows);
 
-    f32x16 dk[BLOCKS][DP / 32] = {}, dv[BLOCKS][DP / 32] = {};
-    float ds_scale[BLOCKS];  // beside that of the weights
-    bool lowered = false;    // any lane's
-#pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) ds_scale[n] = 1.0f;
+    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    float ds_scale = 1.0f;  // beside that of the weights
+    bool lowered = false;   // any lane's
     auto sub_tile = [&](const typename Tile::Lds &t, int first, bool limited, bool exact, bool near) {
         F qf[DP / 16], gf[DP / 16];
 #pragma unroll
@@ -524,124 +512,112 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
             gf[st] = read_rows<T, Tile::kPitch>(t.g, first + col, st, h);
         }
         // the columns are read here where registers allow it, to be there when the weights are
-        constexpr bool EARLY = DP <= 64 && !(DIST && (CAP || kScaled<T>));
-        F gc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1], qc[EARLY ? 2 : 1][EARLY ? DP / 32 : 1];
-        if (EARLY) {
-#pragma unroll
-            for (int part = 0; part < 2; ++part)
-#pragma unroll
-                for (int blk = 0; blk < DP / 32; ++blk) {
-                    gc[part][blk] = read_columns<T, Tile::kPitch>(t.g, first + 16 * part, blk, lane);
-                    qc[part][blk] = read_columns<T, Tile::kPitch>(t.q, first + 16 * part, blk, lane);
-                }
-        }
-        F p[BLOCKS][2], ds[BLOCKS][2];
-#pragma unroll
-        for (int n = 0; n < BLOCKS; ++n) {
-            f32x16 s = {}, dp = {};
-#pragma unroll
-            for (int st = 0; st < DP / 16; ++st) {
-                s = mfma(qf[st], k[n][st], s);
-                dp = mfma(gf[st], v[n][st], dp);
-            }
-            if (CAP) cap_parts<CAP>(s, scale);
-            if (near) {
-                const bf16x8 row = __builtin_bit_cast(bf16x8, t.near[h * kTileRows + first + col]);
-                f32x16 bias;
-                if (CAP) bias = mfma(row, key_slots[n], f32x16{});
-                else s = mfma(row, key_slots[n], s);
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    float shift[4], delta[4];
-                    *reinterpret_cast<float4 *>(shift) = read4(t.near_shift, first, r, h);
-                    *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float d = dp[r + e] - delta[e];
-                        if (CAP) {
-                            d *= cap_slope<CAP>(s[r + e]);
-                            s[r + e] = exp2_fast(capped<CAP>(s[r + e], cap2, bias[r + e]) - shift[e]);
-                        } else {
-                            s[r + e] = exp2_fast(__builtin_fmaf(s[r + e], scale, -shift[e]));
-                        }
-                        dp[r + e] = s[r + e] * d;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    float x[4], y[4], slope[4] = {}, shift[4], delta[4];
-                    if (DIST) {
-                        *reinterpret_cast<float4 *>(x) = read4(t.x, first, r, h);
-                        *reinterpret_cast<float4 *>(y) = read4(t.y, first, r, h);
-                        *reinterpret_cast<float4 *>(slope) = read4(t.slope, first, r, h);
-                    }
-                    *reinterpret_cast<float4 *>(shift) = read4(t.shift, first, r, h);
-                    *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float d2 = DIST ? distance2(x[e] - kx[n], y[e] - ky[n]) : 0.0f;
-                        const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e]);
-                        const float p = exp2_fast(z - shift[e]);
-                        float d = p * (dp[r + e] - delta[e]);
-                        if (CAP) d *= cap_slope<CAP>(s[r + e]);
-                        s[r + e] = p;
-                        dp[r + e] = d;
-                    }
-                }
-            }
-            if (limited) {
-                const int key = wave_key + 32 * n + col;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (key >= t.limit[first + out_row(r, h)]) s[r] = dp[r] = 0.0f;
-            }
-            if (!exact) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float rest = t.rest[first + out_row(r, h)];
-                    s[r] *= rest;
-                    dp[r] *= rest;
-                }
-            }
-            if (kScaled<T>) {
-                if (lowered) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) dp[r] *= ds_scale[n];
-                }
-                const float most = most_of(dp);
-                if (__any(most > kLargestFactor)) {
-                    lowered = true;
-                    const float step = scale_step(most);
-                    ds_scale[n] *= step;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) dp[r] *= step;
-#pragma unroll
-                    for (int blk = 0; blk < DP / 32; ++blk)
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) dk[n][blk][r] *= step;
-                }
-            }
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                p[n][part] = round_frag<T>(s, part);
-                ds[n][part] = round_frag<T>(dp, part);
-            }
-        }
+        // (halves of the 32 rows; with distances a fourth of them more would spill)
+        constexpr int G_EARLY = DP <= 64 && !(DIST && (CAP || kScaled<T>)) ? 2 : 0;
+        constexpr int Q_EARLY = DIST && G_EARLY ? 1 : G_EARLY;
+        F gc[2][DP / 32], qc[2][DP / 32];
+        auto columns = [&](int part, int blk, bool g, bool q) {
+            if (g) gc[part][blk] = read_columns<T, Tile::kPitch>(t.g, first + 16 * part, blk, lane);
+            if (q) qc[part][blk] = read_columns<T, Tile::kPitch>(t.q, first + 16 * part, blk, lane);
+        };
 #pragma unroll
         for (int part = 0; part < 2; ++part)
 #pragma unroll
-            for (int blk = 0; blk < DP / 32; ++blk) {
-                if (!EARLY) {
-                    gc[0][0] = read_columns<T, Tile::kPitch>(t.g, first + 16 * part, blk, lane);
-                    qc[0][0] = read_columns<T, Tile::kPitch>(t.q, first + 16 * part, blk, lane);
-                }
+            for (int blk = 0; blk < DP / 32; ++blk) columns(part, blk, part < G_EARLY, part < Q_EARLY);
+        f32x16 s = {}, dp = {};
 #pragma unroll
-                for (int n = 0; n < BLOCKS; ++n) {
-                    dv[n][blk] = mfma(gc[EARLY ? part : 0][EARLY ? blk : 0], p[n][part], dv[n][blk]);
-                    dk[n][blk] = mfma(qc[EARLY ? part : 0][EARLY ? blk : 0], ds[n][part], dk[n][blk]);
+        for (int st = 0; st < DP / 16; ++st) {
+            s = mfma(qf[st], k[st], s);
+            dp = mfma(gf[st], v[st], dp);
+        }
+        if (CAP) cap_parts<CAP>(s, scale);
+        if (near) {
+            const bf16x8 row = __builtin_bit_cast(bf16x8, t.near[h * kTileRows + first + col]);
+            f32x16 bias;
+            if (CAP) bias = mfma(row, key_slots, f32x16{});
+            else s = mfma(row, key_slots, s);
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                float shift[4], delta[4];
+                *reinterpret_cast<float4 *>(shift) = read4(t.near_shift, first, r, h);
+                *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float d = dp[r + e] - delta[e];
+                    if (CAP) {
+                        d *= cap_slope<CAP>(s[r + e]);
+                        s[r + e] = exp2_fast(capped<CAP>(s[r + e], cap2, bias[r + e]) - shift[e]);
+                    } else {
+                        s[r + e] = exp2_fast(__builtin_fmaf(s[r + e], scale, -shift[e]));
+                    }
+                    dp[r + e] = s[r + e] * d;
                 }
             }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                float x[4], y[4], slope[4] = {}, shift[4], delta[4];
+                if (DIST) {
+                    *reinterpret_cast<float4 *>(x) = read4(t.x, first, r, h);
+                    *reinterpret_cast<float4 *>(y) = read4(t.y, first, r, h);
+                    *reinterpret_cast<float4 *>(slope) = read4(t.slope, first, r, h);
+                }
+                *reinterpret_cast<float4 *>(shift) = read4(t.shift, first, r, h);
+                *reinterpret_cast<float4 *>(delta) = read4(t.delta, first, r, h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float d2 = DIST ? distance2(x[e] - kx, y[e] - ky) : 0.0f;
+                    const float z = score<DIST, CAP>(s[r + e], scale, cap2, d2, slope[e]);
+                    const float p = exp2_fast(z - shift[e]);
+                    float d = p * (dp[r + e] - delta[e]);
+                    if (CAP) d *= cap_slope<CAP>(s[r + e]);
+                    s[r + e] = p;
+                    dp[r + e] = d;
+                }
+            }
+        }
+        if (limited) {
+            const int key = wave_key + col;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (key >= t.limit[first + out_row(r, h)]) s[r] = dp[r] = 0.0f;
+        }
+        if (!exact) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float rest = t.rest[first + out_row(r, h)];
+                s[r] *= rest;
+                dp[r] *= rest;
+            }
+        }
+        if (kScaled<T>) {
+            if (lowered) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] *= ds_scale;
+            }
+            const float most = most_of(dp);
+            if (__any(most > kLargestFactor)) {
+                lowered = true;
+                const float step = scale_step(most);
+                ds_scale *= step;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] *= step;
+#pragma unroll
+                for (int blk = 0; blk < DP / 32; ++blk)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) dk[blk][r] *= step;
+            }
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const F p = round_frag<T>(s, part), ds = round_frag<T>(dp, part);
+#pragma unroll
+            for (int blk = 0; blk < DP / 32; ++blk) {
+                columns(part, blk, part >= G_EARLY, part >= Q_EARLY);
+                dv[blk] = mfma(gc[part][blk], p, dv[blk]);
+                dk[blk] = mfma(qc[part][blk], ds, dk[blk]);
+            }
+        }
     };
 
     const float units = CAP ? 1.0f : 1.0f / scale, constant = CAP ? cap_constant<CAP>(cap2) : 0.0f;
@@ -667,39 +643,35 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         if (wave_key < some) {
 #pragma unroll 1
             for (int sub = 0; sub < kTileRows / 32; ++sub)
-                sub_tile(t, 32 * sub, min(wave_key + 32 * BLOCKS, sp.nk) > all, exact, near);
+                sub_tile(t, 32 * sub, min(wave_key + 32, sp.nk) > all, exact, near);
         }
         buffer ^= 1;
         if (more) next.template store<DIST>(typename Tile::Lds(shared + buffer * Tile::kBytes), origin, largest, units, constant);
         __syncthreads();
     }
+    if (wave_key + col >= sp.nk) return;
+    const int64_t row = sp.k0 + wave_key + col;
+    T *dk_out = static_cast<T *>(b.grad_k) + row * b.grad_k_stride + head * a.dim;
+    T *dv_out = static_cast<T *>(b.grad_v) + row * b.grad_v_stride + head * a.dim;
+    constexpr float kUnscale = 1.0f / kFactorScale<T>;
+    const float dk_scale = a.scale * kUnscale / ds_scale;
 #pragma unroll
-    for (int n = 0; n < BLOCKS; ++n) {
-        const int key = wave_key + 32 * n + col;
-        if (key >= sp.nk) continue;
-        const int64_t krow = sp.k0 + key;
-        T *dk_out = static_cast<T *>(b.grad_k) + krow * b.grad_k_stride + head * a.dim;
-        T *dv_out = static_cast<T *>(b.grad_v) + krow * b.grad_v_stride + head * a.dim;
-        constexpr float kUnscale = 1.0f / kFactorScale<T>;
-        const float dk_scale = a.scale * kUnscale / ds_scale[n];
+    for (int blk = 0; blk < DP / 32; ++blk)
 #pragma unroll
-        for (int blk = 0; blk < DP / 32; ++blk)
+        for (int r = 0; r < 16; r += 4) {
+            const int d = 32 * blk + out_row(r, h);
+            if (d < a.dim) {
+                // a hidden key's scores are not masked above: its gradients are zero
+                float x[4], y[4];
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int d = 32 * blk + out_row(r, h);
-                if (d < a.dim) {
-                    // a hidden key's scores are not masked above: its gradients are zero
-                    float x[4], y[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        x[e] = kept[n] ? dk[n][blk][r + e] * dk_scale : 0.0f;
-                        y[e] = kept[n] ? dv[n][blk][r + e] * kUnscale : 0.0f;
-                    }
-                    store_pack<T, 4>(dk_out + d, x);
-                    store_pack<T, 4>(dv_out + d, y);
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = kept ? dk[blk][r + e] * dk_scale : 0.0f;
+                    y[e] = kept ? dv[blk][r + e] * kUnscale : 0.0f;
                 }
+                store_pack<T, 4>(dk_out + d, x);
+                store_pack<T, 4>(dv_out + d, y);
             }
-    }
+        }
 }
 
 // Gradient of a head's slope: the workgroups' shares, in 64 bits and a fixed
@@ -758,9 +730,8 @@ hipError_t launch_attention_backward(AttentionBackwardArgs b, int32_t dtype, voi
         }
         if (a.total_k > 0) {
             constexpr size_t bytes = 2 * RowTile<T, DP, DIST>::kBytes;
-            constexpr int kBlocks = 1;
             b.key_slots = backward_key_slots(a.n_frames, a.total_k);
-            auto kernel = attention_dkv_kernel<T, DP, kBlocks, DIST, CAP>;
+            auto kernel = attention_dkv_kernel<T, DP, DIST, CAP>;
             hipLaunchKernelGGL(kernel, dim3((uint32_t)(b.key_slots * a.kv_heads)), dim3(kThreads), bytes, stream, b);
             e = hipGetLastError();
         }
