@@ -104,9 +104,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 3 : 2) attention_rows_ker
         int i, gg;
         run.find(a, min(col, n_rows - 1 - row0), i, gg);
         origin = near_origin(reinterpret_cast<const int2 *>(a.q_xy)[sp.q0 + i]);
-        float steepest = 0.0f;
-        for (int e = 0; e < a.group; ++e) steepest = fmaxf(steepest, fabsf(a.slopes[head * a.group + e]) * kLog2e);
-        largest = near_limit<T>() * 256.0f / steepest;
+        largest = near_largest<T, CAP>(a, head, scale);
         const int ax = (int)(qx * 16.0f) - origin.x, ay = (int)(qy * 16.0f) - origin.y;
         const float n = square_quanta(ax, ay), weight = slope2 / 256.0f;
         row_near = !a.lse && __all(!valid || near_enough(ax, ay, n, largest));

@@ -479,22 +479,20 @@ __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kern
         kx = (float)place.x * kPxPerQuantum;
         ky = (float)place.y * kPxPerQuantum;
     }
+    const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     float largest = 0.0f;
     int2 origin = make_int2(0, 0);
     bool keys_near = false;
     bf16x8 key_slots = {};
     if (DIST) {
         origin = near_origin(reinterpret_cast<const int2 *>(a.k_xy)[sp.k0 + min((int)key0 + col, sp.nk - 1)]);
-        float steepest = 0.0f;
-        for (int e = 0; e < a.group; ++e) steepest = fmaxf(steepest, fabsf(a.slopes[head * a.group + e]) * kLog2e);
-        largest = near_limit<T>() * 256.0f / steepest;
+        largest = near_largest<T, CAP>(a, head, scale);
         const int bx = (int)(kx * 16.0f) - origin.x, by = (int)(ky * 16.0f) - origin.y;
         const float n2 = square_quanta(bx, by);
         const NearSlots s = near_key(bx, by, n2);
         key_slots = __builtin_bit_cast(bf16x8, h ? s.half[1] : s.half[0]);
         keys_near = __all(!valid || near_enough(bx, by, n2, largest));
     }
-    const float scale = score_scale<CAP>(a), cap2 = a.cap * kLog2e;
     const int prefix = a.causal && a.prefix ? min(max(a.prefix[f], 0), sp.nk) : 0;
     // the first query that sees the workgroup's first key
     int begin = 0;

@@ -93,10 +93,12 @@ __device__ __forceinline__ float capped(float r, float cap2, float other) {
 }
 template <int CAP>
 __device__ __forceinline__ float cap_constant(float cap2) { return CAP == kLow ? cap2 : 0.0f; }
-// What products are multiplied by first.
+// What products are multiplied by first (finite, so that a hidden key's zero stays
+// one under caps near the smallest number).
 template <int CAP>
 __device__ __forceinline__ float score_scale(const AttentionArgs &a) {
-    return CAP == kHigh ? a.scale / a.cap : (CAP == kLow ? 2.0f * a.scale / a.cap : a.scale) * kLog2e;
+    if (CAP == kHigh) return a.scale / a.cap;
+    return CAP == kLow ? fminf(2.0f * kLog2e * a.scale / a.cap, 0x1p127f) : a.scale * kLog2e;
 }
 
 __device__ __forceinline__ int wave_max(int x) {
@@ -316,6 +318,15 @@ __device__ __forceinline__ int2 near_origin(int2 p) {
         y1 = max(y1, __shfl_xor(y1, d));
     }
     return make_int2(__builtin_amdgcn_readfirstlane((x0 + x1) / 2), __builtin_amdgcn_readfirstlane((y0 + y1) / 2));
+}
+
+// The largest |b|^2 that the heads of kv head `head` allow.  Without caps distances
+// are added in the products' units, which scales below 2^-40 leave no room for.
+template <typename T, int CAP>
+__device__ __forceinline__ float near_largest(const AttentionArgs &a, int head, float scale) {
+    float steepest = 0.0f;
+    for (int e = 0; e < a.group; ++e) steepest = fmaxf(steepest, fabsf(a.slopes[head * a.group + e]) * kLog2e);
+    return !CAP && scale < 0x1p-40f ? -1.0f : near_limit<T>() * 256.0f / steepest;
 }
 
 __device__ __forceinline__ bool near_enough(int x, int y, float n, float largest) {

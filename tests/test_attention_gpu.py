@@ -658,3 +658,27 @@ def test_inconsistent_frames(form, bad):
         if not ok[f]:
             keys = slice(f * n_k, (f + 1) * n_k)
             assert (dk[keys] == 7).all() and (dv[keys] == 7).all(), f
+
+
+@pytest.mark.parametrize("cap", [1e-30, 1e-37, 1e-38, 1e-40, 1e-45])
+def test_tiny_caps(cap):
+    """Down to the smallest number: the products no longer matter, and hidden
+    keys stay hidden."""
+    compare(make(50, [130, 20], [130, 20], 2, 2, 64, torch.bfloat16, cap=cap, hidden=0.3, distance=True))
+
+
+@pytest.mark.parametrize("scale", [1e-10, 1e-30, 1e-36, 1e-38, 1e-40])
+@pytest.mark.parametrize("cap", [0.0, 5.0, 100.0])
+def test_tiny_scales(scale, cap):
+    """Distances alone make the scores, with lse and without."""
+    counts = [(53 * f) % 260 for f in range(80)]
+    c = make(51, counts, counts, 8, 4, 64, torch.bfloat16, distance=True, sigma=(10.0, 300.0), cap=cap)
+    c["scale"] = scale
+    got = call(c)
+    want, bound = reference(c)
+    for n in want:
+        ref.check(got[n], want[n], bound[n], n)
+    d = {n: (t.cuda() if torch.is_tensor(t) else t) for n, t in c.items()}
+    off = torch.tensor(c["q_off"], dtype=torch.int32).cuda()
+    out = flock.attention_frames(d["q"], d["k"], d["v"], off, q_xy=d["q_xy"], slopes=d["slopes"], scale=scale, cap=cap)
+    ref.check(out, want["out"], bound["out"], "out")
