@@ -809,9 +809,9 @@ flock_status check_attention_pointers(const flock::AttentionArgs &a) {
     if (!aligned(a.q_offsets, 4) || !aligned(a.k_offsets, 4) || !aligned(a.slopes, 4) || !aligned(a.prefix, 4))
         return fail(FLOCK_EINVAL, "q_offsets, k_offsets, slopes and prefix must be 4-byte aligned");
     if (!aligned(a.lse, 8)) return fail(FLOCK_EINVAL, "lse must be 8-byte aligned");
-    // rows are numbered in 31 bits
-    if ((int64_t)a.total_q * a.group > 0x7fffff00LL)
-        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 rows of queries and shared heads");
+    // rows and keys are numbered in 31 bits, up to the end of the tile after the last
+    if ((int64_t)a.total_q * a.group > 0x7fffff00LL || a.total_k > 0x7fffff00)
+        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 - 256 keys, or rows of queries and shared heads");
     return FLOCK_OK;
 }
 

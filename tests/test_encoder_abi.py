@@ -174,3 +174,13 @@ def test_attention_takes_batches_within_a_launch(kwargs):
 def test_attention_backward_rejects_too_many_keys():
     assert attention_back(tk=2 ** 31 - 1, tq=8, frames=1, hq=2, hk=2, ks=128, vs=128, dks=128, dvs=128) == \
         binding.FLOCK_EUNSUPPORTED
+
+
+def test_attention_rejects_keys_beyond_its_numbers():
+    """A loop over a frame's keys looks up to two tiles of 128 ahead, in 31 bits."""
+    most = 2 ** 31 - 256
+    assert attention(frames=1, tq=1, tk=most + 1, hq=1, hk=1) == binding.FLOCK_EUNSUPPORTED
+    assert "keys" in binding.lib().flock_last_error().decode()
+    assert attention(frames=1, tq=1, tk=most, hq=1, hk=1, lse=FAKE4) == binding.FLOCK_EINVAL
+    if not torch.cuda.is_available():
+        assert attention(frames=1, tq=1, tk=most, hq=1, hk=1) == binding.FLOCK_EDEVICE
