@@ -374,9 +374,14 @@ def _like(t, stream):
     return _new(t.shape, t.dtype, t.device, stream)
 
 
+_MOST = 2 ** 31 - 1  # rows, birds and frames are numbered in 32 bits; ctypes would cut what is more
+
+
 def _rows(t, name, like=None):
     """Stride of a device matrix [rows, width] whose rows are contiguous."""
     shape = t.shape
+    if max(shape, default=0) > _MOST:
+        raise ValueError(f"{name} has more than 2^31 - 1 rows or columns")
     if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name} must be a device matrix with contiguous rows")
     stride = t.stride()
@@ -393,6 +398,8 @@ def _heads(t, name, like=None):
     shape = t.shape
     if len(shape) != 3 or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor [birds, heads, head_dim] with contiguous rows")
+    if max(shape) > _MOST:
+        raise ValueError(f"{name} has more than 2^31 - 1 birds, heads or dimensions")
     n, heads, dim = shape
     stride = t.stride()
     if n > 0 and ((stride[2] != 1 and dim > 1) or (stride[1] != dim and heads > 1)):
@@ -552,7 +559,7 @@ def _attention(q, k, v, q_offsets, k_offsets, q_xy, k_xy, slopes, keep, prefix, 
         raise ValueError("k and v must have one shape, with the head_dim of q")
     index = q.get_device()
     frames = q_offsets.numel() - 1
-    if frames < 0 or q_offsets.dim() != 1:
+    if not 0 <= frames <= _MOST or q_offsets.dim() != 1:
         raise ValueError("q_offsets must be a contiguous [F + 1] tensor")
     qo = _vector(q_offsets, "q_offsets", torch.int32, frames + 1, index)
     ko = qo

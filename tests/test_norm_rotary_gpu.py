@@ -278,3 +278,17 @@ def test_rotary_of_more_birds_than_a_launch_holds(interleaved):
     flock.rotary_frames(q, None, None, axes, time=time, interleaved=interleaved, out=(q, None))
     for r, w in zip(ends(n, most), want):
         assert torch.equal(q[r], w)
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """Not cut to what is left modulo 2^32."""
+    wide = torch.zeros(1, 8, dtype=torch.bfloat16, device="cuda").expand(2 ** 31 + 5, 8)
+    with pytest.raises(ValueError, match="2\\^31"):
+        flock.layer_norm_rows(wide)
+    birds = wide[:, None]
+    one = torch.zeros(1, dtype=torch.int32, device="cuda").expand(2 ** 31 + 5)
+    with pytest.raises(ValueError, match="2\\^31"):
+        flock.rotary_frames(birds, None, None, flock.RotaryAxes(time=[1.0]), time=one)
+    off = torch.zeros(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="2\\^31"):
+        flock.attention_frames(birds, birds, birds, off)
