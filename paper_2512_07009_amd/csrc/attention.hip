@@ -9,6 +9,7 @@
 //   backward: P = exp(s - lse), delta_i = dout_i.out_i, dP = dout_i.v_j
 //   dS = P (dP - delta), dT = dS (1 - (t / cap)^2)
 //   dq = scale dT k, dk = scale dT^T q, dv = P^T dout, dslope_h = -sum dS d2
+// (out is rounded, and with it delta; what that leaves in sum_j dS is taken off)
 //
 // Queries of the heads that share a kv head are packed as rows r = (i, g) of
 // one problem per frame and kv head, so that shared keys are read once and
@@ -40,10 +41,10 @@ using namespace attention;
 // heads of 64 the products take 8 x 32 cycles, the softmax at least 320 (a multiply
 // and add, half a maximum, an exponential at half the rate, a sum and half a rounding
 // to 16 bits each), and distances, caps and masks add to that.  8 heads of 64: 96
-// tracks in order 885 us, 0.63 PFLOP/s (VALU 69% of the time, matrix cores 38%); 64
-// frames of 2000 with distances and lse 1037 us, 0.46 (91%, 23%), with distances and
-// cap 1075 us, 0.44 (86%, 25%).  24 frames of 8000, 8 heads of 128 over 2: 8.9 ms, 0.64
-// PFLOP/s (51%, 33%); registers leave two waves a SIMD there, which do not cover
+// tracks in order 875 us, 0.70 PFLOP/s (VALU 69% of the time, matrix cores 38%); 64
+// frames of 2000 with distances and lse 999 us, 0.52 (91%, 23%), with distances and
+// cap 1065 us, 0.49 (84%, 24%).  24 frames of 8000, 8 heads of 128 over 2: 8.9 ms, 0.71
+// PFLOP/s (50%, 32%); registers leave two waves a SIMD there, which do not cover
 // each other's waits, and a third would spill.
 // ---------------------------------------------------------------------------
 

@@ -1,6 +1,7 @@
 // attention_backward.hip - gradients of attention (the formulas stand in
 // attention.hip): two kernels, each summing its own outputs in a fixed order,
-// at the price of computing scores and dP twice (seven products for five).
+// at the price of computing scores and dP twice, and P K beside dS K (eight
+// products for five).
 
 #include "attention_common.h"
 
@@ -48,10 +49,10 @@ using DqTile = KeyTile<DP, DP <= 96 ? 64 : 32, Pitch<DP>::kBoth, Pitch<DP>::kRow
 // gradients take from here, and each workgroup's share of its heads' slope
 // gradients (zeros from one without rows, so that every share is written).
 // Bound by vector instructions: 64 frames of 2000, 8 heads of 64 with distances
-// 1460 us, 0.49 PFLOP/s of its three products (VALU 76% of the time, matrix cores
-// 25%); 96 tracks in order 1181 us, 0.71 (66%, 44%).
+// 1550 us, 0.68 PFLOP/s of its four products (VALU 74% of the time, matrix cores
+// 32%); 96 tracks in order 1611 us, 0.76 (56%, 38%: two waves a SIMD).
 // dS is rounded to the operands' type as a factor of the product with K: that
-// makes dq's error 2.7e-3 of its norm in bfloat16 where rounding dq alone costs
+// makes dq's error 2.4e-3 of its norm in bfloat16 where rounding dq alone costs
 // 1.7e-3.
 template <typename T, int DP, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, (DP >= 96 && DIST) || (DP == 128 && CAP) ? 1 : 2) attention_dq_kernel(AttentionBackwardArgs b) {
@@ -440,9 +441,9 @@ struct RowTile {
 // products are S = Q K^T and dP = dO V^T here, so that a lane holds one key.  64 keys
 // a wave would halve what is read of LDS for each, but leave one wave a SIMD (4.37 ms
 // against 3.67 for a training step on 64 frames of 2000, 8 heads of 64 with
-// distances).  Same frames, 1454 us, 0.65 PFLOP/s of four products (VALU 43%, matrix cores 36%, LDS 41% of the time, a fifth
-// of that bank conflicts of rows that are read both ways); the phases of the two
-// waves a SIMD overlap only in part.
+// distances).  Same frames, 1451 us, 0.72 PFLOP/s of four products (VALU 42%, matrix
+// cores 35%, LDS 40% of the time, a fifth of that bank conflicts of rows that are
+// read both ways); the phases of the two waves a SIMD overlap only in part.
 template <typename T, int DP, bool DIST, int CAP>
 __global__ void __launch_bounds__(kThreads, DP <= 64 ? 2 : 1) attention_dkv_kernel(AttentionBackwardArgs b) {
     using F = typename Frag<T>::type;
