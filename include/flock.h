@@ -431,6 +431,64 @@ flock_status layer_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t
 size_t layer_norm_rows_backward_workspace(int32_t rows, int32_t width);
 
 /*
+ * rms_norm_rows - root-mean-square norm of every row, with an optional residual.
+ *
+ *   h = x, or x + residual rounded to dtype, which is written to sum;
+ *   y = h * rstd * weight,  rstd = 1 / sqrt(sum h^2 / width + eps)
+ * Squares are summed in 32 bits.
+ *
+ * Arguments: as for layer_norm_rows, without bias and mean.
+ */
+flock_status rms_norm_rows(int32_t dtype, const void *x, int64_t x_stride, const void *residual,
+                           int64_t residual_stride, int32_t rows, int32_t width, const float *weight, float eps,
+                           void *y, int64_t y_stride, void *sum, int64_t sum_stride, float *rstd, void *stream);
+
+/*
+ * rms_norm_rows_backward - gradients of rms_norm_rows.
+ *
+ * With xh = x * rstd and g = grad_y * weight, per row
+ *   grad_x = rstd * (g - xh * mean(g * xh)) (+ grad_sum)
+ * and over the rows, in a fixed order, grad_weight = sum grad_y * xh.
+ *
+ * Arguments: as for layer_norm_rows_backward, without mean and grad_bias;
+ * workspace sized by rms_norm_rows_backward_workspace(...).
+ */
+flock_status rms_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t grad_y_stride,
+                                    const void *grad_sum, int64_t grad_sum_stride, const void *x,
+                                    int64_t x_stride, int32_t rows, int32_t width, const float *weight,
+                                    const float *rstd, void *grad_x, int64_t grad_x_stride, float *grad_weight,
+                                    void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace rms_norm_rows_backward needs for its column sums. */
+size_t rms_norm_rows_backward_workspace(int32_t rows, int32_t width);
+
+/*
+ * rms_norm_rows_i8 - rms_norm_rows with its output in 8 bits.
+ *
+ * y as for rms_norm_rows, in 32 bits, is not written; per row
+ *   scale = max |y| / 127,  q = y / scale to the nearest whole number, ties to even
+ * so that y is scale * q to half a scale.  A row whose largest |y| is below
+ * 2^-100 has scale and q 0; one with a value that is not finite has scale NaN
+ * and q 0.
+ *
+ * Arguments: as for rms_norm_rows, and
+ *   q              device out, int8[rows][width], rows q_stride bytes apart
+ *                  (>= width; what lies between rows is left as it was).
+ *   scale          device out, float[rows].
+ */
+flock_status rms_norm_rows_i8(int32_t dtype, const void *x, int64_t x_stride, const void *residual,
+                              int64_t residual_stride, int32_t rows, int32_t width, const float *weight,
+                              float eps, int8_t *q, int64_t q_stride, float *scale, void *sum,
+                              int64_t sum_stride, void *stream);
+
+/*
+ * quantize_rows - rows in 8 bits with a scale each: q and scale as for
+ * rms_norm_rows_i8, with y = x.  A weight's rows are its outputs.
+ */
+flock_status quantize_rows(int32_t dtype, const void *x, int64_t x_stride, int32_t rows, int32_t width, int8_t *q,
+                           int64_t q_stride, float *scale, void *stream);
+
+/*
  * rotary_frames - rotary positions of queries and keys from time, y and x.
  *
  * Pair p of a head's dimensions is turned by angle_p = position * freq[p]:

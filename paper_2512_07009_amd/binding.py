@@ -77,6 +77,16 @@ def lib() -> ctypes.CDLL:
         L.layer_norm_rows_backward.restype = i32
         L.layer_norm_rows_backward_workspace.argtypes = [i32, i32]
         L.layer_norm_rows_backward_workspace.restype = sz
+        L.rms_norm_rows.argtypes = [i32, p, i64, p, i64, i32, i32, p, f32, p, i64, p, i64, p, p]
+        L.rms_norm_rows.restype = i32
+        L.rms_norm_rows_backward.argtypes = [i32, p, i64, p, i64, p, i64, i32, i32, p, p, p, i64, p, p, sz, p]
+        L.rms_norm_rows_backward.restype = i32
+        L.rms_norm_rows_backward_workspace.argtypes = [i32, i32]
+        L.rms_norm_rows_backward_workspace.restype = sz
+        L.rms_norm_rows_i8.argtypes = [i32, p, i64, p, i64, i32, i32, p, f32, p, i64, p, p, i64, p]
+        L.rms_norm_rows_i8.restype = i32
+        L.quantize_rows.argtypes = [i32, p, i64, i32, i32, p, i64, p, p]
+        L.quantize_rows.restype = i32
         L.rotary_frames.argtypes = [i32, p, i64, p, i64, i32, i32, i32, i32, p, p, p, i32, i32, i32, i32, i32,
                                     p, i64, p, i64, p]
         L.rotary_frames.restype = i32
@@ -485,6 +495,129 @@ def layer_norm_rows_backward(grad_y: torch.Tensor, h: torch.Tensor, weight: torc
           width, wp, mp, rp, dx.data_ptr(), width, dw.data_ptr(), db.data_ptr(),
           _ptr(ws), ws_bytes)
     return dx, dw, db
+
+
+def rms_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-6,
+                  residual: torch.Tensor | None = None, out=None, stream=None):
+    """Root-mean-square norm of every row of x [N, width] (float32, float16 or
+    bfloat16), or of x + residual, with a float32 weight.
+
+    Returns (y, h, rstd): h is what was normalised (x itself, or the sum in x's
+    type), and h and rstd (float32 [N]) are what rms_norm_rows_backward takes.
+    out: optional (y, h, rstd) tensors to write into (h only with residual).
+    """
+    code, xs = _dtype(x), _rows(x, "x")
+    n, width = x.shape
+    dev = x.device
+    index = dev.index
+    wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
+    rs = _rows(residual, "residual", x) if residual is not None else 0
+    if out is None:
+        y = _like(x, stream)
+        h = _like(x, stream) if residual is not None else x
+        rstd = _new(n, torch.float32, dev, stream)
+        ys = hs = width
+    else:
+        y, h, rstd = out
+        ys = _rows(y, "y", x)
+        hs = _rows(h, "h", x) if residual is not None else 0
+        _vector(rstd, "rstd", torch.float32, n, index)
+        if residual is None:
+            h = x
+    _call(lib().rms_norm_rows, dev, stream, code, x.data_ptr(), xs, _ptr(residual), rs, n, width, wp, eps, y.data_ptr(),
+          ys, h.data_ptr() if residual is not None else None, hs, rstd.data_ptr())
+    return y, h, rstd
+
+
+def rms_norm_rows_backward(grad_y: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None, rstd: torch.Tensor,
+                           grad_sum: torch.Tensor | None = None, stream=None):
+    """Gradients of rms_norm_rows from its h and rstd; grad_sum is the gradient
+    that h got elsewhere.
+
+    Returns (grad_x in h's type, also the residual's gradient; grad_weight
+    float32 [width]).
+    """
+    code, xs = _dtype(h), _rows(h, "h")
+    n, width = h.shape
+    dev = h.device
+    gs = _rows(grad_y, "grad_y", h)
+    ss = _rows(grad_sum, "grad_sum", h) if grad_sum is not None else 0
+    index = dev.index
+    wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
+    rp = _vector(rstd, "rstd", torch.float32, n, index)
+    dx = _like(h, stream)
+    dw = _new(width, torch.float32, dev, stream)
+    L = lib()
+    ws_bytes = L.rms_norm_rows_backward_workspace(n, width)
+    ws = _workspace(ws_bytes, dev, stream)
+    _call(L.rms_norm_rows_backward, dev, stream, code, grad_y.data_ptr(), gs, _ptr(grad_sum), ss, h.data_ptr(), xs, n,
+          width, wp, rp, dx.data_ptr(), width, dw.data_ptr(), _ptr(ws), ws_bytes)
+    return dx, dw
+
+
+def _whole(n, width, dev, stream):
+    """int8 [n, width], rows 16 bytes or a multiple apart: what products load fastest."""
+    t = _new((n, (width + 15) // 16 * 16), torch.int8, dev, stream)
+    return t if width % 16 == 0 else t[:, :width]
+
+
+def _whole_rows(t, name, shape, index):
+    """Stride of an int8 device matrix of this shape whose rows are contiguous."""
+    if t.dtype != torch.int8 or t.get_device() != index or t.shape != shape:
+        raise ValueError(f"{name} must be an int8 {list(shape)} tensor on the features' device")
+    return _rows(t, name)
+
+
+def rms_norm_rows_i8(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-6,
+                     residual: torch.Tensor | None = None, out=None, stream=None):
+    """rms_norm_rows with its output in 8 bits, for linear_rows_i8.
+
+    Returns (q, scale, h): q int8 [N, width] and scale float32 [N], so that the
+    norm is scale[:, None] * q to half a scale; h as for rms_norm_rows.
+    out: optional (q, scale, h) tensors to write into (h only with residual).
+    """
+    code, xs = _dtype(x), _rows(x, "x")
+    n, width = x.shape
+    dev = x.device
+    index = dev.index
+    wp = _vector(weight, "weight", torch.float32, width, index) if weight is not None else None
+    rs = _rows(residual, "residual", x) if residual is not None else 0
+    if out is None:
+        q = _whole(n, width, dev, stream)
+        scale = _new(n, torch.float32, dev, stream)
+        h = _like(x, stream) if residual is not None else x
+        qs, hs = (width + 15) // 16 * 16, width
+    else:
+        q, scale, h = out
+        qs = _whole_rows(q, "q", x.shape, index)
+        _vector(scale, "scale", torch.float32, n, index)
+        hs = _rows(h, "h", x) if residual is not None else 0
+        if residual is None:
+            h = x
+    _call(lib().rms_norm_rows_i8, dev, stream, code, x.data_ptr(), xs, _ptr(residual), rs, n, width, wp, eps, q.data_ptr(),
+          qs, scale.data_ptr(), h.data_ptr() if residual is not None else None, hs)
+    return q, scale, h
+
+
+def quantize_rows(x: torch.Tensor, out=None, stream=None):
+    """Rows of x [N, width] (float32, float16 or bfloat16) in 8 bits: (q int8
+    [N, width], scale float32 [N]), x being scale[:, None] * q to half a scale.
+    A weight [outputs, width] gets a scale for each output.
+    out: optional (q, scale) tensors to write into.
+    """
+    code, xs = _dtype(x), _rows(x, "x")
+    n, width = x.shape
+    dev = x.device
+    if out is None:
+        q = _whole(n, width, dev, stream)
+        scale = _new(n, torch.float32, dev, stream)
+        qs = (width + 15) // 16 * 16
+    else:
+        q, scale = out
+        qs = _whole_rows(q, "q", x.shape, dev.index)
+        _vector(scale, "scale", torch.float32, n, dev.index)
+    _call(lib().quantize_rows, dev, stream, code, x.data_ptr(), xs, n, width, q.data_ptr(), qs, scale.data_ptr())
+    return q, scale
 
 
 class RotaryAxes:

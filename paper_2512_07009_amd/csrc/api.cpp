@@ -944,6 +944,138 @@ flock_status layer_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t
     return err == hipSuccess ? FLOCK_OK : hip_fail(err, "layer norm backward kernels");
 }
 
+static flock_status rms_rows(int32_t dtype, flock::RmsArgs a, int32_t rows, void *stream) {
+    g_error[0] = '\0';
+    flock_status st = check_norm(dtype, rows, a.width);
+    if (st != FLOCK_OK) return st;
+    if (!std::isfinite(a.eps) || !(a.eps >= 0.0f)) return fail(FLOCK_EINVAL, "eps must be finite and >= 0");
+    if (a.x_stride < 0 || (a.residual && a.residual_stride < 0)) return fail(FLOCK_EINVAL, "input strides must be >= 0");
+    if (a.y_stride < a.width || (a.residual && a.sum_stride < a.width))
+        return fail(FLOCK_EINVAL, "output strides must hold a row");
+    if (rows == 0) return FLOCK_OK;
+    if (!a.x || !a.y) return fail(FLOCK_EINVAL, "x and the output must be non-NULL");
+    if (a.residual && !a.sum) return fail(FLOCK_EINVAL, "sum must be non-NULL with residual");
+    const size_t size = dtype_size(dtype);
+    if (!aligned(a.x, size) || (!a.scale && !aligned(a.y, size)) || !aligned(a.residual, size) || !aligned(a.sum, size))
+        return fail(FLOCK_EINVAL, "x, residual, y and sum must be aligned to their elements");
+    if (!aligned(a.weight, 4) || !aligned(a.rstd, 4) || !aligned(a.scale, 4))
+        return fail(FLOCK_EINVAL, "weight, rstd and scale must be 4-byte aligned");
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    a.rows = rows;
+    if (!a.residual) {
+        a.sum = nullptr;
+        a.residual_stride = a.sum_stride = 0;
+    }
+    const hipError_t err = flock::launch_rms(a, dtype, reinterpret_cast<hipStream_t>(stream));
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "root-mean-square norm kernel launch");
+}
+
+flock_status rms_norm_rows(int32_t dtype, const void *x, int64_t x_stride, const void *residual,
+                           int64_t residual_stride, int32_t rows, int32_t width, const float *weight, float eps,
+                           void *y, int64_t y_stride, void *sum, int64_t sum_stride, float *rstd, void *stream) {
+    flock::RmsArgs a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.residual = residual;
+    a.residual_stride = residual_stride;
+    a.width = width;
+    a.weight = weight;
+    a.eps = eps;
+    a.y = y;
+    a.y_stride = y_stride;
+    a.sum = sum;
+    a.sum_stride = sum_stride;
+    a.rstd = rstd;
+    return rms_rows(dtype, a, rows, stream);
+}
+
+flock_status rms_norm_rows_i8(int32_t dtype, const void *x, int64_t x_stride, const void *residual,
+                              int64_t residual_stride, int32_t rows, int32_t width, const float *weight, float eps,
+                              int8_t *q, int64_t q_stride, float *scale, void *sum, int64_t sum_stride, void *stream) {
+    g_error[0] = '\0';
+    if (rows > 0 && !scale) return fail(FLOCK_EINVAL, "scale must be non-NULL");
+    flock::RmsArgs a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.residual = residual;
+    a.residual_stride = residual_stride;
+    a.width = width;
+    a.weight = weight;
+    a.eps = eps;
+    a.y = q;
+    a.y_stride = q_stride;
+    a.sum = sum;
+    a.sum_stride = sum_stride;
+    a.scale = scale;
+    return rms_rows(dtype, a, rows, stream);
+}
+
+flock_status quantize_rows(int32_t dtype, const void *x, int64_t x_stride, int32_t rows, int32_t width, int8_t *q,
+                           int64_t q_stride, float *scale, void *stream) {
+    g_error[0] = '\0';
+    if (rows > 0 && !scale) return fail(FLOCK_EINVAL, "scale must be non-NULL");
+    flock::RmsArgs a{};
+    a.x = x;
+    a.x_stride = x_stride;
+    a.width = width;
+    a.y = q;
+    a.y_stride = q_stride;
+    a.scale = scale;
+    a.as_is = 1;
+    return rms_rows(dtype, a, rows, stream);
+}
+
+size_t rms_norm_rows_backward_workspace(int32_t rows, int32_t width) {
+    return flock::rms_backward_workspace_bytes(rows, width, device_cus());
+}
+
+flock_status rms_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t grad_y_stride, const void *grad_sum,
+                                    int64_t grad_sum_stride, const void *x, int64_t x_stride, int32_t rows, int32_t width,
+                                    const float *weight, const float *rstd, void *grad_x, int64_t grad_x_stride,
+                                    float *grad_weight, void *workspace, size_t workspace_bytes, void *stream) {
+    g_error[0] = '\0';
+    flock_status st = check_norm(dtype, rows, width);
+    if (st != FLOCK_OK) return st;
+    if (grad_y_stride < 0 || x_stride < 0 || (grad_sum && grad_sum_stride < 0))
+        return fail(FLOCK_EINVAL, "input strides must be >= 0");
+    if (grad_x_stride < width) return fail(FLOCK_EINVAL, "output strides must hold a row");
+    if (rows > 0 && (!grad_y || !x || !rstd || !grad_x))
+        return fail(FLOCK_EINVAL, "grad_y, x, rstd and grad_x must be non-NULL");
+    const size_t size = dtype_size(dtype);
+    if (!aligned(grad_y, size) || !aligned(x, size) || !aligned(grad_sum, size) || !aligned(grad_x, size))
+        return fail(FLOCK_EINVAL, "grad_y, grad_sum, x and grad_x must be aligned to their elements");
+    if (!aligned(weight, 4) || !aligned(rstd, 4) || !aligned(grad_weight, 4))
+        return fail(FLOCK_EINVAL, "weight, rstd and grad_weight must be 4-byte aligned");
+    if (rows == 0 && !grad_weight) return FLOCK_OK;
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    Workspace ws;
+    st = ws.take(workspace, workspace_bytes,
+                 grad_weight ? flock::rms_backward_workspace_bytes(rows, width, dev->n_cus) : 0, s);
+    if (st != FLOCK_OK) return st;
+    flock::RmsBackwardArgs a{};
+    a.grad_y = grad_y;
+    a.grad_y_stride = grad_y_stride;
+    a.grad_sum = grad_sum;
+    a.grad_sum_stride = grad_sum ? grad_sum_stride : 0;
+    a.x = x;
+    a.x_stride = x_stride;
+    a.rows = rows;
+    a.width = width;
+    a.weight = weight;
+    a.rstd = rstd;
+    a.grad_x = grad_x;
+    a.grad_x_stride = grad_x_stride;
+    hipError_t err = flock::launch_rms_backward(a, dtype, ws.ptr, dev->n_cus, grad_weight, s);
+    const hipError_t ferr = ws.release(s);
+    if (err == hipSuccess) err = ferr;
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "root-mean-square norm backward kernels");
+}
+
 flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                            int32_t total, int32_t q_heads, int32_t k_heads, int32_t head_dim, const int32_t *xy,
                            const int32_t *time, const double *freq, int32_t n_time, int32_t n_y, int32_t n_x,

@@ -250,6 +250,53 @@ size_t norm_backward_workspace_bytes(int64_t rows, int32_t width, int n_cus);
 hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspace, int n_cus, float *grad_weight,
                                 float *grad_bias, hipStream_t stream);
 
+// Root-mean-square norm of rows, or rows as they are, in the features' type or in 8 bits.
+struct RmsArgs {
+    const void *x, *residual;          // [rows][width], strides in elements; residual may be nullptr
+    int64_t x_stride, residual_stride;
+    int64_t rows;
+    int32_t width;
+    const float *weight;               // [width] or nullptr
+    float eps;
+    void *y, *sum;                     // y is int8 where scale is given; sum only with residual
+    int64_t y_stride, sum_stride;
+    float *rstd, *scale;               // [rows] or nullptr
+    int32_t as_is;                     // 1: no norm (with scale)
+
+    void advance(int64_t first, size_t size) {
+        move_on(x, first * x_stride, size);
+        move_on(residual, first * residual_stride, size);
+        move_on(y, first * y_stride, scale ? 1 : size);
+        move_on(sum, first * sum_stride, size);
+        move_on(rstd, first, sizeof(float));
+        move_on(scale, first, sizeof(float));
+    }
+};
+hipError_t launch_rms(const RmsArgs &a, int32_t dtype, hipStream_t stream);
+
+struct RmsBackwardArgs {
+    const void *grad_y, *grad_sum, *x;  // grad_sum may be nullptr
+    int64_t grad_y_stride, grad_sum_stride, x_stride;
+    int64_t rows;
+    int32_t width;
+    const float *weight;                // [width] or nullptr
+    const float *rstd;                  // [rows]
+    void *grad_x;
+    int64_t grad_x_stride;
+    float *partial;                     // set by launch_rms_backward
+
+    void advance(int64_t first, size_t size) {
+        move_on(grad_y, first * grad_y_stride, size);
+        move_on(grad_sum, first * grad_sum_stride, size);
+        move_on(x, first * x_stride, size);
+        move_on(grad_x, first * grad_x_stride, size);
+        move_on(rstd, first, sizeof(float));
+    }
+};
+size_t rms_backward_workspace_bytes(int64_t rows, int32_t width, int n_cus);
+hipError_t launch_rms_backward(RmsBackwardArgs a, int32_t dtype, void *workspace, int n_cus, float *grad_weight,
+                               hipStream_t stream);
+
 constexpr int kRotaryMaxPairs = 128;
 
 struct RotaryArgs {

@@ -15,29 +15,12 @@
 // (5.0 TB/s) and 4 us for the columns' sums; 500 rows: 3.7 us, less than a call
 // takes on the host.
 
-#include "encoder_common.h"
+#include "norm_common.h"
 
 namespace flock {
 namespace {
 
-constexpr int kThreads = 256;
-
-// Sum over the TPR lanes that share a row; every lane gets it.  slot: LDS for
-// the four waves' sums (TPR = 256), a different one in each of the calls
-// between two barriers.
-template <int TPR>
-__device__ __forceinline__ float row_sum(float x, float *slot) {
-    constexpr int kLanes = TPR < 64 ? TPR : 64;
-#pragma unroll
-    for (int d = kLanes / 2; d > 0; d >>= 1) x += __shfl_xor(x, d);
-    if (TPR > 64) {
-        const int wave = threadIdx.x >> 6;
-        if ((threadIdx.x & 63) == 0) slot[wave] = x;
-        __syncthreads();
-        x = (slot[0] + slot[1]) + (slot[2] + slot[3]);
-    }
-    return x;
-}
+using namespace norm;
 
 template <typename T, int VEC, int ITER, int TPR>
 __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
@@ -285,80 +268,6 @@ __global__ void __launch_bounds__(kThreads) norm_columns_kernel(NormBackwardArgs
     a.partial[(int64_t)blockIdx.y * 2 * a.width + a.width + c] = db;
 }
 
-// Sum of the blocks' shares, in a fixed order: 16 columns a block, 64 lanes of
-// shares each (64 columns and 16 lanes: 16 workgroups for 512 columns, 20 us for
-// 1024 shares).
-__global__ void __launch_bounds__(1024) norm_reduce_kernel(const float *partial, int n, int width, float *dw,
-                                                           float *db) {
-    __shared__ float part[64][16];
-    const int lane = threadIdx.x & 15, share = threadIdx.x >> 4;
-    const int c = blockIdx.x * 16 + lane;
-    float s = 0.0f;
-    if (c < 2 * width) {
-#pragma unroll 4
-        for (int i = share; i < n; i += 64) s += partial[(int64_t)i * 2 * width + c];
-    }
-    part[share][lane] = s;
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) {
-        __syncthreads();
-        if (share < d) part[share][lane] += part[share + d][lane];
-    }
-    if (share != 0 || c >= 2 * width) return;
-    if (c < width) {
-        if (dw) dw[c] = part[0][lane];
-    } else if (db) {
-        db[c - width] = part[0][lane];
-    }
-}
-
-// fn(ITER, TPR) for a row of `width`: TPR lanes a row, ITER packs a lane.  A pack a
-// lane up to a wave (the fewest lanes of 8, 16, 32 and 64), then 2 or 4 packs a lane
-// of a wave, then of four waves; wide() above 4 packs x 256 lanes.  2 or 3 packs over
-// 32 lanes instead were slower (30000 rows of 333 fp32 64 -> 69 us with the backward
-// pass).  64 million bfloat16 elements, forward and backward: rows of 1500 300 us, of
-// 2048 230, of 6000 280, of 20000 (wide) 558; the bytes alone take 126.
-template <int VEC, typename F, typename W>
-hipError_t with_shape(int32_t width, F &&fn, W &&wide) {
-    const int packs = (width + VEC - 1) / VEC;
-    if (packs <= 8) return fn(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
-    if (packs <= 16) return fn(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
-    if (packs <= 32) return fn(std::integral_constant<int, 1>{}, std::integral_constant<int, 32>{});
-    if (packs <= 64) return fn(std::integral_constant<int, 1>{}, std::integral_constant<int, 64>{});
-    if (packs <= 128) return fn(std::integral_constant<int, 2>{}, std::integral_constant<int, 64>{});
-    if (packs <= 256) return fn(std::integral_constant<int, 4>{}, std::integral_constant<int, 64>{});
-    if (packs <= 512) return fn(std::integral_constant<int, 2>{}, std::integral_constant<int, 256>{});
-    if (packs <= 1024) return fn(std::integral_constant<int, 4>{}, std::integral_constant<int, 256>{});
-    return wide();
-}
-
-// launch(part, blocks) over the rows of a, by as many as a launch holds.  Parts
-// begin at a group of rows, so that a row gets the same lanes in any of them.
-template <typename T, typename A, typename F>
-hipError_t by_parts(A a, int rows_per_block, F &&launch) {
-    const int64_t rows = a.rows, most = kMaxWorkgroups * rows_per_block;
-    hipError_t err = hipSuccess;
-    for (int64_t first = 0; first < rows && err == hipSuccess; first += most) {
-        A part = a;
-        part.rows = std::min(rows - first, most);
-        part.advance(first, sizeof(T));
-        launch(part, dim3((uint32_t)((part.rows + rows_per_block - 1) / rows_per_block)));
-        err = hipGetLastError();
-    }
-    return err;
-}
-
-constexpr int kWideShares = 64;
-
-// Blocks of the backward pass: enough to fill the card (four of 256 threads a
-// compute unit; with 4 packs of 16-bit elements a lane registers let two of them
-// run at a time, the others follow), and each block's share of the weight's gradient
-// is one row of the workspace, 4 MB at 512 columns beside the 524 MB of the case above.
-int backward_blocks(int64_t rows, int n_cus) {
-    const int64_t blocks = (rows + 3) / 4;
-    return (int)std::min<int64_t>(std::max<int64_t>(blocks, 1), 4 * (int64_t)n_cus);
-}
-
 }  // namespace
 
 size_t norm_backward_workspace_bytes(int64_t rows, int32_t width, int n_cus) {
@@ -416,8 +325,8 @@ hipError_t launch_norm_backward(NormBackwardArgs a, int32_t dtype, void *workspa
                 });
     });
     if (err != hipSuccess || !(grad_weight || grad_bias)) return err;
-    hipLaunchKernelGGL(norm_reduce_kernel, dim3((2 * a.width + 15) / 16), dim3(1024), 0, stream, a.partial, shares,
-                       a.width, grad_weight, grad_bias);
+    hipLaunchKernelGGL(columns_kernel, dim3((2 * a.width + 15) / 16), dim3(1024), 0, stream, a.partial, shares,
+                       2 * a.width, a.width, grad_weight, grad_bias);
     return hipGetLastError();
 }
 
