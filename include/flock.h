@@ -489,6 +489,35 @@ flock_status quantize_rows(int32_t dtype, const void *x, int64_t x_stride, int32
                            int64_t q_stride, float *scale, void *stream);
 
 /*
+ * linear_rows_i8 - products of rows in 8 bits with weights in 8 bits.
+ *
+ *   y[m][n] = act(x_scale[m] * w_scale[n] * sum_k x[m][k] * w[n][k] + bias[n])
+ * Sums over k are exact; what follows is in 32 bits, with one rounding to dtype.
+ * act is the identity, or with gelu act(t) = t Phi(t), Phi being the normal
+ * distribution (to 1e-5 of itself).
+ *
+ * Arguments:
+ *   dtype          FLOCK_F32, FLOCK_F16 or FLOCK_BF16: y.
+ *   x              device in, int8[rows][width], rows x_stride bytes apart
+ *                  (0 <= x_stride < 2^24), from rms_norm_rows_i8 or
+ *                  quantize_rows.  Rows that begin at multiples of 16 bytes, of x
+ *                  and w both, are loaded fastest.
+ *   x_scale        device in, float[rows].
+ *   w              device in, int8[outputs][width], rows w_stride bytes apart.
+ *   w_scale        device in, float[outputs].
+ *   rows           >= 0.
+ *   width          1 .. 2^17 - 1.
+ *   outputs        1 .. 2^20.
+ *   bias           device in, float[outputs], or NULL (0).
+ *   gelu           0 or 1.
+ *   y              device out, [rows][outputs].
+ */
+flock_status linear_rows_i8(int32_t dtype, const int8_t *x, int64_t x_stride, const float *x_scale,
+                            const int8_t *w, int64_t w_stride, const float *w_scale, int32_t rows, int32_t width,
+                            int32_t outputs, const float *bias, int32_t gelu, void *y, int64_t y_stride,
+                            void *stream);
+
+/*
  * rotary_frames - rotary positions of queries and keys from time, y and x.
  *
  * Pair p of a head's dimensions is turned by angle_p = position * freq[p]:

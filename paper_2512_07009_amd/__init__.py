@@ -27,11 +27,11 @@ frame or of a track, with their gradients:
 
 from .binding import (FlockError, RotaryAxes, attention_frames, attention_frames_backward,  # noqa: F401
                       cluster_frames, density_frames, drinker_proximity_frames, eps_to_quanta, heatmap_frames,
-                      layer_norm_rows, layer_norm_rows_backward, lib, mask_capacity, mask_components_frames,
-                      quantize_rows, rms_norm_rows, rms_norm_rows_backward, rms_norm_rows_i8, roi_filter_frames,
+                      layer_norm_rows, layer_norm_rows_backward, lib, linear_rows_i8, mask_capacity,
+                      mask_components_frames, quantize_rows, rms_norm_rows, rms_norm_rows_backward, rms_norm_rows_i8, roi_filter_frames,
                       rotary_frames, version)
 
 __all__ = ["cluster_frames", "density_frames", "heatmap_frames", "roi_filter_frames", "drinker_proximity_frames",
            "mask_components_frames", "mask_capacity", "layer_norm_rows", "layer_norm_rows_backward", "rms_norm_rows",
-           "rms_norm_rows_backward", "rms_norm_rows_i8", "quantize_rows", "RotaryAxes",
+           "rms_norm_rows_backward", "rms_norm_rows_i8", "quantize_rows", "linear_rows_i8", "RotaryAxes",
            "rotary_frames", "attention_frames", "attention_frames_backward", "eps_to_quanta", "lib", "version", "FlockError"]

@@ -87,6 +87,8 @@ def lib() -> ctypes.CDLL:
         L.rms_norm_rows_i8.restype = i32
         L.quantize_rows.argtypes = [i32, p, i64, i32, i32, p, i64, p, p]
         L.quantize_rows.restype = i32
+        L.linear_rows_i8.argtypes = [i32, p, i64, p, p, i64, p, i32, i32, i32, p, i32, p, i64, p]
+        L.linear_rows_i8.restype = i32
         L.rotary_frames.argtypes = [i32, p, i64, p, i64, i32, i32, i32, i32, p, p, p, i32, i32, i32, i32, i32,
                                     p, i64, p, i64, p]
         L.rotary_frames.restype = i32
@@ -618,6 +620,42 @@ def quantize_rows(x: torch.Tensor, out=None, stream=None):
         _vector(scale, "scale", torch.float32, n, dev.index)
     _call(lib().quantize_rows, dev, stream, code, x.data_ptr(), xs, n, width, q.data_ptr(), qs, scale.data_ptr())
     return q, scale
+
+
+def linear_rows_i8(x: torch.Tensor, x_scale: torch.Tensor, weight: torch.Tensor, weight_scale: torch.Tensor,
+                   bias: torch.Tensor | None = None, gelu: bool = False, dtype=torch.bfloat16, out=None, stream=None):
+    """Product of rows in 8 bits, x int8 [N, width] with x_scale float32 [N], with a
+    weight in 8 bits, int8 [outputs, width] with weight_scale float32 [outputs]:
+    (x_scale x) (weight_scale weight)^T + bias, through gelu where asked, in
+    `dtype` [N, outputs].  Rows come from rms_norm_rows_i8 or quantize_rows.
+
+    bias: float32 [outputs].  gelu(t) is t Phi(t).  There are no gradients.
+    out: optional tensor to write into, whose type counts then.
+    """
+    if x.dtype != torch.int8 or weight.dtype != torch.int8:
+        raise ValueError("x and weight must be int8")
+    xs, ws = _rows(x, "x"), _rows(weight, "weight")
+    (n, width), (outputs, w_width) = x.shape, weight.shape
+    dev = x.device
+    index = dev.index
+    if w_width != width or weight.get_device() != index:
+        raise ValueError("weight must be [outputs, width] on x's device")
+    xp = _vector(x_scale, "x_scale", torch.float32, n, index)
+    wp = _vector(weight_scale, "weight_scale", torch.float32, outputs, index)
+    bp = _vector(bias, "bias", torch.float32, outputs, index) if bias is not None else None
+    if out is None:
+        code = _DTYPES.get(dtype)
+        if code is None:
+            raise ValueError(f"outputs of {dtype}: expected float32, float16 or bfloat16")
+        out = _new((n, outputs), dtype, dev, stream)
+        os = outputs
+    else:
+        code, os = _dtype(out), _rows(out, "out")
+        if out.shape != (n, outputs) or out.get_device() != index:
+            raise ValueError(f"out must be [{n}, {outputs}] on x's device")
+    _call(lib().linear_rows_i8, dev, stream, code, x.data_ptr(), xs, xp, weight.data_ptr(), ws, wp, n, width, outputs, bp,
+          int(gelu), out.data_ptr(), os)
+    return out
 
 
 class RotaryAxes:

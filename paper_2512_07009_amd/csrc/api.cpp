@@ -1076,6 +1076,46 @@ flock_status rms_norm_rows_backward(int32_t dtype, const void *grad_y, int64_t g
     return err == hipSuccess ? FLOCK_OK : hip_fail(err, "root-mean-square norm backward kernels");
 }
 
+flock_status linear_rows_i8(int32_t dtype, const int8_t *x, int64_t x_stride, const float *x_scale, const int8_t *w,
+                            int64_t w_stride, const float *w_scale, int32_t rows, int32_t width, int32_t outputs,
+                            const float *bias, int32_t gelu, void *y, int64_t y_stride, void *stream) {
+    g_error[0] = '\0';
+    if (!is_dtype(dtype)) return fail(FLOCK_EINVAL, "dtype = %d, expected FLOCK_F32, FLOCK_F16 or FLOCK_BF16", dtype);
+    if (rows < 0) return fail(FLOCK_EINVAL, "rows = %d < 0", rows);
+    if (width < 1 || width > flock::kLinearMaxWidth)
+        return fail(FLOCK_EINVAL, "width = %d outside 1..%d", width, flock::kLinearMaxWidth);
+    if (outputs < 1 || outputs > (1 << 20)) return fail(FLOCK_EINVAL, "outputs = %d outside 1..2^20", outputs);
+    if (gelu != 0 && gelu != 1) return fail(FLOCK_EINVAL, "gelu = %d, expected 0 or 1", gelu);
+    if (x_stride < 0 || w_stride < 0 || x_stride > flock::kLinearMaxStride || w_stride > flock::kLinearMaxStride)
+        return fail(FLOCK_EINVAL, "strides of x and w outside 0..%lld", (long long)flock::kLinearMaxStride);
+    if (y_stride < outputs) return fail(FLOCK_EINVAL, "y's stride must hold a row");
+    if (rows == 0) return FLOCK_OK;
+    if (!x || !x_scale || !w || !w_scale || !y)
+        return fail(FLOCK_EINVAL, "x, x_scale, w, w_scale and y must be non-NULL");
+    if (!aligned(y, dtype_size(dtype))) return fail(FLOCK_EINVAL, "y must be aligned to its elements");
+    if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(bias, 4))
+        return fail(FLOCK_EINVAL, "x_scale, w_scale and bias must be 4-byte aligned");
+    const DeviceInfo *dev = nullptr;
+    const flock_status st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    flock::LinearArgs a{};
+    a.x = x;
+    a.w = w;
+    a.x_stride = x_stride;
+    a.w_stride = w_stride;
+    a.rows = rows;
+    a.width = width;
+    a.outputs = outputs;
+    a.x_scale = x_scale;
+    a.w_scale = w_scale;
+    a.bias = bias;
+    a.gelu = gelu;
+    a.y = y;
+    a.y_stride = y_stride;
+    const hipError_t err = flock::launch_linear(a, dtype, dev->n_cus, reinterpret_cast<hipStream_t>(stream));
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "linear kernel launch");
+}
+
 flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                            int32_t total, int32_t q_heads, int32_t k_heads, int32_t head_dim, const int32_t *xy,
                            const int32_t *time, const double *freq, int32_t n_time, int32_t n_y, int32_t n_x,

@@ -297,6 +297,30 @@ size_t rms_backward_workspace_bytes(int64_t rows, int32_t width, int n_cus);
 hipError_t launch_rms_backward(RmsBackwardArgs a, int32_t dtype, void *workspace, int n_cus, float *grad_weight,
                                hipStream_t stream);
 
+// Products of rows and weights in 8 bits.
+constexpr int32_t kLinearMaxWidth = (1 << 17) - 1;   // sums stay within 32 bits
+constexpr int64_t kLinearMaxStride = (1 << 24) - 16; // a tile's rows lie within 2^32 bytes
+
+struct LinearArgs {
+    const int8_t *x, *w;               // [rows][width], [outputs][width], strides in bytes
+    int64_t x_stride, w_stride;
+    int64_t rows;
+    int32_t width, outputs;
+    const float *x_scale, *w_scale;    // [rows], [outputs]
+    const float *bias;                 // [outputs] or nullptr
+    int32_t gelu;
+    void *y;                           // [rows][outputs]
+    int64_t y_stride;
+    int32_t aligned, column_tiles;     // set by launch_linear: rows begin at 16 bytes; tiles of outputs
+
+    void advance(int64_t first, size_t size) {
+        move_on(x, first * x_stride, 1);
+        move_on(x_scale, first, sizeof(float));
+        move_on(y, first * y_stride, size);
+    }
+};
+hipError_t launch_linear(LinearArgs a, int32_t dtype, int n_cus, hipStream_t stream);
+
 constexpr int kRotaryMaxPairs = 128;
 
 struct RotaryArgs {
