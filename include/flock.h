@@ -628,6 +628,102 @@ flock_status attention_frames_backward(
 size_t attention_frames_backward_workspace(int32_t n_frames, int32_t total_q, int32_t total_k, int32_t q_heads,
                                            int32_t kv_heads, int32_t head_dim);
 
+/*
+ * Tracks: a paged cache of keys and values in 8 bits
+ * --------------------------------------------------
+ * What a bird's earlier detections leave for its later ones.  A cache is a pool of
+ * pages of FLOCK_TRACK_PAGE tokens, of any track each:
+ *   k          int8[pages][kv_heads][64][head_dim]
+ *   v          int8[pages][kv_heads][head_dim][64], token t of the page at place
+ *              16 * (t % 16 / 4) + 4 * (t / 16) + t % 4 of a dimension
+ *   k_scale, v_scale   float[pages][kv_heads]: keys and values are the whole
+ *              numbers times their page's and head's scale
+ * k and v are 16-byte aligned; a new pool may hold anything.  A table says which
+ * page holds which 64 tokens of a track:
+ *   table      device in, int32[n_tracks][max_pages], rows table_stride apart:
+ *              token t of track i is in page table[i][t / 64].  Numbers outside
+ *              0 .. pages - 1 stand for no page: what would go there is not kept,
+ *              and its tokens are not seen.
+ *   lengths    device in, int32[n_tracks]: the tokens of each track, the batch's
+ *              own among them, 0 .. 64 * max_pages.
+ *   offsets    device in, int32[n_tracks + 1]: the batch's rows of each track,
+ *              which are its last tokens, oldest first; none is allowed.
+ * A track whose offsets or length are out of range is passed over: nothing is
+ * appended, and its rows of outputs are left as they were.
+ */
+#define FLOCK_TRACK_PAGE 64
+
+/*
+ * append_tracks - keys and values of new detections into their tracks' pages.
+ *
+ * Keys are turned as by rotary_frames (in 32 bits, not rounded in between), and per
+ * page and head, for keys and values alike,
+ *   scale = max(the scale it has, if it holds earlier tokens; max |new| / 127)
+ *   new tokens:  value / scale, to the nearest whole number, ties to even
+ *   held tokens, where the scale grew:  whole number * (old scale / scale), likewise
+ * A page's first token begins it anew, whatever its scale was.  Places of tokens to
+ * come are left as they are.  A page that gets a value that is not finite has scale
+ * NaN and zeros from then on; new tokens below 2^-100 are zeros.
+ * Rows of one call must not meet in a page: where the table names a page for two
+ * tracks, or twice for one, what it holds after both were appended to is undefined.
+ * (Pages that tracks share may be read by all.)
+ *
+ * Arguments:
+ *   dtype          FLOCK_F32, FLOCK_F16 or FLOCK_BF16: new_k, new_v.
+ *   new_k, new_v   device in, [total][kv_heads][head_dim], strides >= 0.
+ *   total          rows of all tracks; a track with more rows than `lengths`
+ *                  has tokens is passed over.
+ *   xy, time, freq, n_time, n_y, n_x, interleaved   as for rotary_frames, the
+ *                  positions of the rows; without pairs (n_time + n_y + n_x = 0)
+ *                  keys are not turned.
+ *   k, v, k_scale, v_scale   device in and out: the cache.
+ *   pages          >= 0.
+ *   kv_heads       1 .. 256.
+ *   head_dim       16 .. 128, a multiple of 16.
+ *   max_pages      0 .. 2^24.
+ */
+flock_status append_tracks(int32_t dtype, const void *new_k, int64_t new_k_stride, const void *new_v,
+                           int64_t new_v_stride, const int32_t *offsets, int32_t n_tracks, int32_t total,
+                           const int32_t *table, int64_t table_stride, int32_t max_pages, const int32_t *lengths,
+                           const int32_t *xy, const int32_t *time, const double *freq, int32_t n_time, int32_t n_y,
+                           int32_t n_x, int32_t interleaved, int8_t *k, int8_t *v, float *k_scale, float *v_scale,
+                           int32_t pages, int32_t kv_heads, int32_t head_dim, void *stream);
+
+/*
+ * attention_tracks - attention of the newest detections of tracks over their pages.
+ *
+ * For query i of n of a track (its last n of `length` tokens, p_i = length - n + i)
+ * and token j, query head h and its kv head h / (q_heads / kv_heads):
+ *   t = scale * q_i . k_j;  with cap > 0: t = cap * tanh(t / cap)
+ *   seen: j <= p_i, and with window > 0: j > p_i - window
+ *   out_i = sum over the tokens seen of softmax_j(t) v_j
+ * A query that sees no token gets zeros.  Keys and values are taken as the whole
+ * numbers they are, with products in 32-bit sums and a softmax in 32 bits; weights
+ * are rounded to 11 bits for the product with v.
+ *
+ * Arguments:
+ *   dtype          FLOCK_F16 or FLOCK_BF16: q, out.
+ *   q              device in, [total][q_heads][head_dim], stride >= 0; turned by
+ *                  rotary_frames where keys were.
+ *   window         >= 0; 0: all tokens up to the query's own.
+ *   scale, cap     finite; scale > 0, cap >= 0 (none: 0, or 2^96 and more).
+ *   out            device out, [total][q_heads][head_dim].
+ *   workspace      as for cluster_frames, sized by attention_tracks_workspace(...).
+ * Others as for append_tracks; q_heads is 1 .. 256, a multiple of kv_heads.  A batch
+ * of more workgroups than a launch holds is refused (FLOCK_EUNSUPPORTED).
+ */
+flock_status attention_tracks(int32_t dtype, const void *q, int64_t q_stride, const int32_t *offsets,
+                              int32_t n_tracks, int32_t total, const int32_t *table, int64_t table_stride,
+                              int32_t max_pages, const int32_t *lengths, const int8_t *k, const int8_t *v,
+                              const float *k_scale, const float *v_scale, int32_t pages, int32_t q_heads,
+                              int32_t kv_heads, int32_t head_dim, int32_t window, float scale, float cap, void *out,
+                              int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of workspace attention_tracks needs for this batch shape (may be 0):
+ * partial results where several workgroups share a row's pages. */
+size_t attention_tracks_workspace(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads,
+                                  int32_t kv_heads, int32_t head_dim);
+
 /* Text of the last error on this thread ("" if none); valid until the next
  * library call on this thread. */
 const char *flock_last_error(void);

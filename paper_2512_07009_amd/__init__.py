@@ -22,16 +22,25 @@ frame or of a track, with their gradients:
     q, k = rotary_frames(q, k, xy, RotaryAxes(time=..., y=..., x=...), time)
     out = attention_frames(q, k, v, offsets, q_xy=xy, slopes=slopes)
 
+and what serves them on the live stream, in 8 bits: the newest detections of
+each track over a paged cache of what came before:
+
+    x, scale, h = rms_norm_rows_i8(h, weight, eps, residual)
+    qkv = linear_rows_i8(x, scale, *quantize_rows(w))
+    append_tracks(cache, k, v, offsets, table, lengths, axes, xy, time)
+    out = attention_tracks(q, cache, offsets, table, lengths)
+
 ``workloads`` holds the seeded synthetic input generators.
 """
 
-from .binding import (FlockError, RotaryAxes, attention_frames, attention_frames_backward,  # noqa: F401
-                      cluster_frames, density_frames, drinker_proximity_frames, eps_to_quanta, heatmap_frames,
-                      layer_norm_rows, layer_norm_rows_backward, lib, linear_rows_i8, mask_capacity,
-                      mask_components_frames, quantize_rows, rms_norm_rows, rms_norm_rows_backward, rms_norm_rows_i8, roi_filter_frames,
-                      rotary_frames, version)
+from .binding import (FlockError, RotaryAxes, TrackCache, append_tracks, attention_frames,  # noqa: F401
+                      attention_frames_backward, attention_tracks, cluster_frames, density_frames,
+                      drinker_proximity_frames, eps_to_quanta, heatmap_frames, layer_norm_rows, layer_norm_rows_backward,
+                      lib, linear_rows_i8, mask_capacity, mask_components_frames, quantize_rows, rms_norm_rows,
+                      rms_norm_rows_backward, rms_norm_rows_i8, roi_filter_frames, rotary_frames, version)
 
 __all__ = ["cluster_frames", "density_frames", "heatmap_frames", "roi_filter_frames", "drinker_proximity_frames",
            "mask_components_frames", "mask_capacity", "layer_norm_rows", "layer_norm_rows_backward", "rms_norm_rows",
            "rms_norm_rows_backward", "rms_norm_rows_i8", "quantize_rows", "linear_rows_i8", "RotaryAxes",
-           "rotary_frames", "attention_frames", "attention_frames_backward", "eps_to_quanta", "lib", "version", "FlockError"]
+           "rotary_frames", "attention_frames", "attention_frames_backward",
+           "TrackCache", "append_tracks", "attention_tracks", "eps_to_quanta", "lib", "version", "FlockError"]

@@ -103,6 +103,14 @@ def lib() -> ctypes.CDLL:
         L.attention_frames_backward.restype = i32
         L.attention_frames_backward_workspace.argtypes = [i32, i32, i32, i32, i32, i32]
         L.attention_frames_backward_workspace.restype = sz
+        L.append_tracks.argtypes = [i32, p, i64, p, i64, p, i32, i32, p, i64, i32, p, p, p, p, i32, i32, i32, i32,
+                                    p, p, p, p, i32, i32, i32, p]
+        L.append_tracks.restype = i32
+        L.attention_tracks.argtypes = [i32, p, i64, p, i32, i32, p, i64, i32, p, p, p, p, p, i32, i32, i32, i32, i32,
+                                       f32, f32, p, i64, p, sz, p]
+        L.attention_tracks.restype = i32
+        L.attention_tracks_workspace.argtypes = [i32, i32, i32, i32, i32, i32]
+        L.attention_tracks_workspace.restype = sz
         L.flock_last_error.argtypes = []
         L.flock_last_error.restype = ctypes.c_char_p
         L.flock_version.argtypes = []
@@ -809,6 +817,137 @@ def attention_frames_backward(grad_out: torch.Tensor, q: torch.Tensor, k: torch.
           lp, *tail, shape[5] ** -0.5 if scale is None else scale, cap, dq.data_ptr(), q_row,
           dk.data_ptr(), k_row, dv.data_ptr(), k_row, _ptr(ds), _ptr(ws), ws_bytes)
     return dq, dk, dv, ds
+
+
+class TrackCache:
+    """Keys and values of tracks in 8 bits, in pages of 64 tokens, with a scale for
+    each page and head.
+
+    k int8 [pages, kv_heads, 64, head_dim], v int8 [pages, kv_heads, head_dim, 64]
+    (tokens in the order of TrackCache.places), k_scale and v_scale float32 [pages,
+    kv_heads].  Which page holds which tokens of which track is said by the table
+    that append_tracks and attention_tracks take; the pages' contents need no
+    clearing, since a page begins anew with its first token.
+    """
+
+    PAGE = 64
+    # where a page's token t is among the 64 places of a value's dimension
+    places = tuple(16 * (t % 16 // 4) + 4 * (t // 16) + t % 4 for t in range(64))
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k.dim() != 4 or k.shape[2] != 64 or k.dtype != torch.int8 or not k.is_cuda or not k.is_contiguous():
+            raise ValueError("k must be a contiguous int8 [pages, kv_heads, 64, head_dim] device tensor")
+        pages, heads, _, dim = k.shape
+        for t, name, dtype, shape in ((v, "v", torch.int8, (pages, heads, dim, 64)),
+                                      (k_scale, "k_scale", torch.float32, (pages, heads)),
+                                      (v_scale, "v_scale", torch.float32, (pages, heads))):
+            if t.dtype != dtype or t.shape != shape or t.device != k.device or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on k's device")
+        if max(pages, heads, dim) > _MOST:
+            raise ValueError("k has more than 2^31 - 1 pages, heads or dimensions")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.kv_heads, self.head_dim, self.device = pages, heads, dim, k.device
+        self.index = k.get_device()
+        self.pointers = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, head_dim: int, device="cuda"):
+        """A pool of `pages` pages that hold nothing yet."""
+        new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=device)  # noqa: E731
+        return cls(new(torch.int8, pages, kv_heads, 64, head_dim), new(torch.int8, pages, kv_heads, head_dim, 64),
+                   new(torch.float32, pages, kv_heads), new(torch.float32, pages, kv_heads))
+
+    def values(self, pages: torch.Tensor | None = None):
+        """What the pool's (or some) pages stand for, for a look at them: (k, v)
+        float32 [pages, kv_heads, 64, head_dim], token after token."""
+        k, v, ks, vs = (t if pages is None else t[pages.long()] for t in (self.k, self.v, self.k_scale, self.v_scale))
+        v = v[..., torch.tensor(self.places, device=v.device)].transpose(2, 3)
+        return k * ks[:, :, None, None], v * vs[:, :, None, None]
+
+
+def _tracks(cache, offsets, table, lengths, total):
+    """The checked arguments that say which rows and pages are whose."""
+    index = cache.index
+    n = offsets.numel() - 1
+    if offsets.dim() != 1 or not 0 <= n <= _MOST:
+        raise ValueError("offsets must be a contiguous [tracks + 1] tensor")
+    op = _vector(offsets, "offsets", torch.int32, n + 1, index)
+    lp = _vector(lengths, "lengths", torch.int32, n, index)
+    if table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != n or table.get_device() != index \
+            or (table.stride(1) != 1 and table.shape[1] > 1 and n > 0):
+        raise ValueError(f"table must be an int32 [{n}, pages] tensor with contiguous rows on the cache's device")
+    if max(table.shape[1], total) > _MOST:
+        raise ValueError("table or rows have more than 2^31 - 1 columns or rows")
+    return op, n, total, table.data_ptr(), table.stride(0) if n > 1 else table.shape[1], table.shape[1], lp
+
+
+def append_tracks(cache: TrackCache, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, table: torch.Tensor,
+                  lengths: torch.Tensor, axes: RotaryAxes | None = None, xy: torch.Tensor | None = None,
+                  time: torch.Tensor | None = None, interleaved: bool = False, stream=None) -> None:
+    """Keys and values of new detections, k and v [T, kv_heads, head_dim] (float32,
+    float16 or bfloat16), into the pages of their tracks, in 8 bits.
+
+    offsets: int32 [tracks + 1], the rows of each track, oldest first.  table: int32
+    [tracks, pages of a track]: the page of the pool that holds tokens 64 i .. 64 i +
+    63 of a track.  lengths: int32 [tracks], tokens of each track after the call, so
+    that its rows are tokens lengths - rows .. lengths - 1.  axes: keys are turned by
+    their time and places as rotary_frames turns them (None: not).  A page's scale
+    grows with its largest value, and what it holds is rounded again then.
+    The cache is changed in place.  There are no gradients.
+    """
+    code = _dtype(k)
+    ks, vs = _heads(k, "k"), _heads(v, "v", k)
+    total, heads, dim = k.shape
+    index = cache.index
+    if v.shape != k.shape or heads != cache.kv_heads or dim != cache.head_dim or k.get_device() != index:
+        raise ValueError(f"k and v must be [T, {cache.kv_heads}, {cache.head_dim}] on the cache's device")
+    rows = _tracks(cache, offsets, table, lengths, total)
+    nt, ny, nx = axes.counts if axes is not None else (0, 0, 0)
+    xp = tp = None
+    if ny or nx:
+        if xy is None:
+            raise ValueError("xy is needed by the axes' y and x pairs")
+        xp = _matrix(xy, "xy", torch.int32, total, 2, index)
+    if nt:
+        if time is None:
+            raise ValueError("time is needed by the axes' time pairs")
+        tp = _vector(time, "time", torch.int32, total, index)
+    _call(lib().append_tracks, k.device, stream, code, k.data_ptr(), ks, v.data_ptr(), vs, *rows, xp, tp,
+          axes.freq if axes is not None else None, nt, ny, nx, int(interleaved), *cache.pointers, cache.pages, heads, dim)
+
+
+def attention_tracks(q: torch.Tensor, cache: TrackCache, offsets: torch.Tensor, table: torch.Tensor,
+                     lengths: torch.Tensor, scale: float | None = None, cap: float = 0.0, window: int = 0, out=None,
+                     stream=None):
+    """Attention of the newest detections of tracks, q [T, Hq, head_dim] (float16 or
+    bfloat16, turned as the keys were), over what the cache holds of them.
+
+    offsets, table and lengths as for append_tracks: the rows of a track are its last
+    tokens, and each sees the tokens up to its own, the last `window` of them where
+    that is not 0.  scale: 1 / sqrt(head_dim) if None.  cap: scores become cap *
+    tanh(score / cap).  A row that sees nothing gets zeros.  There are no gradients.
+    Returns out [T, Hq, head_dim].  out: optional tensor to write into.
+    """
+    code = _dtype(q)
+    qs = _heads(q, "q")
+    total, heads, dim = q.shape
+    if dim != cache.head_dim or q.get_device() != cache.index:
+        raise ValueError(f"q must be [T, heads, {cache.head_dim}] on the cache's device")
+    rows = _tracks(cache, offsets, table, lengths, total)
+    dev = q.device
+    if out is None:
+        out = _like(q, stream)
+        os = heads * dim
+    else:
+        os = _heads(out, "out", q)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    L = lib()
+    ws_bytes = L.attention_tracks_workspace(rows[1], total, rows[5], heads, cache.kv_heads, dim)
+    ws = _workspace(ws_bytes, dev, stream)
+    _call(L.attention_tracks, dev, stream, code, q.data_ptr(), qs, *rows, *cache.pointers, cache.pages, heads,
+          cache.kv_heads, dim, window, dim ** -0.5 if scale is None else scale, cap, out.data_ptr(), os, _ptr(ws), ws_bytes)
+    return out
 
 
 def version() -> str:

@@ -837,6 +837,42 @@ flock_status validate_offsets(const char *name, const int32_t *offsets, int32_t 
     return FLOCK_OK;
 }
 
+void rotary_steps(const double *freq, int32_t n_time, int32_t pairs, uint64_t *steps) {
+    for (int32_t p = 0; p < pairs; ++p) {
+        // turns per unit, whole turns dropped, in 2^-64 turns (rounded down to the double's last digit)
+        double turns = freq[p] / (2.0 * 3.14159265358979323846) / (p < n_time ? 1.0 : 16.0);
+        const bool back = turns < 0.0;
+        turns = std::fmod(std::fabs(turns), 1.0);
+        const uint64_t step = (uint64_t)std::ldexp(turns, 64);
+        steps[p] = back ? 0 - step : step;
+    }
+}
+
+// What append_tracks and attention_tracks share.
+flock_status check_tracks(const flock::TrackArgs &t, const flock::TrackCacheArgs &c) {
+    if (t.n_tracks < 0) return fail(FLOCK_EINVAL, "n_tracks = %d < 0", t.n_tracks);
+    if (t.total < 0) return fail(FLOCK_EINVAL, "total = %d < 0", t.total);
+    if (c.pages < 0) return fail(FLOCK_EINVAL, "pages = %d < 0", c.pages);
+    if (t.max_pages < 0 || t.max_pages > flock::kTrackMaxPages)
+        return fail(FLOCK_EINVAL, "max_pages = %d outside 0..%d", t.max_pages, flock::kTrackMaxPages);
+    if (t.table_stride < 0) return fail(FLOCK_EINVAL, "table_stride = %lld < 0", (long long)t.table_stride);
+    if (c.kv_heads < 1 || c.kv_heads > 256) return fail(FLOCK_EINVAL, "kv_heads = %d outside 1..256", c.kv_heads);
+    if (c.dim < 16 || c.dim > flock::kAttentionMaxDim || c.dim % 16)
+        return fail(FLOCK_EINVAL, "head_dim = %d is not a multiple of 16 in 16..%d", c.dim, flock::kAttentionMaxDim);
+    return FLOCK_OK;
+}
+
+flock_status check_tracks_pointers(const flock::TrackArgs &t, const flock::TrackCacheArgs &c) {
+    if (!t.offsets || !t.lengths) return fail(FLOCK_EINVAL, "offsets and lengths must be non-NULL");
+    if (t.max_pages > 0 && !t.table) return fail(FLOCK_EINVAL, "table must be non-NULL when max_pages > 0");
+    if (c.pages > 0 && (!c.k || !c.v || !c.k_scale || !c.v_scale))
+        return fail(FLOCK_EINVAL, "k, v, k_scale and v_scale must be non-NULL when pages > 0");
+    if (!aligned(c.k, 16) || !aligned(c.v, 16)) return fail(FLOCK_EINVAL, "k and v must be 16-byte aligned");
+    if (!aligned(t.offsets, 4) || !aligned(t.lengths, 4) || !aligned(t.table, 4) || !aligned(c.k_scale, 4) || !aligned(c.v_scale, 4))
+        return fail(FLOCK_EINVAL, "offsets, lengths, table, k_scale and v_scale must be 4-byte aligned");
+    return FLOCK_OK;
+}
+
 flock_status validate_attention(const flock::AttentionArgs &a, hipStream_t s) {
     flock_status st = validate_offsets("q_offsets", a.q_offsets, a.n_frames, a.total_q, s);
     if (st == FLOCK_OK && a.k_offsets != a.q_offsets)
@@ -1174,14 +1210,7 @@ flock_status rotary_frames(int32_t dtype, const void *q, int64_t q_stride, const
     a.pairs = pairs;
     a.interleaved = interleaved != 0;
     a.inverse = inverse != 0;
-    for (int32_t p = 0; p < pairs; ++p) {
-        // turns per unit, whole turns dropped, in 2^-64 turns (rounded down to the double's last digit)
-        double turns = freq[p] / (2.0 * 3.14159265358979323846) / (p < n_time ? 1.0 : 16.0);
-        const bool back = turns < 0.0;
-        turns = std::fmod(std::fabs(turns), 1.0);
-        const uint64_t step = (uint64_t)std::ldexp(turns, 64);
-        a.step[p] = back ? 0 - step : step;
-    }
+    rotary_steps(freq, n_time, pairs, a.step);
     const hipError_t err = flock::launch_rotary(a, dtype, reinterpret_cast<hipStream_t>(stream));
     return err == hipSuccess ? FLOCK_OK : hip_fail(err, "rotary kernel launch");
 }
@@ -1341,6 +1370,132 @@ flock_status attention_frames_backward(
     const hipError_t ferr = ws.release(s);
     if (err == hipSuccess) err = ferr;
     return err == hipSuccess ? FLOCK_OK : hip_fail(err, "attention backward kernels");
+}
+
+flock_status append_tracks(int32_t dtype, const void *new_k, int64_t new_k_stride, const void *new_v, int64_t new_v_stride,
+                           const int32_t *offsets, int32_t n_tracks, int32_t total, const int32_t *table,
+                           int64_t table_stride, int32_t max_pages, const int32_t *lengths, const int32_t *xy,
+                           const int32_t *time, const double *freq, int32_t n_time, int32_t n_y, int32_t n_x,
+                           int32_t interleaved, int8_t *k, int8_t *v, float *k_scale, float *v_scale, int32_t pages,
+                           int32_t kv_heads, int32_t head_dim, void *stream) {
+    g_error[0] = '\0';
+    flock::AppendArgs a{};
+    a.tracks = {offsets, lengths, table, table_stride, n_tracks, total, max_pages};
+    a.cache = {k, v, k_scale, v_scale, pages, kv_heads, head_dim};
+    if (!is_dtype(dtype)) return fail(FLOCK_EINVAL, "dtype = %d, expected FLOCK_F32, FLOCK_F16 or FLOCK_BF16", dtype);
+    flock_status st = check_tracks(a.tracks, a.cache);
+    if (st != FLOCK_OK) return st;
+    if (new_k_stride < 0 || new_v_stride < 0) return fail(FLOCK_EINVAL, "strides of new_k and new_v must be >= 0");
+    if (n_time < 0 || n_y < 0 || n_x < 0 || 2 * ((int64_t)n_time + n_y + n_x) > head_dim)
+        return fail(FLOCK_EINVAL, "n_time = %d, n_y = %d, n_x = %d pairs do not fit head_dim = %d", n_time, n_y, n_x,
+                    head_dim);
+    const int32_t pairs = n_time + n_y + n_x;
+    if (pairs && !freq) return fail(FLOCK_EINVAL, "freq is NULL with pairs");
+    for (int32_t p = 0; p < pairs; ++p)
+        if (!std::isfinite(freq[p])) return fail(FLOCK_EINVAL, "freq[%d] is not finite", p);
+    if (n_tracks == 0 || total == 0) return FLOCK_OK;
+    st = check_tracks_pointers(a.tracks, a.cache);
+    if (st != FLOCK_OK) return st;
+    if (!new_k || !new_v) return fail(FLOCK_EINVAL, "new_k and new_v must be non-NULL when total > 0");
+    const size_t size = dtype_size(dtype);
+    if (!aligned(new_k, size) || !aligned(new_v, size))
+        return fail(FLOCK_EINVAL, "new_k and new_v must be aligned to their elements");
+    if ((n_y || n_x) && !xy) return fail(FLOCK_EINVAL, "xy is NULL with y or x pairs");
+    if (n_time && !time) return fail(FLOCK_EINVAL, "time is NULL with time pairs");
+    if (!aligned(xy, 8) || !aligned(time, 4))
+        return fail(FLOCK_EINVAL, "xy must be 8-byte aligned, time 4-byte aligned");
+    st = check_workgroups(flock::append_workgroups(n_tracks, total, kv_heads));
+    if (st != FLOCK_OK) return st;
+    if (pages == 0 || max_pages == 0) return FLOCK_OK;  // no page to go to
+    const DeviceInfo *dev = nullptr;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (validate_requested()) {
+        st = validate_offsets("offsets", offsets, n_tracks, total, s);
+        if (st != FLOCK_OK) return st;
+    }
+    a.k = new_k;
+    a.v = new_v;
+    a.k_stride = new_k_stride;
+    a.v_stride = new_v_stride;
+    a.xy = xy;
+    a.time = time;
+    a.n_time = n_time;
+    a.n_y = n_y;
+    a.pairs = pairs;
+    a.interleaved = interleaved != 0;
+    rotary_steps(freq, n_time, pairs, a.step);
+    const hipError_t err = flock::launch_append(a, dtype, s);
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "append kernel launch");
+}
+
+size_t attention_tracks_workspace(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads, int32_t kv_heads,
+                                  int32_t head_dim) {
+    if (n_tracks <= 0 || total <= 0 || max_pages < 0 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || head_dim < 1)
+        return 0;
+    return flock::track_attention_workspace_bytes(
+            flock::plan_track_attention(n_tracks, total, max_pages, q_heads, kv_heads, device_cus()), total, q_heads,
+            head_dim);
+}
+
+flock_status attention_tracks(int32_t dtype, const void *q, int64_t q_stride, const int32_t *offsets, int32_t n_tracks,
+                              int32_t total, const int32_t *table, int64_t table_stride, int32_t max_pages,
+                              const int32_t *lengths, const int8_t *k, const int8_t *v, const float *k_scale,
+                              const float *v_scale, int32_t pages, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                              int32_t window, float scale, float cap, void *out, int64_t out_stride, void *workspace,
+                              size_t workspace_bytes, void *stream) {
+    g_error[0] = '\0';
+    flock::TrackAttentionArgs a{};
+    a.tracks = {offsets, lengths, table, table_stride, n_tracks, total, max_pages};
+    // (the cache is only read)
+    a.cache = {const_cast<int8_t *>(k), const_cast<int8_t *>(v), const_cast<float *>(k_scale),
+               const_cast<float *>(v_scale), pages, kv_heads, head_dim};
+    if (dtype != FLOCK_F16 && dtype != FLOCK_BF16)
+        return fail(FLOCK_EINVAL, "dtype = %d, expected FLOCK_F16 or FLOCK_BF16", dtype);
+    flock_status st = check_tracks(a.tracks, a.cache);
+    if (st != FLOCK_OK) return st;
+    if (q_heads < 1 || q_heads > 256 || q_heads % kv_heads)
+        return fail(FLOCK_EINVAL, "q_heads = %d is not a multiple of kv_heads = %d in 1..256", q_heads, kv_heads);
+    if (window < 0) return fail(FLOCK_EINVAL, "window = %d < 0", window);
+    if (!std::isfinite(scale) || !(scale > 0.0f)) return fail(FLOCK_EINVAL, "scale must be finite and > 0");
+    if (!std::isfinite(cap) || !(cap >= 0.0f)) return fail(FLOCK_EINVAL, "cap must be finite and >= 0");
+    if (q_stride < 0 || out_stride < (int64_t)q_heads * head_dim)
+        return fail(FLOCK_EINVAL, "q's stride must be >= 0, and out's hold a row");
+    if (n_tracks == 0 || total == 0) return FLOCK_OK;
+    st = check_tracks_pointers(a.tracks, a.cache);
+    if (st != FLOCK_OK) return st;
+    if (!q || !out) return fail(FLOCK_EINVAL, "q and out must be non-NULL when total > 0");
+    if (!aligned(q, 2) || !aligned(out, 2)) return fail(FLOCK_EINVAL, "q and out must be aligned to their elements");
+    // rows are numbered in 31 bits, up to the end of the tile after the last
+    if ((int64_t)total * (q_heads / kv_heads) > 0x7fffff00LL)
+        return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 - 256 rows of queries and shared heads");
+    const DeviceInfo *dev = nullptr;
+    const flock::TrackPlan plan = flock::plan_track_attention(n_tracks, total, max_pages, q_heads, kv_heads, device_cus());
+    st = check_workgroups(plan.slots * kv_heads * plan.splits);
+    if (st != FLOCK_OK) return st;
+    st = device_info(&dev);
+    if (st != FLOCK_OK) return st;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (validate_requested()) {
+        st = validate_offsets("offsets", offsets, n_tracks, total, s);
+        if (st != FLOCK_OK) return st;
+    }
+    a.q = q;
+    a.q_stride = q_stride;
+    a.out = out;
+    a.out_stride = out_stride;
+    a.q_heads = q_heads;
+    a.window = std::min(window, 1 << 30);  // (as long as any track)
+    a.scale = scale;
+    a.cap = cap;
+    Workspace ws;
+    st = ws.take(workspace, workspace_bytes, flock::track_attention_workspace_bytes(plan, total, q_heads, head_dim), s);
+    if (st != FLOCK_OK) return st;
+    hipError_t err = flock::launch_track_attention(a, dtype, plan, ws.ptr, s);
+    const hipError_t ferr = ws.release(s);
+    if (err == hipSuccess) err = ferr;
+    return err == hipSuccess ? FLOCK_OK : hip_fail(err, "track attention kernels");
 }
 
 }  // extern "C"

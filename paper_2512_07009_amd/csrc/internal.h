@@ -348,6 +348,60 @@ struct RotaryArgs {
 };
 hipError_t launch_rotary(RotaryArgs a, int32_t dtype, hipStream_t stream);
 
+// Tracks: a paged cache of keys and values in 8 bits (layout: tracks_common.h).
+constexpr int kTrackPage = 64;
+constexpr int32_t kTrackMaxPages = 1 << 24;  // of a track: tokens are numbered in 31 bits
+
+struct TrackCacheArgs {
+    int8_t *k, *v;                     // [pages][kv_heads][64 * dim]
+    float *k_scale, *v_scale;          // [pages][kv_heads]
+    int32_t pages, kv_heads, dim;
+};
+
+struct TrackArgs {
+    const int32_t *offsets;            // [n_tracks + 1]: rows of each track
+    const int32_t *lengths;            // [n_tracks]: tokens, those of the rows among them
+    const int32_t *table;              // [n_tracks][max_pages], rows table_stride apart
+    int64_t table_stride;
+    int32_t n_tracks, total, max_pages;
+};
+
+struct AppendArgs {
+    TrackArgs tracks;
+    TrackCacheArgs cache;
+    const void *k, *v;                 // [total][kv_heads][dim], strides of rows in elements
+    int64_t k_stride, v_stride;
+    const int32_t *xy, *time;
+    int32_t n_time, n_y, pairs, interleaved;
+    uint64_t step[kRotaryMaxPairs];
+};
+int64_t append_workgroups(int32_t n_tracks, int32_t total, int32_t kv_heads);
+hipError_t launch_append(const AppendArgs &a, int32_t dtype, hipStream_t stream);
+
+struct TrackAttentionArgs {
+    TrackArgs tracks;
+    TrackCacheArgs cache;
+    const void *q;                     // [total][q_heads][dim]
+    void *out;
+    int64_t q_stride, out_stride;
+    int32_t q_heads, window;
+    float scale, cap;
+    int32_t group, splits, split_pages;  // set by launch_track_attention
+    float *part_out, *part_stat;
+};
+
+// How the pages of a row are dealt out.
+struct TrackPlan {
+    int64_t slots;        // numbers of row tiles
+    int32_t splits;       // workgroups that may share a row's pages ...
+    int32_t split_pages;  // ... and how many pages each takes
+};
+TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads, int32_t kv_heads,
+                               int n_cus);
+size_t track_attention_workspace_bytes(const TrackPlan &p, int32_t total, int32_t q_heads, int32_t dim);
+hipError_t launch_track_attention(TrackAttentionArgs a, int32_t dtype, const TrackPlan &p, void *workspace,
+                                  hipStream_t stream);
+
 constexpr int kAttentionMaxDim = 128;
 // 64 rows lie within 2^31 bytes: a tile's loads go through resources of 64 rows at most
 constexpr int64_t kAttentionMaxStride = (1 << 24) - 8;
