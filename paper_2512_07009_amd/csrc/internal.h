@@ -311,7 +311,8 @@ struct LinearArgs {
     int32_t gelu;
     void *y;                           // [rows][outputs]
     int64_t y_stride;
-    int32_t aligned, column_tiles;     // set by launch_linear: rows begin at 16 bytes; tiles of outputs
+    int32_t column_tiles;              // set by launch_linear: tiles of outputs, and of all
+    int64_t tiles;
 
     void advance(int64_t first, size_t size) {
         move_on(x, first * x_stride, 1);

@@ -50,162 +50,306 @@ __device__ __forceinline__ float gelu(float x) {
 }
 
 // ---------------------------------------------------------------------------
-// Many rows: BM x BN outputs a workgroup, a quarter of them a wave.
+// Many rows: BM x BN outputs a tile, a quarter of them a wave.
 //
 // The weights are the left factor (32 outputs), the rows the right one (32 rows),
-// so that a lane holds four outputs of one row side by side.  Tiles of BK bytes of
-// every row go to LDS without registers in between (16 bytes a lane), one while the
-// one before is multiplied, with one barrier a tile.  A row's chunks of 16 bytes are
-// stored in an order that turns with the row, so that the 32 rows that a wave reads
-// a chunk of lie in different banks.
+// so that a lane holds four outputs of one row side by side; halves of a wave trade
+// fours for eights, and each lane stores 16 bytes of a row.
+//
+// Tiles of kStep bytes of every row go to LDS without registers in between (16 bytes
+// a lane).  A row's chunks of 16 bytes are stored in an order that turns with the row,
+// so that the 32 rows that a wave reads a chunk of lie in different banks.
+//
+// A workgroup stays for many tiles, and its steps are one stream: loads run kAhead
+// steps before the products, across the ends of tiles, and a step waits for its own
+// loads alone (they come back in order), with one barrier a step.
 // ---------------------------------------------------------------------------
 
-template <int BK>
-__device__ __forceinline__ int turned(int row, int chunk) {
-    return BK == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3);
-}
+constexpr int kStep = 64, kAhead = 3, kStages = kAhead + 1, kChunks = kStep / 16;
 
-// A tile of ROWS rows: where its lanes load from, in the order in which they store.
-template <int ROWS, int BK>
-struct Loader {
-    static constexpr int kChunks = BK / 16, kLoads = ROWS * kChunks / kThreads;
-    const int8_t *base;
-    int left;               // rows there are
-    uint32_t at[kLoads];    // of the lane's chunk, from base
-    uint32_t pitch;
+__device__ const __attribute__((aligned(16))) int8_t kZeros[16] = {};
 
-    __device__ __forceinline__ Loader(const int8_t *p, int64_t stride, int rows) {
-        base = p;
-        left = rows;
-        pitch = (uint32_t)stride;
+__device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row >> 1) & 3); }
+
+#define FLOCK_TO_LDS(FROM, TO, SIZE)                                                                  \
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(FROM),         \
+                                     (__attribute__((address_space(3))) void *)(TO), SIZE, 0, 0)
+
+template <int BM, int BN>
+struct __attribute__((aligned(16))) LinearShared {
+    int8_t x[kStages][BM * kStep], w[kStages][BN * kStep];
+    float x_scale[kStages][BM], w_scale[kStages][BN], bias[kStages][BN];  // of a tile, in turn: a step may be all of one
+};
+
+// Where a tile's rows begin, for the loads or for the products.
+template <int BM, int BN>
+struct LinearTile {
+    int64_t m0;
+    int n0, rows, columns;
+    __device__ __forceinline__ LinearTile(const LinearArgs &a, int64_t tile) {
+        m0 = tile / a.column_tiles * BM;
+        n0 = (int)(tile % a.column_tiles) * BN;
+        rows = (int)min((int64_t)BM, a.rows - m0);
+        columns = min(BN, a.outputs - n0);
+    }
+};
+
+// The loads' side of the stream.
+template <int BM, int BN>
+struct LinearLoads {
+    static constexpr int kX = BM * kChunks / kThreads, kW = BN * kChunks / kThreads, kLoads = kX + kW;
+    const int8_t *x, *w;          // the tile's first rows
+    uint32_t x_at[kX], w_at[kW];  // the lane's chunks, from them
+    int wave;
+
+    __device__ __forceinline__ LinearLoads() { wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+    __device__ __forceinline__ void begin(const LinearArgs &a, int64_t tile, int turn, LinearShared<BM, BN> &s) {
+        const LinearTile<BM, BN> t(a, tile);
+        x = a.x + t.m0 * a.x_stride;
+        w = a.w + t.n0 * a.w_stride;
+        // (rows beyond the last are the last: what they give is not stored)
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
+        for (int i = 0; i < kX; ++i) {
             const int slot = i * kThreads + threadIdx.x, row = slot / kChunks;
-            // (rows beyond the last are the last: what they give is not stored)
-            at[i] = (uint32_t)min(row, left - 1) * pitch + 16u * turned<BK>(row, slot % kChunks);
+            x_at[i] = (uint32_t)min(row, t.rows - 1) * (uint32_t)a.x_stride + 16u * turned(row, slot % kChunks);
+        }
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            const int slot = i * kThreads + threadIdx.x, row = slot / kChunks;
+            w_at[i] = (uint32_t)min(row, t.columns - 1) * (uint32_t)a.w_stride + 16u * turned(row, slot % kChunks);
+        }
+        // the scales and the bias: a load of 64 of each a wave, where there are so many
+        const int lane = threadIdx.x & 63, part = 64 * wave;
+        if (part < BM) FLOCK_TO_LDS(a.x_scale + t.m0 + min(part + lane, t.rows - 1), s.x_scale[turn] + part, 4);
+        if (part < BN) {
+            const int n = t.n0 + min(part + lane, t.columns - 1);
+            FLOCK_TO_LDS(a.w_scale + n, s.w_scale[turn] + part, 4);
+            FLOCK_TO_LDS(a.bias ? static_cast<const void *>(a.bias + n) : kZeros, s.bias[turn] + part, 4);
         }
     }
 
-    __device__ __forceinline__ void direct(int8_t *tile, int k0) const {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    __device__ __forceinline__ void step(int k0, int width, int8_t *xs, int8_t *ws) const {
+        if (k0 + kStep <= width) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void *)(base + k0 + at[i]),
-                    (__attribute__((address_space(3))) void *)(tile + 16 * (i * kThreads + 64 * wave)), 16, 0, 0);
+            for (int i = 0; i < kX; ++i) FLOCK_TO_LDS(x + k0 + x_at[i], xs + 16 * (i * kThreads + 64 * wave), 16);
+#pragma unroll
+            for (int i = 0; i < kW; ++i) FLOCK_TO_LDS(w + k0 + w_at[i], ws + 16 * (i * kThreads + 64 * wave), 16);
+            return;
+        }
+        // the row's end: no chunks beyond it, of the weights zeros instead
+#pragma unroll
+        for (int i = 0; i < kX; ++i) {
+            const int slot = i * kThreads + threadIdx.x, c = 16 * turned(slot / kChunks, slot % kChunks);
+            FLOCK_TO_LDS(x + (k0 + c < width ? k0 + x_at[i] : x_at[i] - c), xs + 16 * (i * kThreads + 64 * wave), 16);
+        }
+#pragma unroll
+        for (int i = 0; i < kW; ++i) {
+            const int slot = i * kThreads + threadIdx.x, c = 16 * turned(slot / kChunks, slot % kChunks);
+            FLOCK_TO_LDS(k0 + c < width ? w + k0 + w_at[i] : kZeros, ws + 16 * (i * kThreads + 64 * wave), 16);
+        }
     }
 
-    // The row's end, or rows that do not begin at 16 bytes.
-    __device__ __forceinline__ void by_registers(int8_t *tile, int k0, int width) const {
+    // Zeros for the weights' bytes beyond the width in a chunk that it ends in.
+    __device__ __forceinline__ void mask(int k0, int width, int8_t *ws) const {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int slot = i * kThreads + threadIdx.x, row = slot / kChunks;
-            const int8_t *p = base + (uint32_t)min(row, left - 1) * pitch;
-            *reinterpret_cast<i32x4 *>(tile + 16 * slot) = load_chunk(p, k0 + 16 * turned<BK>(row, slot % kChunks), width);
+        for (int i = 0; i < kW; ++i) {
+            const int slot = i * kThreads + threadIdx.x, left = width - k0 - 16 * turned(slot / kChunks, slot % kChunks);
+            if (left > 0 && left < 16) {
+                i32x4 v = *reinterpret_cast<i32x4 *>(ws + 16 * slot);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int bytes = min(max(left - 4 * e, 0), 4);
+                    v[e] = bytes == 4 ? v[e] : v[e] & ((1 << (8 * bytes)) - 1);
+                }
+                *reinterpret_cast<i32x4 *>(ws + 16 * slot) = v;
+            }
         }
     }
 };
 
-template <typename T, int BM, int BN, int BK>
+// One step of a wave: its rows' and outputs' chunks from LDS.  (The stage that loads go
+// to is another one: `ahead` only says so.)
+template <int KM, int KN>
+__device__ __forceinline__ void multiply(const int8_t *__restrict__ x, const int8_t *__restrict__ w, i32x16 (&acc)[KN][KM]) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int k = 0; k < kStep / 32; ++k) {
+        i32x4 wf[KN], xf[KM];
+#pragma unroll
+        for (int i = 0; i < KN; ++i)
+            wf[i] = *reinterpret_cast<const i32x4 *>(w + (32 * i + col) * kStep + 16 * turned(col, 2 * k + h));
+#pragma unroll
+        for (int j = 0; j < KM; ++j)
+            xf[j] = *reinterpret_cast<const i32x4 *>(x + (32 * j + col) * kStep + 16 * turned(col, 2 * k + h));
+#pragma unroll
+        for (int i = 0; i < KN; ++i)
+#pragma unroll
+            for (int j = 0; j < KM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[i], xf[j], acc[i][j], 0, 0, 0);
+    }
+}
+
+// A wave's outputs of a tile.  Returns whether every store was made.
+template <typename T, bool GELU, int KM, int KN, typename S, typename Tile>
+__device__ __forceinline__ void finish(const LinearArgs &a, const Tile &t, const S &s, int turn, int wm, int wn,
+                                       const i32x16 (&acc)[KN][KM]) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int j = 0; j < KM; ++j) {
+        const int m = wm + 32 * j + col;
+        const float xs = s.x_scale[turn][m];
+        T *y = static_cast<T *>(a.y) + (t.m0 + m) * a.y_stride + t.n0;
+#pragma unroll
+        for (int i = 0; i < KN; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 8) {
+                // outputs n .. n + 3 and n + 8 .. n + 11 of the lane's row
+                const int n = wn + 32 * i + 2 * r + 4 * h;
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = n + (e & 3) + 8 * (e >> 2);
+                    o[e] = (float)acc[i][j][r + e] * xs * s.w_scale[turn][at] + s.bias[turn][at];
+                    if (GELU) o[e] = gelu(o[e]);
+                }
+                // 8 outputs side by side: the first eight here, the others in the lane 32 on
+                Pack<T, 8> out;
+                if constexpr (sizeof(T) == 2) {
+                    Pack<T, 8> mine;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) mine.v[e] = static_cast<T>(o[e]);
+                    const i32x4 v = __builtin_bit_cast(i32x4, mine);
+                    const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+                    const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+                    const i32x4 u = {(int)p[0], (int)q[0], (int)p[1], (int)q[1]};
+                    out = __builtin_bit_cast(Pack<T, 8>, u);
+                } else {
+                    float f[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[e]), __float_as_uint(o[e + 4]), false, false);
+                        f[e] = __uint_as_float(p[0]);
+                        f[e + 4] = __uint_as_float(p[1]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out.v[e] = static_cast<T>(f[e]);
+                }
+                const int first = wn + 32 * i + 2 * r + 8 * h, left = t.columns - first;
+                if (m < t.rows) {
+                    if (left >= 8) {
+                        *reinterpret_cast<Pack<T, 8> *>(y + first) = out;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < left) y[first + e] = out.v[e];
+                    }
+                }
+            }
+    }
+}
+
+// Waits for LDS, and for all but the last N loads and stores.
+template <int N>
+__device__ __forceinline__ void wait_but() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x070);
+}
+
+// The compiler moves no access to memory over this.
+__device__ __forceinline__ void stand() { asm volatile("" ::: "memory"); }
+
+template <typename T, bool GELU, int BM, int BN>
 __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
     constexpr int kMT = BM / 64, kNT = BN / 64;      // 32 x 32 parts of a wave
-    constexpr int kPitch = 32 * kNT + 16 / (int)sizeof(T);
-    constexpr int kTiles = 2 * (BM + BN) * BK, kStage = 4 * 32 * kPitch * (int)sizeof(T);
-    __shared__ __attribute__((aligned(16))) int8_t shared[kTiles > kStage ? kTiles : kStage];
-    __shared__ float scales[2][BN];
+    constexpr int kLoads = LinearLoads<BM, BN>::kLoads;
+    __shared__ LinearShared<BM, BN> s;
 
-    const int64_t tile = blockIdx.x;
-    const int64_t m0 = tile / a.column_tiles * BM;
-    const int n0 = (int)(tile % a.column_tiles) * BN;
-    const int rows = (int)min((int64_t)BM, a.rows - m0), columns = min(BN, a.outputs - n0);
-    for (int i = threadIdx.x; i < BN; i += kThreads) {
-        scales[0][i] = i < columns ? a.w_scale[n0 + i] : 0.0f;
-        scales[1][i] = i < columns && a.bias ? a.bias[n0 + i] : 0.0f;
+    // tiles of this workgroup: an eighth of all to each XCD, in one piece, its workgroups side by side
+    int64_t first, end;
+    int beside = 1;
+    if (a.tiles <= gridDim.x) {  // one each
+        const int64_t per = a.tiles / 8, id = blockIdx.x;
+        first = id < per * 8 ? (id & 7) * per + (id >> 3) : id;
+        end = first + 1;
+    } else {                     // (as many workgroups on each XCD)
+        const int xcd = blockIdx.x & 7;
+        beside = gridDim.x >> 3;
+        first = a.tiles * xcd / 8 + (blockIdx.x >> 3);
+        end = a.tiles * (xcd + 1) / 8;
+        if (first >= end) return;
     }
-    const Loader<BM, BK> load_x(a.x + m0 * a.x_stride, a.x_stride, rows);
-    const Loader<BN, BK> load_w(a.w + n0 * a.w_stride, a.w_stride, columns);
-    const auto fetch = [&](int t) {
-        int8_t *x = shared + (t & 1) * (BM + BN) * BK, *w = x + BM * BK;
-        const int k0 = t * BK;
-        if (a.aligned && k0 + BK <= a.width) {
-            load_x.direct(x, k0);
-            load_w.direct(w, k0);
-        } else {
-            load_x.by_registers(x, k0, a.width);
-            load_w.by_registers(w, k0, a.width);
+    const int steps = (a.width + kStep - 1) / kStep;
+    int64_t left = ((end - first - 1) / beside + 1) * steps;  // steps to multiply
+
+    LinearLoads<BM, BN> loads;
+    int64_t next_tile = first;
+    int next_step = 0, next_turn = 0, next_stage = 0;
+    const auto load = [&] {
+        if (next_tile >= end) return;
+        if (next_step == 0) loads.begin(a, next_tile, next_turn, s);
+        loads.step(next_step * kStep, a.width, s.x[next_stage], s.w[next_stage]);
+        next_stage = (next_stage + 1) & (kStages - 1);
+        if (++next_step == steps) {
+            next_step = 0;
+            next_tile += beside;
+            next_turn = (next_turn + 1) & (kStages - 1);
         }
     };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) load();
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, col = lane & 31;
-    const int wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
-    i32x16 acc[kNT][kMT] = {};
-    const int steps = (a.width + BK - 1) / BK;
-    fetch(0);
-    for (int t = 0; t < steps; ++t) {
-        __syncthreads();  // this tile is there, and the one before has been read
-        if (t + 1 < steps) fetch(t + 1);
-        const int8_t *x = shared + (t & 1) * (BM + BN) * BK, *w = x + BM * BK;
-#pragma unroll
-        for (int k = 0; k < BK / 32; ++k) {
-            i32x4 wf[kNT], xf[kMT];
-#pragma unroll
-            for (int i = 0; i < kNT; ++i) {
-                const int row = wn + 32 * i + col;
-                wf[i] = *reinterpret_cast<const i32x4 *>(w + row * BK + 16 * turned<BK>(row, 2 * k + h));
+    const int wave = threadIdx.x >> 6, wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
+    int stage = 0, turn = 0;
+    for (int64_t tile = first; tile < end; tile += beside, turn = (turn + 1) & (kStages - 1)) {
+        i32x16 acc[kNT][kMT] = {};
+        for (int t = 0; t < steps; ++t) {
+            // this step's loads are all but the last of the steps after it (a tile's first step has more of them)
+            stand();
+            if (left >= kAhead) wait_but<(kAhead - 1) * kLoads>();
+            else wait_but<0>();
+            stand();
+            if (a.width % 16 && t == steps - 1) {
+                loads.mask(t * kStep, a.width, s.w[stage]);
+                stand();
+                __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS)
             }
-#pragma unroll
-            for (int j = 0; j < kMT; ++j) {
-                const int row = wm + 32 * j + col;
-                xf[j] = *reinterpret_cast<const i32x4 *>(x + row * BK + 16 * turned<BK>(row, 2 * k + h));
-            }
-#pragma unroll
-            for (int i = 0; i < kNT; ++i)
-#pragma unroll
-                for (int j = 0; j < kMT; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[i], xf[j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_s_barrier();  // ... of all waves, and the stage before has been read by all
+            stand();
+            load();
+            multiply<kMT, kNT>(s.x[stage] + wm * kStep, s.w[stage] + wn * kStep, acc);
+            stage = (stage + 1) & (kStages - 1);
+            --left;
         }
+        finish<T, GELU>(a, LinearTile<BM, BN>(a, tile), s, turn, wm, wn, acc);
     }
-    __syncthreads();  // the tiles' memory is free
+}
 
-    // by 32 rows of a wave through LDS, so that a row's outputs are stored side by side
-    T *stage = reinterpret_cast<T *>(shared) + wave * 32 * kPitch;
-    constexpr int kVec = 16 / (int)sizeof(T), kLanes = 32 * kNT / kVec;  // of a row
-#pragma unroll
-    for (int j = 0; j < kMT; ++j) {
-        const int m = wm + 32 * j + col;
-        const float xs = m < rows ? a.x_scale[m0 + m] : 0.0f;
-#pragma unroll
-        for (int i = 0; i < kNT; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int n = 32 * i + 2 * r + 4 * h;
-                float o[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    o[e] = (float)acc[i][j][r + e] * xs * scales[0][wn + n + e] + scales[1][wn + n + e];
-                    if (a.gelu) o[e] = gelu(o[e]);
-                }
-                store_pack<T, 4>(stage + col * kPitch + n, o);
-            }
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int i = 0; i < 32 * kLanes / 64; ++i) {
-            const int part = i * 64 + lane, row = part / kLanes, n = part % kLanes * kVec;
-            const int left = columns - wn - n;
-            if (wm + 32 * j + row < rows && left > 0) {
-                T *y = static_cast<T *>(a.y) + (m0 + wm + 32 * j + row) * a.y_stride + n0 + wn + n;
-                const T *s = stage + row * kPitch + n;
-                if (left >= kVec) {
-                    *reinterpret_cast<Pack<T, kVec> *>(y) = *reinterpret_cast<const Pack<T, kVec> *>(s);
-                } else {
-                    for (int e = 0; e < left; ++e) y[e] = s[e];
-                }
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+// Rows that begin anywhere: 64 x 64 outputs a workgroup, chunks through registers, one
+// step at a time.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
+    constexpr int B = 64;
+    __shared__ LinearShared<B, B> s;
+    const LinearTile<B, B> t(a, blockIdx.x);
+    if (threadIdx.x < B) {
+        const int m = min((int)threadIdx.x, t.rows - 1), n = t.n0 + min((int)threadIdx.x, t.columns - 1);
+        s.x_scale[0][threadIdx.x] = a.x_scale[t.m0 + m];
+        s.w_scale[0][threadIdx.x] = a.w_scale[n];
+        s.bias[0][threadIdx.x] = a.bias ? a.bias[n] : 0.0f;
     }
+    const int row = threadIdx.x / kChunks, chunk = turned(row, threadIdx.x % kChunks);
+    const int8_t *x = a.x + (t.m0 + min(row, t.rows - 1)) * a.x_stride, *w = a.w + (t.n0 + min(row, t.columns - 1)) * a.w_stride;
+    const int wave = threadIdx.x >> 6, wm = (wave & 1) * (B / 2), wn = (wave >> 1) * (B / 2);
+    i32x16 acc[1][1] = {};
+    for (int k0 = 0; k0 < a.width; k0 += kStep) {
+        const i32x4 xv = load_chunk(x, k0 + 16 * chunk, a.width), wv = load_chunk(w, k0 + 16 * chunk, a.width);
+        __syncthreads();
+        *reinterpret_cast<i32x4 *>(s.x[0] + 16 * threadIdx.x) = xv;
+        *reinterpret_cast<i32x4 *>(s.w[0] + 16 * threadIdx.x) = wv;
+        __syncthreads();
+        multiply<1, 1>(s.x[0] + wm * kStep, s.w[0] + wn * kStep, acc);
+    }
+    if (a.gelu) finish<T, true>(a, t, s, 0, wm, wn, acc);
+    else finish<T, false>(a, t, s, 0, wm, wn, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -259,21 +403,32 @@ __global__ void __launch_bounds__(64 * kFewWaves) linear_few_kernel(LinearArgs a
     }
 }
 
-template <typename T, int BM, int BN, int BK>
-hipError_t launch_tiles(LinearArgs a, hipStream_t stream) {
+// launch(part) over the rows of a, by as many as `most` tiles hold.
+template <typename T, int BM, int BN, typename F>
+hipError_t by_tiles(LinearArgs a, F &&launch) {
     a.column_tiles = (a.outputs + BN - 1) / BN;
-    // by as many rows as a launch holds
     const int64_t rows = a.rows, most = kMaxWorkgroups / a.column_tiles * BM;
     hipError_t err = hipSuccess;
     for (int64_t first = 0; first < rows && err == hipSuccess; first += most) {
         LinearArgs part = a;
         part.rows = std::min(rows - first, most);
         part.advance(first, sizeof(T));
-        const dim3 grid((uint32_t)((part.rows + BM - 1) / BM * a.column_tiles));
-        hipLaunchKernelGGL((linear_kernel<T, BM, BN, BK>), grid, dim3(kThreads), 0, stream, part);
+        part.tiles = (part.rows + BM - 1) / BM * a.column_tiles;
+        launch(part);
         err = hipGetLastError();
     }
     return err;
+}
+
+template <typename T, int BM, int BN>
+hipError_t launch_tiles(const LinearArgs &a, int per_cu, int n_cus, hipStream_t stream) {
+    const int64_t workgroups = std::max(per_cu * n_cus / 8 * 8, 8);
+
+    return by_tiles<T, BM, BN>(a, [&](const LinearArgs &part) {
+        const dim3 grid((uint32_t)std::min(part.tiles, workgroups));
+        if (a.gelu) hipLaunchKernelGGL((linear_kernel<T, true, BM, BN>), grid, dim3(kThreads), 0, stream, part);
+        else hipLaunchKernelGGL((linear_kernel<T, false, BM, BN>), grid, dim3(kThreads), 0, stream, part);
+    });
 }
 
 template <typename T, int MT>
@@ -286,14 +441,17 @@ hipError_t launch_few(const LinearArgs &a, hipStream_t stream) {
 
 hipError_t launch_linear(LinearArgs a, int32_t dtype, int n_cus, hipStream_t stream) {
     const auto fits = [](const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 16 == 0; };
-    a.aligned = fits(a.x, a.x_stride) && fits(a.w, a.w_stride);
     return with_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
         if (a.rows <= 16) return launch_few<T, 1>(a, stream);
         if (a.rows <= 32) return launch_few<T, 2>(a, stream);
+        if (!fits(a.x, a.x_stride) || !fits(a.w, a.w_stride))
+            return by_tiles<T, 64, 64>(a, [&](const LinearArgs &part) {
+                hipLaunchKernelGGL((linear_any_kernel<T>), dim3((uint32_t)part.tiles), dim3(kThreads), 0, stream, part);
+            });
         const int64_t tiles = (a.rows + 127) / 128 * ((a.outputs + 127) / 128);
-        if (tiles < 2 * (int64_t)n_cus) return launch_tiles<T, 64, 64, 128>(a, stream);
-        return launch_tiles<T, 128, 128, 128>(a, stream);
+        if (tiles < 2 * (int64_t)n_cus) return launch_tiles<T, 64, 64>(a, 4, n_cus, stream);
+        return launch_tiles<T, 128, 128>(a, 2, n_cus, stream);
     });
 }
 
