@@ -189,16 +189,63 @@ __device__ __forceinline__ void multiply(const int8_t *__restrict__ x, const int
     }
 }
 
-// A wave's outputs of a tile.  Returns whether every store was made.
-template <typename T, bool GELU, int KM, int KN, typename S, typename Tile>
-__device__ __forceinline__ void finish(const LinearArgs &a, const Tile &t, const S &s, int turn, int wm, int wn,
+// Four outputs and four others of a lane's row, 8 on, for eight side by side: the first
+// eight of sixteen in the lower half of the wave, the others in the upper.
+template <typename T>
+__device__ __forceinline__ Pack<T, 8> side_by_side(const float (&o)[8]) {
+    Pack<T, 8> out;
+    if constexpr (sizeof(T) == 2) {
+        Pack<T, 8> mine;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mine.v[e] = static_cast<T>(o[e]);
+        const i32x4 v = __builtin_bit_cast(i32x4, mine);
+        const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+        const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+        const i32x4 u = {(int)p[0], (int)q[0], (int)p[1], (int)q[1]};
+        out = __builtin_bit_cast(Pack<T, 8>, u);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[e]), __float_as_uint(o[e + 4]), false, false);
+            out.v[e] = static_cast<T>(__uint_as_float(p[0]));
+            out.v[e + 4] = static_cast<T>(__uint_as_float(p[1]));
+        }
+    }
+    return out;
+}
+
+// The first `left` of a pack, all of it where FULL.
+template <bool FULL, typename T>
+__device__ __forceinline__ void store_left(T *y, const Pack<T, 8> &v, int left) {
+    if (FULL || left >= 8) {
+        *reinterpret_cast<Pack<T, 8> *>(y) = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e < left) y[e] = v.v[e];
+}
+
+// The compiler moves no access to memory over this.
+__device__ __forceinline__ void stand() { asm volatile("" ::: "memory"); }
+
+// A wave's outputs of a tile.  FULL: all of its rows and outputs are there.  Outputs of
+// 16 bits go through LDS (`room`, 2 KN KB of the wave's own), 32 rows at a time, so that a row's
+// are stored as 64 KN bytes in one piece: in the pieces of 32 bytes that lanes hold
+// them stores alone took longer than all else (128000 x 512 to 1536: 233 us, 138
+// without its stores).
+template <typename T, bool GELU, bool FULL, int KM, int KN, typename S, typename Tile>
+__device__ __forceinline__ void finish(const LinearArgs &a, const Tile &t, const S &s, int turn, int wm, int wn, int8_t *room,
                                        const i32x16 (&acc)[KN][KM]) {
+    constexpr bool kStaged = sizeof(T) == 2;
+    constexpr int kParts = 4 * KN;  // of 8 outputs, a row
     const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    const auto part_at = [](int row, int part) { return row * kParts + (part ^ (KN == 2 ? row & 7 : (row >> 1) & 3)); };
+    Pack<T, 8> *stage = reinterpret_cast<Pack<T, 8> *>(room);
+    T *y = static_cast<T *>(a.y) + (t.m0 + wm) * a.y_stride + t.n0 + wn;
 #pragma unroll
     for (int j = 0; j < KM; ++j) {
-        const int m = wm + 32 * j + col;
-        const float xs = s.x_scale[turn][m];
-        T *y = static_cast<T *>(a.y) + (t.m0 + m) * a.y_stride + t.n0;
+        const float xs = s.x_scale[turn][wm + 32 * j + col];
 #pragma unroll
         for (int i = 0; i < KN; ++i)
 #pragma unroll
@@ -212,39 +259,22 @@ __device__ __forceinline__ void finish(const LinearArgs &a, const Tile &t, const
                     o[e] = (float)acc[i][j][r + e] * xs * s.w_scale[turn][at] + s.bias[turn][at];
                     if (GELU) o[e] = gelu(o[e]);
                 }
-                // 8 outputs side by side: the first eight here, the others in the lane 32 on
-                Pack<T, 8> out;
-                if constexpr (sizeof(T) == 2) {
-                    Pack<T, 8> mine;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) mine.v[e] = static_cast<T>(o[e]);
-                    const i32x4 v = __builtin_bit_cast(i32x4, mine);
-                    const auto p = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
-                    const auto q = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-                    const i32x4 u = {(int)p[0], (int)q[0], (int)p[1], (int)q[1]};
-                    out = __builtin_bit_cast(Pack<T, 8>, u);
-                } else {
-                    float f[8];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(o[e]), __float_as_uint(o[e + 4]), false, false);
-                        f[e] = __uint_as_float(p[0]);
-                        f[e + 4] = __uint_as_float(p[1]);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) out.v[e] = static_cast<T>(f[e]);
-                }
-                const int first = wn + 32 * i + 2 * r + 8 * h, left = t.columns - first;
-                if (m < t.rows) {
-                    if (left >= 8) {
-                        *reinterpret_cast<Pack<T, 8> *>(y + first) = out;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e < left) y[first + e] = out.v[e];
-                    }
-                }
+                const Pack<T, 8> out = side_by_side<T>(o);
+                const int part = 4 * i + r / 4 + h;
+                if (kStaged) stage[part_at(col, part)] = out;
+                else if (FULL || wm + 32 * j + col < t.rows)
+                    store_left<FULL>(y + (int64_t)(32 * j + col) * a.y_stride + 8 * part, out, t.columns - wn - 8 * part);
             }
+        if (!kStaged) continue;
+        stand();
+#pragma unroll
+        for (int i = 0; i < kParts / 2; ++i) {
+            const int row = (64 * i + lane) / kParts, part = lane % kParts;
+            const Pack<T, 8> out = stage[part_at(row, part)];
+            if (FULL || wm + 32 * j + row < t.rows)
+                store_left<FULL>(y + (int64_t)(32 * j + row) * a.y_stride + 8 * part, out, t.columns - wn - 8 * part);
+        }
+        stand();
     }
 }
 
@@ -253,9 +283,6 @@ template <int N>
 __device__ __forceinline__ void wait_but() {
     __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x070);
 }
-
-// The compiler moves no access to memory over this.
-__device__ __forceinline__ void stand() { asm volatile("" ::: "memory"); }
 
 template <typename T, bool GELU, int BM, int BN>
 __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
@@ -298,14 +325,19 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
     for (int i = 0; i < kAhead; ++i) load();
 
     const int wave = threadIdx.x >> 6, wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
-    int stage = 0, turn = 0;
+    // a whole tile's stores, at least; they come between the loads of kAhead steps, which need not wait for them
+    constexpr int kStores = 2 * kMT * kNT;
+    static_assert(BM == BN, "finish() takes a quarter of a stage");
+    int stage = 0, turn = 0, since = kAhead;
     for (int64_t tile = first; tile < end; tile += beside, turn = (turn + 1) & (kStages - 1)) {
         i32x16 acc[kNT][kMT] = {};
         for (int t = 0; t < steps; ++t) {
             // this step's loads are all but the last of the steps after it (a tile's first step has more of them)
             stand();
-            if (left >= kAhead) wait_but<(kAhead - 1) * kLoads>();
-            else wait_but<0>();
+            if (left < kAhead) wait_but<0>();
+            else if (since < kAhead) wait_but<(kAhead - 1) * kLoads + kStores>();
+            else wait_but<(kAhead - 1) * kLoads>();
+            ++since;
             stand();
             if (a.width % 16 && t == steps - 1) {
                 loads.mask(t * kStep, a.width, s.w[stage]);
@@ -319,7 +351,20 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
             stage = (stage + 1) & (kStages - 1);
             --left;
         }
-        finish<T, GELU>(a, LinearTile<BM, BN>(a, tile), s, turn, wm, wn, acc);
+        // the stage that was multiplied last is free until the next step's barrier
+        const int last = (stage + kStages - 1) & (kStages - 1);
+        int8_t *room = (wave < 2 ? s.x[last] : s.w[last]) + (wave & 1) * (BM * kStep / 2);
+        stand();
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS)
+        __builtin_amdgcn_s_barrier();
+        stand();
+        const LinearTile<BM, BN> t(a, tile);
+        if (t.rows == BM && t.columns == BN) {
+            finish<T, GELU, true>(a, t, s, turn, wm, wn, room, acc);
+            since = 0;
+        } else {
+            finish<T, GELU, false>(a, t, s, turn, wm, wn, room, acc);
+        }
     }
 }
 
@@ -348,8 +393,9 @@ __global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
         __syncthreads();
         multiply<1, 1>(s.x[0] + wm * kStep, s.w[0] + wn * kStep, acc);
     }
-    if (a.gelu) finish<T, true>(a, t, s, 0, wm, wn, acc);
-    else finish<T, false>(a, t, s, 0, wm, wn, acc);
+    int8_t *room = s.x[1] + wave * (B * kStep / 2);  // (stages are not used but the first)
+    if (a.gelu) finish<T, true, false>(a, t, s, 0, wm, wn, room, acc);
+    else finish<T, false, false>(a, t, s, 0, wm, wn, room, acc);
 }
 
 // ---------------------------------------------------------------------------
