@@ -69,7 +69,7 @@ constexpr int kStep = 64, kAhead = 3, kStages = kAhead + 1, kChunks = kStep / 16
 
 __device__ const __attribute__((aligned(16))) int8_t kZeros[16] = {};
 
-__device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row >> 1) & 3); }
+__device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row >> 2) & 3); }
 
 #define FLOCK_TO_LDS(FROM, TO, SIZE)                                                                  \
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(FROM),         \
@@ -173,20 +173,26 @@ struct LinearLoads {
 template <int KM, int KN>
 __device__ __forceinline__ void multiply(const int8_t *__restrict__ x, const int8_t *__restrict__ w, i32x16 (&acc)[KN][KM]) {
     const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
+    constexpr int kParts = kStep / 32;
+    i32x4 wf[kParts][KN], xf[kParts][KM];
 #pragma unroll
-    for (int k = 0; k < kStep / 32; ++k) {
-        i32x4 wf[KN], xf[KM];
+    for (int k = 0; k < kParts; ++k) {
 #pragma unroll
         for (int i = 0; i < KN; ++i)
-            wf[i] = *reinterpret_cast<const i32x4 *>(w + (32 * i + col) * kStep + 16 * turned(col, 2 * k + h));
+            wf[k][i] = *reinterpret_cast<const i32x4 *>(w + (32 * i + col) * kStep + 16 * turned(col, 2 * k + h));
 #pragma unroll
         for (int j = 0; j < KM; ++j)
-            xf[j] = *reinterpret_cast<const i32x4 *>(x + (32 * j + col) * kStep + 16 * turned(col, 2 * k + h));
+            xf[k][j] = *reinterpret_cast<const i32x4 *>(x + (32 * j + col) * kStep + 16 * turned(col, 2 * k + h));
+    }
+    // (all of a step's factors are on their way before the first product)
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
 #pragma unroll
         for (int i = 0; i < KN; ++i)
 #pragma unroll
-            for (int j = 0; j < KM; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[i], xf[j], acc[i][j], 0, 0, 0);
-    }
+            for (int j = 0; j < KM; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[k][i], xf[k][j], acc[i][j], 0, 0, 0);
 }
 
 // Four outputs and four others of a lane's row, 8 on, for eight side by side: the first
@@ -218,7 +224,12 @@ __device__ __forceinline__ Pack<T, 8> side_by_side(const float (&o)[8]) {
 template <bool FULL, typename T>
 __device__ __forceinline__ void store_left(T *y, const Pack<T, 8> &v, int left) {
     if (FULL || left >= 8) {
-        *reinterpret_cast<Pack<T, 8> *>(y) = v;
+        // (past the caches: outputs larger than they are have no use of them, 210 -> 174 us above)
+        typedef i32x4 __attribute__((aligned(2))) Words;
+        const Words *from = reinterpret_cast<const Words *>(&v);
+        Words *to = reinterpret_cast<Words *>(y);
+#pragma unroll
+        for (int e = 0; e < (int)sizeof(v) / 16; ++e) __builtin_nontemporal_store(from[e], to + e);
         return;
     }
 #pragma unroll
