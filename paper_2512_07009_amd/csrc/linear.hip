@@ -65,11 +65,11 @@ __device__ __forceinline__ float gelu(float x) {
 // loads alone (they come back in order), with one barrier a step.
 // ---------------------------------------------------------------------------
 
-constexpr int kStep = 64, kAhead = 3, kStages = kAhead + 1, kChunks = kStep / 16;
+constexpr int kStep = 128, kAhead = 1, kStages = kAhead + 1, kChunks = kStep / 16;
 
 __device__ const __attribute__((aligned(16))) int8_t kZeros[16] = {};
 
-__device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row >> 2) & 3); }
+__device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
 
 #define FLOCK_TO_LDS(FROM, TO, SIZE)                                                                  \
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(FROM),         \
@@ -392,15 +392,22 @@ __global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
         s.w_scale[0][threadIdx.x] = a.w_scale[n];
         s.bias[0][threadIdx.x] = a.bias ? a.bias[n] : 0.0f;
     }
-    const int row = threadIdx.x / kChunks, chunk = turned(row, threadIdx.x % kChunks);
-    const int8_t *x = a.x + (t.m0 + min(row, t.rows - 1)) * a.x_stride, *w = a.w + (t.n0 + min(row, t.columns - 1)) * a.w_stride;
     const int wave = threadIdx.x >> 6, wm = (wave & 1) * (B / 2), wn = (wave >> 1) * (B / 2);
     i32x16 acc[1][1] = {};
     for (int k0 = 0; k0 < a.width; k0 += kStep) {
-        const i32x4 xv = load_chunk(x, k0 + 16 * chunk, a.width), wv = load_chunk(w, k0 + 16 * chunk, a.width);
+        i32x4 xv[B * kChunks / kThreads], wv[B * kChunks / kThreads];
+#pragma unroll
+        for (int i = 0; i < B * kChunks / kThreads; ++i) {
+            const int slot = i * kThreads + threadIdx.x, row = slot / kChunks, k = k0 + 16 * turned(row, slot % kChunks);
+            xv[i] = load_chunk(a.x + (t.m0 + min(row, t.rows - 1)) * a.x_stride, k, a.width);
+            wv[i] = load_chunk(a.w + (t.n0 + min(row, t.columns - 1)) * a.w_stride, k, a.width);
+        }
         __syncthreads();
-        *reinterpret_cast<i32x4 *>(s.x[0] + 16 * threadIdx.x) = xv;
-        *reinterpret_cast<i32x4 *>(s.w[0] + 16 * threadIdx.x) = wv;
+#pragma unroll
+        for (int i = 0; i < B * kChunks / kThreads; ++i) {
+            *reinterpret_cast<i32x4 *>(s.x[0] + 16 * (i * kThreads + threadIdx.x)) = xv[i];
+            *reinterpret_cast<i32x4 *>(s.w[0] + 16 * (i * kThreads + threadIdx.x)) = wv[i];
+        }
         __syncthreads();
         multiply<1, 1>(s.x[0] + wm * kStep, s.w[0] + wn * kStep, acc);
     }
