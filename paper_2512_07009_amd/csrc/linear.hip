@@ -342,6 +342,8 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
     int stage = 0, turn = 0, since = kAhead;
     for (int64_t tile = first; tile < end; tile += beside, turn = (turn + 1) & (kStages - 1)) {
         i32x16 acc[kNT][kMT] = {};
+        // (a wave that multiplies goes before the one beside it that has a tile's outputs to make: 2 to 4%)
+        __builtin_amdgcn_s_setprio(2);
         for (int t = 0; t < steps; ++t) {
             // this step's loads are all but the last of the steps after it (a tile's first step has more of them)
             stand();
@@ -363,6 +365,7 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
             --left;
         }
         // the stage that was multiplied last is free until the next step's barrier
+        __builtin_amdgcn_s_setprio(0);
         const int last = (stage + kStages - 1) & (kStages - 1);
         int8_t *room = (wave < 2 ? s.x[last] : s.w[last]) + (wave & 1) * (BM * kStep / 2);
         stand();
