@@ -698,8 +698,11 @@ flock_status append_tracks(int32_t dtype, const void *new_k, int64_t new_k_strid
  *   seen: j <= p_i, and with window > 0: j > p_i - window
  *   out_i = sum over the tokens seen of softmax_j(t) v_j
  * A query that sees no token gets zeros.  Keys and values are taken as the whole
- * numbers they are, with products in 32-bit sums and a softmax in 32 bits; weights
- * are rounded to 11 bits for the product with v.
+ * numbers they are, with products in 32-bit sums and a softmax in 32 bits.  A query's
+ * dimension is rounded by at most 2^-17 of its head's largest (a head whose largest is
+ * below 2^-100 is zeros, one that is not finite gives NaN), and weights are rounded to 11
+ * bits for the product with v, relative to the largest v_scale seen before them.
+ * Scales are >= 0, or NaN: then what sees the page is NaN.
  *
  * Arguments:
  *   dtype          FLOCK_F16 or FLOCK_BF16: q, out.

@@ -9,16 +9,18 @@
 // The heads that share a kv head are packed with the queries as rows r = (i, g), 16 a
 // workgroup.  Its four waves take every fourth page and join what they have in LDS;
 // where there are few rows, several workgroups share a row's pages and a second kernel
-// joins them.  Bound by the bytes of the pages for single tokens.
+// joins them.
 //
-// Whole numbers of 8 bits are exact in float16, so products run on the matrix cores in
-// float16 (16 x 16 x 32) with no rounding of keys and values.  Queries in bfloat16 are
-// scaled by a power of two that brings their largest dimension near 1: exact above 2^-14
-// of it, and below off by 2^-25 of it at most.  Scores are transposed, S^T = K Q^T: a
-// lane holds 16 tokens of one row, four of each 16, which is the order in which the
-// product with the values takes its weights; the values lie in pages so that a lane's 16
-// bytes are the factors of two such products.  Weights carry the page's scale relative to
-// the largest so far and are rounded to float16 (2^-11), after they were summed in 32 bits.
+// Scores are products of whole numbers on the matrix cores (16 x 16 x 64, 8 bits, exact
+// sums): keys as they lie in pages, and queries as 256 a + b with a, b in 8 bits.  That
+// rounds a query's dimension by 2^-17 of its row's largest at most, below what its own
+// 16-bit type leaves of it, and spares a lane 80 instructions a page to convert keys to
+// float16 (of some 350).  Scores are transposed, S^T = K Q^T: a
+// lane holds 16 tokens of one row, four of each 16, which is the order in which the product
+// with the values takes its weights.  Values lie in pages so that a lane's 16 bytes are the
+// factors of two such products (16 x 16 x 32); they go to float16, which holds them exactly.
+// Weights carry the page's scale relative to the largest so far, within the exponent, and
+// are rounded to float16 (2^-11) after they were summed in 32 bits.
 
 #include "attention_common.h"
 #include "tracks_common.h"
@@ -38,7 +40,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef half_t f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kThreads = 256, kWaves = 4, kRows = 16;
-constexpr float kSlack = 8.0f;  // scores above the shift by less are left there
+constexpr float kSlack = 8.0f;    // scores above the shift by less are left there
+constexpr float kQuery = 32512.0f;  // a query's largest dimension as 256 a + b
 
 // Eight whole numbers in float16: 1024 + u, u = x + 128, is 0x6400 | u, and 1152 is taken off.
 __device__ __forceinline__ f16x8 to_half(int lo, int hi) {
@@ -63,7 +66,7 @@ __device__ __forceinline__ float over_parts(float x, F &&f) {
 
 // What a workgroup, or the one that joins, works on.
 struct Item {
-    int track, head, row0, rows;   // rows row0 .. row0 + rows of the track's queries and shared heads
+    int head, row0, rows;          // rows row0 .. row0 + rows of the track's queries and shared heads
     int first_page, pages;         // that any of them sees
     Track at;
     bool ok;
@@ -73,9 +76,8 @@ __device__ __forceinline__ Item item_of(const TrackAttentionArgs &a, int64_t slo
     Item s;
     int64_t tile;
     const int group = a.group;
-    s.track = find_track(a.tracks.n_tracks, slot,
-                         [&](int i) { return (int64_t)a.tracks.offsets[i] * group / kRows + i; }, &tile);
-    s.at = track_of(a.tracks, s.track);
+    s.at = find_track(a.tracks, slot, (int64_t)a.tracks.total * group / kRows + a.tracks.n_tracks,
+                      [=](int offset, int t) { return (int64_t)offset * group / kRows + t; }, &tile);
     s.head = head;
     const int64_t all = (int64_t)s.at.n * group;
     s.ok = s.at.ok && tile >= 0 && tile * kRows < all;
@@ -89,8 +91,61 @@ __device__ __forceinline__ Item item_of(const TrackAttentionArgs &a, int64_t slo
     return s;
 }
 
+// What a lane holds of a row: its dimensions as right factors, the tokens that it sees
+// (lo, own], and the softmax so far.
+template <int DI>
+struct Row {
+    i32x4 high[DI], low[DI];
+    float factor;          // of products of whole numbers and the page's scale
+    int lo, own;
+    float shift, total;
+    f32x4 acc[4 * DI];
+};
+
 template <typename T, int DI, int CAP>
-__global__ void __launch_bounds__(kThreads) track_attention_kernel(TrackAttentionArgs a) {
+__device__ __forceinline__ void begin(Row<DI> &w, const TrackAttentionArgs &a, const Item &it, int r) {
+    const int part = (threadIdx.x & 63) >> 4, dim = a.cache.dim;
+    const bool valid = r < it.rows;
+    const int row = it.row0 + (valid ? r : 0), query = row / a.group, head = it.head * a.group + row % a.group;
+    w.own = it.at.length - it.at.n + query;
+    w.lo = a.window ? max(w.own, 0) - a.window : -1;
+    w.shift = -INFINITY;
+    w.total = 0.0f;
+#pragma unroll
+    for (int b = 0; b < 4 * DI; ++b) w.acc[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const T *q = static_cast<const T *>(a.q) + (int64_t)(it.at.row0 + query) * a.q_stride + head * dim;
+    float x[DI][16];
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < DI; ++i) {
+        const int d = 16 * (part + 4 * i);
+        load_some<T, 16>(q + min(d, dim - 16), valid && d < dim ? 16 : 0, x[i]);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bits = max(bits, __float_as_uint(x[i][e]) & 0x7fffffffu);
+    }
+    bits = max(bits, (uint32_t)__shfl_xor((int)bits, 16));
+    bits = max(bits, (uint32_t)__shfl_xor((int)bits, 32));
+    // (a row below 2^-100 is zeros, one that is not finite NaN)
+    const float most = __uint_as_float(bits);
+    const bool finite = bits < 0x7f800000u, some = finite && most >= 0x1p-100f;
+    const float per = some ? kQuery / most : 0.0f;
+#pragma unroll
+    for (int i = 0; i < DI; ++i) {
+        w.high[i] = w.low[i] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int n = some ? (int)rintf(x[i][e] * per) : 0, high = (n + 128) >> 8;
+            w.high[i][e >> 2] |= (high & 0xff) << (8 * (e & 3));
+            w.low[i][e >> 2] |= (n & 0xff) << (8 * (e & 3));
+        }
+    }
+    // (finite, so that a zero times it stays one)
+    const float scale = CAP == kHigh ? a.scale / a.cap : CAP == kLow ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+    w.factor = finite ? fminf(scale * (some ? most / kQuery : 1.0f), 0x1p127f) : NAN;
+}
+
+template <typename T, int DI, int CAP>
+__global__ void __launch_bounds__(kThreads, DI == 1 ? 4 : 2) track_attention_kernel(TrackAttentionArgs a) {
     constexpr int kBlocks = 4 * DI;   // 16 dimensions each, at most
     __shared__ float sums[kWaves][kRows][64 * DI + 1];
     __shared__ float stats[2][kWaves][kRows];
@@ -102,172 +157,180 @@ __global__ void __launch_bounds__(kThreads) track_attention_kernel(TrackAttentio
     if (!it.ok) return;
     const int active = max((it.pages + a.split_pages - 1) / a.split_pages, 1);
     if (split >= active) return;
-    const int p0 = it.first_page + split * a.split_pages;
-    const int p1 = min(p0 + a.split_pages, it.first_page + it.pages);
+    const int p0 = it.first_page + split * a.split_pages + wave;
+    const int p1 = min(it.first_page + (split + 1) * a.split_pages, it.first_page + it.pages);
+    const int count = p1 > p0 ? (p1 - p0 + kWaves - 1) / kWaves : 0;  // of this wave: p0, p0 + 4, ...
 
-    // this lane's row: its dimensions as right factors, and the tokens that it sees
-    const bool valid = r < it.rows;
-    const int row = it.row0 + (valid ? r : 0), query = row / a.group, head = it.head * a.group + row % a.group;
-    const int own = it.at.length - it.at.n + query;
-    const int lo = a.window ? max(own, 0) - a.window : -1;  // tokens in (lo, own]
-    const T *qp = static_cast<const T *>(a.q) + (int64_t)(it.at.row0 + query) * a.q_stride + head * dim;
-    f16x8 q[DI][2];
-    float q_scale = 1.0f;
-    {
-        float x[DI][2][8], most = 0.0f;
-#pragma unroll
-        for (int i = 0; i < DI; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int d = 16 * (part + 4 * i) + 8 * h;
-                load_some<T, 8>(qp + min(d, dim - 8), valid && d < dim ? 8 : 0, x[i][h]);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[i][h][e]));
-            }
-        most = over_parts(most, [](float u, float v) { return fmaxf(u, v); });
-        int exponent = 0;
-        if (sizeof(T) == 2 && !__is_same(T, half_t) && most > 0.0f && most < INFINITY) exponent = ilogbf(most);
-        q_scale = ldexpf(1.0f, max(exponent, -126));
-#pragma unroll
-        for (int i = 0; i < DI; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[i][h][e] = (half_t)ldexpf(x[i][h][e], -max(exponent, -126));
-    }
-    // (finite, so that a zero times it stays one)
-    const float factor = fminf((CAP == kHigh ? a.scale / a.cap : CAP == kLow ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e) * q_scale, 0x1p127f);
+    Row<DI> w;
+    begin<T, DI, CAP>(w, a, it, r);
     const float cap2 = a.cap * kLog2e, constant = attention::cap_constant<CAP>(cap2);
 
-    f32x4 acc[kBlocks] = {};
-    float shift = -INFINITY, total = 0.0f, unit = 0.0f;
-    // tokens that every row sees, of pages that lie within
-    const int all_lo = a.window ? max(it.at.length - it.at.n + (it.row0 + it.rows - 1) / a.group, 0) - a.window : -1;
-    const int all_own = it.at.length - it.at.n + it.row0 / a.group;
-    int batch = 0, my_page = -1;
+    // the wave's pages, 64 at a time, a lane each
+    int my_page = -1;
     float my_k = 0.0f, my_v = 0.0f;
-    for (int n = 0, p = p0 + wave; p < p1; ++n, p += kWaves) {
-        if ((n & 63) == 0) {  // the next 64 pages of this wave, a lane each
-            batch = n;
-            const int mine = p + kWaves * lane;
-            my_page = mine < p1 ? a.tracks.table[(int64_t)it.track * a.tracks.table_stride + mine] : -1;
-            if (my_page >= a.cache.pages) my_page = -1;
-            const int64_t block = (int64_t)max(my_page, 0) * a.cache.kv_heads + it.head;
-            my_k = my_page >= 0 ? a.cache.k_scale[block] : 0.0f;
-            my_v = my_page >= 0 ? a.cache.v_scale[block] : 0.0f;
+    const int32_t *table = a.tracks.table + (int64_t)it.at.index * a.tracks.table_stride;
+    // the next page from the n-th on that is one of the pool (tokens of others are not seen), and its number
+    const auto next = [&](int &n) {
+        for (; n < count; ++n) {
+            if ((n & 63) == 0) {
+                const int mine = n + lane;
+                my_page = mine < count ? table[p0 + kWaves * mine] : -1;
+                if (my_page >= a.cache.pages) my_page = -1;
+                const int64_t block = (int64_t)max(my_page, 0) * a.cache.kv_heads + it.head;
+                my_k = my_page >= 0 ? a.cache.k_scale[block] : 0.0f;
+                my_v = my_page >= 0 ? a.cache.v_scale[block] : 0.0f;
+            }
+            const int page = __builtin_amdgcn_readlane(my_page, n & 63);
+            if (page >= 0) return page;
         }
-        const int page = __builtin_amdgcn_readlane(my_page, n - batch);
-        if (page < 0) continue;  // no page of the pool: its tokens are not seen
-        const float k_scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_k), n - batch));
-        const float v_scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_v), n - batch));
-        const int64_t block = ((int64_t)page * a.cache.kv_heads + it.head) * (kPage * dim);
-        const int8_t *kp = a.cache.k + block + r * dim + 16 * part, *vp = a.cache.v + block + r * kPage + 16 * part;
-        i32x4 kr[4][DI], vr[kBlocks];
+        return -1;
+    };
+    const auto scale_of = [&](float mine, int n) {
+        return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), n & 63));
+    };
+    i32x4 kr[4][DI], vr[kBlocks];
+    const auto load_k = [&](int page) {
+        const int8_t *p = a.cache.k + ((int64_t)page * a.cache.kv_heads + it.head) * (kPage * dim) + r * dim + 16 * part;
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
             for (int i = 0; i < DI; ++i) {
                 kr[b][i] = i32x4{0, 0, 0, 0};
-                if (part + 4 * i < blocks) kr[b][i] = *reinterpret_cast<const i32x4 *>(kp + 16 * b * dim + 64 * i);
+                if (part + 4 * i < blocks) kr[b][i] = *reinterpret_cast<const i32x4 *>(p + 16 * b * dim + 64 * i);
             }
+    };
+    const auto load_v = [&](int page) {
+        const int8_t *p = a.cache.v + ((int64_t)page * a.cache.kv_heads + it.head) * (kPage * dim) + r * kPage + 16 * part;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
-            if (b < blocks) vr[b] = *reinterpret_cast<const i32x4 *>(vp + 16 * b * kPage);
+            if (b < blocks) vr[b] = *reinterpret_cast<const i32x4 *>(p + 16 * b * kPage);
+    };
+
+    float unit = 0.0f;  // largest scale of values so far
+    // tokens that every row sees, of pages that lie within
+    const int all_lo = a.window ? max(it.at.length - it.at.n + (it.row0 + it.rows - 1) / a.group, 0) - a.window : -1;
+    const int all_own = it.at.length - it.at.n + it.row0 / a.group;
+    int n = 0, page = next(n);
+    if (page >= 0) {
+        load_k(page);
+        load_v(page);
+    }
+    while (page >= 0) {
+        const int token0 = (p0 + kWaves * n) * kPage;
+        const float k_scale = scale_of(my_k, n), v_scale = scale_of(my_v, n);
+        ++n;
+        const int after = next(n);
+        // the values' scale against the largest: 2^-40 for less, which is lost beside it
+        float keep_v = 1.0f;
+        if (v_scale > unit) {
+            keep_v = unit / v_scale;
+            unit = v_scale;
+        }
+        const bool near = v_scale > unit * 0x1p-40f;
+        const float level = near ? __log2f(v_scale / unit) : -40.0f, back = near ? unit / v_scale : 0x1p40f;
+        const bool inside = token0 + kPage - 1 <= all_own && token0 > all_lo;
+        f16x8 weights[2];
         f32x16 s;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            f32x4 c = {};
+            i32x4 high = {0, 0, 0, 0}, low = {0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < DI; ++i) {
-                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(to_half(kr[b][i][0], kr[b][i][1]), q[i][0], c, 0, 0, 0);
-                c = __builtin_amdgcn_mfma_f32_16x16x32_f16(to_half(kr[b][i][2], kr[b][i][3]), q[i][1], c, 0, 0, 0);
+                high = __builtin_amdgcn_mfma_i32_16x16x64_i8(kr[b][i], w.high[i], high, 0, 0, 0);
+                low = __builtin_amdgcn_mfma_i32_16x16x64_i8(kr[b][i], w.low[i], low, 0, 0, 0);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[4 * b + e] = c[e];
+            for (int e = 0; e < 4; ++e) s[4 * b + e] = (float)(256 * high[e] + low[e]);
         }
-        float f = factor * k_scale;
+        if (after >= 0) load_k(after);
+        float f = w.factor * k_scale;
         if (f > 0x1p127f) f = 0x1p127f;  // (NaN stays)
-        if (CAP == kNoCap) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] *= f;
-        } else {
+        if (CAP != kNoCap) {
             attention::cap_parts<CAP>(s, f);
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[e] = attention::capped<CAP>(s[e], cap2, constant);
+            f = 1.0f;
         }
-        const int token0 = p * kPage;
-        if (token0 + kPage - 1 > all_own || token0 <= all_lo) {
+        if (!inside) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int token = token0 + 16 * (e >> 2) + 4 * part + (e & 3);
-                if (token > own || token <= lo) s[e] = -INFINITY;
+                s[e] = token > w.own || token <= w.lo ? -INFINITY : s[e] * f;
             }
+            f = 1.0f;
         }
         float most = s[0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) most = fmaxf(most, s[e]);
-        most = over_parts(most, [](float u, float v) { return fmaxf(u, v); });
-        if (__any(most > shift + kSlack || (shift == -INFINITY && most > shift))) {
-            const float now = fmaxf(shift, most);
-            const float keep = shift == -INFINITY ? 0.0f : attention::exp2_fast(shift - now);
-            total *= keep;
+        most = over_parts(most, [](float u, float v) { return fmaxf(u, v); }) * f;
+        float keep = keep_v;
+        if (__any(most > w.shift + kSlack || (w.shift == -INFINITY && most > w.shift))) {
+            const float now = fmaxf(w.shift, most);
+            const float less = w.shift == -INFINITY ? 0.0f : attention::exp2_fast(w.shift - now);
+            w.total *= less;
+            keep *= less;
+            w.shift = now;
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
-            shift = now;
-        }
-        const float base = shift == -INFINITY ? 0.0f : shift;
-        if (v_scale > unit) {
-            const float keep = unit / v_scale;
+            for (int b = 0; b < kBlocks; ++b) w.acc[b] *= keep;
+        } else if (keep_v != 1.0f) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
-            unit = v_scale;
+            for (int b = 0; b < kBlocks; ++b) w.acc[b] *= keep;
         }
-        const float ratio = unit > 0.0f ? v_scale / unit : v_scale;
-        f16x8 weights[2];
+        const float base = (w.shift == -INFINITY ? 0.0f : w.shift) - level;
+        float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float w = attention::exp2_fast(s[e] - base);
-            total += w;
-            weights[e >> 3][e & 7] = (half_t)(w == 0.0f ? 0.0f : w * ratio);
+            const float x = attention::exp2_fast(__builtin_fmaf(s[e], f, -base));
+            sum += x;
+            weights[e >> 3][e & 7] = (half_t)x;
+        }
+        w.total += sum * back;
+        if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page
+            const float none = over_parts(sum, [](float u, float v) { return u + v; }) == 0.0f ? 0.0f : NAN;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) w.acc[b] += none;
         }
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
             if (b < blocks) {
-                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(to_half(vr[b][0], vr[b][1]), weights[0], acc[b], 0, 0, 0);
-                acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(to_half(vr[b][2], vr[b][3]), weights[1], acc[b], 0, 0, 0);
+                const f16x8 v0 = to_half(vr[b][0], vr[b][1]), v1 = to_half(vr[b][2], vr[b][3]);
+                w.acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, weights[0], w.acc[b], 0, 0, 0);
+                w.acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, weights[1], w.acc[b], 0, 0, 0);
             }
+        if (after >= 0) load_v(after);
+        page = after;
     }
-    total = over_parts(total, [](float u, float v) { return u + v; });
 
     // the waves' parts, joined
-    if (part == 0) stats[0][wave][r] = shift;
+    w.total = over_parts(w.total, [](float u, float v) { return u + v; });
+    if (part == 0) stats[0][wave][r] = w.shift;
     __syncthreads();
     float now = stats[0][0][r];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) now = fmaxf(now, stats[0][w][r]);
-    const float keep = shift == -INFINITY ? (total == total ? 0.0f : total) : attention::exp2_fast(shift - now);
-    if (part == 0) stats[1][wave][r] = keep == 0.0f ? 0.0f : total * keep;
+    for (int v = 1; v < kWaves; ++v) now = fmaxf(now, stats[0][v][r]);
+    // (a shift that nothing has moved: no token, or none but NaN)
+    const float keep = w.shift == -INFINITY ? (w.total == w.total ? 0.0f : w.total) : attention::exp2_fast(w.shift - now);
+    if (part == 0) stats[1][wave][r] = w.total * keep;
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sums[wave][r][16 * b + 4 * part + e] = keep == 0.0f ? 0.0f : acc[b][e] * (keep * unit);
+        for (int e = 0; e < 4; ++e) sums[wave][r][16 * b + 4 * part + e] = w.acc[b][e] * (keep * unit);
     __syncthreads();
-    for (int i = threadIdx.x; i < kRows * dim; i += kThreads) {
+    for (int i = threadIdx.x; i < it.rows * dim; i += kThreads) {
         const int rr = i / dim, d = i % dim;
-        if (rr >= it.rows) break;
         const float l = (stats[1][0][rr] + stats[1][1][rr]) + (stats[1][2][rr] + stats[1][3][rr]);
         const float o = (sums[0][rr][d] + sums[1][rr][d]) + (sums[2][rr][d] + sums[3][rr][d]);
-        const int rw = it.row0 + rr;
-        const int64_t bird = it.at.row0 + rw / a.group;
-        const int hd = it.head * a.group + rw % a.group;
+        const int row = it.row0 + rr;
+        const int64_t bird = it.at.row0 + row / a.group;
+        const int head = it.head * a.group + row % a.group;
         if (active == 1) {
-            static_cast<T *>(a.out)[bird * a.out_stride + hd * dim + d] = static_cast<T>(l == 0.0f ? 0.0f : o / l);
+            static_cast<T *>(a.out)[bird * a.out_stride + head * dim + d] = static_cast<T>(l == 0.0f ? 0.0f : o / l);
         } else {
-            const int64_t to = ((int64_t)split * a.tracks.total + bird) * a.q_heads + hd;
+            const int64_t to = ((int64_t)split * a.tracks.total + bird) * a.q_heads + head;
             a.part_out[to * dim + d] = o;
             if (d == 0) {
                 float m = stats[0][0][rr];
-                for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stats[0][w][rr]);
+                for (int v = 1; v < kWaves; ++v) m = fmaxf(m, stats[0][v][rr]);
                 a.part_stat[2 * to] = m;
                 a.part_stat[2 * to + 1] = l;
             }
@@ -275,7 +338,8 @@ __global__ void __launch_bounds__(kThreads) track_attention_kernel(TrackAttentio
     }
 }
 
-// Rows whose pages several workgroups shared.
+// Rows whose pages several workgroups shared: a wave a row, a lane a dimension (or two)
+// of all shares, whose weights are found first, a lane a share.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) track_join_kernel(TrackAttentionArgs a) {
     const int64_t id = blockIdx.x;
@@ -283,24 +347,42 @@ __global__ void __launch_bounds__(kThreads) track_join_kernel(TrackAttentionArgs
     if (!it.ok) return;
     const int active = (it.pages + a.split_pages - 1) / a.split_pages;
     if (active <= 1) return;
-    const int dim = a.cache.dim;
-    for (int i = threadIdx.x; i < it.rows * dim; i += kThreads) {
-        const int rw = it.row0 + i / dim, d = i % dim;
+    const int dim = a.cache.dim, lane = threadIdx.x & 63, d0 = min(lane, dim - 1), d1 = min(lane + 64, dim - 1);
+    const int64_t pitch = (int64_t)a.tracks.total * a.q_heads;
+    for (int rr = threadIdx.x >> 6; rr < it.rows; rr += kWaves) {
+        const int rw = it.row0 + rr;
         const int64_t bird = it.at.row0 + rw / a.group;
         const int hd = it.head * a.group + rw % a.group;
-        const int64_t pitch = (int64_t)a.tracks.total * a.q_heads, at = bird * a.q_heads + hd;
+        const int64_t at = bird * a.q_heads + hd;
         float m = -INFINITY;
-        for (int s = 0; s < active; ++s) m = fmaxf(m, a.part_stat[2 * (s * pitch + at)]);
-        float o = 0.0f, l = 0.0f;
-        for (int s = 0; s < active; ++s) {
-            const int64_t from = s * pitch + at;
-            const float shift = a.part_stat[2 * from], total = a.part_stat[2 * from + 1];
-            if (total == 0.0f) continue;
-            const float keep = shift == -INFINITY ? total : attention::exp2_fast(shift - m);
-            l += total * keep;
-            o += a.part_out[from * dim + d] * keep;
+        for (int s = lane; s < active; s += 64) m = fmaxf(m, a.part_stat[2 * (s * pitch + at)]);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+        for (int first = 0; first < active; first += 64) {
+            const int s = first + lane;
+            float shift = -INFINITY, total = 0.0f;
+            if (s < active) {
+                shift = a.part_stat[2 * (s * pitch + at)];
+                total = a.part_stat[2 * (s * pitch + at) + 1];
+            }
+            const float keep = total == 0.0f ? 0.0f : shift == -INFINITY ? total : attention::exp2_fast(shift - m);
+            float sum = total * keep;
+#pragma unroll
+            for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+            l += sum;
+            const int here = min(active - first, 64);
+#pragma unroll 8
+            for (int i = 0; i < here; ++i) {
+                const float *p = a.part_out + ((first + i) * pitch + at) * dim;
+                const float k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(keep), i));
+                o0 += p[d0] * k;
+                o1 += p[d1] * k;
+            }
         }
-        static_cast<T *>(a.out)[bird * a.out_stride + hd * dim + d] = static_cast<T>(l == 0.0f ? 0.0f : o / l);
+        T *out = static_cast<T *>(a.out) + bird * a.out_stride + hd * dim;
+        if (lane < dim) out[lane] = static_cast<T>(l == 0.0f ? 0.0f : o0 / l);
+        if (lane + 64 < dim) out[lane + 64] = static_cast<T>(l == 0.0f ? 0.0f : o1 / l);
     }
 }
 
@@ -312,10 +394,11 @@ void launch_cap(const TrackAttentionArgs &a, dim3 grid, hipStream_t stream) {
 }
 
 template <typename T>
-hipError_t launch_type(TrackAttentionArgs a, const TrackPlan &p, hipStream_t stream) {
+hipError_t launch_type(const TrackAttentionArgs &a, const TrackPlan &p, hipStream_t stream) {
     const int64_t items = p.slots * a.cache.kv_heads;
-    if (a.cache.dim <= 64) launch_cap<T, 1>(a, dim3((uint32_t)(items * p.splits)), stream);
-    else launch_cap<T, 2>(a, dim3((uint32_t)(items * p.splits)), stream);
+    const dim3 grid((uint32_t)(items * p.splits));
+    if (a.cache.dim <= 64) launch_cap<T, 1>(a, grid, stream);
+    else launch_cap<T, 2>(a, grid, stream);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || p.splits == 1) return err;
     hipLaunchKernelGGL((track_join_kernel<T>), dim3((uint32_t)items), dim3(kThreads), 0, stream, a);
@@ -330,12 +413,14 @@ TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_page
     const int group = q_heads / kv_heads;
     p.slots = (int64_t)total * group / kRows + n_tracks;
     const int64_t items = std::max<int64_t>(p.slots * kv_heads, 1);
-    // enough workgroups for the card, of at least a page a wave
-    int64_t splits = (8 * (int64_t)n_cus + items - 1) / items;
-    splits = std::max<int64_t>(std::min<int64_t>(splits, (max_pages + kWaves - 1) / kWaves), 1);
-    p.split_pages = (int32_t)((max_pages + splits - 1) / std::max<int64_t>(splits, 1));
-    p.split_pages = std::max(p.split_pages, 1);
-    p.splits = (int32_t)std::max<int64_t>((max_pages + p.split_pages - 1) / p.split_pages, 1);
+    // as many workgroups as the card holds at a time, of at least two pages a wave: more of
+    // them cost more to begin and to join than they even out (24 tracks of 27000, heads of
+    // 128: two a compute unit 69 us, four 78, eight 88; 500 tracks of up to 5400: one
+    // workgroup a track 85 us, two 97)
+    int64_t splits = 2 * (int64_t)n_cus / items;
+    splits = std::max<int64_t>(std::min<int64_t>(splits, (max_pages + 2 * kWaves - 1) / (2 * kWaves)), 1);
+    p.split_pages = std::max((int32_t)((max_pages + splits - 1) / splits), 1);
+    p.splits = std::max((max_pages + p.split_pages - 1) / p.split_pages, 1);
     return p;
 }
 

@@ -38,6 +38,11 @@ __device__ __forceinline__ uint32_t rounded(float x, float per) {
 
 __device__ __forceinline__ float byte_of(const i32x4 &c, int i) { return (float)(int8_t)(c[i >> 2] >> (8 * (i & 3))); }
 
+// Numbers of pages that the rows may touch: a track of n rows at most n / 64 + 2.
+__host__ __device__ inline int64_t append_pages(int32_t n_tracks, int32_t total) {
+    return (int64_t)total / kPage + 2 * (int64_t)n_tracks;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
     extern __shared__ float fresh[];    // [new tokens of the page][dim]
@@ -47,9 +52,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
     const int64_t item = blockIdx.x >> 1;
     const int head = (int)(item % heads);
     int64_t within;
-    const int t = find_track(a.tracks.n_tracks, item / heads,
-                             [&](int i) { return (int64_t)(a.tracks.offsets[i] / kPage) + 2 * (int64_t)i; }, &within);
-    const Track track = track_of(a.tracks, t);
+    const Track track = find_track(a.tracks, item / heads, append_pages(a.tracks.n_tracks, a.tracks.total),
+                                   [](int offset, int t) { return (int64_t)(offset / kPage) + 2 * (int64_t)t; }, &within);
     if (!track.ok || track.n > track.length || within < 0) return;
     const int start = track.length - track.n;
     const int64_t first = (start / kPage + within) * kPage;  // the page's first token
@@ -57,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
     const int s0 = (int)max((int64_t)start - first, (int64_t)0), s1 = (int)min((int64_t)track.length - first, (int64_t)kPage);
     const int n = s1 - s0;  // new tokens of this page
     if (n <= 0) return;
-    const int page = a.tracks.table[(int64_t)t * a.tracks.table_stride + first / kPage];
+    const int page = a.tracks.table[(int64_t)track.index * a.tracks.table_stride + first / kPage];
     if (page < 0 || page >= a.cache.pages) return;
     const int64_t row0 = track.row0 + (first + s0 - start);
     const int64_t block = (int64_t)page * heads + head;
@@ -158,8 +162,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
 }  // namespace
 
 int64_t append_workgroups(int32_t n_tracks, int32_t total, int32_t kv_heads) {
-    // a track of n rows touches at most n / 64 + 2 pages
-    return ((int64_t)total / kPage + 2 * (int64_t)n_tracks) * kv_heads * 2;
+    return append_pages(n_tracks, total) * kv_heads * 2;
 }
 
 hipError_t launch_append(const AppendArgs &a, int32_t dtype, hipStream_t stream) {

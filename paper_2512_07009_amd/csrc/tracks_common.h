@@ -22,36 +22,50 @@ __device__ __forceinline__ constexpr int token_at(int place) { return 16 * (plac
 
 // One track's part of the batch: `n` rows, which are the last of its `length` tokens.
 struct Track {
-    int32_t row0, n, length;
+    int32_t index, row0, n, length;
     bool ok;
 };
 
-__device__ __forceinline__ Track track_of(const TrackArgs &a, int t) {
-    Track s;
-    s.row0 = a.offsets[t];
-    const int32_t end = a.offsets[t + 1];
-    s.length = a.lengths[t];
-    s.ok = s.row0 >= 0 && end >= s.row0 && end <= a.total && s.length >= 0 && s.length <= (int64_t)a.max_pages * kPage;
-    s.n = end - s.row0;
-    return s;
-}
-
-// Track of a work item, and the item's number within the track: items of track t
-// begin at begin(t), which grows with t.  All lanes of a wave look together, a 64th
-// of what is left each time.
+// The track of work item `item` of `items`, and the item's number within it: items of
+// track t begin at begin(offsets[t], t), which grows with t.
+//
+// Most workgroups live for a few trips to memory, so this is one: the lanes of a wave
+// read 64 tracks around the place where the item is in an even batch, and the track's
+// offsets and length come from them.  Where the track is not among those, a 64th of what
+// is left is looked up each time.
 template <typename F>
-__device__ __forceinline__ int find_track(int n_tracks, int64_t item, F &&begin, int64_t *within) {
-    int lo = 0, left = n_tracks;
-    while (left > 1) {
-        const int step = (left + 63) >> 6, t = lo + step * (int)(threadIdx.x & 63);
-        const bool before = t < lo + left && begin(t) <= item;
-        const int at = max(__builtin_popcountll(__ballot(before)), 1) - 1;
-        left = min(step, left - at * step);
-        lo += at * step;
+__device__ __forceinline__ Track find_track(const TrackArgs &a, int64_t item, int64_t items, F &&begin, int64_t *within) {
+    const int lane = threadIdx.x & 63, n = a.n_tracks;
+    const int middle = (int)((float)item / (float)items * (float)n);
+    int lo = max(min(middle - 31, n - 63), 0);
+    Track s;
+    for (bool sought = false;; sought = true) {
+        const int t = min(lo + lane, n);
+        const int32_t offset = a.offsets[t], length = a.lengths[min(t, n - 1)];
+        const uint64_t before = __ballot(lo + lane < n && begin(offset, t) <= item);
+        int at = 63 - __builtin_clzll(before | 1);
+        if (!sought && ((before & 1) == 0 ? lo > 0 : at == 63)) {
+            lo = 0;
+            for (int left = n; left > 1;) {
+                const int step = (left + 63) >> 6, u = lo + step * lane;
+                const bool early = u < lo + left && begin(a.offsets[min(u, n)], u) <= item;
+                const int past = max(__builtin_popcountll(__ballot(early)), 1) - 1;
+                left = min(step, left - past * step);
+                lo += past * step;
+            }
+            continue;
+        }
+        if (sought) at = 0;
+        at = __builtin_amdgcn_readfirstlane(at);
+        s.index = lo + at;
+        s.row0 = __builtin_amdgcn_readlane(offset, at);
+        const int32_t end = __builtin_amdgcn_readlane(offset, at + 1);
+        s.length = __builtin_amdgcn_readlane(length, at);
+        s.ok = s.row0 >= 0 && end >= s.row0 && end <= a.total && s.length >= 0 && s.length <= (int64_t)a.max_pages * kPage;
+        s.n = end - s.row0;
+        *within = item - begin(s.row0, s.index);
+        return s;
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    *within = item - begin(lo);
-    return lo;
 }
 
 }  // namespace tracks

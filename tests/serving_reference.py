@@ -160,9 +160,9 @@ def attention_tracks(q, cache, offsets, table, lengths, scale, cap=0.0, window=0
             K[~seen0], V[~seen0] = 0, 0
             Q = q[offsets[t]:offsets[t + 1], h].double()
             s = scale * (Q @ K.T)
-            # 32-bit sums; dimensions of bfloat16 queries far below the largest are off by 2^-25 of it
-            ds = scale * (E32 * (8 + D ** 0.5) * (Q.abs() @ K.abs().T)
-                          + (2.0 ** -25 * Q.abs().amax(1, keepdim=True) * K.abs().sum(1) if q.dtype == torch.bfloat16 else 0.0))
+            # A query's dimension is a whole number of 1 / 32512 of its row's largest: off by half of that (2^-16 / 1.98),
+            # a score by the sum of those times the keys.  Then steps in 32 bits.
+            ds = scale * (E32 * (8 + D ** 0.5) * (Q.abs() @ K.abs().T) + Q.abs().amax(1, keepdim=True) / 65024 * K.abs().sum(1))
             if cap:
                 s = cap * torch.tanh(s / cap)
                 ds = ds + 4e-7 * (s.abs() if cap > 64 else torch.full_like(s, cap))
