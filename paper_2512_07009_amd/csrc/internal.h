@@ -374,10 +374,11 @@ struct AppendArgs {
     int64_t k_stride, v_stride;
     const int32_t *xy, *time;
     int32_t n_time, n_y, pairs, interleaved;
+    int32_t pack_shift, pair_shift;    // set by launch_append
     uint64_t step[kRotaryMaxPairs];
 };
 int64_t append_workgroups(int32_t n_tracks, int32_t total, int32_t kv_heads);
-hipError_t launch_append(const AppendArgs &a, int32_t dtype, hipStream_t stream);
+hipError_t launch_append(AppendArgs a, int32_t dtype, hipStream_t stream);
 
 struct TrackAttentionArgs {
     TrackArgs tracks;

@@ -9,6 +9,10 @@
 // A workgroup takes the keys or the values of one page and kv head, so that no two
 // meet in memory: values stay in LDS in 32 bits between the search for the largest and
 // the rounding.  Tokens that the page does not get yet are left as they are.
+//
+// With a token or a few a track the time is that of the trips to memory one after the
+// other (the track, its page, the rows with their positions and the page's scale), and a
+// workgroup is one wave; clips take four waves.
 
 #include "tracks_common.h"
 
@@ -17,16 +21,20 @@ namespace {
 
 using namespace tracks;
 
-constexpr int kThreads = 256;
-constexpr int kVec = 8;
+constexpr int kVec = 8, kItems = 4;
+constexpr int kPad = 4;  // between tokens in LDS: those of four parts of a dimension's places lie in other banks
 
 // Largest |x| over the workgroup, as bits (those of NaN are the largest).
+template <int WAVES>
 __device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t *slot) {
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+    if (WAVES == 1) return x;
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
     __syncthreads();
-    return max(max(slot[0], slot[1]), max(slot[2], slot[3]));
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) x = max(x, slot[w]);
+    return x;
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
@@ -38,23 +46,35 @@ __device__ __forceinline__ uint32_t rounded(float x, float per) {
 
 __device__ __forceinline__ float byte_of(const i32x4 &c, int i) { return (float)(int8_t)(c[i >> 2] >> (8 * (i & 3))); }
 
-// Numbers of pages that the rows may touch: a track of n rows at most n / 64 + 2.
-__host__ __device__ inline int64_t append_pages(int32_t n_tracks, int32_t total) {
-    return (int64_t)total / kPage + 2 * (int64_t)n_tracks;
+// Pages that rows go to are numbered as a first one of every track, and after those the
+// others: a track of n rows has at most (n + 62) / 64 of them, so that those of the track
+// whose rows begin at `offset` begin at other_pages().
+__host__ __device__ inline int64_t other_pages(int32_t offset, int32_t track) {
+    const int64_t each = (int64_t)(offset / kPage) + track, pairs = offset / 2;
+    return each < pairs ? each : pairs;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
-    extern __shared__ float fresh[];    // [new tokens of the page][dim]
-    __shared__ uint32_t slot[4];
-    const int dim = a.cache.dim, heads = a.cache.kv_heads;
+template <typename T, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
+    constexpr int kThreads = 64 * WAVES;
+    extern __shared__ __attribute__((aligned(16))) float fresh[];    // [new tokens of the page][pitch]
+    __shared__ uint32_t slot[WAVES];
+    __shared__ int32_t places[3][kPage];   // time, y, x of the new tokens
+    const int dim = a.cache.dim, pitch = dim + kPad, heads = a.cache.kv_heads;
     const bool values = blockIdx.x & 1;
     const int64_t item = blockIdx.x >> 1;
     const int head = (int)(item % heads);
-    int64_t within;
-    const Track track = find_track(a.tracks, item / heads, append_pages(a.tracks.n_tracks, a.tracks.total),
-                                   [](int offset, int t) { return (int64_t)(offset / kPage) + 2 * (int64_t)t; }, &within);
-    if (!track.ok || track.n > track.length || within < 0) return;
+    const int64_t number = item / heads, others = number - a.tracks.n_tracks;
+    int64_t within = 0;
+    Track track;
+    if (others < 0) {
+        track = track_of(a.tracks, (int)number);
+    } else {
+        track = find_track(a.tracks, others, other_pages(a.tracks.total, a.tracks.n_tracks), other_pages, &within);
+        if (within < 0) return;
+        ++within;
+    }
+    if (!track.ok || track.n > track.length) return;
     const int start = track.length - track.n;
     const int64_t first = (start / kPage + within) * kPage;  // the page's first token
     if (first >= track.length) return;
@@ -62,60 +82,81 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
     const int n = s1 - s0;  // new tokens of this page
     if (n <= 0) return;
     const int page = a.tracks.table[(int64_t)track.index * a.tracks.table_stride + first / kPage];
-    if (page < 0 || page >= a.cache.pages) return;
     const int64_t row0 = track.row0 + (first + s0 - start);
+
+    // a new token is 2^pack_shift packs, its turns 2^pair_shift pairs: some of them none.
+    // A thread's pairs are the same of every token.
+    const int pairs = values ? 0 : a.pairs, p = threadIdx.x & ((1 << a.pair_shift) - 1);
+    const uint64_t step = p < pairs ? a.step[p] : 0;
+    if (page < 0 || page >= a.cache.pages) return;
     const int64_t block = (int64_t)page * heads + head;
-
-    // the new tokens, in 32 bits
-    const T *in = static_cast<const T *>(values ? a.v : a.k) + row0 * (values ? a.v_stride : a.k_stride) + head * dim;
-    const int64_t stride = values ? a.v_stride : a.k_stride;
-    const int packs = dim / kVec;
-    uint32_t largest = 0;
-    for (int i = threadIdx.x; i < n * packs; i += kThreads) {
-        const int token = i / packs, d = i % packs * kVec;
-        float x[kVec];
-        load_pack<T, kVec>(in + token * stride + d, x);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) {
-            fresh[token * dim + d + e] = x[e];
-            if (values || d + e >= 2 * a.pairs) largest = max(largest, magnitude(x[e]));
-        }
-    }
-    if (!values && a.pairs) {
-        __syncthreads();
-        for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
-            const int token = i / a.pairs, p = i % a.pairs;
-            const int64_t bird = row0 + token;
-            const int64_t pos = p < a.n_time ? a.time[bird] : a.xy[2 * bird + (p < a.n_time + a.n_y ? 1 : 0)];
-            const uint64_t phase = (uint64_t)pos * a.step[p];
-            const float turns = (float)(int32_t)(phase >> 32) * 0x1p-32f;
-            const float sn = __builtin_amdgcn_sinf(turns), cs = __builtin_amdgcn_cosf(turns);
-            float *u = fresh + token * dim + (a.interleaved ? 2 * p : p), *v = u + (a.interleaved ? 1 : a.pairs);
-            const float x = *u, y = *v;
-            *u = x * cs - y * sn;
-            *v = x * sn + y * cs;
-            largest = max(largest, max(magnitude(*u), magnitude(*v)));
-        }
-    }
-    largest = block_largest(largest, slot);
-
-    // the page's scale; one with values that are not finite has NaN, and zeros
     float *scales = values ? a.cache.v_scale : a.cache.k_scale;
     const float old = s0 > 0 ? scales[block] : 0.0f;
+    int8_t *const v = a.cache.v + block * (kPage * dim);
+    if (pairs && (int)threadIdx.x < n) {
+        const int64_t bird = row0 + threadIdx.x;
+        if (a.n_time) places[0][threadIdx.x] = a.time[bird];
+        if (pairs > a.n_time) {
+            const int2 xy = reinterpret_cast<const int2 *>(a.xy)[bird];
+            places[1][threadIdx.x] = xy.y;
+            places[2][threadIdx.x] = xy.x;
+        }
+    }
+
+    // the new tokens, in 32 bits: kItems packs of a thread on their way at a time
+    const int64_t stride = values ? a.v_stride : a.k_stride;
+    const T *in = static_cast<const T *>(values ? a.v : a.k) + row0 * stride + head * dim;
+    uint32_t largest = 0;
+    for (int first_item = threadIdx.x; first_item < n << a.pack_shift; first_item += kItems * kThreads) {
+        float x[kItems][kVec];
+#pragma unroll
+        for (int m = 0; m < kItems; ++m) {
+            const int i = first_item + m * kThreads, token = i >> a.pack_shift, d = (i & ((1 << a.pack_shift) - 1)) * kVec;
+            load_some<T, kVec>(in + token * stride + d, token < n && d < dim ? kVec : 0, x[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < kItems; ++m) {
+            const int i = first_item + m * kThreads, token = i >> a.pack_shift, d = (i & ((1 << a.pack_shift) - 1)) * kVec;
+            if (token >= n || d >= dim) continue;
+            *reinterpret_cast<float4 *>(fresh + token * pitch + d) = make_float4(x[m][0], x[m][1], x[m][2], x[m][3]);
+            *reinterpret_cast<float4 *>(fresh + token * pitch + d + 4) = make_float4(x[m][4], x[m][5], x[m][6], x[m][7]);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (d + e >= 2 * pairs) largest = max(largest, magnitude(x[m][e]));
+        }
+    }
+    __syncthreads();
+    if (p < pairs) {
+        const int axis = p < a.n_time ? 0 : p < a.n_time + a.n_y ? 1 : 2;
+        for (int token = threadIdx.x >> a.pair_shift; token < n; token += kThreads >> a.pair_shift) {
+            const uint64_t phase = (uint64_t)(int64_t)places[axis][token] * step;
+            const float turned = (float)(int32_t)(phase >> 32) * 0x1p-32f;
+            const float sn = __builtin_amdgcn_sinf(turned), cs = __builtin_amdgcn_cosf(turned);
+            float *u = fresh + token * pitch + (a.interleaved ? 2 * p : p), *w = u + (a.interleaved ? 1 : pairs);
+            const float x = *u, y = *w, c = x * cs - y * sn, d = x * sn + y * cs;
+            *u = c;
+            *w = d;
+            largest = max(largest, max(magnitude(c), magnitude(d)));
+        }
+    }
+    largest = block_largest<WAVES>(largest, slot);
+    __syncthreads();  // (every turned token is there, and every wave has read the old scale)
+
+    // the page's scale; one with values that are not finite has NaN, and zeros
     float scale = largest < 0x7f800000u ? __uint_as_float(largest) / 127.0f : __uint_as_float(0x7fc00000u);
     if (largest < __float_as_uint(0x1p-100f)) scale = 0.0f;
     scale = old > scale || old != old ? old : scale;
     const float per = scale > 0.0f ? 1.0f / scale : 0.0f;
     const float again = old == scale ? 1.0f : per * old;  // what held tokens are multiplied by
     const bool held = s0 > 0 && old != scale;             // ... and have to be
-    __syncthreads();                                      // (every wave has read the old scale)
     if (threadIdx.x == 0) scales[block] = scale;
 
     if (!values) {
         int8_t *k = a.cache.k + block * (kPage * dim);
-        const int chunks = dim / 16, begin = held ? 0 : s0 * chunks;
-        for (int i = begin + threadIdx.x; i < s1 * chunks; i += kThreads) {
-            const int token = i / chunks, d = i % chunks * 16;
+        const int shift = a.pack_shift - 1;  // chunks of 16
+        for (int i = ((held ? 0 : s0) << shift) + threadIdx.x; i < s1 << shift; i += kThreads) {
+            const int token = i >> shift, d = (i & ((1 << shift) - 1)) * 16;
+            if (d >= dim) continue;
             i32x4 *at = reinterpret_cast<i32x4 *>(k + token * dim + d);
             i32x4 c = {0, 0, 0, 0};
             if (token < s0) {
@@ -123,36 +164,35 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) c[e >> 2] |= rounded(byte_of(before, e), again) << (8 * (e & 3));
             } else {
-                const float *x = fresh + (token - s0) * dim + d;
+                const float4 *x = reinterpret_cast<const float4 *>(fresh + (token - s0) * pitch + d);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) c[e >> 2] |= rounded(x[e], per) << (8 * (e & 3));
+                for (int e = 0; e < 4; ++e) {
+                    const float4 y = x[e];
+                    c[e] = rounded(y.x, per) | rounded(y.y, per) << 8 | rounded(y.z, per) << 16 | rounded(y.w, per) << 24;
+                }
             }
             *at = c;
         }
         return;
     }
-    int8_t *v = a.cache.v + block * (kPage * dim);
+    // 16 places of a dimension at a time, which hold tokens 4 part + 0 .. 3 of each 16
+    const uint64_t ends = s1 == 64 ? ~0ull : (1ull << s1) - 1, begins = (1ull << s0) - 1;
     for (int i = threadIdx.x; i < 4 * dim; i += kThreads) {
-        const int d = i % dim, part = i / dim;  // 16 places of a dimension
-        // whether any of its tokens is written
-        bool some = false, all = true;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int token = token_at(16 * part + e);
-            const bool writes = token < s1 && (token >= s0 || held);
-            some |= writes;
-            all &= writes && token >= s0;
-        }
-        if (!some) continue;
+        const int part = i & 3, d = i >> 2;
+        const auto of_part = [&](uint64_t tokens) {
+            const uint64_t m = tokens >> (4 * part);
+            return (uint32_t)(m & 0xf) | (uint32_t)(m >> 12 & 0xf0) | (uint32_t)(m >> 24 & 0xf00) | (uint32_t)(m >> 36 & 0xf000);
+        };
+        const uint32_t brings = of_part(ends & ~begins), holds = held ? of_part(begins) : 0;
+        if (!(brings | holds)) continue;
         i32x4 *at = reinterpret_cast<i32x4 *>(v + d * kPage + 16 * part);
         i32x4 before = {0, 0, 0, 0}, c = {0, 0, 0, 0};
-        if (!all) before = *at;
+        if (brings != 0xffff) before = *at;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const int token = token_at(16 * part + e);
             uint32_t b = (uint32_t)(before[e >> 2] >> (8 * (e & 3))) & 0xffu;
-            if (token >= s0 && token < s1) b = rounded(fresh[(token - s0) * dim + d], per);
-            else if (token < s0 && held) b = rounded(byte_of(before, e), again);
+            if (brings >> e & 1) b = rounded(fresh[(16 * (e >> 2) + 4 * part + (e & 3) - s0) * pitch + d], per);
+            else if (holds >> e & 1) b = rounded(byte_of(before, e), again);
             c[e >> 2] |= b << (8 * (e & 3));
         }
         *at = c;
@@ -162,15 +202,23 @@ __global__ void __launch_bounds__(kThreads) append_kernel(AppendArgs a) {
 }  // namespace
 
 int64_t append_workgroups(int32_t n_tracks, int32_t total, int32_t kv_heads) {
-    return append_pages(n_tracks, total) * kv_heads * 2;
+    return (n_tracks + other_pages(total, n_tracks)) * kv_heads * 2;
 }
 
-hipError_t launch_append(const AppendArgs &a, int32_t dtype, hipStream_t stream) {
+hipError_t launch_append(AppendArgs a, int32_t dtype, hipStream_t stream) {
     const dim3 grid((uint32_t)append_workgroups(a.tracks.n_tracks, a.tracks.total, a.cache.kv_heads));
-    const size_t lds = (size_t)std::min<int64_t>(kPage, a.tracks.total) * a.cache.dim * sizeof(float);
+    const size_t lds = (size_t)std::min<int64_t>(kPage, a.tracks.total) * (a.cache.dim + kPad) * sizeof(float);
+    const auto shift = [](int n) {
+        int s = 0;
+        while ((1 << s) < n) ++s;
+        return s;
+    };
+    a.pack_shift = shift(a.cache.dim / kVec);
+    a.pair_shift = shift(a.pairs);
     return with_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL((append_kernel<T>), grid, dim3(kThreads), lds, stream, a);
+        if (a.tracks.total <= 8 * (int64_t)a.tracks.n_tracks) hipLaunchKernelGGL((append_kernel<T, 1>), grid, dim3(64), lds, stream, a);
+        else hipLaunchKernelGGL((append_kernel<T, 4>), grid, dim3(256), lds, stream, a);
         return hipGetLastError();
     });
 }

@@ -26,6 +26,20 @@ struct Track {
     bool ok;
 };
 
+__device__ __forceinline__ Track make_track(const TrackArgs &a, int index, int32_t row0, int32_t end, int32_t length) {
+    Track s;
+    s.index = index;
+    s.row0 = row0;
+    s.n = end - row0;
+    s.length = length;
+    s.ok = row0 >= 0 && end >= row0 && end <= a.total && length >= 0 && length <= (int64_t)a.max_pages * kPage;
+    return s;
+}
+
+__device__ __forceinline__ Track track_of(const TrackArgs &a, int t) {
+    return make_track(a, t, a.offsets[t], a.offsets[t + 1], a.lengths[t]);
+}
+
 // The track of work item `item` of `items`, and the item's number within it: items of
 // track t begin at begin(offsets[t], t), which grows with t.
 //
@@ -38,7 +52,6 @@ __device__ __forceinline__ Track find_track(const TrackArgs &a, int64_t item, in
     const int lane = threadIdx.x & 63, n = a.n_tracks;
     const int middle = (int)((float)item / (float)items * (float)n);
     int lo = max(min(middle - 31, n - 63), 0);
-    Track s;
     for (bool sought = false;; sought = true) {
         const int t = min(lo + lane, n);
         const int32_t offset = a.offsets[t], length = a.lengths[min(t, n - 1)];
@@ -57,12 +70,8 @@ __device__ __forceinline__ Track find_track(const TrackArgs &a, int64_t item, in
         }
         if (sought) at = 0;
         at = __builtin_amdgcn_readfirstlane(at);
-        s.index = lo + at;
-        s.row0 = __builtin_amdgcn_readlane(offset, at);
-        const int32_t end = __builtin_amdgcn_readlane(offset, at + 1);
-        s.length = __builtin_amdgcn_readlane(length, at);
-        s.ok = s.row0 >= 0 && end >= s.row0 && end <= a.total && s.length >= 0 && s.length <= (int64_t)a.max_pages * kPage;
-        s.n = end - s.row0;
+        const Track s = make_track(a, lo + at, __builtin_amdgcn_readlane(offset, at),
+                                   __builtin_amdgcn_readlane(offset, at + 1), __builtin_amdgcn_readlane(length, at));
         *within = item - begin(s.row0, s.index);
         return s;
     }
