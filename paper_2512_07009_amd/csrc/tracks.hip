@@ -39,9 +39,13 @@ __device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t *slot) {
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// x / scale to the nearest whole number, given what to multiply by instead (0: zeros).
-__device__ __forceinline__ uint32_t rounded(float x, float per) {
-    return per > 0.0f ? (uint32_t)(int)fminf(fmaxf(rintf(x * per), -127.0f), 127.0f) & 0xffu : 0u;
+// x / scale to the nearest whole number, ties to even, given 1 / scale: the low byte of
+// what is left of x / scale beside 1.5 x 2^23 (|x / scale| is below 128).
+__device__ __forceinline__ uint32_t rounded(float x, float per) { return __float_as_uint(__builtin_fmaf(x, per, 12582912.0f)); }
+
+// Four low bytes in one word.
+__device__ __forceinline__ int bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
 __device__ __forceinline__ float byte_of(const i32x4 &c, int i) { return (float)(int8_t)(c[i >> 2] >> (8 * (i & 3))); }
@@ -147,8 +151,9 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
     if (largest < __float_as_uint(0x1p-100f)) scale = 0.0f;
     scale = old > scale || old != old ? old : scale;
     const float per = scale > 0.0f ? 1.0f / scale : 0.0f;
-    const float again = old == scale ? 1.0f : per * old;  // what held tokens are multiplied by
-    const bool held = s0 > 0 && old != scale;             // ... and have to be
+    const float again = per * old;             // what held tokens are multiplied by
+    const bool held = s0 > 0 && old != scale;  // ... and have to be
+    const int kept = scale == scale ? -1 : 0;  // bits (a page with NaN holds zeros)
     if (threadIdx.x == 0) scales[block] = scale;
 
     if (!values) {
@@ -162,13 +167,15 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
             if (token < s0) {
                 const i32x4 before = *at;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) c[e >> 2] |= rounded(byte_of(before, e), again) << (8 * (e & 3));
+                for (int e = 0; e < 4; ++e)
+                    c[e] = kept & bytes(rounded(byte_of(before, 4 * e), again), rounded(byte_of(before, 4 * e + 1), again),
+                                        rounded(byte_of(before, 4 * e + 2), again), rounded(byte_of(before, 4 * e + 3), again));
             } else {
                 const float4 *x = reinterpret_cast<const float4 *>(fresh + (token - s0) * pitch + d);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float4 y = x[e];
-                    c[e] = rounded(y.x, per) | rounded(y.y, per) << 8 | rounded(y.z, per) << 16 | rounded(y.w, per) << 24;
+                    c[e] = kept & bytes(rounded(y.x, per), rounded(y.y, per), rounded(y.z, per), rounded(y.w, per));
                 }
             }
             *at = c;
@@ -186,14 +193,22 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
         const uint32_t brings = of_part(ends & ~begins), holds = held ? of_part(begins) : 0;
         if (!(brings | holds)) continue;
         i32x4 *at = reinterpret_cast<i32x4 *>(v + d * kPage + 16 * part);
-        i32x4 before = {0, 0, 0, 0}, c = {0, 0, 0, 0};
-        if (brings != 0xffff) before = *at;
+        i32x4 c = {0, 0, 0, 0};
+        if (brings == 0xffff) {
+            const float *x = fresh + (4 * part - s0) * pitch + d;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            uint32_t b = (uint32_t)(before[e >> 2] >> (8 * (e & 3))) & 0xffu;
-            if (brings >> e & 1) b = rounded(fresh[(16 * (e >> 2) + 4 * part + (e & 3) - s0) * pitch + d], per);
-            else if (holds >> e & 1) b = rounded(byte_of(before, e), again);
-            c[e >> 2] |= b << (8 * (e & 3));
+            for (int e = 0; e < 4; ++e)
+                c[e] = kept & bytes(rounded(x[16 * e * pitch], per), rounded(x[(16 * e + 1) * pitch], per),
+                                    rounded(x[(16 * e + 2) * pitch], per), rounded(x[(16 * e + 3) * pitch], per));
+        } else {
+            const i32x4 before = *at;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                uint32_t b = (uint32_t)(before[e >> 2] >> (8 * (e & 3)));
+                if (brings >> e & 1) b = kept & rounded(fresh[(16 * (e >> 2) + 4 * part + (e & 3) - s0) * pitch + d], per);
+                else if (holds >> e & 1) b = kept & rounded(byte_of(before, e), again);
+                c[e >> 2] |= (b & 0xff) << (8 * (e & 3));
+            }
         }
         *at = c;
     }
