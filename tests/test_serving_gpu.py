@@ -1,0 +1,314 @@
+"""An encoder block trained on tracks and served in 8 bits: the norm's gradients in the
+block, a served block against the block itself (all at once, in clips, detection by
+detection), captured and replayed, on another stream, and what it refuses."""
+
+import math
+
+import pytest
+import torch
+
+import paper_2512_07009_amd as flock
+from paper_2512_07009_amd import encoder
+
+pytestmark = pytest.mark.gpu
+
+WAVES = [2 * math.pi / w for w in (16, 64, 256, 1024)]
+AXES = dict(time=WAVES, y=WAVES, x=WAVES)
+
+
+def int32(values):
+    return torch.tensor(values, dtype=torch.int32, device="cuda")
+
+
+def tracks(seed, counts, width, dtype=torch.bfloat16):
+    gen = torch.Generator().manual_seed(seed)
+    total = sum(counts)
+    x = torch.randn(total, width, generator=gen).to(dtype).cuda()
+    xy = (torch.rand(total, 2, generator=gen) * 16 * 1000).int().cuda()
+    time = torch.cat([torch.arange(n) + 7 * i for i, n in enumerate(counts)]).int().cuda()
+    return x, xy, time, int32([0, *torch.tensor(counts).cumsum(0).tolist()])
+
+
+def block_of(seed, width=128, q_heads=4, kv_heads=2, head_dim=64, dtype=torch.bfloat16, cap=0.0):
+    torch.manual_seed(seed)
+    b = encoder.EncoderBlock(width, q_heads, flock.RotaryAxes(**AXES), kv_heads=kv_heads, head_dim=head_dim, sigma_px=None,
+                             norm="rms", dtype=dtype, cap=cap).cuda()
+    with torch.no_grad():
+        b.norm_weight += 0.2 * torch.randn_like(b.norm_weight)
+    return b
+
+
+def pages_of(counts, spare=0):
+    """Pages of each track in an order of their own."""
+    each = [(n + 63) // 64 for n in counts]
+    table = torch.full((len(counts), max(each) + spare), -1, dtype=torch.int32)
+    order, at = torch.randperm(sum(each), generator=torch.Generator().manual_seed(1)).int(), 0
+    for t, n in enumerate(each):
+        table[t, :n] = order[at:at + n]
+        at += n
+    return table.cuda(), max(1, at)
+
+
+def near(got, want, x, limit):
+    """The block adds two layers' outputs to x; each goes through two or three products of
+    factors in 8 bits.  A value in 8 bits is off by a uniform part of a step: 1 / (127 sqrt 12)
+    = 0.23% of the row's largest, which is 3 to 4 times the root mean square: 0.9% of it.  A
+    product has two such factors (1.3%), the first layer two products and keys and values in 8
+    bits on the way, the second two products of what the first left: some 3% of what they add."""
+    off = (got.double() - want.double()).norm() / (want.double() - x.double()).norm()
+    assert torch.isfinite(got).all() and off < limit, f"off by {off:.4f} of what the layers add"
+
+
+def serve(served, cache, x, xy, time, counts, table, clip, window=0):
+    """The tracks' detections in clips of `clip` each, as they would come in."""
+    starts = [sum(counts[:i]) for i in range(len(counts))]
+    out = torch.empty_like(x)
+    for first in range(0, max(counts), clip):
+        rows = [torch.arange(s + min(first, n), s + min(first + clip, n)) for s, n in zip(starts, counts)]
+        at = torch.cat(rows).cuda()
+        offsets = int32([0, *torch.tensor([len(r) for r in rows]).cumsum(0).tolist()])
+        lengths = int32([min(first + clip, n) for n in counts])
+        out[at] = served(x[at], cache, offsets, table, lengths, xy[at], time[at], window=window)
+    return out
+
+
+@pytest.mark.parametrize("dtype,cap,head_dim", [(torch.bfloat16, 0.0, 64), (torch.float16, 20.0, 128), (torch.bfloat16, 0.0, 32)])
+@pytest.mark.parametrize("clip", [1, 7, 64, 1000])
+def test_served_block_is_the_block(clip, dtype, cap, head_dim):
+    counts = [1, 64, 65, 130] if clip == 1 else [300, 1, 64, 700, 129]
+    block = block_of(1, dtype=dtype, cap=cap, head_dim=head_dim)
+    x, xy, time, offsets = tracks(2, counts, 128, dtype)
+    want = block(x, offsets, xy, time, causal=True).detach()
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts, spare=2)
+    got = serve(served, served.cache(pages), x, xy, time, counts, table, clip)
+    near(got, want, x, 0.05)
+
+
+def test_clips_agree_with_all_at_once():
+    """The rows' company changes nothing but the pages' scales: what they held is rounded again as they grow."""
+    counts = [90, 200]
+    block = block_of(3)
+    x, xy, time, offsets = tracks(4, counts, 128)
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts)
+    once = serve(served, served.cache(pages), x, xy, time, counts, table, 1000)
+    near(serve(served, served.cache(pages), x, xy, time, counts, table, 1), once, x, 0.03)
+    # pages that held other tracks before
+    cache = served.cache(pages)
+    serve(served, cache, 5 * x, xy, time, counts, table, 50)
+    assert torch.equal(serve(served, cache, x, xy, time, counts, table, 1000), once)
+
+
+def test_window_sees_the_last_detections():
+    counts = [150, 40]
+    block = block_of(5)
+    x, xy, time, _ = tracks(6, counts, 128)
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts)
+    full = serve(served, served.cache(pages), x, xy, time, counts, table, 30)
+    cut = serve(served, served.cache(pages), x, xy, time, counts, table, 30, window=1000)
+    assert torch.equal(full, cut)
+    # one detection back only: what it adds is the layer of its own value
+    cut = serve(served, served.cache(pages), x, xy, time, counts, table, 30, window=1)
+    assert torch.equal(cut[:1], full[:1]) and not torch.equal(cut[1:], full[1:])
+
+
+def test_captured_and_replayed():
+    """A step of the stream in a graph: the track's lengths grow on the device between replays,
+    with the program's own eager work in between."""
+    counts = [200, 70, 130]
+    block = block_of(7)
+    x, xy, time, _ = tracks(8, counts, 128)
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts)
+    starts = torch.tensor([0, 200, 270], device="cuda")
+    offsets = int32([0, 1, 2, 3])
+    steps = 70
+    want, cache = [], served.cache(pages)
+    for i in range(steps):
+        at = starts + i
+        want.append(served(x[at], cache, offsets, table, int32([i + 1] * 3), xy[at], time[at]))
+    cache2 = served.cache(pages)
+    fx, fxy, ft, lengths = x[starts].clone(), xy[starts].clone(), time[starts].clone(), int32([1, 1, 1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        served(fx, cache2, offsets, table, lengths, fxy, ft)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = served(fx, cache2, offsets, table, lengths, fxy, ft)
+    for i in range(steps):
+        at = starts + i
+        fx.copy_(x[at])
+        fxy.copy_(xy[at])
+        ft.copy_(time[at])
+        lengths.fill_(i + 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i]), f"replay {i}"
+        (x.float() @ x.float().t()).sum()
+    used = table[:, :2].flatten().long()
+    for a, b in zip((cache.k_scale, cache.v_scale), (cache2.k_scale, cache2.v_scale)):
+        assert torch.equal(a[used], b[used])
+
+
+def test_two_streams_with_caches_of_their_own():
+    counts = [3000] * 6
+    block = block_of(9)
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts)
+    x, xy, time, offsets = tracks(10, counts, 128)
+    lengths = int32(counts)
+    ask = int32([0, 1, 2, 3, 4, 5, 6])
+    q = x[:6]
+
+    def run(cache):
+        served(x, cache, offsets, table, lengths, xy, time)
+        return served(q, cache, ask, table, lengths, xy[:6], time[:6])
+    want = run(served.cache(pages))
+    caches = [served.cache(pages) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s, c in zip(streams, caches):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for _ in range(3):
+                got.append(run(c))
+    torch.cuda.synchronize()
+    for g in got[0], got[3]:
+        assert torch.equal(g, want)
+
+
+def test_operators_on_another_stream_than_the_current():
+    counts = [500, 900]
+    block = block_of(11)
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts)
+    x, xy, time, offsets = tracks(12, counts, 128)
+    lengths = int32(counts)
+    q = torch.randn(2, 4, 64, device="cuda").bfloat16()
+    k = torch.randn(1400, 2, 64, device="cuda").bfloat16()
+    ask = int32([0, 1, 2])
+    a, b = served.cache(pages), served.cache(pages)
+    flock.append_tracks(a, k, k, offsets, table, lengths)
+    want = flock.attention_tracks(q, a, ask, table, lengths)
+    rows = torch.randn(300, 256, device="cuda")
+    q8, s8 = flock.quantize_rows(rows)
+    y = flock.linear_rows_i8(q8, s8, q8, s8)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    flock.append_tracks(b, k, k, offsets, table, lengths, stream=side)
+    got = flock.attention_tracks(q, b, ask, table, lengths, stream=side)
+    q8, s8 = flock.quantize_rows(rows, stream=side)
+    y2 = flock.linear_rows_i8(q8, s8, q8, s8, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want) and torch.equal(y, y2)
+
+
+def plain_block(block, x, counts, xy, time, weights):
+    """EncoderBlock(norm="rms") in 64 bits on the CPU, from its definition."""
+    hq, hk, dim = block.heads
+    norm, qkv_w, out_w, up, down = weights
+
+    def rms(h, w):
+        return h / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6) * w
+
+    def turn(z):
+        angle = torch.cat([torch.outer(time.double(), torch.tensor(WAVES, dtype=torch.float64)),
+                           torch.outer(xy[:, 1].double() / 16, torch.tensor(WAVES, dtype=torch.float64)),
+                           torch.outer(xy[:, 0].double() / 16, torch.tensor(WAVES, dtype=torch.float64))], 1)[:, None]
+        p = angle.shape[2]
+        a, b = z[..., :p], z[..., p:2 * p]
+        return torch.cat([a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos(), z[..., 2 * p:]], -1)
+
+    qkv = (rms(x, norm[0]) @ qkv_w.t()).view(-1, hq + 2 * hk, dim)
+    q, k, v = turn(qkv[:, :hq]), turn(qkv[:, hq:hq + hk]), qkv[:, hq + hk:]
+    parts, at = [], 0
+    for n in counts:
+        s = slice(at, at + n)
+        at += n
+        kk, vv = (t[s].repeat_interleave(hq // hk, 1).transpose(0, 1) for t in (k, v))
+        t = q[s].transpose(0, 1) @ kk.transpose(1, 2) * dim ** -0.5
+        t = t.masked_fill(torch.ones(n, n).triu(1).bool(), -math.inf)
+        parts.append((torch.softmax(t, -1) @ vv).transpose(0, 1))
+    h = x + torch.cat(parts).flatten(1) @ out_w.t()
+    return h + torch.nn.functional.gelu(rms(h, norm[1]) @ up.t()) @ down.t()
+
+
+def test_block_with_rms_norm_trains():
+    """Outputs and gradients of the block against 64 bits.  Products of 16-bit features: some
+    rounding of 2^-9 (root mean square half of 2^-8) each, some ten of them on the way."""
+    counts = [40, 1, 90]
+    block = block_of(13)
+    x, xy, time, offsets = tracks(14, counts, 128)
+    x.requires_grad_()
+    gen = torch.Generator().manual_seed(1)
+    g = torch.randn(x.shape, generator=gen).bfloat16()
+    out = block(x, offsets, xy, time, causal=True)
+    out.backward(g.cuda())
+    names = ("norm_weight", "qkv", "out", "up", "down")
+    weights = [getattr(block, n).detach().cpu().double().requires_grad_() for n in names]
+    x64 = x.detach().cpu().double().requires_grad_()
+    want = plain_block(block, x64, counts, xy.cpu(), time.cpu(), weights)
+    want.backward(g.double())
+
+    def off(a, b):
+        return (a.detach().cpu().double() - b).norm() / b.norm()
+    assert off(out, want.detach()) < 0.01
+    assert off(x.grad, x64.grad) < 0.01
+    for n, w in zip(names, weights):
+        assert off(getattr(block, n).grad, w.grad) < 0.02, n
+
+
+def test_norms_function_differentiates_once():
+    x = torch.randn(6, 40, device="cuda", requires_grad=True)
+    w = torch.ones(40, device="cuda", requires_grad=True)
+    y = encoder.rms_norm(x, w)
+    g, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="second"):
+        g.sum().backward()
+    y, h = encoder.rms_norm(x, None, residual=x)
+    (y.sum() + h.sum()).backward()
+    assert w.grad is None and torch.isfinite(x.grad).all()
+
+
+def test_captured_backward_of_the_norm():
+    x = torch.randn(50, 64, device="cuda").bfloat16().requires_grad_()
+    w = torch.rand(64, device="cuda").requires_grad_()
+    g = torch.randn(50, 64, device="cuda").bfloat16()
+    want = torch.autograd.grad(encoder.rms_norm(x, w), (x, w), g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.autograd.grad(encoder.rms_norm(x, w), (x, w), g)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = torch.autograd.grad(encoder.rms_norm(x, w), (x, w), g)
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        x.detach().float().sum()
+
+
+def test_refusals():
+    axes = flock.RotaryAxes(**AXES)
+    with pytest.raises(ValueError, match="norm"):
+        encoder.EncoderBlock(64, 2, axes, norm="batch")
+    with pytest.raises(ValueError, match="layer norm"):
+        encoder.ServedBlock(encoder.EncoderBlock(64, 2, axes, sigma_px=None).cuda())
+    with pytest.raises(ValueError, match="distances"):
+        encoder.ServedBlock(encoder.EncoderBlock(64, 2, axes, norm="rms").cuda())
+    with pytest.raises(ValueError, match="GPU"):
+        encoder.ServedBlock(encoder.EncoderBlock(64, 2, axes, norm="rms", sigma_px=None))
+    with pytest.raises(ValueError, match="multiples of 16"):
+        encoder.ServedBlock(encoder.EncoderBlock(64, 2, axes, norm="rms", sigma_px=None, head_dim=24).cuda())
+    served = encoder.ServedBlock(encoder.EncoderBlock(64, 2, axes, norm="rms", sigma_px=None).cuda())
+    with pytest.raises(ValueError, match="features of"):
+        served(torch.zeros(1, 64, device="cuda"), served.cache(1), int32([0, 1]), int32([[0]]), int32([1]),
+               int32([[0, 0]]), int32([0]))
