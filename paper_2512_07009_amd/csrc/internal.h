@@ -388,18 +388,19 @@ struct TrackAttentionArgs {
     int64_t q_stride, out_stride;
     int32_t q_heads, window;
     float scale, cap;
-    int32_t group, splits, split_pages;  // set by launch_track_attention
+    int32_t group, tile_shift, gathered, splits, split_pages;  // set by launch_track_attention
     float *part_out, *part_stat;
 };
 
 // How the pages of a row are dealt out.
 struct TrackPlan {
+    int32_t tile_rows;    // rows of a workgroup
     int64_t slots;        // numbers of row tiles
     int32_t splits;       // workgroups that may share a row's pages ...
     int32_t split_pages;  // ... and how many pages each takes
 };
 TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads, int32_t kv_heads,
-                               int n_cus);
+                               int32_t dim, bool capped, int n_cus);
 size_t track_attention_workspace_bytes(const TrackPlan &p, int32_t total, int32_t q_heads, int32_t dim);
 hipError_t launch_track_attention(TrackAttentionArgs a, int32_t dtype, const TrackPlan &p, void *workspace,
                                   hipStream_t stream);

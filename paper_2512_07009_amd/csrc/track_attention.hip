@@ -38,8 +38,11 @@ using attention::f32x16;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef half_t f16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kThreads = 256, kWaves = 4, kRows = 16;
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kRows = 16, kManyRows = 128;  // of a workgroup, 2^4 and 2^7
+constexpr int kFewRows = 128;
 constexpr float kSlack = 8.0f;    // scores above the shift by less are left there
 constexpr float kQuery = 32512.0f;  // a query's largest dimension as 256 a + b
 
@@ -75,14 +78,14 @@ struct Item {
 __device__ __forceinline__ Item item_of(const TrackAttentionArgs &a, int64_t slot, int head) {
     Item s;
     int64_t tile;
-    const int group = a.group;
-    s.at = find_track(a.tracks, slot, (int64_t)a.tracks.total * group / kRows + a.tracks.n_tracks,
-                      [=](int offset, int t) { return (int64_t)offset * group / kRows + t; }, &tile);
+    const int group = a.group, shift = a.tile_shift;
+    s.at = find_track(a.tracks, slot, ((int64_t)a.tracks.total * group >> shift) + a.tracks.n_tracks,
+                      [=](int offset, int t) { return ((int64_t)offset * group >> shift) + t; }, &tile);
     s.head = head;
     const int64_t all = (int64_t)s.at.n * group;
-    s.ok = s.at.ok && tile >= 0 && tile * kRows < all;
-    s.row0 = (int)(tile * kRows);
-    s.rows = (int)min((int64_t)kRows, all - s.row0);
+    s.ok = s.at.ok && tile >= 0 && tile << shift < all;
+    s.row0 = (int)(tile << shift);
+    s.rows = (int)min((int64_t)1 << shift, all - s.row0);
     const int before = s.at.length - s.at.n;  // tokens before the first query's own (may be negative)
     const int last = before + (s.row0 + s.rows - 1) / group, first = before + s.row0 / group;
     const int lo = a.window && first >= a.window ? first - a.window + 1 : 0;
@@ -90,6 +93,34 @@ __device__ __forceinline__ Item item_of(const TrackAttentionArgs &a, int64_t slo
     s.pages = last < 0 || last < lo ? 0 : last / kPage + 1 - s.first_page;
     return s;
 }
+
+// How a query whose largest dimension has these bits goes to whole numbers.  One below
+// 2^-100 is zeros, one that is not finite NaN.
+struct Whole {
+    float most, per;
+    bool finite;
+    __device__ __forceinline__ explicit Whole(uint32_t largest) {
+        most = __uint_as_float(largest);
+        finite = largest < 0x7f800000u;
+        per = finite && most >= 0x1p-100f ? kQuery / most : 0.0f;
+    }
+    __device__ __forceinline__ void split(const float (&x)[16], i32x4 &high, i32x4 &low) const {
+        high = low = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int n = per > 0.0f ? (int)rintf(x[e] * per) : 0;
+            high[e >> 2] |= ((n + 128) >> 8 & 0xff) << (8 * (e & 3));
+            low[e >> 2] |= (n & 0xff) << (8 * (e & 3));
+        }
+    }
+    // What products of whole numbers are multiplied by, beside the page's scale (finite, so
+    // that a zero times it stays one).
+    template <int CAP>
+    __device__ __forceinline__ float factor(const TrackAttentionArgs &a) const {
+        const float scale = CAP == kHigh ? a.scale / a.cap : CAP == kLow ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
+        return finite ? fminf(scale * (per > 0.0f ? most / kQuery : 1.0f), 0x1p127f) : NAN;
+    }
+};
 
 // What a lane holds of a row: its dimensions as right factors, the tokens that it sees
 // (lo, own], and the softmax so far.
@@ -125,35 +156,23 @@ __device__ __forceinline__ void begin(Row<DI> &w, const TrackAttentionArgs &a, c
     }
     bits = max(bits, (uint32_t)__shfl_xor((int)bits, 16));
     bits = max(bits, (uint32_t)__shfl_xor((int)bits, 32));
-    // (a row below 2^-100 is zeros, one that is not finite NaN)
-    const float most = __uint_as_float(bits);
-    const bool finite = bits < 0x7f800000u, some = finite && most >= 0x1p-100f;
-    const float per = some ? kQuery / most : 0.0f;
+    const Whole whole(bits);
 #pragma unroll
-    for (int i = 0; i < DI; ++i) {
-        w.high[i] = w.low[i] = i32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int n = some ? (int)rintf(x[i][e] * per) : 0, high = (n + 128) >> 8;
-            w.high[i][e >> 2] |= (high & 0xff) << (8 * (e & 3));
-            w.low[i][e >> 2] |= (n & 0xff) << (8 * (e & 3));
-        }
-    }
-    // (finite, so that a zero times it stays one)
-    const float scale = CAP == kHigh ? a.scale / a.cap : CAP == kLow ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
-    w.factor = finite ? fminf(scale * (some ? most / kQuery : 1.0f), 0x1p127f) : NAN;
+    for (int i = 0; i < DI; ++i) whole.split(x[i], w.high[i], w.low[i]);
+    w.factor = whole.factor<CAP>(a);
 }
 
 template <typename T, int DI, int CAP>
-__global__ void __launch_bounds__(kThreads, DI == 1 ? 4 : 2) track_attention_kernel(TrackAttentionArgs a) {
+__global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) track_attention_kernel(TrackAttentionArgs a) {
     constexpr int kBlocks = 4 * DI;   // 16 dimensions each, at most
     __shared__ float sums[kWaves][kRows][64 * DI + 1];
     __shared__ float stats[2][kWaves][kRows];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane >> 4, r = lane & 15;
     const int dim = a.cache.dim, blocks = dim / 16;
-    const int split = (int)(blockIdx.x % a.splits);
-    const int64_t id = blockIdx.x / a.splits;
-    const Item it = item_of(a, id / a.cache.kv_heads, (int)(id % a.cache.kv_heads));
+    const uint32_t block_id = a.gathered ? (uint32_t)attention::xcd_order(blockIdx.x, gridDim.x) : blockIdx.x;
+    const uint32_t id = block_id / a.splits, heads = a.cache.kv_heads;
+    const int split = (int)(block_id - id * a.splits);
+    const Item it = item_of(a, id / heads, (int)(id % heads));
     if (!it.ok) return;
     const int active = max((it.pages + a.split_pages - 1) / a.split_pages, 1);
     if (split >= active) return;
@@ -179,6 +198,7 @@ __global__ void __launch_bounds__(kThreads, DI == 1 ? 4 : 2) track_attention_ker
                 const int64_t block = (int64_t)max(my_page, 0) * a.cache.kv_heads + it.head;
                 my_k = my_page >= 0 ? a.cache.k_scale[block] : 0.0f;
                 my_v = my_page >= 0 ? a.cache.v_scale[block] : 0.0f;
+                asm volatile("" ::"v"(my_k), "v"(my_v));  // (waited for here, not where pages' loads are on their way)
             }
             const int page = __builtin_amdgcn_readlane(my_page, n & 63);
             if (page >= 0) return page;
@@ -316,25 +336,306 @@ __global__ void __launch_bounds__(kThreads, DI == 1 ? 4 : 2) track_attention_ker
 #pragma unroll
         for (int e = 0; e < 4; ++e) sums[wave][r][16 * b + 4 * part + e] = w.acc[b][e] * (keep * unit);
     __syncthreads();
-    for (int i = threadIdx.x; i < it.rows * dim; i += kThreads) {
-        const int rr = i / dim, d = i % dim;
+    // a wave a row, a lane a dimension
+#pragma unroll 1
+    for (int rr = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); rr < it.rows; rr += kWaves) {
         const float l = (stats[1][0][rr] + stats[1][1][rr]) + (stats[1][2][rr] + stats[1][3][rr]);
-        const float o = (sums[0][rr][d] + sums[1][rr][d]) + (sums[2][rr][d] + sums[3][rr][d]);
-        const int row = it.row0 + rr;
-        const int64_t bird = it.at.row0 + row / a.group;
-        const int head = it.head * a.group + row % a.group;
-        if (active == 1) {
-            static_cast<T *>(a.out)[bird * a.out_stride + head * dim + d] = static_cast<T>(l == 0.0f ? 0.0f : o / l);
-        } else {
-            const int64_t to = ((int64_t)split * a.tracks.total + bird) * a.q_heads + head;
-            a.part_out[to * dim + d] = o;
-            if (d == 0) {
-                float m = stats[0][0][rr];
-                for (int v = 1; v < kWaves; ++v) m = fmaxf(m, stats[0][v][rr]);
-                a.part_stat[2 * to] = m;
-                a.part_stat[2 * to + 1] = l;
-            }
+        const uint32_t row = it.row0 + rr, query = row / (uint32_t)a.group;
+        const int64_t bird = it.at.row0 + query;
+        const int head = it.head * a.group + (int)(row - query * a.group);
+        const int64_t to = ((int64_t)split * a.tracks.total + bird) * a.q_heads + head;
+        for (int d = threadIdx.x & 63; d < dim; d += 64) {
+            const float o = (sums[0][rr][d] + sums[1][rr][d]) + (sums[2][rr][d] + sums[3][rr][d]);
+            if (active == 1) static_cast<T *>(a.out)[bird * a.out_stride + head * dim + d] = static_cast<T>(l == 0.0f ? 0.0f : o / l);
+            else a.part_out[to * dim + d] = o;
         }
+        if (active > 1 && (threadIdx.x & 63) == 0) {
+            const float m = fmaxf(fmaxf(stats[0][0][rr], stats[0][1][rr]), fmaxf(stats[0][2][rr], stats[0][3][rr]));
+            reinterpret_cast<float2 *>(a.part_stat)[to] = make_float2(m, l);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: 128 a workgroup, 32 a wave, all waves over the same pages.
+//
+// Pages go to LDS as they are, without registers in between, kAhead pages ahead of the
+// products: a page waits for its own loads alone (they come back in order), with one
+// barrier a page.  Chunks of 16 bytes of a key or of a dimension are stored in an order
+// that turns with it, so that the 32 that a wave reads a chunk of lie in different banks.
+// Products are 32 x 32 x 32 (8 bits) and 32 x 32 x 16: a lane holds 32 tokens of one row, and
+// of a dimension it takes the two parts that hold the same tokens.  Bound by vector
+// instructions, some seven a score and 80 a page to convert its values.
+// ---------------------------------------------------------------------------
+
+constexpr int kAhead = 3, kBuffers = kAhead + 1;
+
+template <int DP>
+struct ManyShared {
+    int8_t k[kBuffers][kPage * DP], v[kBuffers][DP * kPage];
+};
+
+// Where chunk `chunk` (16 bytes) of a row of WIDTH bytes lies in LDS.
+template <int WIDTH>
+__device__ __forceinline__ int turned(int row, int chunk) {
+    return WIDTH == 64 ? chunk ^ ((row >> 2) & 3) : chunk ^ ((row >> 1) & 7);
+}
+
+// Waits for LDS, and for all but the last N loads.
+template <int N>
+__device__ __forceinline__ void wait_but() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | 0x070);
+}
+
+// The compiler moves no access to memory over this.
+__device__ __forceinline__ void stand() { asm volatile("" ::: "memory"); }
+
+template <typename T, int DP, int CAP>
+__global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(TrackAttentionArgs a) {
+    constexpr int kChunks = DP / 16, kSteps = DP / 32, kBlocks = DP / 32;
+    constexpr int kLoads = kPage * DP / 16 / kThreads;  // of 16 bytes a thread, for keys and for values
+    __shared__ ManyShared<DP> shared;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, r = lane & 31;
+    const int dim = a.cache.dim;
+    const uint32_t block_id = a.gathered ? (uint32_t)attention::xcd_order(blockIdx.x, gridDim.x) : blockIdx.x;
+    const uint32_t id = block_id / a.splits, heads = a.cache.kv_heads;
+    const int split = (int)(block_id - id * a.splits);
+    const Item it = item_of(a, id / heads, (int)(id % heads));
+    if (!it.ok) return;
+    const int active = max((it.pages + a.split_pages - 1) / a.split_pages, 1);
+    if (split >= active) return;
+    const int p0 = it.first_page + split * a.split_pages;
+    const int count = min(a.split_pages, it.first_page + it.pages - p0);
+
+    // this lane's row: its dimensions as right factors, and the tokens that it sees
+    const int at = 32 * wave + r;
+    const bool valid = at < it.rows;
+    const int row = it.row0 + (valid ? at : 0), query = row / a.group, head = it.head * a.group + row % a.group;
+    const int before = it.at.length - it.at.n, own = before + query;
+    const int lo = a.window ? max(own, 0) - a.window : -1;  // tokens in (lo, own]
+    i32x4 high[kSteps], low[kSteps];
+    float factor;
+    {
+        const T *q = static_cast<const T *>(a.q) + (int64_t)(it.at.row0 + query) * a.q_stride + head * dim;
+        float x[kSteps][16];
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int d = 32 * i + 16 * h;
+            load_some<T, 16>(q + min(d, dim - 16), valid && d < dim ? 16 : 0, x[i]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) bits = max(bits, __float_as_uint(x[i][e]) & 0x7fffffffu);
+        }
+        bits = max(bits, (uint32_t)__shfl_xor((int)bits, 32));
+        const Whole whole(bits);
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) whole.split(x[i], high[i], low[i]);
+        factor = whole.factor<CAP>(a);
+    }
+    const float cap2 = a.cap * kLog2e, constant = attention::cap_constant<CAP>(cap2);
+    // tokens that some and that every row of the wave sees
+    const bool some_rows = 32 * wave < it.rows;
+    const int wave_first = before + (it.row0 + 32 * wave) / a.group;
+    const int wave_last = before + (it.row0 + min(32 * wave + 31, it.rows - 1)) / a.group;
+    const int all_lo = a.window ? max(wave_last, 0) - a.window : -1, some_lo = a.window ? wave_first - a.window : -1;
+
+    int my_page = -1;
+    float my_k = 0.0f, my_v = 0.0f;
+    const int32_t *table = a.tracks.table + (int64_t)it.at.index * a.tracks.table_stride;
+    const auto next = [&](int &n) {
+        for (; n < count; ++n) {
+            if ((n & 63) == 0) {
+                const int mine = n + lane;
+                my_page = mine < count ? table[p0 + mine] : -1;
+                if (my_page >= a.cache.pages) my_page = -1;
+                const int64_t block = (int64_t)max(my_page, 0) * a.cache.kv_heads + it.head;
+                my_k = my_page >= 0 ? a.cache.k_scale[block] : 0.0f;
+                my_v = my_page >= 0 ? a.cache.v_scale[block] : 0.0f;
+                asm volatile("" ::"v"(my_k), "v"(my_v));  // (waited for here, not where pages' loads are on their way)
+            }
+            const int page = __builtin_amdgcn_readlane(my_page, n & 63);
+            if (page >= 0) return page;
+        }
+        return -1;
+    };
+    const auto scale_of = [&](float mine, int n) {
+        return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(mine), n & 63));
+    };
+    // the stream of pages: number, scales, and loads into the buffers in turn
+    struct Ahead {
+        int n;  // -1: none
+        float k, v;
+    };
+    int n_next = 0, buffer_next = 0;
+    const auto load = [&]() -> Ahead {
+        const int page = next(n_next);
+        if (page < 0) return {-1, 0.0f, 0.0f};
+        const Ahead one = {n_next, scale_of(my_k, n_next), scale_of(my_v, n_next)};
+        ++n_next;
+        const int64_t block = ((int64_t)page * a.cache.kv_heads + it.head) * (kPage * dim);
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int slot = i * kThreads + threadIdx.x, token = slot / kChunks, chunk = turned<DP>(token, slot % kChunks);
+            // (dimensions beyond the head's: queries have zeros there)
+            const int8_t *from = a.cache.k + block + token * dim + 16 * (16 * chunk < dim ? chunk : 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                             (__attribute__((address_space(3))) void *)(shared.k[buffer_next] + 16 * (i * kThreads + 64 * wave)),
+                                             16, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int slot = i * kThreads + threadIdx.x, d = slot >> 2, part = turned<kPage>(d, slot & 3);
+            // (... and nothing is stored of them)
+            const int8_t *from = a.cache.v + block + (d < dim ? d : 0) * kPage + 16 * part;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from,
+                                             (__attribute__((address_space(3))) void *)(shared.v[buffer_next] + 16 * (i * kThreads + 64 * wave)),
+                                             16, 0, 0);
+        }
+        buffer_next = (buffer_next + 1) & (kBuffers - 1);
+        return one;
+    };
+
+    f32x16 acc[kBlocks] = {};
+    float shift = -INFINITY, total = 0.0f, unit = 0.0f;
+    static_assert(kAhead == 3, "the pages ahead have a name each");
+    Ahead now = load(), second = load(), third = load();
+    int buffer = 0;
+    while (now.n >= 0) {
+        const int token0 = (p0 + now.n) * kPage;
+        const float k_scale = now.k, v_scale = now.v;
+        stand();
+        if (third.n >= 0) wait_but<(kAhead - 1) * 2 * kLoads>();
+        else wait_but<0>();
+        stand();
+        __builtin_amdgcn_s_barrier();  // this page is there, and the one before has been read by all
+        stand();
+        now = second;
+        second = third;
+        third = load();
+        // the values' scale against the largest: 2^-40 for less, which is lost beside it
+        float keep_v = 1.0f;
+        if (v_scale > unit) {
+            keep_v = unit / v_scale;
+            unit = v_scale;
+        }
+        if (some_rows && token0 <= wave_last && token0 + kPage - 1 > some_lo) {
+            const bool near = v_scale > unit * 0x1p-40f;
+            const float level = near ? __log2f(v_scale / unit) : -40.0f, back = near ? unit / v_scale : 0x1p40f;
+            f32x16 s[2];
+            float f = factor * k_scale;
+            if (f > 0x1p127f) f = 0x1p127f;  // (NaN stays)
+            float g = f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int token = 32 * t + r;
+                i32x16 hi = {}, lw = {};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    const i32x4 k = *reinterpret_cast<const i32x4 *>(shared.k[buffer] + token * DP + 16 * turned<DP>(token, 2 * i + h));
+                    hi = __builtin_amdgcn_mfma_i32_32x32x32_i8(k, high[i], hi, 0, 0, 0);
+                    lw = __builtin_amdgcn_mfma_i32_32x32x32_i8(k, low[i], lw, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[t][e] = (float)(256 * hi[e] + lw[e]);
+                if (CAP != kNoCap) {
+                    attention::cap_parts<CAP>(s[t], f);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[t][e] = attention::capped<CAP>(s[t][e], cap2, constant);
+                    g = 1.0f;
+                }
+            }
+            if (token0 + kPage - 1 > wave_first || token0 <= all_lo) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int token = token0 + 32 * t + attention::out_row(e, h);
+                        s[t][e] = token > own || token <= lo ? -INFINITY : s[t][e] * g;
+                    }
+                g = 1.0f;
+            }
+            float most = s[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) most = fmaxf(most, s[t][e]);
+            most = attention::across(most, [](float u, float v) { return fmaxf(u, v); }) * g;
+            float keep = keep_v;
+            if (__any(most > shift + kSlack || (shift == -INFINITY && most > shift))) {
+                const float now = fmaxf(shift, most);
+                const float less = shift == -INFINITY ? 0.0f : attention::exp2_fast(shift - now);
+                total *= less;
+                keep *= less;
+                shift = now;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
+            } else if (keep_v != 1.0f) {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
+            }
+            const float base = (shift == -INFINITY ? 0.0f : shift) - level;
+            float sum = 0.0f;
+            f16x8 weights[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float x = attention::exp2_fast(__builtin_fmaf(s[t][e], g, -base));
+                    sum += x;
+                    weights[2 * t + (e >> 3)][e & 7] = (half_t)x;
+                }
+            total += sum * back;
+            if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page
+                const float none = attention::across(sum, [](float u, float v) { return u + v; }) == 0.0f ? 0.0f : NAN;
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) acc[b] += none;
+            }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) {
+                const int d = 32 * b + r;
+                const int8_t *v = shared.v[buffer] + d * kPage;
+                const i32x4 x = *reinterpret_cast<const i32x4 *>(v + 16 * turned<kPage>(d, h));
+                const i32x4 y = *reinterpret_cast<const i32x4 *>(v + 16 * turned<kPage>(d, h + 2));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_half(x[i], y[i]), weights[i], acc[b], 0, 0, 0);
+            }
+        } else if (keep_v != 1.0f) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b) acc[b] *= keep_v;
+        }
+        buffer = (buffer + 1) & (kBuffers - 1);
+    }
+    total = attention::across(total, [](float u, float v) { return u + v; });
+    if (!valid) return;
+    const int64_t bird = it.at.row0 + query;
+    // (a shift that nothing has moved: no token, or none but NaN)
+    const bool none = shift == -INFINITY && total == total;
+    if (active == 1) {
+        T *out = static_cast<T *>(a.out) + bird * a.out_stride + head * dim;
+        const float per = none || total == 0.0f ? 0.0f : unit / total;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int d = 32 * b + 8 * q + 4 * h;
+                const float o[4] = {acc[b][4 * q] * per, acc[b][4 * q + 1] * per, acc[b][4 * q + 2] * per, acc[b][4 * q + 3] * per};
+                if (d < dim) store_pack<T, 4>(out + d, o);
+            }
+        return;
+    }
+    const int64_t to = ((int64_t)split * a.tracks.total + bird) * a.q_heads + head;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int d = 32 * b + 8 * q + 4 * h;
+            const float o[4] = {acc[b][4 * q] * unit, acc[b][4 * q + 1] * unit, acc[b][4 * q + 2] * unit, acc[b][4 * q + 3] * unit};
+            if (d < dim) store_pack<float, 4>(a.part_out + to * dim + d, o);
+        }
+    if (h == 0) {
+        a.part_stat[2 * to] = shift;
+        a.part_stat[2 * to + 1] = total;
     }
 }
 
@@ -342,48 +643,50 @@ __global__ void __launch_bounds__(kThreads, DI == 1 ? 4 : 2) track_attention_ker
 // of all shares, whose weights are found first, a lane a share.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) track_join_kernel(TrackAttentionArgs a) {
-    const int64_t id = blockIdx.x;
-    const Item it = item_of(a, id / a.cache.kv_heads, (int)(id % a.cache.kv_heads));
-    if (!it.ok) return;
+    const uint32_t id = blockIdx.x, heads = a.cache.kv_heads;
+    const Item it = item_of(a, id / heads, (int)(id % heads));
+    const int rr = kWaves * blockIdx.y + (threadIdx.x >> 6);
+    if (!it.ok || rr >= it.rows) return;
     const int active = (it.pages + a.split_pages - 1) / a.split_pages;
     if (active <= 1) return;
     const int dim = a.cache.dim, lane = threadIdx.x & 63, d0 = min(lane, dim - 1), d1 = min(lane + 64, dim - 1);
-    const int64_t pitch = (int64_t)a.tracks.total * a.q_heads;
-    for (int rr = threadIdx.x >> 6; rr < it.rows; rr += kWaves) {
-        const int rw = it.row0 + rr;
-        const int64_t bird = it.at.row0 + rw / a.group;
-        const int hd = it.head * a.group + rw % a.group;
-        const int64_t at = bird * a.q_heads + hd;
-        float m = -INFINITY;
-        for (int s = lane; s < active; s += 64) m = fmaxf(m, a.part_stat[2 * (s * pitch + at)]);
+    const int row = it.row0 + rr, head = it.head * a.group + row % a.group;
+    const int64_t bird = it.at.row0 + row / a.group;
+    const int64_t pitch = (int64_t)a.tracks.total * a.q_heads, at = bird * a.q_heads + head;
+    float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    for (int first = 0; first < active; first += 64) {
+        const int s = first + lane, here = min(active - first, 64);
+        float2 stat = make_float2(-INFINITY, 0.0f);
+        if (s < active) stat = reinterpret_cast<const float2 *>(a.part_stat)[s * pitch + at];
+        float now = stat.x;
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-        for (int first = 0; first < active; first += 64) {
-            const int s = first + lane;
-            float shift = -INFINITY, total = 0.0f;
-            if (s < active) {
-                shift = a.part_stat[2 * (s * pitch + at)];
-                total = a.part_stat[2 * (s * pitch + at) + 1];
+        for (int d = 32; d > 0; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+        now = fmaxf(now, m);
+        if (now > m) {
+            if (m != -INFINITY) {
+                const float less = attention::exp2_fast(m - now);
+                l *= less;
+                o0 *= less;
+                o1 *= less;
             }
-            const float keep = total == 0.0f ? 0.0f : shift == -INFINITY ? total : attention::exp2_fast(shift - m);
-            float sum = total * keep;
-#pragma unroll
-            for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-            l += sum;
-            const int here = min(active - first, 64);
-#pragma unroll 8
-            for (int i = 0; i < here; ++i) {
-                const float *p = a.part_out + ((first + i) * pitch + at) * dim;
-                const float k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(keep), i));
-                o0 += p[d0] * k;
-                o1 += p[d1] * k;
-            }
+            m = now;
         }
-        T *out = static_cast<T *>(a.out) + bird * a.out_stride + hd * dim;
-        if (lane < dim) out[lane] = static_cast<T>(l == 0.0f ? 0.0f : o0 / l);
-        if (lane + 64 < dim) out[lane + 64] = static_cast<T>(l == 0.0f ? 0.0f : o1 / l);
+        const float keep = stat.y == 0.0f ? 0.0f : stat.x == -INFINITY ? stat.y : attention::exp2_fast(stat.x - m);
+        float sum = stat.y * keep;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        l += sum;
+        const float *p = a.part_out + (first * pitch + at) * dim;
+#pragma unroll 8
+        for (int i = 0; i < here; ++i, p += pitch * dim) {
+            const float k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(keep), i));
+            o0 += p[d0] * k;
+            o1 += p[d1] * k;
+        }
     }
+    T *out = static_cast<T *>(a.out) + bird * a.out_stride + head * dim;
+    if (lane < dim) out[lane] = static_cast<T>(l == 0.0f ? 0.0f : o0 / l);
+    if (lane + 64 < dim) out[lane + 64] = static_cast<T>(l == 0.0f ? 0.0f : o1 / l);
 }
 
 template <typename T, int DI>
@@ -393,31 +696,46 @@ void launch_cap(const TrackAttentionArgs &a, dim3 grid, hipStream_t stream) {
     else hipLaunchKernelGGL((track_attention_kernel<T, DI, kHigh>), grid, dim3(kThreads), 0, stream, a);
 }
 
+template <typename T, int DP>
+void launch_many(const TrackAttentionArgs &a, dim3 grid, hipStream_t stream) {
+    if (a.cap == 0.0f) hipLaunchKernelGGL((track_rows_kernel<T, DP, kNoCap>), grid, dim3(kThreads), 0, stream, a);
+    else if (a.cap <= attention::kLowCap) hipLaunchKernelGGL((track_rows_kernel<T, DP, kLow>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((track_rows_kernel<T, DP, kHigh>), grid, dim3(kThreads), 0, stream, a);
+}
+
 template <typename T>
 hipError_t launch_type(const TrackAttentionArgs &a, const TrackPlan &p, hipStream_t stream) {
     const int64_t items = p.slots * a.cache.kv_heads;
     const dim3 grid((uint32_t)(items * p.splits));
-    if (a.cache.dim <= 64) launch_cap<T, 1>(a, grid, stream);
-    else launch_cap<T, 2>(a, grid, stream);
+    if (p.tile_rows == kRows) {
+        if (a.cache.dim <= 64) launch_cap<T, 1>(a, grid, stream);
+        else launch_cap<T, 2>(a, grid, stream);
+    } else {
+        if (a.cache.dim <= 64) launch_many<T, 64>(a, grid, stream);
+        else launch_many<T, 128>(a, grid, stream);
+    }
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || p.splits == 1) return err;
-    hipLaunchKernelGGL((track_join_kernel<T>), dim3((uint32_t)items), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((track_join_kernel<T>), dim3((uint32_t)items, p.tile_rows / kWaves), dim3(kThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 }  // namespace
 
 TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads, int32_t kv_heads,
-                               int n_cus) {
+                               int32_t dim, bool capped, int n_cus) {
     TrackPlan p;
     const int group = q_heads / kv_heads;
-    p.slots = (int64_t)total * group / kRows + n_tracks;
-    const int64_t items = std::max<int64_t>(p.slots * kv_heads, 1);
-    // as many workgroups as the card holds at a time, of at least two pages a wave: more of
-    // them cost more to begin and to join than they even out (24 tracks of 27000, heads of
-    // 128: two a compute unit 69 us, four 78, eight 88; 500 tracks of up to 5400: one
-    // workgroup a track 85 us, two 97)
-    int64_t splits = 2 * (int64_t)n_cus / items;
+    // 128 rows a workgroup where tracks have more than kFewRows on average
+    const bool many = (int64_t)total * group > kFewRows * (int64_t)n_tracks;
+    p.tile_rows = many ? kManyRows : kRows;
+    p.slots = (int64_t)total * group / p.tile_rows + n_tracks;
+    // as many workgroups as the card holds at a time, of at least two pages a wave: with
+    // more of them some begin when others end (24 tracks of 27000, heads of 128: two a
+    // compute unit 68 us, four 77, eight 88)
+    const int64_t items = std::max<int64_t>(n_tracks, (int64_t)total * group / p.tile_rows) * kv_heads;
+    const int resident = many ? 3 : 2;
+    int64_t splits = resident * (int64_t)n_cus / items;
     splits = std::max<int64_t>(std::min<int64_t>(splits, (max_pages + 2 * kWaves - 1) / (2 * kWaves)), 1);
     p.split_pages = std::max((int32_t)((max_pages + splits - 1) / splits), 1);
     p.splits = std::max((max_pages + p.split_pages - 1) / p.split_pages, 1);
@@ -431,6 +749,10 @@ size_t track_attention_workspace_bytes(const TrackPlan &p, int32_t total, int32_
 hipError_t launch_track_attention(TrackAttentionArgs a, int32_t dtype, const TrackPlan &p, void *workspace,
                                   hipStream_t stream) {
     a.group = a.q_heads / a.cache.kv_heads;
+    a.tile_shift = p.tile_rows == kManyRows ? 7 : 4;
+    // workgroups of a track that read the same pages meet in one XCD's L2 (96 clips: 102 -> 94 us);
+    // with one tile a track they would only be spread less evenly (24 long tracks: 67 -> 84)
+    a.gathered = (int64_t)a.tracks.total * a.group > kRows * (int64_t)a.tracks.n_tracks;
     a.splits = p.splits;
     a.split_pages = p.split_pages;
     a.part_stat = static_cast<float *>(workspace);
