@@ -86,9 +86,10 @@ template <int BM, int BN>
 struct LinearTile {
     int64_t m0;
     int n0, rows, columns;
-    __device__ __forceinline__ LinearTile(const LinearArgs &a, int64_t tile) {
-        m0 = tile / a.column_tiles * BM;
-        n0 = (int)(tile % a.column_tiles) * BN;
+    __device__ __forceinline__ LinearTile(const LinearArgs &a, uint32_t tile) {
+        const uint32_t row = tile / (uint32_t)a.column_tiles;
+        m0 = (int64_t)row * BM;
+        n0 = (int)(tile - row * a.column_tiles) * BN;
         rows = (int)min((int64_t)BM, a.rows - m0);
         columns = min(BN, a.outputs - n0);
     }
@@ -104,7 +105,7 @@ struct LinearLoads {
 
     __device__ __forceinline__ LinearLoads() { wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-    __device__ __forceinline__ void begin(const LinearArgs &a, int64_t tile, int turn, LinearShared<BM, BN> &s) {
+    __device__ __forceinline__ void begin(const LinearArgs &a, uint32_t tile, int turn, LinearShared<BM, BN> &s) {
         const LinearTile<BM, BN> t(a, tile);
         x = a.x + t.m0 * a.x_stride;
         w = a.w + t.n0 * a.w_stride;
@@ -302,24 +303,24 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
     __shared__ LinearShared<BM, BN> s;
 
     // tiles of this workgroup: an eighth of all to each XCD, in one piece, its workgroups side by side
-    int64_t first, end;
-    int beside = 1;
-    if (a.tiles <= gridDim.x) {  // one each
-        const int64_t per = a.tiles / 8, id = blockIdx.x;
+    uint32_t first, end, beside = 1;
+    const uint32_t tiles = a.tiles;
+    if (tiles <= gridDim.x) {  // one each
+        const uint32_t per = tiles / 8, id = blockIdx.x;
         first = id < per * 8 ? (id & 7) * per + (id >> 3) : id;
         end = first + 1;
     } else {                     // (as many workgroups on each XCD)
-        const int xcd = blockIdx.x & 7;
+        const uint32_t xcd = blockIdx.x & 7;
         beside = gridDim.x >> 3;
-        first = a.tiles * xcd / 8 + (blockIdx.x >> 3);
-        end = a.tiles * (xcd + 1) / 8;
+        first = tiles * xcd / 8 + (blockIdx.x >> 3);
+        end = tiles * (xcd + 1) / 8;
         if (first >= end) return;
     }
     const int steps = (a.width + kStep - 1) / kStep;
-    int64_t left = ((end - first - 1) / beside + 1) * steps;  // steps to multiply
+    int64_t left = (int64_t)((end - first - 1) / beside + 1) * steps;  // steps to multiply
 
     LinearLoads<BM, BN> loads;
-    int64_t next_tile = first;
+    uint32_t next_tile = first;
     int next_step = 0, next_turn = 0, next_stage = 0;
     const auto load = [&] {
         if (next_tile >= end) return;
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
     constexpr int kStores = 2 * kMT * kNT;
     static_assert(BM == BN, "finish() takes a quarter of a stage");
     int stage = 0, turn = 0, since = kAhead;
-    for (int64_t tile = first; tile < end; tile += beside, turn = (turn + 1) & (kStages - 1)) {
+    for (uint32_t tile = first; tile < end; tile += beside, turn = (turn + 1) & (kStages - 1)) {
         i32x16 acc[kNT][kMT] = {};
         // (a wave that multiplies goes before the one beside it that has a tile's outputs to make: 2 to 4%)
         __builtin_amdgcn_s_setprio(2);
