@@ -501,7 +501,8 @@ flock_status quantize_rows(int32_t dtype, const void *x, int64_t x_stride, int32
  *   x              device in, int8[rows][width], rows x_stride bytes apart
  *                  (0 <= x_stride < 2^24), from rms_norm_rows_i8 or
  *                  quantize_rows.  Rows that begin at multiples of 16 bytes, of x
- *                  and w both, are loaded fastest.
+ *                  and w both, are loaded fastest; what follows a row's end in the
+ *                  same 16 bytes may be read then, and has no influence.
  *   x_scale        device in, float[rows].
  *   w              device in, int8[outputs][width], rows w_stride bytes apart.
  *   w_scale        device in, float[outputs].

@@ -845,10 +845,16 @@ class TrackCache:
                 raise ValueError(f"{name} must be a contiguous {dtype} {list(shape)} tensor on k's device")
         if max(pages, heads, dim) > _MOST:
             raise ValueError("k has more than 2^31 - 1 pages, heads or dimensions")
-        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self._tensors = (k, v, k_scale, v_scale)
         self.pages, self.kv_heads, self.head_dim, self.device = pages, heads, dim, k.device
         self.index = k.get_device()
         self.pointers = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+
+    # (read only: the pointers are these tensors')
+    k = property(lambda self: self._tensors[0])
+    v = property(lambda self: self._tensors[1])
+    k_scale = property(lambda self: self._tensors[2])
+    v_scale = property(lambda self: self._tensors[3])
 
     @classmethod
     def empty(cls, pages: int, kv_heads: int, head_dim: int, device="cuda"):

@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
     const bool some_rows = 32 * wave < it.rows;
     const int wave_first = before + (it.row0 + 32 * wave) / a.group;
     const int wave_last = before + (it.row0 + min(32 * wave + 31, it.rows - 1)) / a.group;
-    const int all_lo = a.window ? max(wave_last, 0) - a.window : -1, some_lo = a.window ? wave_first - a.window : -1;
+    const int all_lo = a.window ? max(wave_last, 0) - a.window : -1, some_lo = a.window ? max(wave_first, 0) - a.window : -1;
 
     int my_page = -1;
     float my_k = 0.0f, my_v = 0.0f;
