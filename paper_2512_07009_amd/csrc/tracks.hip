@@ -7,12 +7,14 @@
 //   new tokens: value / scale, to the nearest; ties to even
 //
 // A workgroup takes the keys or the values of one page and kv head, so that no two
-// meet in memory: values stay in LDS in 32 bits between the search for the largest and
-// the rounding.  Tokens that the page does not get yet are left as they are.
+// meet in memory: they stay in LDS as they came between the search for the largest and
+// the rounding, and keys are turned in both.  Tokens that the page does not get yet are
+// left as they are.
 //
-// With a token or a few a track the time is that of the trips to memory one after the
-// other (the track, its page, the rows with their positions and the page's scale), and a
-// workgroup is one wave; clips take four waves.
+// The time is that of a workgroup's trips to memory one after the other (the track, its
+// page, the rows with their positions and the page's scale), not of bytes: as many
+// workgroups run beside each other as LDS allows.  With a token or a few a track one is
+// a wave; clips take four.
 
 #include "tracks_common.h"
 
@@ -22,7 +24,7 @@ namespace {
 using namespace tracks;
 
 constexpr int kVec = 8, kItems = 4;
-constexpr int kPad = 4;  // between tokens in LDS: those of four parts of a dimension's places lie in other banks
+constexpr int kPad = 8;  // between tokens in LDS: those of four parts of a dimension's places lie in other banks
 
 // Largest |x| over the workgroup, as bits (those of NaN are the largest).
 template <int WAVES>
@@ -48,6 +50,9 @@ __device__ __forceinline__ int bytes(uint32_t a, uint32_t b, uint32_t c, uint32_
     return (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
+// A byte of ones for each of the four low bits.
+__device__ __forceinline__ int of_bits(uint32_t bits) { return (int)(((bits & 0xf) * 0x00204081u & 0x01010101u) * 0xffu); }
+
 __device__ __forceinline__ float byte_of(const i32x4 &c, int i) { return (float)(int8_t)(c[i >> 2] >> (8 * (i & 3))); }
 
 // Pages that rows go to are numbered as a first one of every track, and after those the
@@ -61,14 +66,16 @@ __host__ __device__ inline int64_t other_pages(int32_t offset, int32_t track) {
 template <typename T, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
     constexpr int kThreads = 64 * WAVES;
-    extern __shared__ __attribute__((aligned(16))) float fresh[];    // [new tokens of the page][pitch]
+    extern __shared__ __attribute__((aligned(16))) char shared[];
     __shared__ uint32_t slot[WAVES];
     __shared__ int32_t places[3][kPage];   // time, y, x of the new tokens
     const int dim = a.cache.dim, pitch = dim + kPad, heads = a.cache.kv_heads;
+    T *const fresh = reinterpret_cast<T *>(shared);                                    // [token of the page][pitch]
+    int8_t *const whole = reinterpret_cast<int8_t *>(shared) + kPage * pitch * sizeof(T);  // keys: [new token][dim]
     const bool values = blockIdx.x & 1;
-    const int64_t item = blockIdx.x >> 1;
-    const int head = (int)(item % heads);
-    const int64_t number = item / heads, others = number - a.tracks.n_tracks;
+    const uint32_t item = blockIdx.x >> 1, number = item / (uint32_t)heads;
+    const int head = (int)(item - number * heads);
+    const int64_t others = (int64_t)number - a.tracks.n_tracks;
     int64_t within = 0;
     Track track;
     if (others < 0) {
@@ -107,44 +114,52 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
         }
     }
 
-    // the new tokens, in 32 bits: kItems packs of a thread on their way at a time
+    // the new tokens, kItems packs of a thread on their way at a time
     const int64_t stride = values ? a.v_stride : a.k_stride;
     const T *in = static_cast<const T *>(values ? a.v : a.k) + row0 * stride + head * dim;
     uint32_t largest = 0;
     for (int first_item = threadIdx.x; first_item < n << a.pack_shift; first_item += kItems * kThreads) {
-        float x[kItems][kVec];
+        Pack<T, kVec> x[kItems];
 #pragma unroll
         for (int m = 0; m < kItems; ++m) {
             const int i = first_item + m * kThreads, token = i >> a.pack_shift, d = (i & ((1 << a.pack_shift) - 1)) * kVec;
-            load_some<T, kVec>(in + token * stride + d, token < n && d < dim ? kVec : 0, x[m]);
+            if (token < n && d < dim) x[m] = *reinterpret_cast<const Pack<T, kVec> *>(in + token * stride + d);
         }
 #pragma unroll
         for (int m = 0; m < kItems; ++m) {
             const int i = first_item + m * kThreads, token = i >> a.pack_shift, d = (i & ((1 << a.pack_shift) - 1)) * kVec;
             if (token >= n || d >= dim) continue;
-            *reinterpret_cast<float4 *>(fresh + token * pitch + d) = make_float4(x[m][0], x[m][1], x[m][2], x[m][3]);
-            *reinterpret_cast<float4 *>(fresh + token * pitch + d + 4) = make_float4(x[m][4], x[m][5], x[m][6], x[m][7]);
+            *reinterpret_cast<Pack<T, kVec> *>(__builtin_assume_aligned(fresh + (s0 + token) * pitch + d, 16)) = x[m];
+            if (pairs == 0) {
 #pragma unroll
-            for (int e = 0; e < kVec; ++e)
-                if (d + e >= 2 * pairs) largest = max(largest, magnitude(x[m][e]));
+                for (int e = 0; e < kVec; ++e) largest = max(largest, magnitude(static_cast<float>(x[m].v[e])));
+            }
         }
     }
     __syncthreads();
-    if (p < pairs) {
-        const int axis = p < a.n_time ? 0 : p < a.n_time + a.n_y ? 1 : 2;
-        for (int token = threadIdx.x >> a.pair_shift; token < n; token += kThreads >> a.pair_shift) {
-            const uint64_t phase = (uint64_t)(int64_t)places[axis][token] * step;
-            const float turned = (float)(int32_t)(phase >> 32) * 0x1p-32f;
-            const float sn = __builtin_amdgcn_sinf(turned), cs = __builtin_amdgcn_cosf(turned);
-            float *u = fresh + token * pitch + (a.interleaved ? 2 * p : p), *w = u + (a.interleaved ? 1 : pairs);
-            const float x = *u, y = *w, c = x * cs - y * sn, d = x * sn + y * cs;
-            *u = c;
-            *w = d;
-            largest = max(largest, max(magnitude(c), magnitude(d)));
+    // each(token, dimension, key) of the keys, turned
+    const int axis = p < a.n_time ? 0 : p < a.n_time + a.n_y ? 1 : 2;
+    const int d0 = a.interleaved ? 2 * p : p, d1 = d0 + (a.interleaved ? 1 : pairs);
+    const auto turn = [&](auto &&each) {
+        if (p < pairs) {
+            for (int token = threadIdx.x >> a.pair_shift; token < n; token += kThreads >> a.pair_shift) {
+                const uint64_t phase = (uint64_t)(int64_t)places[axis][token] * step;
+                const float turned = (float)(int32_t)(phase >> 32) * 0x1p-32f;
+                const float sn = __builtin_amdgcn_sinf(turned), cs = __builtin_amdgcn_cosf(turned);
+                const T *row = fresh + (s0 + token) * pitch;
+                const float x = static_cast<float>(row[d0]), y = static_cast<float>(row[d1]);
+                each(token, d0, x * cs - y * sn);
+                each(token, d1, x * sn + y * cs);
+            }
         }
-    }
+        // dimensions beyond the pairs
+        for (int token = threadIdx.x >> 6; token < n; token += WAVES)
+            for (int d = 2 * pairs + (threadIdx.x & 63); d < dim; d += 64)
+                each(token, d, static_cast<float>(fresh[(s0 + token) * pitch + d]));
+    };
+    if (pairs) turn([&](int, int, float x) { largest = max(largest, magnitude(x)); });
     largest = block_largest<WAVES>(largest, slot);
-    __syncthreads();  // (every turned token is there, and every wave has read the old scale)
+    __syncthreads();  // (every wave has read the old scale)
 
     // the page's scale; one with values that are not finite has NaN, and zeros
     float scale = largest < 0x7f800000u ? __uint_as_float(largest) / 127.0f : __uint_as_float(0x7fc00000u);
@@ -158,26 +173,23 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
 
     if (!values) {
         int8_t *k = a.cache.k + block * (kPage * dim);
+        turn([&](int token, int d, float x) { whole[token * dim + d] = (int8_t)(kept & rounded(x, per)); });
+        __syncthreads();
         const int shift = a.pack_shift - 1;  // chunks of 16
         for (int i = ((held ? 0 : s0) << shift) + threadIdx.x; i < s1 << shift; i += kThreads) {
             const int token = i >> shift, d = (i & ((1 << shift) - 1)) * 16;
             if (d >= dim) continue;
             i32x4 *at = reinterpret_cast<i32x4 *>(k + token * dim + d);
-            i32x4 c = {0, 0, 0, 0};
-            if (token < s0) {
-                const i32x4 before = *at;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    c[e] = kept & bytes(rounded(byte_of(before, 4 * e), again), rounded(byte_of(before, 4 * e + 1), again),
-                                        rounded(byte_of(before, 4 * e + 2), again), rounded(byte_of(before, 4 * e + 3), again));
-            } else {
-                const float4 *x = reinterpret_cast<const float4 *>(fresh + (token - s0) * pitch + d);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float4 y = x[e];
-                    c[e] = kept & bytes(rounded(y.x, per), rounded(y.y, per), rounded(y.z, per), rounded(y.w, per));
-                }
+            if (token >= s0) {
+                *at = *reinterpret_cast<const i32x4 *>(whole + (token - s0) * dim + d);
+                continue;
             }
+            const i32x4 before = *at;
+            i32x4 c;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                c[e] = kept & bytes(rounded(byte_of(before, 4 * e), again), rounded(byte_of(before, 4 * e + 1), again),
+                                    rounded(byte_of(before, 4 * e + 2), again), rounded(byte_of(before, 4 * e + 3), again));
             *at = c;
         }
         return;
@@ -193,21 +205,22 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
         const uint32_t brings = of_part(ends & ~begins), holds = held ? of_part(begins) : 0;
         if (!(brings | holds)) continue;
         i32x4 *at = reinterpret_cast<i32x4 *>(v + d * kPage + 16 * part);
-        i32x4 c = {0, 0, 0, 0};
-        if (brings == 0xffff) {
-            const float *x = fresh + (4 * part - s0) * pitch + d;
+        // (no branches: what the places of other tokens have in LDS is read and left out)
+        const T *x = fresh + 4 * part * pitch + d;
+        const auto value = [&](int e, int i) { return rounded(static_cast<float>(x[(16 * e + i) * pitch]), per); };
+        i32x4 c, before = {0, 0, 0, 0};
+        if (brings != 0xffff) before = *at;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                c[e] = kept & bytes(rounded(x[16 * e * pitch], per), rounded(x[(16 * e + 1) * pitch], per),
-                                    rounded(x[(16 * e + 2) * pitch], per), rounded(x[(16 * e + 3) * pitch], per));
-        } else {
-            const i32x4 before = *at;
+        for (int e = 0; e < 4; ++e) {
+            c[e] = kept & bytes(value(e, 0), value(e, 1), value(e, 2), value(e, 3));
+            c[e] = (c[e] & of_bits(brings >> (4 * e))) | (before[e] & ~of_bits(brings >> (4 * e)));
+        }
+        if (held) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                uint32_t b = (uint32_t)(before[e >> 2] >> (8 * (e & 3)));
-                if (brings >> e & 1) b = kept & rounded(fresh[(16 * (e >> 2) + 4 * part + (e & 3) - s0) * pitch + d], per);
-                else if (holds >> e & 1) b = kept & rounded(byte_of(before, e), again);
-                c[e >> 2] |= (b & 0xff) << (8 * (e & 3));
+            for (int e = 0; e < 4; ++e) {
+                const int again_4 = kept & bytes(rounded(byte_of(before, 4 * e), again), rounded(byte_of(before, 4 * e + 1), again),
+                                                 rounded(byte_of(before, 4 * e + 2), again), rounded(byte_of(before, 4 * e + 3), again));
+                c[e] = (again_4 & of_bits(holds >> (4 * e))) | (c[e] & ~of_bits(holds >> (4 * e)));
             }
         }
         *at = c;
@@ -222,7 +235,6 @@ int64_t append_workgroups(int32_t n_tracks, int32_t total, int32_t kv_heads) {
 
 hipError_t launch_append(AppendArgs a, int32_t dtype, hipStream_t stream) {
     const dim3 grid((uint32_t)append_workgroups(a.tracks.n_tracks, a.tracks.total, a.cache.kv_heads));
-    const size_t lds = (size_t)std::min<int64_t>(kPage, a.tracks.total) * (a.cache.dim + kPad) * sizeof(float);
     const auto shift = [](int n) {
         int s = 0;
         while ((1 << s) < n) ++s;
@@ -232,6 +244,7 @@ hipError_t launch_append(AppendArgs a, int32_t dtype, hipStream_t stream) {
     a.pair_shift = shift(a.pairs);
     return with_dtype(dtype, [&](auto zero) {
         using T = decltype(zero);
+        const size_t lds = kPage * (a.cache.dim + kPad) * sizeof(T) + kPage * a.cache.dim;
         if (a.tracks.total <= 8 * (int64_t)a.tracks.n_tracks) hipLaunchKernelGGL((append_kernel<T, 1>), grid, dim3(64), lds, stream, a);
         else hipLaunchKernelGGL((append_kernel<T, 4>), grid, dim3(256), lds, stream, a);
         return hipGetLastError();
