@@ -8,7 +8,7 @@
 //
 // A workgroup takes the keys or the values of one page and kv head, so that no two
 // meet in memory: they stay in LDS as they came between the search for the largest and
-// the rounding, and keys are turned in both.  Tokens that the page does not get yet are
+// the rounding.  Tokens that the page does not get yet are
 // left as they are.
 //
 // The time is that of a workgroup's trips to memory one after the other (the track, its
@@ -137,27 +137,48 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
         }
     }
     __syncthreads();
-    // each(token, dimension, key) of the keys, turned
+    // keys, turned: a pair of a token at a time, and what is beyond the pairs
     const int axis = p < a.n_time ? 0 : p < a.n_time + a.n_y ? 1 : 2;
     const int d0 = a.interleaved ? 2 * p : p, d1 = d0 + (a.interleaved ? 1 : pairs);
-    const auto turn = [&](auto &&each) {
-        if (p < pairs) {
-            for (int token = threadIdx.x >> a.pair_shift; token < n; token += kThreads >> a.pair_shift) {
-                const uint64_t phase = (uint64_t)(int64_t)places[axis][token] * step;
-                const float turned = (float)(int32_t)(phase >> 32) * 0x1p-32f;
-                const float sn = __builtin_amdgcn_sinf(turned), cs = __builtin_amdgcn_cosf(turned);
-                const T *row = fresh + (s0 + token) * pitch;
-                const float x = static_cast<float>(row[d0]), y = static_cast<float>(row[d1]);
-                each(token, d0, x * cs - y * sn);
-                each(token, d1, x * sn + y * cs);
-            }
-        }
-        // dimensions beyond the pairs
+    const int first_token = threadIdx.x >> a.pair_shift, apart = kThreads >> a.pair_shift;
+    const auto turn = [&](int token) {
+        const uint64_t phase = (uint64_t)(int64_t)places[axis][token] * step;
+        const float turned = (float)(int32_t)(phase >> 32) * 0x1p-32f;
+        const float sn = __builtin_amdgcn_sinf(turned), cs = __builtin_amdgcn_cosf(turned);
+        const T *row = fresh + (s0 + token) * pitch;
+        const float x = static_cast<float>(row[d0]), y = static_cast<float>(row[d1]);
+        return make_float2(x * cs - y * sn, x * sn + y * cs);
+    };
+    const auto others_of = [&](auto &&each) {
         for (int token = threadIdx.x >> 6; token < n; token += WAVES)
             for (int d = 2 * pairs + (threadIdx.x & 63); d < dim; d += 64)
                 each(token, d, static_cast<float>(fresh[(s0 + token) * pitch + d]));
     };
-    if (pairs) turn([&](int, int, float x) { largest = max(largest, magnitude(x)); });
+    // (four waves keep what they turned, at most 64 x 64 pairs; one has a few tokens, and turns them again)
+    constexpr int kTurns = WAVES == 4 ? kPage * 64 / kThreads : 1;
+    float2 mine[kTurns];
+    const auto note = [&](float x) { largest = max(largest, magnitude(x)); };
+    if (pairs) {
+        if (p < pairs) {
+            if constexpr (WAVES == 4) {
+#pragma unroll
+                for (int m = 0; m < kTurns; ++m) {
+                    const int token = first_token + m * apart;
+                    if (token >= n) break;
+                    mine[m] = turn(token);
+                    note(mine[m].x);
+                    note(mine[m].y);
+                }
+            } else {
+                for (int token = first_token; token < n; token += apart) {
+                    const float2 z = turn(token);
+                    note(z.x);
+                    note(z.y);
+                }
+            }
+        }
+        others_of([&](int, int, float x) { note(x); });
+    }
     largest = block_largest<WAVES>(largest, slot);
     __syncthreads();  // (every wave has read the old scale)
 
@@ -173,7 +194,25 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
 
     if (!values) {
         int8_t *k = a.cache.k + block * (kPage * dim);
-        turn([&](int token, int d, float x) { whole[token * dim + d] = (int8_t)(kept & rounded(x, per)); });
+        const auto keep = [&](int token, int d, float x) { whole[token * dim + d] = (int8_t)(kept & rounded(x, per)); };
+        if (p < pairs) {
+            if constexpr (WAVES == 4) {
+#pragma unroll
+                for (int m = 0; m < kTurns; ++m) {
+                    const int token = first_token + m * apart;
+                    if (token >= n) break;
+                    keep(token, d0, mine[m].x);
+                    keep(token, d1, mine[m].y);
+                }
+            } else {
+                for (int token = first_token; token < n; token += apart) {
+                    const float2 z = turn(token);
+                    keep(token, d0, z.x);
+                    keep(token, d1, z.y);
+                }
+            }
+        }
+        others_of(keep);
         __syncthreads();
         const int shift = a.pack_shift - 1;  // chunks of 16
         for (int i = ((held ? 0 : s0) << shift) + threadIdx.x; i < s1 << shift; i += kThreads) {
