@@ -395,6 +395,7 @@ struct TrackAttentionArgs {
 // How the pages of a row are dealt out.
 struct TrackPlan {
     int32_t tile_rows;    // rows of a workgroup
+    int32_t waves;        // ... and its waves, which share their pages
     int64_t slots;        // numbers of row tiles
     int32_t splits;       // workgroups that may share a row's pages ...
     int32_t split_pages;  // ... and how many pages each takes

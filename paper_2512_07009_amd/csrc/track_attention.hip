@@ -161,11 +161,11 @@ __device__ __forceinline__ void begin(Row<DI> &w, const TrackAttentionArgs &a, c
     w.factor = whole.factor<CAP>(a);
 }
 
-template <typename T, int DI, int CAP>
-__global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) track_attention_kernel(TrackAttentionArgs a) {
+template <typename T, int DI, int CAP, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) track_attention_kernel(TrackAttentionArgs a) {
     constexpr int kBlocks = 4 * DI;   // 16 dimensions each, at most
-    __shared__ float sums[kWaves][kRows][64 * DI + 1];
-    __shared__ float stats[2][kWaves][kRows];
+    __shared__ float sums[WAVES][kRows][64 * DI + 1];
+    __shared__ float stats[2][WAVES][kRows];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = lane >> 4, r = lane & 15;
     const int dim = a.cache.dim, blocks = dim / 16;
     const uint32_t block_id = a.gathered ? (uint32_t)attention::xcd_order(blockIdx.x, gridDim.x) : blockIdx.x;
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) 
     if (split >= active) return;
     const int p0 = it.first_page + split * a.split_pages + wave;
     const int p1 = min(it.first_page + (split + 1) * a.split_pages, it.first_page + it.pages);
-    const int count = p1 > p0 ? (p1 - p0 + kWaves - 1) / kWaves : 0;  // of this wave: p0, p0 + 4, ...
+    const int count = p1 > p0 ? (p1 - p0 + WAVES - 1) / WAVES : 0;  // of this wave: p0, p0 + 4, ...
 
     Row<DI> w;
     begin<T, DI, CAP>(w, a, it, r);
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) 
         for (; n < count; ++n) {
             if ((n & 63) == 0) {
                 const int mine = n + lane;
-                my_page = mine < count ? table[p0 + kWaves * mine] : -1;
+                my_page = mine < count ? table[p0 + WAVES * mine] : -1;
                 if (my_page >= a.cache.pages) my_page = -1;
                 const int64_t block = (int64_t)max(my_page, 0) * a.cache.kv_heads + it.head;
                 my_k = my_page >= 0 ? a.cache.k_scale[block] : 0.0f;
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) 
         load_v(page);
     }
     while (page >= 0) {
-        const int token0 = (p0 + kWaves * n) * kPage;
+        const int token0 = (p0 + WAVES * n) * kPage;
         const float k_scale = scale_of(my_k, n), v_scale = scale_of(my_v, n);
         ++n;
         const int after = next(n);
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) 
     __syncthreads();
     float now = stats[0][0][r];
 #pragma unroll
-    for (int v = 1; v < kWaves; ++v) now = fmaxf(now, stats[0][v][r]);
+    for (int v = 1; v < WAVES; ++v) now = fmaxf(now, stats[0][v][r]);
     // (a shift that nothing has moved: no token, or none but NaN)
     const float keep = w.shift == -INFINITY ? (w.total == w.total ? 0.0f : w.total) : attention::exp2_fast(w.shift - now);
     if (part == 0) stats[1][wave][r] = w.total * keep;
@@ -337,21 +337,25 @@ __global__ void __launch_bounds__(kThreads, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3) 
     __syncthreads();
     // a wave a row, a lane a dimension
 #pragma unroll 1
-    for (int rr = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); rr < it.rows; rr += kWaves) {
-        const float l = (stats[1][0][rr] + stats[1][1][rr]) + (stats[1][2][rr] + stats[1][3][rr]);
+    for (int rr = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); rr < it.rows; rr += WAVES) {
+        float l = 0.0f, m = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) {
+            l += stats[1][v][rr];
+            m = fmaxf(m, stats[0][v][rr]);
+        }
         const uint32_t row = it.row0 + rr, query = row / (uint32_t)a.group;
         const int64_t bird = it.at.row0 + query;
         const int head = it.head * a.group + (int)(row - query * a.group);
         const int64_t to = ((int64_t)split * a.tracks.total + bird) * a.q_heads + head;
         for (int d = threadIdx.x & 63; d < dim; d += 64) {
-            const float o = (sums[0][rr][d] + sums[1][rr][d]) + (sums[2][rr][d] + sums[3][rr][d]);
+            float o = 0.0f;
+#pragma unroll
+            for (int v = 0; v < WAVES; ++v) o += sums[v][rr][d];
             if (active == 1) static_cast<T *>(a.out)[bird * a.out_stride + head * dim + d] = static_cast<T>(l == 0.0f ? 0.0f : o / l);
             else a.part_out[to * dim + d] = o;
         }
-        if (active > 1 && (threadIdx.x & 63) == 0) {
-            const float m = fmaxf(fmaxf(stats[0][0][rr], stats[0][1][rr]), fmaxf(stats[0][2][rr], stats[0][3][rr]));
-            reinterpret_cast<float2 *>(a.part_stat)[to] = make_float2(m, l);
-        }
+        if (active > 1 && (threadIdx.x & 63) == 0) reinterpret_cast<float2 *>(a.part_stat)[to] = make_float2(m, l);
     }
 }
 
@@ -688,11 +692,12 @@ __global__ void __launch_bounds__(kThreads) track_join_kernel(TrackAttentionArgs
     if (lane + 64 < dim) out[lane + 64] = static_cast<T>(l == 0.0f ? 0.0f : o1 / l);
 }
 
-template <typename T, int DI>
-void launch_cap(const TrackAttentionArgs &a, dim3 grid, hipStream_t stream) {
-    if (a.cap == 0.0f) hipLaunchKernelGGL((track_attention_kernel<T, DI, kNoCap>), grid, dim3(kThreads), 0, stream, a);
-    else if (a.cap <= attention::kLowCap) hipLaunchKernelGGL((track_attention_kernel<T, DI, kLow>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((track_attention_kernel<T, DI, kHigh>), grid, dim3(kThreads), 0, stream, a);
+template <typename T, int DI, int WAVES>
+void launch_few(const TrackAttentionArgs &a, dim3 grid, hipStream_t stream) {
+    const dim3 block(64 * WAVES);
+    if (a.cap == 0.0f) hipLaunchKernelGGL((track_attention_kernel<T, DI, kNoCap, WAVES>), grid, block, 0, stream, a);
+    else if (a.cap <= attention::kLowCap) hipLaunchKernelGGL((track_attention_kernel<T, DI, kLow, WAVES>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((track_attention_kernel<T, DI, kHigh, WAVES>), grid, block, 0, stream, a);
 }
 
 template <typename T, int DP>
@@ -707,8 +712,8 @@ hipError_t launch_type(const TrackAttentionArgs &a, const TrackPlan &p, hipStrea
     const int64_t items = p.slots * a.cache.kv_heads;
     const dim3 grid((uint32_t)(items * p.splits));
     if (p.tile_rows == kRows) {
-        if (a.cache.dim <= 64) launch_cap<T, 1>(a, grid, stream);
-        else launch_cap<T, 2>(a, grid, stream);
+        if (a.cache.dim <= 64) p.waves == 1 ? launch_few<T, 1, 1>(a, grid, stream) : launch_few<T, 1, kWaves>(a, grid, stream);
+        else p.waves == 1 ? launch_few<T, 2, 1>(a, grid, stream) : launch_few<T, 2, kWaves>(a, grid, stream);
     } else {
         if (a.cache.dim <= 64) launch_many<T, 64>(a, grid, stream);
         else launch_many<T, 128>(a, grid, stream);
@@ -736,6 +741,9 @@ TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_page
     // compute unit 68 us, four 77, eight 88)
     const int64_t items = std::max<int64_t>(n_tracks, (int64_t)total * group / p.tile_rows) * kv_heads;
     const int resident = many ? 3 : 2;
+    // one wave a workgroup where short tracks fill the card so (4096 of 64 tokens 48 -> 22 us, of 256
+    // 68 -> 49; of 1024 196 -> 204, 2000 of up to 1800 94 -> 110)
+    p.waves = !many && max_pages <= 8 && items >= 12 * (int64_t)n_cus ? 1 : kWaves;
     int64_t splits = resident * (int64_t)n_cus / items;
     splits = std::max<int64_t>(std::min<int64_t>(splits, (max_pages + 2 * kWaves - 1) / (2 * kWaves)), 1);
     p.split_pages = std::max((int32_t)((max_pages + splits - 1) / splits), 1);

@@ -424,3 +424,50 @@ def test_empty_calls():
     no_pages = flock.TrackCache.empty(0, 1, 64)
     flock.append_tracks(no_pages, one, one, int32([0, 1]), int32([[0]]), int32([1]))
     assert (flock.attention_tracks(one, no_pages, int32([0, 1]), int32([[0]]), int32([1])) == 0).all()
+
+
+@pytest.mark.parametrize("dim,cap", [(32, 0.0), (64, 20.0), (128, 0.0)])
+def test_attention_of_many_short_tracks(dim, cap):
+    """A wave a workgroup: 1600 tracks of two kv heads."""
+    gen = torch.Generator().manual_seed(18)
+    lengths = torch.randint(0, 200, (1600,), generator=gen).tolist()
+    queries = [min(n, int(m)) for n, m in zip(lengths, torch.randint(0, 3, (1600,), generator=gen))]
+    attend(18, lengths, queries, dim=dim, cap=cap)
+
+
+@pytest.mark.parametrize("dim,cap,dtype", [(64, 0.0, torch.bfloat16), (96, 30.0, torch.float16), (128, 100.0, torch.bfloat16)])
+def test_attention_of_long_runs_of_queries(dim, cap, dtype):
+    """128 rows a workgroup: 150 to 700 rows of each track and kv head."""
+    gen = torch.Generator().manual_seed(19)
+    lengths = (300 + torch.randint(0, 200, (40,), generator=gen)).tolist()
+    queries = (75 + torch.randint(0, 100, (40,), generator=gen)).tolist()
+    lengths[3], queries[3] = 100, 140       # rows before the track's first token
+    queries[5] = 0
+    lengths[7], queries[7] = 360, 350
+    attend(19, lengths, queries, q_heads=16, kv_heads=8, dim=dim, cap=cap, dtype=dtype)
+    attend(19, lengths, queries, q_heads=16, kv_heads=8, dim=dim, cap=cap, dtype=dtype, window=70)
+
+
+def test_attention_of_long_runs_with_pages_that_are_none_or_not_finite():
+    def spoil(table, c):
+        table[0, 1] = -1
+        table[1, 0] = len(c[0])
+        table[2, :] = 2 ** 31 - 1
+        c[3][int(table[4, 0])] = 0
+        c[2][int(table[5, 1])] = 0
+        c[3][:] *= torch.logspace(-3, 3, c[3].numel()).reshape(c[3].shape)
+    lengths, queries = [300] * 40, [150] * 40
+    got = attend(20, lengths, queries, q_heads=16, kv_heads=8, spoil=spoil)
+    assert (got[300:450] == 0).all()
+
+    gen = torch.Generator().manual_seed(21)
+    c = pool(gen, 200, 8, 64)
+    table = table_of(gen, lengths, 200)
+    c[2][int(table[0, 1]), 3] = math.nan    # tokens 64 .. 127 of track 0: none of its queries is before them
+    c[3][int(table[1, 3]), 2] = math.nan    # tokens 192 .. 255 of track 1: seen from its 43rd query on
+    q = torch.randn(6000, 16, 64, generator=gen).bfloat16()
+    got = flock.attention_tracks(q.cuda(), cuda(c), int32(offsets_of(queries)), table.cuda(), int32(lengths)).cpu()
+    bad = torch.zeros(6000, 16, dtype=torch.bool)
+    bad[:150, 6:8] = True
+    bad[192:300, 4:6] = True
+    assert torch.equal(torch.isnan(got).all(2), bad) and torch.equal(torch.isnan(got).any(2), bad)
