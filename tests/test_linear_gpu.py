@@ -74,9 +74,23 @@ def test_widths(width, rows):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
 @pytest.mark.parametrize("rows,outputs", [(9, 48), (100, 100), (9000, 600), (4097, 1030)])
 def test_types(rows, outputs, dtype):
-    """The last two are products by the larger tiles."""
     compare(case(3, rows, 160, outputs, bias=False), dtype)
     compare(case(4, rows, 160, outputs), dtype, gelu=True)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("width", [40, 128, 130, 256, 384, 500, 1000])
+def test_tiles_of_128_by_workgroups_that_stay(width, dtype):
+    """785 tiles, the last of each side cut, over 512 workgroups: steps of one to eight a tile."""
+    c = case(width, 20001, width, 601)
+    pitch = (width + 15) // 16 * 16
+    compare(c, dtype, x=padded(c["x"], pitch), w=padded(c["w"], pitch))
+    if width in (40, 500):
+        compare(c, dtype, gelu=True, x=padded(c["x"], pitch + 16), w=padded(c["w"], pitch))
+
+
+def test_whole_tiles_of_128():
+    compare(case(1, 128 * 160, 256, 128 * 8), torch.bfloat16)
 
 
 @pytest.mark.parametrize("rows", [3, 50, 8500])
