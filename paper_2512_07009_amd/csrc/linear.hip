@@ -36,7 +36,7 @@ __device__ __forceinline__ i32x4 load_chunk(const int8_t *row, int k, int width)
 // result in all, against 3.9e-3 for half a step of bfloat16.  The library's erfc takes some
 // three times the instructions, which the products do not cover.
 __device__ __forceinline__ float gelu(float x) {
-    const float z = fabsf(x);
+    const float z = fminf(fabsf(x), 0x1p60f);  // (infinity times nothing)
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.36062445840513924f, z, 1.0f));
     float p = 0.047249945f;
     p = __builtin_fmaf(p, t, -0.1795673f);

@@ -20,8 +20,7 @@ constexpr int kThreads = 256;
 template <int TPR>
 __device__ __forceinline__ float row_sum(float x, float *slot) {
     constexpr int kLanes = TPR < 64 ? TPR : 64;
-#pragma unroll
-    for (int d = kLanes / 2; d > 0; d >>= 1) x += __shfl_xor(x, d);
+    x = over_lanes<kLanes>(x, [](float u, float v) { return u + v; });
     if (TPR > 64) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) slot[wave] = x;

@@ -13,19 +13,20 @@
 // nothing but whole numbers and a scale a row is written.
 
 #include "norm_common.h"
+#include "whole.h"
 
 namespace flock {
 namespace {
 
 using namespace norm;
+using namespace whole;
 
 // Largest |x| over the TPR lanes that share a row, as bits: those of NaN are above
 // those of infinity, and both above those of any number.
 template <int TPR>
 __device__ __forceinline__ uint32_t row_largest(uint32_t x, uint32_t *slot) {
     constexpr int kLanes = TPR < 64 ? TPR : 64;
-#pragma unroll
-    for (int d = kLanes / 2; d > 0; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+    x = over_lanes<kLanes>(x, [](uint32_t u, uint32_t v) { return max(u, v); });
     if (TPR > 64) {
         const int wave = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0) slot[wave] = x;
@@ -35,34 +36,37 @@ __device__ __forceinline__ uint32_t row_largest(uint32_t x, uint32_t *slot) {
     return x;
 }
 
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
 // How a row whose largest |y| has these bits goes to 8 bits.  Rows below 2^-100
 // are zeros (127 / largest would leave 32 bits), those with values that are not
 // finite zeros with a scale of NaN, which every product with them then is.
 struct Steps {
     float scale, per;
+    int kept;  // bits of a whole number: none of one that is zero by this
     __device__ __forceinline__ explicit Steps(uint32_t largest) {
         const float most = __uint_as_float(largest);
         const bool finite = largest < 0x7f800000u, some = finite && most >= 0x1p-100f;
         scale = finite ? (some ? most / 127.0f : 0.0f) : __uint_as_float(0x7fc00000u);
         per = some ? 127.0f / most : 0.0f;
+        kept = some ? -1 : 0;
     }
-    __device__ __forceinline__ int round(float y) const { return per > 0.0f ? (int)rintf(y * per) : 0; }
+    __device__ __forceinline__ int round(float y) const { return (int)rounded(y, per) & kept; }
+    __device__ __forceinline__ int round(float y0, float y1, float y2, float y3) const {
+        return bytes(rounded(y0, per), rounded(y1, per), rounded(y2, per), rounded(y3, per)) & kept;
+    }
 };
 
 template <int N>
 __device__ __forceinline__ void store_whole(int8_t *p, int n, const float (&y)[N], const Steps &s) {
-    Pack<int8_t, N> a;
+    struct __attribute__((packed, aligned(1))) Words { int v[N / 4]; } a;
 #pragma unroll
-    for (int i = 0; i < N; ++i) a.v[i] = (int8_t)s.round(y[i]);
+    for (int i = 0; i < N / 4; ++i) a.v[i] = s.round(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
     if (n >= N) {
-        *reinterpret_cast<Pack<int8_t, N> *>(p) = a;
+        *reinterpret_cast<Words *>(p) = a;
         return;
     }
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if (i < n) p[i] = a.v[i];
+        if (i < n) p[i] = (int8_t)(a.v[i / 4] >> (8 * (i % 4)));
 }
 
 // What is made of a row: its norm in the features' type, in 8 bits, or the row as
@@ -123,13 +127,12 @@ __global__ void __launch_bounds__(kThreads) rms_kernel(RmsArgs a) {
         }
     }
     if (FORM == kNormed) return;
+    // (what lies beyond the row was loaded as zeros)
     uint32_t largest = 0;
 #pragma unroll
-    for (int i = 0; i < ITER; ++i) {
-        const int c = (i * TPR + lane) * VEC;
+    for (int i = 0; i < ITER; ++i)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) largest = max(largest, c + e < width ? magnitude(h[i][e]) : 0u);
-    }
+        for (int e = 0; e < VEC; ++e) largest = max(largest, magnitude(h[i][e]));
     const Steps steps(row_largest<TPR>(largest, most));
     if (lane == 0) a.scale[row] = steps.scale;
     int8_t *q = static_cast<int8_t *>(a.y) + row * a.y_stride;

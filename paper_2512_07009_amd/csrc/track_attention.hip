@@ -60,10 +60,15 @@ __device__ __forceinline__ f16x8 to_half(int lo, int hi) {
     return r;
 }
 
-template <typename F>
-__device__ __forceinline__ float over_parts(float x, F &&f) {
-    x = f(x, __shfl_xor(x, 16));
-    return f(x, __shfl_xor(x, 32));
+// f over the four lanes that share a row.
+template <typename V, typename F>
+__device__ __forceinline__ V over_parts(V x, F &&f) {
+    const auto bits = [](V v) { return __builtin_bit_cast(uint32_t, v); };
+    const auto value = [](uint32_t v) { return __builtin_bit_cast(V, v); };
+    const auto p = __builtin_amdgcn_permlane16_swap(bits(x), bits(x), false, false);
+    x = f(value(p[0]), value(p[1]));
+    const auto q = __builtin_amdgcn_permlane32_swap(bits(x), bits(x), false, false);
+    return f(value(q[0]), value(q[1]));
 }
 
 // What a workgroup, or the one that joins, works on.
@@ -153,8 +158,7 @@ __device__ __forceinline__ void begin(Row<DI> &w, const TrackAttentionArgs &a, c
 #pragma unroll
         for (int e = 0; e < 16; ++e) bits = max(bits, __float_as_uint(x[i][e]) & 0x7fffffffu);
     }
-    bits = max(bits, (uint32_t)__shfl_xor((int)bits, 16));
-    bits = max(bits, (uint32_t)__shfl_xor((int)bits, 32));
+    bits = over_parts(bits, [](uint32_t u, uint32_t v) { return max(u, v); });
     const Whole whole(bits);
 #pragma unroll
     for (int i = 0; i < DI; ++i) whole.split(x[i], w.high[i], w.low[i]);
@@ -662,8 +666,7 @@ __global__ void __launch_bounds__(kThreads) track_join_kernel(TrackAttentionArgs
         float2 stat = make_float2(-INFINITY, 0.0f);
         if (s < active) stat = reinterpret_cast<const float2 *>(a.part_stat)[s * pitch + at];
         float now = stat.x;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) now = fmaxf(now, __shfl_xor(now, d));
+        now = over_lanes<64>(now, [](float u, float v) { return fmaxf(u, v); });
         now = fmaxf(now, m);
         if (now > m) {
             if (m != -INFINITY) {
@@ -676,8 +679,7 @@ __global__ void __launch_bounds__(kThreads) track_join_kernel(TrackAttentionArgs
         }
         const float keep = stat.y == 0.0f ? 0.0f : stat.x == -INFINITY ? stat.y : attention::exp2_fast(stat.x - m);
         float sum = stat.y * keep;
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        sum = over_lanes<64>(sum, [](float u, float v) { return u + v; });
         l += sum;
         const float *p = a.part_out + (first * pitch + at) * dim;
 #pragma unroll 8

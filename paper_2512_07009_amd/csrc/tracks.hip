@@ -8,8 +8,7 @@
 //
 // A workgroup takes the keys or the values of one page and kv head, so that no two
 // meet in memory: they stay in LDS as they came between the search for the largest and
-// the rounding.  Tokens that the page does not get yet are
-// left as they are.
+// the rounding.  Tokens that the page does not get yet are left as they are.
 //
 // The time is that of a workgroup's trips to memory one after the other (the track, its
 // page, the rows with their positions and the page's scale), not of bytes: as many
@@ -17,11 +16,13 @@
 // a wave; clips take four.
 
 #include "tracks_common.h"
+#include "whole.h"
 
 namespace flock {
 namespace {
 
 using namespace tracks;
+using namespace whole;
 
 constexpr int kVec = 8, kItems = 4;
 constexpr int kPad = 8;  // between tokens in LDS: those of four parts of a dimension's places lie in other banks
@@ -29,25 +30,13 @@ constexpr int kPad = 8;  // between tokens in LDS: those of four parts of a dime
 // Largest |x| over the workgroup, as bits (those of NaN are the largest).
 template <int WAVES>
 __device__ __forceinline__ uint32_t block_largest(uint32_t x, uint32_t *slot) {
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+    x = over_lanes<64>(x, [](uint32_t u, uint32_t v) { return max(u, v); });
     if (WAVES == 1) return x;
     if ((threadIdx.x & 63) == 0) slot[threadIdx.x >> 6] = x;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) x = max(x, slot[w]);
     return x;
-}
-
-__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// x / scale to the nearest whole number, ties to even, given 1 / scale: the low byte of
-// what is left of x / scale beside 1.5 x 2^23 (|x / scale| is below 128).
-__device__ __forceinline__ uint32_t rounded(float x, float per) { return __float_as_uint(__builtin_fmaf(x, per, 12582912.0f)); }
-
-// Four low bytes in one word.
-__device__ __forceinline__ int bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-    return (int)__builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
 }
 
 // A byte of ones for each of the four low bits.
