@@ -62,7 +62,7 @@ __device__ __forceinline__ void store_some(T *p, int n, const float (&in)[N]) {
 // apart first: the lanes 32 and 16 away by swaps of rows, the others by turns of a row of 16,
 // which is a lane 8, and then, where all that are 8 apart are alike, 4 away.  All lanes of
 // the LANES are active.  (Norms of 128000 rows of 512 in 8 bits, two of these a row: by
-// way of LDS, as __shfl_xor goes, 63 us, so 50; of 500 such rows and of pages no less.)
+// way of LDS, as __shfl_xor goes, 63 us, so 50.)
 template <int LANES, typename V, typename F>
 __device__ __forceinline__ V over_lanes(V x, F &&f) {
     static_assert(LANES == 8 || LANES == 16 || LANES == 32 || LANES == 64, "a row's lanes");

@@ -30,21 +30,33 @@ __device__ __forceinline__ i32x4 load_chunk(const int8_t *row, int k, int width)
     return v;
 }
 
-// x Phi(x), Phi the normal distribution.  With z = |x| / sqrt 2 and t = 1 / (1 + 0.51 z),
-// e^(z^2) erfc(z) / t is a polynomial of t to 9e-7 of itself (fitted to erfc over z <= 10, 7
-// terms; 6 are off by 5e-6), so that the tail of negative x keeps its digits: 6.5e-6 of the
-// result in all, against 3.9e-3 for half a step of bfloat16.  The library's erfc takes some
-// three times the instructions, which the products do not cover.
+// x Phi(x), Phi the normal distribution.  With z = |x| / sqrt 2 and t = 1 / (1 + c z),
+// e^(z^2) erfc(z) / t is nearly a polynomial of t (fitted to erfc over z <= 10), so that the
+// tail of negative x keeps its digits: 7 terms are off by 9e-7 of it, and with the roundings
+// the result by 6.5e-6; 5 by 3.2e-5, and the result by 3.7e-5 against 4.9e-4 and 3.9e-3 for
+// half a step of float16 and bfloat16, which get those.  The library's erfc takes some three
+// times the instructions, and instructions are what bounds the products that end in it.
+template <typename T>
 __device__ __forceinline__ float gelu(float x) {
+    constexpr bool kShort = sizeof(T) == 2;
     const float z = fminf(fabsf(x), 0x1p60f);  // (infinity times nothing)
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.36062445840513924f, z, 1.0f));
-    float p = 0.047249945f;
-    p = __builtin_fmaf(p, t, -0.1795673f);
-    p = __builtin_fmaf(p, t, 0.17922265f);
-    p = __builtin_fmaf(p, t, 0.027526545f);
-    p = __builtin_fmaf(p, t, 0.13953302f);
-    p = __builtin_fmaf(p, t, 0.142076165f);
-    p = __builtin_fmaf(p, t, 0.14395875f);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(kShort ? 0.3747665940288702f : 0.36062445840513924f, z, 1.0f));
+    float p;
+    if constexpr (kShort) {
+        p = -0.09049928f;
+        p = __builtin_fmaf(p, t, 0.20043353f);
+        p = __builtin_fmaf(p, t, 0.08345564f);
+        p = __builtin_fmaf(p, t, 0.15764168f);
+        p = __builtin_fmaf(p, t, 0.14896917f);
+    } else {
+        p = 0.047249945f;
+        p = __builtin_fmaf(p, t, -0.1795673f);
+        p = __builtin_fmaf(p, t, 0.17922265f);
+        p = __builtin_fmaf(p, t, 0.027526545f);
+        p = __builtin_fmaf(p, t, 0.13953302f);
+        p = __builtin_fmaf(p, t, 0.142076165f);
+        p = __builtin_fmaf(p, t, 0.14395875f);
+    }
     const float tail = p * t * __builtin_amdgcn_exp2f(x * x * -0.72134752044448170368f);  // 1 - Phi(|x|)
     return __builtin_fmaf(-z, tail, fmaxf(x, 0.0f));
 }
@@ -221,6 +233,12 @@ __device__ __forceinline__ Pack<T, 8> side_by_side(const float (&o)[8]) {
     return out;
 }
 
+// A pack of 16 bytes to LDS, where it begins at a multiple of them.
+template <typename T>
+__device__ __forceinline__ void put(Pack<T, 8> *at, const Pack<T, 8> &v) {
+    if constexpr (sizeof(v) == 16) *reinterpret_cast<i32x4 *>(__builtin_assume_aligned(at, 16)) = __builtin_bit_cast(i32x4, v);
+}
+
 // The first `left` of a pack, all of it where FULL.
 template <bool FULL, typename T>
 __device__ __forceinline__ void store_left(T *y, const Pack<T, 8> &v, int left) {
@@ -269,11 +287,11 @@ __device__ __forceinline__ void finish(const LinearArgs &a, const Tile &t, const
                 for (int e = 0; e < 8; ++e) {
                     const int at = n + (e & 3) + 8 * (e >> 2);
                     o[e] = (float)acc[i][j][r + e] * xs * s.w_scale[turn][at] + s.bias[turn][at];
-                    if (GELU) o[e] = gelu(o[e]);
+                    if (GELU) o[e] = gelu<T>(o[e]);
                 }
                 const Pack<T, 8> out = side_by_side<T>(o);
                 const int part = 4 * i + r / 4 + h;
-                if (kStaged) stage[part_at(col, part)] = out;
+                if (kStaged) put(stage + part_at(col, part), out);
                 else if (FULL || wm + 32 * j + col < t.rows)
                     store_left<FULL>(y + (int64_t)(32 * j + col) * a.y_stride + 8 * part, out, t.columns - wn - 8 * part);
             }
@@ -421,6 +439,172 @@ __global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// Very many rows of a width that fits: the weights stay.
+//
+// A workgroup keeps the weights of 256 outputs in LDS (128 KB) and takes rows, 32 at a
+// time and wave: their bytes go from memory to the wave's registers as factors, the next
+// rows' while this one's last outputs are made.  Waves wait for their own loads alone, so
+// that one's products run beside another's outputs and stores.  The workgroups of all
+// outputs of the same rows run side by side on one XCD, whose L2 then serves them.
+// Twelve waves are what registers allow, and one workgroup: two of six waves and half
+// the weights each lie three and three on two units of four, and do not fit together.
+// ---------------------------------------------------------------------------
+
+constexpr int kStayWidth = 512, kStayWaves = 12, kStayOutputs = 256, kStayHalf = 128;
+
+struct __attribute__((aligned(16))) StayShared {
+    float w_scale[kStayOutputs], bias[kStayOutputs];
+    int8_t room[kStayWaves][16 * 64 * 2];  // 16 rows of 64 outputs
+    int8_t w[kStayOutputs / kStayHalf][kStayWidth / kStep][kStayHalf * kStep];
+};
+
+template <typename T, bool GELU>
+__global__ void __launch_bounds__(64 * kStayWaves) linear_stay_kernel(LinearArgs a) {
+    constexpr int kBlocks = kStayHalf / 32, kParts = kStayWidth / 32;
+    __shared__ StayShared s;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    // this workgroup's outputs and rows
+    const int per_xcd = (int)(gridDim.x >> 3), groups = per_xcd / a.column_tiles;
+    const int xcd = blockIdx.x & 7, at = (int)(blockIdx.x >> 3), group = at / a.column_tiles;
+    if (group >= groups) return;
+    const int n0 = (at - group * a.column_tiles) * kStayOutputs, columns = min(kStayOutputs, a.outputs - n0);
+    const int64_t tiles = a.tiles, end = tiles * (xcd + 1) / 8;
+    int64_t tile = tiles * xcd / 8 + group * kStayWaves + wave;
+
+    const int8_t *w = a.w + n0 * (int64_t)a.w_stride;
+    for (int i = wave; i < kStayWidth / kStep * kStayOutputs * kChunks / 64; i += kStayWaves) {
+        const int slot = i * 64 + lane, row = slot / kChunks % kStayHalf, step = slot / (kStayHalf * kChunks);
+        const int k = step % (kStayWidth / kStep) * kStep + 16 * turned(row, slot % kChunks);
+        const int n = row + step / (kStayWidth / kStep) * kStayHalf;
+        i32x4 v = {0, 0, 0, 0};
+        if (k < a.width) v = load_chunk(w + (int64_t)min(n, columns - 1) * a.w_stride, k, a.width);
+        *reinterpret_cast<i32x4 *>(s.w[0][0] + 16 * slot) = v;
+    }
+    for (int i = threadIdx.x; i < kStayOutputs; i += 64 * kStayWaves) {
+        const int n = n0 + min(i, columns - 1);
+        s.w_scale[i] = a.w_scale[n];
+        s.bias[i] = a.bias ? a.bias[n] : 0.0f;
+    }
+    __syncthreads();
+    if (tile >= end) return;
+
+    i32x4 x[kParts];
+    float xs;
+    // a half of the next rows' chunks (rows beyond the last are the last; chunks beyond the width any bytes of
+    // the row, the weights are zeros there)
+    const auto load = [&](int64_t tile, int half) {
+        const int64_t row0 = tile * 32;
+        const uint32_t row = (uint32_t)min((int64_t)col, a.rows - 1 - row0), first = row * (uint32_t)a.x_stride;
+        uint32_t at = first + 16 * h;
+        asm volatile("" : "+v"(at));  // (not 16 places kept)
+        const int8_t *from = a.x + row0 * a.x_stride;
+        if (half == 0) xs = (a.x_scale + row0)[row];
+#pragma unroll
+        for (int k = half * kParts / 2; k < (half + 1) * kParts / 2; ++k)
+            x[k] = *reinterpret_cast<const i32x4 *>(from + (32 * k < a.width ? 32 * k : 0) + (32 * k + 16 < a.width ? at : first));
+    };
+    const auto part_at = [](int row, int part) { return row * 8 + (part ^ (row & 7)); };
+    Pack<T, 8> *room = reinterpret_cast<Pack<T, 8> *>(s.room[wave]);
+    // outputs of two blocks, by way of LDS
+    const auto make = [&](auto full, int n1, auto block, int64_t row0, const i32x16 (&acc)[kBlocks], float scale) {
+        constexpr int i = decltype(block)::value;
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));  // (places in LDS are made here, not kept)
+        const int h = lane >> 5, col = lane & 31;
+        const int rows = (int)min((int64_t)32, a.rows - row0), here = min(columns - n1 - 32 * i, 64);
+        T *y = static_cast<T *>(a.y) + row0 * a.y_stride + n0 + n1 + 32 * i;
+        Pack<T, 8> out[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int n = n1 + 32 * i + 16 * u + 4 * h;
+            float o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int at = n + (e & 3) + 8 * (e >> 2);
+                o[e] = (float)acc[i + u / 2][8 * (u & 1) + e] * scale * s.w_scale[at] + s.bias[at];
+                if (GELU) o[e] = gelu<T>(o[e]);
+            }
+            out[u] = side_by_side<T>(o);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            stand();
+            if (col >> 4 == half) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) put(room + part_at(col & 15, 2 * u + h), out[u]);
+            }
+            stand();
+            if (decltype(full)::value) {
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const int row = lane / 8, part = lane & 7;
+                    store_left<true>(y + (16 * half + 8 * v) * a.y_stride + ((uint32_t)row * (uint32_t)a.y_stride + 8 * part),
+                                     room[part_at(8 * v + row, part)], 8);
+                }
+            } else if (lane < here) {
+#pragma unroll 1
+                for (int row = 0; row < min(16, rows - 16 * half); ++row)
+                    y[(16 * half + row) * a.y_stride + lane] = room[part_at(row, lane / 8)].v[lane & 7];
+            }
+        }
+        stand();
+    };
+
+    const auto multiply = [&](int half, i32x16 (&acc)[kBlocks]) {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
+        const int h = lane >> 5, col = lane & 31;
+        __builtin_amdgcn_s_setprio(2);
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            i32x4 wf[kBlocks];
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i)
+                wf[i] = *reinterpret_cast<const i32x4 *>(s.w[half][k / 4] + (32 * i + col) * kStep + 16 * turned(col, 2 * (k % 4) + h));
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) acc[i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[i], x[k], acc[i], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    constexpr std::integral_constant<int, 0> kFirst;
+    constexpr std::integral_constant<int, 2> kSecond;
+    // rows up to a tile, all of whose rows and outputs are there where FULL; nothing branches
+    // there, so that a wait for rows is for those alone and not for stores
+    const auto go = [&](auto full, int64_t last) {
+        while (tile < last) {
+            const int64_t row0 = tile * 32;
+            const float scale = xs;
+            {
+                i32x16 acc[kBlocks] = {};
+                multiply(0, acc);
+                stand();
+                make(full, 0, kFirst, row0, acc, scale);
+                make(full, 0, kSecond, row0, acc, scale);
+            }
+            i32x16 acc[kBlocks] = {};
+            multiply(1, acc);
+            tile += groups * kStayWaves;
+            // (the second half of the next rows when there is room for it)
+            stand();
+            load(min(tile, end - 1), 0);
+            stand();
+            make(full, kStayHalf, kFirst, row0, acc, scale);
+            stand();
+            load(min(tile, end - 1), 1);
+            stand();
+            make(full, kStayHalf, kSecond, row0, acc, scale);
+        }
+    };
+    load(tile, 0);
+    load(tile, 1);
+    wait_but<0>();  // (so that the loop's waits are those of its later turns)
+    if (columns == kStayOutputs) go(std::true_type{}, min(end, a.rows / 32));
+    go(std::false_type{}, end);
+}
+
+// ---------------------------------------------------------------------------
 // Few rows: the weights are what is read, so a workgroup takes 16 outputs and its
 // eight waves share the width, 256 bytes of each output a wave and turn (a lane 64
 // of them in four loads).  Factors go from memory to the matrix cores as they are:
@@ -466,7 +650,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) linear_few_kernel(LinearArgs a
 #pragma unroll
         for (int v = 0; v < kFewWaves; ++v) total += sums[v][m >> 4][m & 15][n];
         float o = (float)total * a.x_scale[m] * a.w_scale[n0 + n] + (a.bias ? a.bias[n0 + n] : 0.0f);
-        if (a.gelu) o = gelu(o);
+        if (a.gelu) o = gelu<T>(o);
         static_cast<T *>(a.y)[m * a.y_stride + n0 + n] = static_cast<T>(o);
     }
 }
@@ -499,6 +683,36 @@ hipError_t launch_tiles(const LinearArgs &a, int per_cu, int n_cus, hipStream_t 
     });
 }
 
+// Workgroups that keep their weights, one a compute unit and an eighth of them on each XCD;
+// 0 where tiles of 128 x 128 are as fast.  128000 rows of 512 to 1536 outputs 170 -> 137 us,
+// to 2048 237 -> 191, with gelu 355 -> 305; 8 waves a compute unit beside each other make
+// those tiles, 12 here, and they copy rows to LDS for every 128 outputs.
+// - Narrower rows leave factors empty: 256 wide 148 -> 158 us, 320 188 -> 166.
+// - Workgroups that outputs do not divide among have nothing.
+// - With fewer than two turns a wave loading the weights is not paid back: 16000 rows
+//   to 2048 29 -> 34 us, 25000 46 -> 39.
+// - Rows of outputs that begin inside 64 bytes are written in parts (pitch 1544: 180 -> 301 us).
+template <typename T>
+int64_t stay_workgroups(const LinearArgs &a, int n_cus) {
+    const int64_t per_xcd = n_cus / 8, columns = (a.outputs + kStayOutputs - 1) / kStayOutputs;
+    if (a.width <= kStayWidth / 2 || a.width > kStayWidth || columns > per_xcd) return 0;
+    if (a.x_stride >= 1 << 24 || a.y_stride >= 1 << 24) return 0;  // (places in 32 bits)
+    if (a.y_stride * sizeof(T) % 64 != 0 || reinterpret_cast<uintptr_t>(a.y) % 64 != 0) return 0;
+    const int64_t groups = per_xcd / columns;
+    if (8 * groups * columns < 7 * per_xcd) return 0;
+    if (a.rows < 32 * 8 * groups * kStayWaves * 2) return 0;
+    return 8 * per_xcd;
+}
+
+template <typename T>
+hipError_t launch_stay(LinearArgs a, int64_t workgroups, hipStream_t stream) {
+    a.column_tiles = (a.outputs + kStayOutputs - 1) / kStayOutputs;
+    a.tiles = (a.rows + 31) / 32;
+    if (a.gelu) hipLaunchKernelGGL((linear_stay_kernel<T, true>), dim3((uint32_t)workgroups), dim3(64 * kStayWaves), 0, stream, a);
+    else hipLaunchKernelGGL((linear_stay_kernel<T, false>), dim3((uint32_t)workgroups), dim3(64 * kStayWaves), 0, stream, a);
+    return hipGetLastError();
+}
+
 template <typename T, int MT>
 hipError_t launch_few(const LinearArgs &a, hipStream_t stream) {
     hipLaunchKernelGGL((linear_few_kernel<T, MT>), dim3((a.outputs + 15) / 16), dim3(64 * kFewWaves), 0, stream, a);
@@ -517,6 +731,8 @@ hipError_t launch_linear(LinearArgs a, int32_t dtype, int n_cus, hipStream_t str
             return by_tiles<T, 64, 64>(a, [&](const LinearArgs &part) {
                 hipLaunchKernelGGL((linear_any_kernel<T>), dim3((uint32_t)part.tiles), dim3(kThreads), 0, stream, part);
             });
+        if constexpr (sizeof(T) == 2)
+            if (const int64_t workgroups = stay_workgroups<T>(a, n_cus)) return launch_stay<T>(a, workgroups, stream);
         const int64_t tiles = (a.rows + 127) / 128 * ((a.outputs + 127) / 128);
         if (tiles < 2 * (int64_t)n_cus) return launch_tiles<T, 64, 64>(a, 4, n_cus, stream);
         return launch_tiles<T, 128, 128>(a, 2, n_cus, stream);
