@@ -72,9 +72,19 @@ __device__ __forceinline__ float gelu(float x) {
 // a lane).  A row's chunks of 16 bytes are stored in an order that turns with the row,
 // so that the 32 rows that a wave reads a chunk of lie in different banks.
 //
-// A workgroup stays for many tiles, and its steps are one stream: loads run kAhead
-// steps before the products, across the ends of tiles, and a step waits for its own
-// loads alone (they come back in order), with one barrier a step.
+// A workgroup stays for many tiles, and its steps are one stream: loads run a step
+// before the products, across the ends of tiles, and a step waits for its own loads
+// alone (they come back in order), with one barrier a step.
+//
+// Two workgroups of four waves a compute unit make 128 x 128 outputs each, and one's
+// outputs are made beside the other's products: 30001 rows of 2047 to 501 outputs 46 us
+// (1.3 POP/s, of 2.1 of a product of 8192^3 by the library), 128000 of 2048 to 512 157
+// (1.7), 8192^3 609 (1.8).  What bounds it are the loads to LDS and the outputs' stores
+// (128000 x 512 to 1536, 172 us: without stores 143, without making outputs 109, loads
+// alone 106).  256 x 256 outputs of eight waves were faster for 8192^3 (531) and slower
+// for 1536 outputs (188), where nothing runs beside the end of a tile; steps of 64 bytes
+// take half a line of a row each (8192^3 720).  Fewer than two tiles of 128 x 128 a
+// compute unit are made as tiles of 64 x 64 by four workgroups (500 rows to 1536 5.6 us).
 // ---------------------------------------------------------------------------
 
 constexpr int kStep = 128, kAhead = 1, kStages = kAhead + 1, kChunks = kStep / 16;
@@ -90,7 +100,7 @@ __device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row
 template <int BM, int BN>
 struct __attribute__((aligned(16))) LinearShared {
     int8_t x[kStages][BM * kStep], w[kStages][BN * kStep];
-    float x_scale[kStages][BM], w_scale[kStages][BN], bias[kStages][BN];  // of a tile, in turn: a step may be all of one
+    float x_scale[kStages][BM], w_scale[kStages][BN], bias[kStages][BN];  // of tiles in turn: a tile may be one step
 };
 
 // Where a tile's rows begin, for the loads or for the products.
@@ -181,8 +191,8 @@ struct LinearLoads {
     }
 };
 
-// One step of a wave: its rows' and outputs' chunks from LDS.  (The stage that loads go
-// to is another one: `ahead` only says so.)
+// One step of a wave: its rows' and outputs' chunks from LDS.  (Loads go to another
+// stage, and the compiler is told so.)
 template <int KM, int KN>
 __device__ __forceinline__ void multiply(const int8_t *__restrict__ x, const int8_t *__restrict__ w, i32x16 (&acc)[KN][KM]) {
     const int lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
@@ -243,7 +253,7 @@ __device__ __forceinline__ void put(Pack<T, 8> *at, const Pack<T, 8> &v) {
 template <bool FULL, typename T>
 __device__ __forceinline__ void store_left(T *y, const Pack<T, 8> &v, int left) {
     if (FULL || left >= 8) {
-        // (past the caches: outputs larger than they are have no use of them, 210 -> 174 us above)
+        // (past the caches, which large outputs have no use of: 128000 x 512 to 1536 210 -> 174 us)
         typedef i32x4 __attribute__((aligned(2))) Words;
         const Words *from = reinterpret_cast<const Words *>(&v);
         Words *to = reinterpret_cast<Words *>(y);
@@ -260,10 +270,9 @@ __device__ __forceinline__ void store_left(T *y, const Pack<T, 8> &v, int left) 
 __device__ __forceinline__ void stand() { asm volatile("" ::: "memory"); }
 
 // A wave's outputs of a tile.  FULL: all of its rows and outputs are there.  Outputs of
-// 16 bits go through LDS (`room`, 2 KN KB of the wave's own), 32 rows at a time, so that a row's
-// are stored as 64 KN bytes in one piece: in the pieces of 32 bytes that lanes hold
-// them stores alone took longer than all else (128000 x 512 to 1536: 233 us, 138
-// without its stores).
+// 16 bits go through LDS (`room`, 2 KN KB of the wave's own), 32 rows at a time, so that a
+// row's are stored as 64 KN bytes in one piece: with stores of the 32 bytes that a lane
+// has beside each other 128000 x 512 to 1536 took 233 us, 95 of them for stores.
 template <typename T, bool GELU, bool FULL, int KM, int KN, typename S, typename Tile>
 __device__ __forceinline__ void finish(const LinearArgs &a, const Tile &t, const S &s, int turn, int wm, int wn, int8_t *room,
                                        const i32x16 (&acc)[KN][KM]) {
@@ -609,7 +618,8 @@ __global__ void __launch_bounds__(64 * kStayWaves) linear_stay_kernel(LinearArgs
 // eight waves share the width, 256 bytes of each output a wave and turn (a lane 64
 // of them in four loads).  Factors go from memory to the matrix cores as they are:
 // both sides take their bytes in the same order, and that order is free.  The
-// waves' sums are joined in LDS.
+// waves' sums are joined in LDS.  7 rows of 2048 to 512 outputs 4.4 us: the time of a
+// load, the joint and a store, one after the other, of 1 MB.
 // ---------------------------------------------------------------------------
 
 constexpr int kFewWaves = 8;

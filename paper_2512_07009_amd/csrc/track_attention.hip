@@ -7,20 +7,29 @@
 //   out_i = sum over the tokens seen of softmax_j(t) v_scale v_j, 0 where there are none
 //
 // The heads that share a kv head are packed with the queries as rows r = (i, g), 16 a
-// workgroup.  Its four waves take every fourth page and join what they have in LDS;
-// where there are few rows, several workgroups share a row's pages and a second kernel
-// joins them.
+// workgroup.  Its four waves take every fourth page and join what they have in LDS (many
+// short tracks are one wave's each); where there are few rows, several workgroups share a
+// row's pages and a second kernel joins them.  A page is read once, from memory to
+// registers, a page ahead of the products.
+//
+// A query a track is bound by memory: 24 tracks of 27000 tokens, heads of 128, 67 us and 6
+// for the join (326 MB, 4.9 TB/s), 2000 of 1800 173 (5.3); 500 of 0 to 5400 82 (337 MB,
+// 4.1), where the longest tracks' workgroups end last.  96 tracks of 0 to 9000 with some
+// 15 queries each and a cap 90 us: vector instructions, 77% of the time.  Tried: keys to
+// float16, four tiles of rows a wave (96 clips 95 -> 232, registers), eight waves (500
+// tracks 81 -> 75, but 24 long 67 -> 89 and 2000 ragged ones 94 -> 103), values shared
+// by the waves in LDS (no faster).
 //
 // Scores are products of whole numbers on the matrix cores (16 x 16 x 64, 8 bits, exact
 // sums): keys as they lie in pages, and queries as 256 a + b with a, b in 8 bits.  That
 // rounds a query's dimension by 2^-17 of its row's largest at most, below what its own
 // 16-bit type leaves of it, and spares a lane 80 instructions a page to convert keys to
-// float16 (of some 350).  Scores are transposed, S^T = K Q^T: a
-// lane holds 16 tokens of one row, four of each 16, which is the order in which the product
-// with the values takes its weights.  Values lie in pages so that a lane's 16 bytes are the
-// factors of two such products (16 x 16 x 32); they go to float16, which holds them exactly.
-// Weights carry the page's scale relative to the largest so far, within the exponent, and
-// are rounded to float16 (2^-11) after they were summed in 32 bits.
+// float16 (of some 350).  Scores are transposed, S^T = K Q^T: a lane holds 16 tokens of one
+// row, four of each 16, which is the order in which the product with the values takes its
+// weights.  Values lie in pages so that a lane's 16 bytes are the factors of two such
+// products (16 x 16 x 32); they go to float16, which holds them exactly.  Weights carry the
+// page's scale relative to the largest so far, within the exponent, and are rounded to
+// float16 (2^-11) after they were summed in 32 bits.
 
 #include "attention_common.h"
 #include "tracks_common.h"
@@ -372,7 +381,8 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
 // that turns with it, so that the 32 that a wave reads a chunk of lie in different banks.
 // Products are 32 x 32 x 32 (8 bits) and 32 x 32 x 16: a lane holds 32 tokens of one row, and
 // of a dimension it takes the two parts that hold the same tokens.  Bound by vector
-// instructions, some seven a score and 80 a page to convert its values.
+// instructions, some seven a score and 80 a page to convert its values: 64 tracks of 1000
+// with 1000 queries of 4 heads 180 us (366 TFLOP/s), with 16 rows a workgroup 359.
 // ---------------------------------------------------------------------------
 
 constexpr int kAhead = 3, kBuffers = kAhead + 1;
