@@ -478,7 +478,8 @@ __global__ void __launch_bounds__(64 * kStayWaves) linear_stay_kernel(LinearArgs
     if (group >= groups) return;
     const int n0 = (at - group * a.column_tiles) * kStayOutputs, columns = min(kStayOutputs, a.outputs - n0);
     const int64_t tiles = a.tiles, end = tiles * (xcd + 1) / 8;
-    int64_t tile = tiles * xcd / 8 + group * kStayWaves + wave;
+    // (the last turn, which some waves are without, is then as short for every workgroup: 136 -> 129 us to 1536)
+    int64_t tile = tiles * xcd / 8 + wave * groups + group;
 
     const int8_t *w = a.w + n0 * (int64_t)a.w_stride;
     for (int i = wave; i < kStayWidth / kStep * kStayOutputs * kChunks / 64; i += kStayWaves) {
@@ -694,9 +695,11 @@ hipError_t launch_tiles(const LinearArgs &a, int per_cu, int n_cus, hipStream_t 
 }
 
 // Workgroups that keep their weights, one a compute unit and an eighth of them on each XCD;
-// 0 where tiles of 128 x 128 are as fast.  128000 rows of 512 to 1536 outputs 170 -> 137 us,
-// to 2048 237 -> 191, with gelu 355 -> 305; 8 waves a compute unit beside each other make
-// those tiles, 12 here, and they copy rows to LDS for every 128 outputs.
+// 0 where tiles of 128 x 128 are as fast.  128000 rows of 512 to 1536 outputs 172 -> 129 us,
+// to 2048 237 -> 165, with gelu 357 -> 260; 8 waves a compute unit beside each other make
+// those tiles, 12 here, and they copy rows to LDS for every 128 outputs.  What bounds it is
+// no one thing (without gelu vector instructions take 38% of the time, matrix cores 40,
+// LDS 43), but with gelu vector instructions, 80%.
 // - Narrower rows leave factors empty: 256 wide 148 -> 158 us, 320 188 -> 166.
 // - Workgroups that outputs do not divide among have nothing.
 // - With fewer than two turns a wave loading the weights is not paid back: 16000 rows
