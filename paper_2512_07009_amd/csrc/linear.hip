@@ -78,13 +78,11 @@ __device__ __forceinline__ float gelu(float x) {
 //
 // Two workgroups of four waves a compute unit make 128 x 128 outputs each, and one's
 // outputs are made beside the other's products: 30001 rows of 2047 to 501 outputs 46 us
-// (1.3 POP/s, of 2.1 of a product of 8192^3 by the library), 128000 of 2048 to 512 157
-// (1.7), 8192^3 609 (1.8).  What bounds it are the loads to LDS and the outputs' stores
-// (128000 x 512 to 1536, 172 us: without stores 143, without making outputs 109, loads
-// alone 106).  256 x 256 outputs of eight waves were faster for 8192^3 (531) and slower
-// for 1536 outputs (188), where nothing runs beside the end of a tile; steps of 64 bytes
-// take half a line of a row each (8192^3 720).  Fewer than two tiles of 128 x 128 a
-// compute unit are made as tiles of 64 x 64 by four workgroups (500 rows to 1536 5.6 us).
+// (1.3 POP/s, of 2.1 of a product of 8192^3 by the library).  What bounds it are the loads
+// to LDS and the outputs' stores (128000 x 512 to 1536, 172 us: without stores 143,
+// without making outputs 109, loads alone 106); steps of 64 bytes take half a line of a
+// row each (8192^3 609 -> 720 us).  Fewer than two tiles of 128 x 128 a compute unit are
+// made as tiles of 64 x 64 by four workgroups (500 rows to 1536 5.6 us).
 // ---------------------------------------------------------------------------
 
 constexpr int kStep = 128, kAhead = 1, kStages = kAhead + 1, kChunks = kStep / 16;
@@ -118,16 +116,17 @@ struct LinearTile {
 };
 
 // The loads' side of the stream.
-template <int BM, int BN>
+template <int BM, int BN, int THREADS = 256>
 struct LinearLoads {
-    static constexpr int kX = BM * kChunks / kThreads, kW = BN * kChunks / kThreads, kLoads = kX + kW;
+    static constexpr int kThreads = THREADS, kX = BM * kChunks / THREADS, kW = BN * kChunks / THREADS, kLoads = kX + kW;
     const int8_t *x, *w;          // the tile's first rows
     uint32_t x_at[kX], w_at[kW];  // the lane's chunks, from them
     int wave;
 
     __device__ __forceinline__ LinearLoads() { wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
-    __device__ __forceinline__ void begin(const LinearArgs &a, uint32_t tile, int turn, LinearShared<BM, BN> &s) {
+    template <typename S>
+    __device__ __forceinline__ void begin(const LinearArgs &a, uint32_t tile, int turn, S &s) {
         const LinearTile<BM, BN> t(a, tile);
         x = a.x + t.m0 * a.x_stride;
         w = a.w + t.n0 * a.w_stride;
@@ -447,6 +446,192 @@ __global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
     else finish<T, false, false>(a, t, s, 0, wm, wn, room, acc);
 }
 
+// Outputs of 16 bits of a wave's 32 rows, 64 of each, by way of LDS (`room`, 2 KB of the
+// wave's own), 16 rows at a time, in pieces of 128 bytes.  FULL: all of them are there, of
+// others the first `rows` and `here`.  Places in LDS are made here, not kept: registers
+// are full where this is called.
+template <bool FULL, bool GELU, typename T>
+__device__ __forceinline__ void make_64(T *y, int64_t y_stride, int rows, int here, Pack<T, 8> *room, const float *w_scale,
+                                        const float *bias, float scale, const i32x16 &first, const i32x16 &second) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int h = lane >> 5, col = lane & 31;
+    const auto part_at = [](int row, int part) { return row * 8 + (part ^ (row & 7)); };
+    Pack<T, 8> out[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int at = 16 * u + 4 * h + (e & 3) + 8 * (e >> 2);
+            o[e] = (float)(u < 2 ? first : second)[8 * (u & 1) + e] * scale * w_scale[at] + bias[at];
+            if (GELU) o[e] = gelu<T>(o[e]);
+        }
+        out[u] = side_by_side<T>(o);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        stand();
+        if (col >> 4 == half) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) put(room + part_at(col & 15, 2 * u + h), out[u]);
+        }
+        stand();
+        if (FULL) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int row = lane / 8, part = lane & 7;
+                store_left<true>(y + (16 * half + 8 * v) * y_stride + ((uint32_t)row * (uint32_t)y_stride + 8 * part),
+                                 room[part_at(8 * v + row, part)], 8);
+            }
+        } else if (lane < here) {
+#pragma unroll 1
+            for (int row = 0; row < min(16, rows - 16 * half); ++row)
+                y[(16 * half + row) * y_stride + lane] = room[part_at(row, lane / 8)].v[lane & 7];
+        }
+    }
+    stand();
+}
+
+// ---------------------------------------------------------------------------
+// Many rows: 256 x 256 outputs a workgroup of eight waves, 64 x 128 a wave.
+//
+// The same steps and loads as above, with half the bytes to LDS and three quarters of
+// those from it for a product, and nothing beside the workgroup on its compute unit, so
+// that a wave reads the next factors from LDS under the products of these, the next
+// step's first ones too: the barrier is before a step's last products, when all of its
+// factors have been read.  8192^3 567 us (1.9 POP/s), 128000 rows of 2048 to 512 150
+// (1.8), without that 600 and 152.
+// ---------------------------------------------------------------------------
+
+constexpr int kWide = 256, kWideThreads = 512;
+
+struct __attribute__((aligned(16))) WideShared {
+    int8_t x[2][kWide * kStep], w[2][kWide * kStep];
+    float x_scale[2][kWide], w_scale[2][kWide], bias[2][kWide];  // of tiles in turn (a tile is two steps or more)
+    int8_t room[kWideThreads / 64][16 * 64 * 2];
+};
+
+template <typename T, bool GELU>
+__global__ void __launch_bounds__(kWideThreads, 2) linear_wide_kernel(LinearArgs a) {
+    using Loads = LinearLoads<kWide, kWide, kWideThreads>;
+    constexpr int kMT = 2, kNT = 4, kParts = kStep / 32;
+    __shared__ WideShared s;
+
+    const uint32_t tiles = a.tiles, id = blockIdx.x, per = tiles / 8;
+    uint32_t tile, end, beside = 1;
+    if (tiles <= gridDim.x) {  // one each, an eighth of all beside each other on each XCD
+        tile = id < per * 8 ? (id & 7) * per + (id >> 3) : id;
+        end = tile + 1;
+    } else {
+        const uint32_t xcd = id & 7;
+        beside = gridDim.x >> 3;
+        tile = tiles * xcd / 8 + (id >> 3);
+        end = tiles * (xcd + 1) / 8;
+        if (tile >= end) return;
+    }
+    const int steps = (a.width + kStep - 1) / kStep;
+    int64_t left = (int64_t)((end - tile - 1) / beside + 1) * steps;  // steps to multiply
+
+    Loads loads;
+    uint32_t next_tile = tile;
+    int next_step = 0, next_turn = 0, next_stage = 0;
+    const auto load = [&] {
+        if (next_tile >= end) return;
+        if (next_step == 0) loads.begin(a, next_tile, next_turn, s);
+        loads.step(next_step * kStep, a.width, s.x[next_stage], s.w[next_stage]);
+        next_stage ^= 1;
+        if (++next_step == steps) {
+            next_step = 0;
+            next_tile += beside;
+            next_turn ^= 1;
+        }
+    };
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, col = lane & 31;
+    const int wm = (wave & 3) * 64, wn = (wave >> 2) * 128;
+    i32x4 wf[2][kNT], xf[2][kMT];
+    const auto read = [&](int to, int stage, int k) {
+        const int chunk = 16 * turned(col, 2 * k + h) + col * kStep;
+#pragma unroll
+        for (int i = 0; i < kNT; ++i) wf[to][i] = *reinterpret_cast<const i32x4 *>(s.w[stage] + (wn + 32 * i) * kStep + chunk);
+#pragma unroll
+        for (int j = 0; j < kMT; ++j) xf[to][j] = *reinterpret_cast<const i32x4 *>(s.x[stage] + (wm + 32 * j) * kStep + chunk);
+    };
+    const auto arrive = [&](int stage, bool last) {  // the waits are the caller's
+        stand();
+        if (a.width % 16 && last) {
+            loads.mask((steps - 1) * kStep, a.width, s.w[stage]);
+            stand();
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS)
+        }
+        __builtin_amdgcn_s_barrier();
+        stand();
+    };
+
+    load();
+    wait_but<0>();
+    arrive(0, false);
+    load();
+    read(0, 0, 0);
+    constexpr int kStores = 16;  // of a whole tile, a wave
+    int stage = 0, turn = 0, since = 1;
+    for (; tile < end; tile += beside, turn ^= 1) {
+        i32x16 acc[kNT][kMT] = {};
+        const auto multiply = [&](int from) {
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kNT; ++i)
+#pragma unroll
+                for (int j = 0; j < kMT; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[from][i], xf[from][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int t = 0; t < steps; ++t) {
+#pragma unroll
+            for (int k = 0; k + 1 < kParts; ++k) {
+                read((k + 1) & 1, stage, k + 1);
+                multiply(k & 1);
+            }
+            if (--left > 0) {
+                // the next step's loads (a whole tile's stores came after them, in a tile's first step)
+                stand();
+                if (since == 0) wait_but<kStores>();
+                else wait_but<0>();
+                ++since;
+                arrive(stage ^ 1, (t + 1 == steps ? 0 : t + 1) == steps - 1);
+                load();
+                read(0, stage ^ 1, 0);
+            }
+            multiply((kParts - 1) & 1);
+            stage ^= 1;
+        }
+        const LinearTile<kWide, kWide> at(a, tile);
+        Pack<T, 8> *room = reinterpret_cast<Pack<T, 8> *>(s.room[wave]);
+        const auto finish = [&](auto full) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < kMT; ++j)
+#pragma unroll
+                for (int i = 0; i < kNT; i += 2) {
+                    const int m = wm + 32 * j, n = wn + 32 * i, rows = at.rows - m, here = at.columns - n;
+                    const auto make = [&](auto all) __attribute__((always_inline)) {
+                        make_64<decltype(all)::value, GELU>(static_cast<T *>(a.y) + (at.m0 + m) * a.y_stride + at.n0 + n,
+                                                            a.y_stride, rows, here, room, s.w_scale[turn] + n, s.bias[turn] + n,
+                                                            s.x_scale[turn][m + col], acc[i][j], acc[i + 1][j]);
+                    };
+                    if (decltype(full)::value || (rows >= 32 && here >= 64)) make(std::true_type{});
+                    else if (rows > 0 && here > 0) make(std::false_type{});
+                }
+        };
+        if (at.rows == kWide && at.columns == kWide) {
+            finish(std::true_type{});
+            since = 0;
+        } else {
+            finish(std::false_type{});
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------
 // Very many rows of a width that fits: the weights stay.
 //
@@ -513,55 +698,16 @@ __global__ void __launch_bounds__(64 * kStayWaves) linear_stay_kernel(LinearArgs
         for (int k = half * kParts / 2; k < (half + 1) * kParts / 2; ++k)
             x[k] = *reinterpret_cast<const i32x4 *>(from + (32 * k < a.width ? 32 * k : 0) + (32 * k + 16 < a.width ? at : first));
     };
-    const auto part_at = [](int row, int part) { return row * 8 + (part ^ (row & 7)); };
     Pack<T, 8> *room = reinterpret_cast<Pack<T, 8> *>(s.room[wave]);
-    // outputs of two blocks, by way of LDS
-    const auto make = [&](auto full, int n1, auto block, int64_t row0, const i32x16 (&acc)[kBlocks], float scale) {
+    const auto make = [&](auto full, int n1, auto block, int64_t row0, const i32x16 (&acc)[kBlocks], float scale) __attribute__((always_inline)) {
         constexpr int i = decltype(block)::value;
-        int lane = threadIdx.x & 63;
-        asm volatile("" : "+v"(lane));  // (places in LDS are made here, not kept)
-        const int h = lane >> 5, col = lane & 31;
-        const int rows = (int)min((int64_t)32, a.rows - row0), here = min(columns - n1 - 32 * i, 64);
-        T *y = static_cast<T *>(a.y) + row0 * a.y_stride + n0 + n1 + 32 * i;
-        Pack<T, 8> out[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int n = n1 + 32 * i + 16 * u + 4 * h;
-            float o[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const int at = n + (e & 3) + 8 * (e >> 2);
-                o[e] = (float)acc[i + u / 2][8 * (u & 1) + e] * scale * s.w_scale[at] + s.bias[at];
-                if (GELU) o[e] = gelu<T>(o[e]);
-            }
-            out[u] = side_by_side<T>(o);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            stand();
-            if (col >> 4 == half) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) put(room + part_at(col & 15, 2 * u + h), out[u]);
-            }
-            stand();
-            if (decltype(full)::value) {
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    const int row = lane / 8, part = lane & 7;
-                    store_left<true>(y + (16 * half + 8 * v) * a.y_stride + ((uint32_t)row * (uint32_t)a.y_stride + 8 * part),
-                                     room[part_at(8 * v + row, part)], 8);
-                }
-            } else if (lane < here) {
-#pragma unroll 1
-                for (int row = 0; row < min(16, rows - 16 * half); ++row)
-                    y[(16 * half + row) * a.y_stride + lane] = room[part_at(row, lane / 8)].v[lane & 7];
-            }
-        }
-        stand();
+        const int n = n1 + 32 * i;
+        make_64<decltype(full)::value, GELU>(static_cast<T *>(a.y) + row0 * a.y_stride + n0 + n, a.y_stride,
+                                             (int)min((int64_t)32, a.rows - row0), columns - n, room, s.w_scale + n,
+                                             s.bias + n, scale, acc[i], acc[i + 1]);
     };
 
-    const auto multiply = [&](int half, i32x16 (&acc)[kBlocks]) {
+    const auto multiply = [&](int half, i32x16 (&acc)[kBlocks]) __attribute__((always_inline)) {
         int lane = threadIdx.x & 63;
         asm volatile("" : "+v"(lane));
         const int h = lane >> 5, col = lane & 31;
@@ -582,7 +728,7 @@ __global__ void __launch_bounds__(64 * kStayWaves) linear_stay_kernel(LinearArgs
     constexpr std::integral_constant<int, 2> kSecond;
     // rows up to a tile, all of whose rows and outputs are there where FULL; nothing branches
     // there, so that a wait for rows is for those alone and not for stores
-    const auto go = [&](auto full, int64_t last) {
+    const auto go = [&](auto full, int64_t last) __attribute__((always_inline)) {
         while (tile < last) {
             const int64_t row0 = tile * 32;
             const float scale = xs;
@@ -694,6 +840,12 @@ hipError_t launch_tiles(const LinearArgs &a, int per_cu, int n_cus, hipStream_t 
     });
 }
 
+// Whether outputs of `y` begin at a multiple of 64 bytes, each row of them.
+template <typename T>
+bool whole_lines(const LinearArgs &a) {
+    return a.y_stride * sizeof(T) % 64 == 0 && reinterpret_cast<uintptr_t>(a.y) % 64 == 0;
+}
+
 // Workgroups that keep their weights, one a compute unit and an eighth of them on each XCD;
 // 0 where tiles of 128 x 128 are as fast.  128000 rows of 512 to 1536 outputs 172 -> 129 us,
 // to 2048 237 -> 165, with gelu 357 -> 260; 8 waves a compute unit beside each other make
@@ -710,11 +862,36 @@ int64_t stay_workgroups(const LinearArgs &a, int n_cus) {
     const int64_t per_xcd = n_cus / 8, columns = (a.outputs + kStayOutputs - 1) / kStayOutputs;
     if (a.width <= kStayWidth / 2 || a.width > kStayWidth || columns > per_xcd) return 0;
     if (a.x_stride >= 1 << 24 || a.y_stride >= 1 << 24) return 0;  // (places in 32 bits)
-    if (a.y_stride * sizeof(T) % 64 != 0 || reinterpret_cast<uintptr_t>(a.y) % 64 != 0) return 0;
+    if (!whole_lines<T>(a)) return 0;
     const int64_t groups = per_xcd / columns;
     if (8 * groups * columns < 7 * per_xcd) return 0;
     if (a.rows < 32 * 8 * groups * kStayWaves * 2) return 0;
     return 8 * per_xcd;
+}
+
+// Whether tiles of 256 x 256 are faster than those of 128 x 128, two of which a compute unit
+// makes at a time: by a tenth for the same outputs a compute unit (128000 x 2048 to 512 162
+// -> 150 us, 30000 41 -> 38), so not where they do not share them as evenly (40000 52 -> 66).
+// Outputs that begin inside 64 bytes are written in parts (30001 x 2047 to 501 47 -> 51),
+// and narrow rows are bound by their outputs (300000 x 128 to 512 65 -> 66).
+template <typename T>
+bool wide_tiles(const LinearArgs &a, int n_cus) {
+    const auto turns = [&](int64_t size, int64_t beside) {
+        const int64_t tiles = (a.rows + size - 1) / size * ((a.outputs + size - 1) / size);
+        return (tiles + beside - 1) / beside;
+    };
+    return a.width >= 2 * kStep && a.y_stride < 1 << 24 && whole_lines<T>(a) &&
+           9 * 4 * turns(kWide, n_cus) <= 10 * 2 * turns(128, 2 * n_cus);
+}
+
+template <typename T>
+hipError_t launch_wide(const LinearArgs &a, int n_cus, hipStream_t stream) {
+    const int64_t workgroups = std::max(n_cus / 8 * 8, 8);
+    return by_tiles<T, kWide, kWide>(a, [&](const LinearArgs &part) {
+        const dim3 grid((uint32_t)std::min(part.tiles, workgroups)), block(kWideThreads);
+        if (a.gelu) hipLaunchKernelGGL((linear_wide_kernel<T, true>), grid, block, 0, stream, part);
+        else hipLaunchKernelGGL((linear_wide_kernel<T, false>), grid, block, 0, stream, part);
+    });
 }
 
 template <typename T>
@@ -746,6 +923,8 @@ hipError_t launch_linear(LinearArgs a, int32_t dtype, int n_cus, hipStream_t str
             });
         if constexpr (sizeof(T) == 2)
             if (const int64_t workgroups = stay_workgroups<T>(a, n_cus)) return launch_stay<T>(a, workgroups, stream);
+        if constexpr (sizeof(T) == 2)
+            if (wide_tiles<T>(a, n_cus)) return launch_wide<T>(a, n_cus, stream);
         const int64_t tiles = (a.rows + 127) / 128 * ((a.outputs + 127) / 128);
         if (tiles < 2 * (int64_t)n_cus) return launch_tiles<T, 64, 64>(a, 4, n_cus, stream);
         return launch_tiles<T, 128, 128>(a, 2, n_cus, stream);

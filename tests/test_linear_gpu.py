@@ -171,6 +171,32 @@ def test_gelu_of_what_is_not_finite(rows, dtype):
 
 @pytest.mark.parametrize("gelu", [False, True])
 @pytest.mark.parametrize("rows,width,outputs,dtype", [
+    (7936, 768, 2048, torch.bfloat16),   # whole tiles, one each
+    (7901, 300, 2016, torch.float16),    # rows, outputs and a width that end inside a tile, a step and a chunk
+    (16301, 256, 2016, torch.bfloat16),  # two tiles each, of two steps
+    (24000, 1001, 2048, torch.float16),  # three, of eight
+    (29001, 577, 480, torch.bfloat16),
+])
+def test_tiles_of_256(rows, width, outputs, dtype, gelu):
+    c = case(19, rows, width, outputs)
+    compare(c, dtype, gelu=gelu, x=padded(c["x"], (width + 15) // 16 * 16), w=padded(c["w"], (width + 15) // 16 * 16))
+
+
+def test_tiles_of_256_leave_what_is_beside_them():
+    """Outputs in rows of a wider tensor, and the tensor's other elements as they were."""
+    c = case(20, 7700, 640, 1952)
+    wide = torch.full((7702, 1952 + 96), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = wide[1:-1, 32:-64]
+    d = {n: (t.cuda() if t is not None else None) for n, t in c.items()}
+    flock.linear_rows_i8(d["x"], d["xs"], d["w"], d["ws"], d["bias"], out=out)
+    want = flock.linear_rows_i8(d["x"], d["xs"], d["w"], d["ws"], d["bias"], dtype=torch.float32).bfloat16()
+    assert torch.equal(out, want)
+    wide[1:-1, 32:-64] = 7.0
+    assert (wide == 7.0).all()
+
+
+@pytest.mark.parametrize("gelu", [False, True])
+@pytest.mark.parametrize("rows,width,outputs,dtype", [
     (6144, 512, 8192, torch.bfloat16),       # whole turns of whole tiles
     (6400 + 31, 272, 7520, torch.float16),   # outputs and rows that end inside a tile, a width inside a chunk pair
     (12400, 509, 3584 + 512, torch.bfloat16),
