@@ -750,9 +750,11 @@ TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_page
     p.slots = (int64_t)total * group / p.tile_rows + n_tracks;
     // as many workgroups as the card holds at a time, of at least two pages a wave: with
     // more of them some begin when others end (24 tracks of 27000, heads of 128: two a
-    // compute unit 68 us, four 77, eight 88)
+    // compute unit 68 us, four 77, eight 88); three where a tile's rows are at least half there
+    // and instructions are what takes the time (256 tracks of 4000, 16 heads of 128 that share
+    // one: two 68 us, three 52, four 83; 96 of 0 to 9000 with 5 queries of 4 heads 50, 45, 50)
     const int64_t items = std::max<int64_t>(n_tracks, (int64_t)total * group / p.tile_rows) * kv_heads;
-    const int resident = many ? 3 : 2;
+    const int resident = many || rows >= kRows / 2 * (int64_t)n_tracks ? 3 : 2;
     // one wave a workgroup where short tracks fill the card so (4096 of 64 tokens 48 -> 22 us, of 256
     // 68 -> 49; of 1024 196 -> 204, 2000 of up to 1800 94 -> 110)
     p.waves = !many && max_pages <= 8 && items >= 12 * (int64_t)n_cus ? 1 : kWaves;
