@@ -154,6 +154,28 @@ def test_captured_and_replayed():
         assert torch.equal(a[used], b[used])
 
 
+def test_steps_without_detections():
+    """A frame in which no bird is seen, and frames in which some tracks have none, leave the others as they are."""
+    counts = [70, 50]
+    block = block_of(21)
+    x, xy, time, _ = tracks(22, counts, 128)
+    served = encoder.ServedBlock(block)
+    table, pages = pages_of(counts)
+    want = serve(served, served.cache(pages), x, xy, time, counts, table, 10)
+    cache, out = served.cache(pages), torch.empty_like(x)
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    for first in range(0, 70, 10):
+        seen = [0, 0]
+        for i, start in enumerate((0, 70)):       # one track's detections a call, the other has none
+            rows = torch.arange(start + min(first, counts[i]), start + min(first + 10, counts[i]), device="cuda")
+            seen = [min(first + (10 if j <= i else 0), counts[j]) for j in range(2)]
+            offsets = int32([0, len(rows), len(rows)] if i == 0 else [0, 0, len(rows)])
+            out[rows] = served(x[rows], cache, offsets, table, int32(seen), xy[rows], time[rows])
+            empty = served(x[none], cache, int32([0, 0, 0]), table, int32(seen), xy[none], time[none])
+            assert empty.shape == (0, 128)
+    assert torch.equal(out, want)
+
+
 def test_two_streams_with_caches_of_their_own():
     counts = [3000] * 6
     block = block_of(9)

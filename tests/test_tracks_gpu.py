@@ -340,6 +340,45 @@ def test_attention_leaves_rows_of_no_track():
     assert (out[9:] == 7).all()
 
 
+def test_attention_of_pages_that_tracks_share():
+    """Two tracks that begin alike read the same pages, one page of a track twice too."""
+    def share(table, c):
+        table[1, :3] = table[0, :3]
+        table[2, 4] = table[2, 1]
+    for queries in ([1, 1, 1], [40, 3, 60], [300, 250, 200]):
+        attend(60, [500, 430, 700], queries, spoil=share)
+
+
+@pytest.mark.parametrize("window", [0, 2000])
+def test_attention_in_two_graphs(window):
+    """Two captured calls that share their pages among workgroups, replayed in turn and beside each other."""
+    lengths, queries = [9000, 4000], [1, 2]
+    gen = torch.Generator().manual_seed(61)
+    pages = sum((n + PAGE - 1) // PAGE for n in lengths)
+    c, table = cuda(pool(gen, pages, 2, 64)), table_of(gen, lengths, pages).cuda()
+    offsets, n = int32(offsets_of(queries)), int32(lengths)
+    qs = [torch.randn(3, 8, 64, generator=gen).bfloat16().cuda() for _ in range(2)]
+    want = [flock.attention_tracks(q, c, offsets, table, n, window=window) for q in qs]
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in qs]
+    for q in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(flock.attention_tracks(q, c, offsets, table, n, window=window))
+        graphs.append(g)
+    for turn in range(4):
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            if turn % 2:
+                with torch.cuda.stream(s):
+                    g.replay()
+            else:
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), f"turn {turn}"
+
+
 def test_attention_strides():
     gen = torch.Generator().manual_seed(16)
     c = cuda(pool(gen, 8, 2, 64))
