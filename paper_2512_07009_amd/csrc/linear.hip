@@ -77,8 +77,8 @@ __device__ __forceinline__ float gelu(float x) {
 // alone (they come back in order), with one barrier a step.
 //
 // Two workgroups of four waves a compute unit make 128 x 128 outputs each, and one's
-// outputs are made beside the other's products: 30001 rows of 2047 to 501 outputs 46 us
-// (1.3 POP/s, of 2.1 of a product of 8192^3 by the library).  What bounds it are the loads
+// outputs are made beside the other's products: 40000 rows of 2048 to 512 outputs 52 us
+// (1.6 POP/s, of 2.1 of a product of 8192^3 by the library).  What bounds it are the loads
 // to LDS and the outputs' stores (128000 x 512 to 1536, 172 us: without stores 143,
 // without making outputs 109, loads alone 106); steps of 64 bytes take half a line of a
 // row each (8192^3 609 -> 720 us).  Fewer than two tiles of 128 x 128 a compute unit are
@@ -448,11 +448,14 @@ __global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
 
 // Outputs of 16 bits of a wave's 32 rows, 64 of each, by way of LDS (`room`, 2 KB of the
 // wave's own), 16 rows at a time, in pieces of 128 bytes.  FULL: all of them are there, of
-// others the first `rows` and `here`.  Places in LDS are made here, not kept: registers
-// are full where this is called.
-template <bool FULL, bool GELU, typename T>
-__device__ __forceinline__ void make_64(T *y, int64_t y_stride, int rows, int here, Pack<T, 8> *room, const float *w_scale,
-                                        const float *bias, float scale, const i32x16 &first, const i32x16 &second) {
+// others the first `rows` and `here`.  Rows that begin inside 64 bytes (not LINES) go
+// through the caches, which join their parts (30001 x 2047 to 501 51 -> 42 us, 40 between
+// other work).  Places in
+// LDS are made here, not kept: registers are full where this is called.
+template <bool FULL, bool LINES, bool GELU, typename T>
+__device__ __forceinline__ void make_64(T *y, int64_t y_stride, int rows, int here, Pack<T, 8> *room,
+                                        const float *w_scale, const float *bias, float scale, const i32x16 &first,
+                                        const i32x16 &second) {
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
     const int h = lane >> 5, col = lane & 31;
@@ -482,8 +485,10 @@ __device__ __forceinline__ void make_64(T *y, int64_t y_stride, int rows, int he
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
                 const int row = lane / 8, part = lane & 7;
-                store_left<true>(y + (16 * half + 8 * v) * y_stride + ((uint32_t)row * (uint32_t)y_stride + 8 * part),
-                                 room[part_at(8 * v + row, part)], 8);
+                T *to = y + (16 * half + 8 * v) * y_stride + ((uint32_t)row * (uint32_t)y_stride + 8 * part);
+                const Pack<T, 8> all = room[part_at(8 * v + row, part)];
+                if constexpr (LINES) store_left<true>(to, all, 8);
+                else *reinterpret_cast<Pack<T, 8> *>(to) = all;
             }
         } else if (lane < here) {
 #pragma unroll 1
@@ -513,7 +518,7 @@ struct __attribute__((aligned(16))) WideShared {
     int8_t room[kWideThreads / 64][16 * 64 * 2];
 };
 
-template <typename T, bool GELU>
+template <typename T, bool GELU, bool LINES>
 __global__ void __launch_bounds__(kWideThreads, 2) linear_wide_kernel(LinearArgs a) {
     using Loads = LinearLoads<kWide, kWide, kWideThreads>;
     constexpr int kMT = 2, kNT = 4, kParts = kStep / 32;
@@ -615,9 +620,10 @@ __global__ void __launch_bounds__(kWideThreads, 2) linear_wide_kernel(LinearArgs
                 for (int i = 0; i < kNT; i += 2) {
                     const int m = wm + 32 * j, n = wn + 32 * i, rows = at.rows - m, here = at.columns - n;
                     const auto make = [&](auto all) __attribute__((always_inline)) {
-                        make_64<decltype(all)::value, GELU>(static_cast<T *>(a.y) + (at.m0 + m) * a.y_stride + at.n0 + n,
-                                                            a.y_stride, rows, here, room, s.w_scale[turn] + n, s.bias[turn] + n,
-                                                            s.x_scale[turn][m + col], acc[i][j], acc[i + 1][j]);
+                        make_64<decltype(all)::value, LINES, GELU>(static_cast<T *>(a.y) + (at.m0 + m) * a.y_stride + at.n0 + n,
+                                                                   a.y_stride, rows, here, room, s.w_scale[turn] + n,
+                                                                   s.bias[turn] + n, s.x_scale[turn][m + col], acc[i][j],
+                                                                   acc[i + 1][j]);
                     };
                     if (decltype(full)::value || (rows >= 32 && here >= 64)) make(std::true_type{});
                     else if (rows > 0 && here > 0) make(std::false_type{});
@@ -702,9 +708,9 @@ __global__ void __launch_bounds__(64 * kStayWaves) linear_stay_kernel(LinearArgs
     const auto make = [&](auto full, int n1, auto block, int64_t row0, const i32x16 (&acc)[kBlocks], float scale) __attribute__((always_inline)) {
         constexpr int i = decltype(block)::value;
         const int n = n1 + 32 * i;
-        make_64<decltype(full)::value, GELU>(static_cast<T *>(a.y) + row0 * a.y_stride + n0 + n, a.y_stride,
-                                             (int)min((int64_t)32, a.rows - row0), columns - n, room, s.w_scale + n,
-                                             s.bias + n, scale, acc[i], acc[i + 1]);
+        make_64<decltype(full)::value, true, GELU>(static_cast<T *>(a.y) + row0 * a.y_stride + n0 + n, a.y_stride,
+                                                   (int)min((int64_t)32, a.rows - row0), columns - n, room,
+                                                   s.w_scale + n, s.bias + n, scale, acc[i], acc[i + 1]);
     };
 
     const auto multiply = [&](int half, i32x16 (&acc)[kBlocks]) __attribute__((always_inline)) {
@@ -871,16 +877,17 @@ int64_t stay_workgroups(const LinearArgs &a, int n_cus) {
 
 // Whether tiles of 256 x 256 are faster than those of 128 x 128, two of which a compute unit
 // makes at a time: by a tenth for the same outputs a compute unit (128000 x 2048 to 512 162
-// -> 150 us, 30000 41 -> 38), so not where they do not share them as evenly (40000 52 -> 66).
-// Outputs that begin inside 64 bytes are written in parts (30001 x 2047 to 501 47 -> 51),
-// and narrow rows are bound by their outputs (300000 x 128 to 512 65 -> 66).
+// -> 150 us, 30000 41 -> 38, 30001 x 2047 to 501 47 -> 42), so not where they do not share
+// them as evenly (40000 52 -> 66).  Narrow rows are bound by their outputs (300000 x 128 to
+// 512 65 -> 66), the more so where those begin anywhere (128000 x 512 to 1000 142 -> 154,
+// 30000 x 1024 53 -> 48).
 template <typename T>
 bool wide_tiles(const LinearArgs &a, int n_cus) {
     const auto turns = [&](int64_t size, int64_t beside) {
         const int64_t tiles = (a.rows + size - 1) / size * ((a.outputs + size - 1) / size);
         return (tiles + beside - 1) / beside;
     };
-    return a.width >= 2 * kStep && a.y_stride < 1 << 24 && whole_lines<T>(a) &&
+    return a.width >= (whole_lines<T>(a) ? 2 : 8) * kStep && a.y_stride < 1 << 24 &&
            9 * 4 * turns(kWide, n_cus) <= 10 * 2 * turns(128, 2 * n_cus);
 }
 
@@ -889,8 +896,11 @@ hipError_t launch_wide(const LinearArgs &a, int n_cus, hipStream_t stream) {
     const int64_t workgroups = std::max(n_cus / 8 * 8, 8);
     return by_tiles<T, kWide, kWide>(a, [&](const LinearArgs &part) {
         const dim3 grid((uint32_t)std::min(part.tiles, workgroups)), block(kWideThreads);
-        if (a.gelu) hipLaunchKernelGGL((linear_wide_kernel<T, true>), grid, block, 0, stream, part);
-        else hipLaunchKernelGGL((linear_wide_kernel<T, false>), grid, block, 0, stream, part);
+        const auto launch = [&](auto gelu, auto lines) {
+            hipLaunchKernelGGL((linear_wide_kernel<T, decltype(gelu)::value, decltype(lines)::value>), grid, block, 0, stream, part);
+        };
+        const auto with_gelu = [&](auto gelu) { whole_lines<T>(part) ? launch(gelu, std::true_type{}) : launch(gelu, std::false_type{}); };
+        a.gelu ? with_gelu(std::true_type{}) : with_gelu(std::false_type{});
     });
 }
 

@@ -176,22 +176,25 @@ def test_gelu_of_what_is_not_finite(rows, dtype):
     (16301, 256, 2016, torch.bfloat16),  # two tiles each, of two steps
     (24000, 1001, 2048, torch.float16),  # three, of eight
     (29001, 577, 480, torch.bfloat16),
+    (30001, 1100, 501, torch.float16),   # outputs that begin anywhere
+    (16000, 1025, 1999, torch.bfloat16),
 ])
 def test_tiles_of_256(rows, width, outputs, dtype, gelu):
     c = case(19, rows, width, outputs)
     compare(c, dtype, gelu=gelu, x=padded(c["x"], (width + 15) // 16 * 16), w=padded(c["w"], (width + 15) // 16 * 16))
 
 
-def test_tiles_of_256_leave_what_is_beside_them():
+@pytest.mark.parametrize("before,after", [(32, 64), (33, 64), (32, 1)])
+def test_tiles_of_256_leave_what_is_beside_them(before, after):
     """Outputs in rows of a wider tensor, and the tensor's other elements as they were."""
-    c = case(20, 7700, 640, 1952)
-    wide = torch.full((7702, 1952 + 96), 7.0, dtype=torch.bfloat16, device="cuda")
-    out = wide[1:-1, 32:-64]
+    c = case(20, 7700, 1040, 1952)
+    wide = torch.full((7702, before + 1952 + after), 7.0, dtype=torch.bfloat16, device="cuda")
+    out = wide[1:-1, before:-after]
     d = {n: (t.cuda() if t is not None else None) for n, t in c.items()}
     flock.linear_rows_i8(d["x"], d["xs"], d["w"], d["ws"], d["bias"], out=out)
     want = flock.linear_rows_i8(d["x"], d["xs"], d["w"], d["ws"], d["bias"], dtype=torch.float32).bfloat16()
     assert torch.equal(out, want)
-    wide[1:-1, 32:-64] = 7.0
+    out.fill_(7.0)
     assert (wide == 7.0).all()
 
 
