@@ -8,9 +8,12 @@
 // one rounding to the output's type.
 
 #include "encoder_common.h"
+#include "linear_common.h"
 
 namespace flock {
 namespace {
+
+using namespace linear;
 
 constexpr int kThreads = 256;
 
@@ -85,8 +88,6 @@ __device__ __forceinline__ float gelu(float x) {
 // made as tiles of 64 x 64 by four workgroups (500 rows to 1536 5.6 us).
 // ---------------------------------------------------------------------------
 
-constexpr int kStep = 128, kAhead = 1, kStages = kAhead + 1, kChunks = kStep / 16;
-
 __device__ const __attribute__((aligned(16))) int8_t kZeros[16] = {};
 
 __device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row >> 1) & 7); }
@@ -94,12 +95,6 @@ __device__ __forceinline__ int turned(int row, int chunk) { return chunk ^ ((row
 #define FLOCK_TO_LDS(FROM, TO, SIZE)                                                                  \
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(FROM),         \
                                      (__attribute__((address_space(3))) void *)(TO), SIZE, 0, 0)
-
-template <int BM, int BN>
-struct __attribute__((aligned(16))) LinearShared {
-    int8_t x[kStages][BM * kStep], w[kStages][BN * kStep];
-    float x_scale[kStages][BM], w_scale[kStages][BN], bias[kStages][BN];  // of tiles in turn: a tile may be one step
-};
 
 // Where a tile's rows begin, for the loads or for the products.
 template <int BM, int BN>
@@ -269,7 +264,7 @@ __device__ __forceinline__ void store_left(T *y, const Pack<T, 8> &v, int left) 
 __device__ __forceinline__ void stand() { asm volatile("" ::: "memory"); }
 
 // A wave's outputs of a tile.  FULL: all of its rows and outputs are there.  Outputs of
-// 16 bits go through LDS (`room`, 2 KN KB of the wave's own), 32 rows at a time, so that a
+// 16 bits go through LDS (`room`, kRoom<KN> bytes of the wave's own), 32 rows at a time, so that a
 // row's are stored as 64 KN bytes in one piece: with stores of the 32 bytes that a lane
 // has beside each other 128000 x 512 to 1536 took 233 us, 95 of them for stores.
 template <typename T, bool GELU, bool FULL, int KM, int KN, typename S, typename Tile>
@@ -365,7 +360,6 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
     const int wave = threadIdx.x >> 6, wm = (wave & 1) * (BM / 2), wn = (wave >> 1) * (BN / 2);
     // a whole tile's stores, at least; they come between the loads of kAhead steps, which need not wait for them
     constexpr int kStores = 2 * kMT * kNT;
-    static_assert(BM == BN, "finish() takes a quarter of a stage");
     int stage = 0, turn = 0, since = kAhead;
     for (uint32_t tile = first; tile < end; tile += beside, turn = (turn + 1) & (kStages - 1)) {
         i32x16 acc[kNT][kMT] = {};
@@ -394,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 2) linear_kernel(LinearArgs a) {
         // the stage that was multiplied last is free until the next step's barrier
         __builtin_amdgcn_s_setprio(0);
         const int last = (stage + kStages - 1) & (kStages - 1);
-        int8_t *room = (wave < 2 ? s.x[last] : s.w[last]) + (wave & 1) * (BM * kStep / 2);
+        int8_t *room = stage_room<kNT>(s, last, wave);
         stand();
         __builtin_amdgcn_s_waitcnt(0xc07f);  // (LDS)
         __builtin_amdgcn_s_barrier();
@@ -441,7 +435,7 @@ __global__ void __launch_bounds__(kThreads) linear_any_kernel(LinearArgs a) {
         __syncthreads();
         multiply<1, 1>(s.x[0] + wm * kStep, s.w[0] + wn * kStep, acc);
     }
-    int8_t *room = s.x[1] + wave * (B * kStep / 2);  // (stages are not used but the first)
+    int8_t *room = stage_room<1>(s, 1, wave);  // (the first stage may still be read by other waves, the second has no use)
     if (a.gelu) finish<T, true, false>(a, t, s, 0, wm, wn, room, acc);
     else finish<T, false, false>(a, t, s, 0, wm, wn, room, acc);
 }

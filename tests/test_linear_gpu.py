@@ -105,6 +105,17 @@ def test_rows_that_begin_anywhere(rows, pitch_x, pitch_w):
     assert torch.equal(whole, compare(c, torch.bfloat16, x=x))
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("rows,width,outputs", [(33, 129, 64), (70, 1, 130), (1000, 127, 513), (4001, 2047, 200)])
+def test_rows_side_by_side_of_odd_widths(rows, width, outputs, dtype):
+    """Contiguous rows that begin anywhere: within their bounds, and the same to the bit every time."""
+    c = case(21, rows, width, outputs)
+    for gelu in (False, True):
+        first = compare(c, dtype, gelu=gelu)
+        for _ in range(10):
+            assert torch.equal(first, compare(c, dtype, gelu=gelu))
+
+
 def test_one_row_for_all():
     c = case(6, 70, 128, 66)
     c["x"] = c["x"][:1].expand(70, 128)
