@@ -27,9 +27,13 @@
 // float16 (of some 350).  Scores are transposed, S^T = K Q^T: a lane holds 16 tokens of one
 // row, four of each 16, which is the order in which the product with the values takes its
 // weights.  Values lie in pages so that a lane's 16 bytes are the factors of two such
-// products (16 x 16 x 32); they go to float16, which holds them exactly.  Weights carry the
-// page's scale relative to the largest so far, within the exponent, and are rounded to
-// float16 (2^-11) after they were summed in 32 bits.
+// products (16 x 16 x 32); they go to float16, which holds them exactly.  Weights are
+// rounded to float16 after they were summed in 32 bits, and carry the page's scale relative
+// to the largest so far while that is within 2^-4 of it: those from 2^-10 of the row's largest
+// on keep float16's 11 bits, others are off by 2^-21 of it at most.  Pages of smaller scales
+// are multiplied without them and join the sums in 32 bits, so that a page of large values
+// takes no digits of others, whether or not a row gives it any weight (500 tracks 82.7 -> 83.6
+// us, 96 clips 90.2 -> 91.3; with a first page of 10^6 times the others' values 84.8 and 92.8).
 
 #include "attention_common.h"
 #include "tracks_common.h"
@@ -52,6 +56,7 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 16, kManyRows = 128;  // of a workgroup, 2^4 and 2^7
 constexpr float kSlack = 8.0f;    // scores above the shift by less are left there
+constexpr float kNear = 0x1p-4f;  // scales of values this near to the largest so far go with the weights
 constexpr float kQuery = 32512.0f;  // a query's largest dimension as 256 a + b
 
 // Eight whole numbers in float16: 1024 + u, u = x + 128, is 0x6400 | u, and 1152 is taken off.
@@ -132,6 +137,21 @@ struct Whole {
     __device__ __forceinline__ float factor(const TrackAttentionArgs &a) const {
         const float scale = CAP == kHigh ? a.scale / a.cap : CAP == kLow ? 2.0f * kLog2e * a.scale / a.cap : a.scale * kLog2e;
         return finite ? fminf(scale * (per > 0.0f ? most / kQuery : 1.0f), 0x1p127f) : NAN;
+    }
+};
+
+// How a page's values, of this scale, are added to rows that count in `unit`, the largest
+// scale of values so far.  Near to it the weights take the quotient (level, its logarithm;
+// the total takes it back).  Where it would cost weights digits of float16 (or there is none)
+// the page's products are made by themselves and multiplied by `times` in 32 bits.
+struct Level {
+    bool near;
+    float level, back, times;
+    __device__ __forceinline__ Level(float v_scale, float unit) {
+        near = v_scale > 0.0f && v_scale >= unit * kNear;
+        level = near ? __log2f(v_scale / unit) : 0.0f;
+        back = near ? unit / v_scale : 1.0f;
+        times = v_scale > 0.0f ? v_scale / unit : 0.0f;
     }
 };
 
@@ -252,14 +272,12 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
         const float k_scale = scale_of(my_k, n), v_scale = scale_of(my_v, n);
         ++n;
         const int after = next(n);
-        // the values' scale against the largest: 2^-40 for less, which is lost beside it
         float keep_v = 1.0f;
         if (v_scale > unit) {
             keep_v = unit / v_scale;
             unit = v_scale;
         }
-        const bool near = v_scale > unit * 0x1p-40f;
-        const float level = near ? __log2f(v_scale / unit) : -40.0f, back = near ? unit / v_scale : 0x1p40f;
+        const Level values(v_scale, unit);
         const bool inside = token0 + kPage - 1 <= all_own && token0 > all_lo;
         f16x8 weights[2];
         f32x16 s;
@@ -308,7 +326,7 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) w.acc[b] *= keep;
         }
-        const float base = (w.shift == -INFINITY ? 0.0f : w.shift) - level;
+        const float base = (w.shift == -INFINITY ? 0.0f : w.shift) - values.level;
         float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -316,19 +334,26 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
             sum += x;
             weights[e >> 3][e & 7] = (half_t)x;
         }
-        w.total += sum * back;
+        w.total += sum * values.back;
         if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page
             const float none = over_parts(sum, [](float u, float v) { return u + v; }) == 0.0f ? 0.0f : NAN;
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) w.acc[b] += none;
         }
+        const auto product = [&](int b, f32x4 to) {
+            const f16x8 v0 = to_half(vr[b][0], vr[b][1]), v1 = to_half(vr[b][2], vr[b][3]);
+            to = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, weights[0], to, 0, 0, 0);
+            return __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, weights[1], to, 0, 0, 0);
+        };
+        if (values.near) {
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
-            if (b < blocks) {
-                const f16x8 v0 = to_half(vr[b][0], vr[b][1]), v1 = to_half(vr[b][2], vr[b][3]);
-                w.acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, weights[0], w.acc[b], 0, 0, 0);
-                w.acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, weights[1], w.acc[b], 0, 0, 0);
-            }
+            for (int b = 0; b < kBlocks; ++b)
+                if (b < blocks) w.acc[b] = product(b, w.acc[b]);
+        } else {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+                if (b < blocks) w.acc[b] += product(b, f32x4{0.0f, 0.0f, 0.0f, 0.0f}) * values.times;
+        }
         if (after >= 0) load_v(after);
         page = after;
     }
@@ -529,15 +554,13 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
         now = second;
         second = third;
         third = load();
-        // the values' scale against the largest: 2^-40 for less, which is lost beside it
-        float keep_v = 1.0f;
-        if (v_scale > unit) {
-            keep_v = unit / v_scale;
-            unit = v_scale;
-        }
         if (some_rows && token0 <= wave_last && token0 + kPage - 1 > some_lo) {
-            const bool near = v_scale > unit * 0x1p-40f;
-            const float level = near ? __log2f(v_scale / unit) : -40.0f, back = near ? unit / v_scale : 0x1p40f;
+            float keep_v = 1.0f;
+            if (v_scale > unit) {
+                keep_v = unit / v_scale;
+                unit = v_scale;
+            }
+            const Level values(v_scale, unit);
             f32x16 s[2];
             float f = factor * k_scale;
             if (f > 0x1p127f) f = 0x1p127f;  // (NaN stays)
@@ -590,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
             }
-            const float base = (shift == -INFINITY ? 0.0f : shift) - level;
+            const float base = (shift == -INFINITY ? 0.0f : shift) - values.level;
             float sum = 0.0f;
             f16x8 weights[4];
 #pragma unroll
@@ -601,25 +624,32 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
                     sum += x;
                     weights[2 * t + (e >> 3)][e & 7] = (half_t)x;
                 }
-            total += sum * back;
+            total += sum * values.back;
             if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page
                 const float none = attention::across(sum, [](float u, float v) { return u + v; }) == 0.0f ? 0.0f : NAN;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) acc[b] += none;
             }
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) {
+            const auto product = [&](int b, f32x16 to) {
                 const int d = 32 * b + r;
                 const int8_t *v = shared.v[buffer] + d * kPage;
                 const i32x4 x = *reinterpret_cast<const i32x4 *>(v + 16 * turned<kPage>(d, h));
                 const i32x4 y = *reinterpret_cast<const i32x4 *>(v + 16 * turned<kPage>(d, h + 2));
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_half(x[i], y[i]), weights[i], acc[b], 0, 0, 0);
-            }
-        } else if (keep_v != 1.0f) {
+                    to = __builtin_amdgcn_mfma_f32_32x32x16_f16(to_half(x[i], y[i]), weights[i], to, 0, 0, 0);
+                return to;
+            };
+            if (values.near) {
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b) acc[b] *= keep_v;
+                for (int b = 0; b < kBlocks; ++b) acc[b] = product(b, acc[b]);
+            } else {
+#pragma unroll
+                for (int b = 0; b < kBlocks; ++b) {
+                    acc[b] += product(b, f32x16{}) * values.times;
+                    __builtin_amdgcn_sched_barrier(0);  // (one product's registers at a time)
+                }
+            }
         }
         buffer = (buffer + 1) & (kBuffers - 1);
     }
