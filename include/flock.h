@@ -704,7 +704,7 @@ flock_status append_tracks(int32_t dtype, const void *new_k, int64_t new_k_strid
  * numbers they are, with products in 32-bit sums and a softmax in 32 bits.  A query's
  * dimension is rounded by at most 2^-17 of its head's largest (a head whose largest is
  * below 2^-100 is zeros, one that is not finite gives NaN), and weights are rounded to 11
- * bits for the product with v, those below 2^-10 of their row's largest to 2^-21 of it,
+ * bits for the product with v, those below 2^-17 of their row's largest to 2^-28 of it,
  * whatever the scales of other pages (up to 2^100 apart).
  * Scales are >= 0, or NaN: then what sees the page is NaN.
  *

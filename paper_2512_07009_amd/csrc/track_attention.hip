@@ -29,8 +29,8 @@
 // weights.  Values lie in pages so that a lane's 16 bytes are the factors of two such
 // products (16 x 16 x 32); they go to float16, which holds them exactly.  Weights are
 // rounded to float16 after they were summed in 32 bits, and carry the page's scale relative
-// to the largest so far while that is within 2^-4 of it: those from 2^-10 of the row's largest
-// on keep float16's 11 bits, others are off by 2^-21 of it at most.  Pages of smaller scales
+// to the largest so far while that is within 2^-4 of it: those from 2^-17 of the row's largest
+// on keep float16's 11 bits, others are off by 2^-28 of it at most.  Pages of smaller scales
 // are multiplied without them and join the sums in 32 bits, so that a page of large values
 // takes no digits of others, whether or not a row gives it any weight (500 tracks 82.7 -> 83.6
 // us, 96 clips 90.2 -> 91.3; with a first page of 10^6 times the others' values 84.8 and 92.8).
@@ -56,6 +56,9 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 16, kManyRows = 128;  // of a workgroup, 2^4 and 2^7
 constexpr float kSlack = 8.0f;    // scores above the shift by less are left there
+// Weights are kept 2^7 times as large, 2^15 at most, so that float16's digits go that much further
+// down; what leaves a workgroup is kUnlift of it.
+constexpr float kLift = 7.0f, kUnlift = 0x1p-7f;
 constexpr float kNear = 0x1p-4f;  // scales of values this near to the largest so far go with the weights
 constexpr float kQuery = 32512.0f;  // a query's largest dimension as 256 a + b
 
@@ -141,15 +144,16 @@ struct Whole {
 };
 
 // How a page's values, of this scale, are added to rows that count in `unit`, the largest
-// scale of values so far.  Near to it the weights take the quotient (level, its logarithm;
-// the total takes it back).  Where it would cost weights digits of float16 (or there is none)
-// the page's products are made by themselves and multiplied by `times` in 32 bits.
+// scale of values so far.  Near to it the weights take the quotient (level: its logarithm and
+// the lift; the total takes the quotient back).  Where it would cost weights digits of
+// float16, or there is none, the page's products are made by themselves and multiplied by
+// `times` in 32 bits.
 struct Level {
     bool near;
     float level, back, times;
     __device__ __forceinline__ Level(float v_scale, float unit) {
         near = v_scale > 0.0f && v_scale >= unit * kNear;
-        level = near ? __log2f(v_scale / unit) : 0.0f;
+        level = near ? __log2f(v_scale / unit) + kLift : kLift;
         back = near ? unit / v_scale : 1.0f;
         times = v_scale > 0.0f ? v_scale / unit : 0.0f;
     }
@@ -359,7 +363,8 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
     }
 
     // the waves' parts, joined
-    w.total = over_parts(w.total, [](float u, float v) { return u + v; });
+    w.total = over_parts(w.total, [](float u, float v) { return u + v; }) * kUnlift;
+    unit *= kUnlift;
     if (part == 0) stats[0][wave][r] = w.shift;
     __syncthreads();
     float now = stats[0][0][r];
@@ -653,7 +658,8 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
         }
         buffer = (buffer + 1) & (kBuffers - 1);
     }
-    total = attention::across(total, [](float u, float v) { return u + v; });
+    total = attention::across(total, [](float u, float v) { return u + v; }) * kUnlift;
+    unit *= kUnlift;
     if (!valid) return;
     const int64_t bird = it.at.row0 + query;
     // (a shift that nothing has moved: no token, or none but NaN)

@@ -1,6 +1,6 @@
 """attention_tracks keeps the digits of values beside pages of far larger ones:
 pages that a row gives no weight or does not see, before, among and after those
-that it does, in each of its kernels."""
+that it does, in each of its kernels; and those of weights far below the largest."""
 
 import math
 
@@ -15,9 +15,9 @@ from tests.test_tracks_gpu import cuda, int32, offsets_of, pool, table_of
 pytestmark = pytest.mark.gpu
 
 PAGE, E32 = 64, ref.E32
-# Weights in float16 are off by 2^-11 of themselves, or by 2^-25 of what they are relative to: the row's largest score at
-# the time, times at least 2^-4 where the page's scale of values is in them.
-LEAST = 2.0 ** -21
+# Weights in float16 are off by 2^-11 of themselves, or by 2^-25 of what they are relative to: 2^-7 of the row's largest at
+# the time, over 2^-4 at least where the page's scale of values is in them.
+LEAST = 2.0 ** -28
 
 
 def reference(q, cache, offsets, table, lengths, scale, cap=0.0, window=0):
@@ -151,3 +151,21 @@ def test_uneven_scales(power):
     attend(11, *FEW, uneven(power))
     attend(12, *SHARED, uneven(power), dim=128)
     attend(13, *RUNS, uneven(power), q_heads=16, kv_heads=8)
+
+
+def small(power):
+    """A track's first token gets 2^power times the weight of any other, and its values are zeros."""
+    def change(c, ids, scale):
+        k, v, k_scale, v_scale = c
+        k[ids] = 0
+        k[ids[0], :, 0, 0] = 127
+        k_scale[ids[0]] = power * math.log(2) / (scale * 8 * 127)
+        v[ids[0], :, :, ref.place(0)] = 0
+    return change
+
+
+@pytest.mark.parametrize("power", [10, 14, 17, 20, 24, 27])
+def test_small_weights(power):
+    attend(14, [64, 3, 40], [1, 1, 2], small(power))
+    attend(15, *RUNS, small(power), q_heads=16, kv_heads=8)
+    attend(16, *RUNS, small(power), q_heads=16, kv_heads=8, dim=128, dtype=torch.float16)
