@@ -317,6 +317,8 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
 #pragma unroll
         for (int e = 1; e < 16; ++e) most = fmaxf(most, s[e]);
         most = over_parts(most, [](float u, float v) { return fmaxf(u, v); }) * f;
+        // values that are not finite: none for rows that see the page, whatever its weight
+        if (v_scale != v_scale && most != -INFINITY) w.total = NAN;
         float keep = keep_v;
         if (__any(most > w.shift + kSlack || (w.shift == -INFINITY && most > w.shift))) {
             const float now = fmaxf(w.shift, most);
@@ -339,11 +341,6 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
             weights[e >> 3][e & 7] = (half_t)x;
         }
         w.total += sum * values.back;
-        if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page
-            const float none = over_parts(sum, [](float u, float v) { return u + v; }) == 0.0f ? 0.0f : NAN;
-#pragma unroll
-            for (int b = 0; b < kBlocks; ++b) w.acc[b] += none;
-        }
         const auto product = [&](int b, f32x4 to) {
             const f16x8 v0 = to_half(vr[b][0], vr[b][1]), v1 = to_half(vr[b][2], vr[b][3]);
             to = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, weights[0], to, 0, 0, 0);
@@ -630,10 +627,9 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
                     weights[2 * t + (e >> 3)][e & 7] = (half_t)x;
                 }
             total += sum * values.back;
-            if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page
-                const float none = attention::across(sum, [](float u, float v) { return u + v; }) == 0.0f ? 0.0f : NAN;
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b) acc[b] += none;
+            if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page, whatever its weight
+                stand();               // (a branch, which keeps the values' registers apart from the scores')
+                if (most != -INFINITY) total = NAN;
             }
             const auto product = [&](int b, f32x16 to) {
                 const int d = 32 * b + r;

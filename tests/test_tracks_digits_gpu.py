@@ -169,3 +169,30 @@ def test_small_weights(power):
     attend(14, [64, 3, 40], [1, 1, 2], small(power))
     attend(15, *RUNS, small(power), q_heads=16, kv_heads=8)
     attend(16, *RUNS, small(power), q_heads=16, kv_heads=8, dim=128, dtype=torch.float16)
+
+
+@pytest.mark.parametrize("lengths,queries,heads,at", [([500, 70], [400, 20], 1, 0), ([420, 700], [1, 1], 1, 5),
+                                                      ([9000], [1], 1, 100), ([300] * 40, [150] * 40, 8, 2),
+                                                      ([490] * 3200, [1] * 3200, 1, 6)])
+@pytest.mark.parametrize("window", [0, 64, 128])
+def test_pages_that_are_not_finite_and_far_below(lengths, queries, heads, at, window):
+    """A page with a scale of NaN is NaN for the rows that see it, even where its weights are nothing in 32 bits."""
+    gen = torch.Generator().manual_seed(17)
+    each = [(n + PAGE - 1) // PAGE for n in lengths]
+    c = pool(gen, max(each), heads, 64)
+    table = torch.full((len(each), max(each)), -1, dtype=torch.int32)
+    for t, n in enumerate(each):
+        table[t, :n] = torch.arange(n)      # (all tracks read the same pages)
+    offsets = offsets_of(queries)
+    q = torch.randn(offsets[-1], 2 * heads, 64, generator=gen)
+    q[:, :, 0] = 8.0
+    c[0][at] = 0
+    c[0][at, :, :, 0] = -127
+    c[2][at] = 120 / 127      # scores of 120 below
+    c[3][at] = math.nan
+    places = torch.cat([torch.arange(n - m, n) for n, m in zip(lengths, queries)])
+    seen = places >= at * PAGE
+    if window:
+        seen &= places - window < at * PAGE + PAGE - 1
+    got = flock.attention_tracks(q.bfloat16().cuda(), cuda(c), int32(offsets), table.cuda(), int32(lengths), window=window).cpu()
+    assert got[seen].isnan().all() and got[~seen].isfinite().all()
