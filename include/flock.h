@@ -702,7 +702,7 @@ flock_status append_tracks(int32_t dtype, const void *new_k, int64_t new_k_strid
  *   out_i = sum over the tokens seen of softmax_j(t) v_j
  * A query that sees no token gets zeros.  Keys and values are taken as the whole
  * numbers they are, with products in 32-bit sums and a softmax in 32 bits.  A query's
- * dimension is rounded by at most 2^-17 of its head's largest (a head whose largest is
+ * dimension is rounded by at most 1/64000 of its head's largest (a head whose largest is
  * below 2^-100 is zeros, one that is not finite gives NaN), and weights are rounded to 11
  * bits for the product with v, those below 2^-17 of their row's largest to 2^-28 of it,
  * whatever the scales of other pages (up to 2^100 apart).

@@ -21,12 +21,14 @@
 // by the waves in LDS (no faster).
 //
 // Scores are products of whole numbers on the matrix cores (16 x 16 x 64, 8 bits, exact
-// sums): keys as they lie in pages, and queries as 256 a + b with a, b in 8 bits.  That
-// rounds a query's dimension by 2^-17 of its row's largest at most, below what its own
-// 16-bit type leaves of it, and spares a lane 80 instructions a page to convert keys to
-// float16 (of some 350).  Scores are transposed, S^T = K Q^T: a lane holds 16 tokens of one
-// row, four of each 16, which is the order in which the product with the values takes its
-// weights.  Values lie in pages so that a lane's 16 bytes are the factors of two such
+// sums): keys as they lie in pages, and queries as 256 a + b with a, b in 8 bits, in steps
+// of 1 / 32512 of their head's largest dimension.  A dimension is off by half a step, some
+// 2^-16 of the largest: below half a step of its own type from 2^-4 (float16) or 2^-7
+// (bfloat16) of the largest on, while smaller ones lose digits, so that a score is off by the
+// largest dimension times the sum of |k| / 65024 at most.  That spares a lane 80 instructions
+// a page to convert keys to float16 (of some 350).  Scores are transposed, S^T = K Q^T: a lane
+// holds 16 tokens of one row, four of each 16, which is the order in which the product with
+// the values takes its weights.  Values lie in pages so that a lane's 16 bytes are the factors of two such
 // products (16 x 16 x 32); they go to float16, which holds them exactly.  Weights are
 // rounded to float16 after they were summed in 32 bits, and carry the page's scale relative
 // to the largest so far while that is within 2^-4 of it: those from 2^-17 of the row's largest
