@@ -467,9 +467,9 @@ size_t rms_norm_rows_backward_workspace(int32_t rows, int32_t width);
  *
  * y as for rms_norm_rows, in 32 bits, is not written; per row
  *   scale = max |y| / 127,  q = y / scale to the nearest whole number, ties to even
- * so that y is scale * q to half a scale.  A row whose largest |y| is below
- * 2^-100 has scale and q 0; one with a value that is not finite has scale NaN
- * and q 0.
+ * (both quotients in 32 bits), so that y is scale * q to half a scale.  A row whose
+ * largest |y| is below 2^-100 has scale and q 0; one with a value that is not
+ * finite has scale NaN and q 0.
  *
  * Arguments: as for rms_norm_rows, and
  *   q              device out, int8[rows][width], rows q_stride bytes apart
@@ -664,9 +664,9 @@ size_t attention_frames_backward_workspace(int32_t n_frames, int32_t total_q, in
  *   scale = max(the scale it has, if it holds earlier tokens; max |new| / 127)
  *   new tokens:  value / scale, to the nearest whole number, ties to even
  *   held tokens, where the scale grew:  whole number * (old scale / scale), likewise
- * A page's first token begins it anew, whatever its scale was.  Places of tokens to
- * come are left as they are.  A page that gets a value that is not finite has scale
- * NaN and zeros from then on; new tokens below 2^-100 are zeros.
+ * with quotients in 32 bits.  A page's first token begins it anew, whatever its scale
+ * was.  Places of tokens to come are left as they are.  A page that gets a value that is
+ * not finite has scale NaN and zeros from then on; new tokens below 2^-100 are zeros.
  * Rows of one call must not meet in a page: where the table names a page for two
  * tracks, or twice for one, what it holds after both were appended to is undefined.
  * (Pages that tracks share may be read by all.)

@@ -41,21 +41,22 @@ __device__ __forceinline__ uint32_t row_largest(uint32_t x, uint32_t *slot) {
 }
 
 // How a row whose largest |y| has these bits goes to 8 bits.  Rows below 2^-100
-// are zeros (127 / largest would leave 32 bits), those with values that are not
+// are zeros (1 / scale would leave 32 bits), those with values that are not
 // finite zeros with a scale of NaN, which every product with them then is.
+__device__ __forceinline__ float scale_of(uint32_t largest) {
+    const float most = __uint_as_float(largest);
+    return largest >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : most >= 0x1p-100f ? most / 127.0f : 0.0f;
+}
+
 struct Steps {
-    float scale, per;
+    float scale;
+    Quotient by;
     int kept;  // bits of a whole number: none of one that is zero by this
-    __device__ __forceinline__ explicit Steps(uint32_t largest) {
-        const float most = __uint_as_float(largest);
-        const bool finite = largest < 0x7f800000u, some = finite && most >= 0x1p-100f;
-        scale = finite ? (some ? most / 127.0f : 0.0f) : __uint_as_float(0x7fc00000u);
-        per = some ? 127.0f / most : 0.0f;
-        kept = some ? -1 : 0;
-    }
-    __device__ __forceinline__ int round(float y) const { return (int)rounded(y, per) & kept; }
+    __device__ __forceinline__ explicit Steps(uint32_t largest)
+        : scale(scale_of(largest)), by(scale), kept(scale > 0.0f ? -1 : 0) {}
+    __device__ __forceinline__ int round(float y) const { return (int)by.rounded(y) & kept; }
     __device__ __forceinline__ int round(float y0, float y1, float y2, float y3) const {
-        return bytes(rounded(y0, per), rounded(y1, per), rounded(y2, per), rounded(y3, per)) & kept;
+        return bytes(by.rounded(y0), by.rounded(y1), by.rounded(y2), by.rounded(y3)) & kept;
     }
 };
 

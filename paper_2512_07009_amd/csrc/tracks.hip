@@ -178,15 +178,15 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
     float scale = largest < 0x7f800000u ? __uint_as_float(largest) / 127.0f : __uint_as_float(0x7fc00000u);
     if (largest < __float_as_uint(0x1p-100f)) scale = 0.0f;
     scale = old > scale || old != old ? old : scale;
-    const float per = scale > 0.0f ? 1.0f / scale : 0.0f;
-    const float again = per * old;             // what held tokens are multiplied by
+    const Quotient to(scale);
+    const float again = scale > 0.0f ? old / scale : 0.0f;  // what held tokens are multiplied by
     const bool held = s0 > 0 && old != scale;  // ... and have to be
     const int kept = scale == scale ? -1 : 0;  // bits (a page with NaN holds zeros)
     if (threadIdx.x == 0) scales[block] = scale;
 
     if (!values) {
         int8_t *k = a.cache.k + block * (kPage * dim);
-        const auto keep = [&](int token, int d, float x) { whole[token * dim + d] = (int8_t)(kept & rounded(x, per)); };
+        const auto keep = [&](int token, int d, float x) { whole[token * dim + d] = (int8_t)(kept & to.rounded(x)); };
         if (p < pairs) {
             if constexpr (WAVES == 4) {
 #pragma unroll
@@ -219,8 +219,8 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
             i32x4 c;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                c[e] = kept & bytes(rounded(byte_of(before, 4 * e), again), rounded(byte_of(before, 4 * e + 1), again),
-                                    rounded(byte_of(before, 4 * e + 2), again), rounded(byte_of(before, 4 * e + 3), again));
+                c[e] = kept & bytes(rounded_again(byte_of(before, 4 * e), again), rounded_again(byte_of(before, 4 * e + 1), again),
+                                    rounded_again(byte_of(before, 4 * e + 2), again), rounded_again(byte_of(before, 4 * e + 3), again));
             *at = c;
         }
         return;
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
         i32x4 *at = reinterpret_cast<i32x4 *>(v + d * kPage + 16 * part);
         // (no branches: what the places of other tokens have in LDS is read and left out)
         const T *x = fresh + 4 * part * pitch + d;
-        const auto value = [&](int e, int i) { return rounded(static_cast<float>(x[(16 * e + i) * pitch]), per); };
+        const auto value = [&](int e, int i) { return to.rounded(static_cast<float>(x[(16 * e + i) * pitch])); };
         i32x4 c, before = {0, 0, 0, 0};
         if (brings != 0xffff) before = *at;
 #pragma unroll
@@ -249,8 +249,8 @@ __global__ void __launch_bounds__(64 * WAVES) append_kernel(AppendArgs a) {
         if (held) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int again_4 = kept & bytes(rounded(byte_of(before, 4 * e), again), rounded(byte_of(before, 4 * e + 1), again),
-                                                 rounded(byte_of(before, 4 * e + 2), again), rounded(byte_of(before, 4 * e + 3), again));
+                const int again_4 = kept & bytes(rounded_again(byte_of(before, 4 * e), again), rounded_again(byte_of(before, 4 * e + 1), again),
+                                                 rounded_again(byte_of(before, 4 * e + 2), again), rounded_again(byte_of(before, 4 * e + 3), again));
                 c[e] = (again_4 & of_bits(holds >> (4 * e))) | (c[e] & ~of_bits(holds >> (4 * e)));
             }
         }

@@ -11,9 +11,24 @@ namespace whole {
 // |x| as bits, in the order of the numbers: infinity above all of them, NaN above it.
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// x / scale to the nearest whole number, ties to even, given 1 / scale: the low byte of
-// what is left of x / scale beside 1.5 x 2^23 (|x / scale| is below 128).
-__device__ __forceinline__ uint32_t rounded(float x, float per) { return __float_as_uint(__builtin_fmaf(x, per, 12582912.0f)); }
+// How numbers go to whole ones: x / scale in 32 bits, rounded as a division is, and that to
+// the nearest, ties to even.  A product with 1 / scale alone would take x on either side where
+// x / scale is a half (16-bit numbers of half their row's largest, 63.5, are), so its remainder
+// goes over it once more.  |x / scale| is below 128.
+struct Quotient {
+    float scale, per;
+    __device__ __forceinline__ explicit Quotient(float scale) : scale(scale), per(scale > 0.0f ? 1.0f / scale : 0.0f) {}
+    // As the low byte of a sum with 1.5 x 2^23.
+    __device__ __forceinline__ uint32_t rounded(float x) const {
+        const float q = x * per;
+        return __float_as_uint(__builtin_fmaf(__builtin_fmaf(-q, scale, x), per, q) + 12582912.0f);
+    }
+};
+
+// A whole number times a quotient of scales to the nearest, likewise.
+__device__ __forceinline__ uint32_t rounded_again(float whole, float quotient) {
+    return __float_as_uint(__builtin_fmaf(whole, quotient, 12582912.0f));
+}
 
 // Four low bytes in one word.
 __device__ __forceinline__ int bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {

@@ -198,3 +198,17 @@ def test_empty_and_refusals():
         flock.quantize_rows(x, out=(torch.empty(4, 16, dtype=torch.uint8, device="cuda"), torch.empty(4, device="cuda")))
     with pytest.raises(ValueError, match="scale"):
         flock.quantize_rows(x, out=(torch.empty(4, 16, dtype=torch.int8, device="cuda"), torch.empty(5, device="cuda")))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("width", [8, 100, 512, 2500, 9000])
+def test_whole_numbers_are_the_rounded_quotients(width, dtype):
+    """To the bit what a division in 32 bits rounds to, numbers at half a step among them (half a row's largest is 63.5)."""
+    gen = torch.Generator().manual_seed(width)
+    x = torch.randn(400, width, generator=gen).to(dtype)
+    most = x.abs().amax(1)
+    x[:, 0], x[:, 1], x[:, 2] = most, most / 2, -most / 2
+    q, scale = flock.quantize_rows(x.cuda())
+    q, scale = q.cpu(), scale.cpu()
+    assert torch.equal(scale, most.float() / 127)
+    assert torch.equal(q.float(), torch.round(x.float() / scale[:, None]))

@@ -199,6 +199,40 @@ def test_append_passes_over_what_is_out_of_range():
     check([0, 4, 8, 12], [[2 ** 31 - 1], [-2 ** 31], [2]], [4, 4, 5])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("tracks,rows", [(3, 100), (300, 2)])
+def test_append_whole_numbers_are_the_rounded_quotients(tracks, rows, dtype):
+    """To the bit what divisions in 32 bits round to, numbers at half a step among them (half a page's largest is 63.5)."""
+    gen = torch.Generator().manual_seed(11)
+    heads, dim = 2, 32
+    lengths = [rows + t % 50 for t in range(tracks)]
+    pages = sum((n + PAGE - 1) // PAGE for n in lengths)
+    start = pool(gen, pages, heads, dim)
+    table = table_of(gen, lengths, pages)
+    new = 4 * torch.randn(2, tracks * rows, heads, dim, generator=gen).to(dtype)
+    new[:, ::2, :, 1] = new[:, ::2].abs().amax(3) / 2
+    cache = cuda(start)
+    flock.append_tracks(cache, new[0].cuda(), new[1].cuda(), int32(offsets_of([rows] * tracks)), table.cuda(), int32(lengths))
+    got = back(cache)
+    for i in (0, 1):
+        whole, before = (c[0] if i == 0 else ref.in_order(c[1]) for c in (got, start))
+        for t, n in enumerate(lengths):
+            for p in range((n + PAGE - 1) // PAGE):
+                page, first = int(table[t, p]), n - rows - p * PAGE
+                s0, s1 = max(first, 0), min(n - p * PAGE, PAGE)
+                if s1 <= s0:
+                    continue
+                x = new[i, t * rows + s0 - first:t * rows + s1 - first].float().transpose(0, 1)
+                scale = x.abs().amax((1, 2)) / 127
+                if s0:
+                    scale = torch.maximum(scale, start[2 + i][page])
+                assert torch.equal(got[2 + i][page], scale)
+                assert torch.equal(whole[page, :, s0:s1].float(), torch.round(x / scale[:, None, None]))
+                # (a whole number times a quotient in 32 bits is exact in 64)
+                held = before[page, :, :s0].double() * (start[2 + i][page] / scale).double()[:, None, None]
+                assert torch.equal(whole[page, :, :s0].double(), torch.round(held))
+
+
 # --- attention ---
 
 def attend(seed, lengths, queries, q_heads=4, kv_heads=2, dim=64, dtype=torch.bfloat16, cap=0.0, window=0, scale=None,
