@@ -438,6 +438,44 @@ def test_attention_repeats_bit_for_bit_in_any_company():
     assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("mine,queries,others,total,columns,heads,dim,dtype", [
+    ((900, 3), 3, 7, 20, 40, (8, 2), 64, torch.bfloat16),            # several workgroups share a track's pages
+    ((900, 3), 40, 300, 500, 40, (4, 1), 128, torch.float16),
+    ((200, 500), 1, 3200, 3202, 8, (2, 1), 64, torch.bfloat16),      # a wave a workgroup
+    ((700, 450), 400, 60, 9000, 20, (8, 4), 64, torch.bfloat16),     # 128 rows a workgroup
+    ((700, 450), 400, 60, 9000, 20, (8, 4), 96, torch.float16),
+])
+@pytest.mark.parametrize("cap,window", [(0.0, 0), (30.0, 100)])
+def test_attention_of_a_track_in_other_company(mine, queries, others, total, columns, heads, dim, dtype, cap, window):
+    """Two tracks' rows to the bit, whatever the lengths, rows, pages and places in the batch of the tracks beside them."""
+    gen = torch.Generator().manual_seed(62)
+    each = [(n + PAGE - 1) // PAGE for n in mine]
+    c = cuda(pool(gen, 100, heads[1], dim))
+    pages = [torch.randperm(100, generator=gen)[:n].int() for n in each]
+    qs = [torch.randn(queries, heads[0], dim, generator=gen).to(dtype) for _ in mine]
+    first = None
+    for seed in range(3):
+        gen = torch.Generator().manual_seed(seed)
+        n = others + len(mine)
+        at = torch.randperm(n, generator=gen)[:len(mine)].tolist()
+        cut = torch.randint(0, total - queries * len(mine) + 1, (others - 1,), generator=gen).sort().values.tolist()
+        rest = [b - a for a, b in zip([0, *cut], [*cut, total - queries * len(mine)])]
+        lengths = torch.randint(0, PAGE * columns + 1, (n,), generator=gen).tolist()
+        table = torch.randint(-1, 101, (n, columns), generator=gen, dtype=torch.int32)
+        q = torch.randn(total, heads[0], dim, generator=gen).to(dtype)
+        counts = [0] * n
+        for t in range(n):
+            counts[t] = queries if t in at else rest.pop()
+        offsets = offsets_of(counts)
+        for i, t in enumerate(at):
+            lengths[t], table[t, :each[i]] = mine[i], pages[i]
+            q[offsets[t]:offsets[t + 1]] = qs[i]
+        out = flock.attention_tracks(q.cuda(), c, int32(offsets), table.cuda(), int32(lengths), cap=cap, window=window)
+        got = torch.cat([out[offsets[t]:offsets[t + 1]] for t in at])
+        first = got if first is None else first
+        assert got.isfinite().all() and torch.equal(got, first)
+
+
 def test_refusals():
     c = flock.TrackCache.empty(4, 2, 64)
     k = torch.zeros(3, 2, 64, device="cuda")
