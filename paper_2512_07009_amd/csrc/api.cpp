@@ -1434,13 +1434,8 @@ size_t attention_tracks_workspace(int32_t n_tracks, int32_t total, int32_t max_p
                                   int32_t head_dim) {
     if (n_tracks <= 0 || total <= 0 || max_pages < 0 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || head_dim < 1)
         return 0;
-    size_t most = 0;
-    for (const bool capped : {false, true})
-        most = std::max(most, flock::track_attention_workspace_bytes(
-                                      flock::plan_track_attention(n_tracks, total, max_pages, q_heads, kv_heads, head_dim,
-                                                                  capped, device_cus()),
-                                      total, q_heads, head_dim));
-    return most;
+    return flock::track_attention_workspace_bytes(
+            flock::plan_track_attention(n_tracks, total, max_pages, q_heads, kv_heads, device_cus()), total, q_heads, head_dim);
 }
 
 flock_status attention_tracks(int32_t dtype, const void *q, int64_t q_stride, const int32_t *offsets, int32_t n_tracks,
@@ -1475,7 +1470,7 @@ flock_status attention_tracks(int32_t dtype, const void *q, int64_t q_stride, co
     if ((int64_t)total * (q_heads / kv_heads) > 0x7fffff00LL)
         return fail(FLOCK_EUNSUPPORTED, "batch of more than 2^31 - 256 rows of queries and shared heads");
     const DeviceInfo *dev = nullptr;
-    const flock::TrackPlan plan = flock::plan_track_attention(n_tracks, total, max_pages, q_heads, kv_heads, head_dim, cap > 0.0f, device_cus());
+    const flock::TrackPlan plan = flock::plan_track_attention(n_tracks, total, max_pages, q_heads, kv_heads, device_cus());
     st = check_workgroups(plan.slots * kv_heads * plan.splits);
     if (st != FLOCK_OK) return st;
     st = device_info(&dev);

@@ -401,7 +401,7 @@ struct TrackPlan {
     int32_t split_pages;  // ... and how many pages each takes
 };
 TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads, int32_t kv_heads,
-                               int32_t dim, bool capped, int n_cus);
+                               int n_cus);
 size_t track_attention_workspace_bytes(const TrackPlan &p, int32_t total, int32_t q_heads, int32_t dim);
 hipError_t launch_track_attention(TrackAttentionArgs a, int32_t dtype, const TrackPlan &p, void *workspace,
                                   hipStream_t stream);

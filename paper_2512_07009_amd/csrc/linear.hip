@@ -861,7 +861,7 @@ template <typename T>
 int64_t stay_workgroups(const LinearArgs &a, int n_cus) {
     const int64_t per_xcd = n_cus / 8, columns = (a.outputs + kStayOutputs - 1) / kStayOutputs;
     if (a.width <= kStayWidth / 2 || a.width > kStayWidth || columns > per_xcd) return 0;
-    if (a.x_stride >= 1 << 24 || a.y_stride >= 1 << 24) return 0;  // (places in 32 bits)
+    if (a.y_stride >= 1 << 24) return 0;  // (places in 32 bits; x's stride is below that in any call)
     if (!whole_lines<T>(a)) return 0;
     const int64_t groups = per_xcd / columns;
     if (8 * groups * columns < 7 * per_xcd) return 0;

@@ -773,7 +773,7 @@ hipError_t launch_type(const TrackAttentionArgs &a, const TrackPlan &p, hipStrea
 }  // namespace
 
 TrackPlan plan_track_attention(int32_t n_tracks, int32_t total, int32_t max_pages, int32_t q_heads, int32_t kv_heads,
-                               int32_t dim, bool capped, int n_cus) {
+                               int n_cus) {
     TrackPlan p;
     const int group = q_heads / kv_heads;
     // 128 rows a workgroup where tracks have more on average and those fill the card: 64 tracks

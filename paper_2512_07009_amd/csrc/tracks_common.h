@@ -18,8 +18,6 @@ constexpr int kPage = kTrackPage;
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ constexpr int token_at(int place) { return 16 * (place % 16 / 4) + 4 * (place / 16) + place % 4; }
-
 // One track's part of the batch: `n` rows, which are the last of its `length` tokens.
 struct Track {
     int32_t index, row0, n, length;
