@@ -939,6 +939,8 @@ def attention_tracks(q: torch.Tensor, cache: TrackCache, offsets: torch.Tensor, 
     total, heads, dim = q.shape
     if dim != cache.head_dim or q.get_device() != cache.index:
         raise ValueError(f"q must be [T, heads, {cache.head_dim}] on the cache's device")
+    if not 0 <= window <= _MOST:
+        raise ValueError(f"window = {window} outside 0..2^31 - 1")
     rows = _tracks(cache, offsets, table, lengths, total)
     dev = q.device
     if out is None:

@@ -525,6 +525,15 @@ def test_refusals():
                             int32([[0]]), int32([1]))
 
 
+@pytest.mark.parametrize("window", [-1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 32 + 5])
+def test_windows_beyond_32_bits_are_refused(window):
+    """(Five tokens are what the low 32 bits of two of them say.)"""
+    c = flock.TrackCache.empty(1, 1, 64)
+    q = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="window"):
+        flock.attention_tracks(q, c, int32([0, 1]), int32([[0]]), int32([1]), window=window)
+
+
 def test_empty_calls():
     c = flock.TrackCache.empty(2, 1, 64)
     none = torch.zeros(0, 1, 64, dtype=torch.bfloat16, device="cuda")
