@@ -13,9 +13,9 @@
 // registers, a page ahead of the products.
 //
 // A query a track is bound by memory: 24 tracks of 27000 tokens, heads of 128, 67 us and 6
-// for the join (326 MB, 4.9 TB/s), 2000 of 1800 173 (5.3); 500 of 0 to 5400 82 (337 MB,
+// for the join (326 MB, 4.9 TB/s), 2000 of 1800 173 (5.3); 500 of 0 to 5400 83 (337 MB,
 // 4.1), where the longest tracks' workgroups end last.  96 tracks of 0 to 9000 with some
-// 15 queries each and a cap 90 us: vector instructions, 77% of the time.  Tried: keys to
+// 15 queries each and a cap 86 us: vector instructions, 76% of the time.  Tried: keys to
 // float16, four tiles of rows a wave (96 clips 95 -> 232, registers), eight waves (500
 // tracks 81 -> 75, but 24 long 67 -> 89 and 2000 ragged ones 94 -> 103), values shared
 // by the waves in LDS (no faster).
@@ -28,14 +28,15 @@
 // largest dimension times the sum of |k| / 65024 at most.  That spares a lane 80 instructions
 // a page to convert keys to float16 (of some 350).  Scores are transposed, S^T = K Q^T: a lane
 // holds 16 tokens of one row, four of each 16, which is the order in which the product with
-// the values takes its weights.  Values lie in pages so that a lane's 16 bytes are the factors of two such
-// products (16 x 16 x 32); they go to float16, which holds them exactly.  Weights are
-// rounded to float16 after they were summed in 32 bits, and carry the page's scale relative
-// to the largest so far while that is within 2^-4 of it: those from 2^-17 of the row's largest
-// on keep float16's 11 bits, others are off by 2^-28 of it at most.  Pages of smaller scales
-// are multiplied without them and join the sums in 32 bits, so that a page of large values
-// takes no digits of others, whether or not a row gives it any weight (500 tracks 82.7 -> 83.6
-// us, 96 clips 90.2 -> 91.3; with a first page of 10^6 times the others' values 84.8 and 92.8).
+// the values takes its weights.  Values lie in pages so that a lane's 16 bytes are the factors
+// of two such products (16 x 16 x 32); they go to float16, which holds them exactly.
+//
+// Weights are rounded to float16 after they were summed in 32 bits, and carry the page's scale
+// relative to the largest so far while that is within 2^-4 of it: those from 2^-17 of the row's
+// largest on keep float16's 11 bits, others are off by 2^-28 of it at most.  Pages of smaller
+// scales are multiplied without them and join the sums in 32 bits, so that a page of large
+// values takes no digits of others, whether or not a row gives it any weight (500 tracks 82.8
+// -> 83.5 us; with a first page of 10^6 times the others' values 84.5, 96 clips 86.4 -> 88.5).
 
 #include "attention_common.h"
 #include "tracks_common.h"
@@ -411,7 +412,7 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
 // Products are 32 x 32 x 32 (8 bits) and 32 x 32 x 16: a lane holds 32 tokens of one row, and
 // of a dimension it takes the two parts that hold the same tokens.  Bound by vector
 // instructions, some seven a score and 80 a page to convert its values: 64 tracks of 1000
-// with 1000 queries of 4 heads 180 us (366 TFLOP/s), with 16 rows a workgroup 359.
+// with 1000 queries, 4 heads on each of 2, 167 us (392 TFLOP/s), with 16 rows a workgroup 359.
 // ---------------------------------------------------------------------------
 
 constexpr int kAhead = 3, kBuffers = kAhead + 1;

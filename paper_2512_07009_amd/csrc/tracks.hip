@@ -13,8 +13,8 @@
 // The time is that of a workgroup's trips to memory one after the other (the track, its
 // page, the rows with their positions and the page's scale), not of bytes: as many
 // workgroups run beside each other as LDS allows.  With a token or a few a track one is
-// a wave; clips take four.  500 tracks of a token, 2 kv heads of 64: 7.8 us for 7 MB;
-// 700 clips of up to 120, 4 heads of 128: 76 us for 200 MB, vector instructions 60%.
+// a wave; clips take four.  500 tracks of a token, 2 kv heads of 64: 8 us for 7 MB;
+// 700 clips of up to 120, 4 heads of 128: 78 us for 200 MB, vector instructions 68%.
 // Rows in LDS as 32 bits left room for half the workgroups (99 us), keys turned twice
 // took 83, and four tokens of values a lane at a time 88 for 82.
 

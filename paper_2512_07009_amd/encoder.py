@@ -235,7 +235,8 @@ class ServedBlock:
     @torch.no_grad()
     def __call__(self, x, cache: TrackCache, offsets, table, lengths, xy, time=None, window: int = 0):
         """x [T, width], the rows of each track by offsets (int32 [tracks + 1]), which
-        become its last tokens; table and lengths as for append_tracks."""
+        become its last tokens; table and lengths as for append_tracks.  Rows that belong
+        to no track, or to one that is passed over, are of no meaning in what is returned."""
         hq, hk, dim = self.heads
         if x.dtype != self.dtype:
             raise ValueError(f"features of {x.dtype}: the block is in {self.dtype}")
