@@ -15,7 +15,7 @@
 // A query a track is bound by memory: 24 tracks of 27000 tokens, heads of 128, 67 us and 6
 // for the join (326 MB, 4.9 TB/s), 2000 of 1800 173 (5.3); 500 of 0 to 5400 83 (337 MB,
 // 4.1), where the longest tracks' workgroups end last.  96 tracks of 0 to 9000 with some
-// 15 queries each and a cap 86 us: vector instructions, 76% of the time.  Tried: keys to
+// 15 queries each and a cap 87 us: vector instructions, 76% of the time.  Tried: keys to
 // float16, four tiles of rows a wave (96 clips 95 -> 232, registers), eight waves (500
 // tracks 81 -> 75, but 24 long 67 -> 89 and 2000 ragged ones 94 -> 103), values shared
 // by the waves in LDS (no faster).
@@ -36,7 +36,7 @@
 // largest on keep float16's 11 bits, others are off by 2^-28 of it at most.  Pages of smaller
 // scales are multiplied without them and join the sums in 32 bits, so that a page of large
 // values takes no digits of others, whether or not a row gives it any weight (500 tracks 82.8
-// -> 83.5 us; with a first page of 10^6 times the others' values 84.5, 96 clips 86.4 -> 88.5).
+// -> 83.5 us; with a first page of 10^6 times the others' values 84.5, 96 clips 86.8 -> 89.7).
 
 #include "attention_common.h"
 #include "tracks_common.h"
@@ -59,6 +59,9 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 16, kManyRows = 128;  // of a workgroup, 2^4 and 2^7
 constexpr float kSlack = 8.0f;    // scores above the shift by less are left there
+// From shifts of this size on scores are taken from them before anything is added: 32 bits hold a
+// smaller one's difference from its shift, the level and the lift to 2^-3, which float16 has room for.
+constexpr float kLarge = 0x1p20f;
 // Weights are kept 2^7 times as large, 2^15 at most, so that float16's digits go that much further
 // down; what leaves a workgroup is kUnlift of it.
 constexpr float kLift = 7.0f, kUnlift = 0x1p-7f;
@@ -89,6 +92,15 @@ __device__ __forceinline__ V over_parts(V x, F &&f) {
     x = f(value(p[0]), value(p[1]));
     const auto q = __builtin_amdgcn_permlane32_swap(bits(x), bits(x), false, false);
     return f(value(q[0]), value(q[1]));
+}
+
+// A score's distance from the shift.  The product is rounded by itself, as the one that the
+// shift was made of, so that the largest score's distance is 0; one above it stays within what
+// is left there (and NaN stays).
+__device__ __forceinline__ float distance(float product, float factor, float shift) {
+#pragma clang fp contract(off)
+    const float score = product * factor, x = score - shift;
+    return x > kSlack ? kSlack : x;
 }
 
 // What a workgroup, or the one that joins, works on.
@@ -266,6 +278,7 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
     };
 
     float unit = 0.0f;  // largest scale of values so far
+    bool large = false;  // some row's shift is
     // tokens that every row sees, of pages that lie within
     const int all_lo = a.window ? max(it.at.length - it.at.n + (it.row0 + it.rows - 1) / a.group, 0) - a.window : -1;
     const int all_own = it.at.length - it.at.n + it.row0 / a.group;
@@ -320,8 +333,6 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
 #pragma unroll
         for (int e = 1; e < 16; ++e) most = fmaxf(most, s[e]);
         most = over_parts(most, [](float u, float v) { return fmaxf(u, v); }) * f;
-        // values that are not finite: none for rows that see the page, whatever its weight
-        if (v_scale != v_scale && most != -INFINITY) w.total = NAN;
         float keep = keep_v;
         if (__any(most > w.shift + kSlack || (w.shift == -INFINITY && most > w.shift))) {
             const float now = fmaxf(w.shift, most);
@@ -329,13 +340,21 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
             w.total *= less;
             keep *= less;
             w.shift = now;
+            large = __any(fabsf(now) > kLarge && now != -INFINITY);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) w.acc[b] *= keep;
         } else if (keep_v != 1.0f) {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) w.acc[b] *= keep;
         }
-        const float base = (w.shift == -INFINITY ? 0.0f : w.shift) - values.level;
+        float from = w.shift == -INFINITY ? 0.0f : w.shift;
+        if (large) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = distance(s[e], f, from);
+            f = 1.0f;
+            from = 0.0f;
+        }
+        const float base = from - values.level;
         float sum = 0.0f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -344,6 +363,11 @@ __global__ void __launch_bounds__(64 * WAVES, DI > 1 ? 2 : CAP == kNoCap ? 4 : 3
             weights[e >> 3][e & 7] = (half_t)x;
         }
         w.total += sum * values.back;
+        if (v_scale != v_scale) {  // values that are not finite: none for rows that see the page, whatever its weight
+            // (a branch, which keeps the values' registers apart from the scores' where those are fewest)
+            if (CAP == kNoCap) asm volatile("" ::: "memory");
+            if (most != -INFINITY) w.total = NAN;
+        }
         const auto product = [&](int b, f32x4 to) {
             const f16x8 v0 = to_half(vr[b][0], vr[b][1]), v1 = to_half(vr[b][2], vr[b][3]);
             to = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, weights[0], to, 0, 0, 0);
@@ -544,6 +568,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
 
     f32x16 acc[kBlocks] = {};
     float shift = -INFINITY, total = 0.0f, unit = 0.0f;
+    bool large = false;
     static_assert(kAhead == 3, "the pages ahead have a name each");
     Ahead now = load(), second = load(), third = load();
     int buffer = 0;
@@ -612,13 +637,23 @@ __global__ void __launch_bounds__(kThreads, DP == 64 ? 3 : 2) track_rows_kernel(
                 total *= less;
                 keep *= less;
                 shift = now;
+                large = __any(fabsf(now) > kLarge && now != -INFINITY);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
             } else if (keep_v != 1.0f) {
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) acc[b] *= keep;
             }
-            const float base = (shift == -INFINITY ? 0.0f : shift) - values.level;
+            float from = shift == -INFINITY ? 0.0f : shift;
+            if (large) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[t][e] = distance(s[t][e], g, from);
+                g = 1.0f;
+                from = 0.0f;
+            }
+            const float base = from - values.level;
             float sum = 0.0f;
             f16x8 weights[4];
 #pragma unroll

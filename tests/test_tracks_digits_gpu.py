@@ -196,3 +196,36 @@ def test_pages_that_are_not_finite_and_far_below(lengths, queries, heads, at, wi
         seen &= places - window < at * PAGE + PAGE - 1
     got = flock.attention_tracks(q.bfloat16().cuda(), cuda(c), int32(offsets), table.cuda(), int32(lengths), window=window).cpu()
     assert got[seen].isnan().all() and got[~seen].isfinite().all()
+
+
+@pytest.mark.parametrize("power", [20, 23, 25, 27, 30, 40, 90])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("lengths,queries,heads,dim", [([300, 70], [3, 20], 1, 64), ([9000], [1], 2, 128), ([300] * 40, [150] * 40, 8, 64),
+                                                       ([280] * 40, [200] * 40, 8, 128), ([70] * 3200, [1] * 3200, 1, 32)])
+@pytest.mark.parametrize("cap", [0.0, 2.0 ** 95])
+def test_scores_far_beyond_whole_numbers(power, sign, lengths, queries, heads, dim, cap):
+    """Scores of up to 2^power, whose steps in 32 bits are far above 1: the largest takes all the weight, and nothing else comes."""
+    gen = torch.Generator().manual_seed(18)
+    each = [(n + PAGE - 1) // PAGE for n in lengths]
+    c = pool(gen, max(each), heads, dim)
+    c[0].zero_()
+    # every token in turn has a largest before it, or is one: others are 2^power / 64 below
+    k = torch.randint(-60, 60, (heads, max(each) * PAGE), generator=gen)
+    for at, most in ((0, 64), (40, 70), (100, 84), (250, 100), (8000, 126)):
+        k[:, at:at + 1] = most
+    c[0][:, :, :, 0] = (sign * k).view(heads, max(each), PAGE).transpose(0, 1)
+    c[2].fill_(1.0)
+    table = torch.full((len(each), max(each)), -1, dtype=torch.int32)
+    for t, n in enumerate(each):
+        table[t, :n] = torch.arange(n)      # (all tracks read the same pages)
+    offsets = offsets_of(queries)
+    q = torch.zeros(offsets[-1], 2 * heads, dim)
+    q[:, :, 0] = sign
+    got = flock.attention_tracks(q.bfloat16().cuda(), cuda(c), int32(offsets), table.cuda(), int32(lengths), scale=2.0 ** power / 127,
+                                 cap=cap)
+    v = (ref.in_order(c[1]).double() * c[3].double()[:, :, None, None]).transpose(0, 1).reshape(heads, -1, dim)
+    best = k.cummax(1).indices
+    rows = [n - m + i for n, m in zip(lengths, queries) for i in range(m)]
+    want = v[torch.arange(heads)[None], best[:, rows].T].repeat_interleave(2, 1)
+    # its weight is the total, both from the same 32 bits, and 2^-11 in float16
+    assert ((got.cpu().double() - want).abs() <= (UNIT[torch.bfloat16] + 2.0 ** -10) * want.abs()).all()
