@@ -705,7 +705,8 @@ flock_status append_tracks(int32_t dtype, const void *new_k, int64_t new_k_strid
  * dimension is rounded by at most 1/64000 of its head's largest (a head whose largest is
  * below 2^-100 is zeros, one that is not finite gives NaN), and weights are rounded to 11
  * bits for the product with v, those below 2^-17 of their row's largest to 2^-28 of it,
- * whatever the scales of other pages (up to 2^100 apart).
+ * whatever the scales of other pages (up to 2^100 apart).  Weights times values are summed
+ * before they are divided by the weights' sum, so those sums have to be below 2^128.
  * Scales are >= 0, or NaN: then what sees the page is NaN.
  *
  * Arguments:

@@ -15,7 +15,7 @@
 // A query a track is bound by memory: 24 tracks of 27000 tokens, heads of 128, 67 us and 6
 // for the join (326 MB, 4.9 TB/s), 2000 of 1800 173 (5.3); 500 of 0 to 5400 83 (337 MB,
 // 4.1), where the longest tracks' workgroups end last.  96 tracks of 0 to 9000 with some
-// 15 queries each and a cap 87 us: vector instructions, 76% of the time.  Tried: keys to
+// 15 queries each and a cap 87 us: vector instructions, 75% of the time.  Tried: keys to
 // float16, four tiles of rows a wave (96 clips 95 -> 232, registers), eight waves (500
 // tracks 81 -> 75, but 24 long 67 -> 89 and 2000 ragged ones 94 -> 103), values shared
 // by the waves in LDS (no faster).
